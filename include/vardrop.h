@@ -9,13 +9,17 @@
  *   vardrop_attn_fwd  gather of the kept Q/K/V variate tokens + scaled dot-product attention (Eq. 3)
  *   vardrop_attn_bwd  derivative of Eq. 3 over the kept tokens, gradients scattered to the full layout
  *
+ * Around the attention, for the layer that it sits in and the end of a training step:
+ *   vardrop_norm_fwd, _bwd          norms before and after a block with its gate and residual scale
+ *   vardrop_grad_clip               global gradient norm over many tensors, and clipping
+ *
  * Conventions shared by every entry point
  *   - Pointers named in the argument lists are DEVICE pointers unless the comment says "host".
  *     Configuration structs are host pointers and are read before the call returns.
  *   - The caller owns every buffer, including the workspace `ws` (size from the matching
  *     *_workspace_bytes query).  The library never allocates or frees device memory, never
  *     synchronises the device and launches only on `stream` (a cudaStream_t passed as void*).
- *   - Device pointers must be 16-byte aligned.
+ *   - Device pointers must be 16-byte aligned (but for those of vardrop_grad_clip's tensors).
  *   - The return value is a vardrop_status.  Problems found on the host (bad argument, unsupported
  *     shape, short workspace, failed launch) are returned at once and nothing is launched.  Problems
  *     found on the device (non-finite amplitude, a bounded wait that ran out) are written to the
@@ -278,6 +282,71 @@ typedef struct {
 size_t vardrop_pearson_workspace_bytes(const vardrop_pearson_cfg* cfg);
 int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* max_rho, int32_t* n_above, void* ws,
                         size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Norms before and after a block, with the block's gate and residual scale (no counterpart in the paper, which takes its encoder's
+ * layers as they are).  With x the residual stream, y what the block (attention, feed-forward) gave for its tokens, per token:
+ *   h = res_scale x + gate o N_post(y)        the stream behind the block
+ *   u = N_pre(h)                              what the next block reads
+ *   N(t) = (t - mean) r o w + b (layer) or t r o w (rms),  r = 1 / sqrt(mean((t - mean)^2) + eps), mean 0 for rms
+ * With a selection, y, h, u hold the kept tokens and x every one: row i of instance b has x[b, sel_idx[s(b), i]], the gather that vardrop_attn_fwd makes of q, k, v.
+ *
+ * cfg (host)  B, N, C (C <= 8192; B N < 2^31); dtype of x, y, h, u and their gradients: 0 bf16, 1 fp16, 2 fp32; pre and post: 0 none, 1 rms, 2 layer;
+ *             gate_rows 0 (no gate), 1 or B; S as in vardrop_attn_cfg; res_scale and eps >= 0 finite.
+ * x           [B, N, C].
+ * y           [B, N, C], rows below n_sel of the instance are read; NULL: h = res_scale x (then post and gate_rows must be 0).
+ * gate        [gate_rows, C] fp32.     w_post, b_post, w_pre, b_pre   [C] fp32, NULL: 1 and 0; b only with the kind 2, none with the kind 0.
+ * sel_idx, n_sel, inv_idx  vardrop_select's outputs, or all NULL.
+ * h           [B, N, C] out; may be NULL (not wanted).
+ * u           [B, N, C] out; NULL exactly when pre = 0.
+ * stats       [B, N, 4] fp32 out: mean and r of N_post(y), mean and r of N_pre(h); may be NULL where no backward call follows.
+ * Rows from n_sel on are left as they are.  x and h, or y and u, may be the same buffer where there is no selection.
+ * Sums in fp32, the mean ahead of the squares (two passes over registers), outputs rounded once.
+ *
+ * Backward: d_h (NULL: 0) and d_u (NULL exactly when pre = 0) are the gradients of h and u, x, y and the parameters as given to the forward call, stats its output.
+ * dx          [B, N, C] out, full layout: rows of dropped tokens are written as zeros.
+ * dy          [B, N, C] out, NULL exactly when y is; rows from n_sel on are left as they are.
+ * d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre   fp32, shaped as the parameters; each may be NULL (not wanted), and has to be where the forward has no such parameter.  They are written, not added to.
+ *             Sums over tokens are taken in fp32 in a fixed order (bit-reproducible).
+ * ws          scratch of vardrop_norm_workspace_bytes.
+ * dx and d_h, dy and d_u may be the same buffer where there is no selection.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t B, N, C, dtype, pre, post, gate_rows, S;
+    float res_scale, eps;
+} vardrop_norm_cfg;
+
+int vardrop_norm_fwd(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const float* b_pre,
+                     const int32_t* sel_idx, const int32_t* n_sel, const vardrop_norm_cfg* cfg, void* h, void* u, float* stats, void* stream);
+size_t vardrop_norm_workspace_bytes(const vardrop_norm_cfg* cfg);
+int vardrop_norm_bwd(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const int32_t* sel_idx,
+                     const int32_t* n_sel, const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg* cfg, void* dx, void* dy,
+                     float* d_gate, float* d_w_post, float* d_b_post, float* d_w_pre, float* d_b_pre, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Global gradient norm over many tensors, and clipping (the end of a training step; no counterpart in the paper):
+ *   norm = sqrt(sum over all tensors and elements of g^2);   out = g min(1, max_norm / (norm + eps))
+ * Squares and sums in fp64, in a fixed order (bit-reproducible); products rounded once to the tensor's type.
+ *
+ * tensors     (host) [count] of device pointers, element counts (>= 0) and types (0 bf16, 1 fp16, 2 fp32); read before the call returns.  `in` and `out` need the
+ *             alignment of their element only; out = in clips in place, otherwise they must not overlap.  count <= 16384.
+ * cfg (host)  max_norm: 0 takes the norm only (no `out` is touched); eps >= 0.
+ * norm        [1] fp32 out.
+ * ws          scratch of vardrop_grad_clip_workspace_bytes.
+ * Device status: VARDROP_ERR_NONFINITE when the norm is not finite; `out` then gets the gradients as they are.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t n;
+    int32_t dtype, reserved;
+} vardrop_tensor;
+typedef struct {
+    float max_norm, eps;
+} vardrop_clip_cfg;
+
+size_t vardrop_grad_clip_workspace_bytes(void);
+int vardrop_grad_clip(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg* cfg, float* norm, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -43,6 +43,19 @@ class PearsonCfg(C.Structure):
     _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("L", C.c_int32), ("threshold", C.c_float)]
 
 
+class NormCfg(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("pre", C.c_int32), ("post", C.c_int32), ("gate_rows", C.c_int32), ("S", C.c_int32),
+                ("res_scale", C.c_float), ("eps", C.c_float)]
+
+
+class ClipCfg(C.Structure):
+    _fields_ = [("max_norm", C.c_float), ("eps", C.c_float)]
+
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+
+
 class VardropError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -52,7 +65,8 @@ class VardropError(RuntimeError):
 
 EXPORTS = ("vardrop_status_string", "vardrop_last_error", "vardrop_version", "vardrop_ws_status", "vardrop_probe_bounded_wait", "vardrop_hash_workspace_bytes", "vardrop_hash",
            "vardrop_select_workspace_bytes", "vardrop_select", "vardrop_select_static", "vardrop_gather_rows", "vardrop_attn_workspace_bytes", "vardrop_attn_fwd",
-           "vardrop_attn_bwd", "vardrop_pearson_workspace_bytes", "vardrop_pearson_max", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
+           "vardrop_attn_bwd", "vardrop_pearson_workspace_bytes", "vardrop_pearson_max", "vardrop_norm_fwd", "vardrop_norm_workspace_bytes", "vardrop_norm_bwd",
+           "vardrop_grad_clip_workspace_bytes", "vardrop_grad_clip", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
            "vardrop_profile_kernel_name", "vardrop_profile_read")
 
 
@@ -67,7 +81,7 @@ def load() -> C.CDLL:
             getattr(lib, name).restype = C.c_char_p
         lib.vardrop_status_string.argtypes = [C.c_int]
         for name in ("vardrop_hash_workspace_bytes", "vardrop_select_workspace_bytes", "vardrop_attn_workspace_bytes",
-                     "vardrop_pearson_workspace_bytes"):
+                     "vardrop_pearson_workspace_bytes", "vardrop_norm_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
             getattr(lib, name).argtypes = [C.c_void_p]
         lib.vardrop_ws_status.restype = C.c_int
@@ -88,6 +102,14 @@ def load() -> C.CDLL:
         lib.vardrop_attn_bwd.argtypes = [C.c_void_p] * 14 + [C.c_size_t, C.c_void_p]
         lib.vardrop_pearson_max.restype = C.c_int
         lib.vardrop_pearson_max.argtypes = [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_norm_fwd.restype = C.c_int
+        lib.vardrop_norm_fwd.argtypes = [C.c_void_p] * 14
+        lib.vardrop_norm_bwd.restype = C.c_int
+        lib.vardrop_norm_bwd.argtypes = [C.c_void_p] * 21 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_grad_clip_workspace_bytes.restype = C.c_size_t
+        lib.vardrop_grad_clip_workspace_bytes.argtypes = []
+        lib.vardrop_grad_clip.restype = C.c_int
+        lib.vardrop_grad_clip.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.vardrop_launch_count.restype = C.c_longlong
         lib.vardrop_profile_kernel_name.restype = C.c_char_p
         lib.vardrop_profile_kernel_name.argtypes = [C.c_int]
@@ -171,6 +193,28 @@ def vardrop_pearson_workspace_bytes(cfg: PearsonCfg) -> int:
 
 def vardrop_pearson_max(x, cfg: PearsonCfg, max_rho, n_above, ws) -> None:
     _check((_marshal or _load_marshal()).pearson_max(x, cfg, max_rho, n_above, ws), "vardrop_pearson_max")
+
+
+def vardrop_norm_fwd(x, y, gate, w_post, b_post, w_pre, b_pre, sel_idx, n_sel, cfg: NormCfg, h, u, stats) -> None:
+    _check((_marshal or _load_marshal()).norm_fwd(x, y, gate, w_post, b_post, w_pre, b_pre, sel_idx, n_sel, cfg, h, u, stats), "vardrop_norm_fwd")
+
+
+def vardrop_norm_workspace_bytes(cfg: NormCfg) -> int:
+    return int(load().vardrop_norm_workspace_bytes(C.byref(cfg)))
+
+
+def vardrop_norm_bwd(x, y, gate, w_post, b_post, w_pre, sel_idx, n_sel, inv_idx, stats, d_h, d_u, cfg: NormCfg, dx, dy, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, ws) -> None:
+    _check((_marshal or _load_marshal()).norm_bwd(x, y, gate, w_post, b_post, w_pre, sel_idx, n_sel, inv_idx, stats, d_h, d_u, cfg, dx, dy, d_gate, d_w_post, d_b_post, d_w_pre,
+                                                  d_b_pre, ws), "vardrop_norm_bwd")
+
+
+def vardrop_grad_clip_workspace_bytes() -> int:
+    return int(load().vardrop_grad_clip_workspace_bytes())
+
+
+def vardrop_grad_clip(grads, cfg: ClipCfg, outs, norm, ws) -> None:
+    """`grads` and `outs`: lists (or tuples) of tensors, bf16, fp16 and fp32 mixed; `outs` None clips in place."""
+    _check((_marshal or _load_marshal()).grad_clip(grads, cfg, outs, norm, ws), "vardrop_grad_clip")
 
 
 def vardrop_launch_count() -> int:

@@ -12,7 +12,8 @@ namespace vardrop {
 // Kernel identities for the launch counter and the optional per-kernel event timer (vardrop_profile_*).
 enum KernelId {
     K_HASH = 0, K_SELECT_SMALL, K_SELECT_COUNT, K_SELECT_GROUP, K_SELECT_SAMPLE, K_ATTN_FWD, K_BWD_PREP, K_ATTN_BWD, K_BWD_CONVERT, K_PEARSON_NORM, K_PEARSON_MAX, K_GATHER_ROWS,
-    K_SELECT_PLACE, K_SELECT_CLUSTER, K_COUNT
+    K_SELECT_PLACE, K_SELECT_CLUSTER, K_NORM_FWD, K_NORM_BWD, K_NORM_PARAMS, K_GRAD_NORM, K_GRAD_SCALE,
+    K_COUNT
 };
 // Wrap a kernel launch: counts it and, when the timer is armed, brackets it with a pair of CUDA events on `stream`.
 struct LaunchScope {
@@ -75,5 +76,19 @@ int attn_bwd_launch(const void* q, const void* k, const void* v, const void* o, 
                     void* dk, void* dv, void* ws, cudaStream_t stream);
 int attn_bwd_many_launch(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o, const int32_t* sel_idx,
                          const int32_t* n_sel, const int32_t* inv_idx, const vardrop_attn_cfg& cfg, void* dq, void* dk, void* dv, void* ws, cudaStream_t stream);
+
+// norm.cu
+int norm_validate(const vardrop_norm_cfg& cfg);
+size_t norm_workspace_bytes(const vardrop_norm_cfg& cfg);
+int norm_fwd_launch(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const float* b_pre, const int32_t* sel_idx,
+                    const int32_t* n_sel, const vardrop_norm_cfg& cfg, void* h, void* u, float* stats, cudaStream_t stream);
+int norm_bwd_launch(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const int32_t* sel_idx, const int32_t* n_sel,
+                    const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg& cfg, void* dx, void* dy, float* d_gate, float* d_w_post,
+                    float* d_b_post, float* d_w_pre, float* d_b_pre, void* ws, cudaStream_t stream);
+
+// grad_clip.cu
+size_t grad_clip_workspace_bytes();
+int grad_clip_validate(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg& cfg);
+int grad_clip_launch(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg& cfg, float* norm, void* ws, cudaStream_t stream);
 
 }  // namespace vardrop

@@ -5,10 +5,12 @@
 // object itself and the stream from PyTorch's current one.
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <vector>
 
 #include "../../include/vardrop.h"
 
@@ -35,6 +37,27 @@ struct Args {
         Py_XDECREF(v);
         ok = !PyErr_Occurred();
         return static_cast<T*>(p);
+    }
+    // The same for the operators around the attention, whose tensors come from many places: on the current device, contiguous (`kStrided`: with strides that the
+    // configuration gives; `kDense`: in any order of its dimensions), of the type, and with at least so many elements.  None: NULL.
+    enum Layout { kContiguous, kDense, kStrided };
+    template <typename T = void>
+    T* checked(int i, const char* name, at::ScalarType type, int64_t count, Layout layout = kContiguous) {
+        if (!ok || a[i] == Py_None) return nullptr;
+        if (!THPVariable_Check(a[i])) return refuse<T>("%s is not a tensor", name);
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (!t.is_cuda()) return refuse<T>("%s is not a CUDA tensor", name);
+        if (t.get_device() != c10::cuda::current_device()) return refuse<T>("%s is on another device than the current one", name);
+        if (t.scalar_type() != type) return refuse<T>("%s has another type than the call expects", name);
+        if (layout == kContiguous ? !t.is_contiguous() : layout == kDense && !t.is_non_overlapping_and_dense()) return refuse<T>("%s is not contiguous", name);
+        if (t.numel() < count) return refuse<T>("%s has fewer elements than the configuration says", name);
+        return static_cast<T*>(t.data_ptr());
+    }
+    template <typename T>
+    T* refuse(const char* text, const char* name) {
+        PyErr_Format(PyExc_ValueError, text, name);
+        ok = false;
+        return nullptr;
     }
     // a ctypes struct through the buffer protocol
     template <typename T>
@@ -163,9 +186,95 @@ PyObject* pearson_max(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+at::ScalarType type_of(int dtype) { return dtype == 2 ? at::kFloat : dtype == 1 ? at::kHalf : at::kBFloat16; }
+
+PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<13>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_norm_cfg>(9);
+        if (!g.ok) return nullptr;
+        const at::ScalarType ty = type_of(cfg->dtype);
+        const int64_t C = cfg->C, rows = static_cast<int64_t>(cfg->B) * cfg->N, all = rows * C, S = cfg->S > 1 ? cfg->S : 1;
+        const void* const x = g.checked(0, "x", ty, all);
+        const void* const y = g.checked(1, "y", ty, all);
+        const auto gate = g.checked<const float>(2, "gate", at::kFloat, cfg->gate_rows * C);
+        const auto w_post = g.checked<const float>(3, "w_post", at::kFloat, C), b_post = g.checked<const float>(4, "b_post", at::kFloat, C);
+        const auto w_pre = g.checked<const float>(5, "w_pre", at::kFloat, C), b_pre = g.checked<const float>(6, "b_pre", at::kFloat, C);
+        const auto sel = g.checked<const int32_t>(7, "sel_idx", at::kInt, S * cfg->N), n_sel = g.checked<const int32_t>(8, "n_sel", at::kInt, S);
+        void* const h = g.checked(10, "h", ty, all);
+        void* const u = g.checked(11, "u", ty, all);
+        const auto stats = g.checked<float>(12, "stats", at::kFloat, rows * 4);
+        return finish(g, [=](void* s) { return vardrop_norm_fwd(x, y, gate, w_post, b_post, w_pre, b_pre, sel, n_sel, cfg, h, u, stats, s); });
+    });
+}
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<21>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_norm_cfg>(12);
+        if (!g.ok) return nullptr;
+        const at::ScalarType ty = type_of(cfg->dtype);
+        const int64_t C = cfg->C, rows = static_cast<int64_t>(cfg->B) * cfg->N, all = rows * C, S = cfg->S > 1 ? cfg->S : 1;
+        const void* const x = g.checked(0, "x", ty, all);
+        const void* const y = g.checked(1, "y", ty, all);
+        const auto gate = g.checked<const float>(2, "gate", at::kFloat, cfg->gate_rows * C);
+        const auto w_post = g.checked<const float>(3, "w_post", at::kFloat, C), b_post = g.checked<const float>(4, "b_post", at::kFloat, C);
+        const auto w_pre = g.checked<const float>(5, "w_pre", at::kFloat, C);
+        const auto sel = g.checked<const int32_t>(6, "sel_idx", at::kInt, S * cfg->N), n_sel = g.checked<const int32_t>(7, "n_sel", at::kInt, S);
+        const auto inv = g.checked<const int32_t>(8, "inv_idx", at::kInt, S * cfg->N);
+        const auto stats = g.checked<const float>(9, "stats", at::kFloat, rows * 4);
+        const void* const d_h = g.checked(10, "d_h", ty, all);
+        const void* const d_u = g.checked(11, "d_u", ty, all);
+        void* const dx = g.checked(13, "dx", ty, all);
+        void* const dy = g.checked(14, "dy", ty, all);
+        const auto d_gate = g.checked<float>(15, "d_gate", at::kFloat, cfg->gate_rows * C);
+        const auto d_w_post = g.checked<float>(16, "d_w_post", at::kFloat, C), d_b_post = g.checked<float>(17, "d_b_post", at::kFloat, C);
+        const auto d_w_pre = g.checked<float>(18, "d_w_pre", at::kFloat, C), d_b_pre = g.checked<float>(19, "d_b_pre", at::kFloat, C);
+        void* const ws = g.checked(20, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(20) : 0;
+        return finish(g, [=](void* s) {
+            return vardrop_norm_bwd(x, y, gate, w_post, b_post, w_pre, sel, n_sel, inv, stats, d_h, d_u, cfg, dx, dy, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, ws, nb, s);
+        });
+    });
+}
+// the tensors of a list or tuple; `out` None: in place
+PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<5>(a, n, [&](Args& g) -> PyObject* {
+        PyObject* const in = a[0];
+        PyObject* const out = a[2];
+        const bool same = out == Py_None;
+        if (!(PyList_Check(in) || PyTuple_Check(in)) || !(same || PyList_Check(out) || PyTuple_Check(out)))
+            return PyErr_Format(PyExc_TypeError, "grads has to be a list or tuple of tensors, outs one or None");
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(in);
+        if (!same && PySequence_Fast_GET_SIZE(out) != count) return PyErr_Format(PyExc_ValueError, "%zd tensors and %zd outputs", count, PySequence_Fast_GET_SIZE(out));
+        std::vector<vardrop_tensor> table(static_cast<size_t>(count));
+        Args ins(PySequence_Fast_ITEMS(in)), outs(same ? PySequence_Fast_ITEMS(in) : PySequence_Fast_ITEMS(out));
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            if (!THPVariable_Check(ins.a[i])) return PyErr_Format(PyExc_ValueError, "a gradient is not a tensor");
+            const at::Tensor& t = THPVariable_Unpack(ins.a[i]);
+            const at::ScalarType ty = t.scalar_type();
+            vardrop_tensor& e = table[static_cast<size_t>(i)];
+            if (ty != at::kBFloat16 && ty != at::kHalf && ty != at::kFloat) return PyErr_Format(PyExc_ValueError, "a gradient is neither bf16, fp16 nor fp32");
+            e.in = ins.checked(static_cast<int>(i), "a gradient", ty, 0, Args::kDense);
+            e.n = t.numel();
+            e.out = same ? const_cast<void*>(e.in) : outs.checked(static_cast<int>(i), "an output", ty, e.n, Args::kDense);
+            e.dtype = ty == at::kFloat ? 2 : ty == at::kHalf ? 1 : 0;
+            e.reserved = 0;
+            if (!ins.ok || !outs.ok) return nullptr;
+            if (same) continue;
+            if (!THPVariable_Check(outs.a[i])) return PyErr_Format(PyExc_ValueError, "an output is not a tensor");
+            const at::Tensor& o = THPVariable_Unpack(outs.a[i]);
+            if (o.sizes() != t.sizes() || o.strides() != t.strides()) return PyErr_Format(PyExc_ValueError, "an output has another shape or other strides than its gradient");
+        }
+        const auto cfg = g.cfg<vardrop_clip_cfg>(1);
+        const auto norm = g.checked<float>(3, "norm", at::kFloat, 1);
+        void* const ws = g.checked(4, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(4) : 0;
+        const vardrop_tensor* const tensors = table.data();
+        return finish(g, [=](void* s) { return vardrop_grad_clip(tensors, static_cast<int32_t>(count), cfg, norm, ws, nb, s); });
+    });
+}
+
 #define VD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VD_METHOD(hash), VD_METHOD(select), VD_METHOD(select_static), VD_METHOD(gather_rows), VD_METHOD(attn_fwd), VD_METHOD(attn_bwd),
-                           VD_METHOD(pearson_max), {nullptr, nullptr, 0, nullptr}};
+                           VD_METHOD(pearson_max), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -49,7 +49,7 @@ std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_prof_events[K_COUNT];   // pa
 std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_prof_free;              // pairs ready for reuse
 const char* const g_kernel_names[K_COUNT] = {"hash_kernel", "select_small_kernel", "select_count_kernel", "select_group_kernel", "select_sample_kernel",
                                              "attn_fwd_kernel", "bwd_prep_kernel", "attn_bwd_kernel", "bwd_convert_kernel", "pearson_normalize_kernel",
-                                             "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel"};
+                                             "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel"};
 }  // namespace
 
 LaunchScope::LaunchScope(int id, cudaStream_t stream) : id_(id), stream_(stream), stop_(nullptr) {
@@ -284,6 +284,82 @@ int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* m
     VD_CHECK(check_ptr(n_above, "n_above", true));
     VD_CHECK(check_ws(ws, ws_bytes, pearson_workspace_bytes(*cfg)));
     return pearson_launch(x, *cfg, max_rho, n_above, ws, static_cast<cudaStream_t>(stream));
+}
+
+// parameters and gradients that a configuration has no use for are refused, not ignored
+static int norm_params_check(const vardrop_norm_cfg& c, const void* y, const void* gate, const void* w_post, const void* b_post, const void* w_pre, const void* b_pre) {
+    if (!y && (c.post || c.gate_rows)) return fail(VARDROP_ERR_INVALID_ARG, "norm: y is NULL, but post=%d gate_rows=%d", c.post, c.gate_rows);
+    if ((gate != nullptr) != (c.gate_rows != 0)) return fail(VARDROP_ERR_INVALID_ARG, "norm: gate_rows=%d and gate %s", c.gate_rows, gate ? "given" : "NULL");
+    if ((w_post && c.post == 0) || (b_post && c.post != 2)) return fail(VARDROP_ERR_INVALID_ARG, "norm: post=%d has no such parameter", c.post);
+    if ((w_pre && c.pre == 0) || (b_pre && c.pre != 2)) return fail(VARDROP_ERR_INVALID_ARG, "norm: pre=%d has no such parameter", c.pre);
+    VD_CHECK(check_ptr(gate, "gate", false));
+    VD_CHECK(check_ptr(w_post, "w_post", false));
+    VD_CHECK(check_ptr(b_post, "b_post", false));
+    VD_CHECK(check_ptr(w_pre, "w_pre", false));
+    return check_ptr(b_pre, "b_pre", false);
+}
+
+int vardrop_norm_fwd(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const float* b_pre,
+                     const int32_t* sel_idx, const int32_t* n_sel, const vardrop_norm_cfg* cfg, void* h, void* u, float* stats, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(norm_validate(*cfg));
+    VD_CHECK(check_ptr(x, "x", true));
+    VD_CHECK(check_ptr(y, "y", false));
+    VD_CHECK(norm_params_check(*cfg, y, gate, w_post, b_post, w_pre, b_pre));
+    VD_CHECK(check_ptr(sel_idx, "sel_idx", false));
+    if (sel_idx) VD_CHECK(check_ptr(n_sel, "n_sel", true));
+    VD_CHECK(check_ptr(h, "h", false));
+    if ((u != nullptr) != (cfg->pre != 0)) return fail(VARDROP_ERR_INVALID_ARG, "norm: pre=%d and u %s", cfg->pre, u ? "given" : "NULL");
+    VD_CHECK(check_ptr(u, "u", false));
+    VD_CHECK(check_ptr(stats, "stats", false));
+    return norm_fwd_launch(x, y, gate, w_post, b_post, w_pre, b_pre, sel_idx, n_sel, *cfg, h, u, stats, static_cast<cudaStream_t>(stream));
+}
+
+size_t vardrop_norm_workspace_bytes(const vardrop_norm_cfg* cfg) {
+    if (!cfg || norm_validate(*cfg) != VARDROP_OK) return 0;
+    return norm_workspace_bytes(*cfg);
+}
+
+int vardrop_norm_bwd(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const int32_t* sel_idx,
+                     const int32_t* n_sel, const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg* cfg, void* dx, void* dy,
+                     float* d_gate, float* d_w_post, float* d_b_post, float* d_w_pre, float* d_b_pre, void* ws, size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(norm_validate(*cfg));
+    VD_CHECK(check_ptr(x, "x", true));
+    VD_CHECK(check_ptr(y, "y", false));
+    VD_CHECK(norm_params_check(*cfg, y, gate, w_post, b_post, w_pre, nullptr));
+    if ((d_gate && !cfg->gate_rows) || (d_w_post && !cfg->post) || (d_b_post && cfg->post != 2) || (d_w_pre && !cfg->pre) || (d_b_pre && cfg->pre != 2))
+        return fail(VARDROP_ERR_INVALID_ARG, "norm: gradient of a parameter that pre=%d post=%d gate_rows=%d does not have", cfg->pre, cfg->post, cfg->gate_rows);
+    VD_CHECK(check_ptr(sel_idx, "sel_idx", false));
+    if (sel_idx) {
+        VD_CHECK(check_ptr(n_sel, "n_sel", true));
+        VD_CHECK(check_ptr(inv_idx, "inv_idx", true));
+    }
+    VD_CHECK(check_ptr(stats, "stats", true));
+    VD_CHECK(check_ptr(d_h, "d_h", false));
+    if ((d_u != nullptr) != (cfg->pre != 0)) return fail(VARDROP_ERR_INVALID_ARG, "norm: pre=%d and d_u %s", cfg->pre, d_u ? "given" : "NULL");
+    VD_CHECK(check_ptr(d_u, "d_u", false));
+    VD_CHECK(check_ptr(dx, "dx", true));
+    if ((dy != nullptr) != (y != nullptr)) return fail(VARDROP_ERR_INVALID_ARG, "norm: y and dy have to be given, or NULL, together");
+    VD_CHECK(check_ptr(dy, "dy", false));
+    VD_CHECK(check_ptr(d_gate, "d_gate", false));
+    VD_CHECK(check_ptr(d_w_post, "d_w_post", false));
+    VD_CHECK(check_ptr(d_b_post, "d_b_post", false));
+    VD_CHECK(check_ptr(d_w_pre, "d_w_pre", false));
+    VD_CHECK(check_ptr(d_b_pre, "d_b_pre", false));
+    VD_CHECK(check_ws(ws, ws_bytes, norm_workspace_bytes(*cfg)));
+    return norm_bwd_launch(x, y, gate, w_post, b_post, w_pre, sel_idx, n_sel, inv_idx, stats, d_h, d_u, *cfg, dx, dy, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, ws,
+                           static_cast<cudaStream_t>(stream));
+}
+
+size_t vardrop_grad_clip_workspace_bytes(void) { return grad_clip_workspace_bytes(); }
+
+int vardrop_grad_clip(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg* cfg, float* norm, void* ws, size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(grad_clip_validate(tensors, count, *cfg));
+    VD_CHECK(check_ptr(norm, "norm", true));
+    VD_CHECK(check_ws(ws, ws_bytes, grad_clip_workspace_bytes()));
+    return grad_clip_launch(tensors, count, *cfg, norm, ws, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

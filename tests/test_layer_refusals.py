@@ -1,0 +1,78 @@
+"""Argument checks of the operators around the attention: they run ahead of any CUDA call, on a machine without a GPU too."""
+import ctypes as C
+
+import pytest
+
+from paper_2501_14183_b200 import binding as vd
+from paper_2501_14183_b200 import build as lib_build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    lib_build.build()
+    return vd.load()
+
+
+GOOD = 4096         # an address that is aligned; nothing is launched in these tests
+
+
+def norm_cfg(**kw):
+    return vd.NormCfg(*[{**dict(B=2, N=8, C=64, dtype=0, pre=1, post=1, gate_rows=1, S=0, res_scale=1.0, eps=1e-5), **kw}[n] for n, _ in vd.NormCfg._fields_])
+
+
+@pytest.mark.parametrize("kw,status", [(dict(B=0), 1), (dict(N=0), 1), (dict(C=0), 1), (dict(C=8193), 2), (dict(B=1 << 16, N=1 << 15, gate_rows=0), 2), (dict(dtype=3), 1), (dict(pre=3), 1),
+                                       (dict(post=-1), 1), (dict(gate_rows=3), 1), (dict(S=3), 1), (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1), (dict(eps=float("inf")), 1),
+                                       (dict(res_scale=float("inf")), 1), (dict(B=65535, gate_rows=65535), 2)])
+def test_norm_configurations(lib, kw, status):
+    cfg = norm_cfg(**kw)
+    assert lib.vardrop_norm_fwd(*[GOOD] * 6, None, None, None, C.byref(cfg), GOOD, GOOD, GOOD, None) == status
+    assert lib.vardrop_last_error().startswith(b"norm")
+    assert vd.vardrop_norm_workspace_bytes(cfg) == 0
+
+
+def test_norm_arguments(lib):
+    cfg = C.byref(norm_cfg())
+    names = ["x", "y", "gate", "w_post", "b_post", "w_pre", "b_pre", "sel_idx", "n_sel"]
+    outs = ["h", "u", "stats"]
+    usual = dict(x=GOOD, y=GOOD, gate=GOOD, w_post=GOOD, b_post=None, w_pre=GOOD, b_pre=None, sel_idx=None, n_sel=None, h=GOOD, u=GOOD, stats=GOOD)
+    for change in (dict(x=None), dict(y=None), dict(gate=None), dict(b_post=GOOD), dict(b_pre=GOOD), dict(u=None), dict(sel_idx=GOOD), dict(x=GOOD + 8), dict(w_pre=GOOD + 4), dict(h=GOOD + 2),
+                   dict(stats=GOOD + 4)):
+        a = {**usual, **change}
+        assert lib.vardrop_norm_fwd(*[a[n] for n in names], cfg, *[a[n] for n in outs], None) == vd.ERR_INVALID_ARG, change
+    assert lib.vardrop_norm_fwd(*[GOOD] * 9, None, *[GOOD] * 3, None) == vd.ERR_INVALID_ARG
+    need = vd.vardrop_norm_workspace_bytes(norm_cfg())
+    names = ["x", "y", "gate", "w_post", "b_post", "w_pre", "sel_idx", "n_sel", "inv_idx", "stats", "d_h", "d_u"]
+    outs = ["dx", "dy", "d_gate", "d_w_post", "d_b_post", "d_w_pre", "d_b_pre"]
+    usual = dict.fromkeys(names + outs, GOOD) | dict(b_post=None, sel_idx=None, n_sel=None, inv_idx=None, d_b_post=None, d_b_pre=None)
+    for change in (dict(x=None), dict(stats=None), dict(d_u=None), dict(dx=None), dict(dy=None), dict(y=None), dict(sel_idx=GOOD, n_sel=GOOD), dict(d_b_post=GOOD), dict(d_b_pre=GOOD),
+                   dict(d_gate=GOOD + 4), dict(gate=None)):
+        a = {**usual, **change}
+        assert lib.vardrop_norm_bwd(*[a[n] for n in names], cfg, *[a[n] for n in outs], GOOD, need, None) == vd.ERR_INVALID_ARG, change
+    a = usual
+    assert lib.vardrop_norm_bwd(*[a[n] for n in names], cfg, *[a[n] for n in outs], GOOD, need - 1, None) == vd.ERR_WORKSPACE
+    assert lib.vardrop_norm_bwd(*[a[n] for n in names], cfg, *[a[n] for n in outs], None, need, None) == vd.ERR_INVALID_ARG
+
+
+class Tensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+def test_clip_arguments(lib):
+    need = vd.vardrop_grad_clip_workspace_bytes()
+
+    def call(*tensors, count=None, max_norm=1.0, eps=0.0, norm=GOOD, nb=need):
+        table = (Tensor * max(1, len(tensors)))(*[Tensor(*t, 0) for t in tensors])
+        return lib.vardrop_grad_clip(table, len(tensors) if count is None else count, C.byref(vd.ClipCfg(max_norm, eps)), norm, GOOD, nb, None)
+
+    ok = (GOOD, GOOD, 10, 2)
+    assert call((GOOD, GOOD, 10, 3)) == call((GOOD, GOOD, -1, 2)) == call((None, GOOD, 10, 2)) == call((GOOD, None, 10, 2)) == vd.ERR_INVALID_ARG
+    assert call((GOOD + 2, GOOD, 10, 2)) == call((GOOD, GOOD + 2, 10, 2)) == call((GOOD + 1, GOOD + 1, 10, 0)) == vd.ERR_INVALID_ARG
+    assert call((GOOD, GOOD + 4, 10, 2)) == call((GOOD + 4, GOOD, 10, 2)) == vd.ERR_INVALID_ARG and b"overlaps" in lib.vardrop_last_error()
+    assert call(ok, max_norm=-1.0) == call(ok, max_norm=float("nan")) == call(ok, eps=-1.0) == call(ok, norm=None) == call(ok, count=-1) == vd.ERR_INVALID_ARG
+    assert call(*[ok] * 16385) == vd.ERR_UNSUPPORTED
+    assert call(ok, nb=need - 1) == vd.ERR_WORKSPACE
+
+
+def test_struct_layouts_match_header():
+    assert C.sizeof(vd.NormCfg) == 40 and vd.NormCfg.res_scale.offset == 32
+    assert C.sizeof(vd.ClipCfg) == 8 and C.sizeof(Tensor) == 32
