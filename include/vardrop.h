@@ -10,6 +10,7 @@
  *   vardrop_attn_bwd  derivative of Eq. 3 over the kept tokens, gradients scattered to the full layout
  *
  * Around the attention, for the layer that it sits in and the end of a training step:
+ *   vardrop_attn_packed_fwd, _bwd   attention over packed sequences of different lengths, causal or not, grouped heads
  *   vardrop_norm_fwd, _bwd          norms before and after a block with its gate and residual scale
  *   vardrop_grad_clip               global gradient norm over many tensors, and clipping
  *
@@ -282,6 +283,50 @@ typedef struct {
 size_t vardrop_pearson_workspace_bytes(const vardrop_pearson_cfg* cfg);
 int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* max_rho, int32_t* n_above, void* ws,
                         size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Attention over packed sequences (the paper has no counterpart: its token sets have one length for
+ * the batch).  T token rows hold n_seqs sequences one behind the other: kept sets of different sizes
+ * without padding (one selection per instance), windows of different lookbacks, causal along their steps.
+ * Query head h reads key head h / (Hq / Hkv).  For token i of a sequence and its tokens j (causal: j <= i):
+ *   S_ij = sm_scale q_i . k_j;   lse_i = log sum_j exp(S_ij);   o_i = sum_j exp(S_ij - lse_i) v_j
+ * bf16 operands, fp32 accumulation and softmax, P rounded to bf16 before the second product.
+ *
+ * The plan of a batch says where its sequences are and in which order their tiles are worked off.  It is made once from the offsets, on
+ * the device, and serves every call on that batch (all layers, forward and backward, any number of them at a time: calls only read it).
+ *
+ * cfg (host)  n_seqs >= 1; T >= 1 rows of the packed tensors (at most 2^24); Hq a multiple of Hkv; D = 32 or 64; sm_scale (0 selects 1/sqrt(D));
+ *             causal 0 or 1; element strides of q (sTq of a token, sHq of a head) and of both k and v (sTkv, sHkv), the head
+ *             dimension contiguous; the two of a tensor both 0 select the contiguous layout, otherwise each must be a multiple of 8 with sT >= sH >= D (views of
+ *             a fused projection [T, Hq + 2 Hkv, D]).  o, lse, d_o, dq, dk, dv are always contiguous.
+ * cu_seqlens  [n_seqs + 1] int32: row of each sequence's first token, then the row behind the last one's last; 0 <= cu_seqlens[0], not decreasing (an empty
+ *             sequence repeats its offset), at most T.  Device status in the plan: VARDROP_ERR_INVALID_ARG when they are not so; calls on such a plan
+ *             write nothing and report the same in their own workspace, as do calls with another n_seqs, T or causal than the plan's.
+ * plan        out, vardrop_packed_plan_bytes; its first int32 is a status word as that of a workspace, but written anew by every call.
+ * q           [T, Hq, D] bf16, k and v [T, Hkv, D] bf16, with the strides above.  What lies in rows that belong to no sequence does not matter.  Values that are not finite
+ *             stay in their sequence (there they may reach outputs of tokens that do not see them: the products run over whole tiles).
+ * o           [T, Hq, D] bf16 out; lse [Hq, T] fp32 out.  Rows that belong to no sequence are left as they are, here and in dq, dk, dv.
+ * d_o         [T, Hq, D] bf16, gradient of o.
+ * dq          [T, Hq, D], dk and dv [T, Hkv, D] bf16 out (dk, dv summed over the query heads of a key head, in fp32).
+ * ws          scratch of vardrop_attn_packed_workspace_bytes for the backward call; the forward call only needs its status word (256 bytes).  Nothing is kept
+ *             in it from one call to the next.
+ * dq is accumulated across key tiles by bulk fp32 reduce-adds that land in no fixed order once a sequence has more than two tiles of 128 tokens, so its low-order bits may
+ * differ from run to run; o, lse, dk and dv are bit-reproducible.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t n_seqs, T, Hq, Hkv, D;
+    float sm_scale;
+    int32_t causal;
+    int64_t sTq, sHq, sTkv, sHkv;   /* element strides; 0, 0 = contiguous */
+} vardrop_packed_cfg;
+
+size_t vardrop_packed_plan_bytes(const vardrop_packed_cfg* cfg);
+int vardrop_packed_plan(const int32_t* cu_seqlens, const vardrop_packed_cfg* cfg, void* plan, size_t plan_bytes, void* stream);
+size_t vardrop_attn_packed_workspace_bytes(const vardrop_packed_cfg* cfg);
+int vardrop_attn_packed_fwd(const void* q, const void* k, const void* v, const void* plan, size_t plan_bytes, const vardrop_packed_cfg* cfg, void* o, float* lse, void* ws,
+                            size_t ws_bytes, void* stream);
+int vardrop_attn_packed_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o, const void* plan, size_t plan_bytes,
+                            const vardrop_packed_cfg* cfg, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Norms before and after a block, with the block's gate and residual scale (no counterpart in the paper, which takes its encoder's

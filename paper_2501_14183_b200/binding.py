@@ -43,6 +43,11 @@ class PearsonCfg(C.Structure):
     _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("L", C.c_int32), ("threshold", C.c_float)]
 
 
+class PackedCfg(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("sm_scale", C.c_float), ("causal", C.c_int32),
+                ("sTq", C.c_int64), ("sHq", C.c_int64), ("sTkv", C.c_int64), ("sHkv", C.c_int64)]       # element strides of q, and of k and v; 0, 0 = contiguous
+
+
 class NormCfg(C.Structure):
     _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("pre", C.c_int32), ("post", C.c_int32), ("gate_rows", C.c_int32), ("S", C.c_int32),
                 ("res_scale", C.c_float), ("eps", C.c_float)]
@@ -65,7 +70,8 @@ class VardropError(RuntimeError):
 
 EXPORTS = ("vardrop_status_string", "vardrop_last_error", "vardrop_version", "vardrop_ws_status", "vardrop_probe_bounded_wait", "vardrop_hash_workspace_bytes", "vardrop_hash",
            "vardrop_select_workspace_bytes", "vardrop_select", "vardrop_select_static", "vardrop_gather_rows", "vardrop_attn_workspace_bytes", "vardrop_attn_fwd",
-           "vardrop_attn_bwd", "vardrop_pearson_workspace_bytes", "vardrop_pearson_max", "vardrop_norm_fwd", "vardrop_norm_workspace_bytes", "vardrop_norm_bwd",
+           "vardrop_attn_bwd", "vardrop_pearson_workspace_bytes", "vardrop_pearson_max", "vardrop_packed_plan_bytes", "vardrop_packed_plan",
+           "vardrop_attn_packed_workspace_bytes", "vardrop_attn_packed_fwd", "vardrop_attn_packed_bwd", "vardrop_norm_fwd", "vardrop_norm_workspace_bytes", "vardrop_norm_bwd",
            "vardrop_grad_clip_workspace_bytes", "vardrop_grad_clip", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
            "vardrop_profile_kernel_name", "vardrop_profile_read")
 
@@ -81,7 +87,8 @@ def load() -> C.CDLL:
             getattr(lib, name).restype = C.c_char_p
         lib.vardrop_status_string.argtypes = [C.c_int]
         for name in ("vardrop_hash_workspace_bytes", "vardrop_select_workspace_bytes", "vardrop_attn_workspace_bytes",
-                     "vardrop_pearson_workspace_bytes", "vardrop_norm_workspace_bytes"):
+                     "vardrop_pearson_workspace_bytes", "vardrop_norm_workspace_bytes", "vardrop_packed_plan_bytes",
+                     "vardrop_attn_packed_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
             getattr(lib, name).argtypes = [C.c_void_p]
         lib.vardrop_ws_status.restype = C.c_int
@@ -102,6 +109,12 @@ def load() -> C.CDLL:
         lib.vardrop_attn_bwd.argtypes = [C.c_void_p] * 14 + [C.c_size_t, C.c_void_p]
         lib.vardrop_pearson_max.restype = C.c_int
         lib.vardrop_pearson_max.argtypes = [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_packed_plan.restype = C.c_int
+        lib.vardrop_packed_plan.argtypes = [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_attn_packed_fwd.restype = C.c_int
+        lib.vardrop_attn_packed_fwd.argtypes = [C.c_void_p] * 4 + [C.c_size_t] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_attn_packed_bwd.restype = C.c_int
+        lib.vardrop_attn_packed_bwd.argtypes = [C.c_void_p] * 7 + [C.c_size_t] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
         lib.vardrop_norm_fwd.restype = C.c_int
         lib.vardrop_norm_fwd.argtypes = [C.c_void_p] * 14
         lib.vardrop_norm_bwd.restype = C.c_int
@@ -195,6 +208,26 @@ def vardrop_pearson_max(x, cfg: PearsonCfg, max_rho, n_above, ws) -> None:
     _check((_marshal or _load_marshal()).pearson_max(x, cfg, max_rho, n_above, ws), "vardrop_pearson_max")
 
 
+def vardrop_packed_plan_bytes(cfg: PackedCfg) -> int:
+    return int(load().vardrop_packed_plan_bytes(C.byref(cfg)))
+
+
+def vardrop_packed_plan(cu_seqlens, cfg: PackedCfg, plan) -> None:
+    _check((_marshal or _load_marshal()).packed_plan(cu_seqlens, cfg, plan), "vardrop_packed_plan")
+
+
+def vardrop_attn_packed_workspace_bytes(cfg: PackedCfg) -> int:
+    return int(load().vardrop_attn_packed_workspace_bytes(C.byref(cfg)))
+
+
+def vardrop_attn_packed_fwd(q, k, v, plan, cfg: PackedCfg, o, lse, ws) -> None:
+    _check((_marshal or _load_marshal()).attn_packed_fwd(q, k, v, plan, cfg, o, lse, ws), "vardrop_attn_packed_fwd")
+
+
+def vardrop_attn_packed_bwd(q, k, v, o, lse, d_o, plan, cfg: PackedCfg, dq, dk, dv, ws) -> None:
+    _check((_marshal or _load_marshal()).attn_packed_bwd(q, k, v, o, lse, d_o, plan, cfg, dq, dk, dv, ws), "vardrop_attn_packed_bwd")
+
+
 def vardrop_norm_fwd(x, y, gate, w_post, b_post, w_pre, b_pre, sel_idx, n_sel, cfg: NormCfg, h, u, stats) -> None:
     _check((_marshal or _load_marshal()).norm_fwd(x, y, gate, w_post, b_post, w_pre, b_pre, sel_idx, n_sel, cfg, h, u, stats), "vardrop_norm_fwd")
 
@@ -252,6 +285,10 @@ def vardrop_probe_bounded_wait(ws, limit_us: int) -> None:
 def alloc_ws(nbytes: int, device="cuda"):
     """A zero-filled workspace: its status word is only ever set by the library, never cleared."""
     return torch.zeros(max(256, (nbytes + 255) // 256 * 256), dtype=torch.uint8, device=device)
+
+
+def alloc_packed_plan(cfg: PackedCfg, device="cuda"):
+    return torch.zeros(vardrop_packed_plan_bytes(cfg), dtype=torch.uint8, device=device)
 
 
 def alloc_hash_outputs(cfg: HashCfg, device="cuda", want_freqs=True, want_amp=False):

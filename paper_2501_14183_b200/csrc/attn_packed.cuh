@@ -1,0 +1,82 @@
+// Shared pieces of attention over packed sequences: the plan of a batch, tensor maps, workspace layout.
+#pragma once
+
+#include "attn_bwd.cuh"
+
+namespace vardrop {
+
+// A plan: a header, then an entry for every 128-token tile of every sequence, those with the most work first.  Entry `level` i of a sequence of n tiles stands for
+// query tile i forward (i + 1 key tiles in causal calls) and key tile n - 1 - i backward (i + 1 query tiles), so that one order serves both.
+constexpr int kPlanMagic = 0x56445031;
+enum PlanWord { kPlanStatus = 0, kPlanMagicWord, kPlanTiles, kPlanSeqs, kPlanRows, kPlanCausal };
+struct alignas(16) PlanEntry {
+    int start;              // row of the sequence's first token
+    int len;                // its tokens
+    int level;
+    int base;               // tiles of the sequences ahead of it: its first tile in layouts where every sequence begins a tile
+};
+
+// Tiles that a batch can have at most: a sequence's last one may hold a single token.
+inline long long packed_tiles(const vardrop_packed_cfg& c) { return c.T / kTile + (c.n_seqs < c.T ? c.n_seqs : c.T); }
+
+struct PackedWs {
+    size_t delta;           // [Hq, tiles 128] fp32
+    size_t dq_acc;          // [tiles 128, Hq, 64] fp32
+    size_t total;
+    int rows;               // tiles 128
+};
+inline PackedWs packed_layout(const vardrop_packed_cfg& c) {
+    PackedWs w;
+    w.rows = static_cast<int>(packed_tiles(c) * kTile);
+    size_t o = align_up(kWsHeaderBytes, 1024);
+    w.delta = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * w.rows, 1024);
+    w.dq_acc = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * kDP * w.rows, 1024);
+    w.total = o;
+    return w;
+}
+
+struct PackedStrides {
+    long long sTq, sHq, sTkv, sHkv;
+};
+inline PackedStrides packed_strides(const vardrop_packed_cfg& c) {
+    PackedStrides s{c.sTq, c.sHq, c.sTkv, c.sHkv};
+    if (s.sTq == 0 && s.sHq == 0) { s.sHq = c.D; s.sTq = static_cast<long long>(c.Hq) * c.D; }
+    if (s.sTkv == 0 && s.sHkv == 0) { s.sHkv = c.D; s.sTkv = static_cast<long long>(c.Hkv) * c.D; }
+    return s;
+}
+
+// Tensor map over [T, H, D] bf16 with the given element strides: box = 128 tokens x 64 elements of a head, 128-byte swizzle; the upper half of a row of a tensor with
+// D = 32, and rows behind the tensor, read as zero.
+int packed_tile_map(CUtensorMap* map, const void* base, int D, int H, int T, long long sT, long long sH);
+// Over the fp32 accumulator [rows, H, 64]: box = 128 rows x 32 floats of a head.
+int packed_acc_map(CUtensorMap* map, const void* base, int rows, int H);
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const void* map, uint64_t* bar, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_reduce_add_3d(const void* map, const void* src, int c0, int c1, int c2) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+
+// What a kernel needs of the plan's header: the number of tiles, 0 where it is not a plan of this call's kind (which the caller reports).
+struct PlanView {
+    const int32_t* words;
+    int n_seqs, T, causal;
+    __device__ __forceinline__ bool fits() const {
+        return words[kPlanStatus] == VARDROP_OK && words[kPlanMagicWord] == kPlanMagic && words[kPlanSeqs] == n_seqs && words[kPlanRows] == T && words[kPlanCausal] == causal;
+    }
+    __device__ __forceinline__ const PlanEntry* entries() const { return reinterpret_cast<const PlanEntry*>(words + kWsHeaderBytes / 4); }
+    __device__ __forceinline__ int tiles() const { return fits() ? words[kPlanTiles] : 0; }
+};
+
+// Item of a CTA's turn: there and back over the grid, so that what one CTA has more of in one turn it has less of in the next (items come with the most work first).
+__device__ __forceinline__ long long turn_item(int turn) {
+    const long long first = static_cast<long long>(turn) * gridDim.x;
+    return first + ((turn & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
+
+}  // namespace vardrop

@@ -12,7 +12,7 @@ namespace vardrop {
 // Kernel identities for the launch counter and the optional per-kernel event timer (vardrop_profile_*).
 enum KernelId {
     K_HASH = 0, K_SELECT_SMALL, K_SELECT_COUNT, K_SELECT_GROUP, K_SELECT_SAMPLE, K_ATTN_FWD, K_BWD_PREP, K_ATTN_BWD, K_BWD_CONVERT, K_PEARSON_NORM, K_PEARSON_MAX, K_GATHER_ROWS,
-    K_SELECT_PLACE, K_SELECT_CLUSTER, K_NORM_FWD, K_NORM_BWD, K_NORM_PARAMS, K_GRAD_NORM, K_GRAD_SCALE,
+    K_SELECT_PLACE, K_SELECT_CLUSTER, K_PACKED_PLAN, K_PACKED_FWD, K_PACKED_PREP, K_PACKED_BWD, K_PACKED_CONVERT, K_NORM_FWD, K_NORM_BWD, K_NORM_PARAMS, K_GRAD_NORM, K_GRAD_SCALE,
     K_COUNT
 };
 // Wrap a kernel launch: counts it and, when the timer is armed, brackets it with a pair of CUDA events on `stream`.
@@ -76,6 +76,15 @@ int attn_bwd_launch(const void* q, const void* k, const void* v, const void* o, 
                     void* dk, void* dv, void* ws, cudaStream_t stream);
 int attn_bwd_many_launch(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o, const int32_t* sel_idx,
                          const int32_t* n_sel, const int32_t* inv_idx, const vardrop_attn_cfg& cfg, void* dq, void* dk, void* dv, void* ws, cudaStream_t stream);
+
+// packed_plan.cu, attn_packed_fwd.cu, attn_packed_bwd.cu
+int packed_validate(const vardrop_packed_cfg& cfg);
+size_t packed_plan_bytes(const vardrop_packed_cfg& cfg);
+int packed_plan_launch(const int32_t* cu_seqlens, const vardrop_packed_cfg& cfg, void* plan, cudaStream_t stream);
+size_t attn_packed_workspace_bytes(const vardrop_packed_cfg& cfg);
+int attn_packed_fwd_launch(const void* q, const void* k, const void* v, const void* plan, const vardrop_packed_cfg& cfg, void* o, float* lse, void* ws, cudaStream_t stream);
+int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o, const void* plan, const vardrop_packed_cfg& cfg, void* dq,
+                           void* dk, void* dv, void* ws, cudaStream_t stream);
 
 // norm.cu
 int norm_validate(const vardrop_norm_cfg& cfg);

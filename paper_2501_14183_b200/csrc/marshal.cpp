@@ -53,6 +53,16 @@ struct Args {
         if (t.numel() < count) return refuse<T>("%s has fewer elements than the configuration says", name);
         return static_cast<T*>(t.data_ptr());
     }
+    // q, k or v of a packed call: [T, H, D] with the strides of the configuration
+    const void* packed(int i, const char* name, const vardrop_packed_cfg& c, int H, int64_t sT, int64_t sH) {
+        const bool plain = sT == 0 && sH == 0;
+        void* const p = checked(i, name, at::kBFloat16, static_cast<int64_t>(c.T) * H * c.D, plain ? kContiguous : kStrided);
+        if (!p || plain) return p;
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (t.dim() != 3 || t.size(0) != c.T || t.size(1) != H || t.size(2) != c.D || (c.T > 1 && t.stride(0) != sT) || (H > 1 && t.stride(1) != sH) || t.stride(2) != 1)
+            return refuse<void>("%s does not have the shape and strides of the configuration", name);
+        return p;
+    }
     template <typename T>
     T* refuse(const char* text, const char* name) {
         PyErr_Format(PyExc_ValueError, text, name);
@@ -186,6 +196,55 @@ PyObject* pearson_max(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+PyObject* packed_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<3>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_packed_cfg>(1);
+        if (!g.ok) return nullptr;
+        const auto cu = g.checked<const int32_t>(0, "cu_seqlens", at::kInt, static_cast<int64_t>(cfg->n_seqs) + 1);
+        void* const plan = g.checked(2, "plan", at::kByte, 0);
+        const size_t nb = g.ok && plan ? g.bytes(2) : 0;
+        return finish(g, [=](void* s) { return vardrop_packed_plan(cu, cfg, plan, nb, s); });
+    });
+}
+PyObject* attn_packed_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<8>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_packed_cfg>(4);
+        if (!g.ok) return nullptr;
+        const int64_t rows = static_cast<int64_t>(cfg->T) * cfg->Hq;
+        const void* const q = g.packed(0, "q", *cfg, cfg->Hq, cfg->sTq, cfg->sHq);
+        const void* const k = g.packed(1, "k", *cfg, cfg->Hkv, cfg->sTkv, cfg->sHkv);
+        const void* const v = g.packed(2, "v", *cfg, cfg->Hkv, cfg->sTkv, cfg->sHkv);
+        const void* const plan = g.checked(3, "plan", at::kByte, 0);
+        const size_t np = g.ok && plan ? g.bytes(3) : 0;
+        void* const o = g.checked(5, "o", at::kBFloat16, rows * cfg->D);
+        const auto lse = g.checked<float>(6, "lse", at::kFloat, rows);
+        void* const ws = g.checked(7, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(7) : 0;
+        return finish(g, [=](void* s) { return vardrop_attn_packed_fwd(q, k, v, plan, np, cfg, o, lse, ws, nb, s); });
+    });
+}
+PyObject* attn_packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<12>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_packed_cfg>(7);
+        if (!g.ok) return nullptr;
+        const int64_t rows = static_cast<int64_t>(cfg->T) * cfg->Hq, kv = static_cast<int64_t>(cfg->T) * cfg->Hkv * cfg->D;
+        const void* const q = g.packed(0, "q", *cfg, cfg->Hq, cfg->sTq, cfg->sHq);
+        const void* const k = g.packed(1, "k", *cfg, cfg->Hkv, cfg->sTkv, cfg->sHkv);
+        const void* const v = g.packed(2, "v", *cfg, cfg->Hkv, cfg->sTkv, cfg->sHkv);
+        const void* const o = g.checked(3, "o", at::kBFloat16, rows * cfg->D);
+        const auto lse = g.checked<const float>(4, "lse", at::kFloat, rows);
+        const void* const d_o = g.checked(5, "d_o", at::kBFloat16, rows * cfg->D);
+        const void* const plan = g.checked(6, "plan", at::kByte, 0);
+        const size_t np = g.ok && plan ? g.bytes(6) : 0;
+        void* const dq = g.checked(8, "dq", at::kBFloat16, rows * cfg->D);
+        void* const dk = g.checked(9, "dk", at::kBFloat16, kv);
+        void* const dv = g.checked(10, "dv", at::kBFloat16, kv);
+        void* const ws = g.checked(11, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(11) : 0;
+        return finish(g, [=](void* s) { return vardrop_attn_packed_bwd(q, k, v, o, lse, d_o, plan, np, cfg, dq, dk, dv, ws, nb, s); });
+    });
+}
+
 at::ScalarType type_of(int dtype) { return dtype == 2 ? at::kFloat : dtype == 1 ? at::kHalf : at::kBFloat16; }
 
 PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -274,7 +333,7 @@ PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define VD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VD_METHOD(hash), VD_METHOD(select), VD_METHOD(select_static), VD_METHOD(gather_rows), VD_METHOD(attn_fwd), VD_METHOD(attn_bwd),
-                           VD_METHOD(pearson_max), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), {nullptr, nullptr, 0, nullptr}};
+                           VD_METHOD(pearson_max), VD_METHOD(packed_plan), VD_METHOD(attn_packed_fwd), VD_METHOD(attn_packed_bwd), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

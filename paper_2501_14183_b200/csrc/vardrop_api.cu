@@ -49,7 +49,8 @@ std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_prof_events[K_COUNT];   // pa
 std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_prof_free;              // pairs ready for reuse
 const char* const g_kernel_names[K_COUNT] = {"hash_kernel", "select_small_kernel", "select_count_kernel", "select_group_kernel", "select_sample_kernel",
                                              "attn_fwd_kernel", "bwd_prep_kernel", "attn_bwd_kernel", "bwd_convert_kernel", "pearson_normalize_kernel",
-                                             "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel"};
+                                             "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel", "packed_plan_kernel",
+                                             "attn_packed_fwd_kernel", "packed_prep_kernel", "attn_packed_bwd_kernel", "packed_convert_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel"};
 }  // namespace
 
 LaunchScope::LaunchScope(int id, cudaStream_t stream) : id_(id), stream_(stream), stop_(nullptr) {
@@ -284,6 +285,62 @@ int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* m
     VD_CHECK(check_ptr(n_above, "n_above", true));
     VD_CHECK(check_ws(ws, ws_bytes, pearson_workspace_bytes(*cfg)));
     return pearson_launch(x, *cfg, max_rho, n_above, ws, static_cast<cudaStream_t>(stream));
+}
+
+size_t vardrop_packed_plan_bytes(const vardrop_packed_cfg* cfg) {
+    if (!cfg || packed_validate(*cfg) != VARDROP_OK) return 0;
+    return packed_plan_bytes(*cfg);
+}
+
+size_t vardrop_attn_packed_workspace_bytes(const vardrop_packed_cfg* cfg) {
+    if (!cfg || packed_validate(*cfg) != VARDROP_OK) return 0;
+    return attn_packed_workspace_bytes(*cfg);
+}
+
+static int check_plan(const void* plan, size_t have, const vardrop_packed_cfg& cfg) {
+    if (int st = check_ptr(plan, "plan", true)) return st;
+    if (have < packed_plan_bytes(cfg)) return fail(VARDROP_ERR_WORKSPACE, "plan of %zu bytes given, %zu needed", have, packed_plan_bytes(cfg));
+    return VARDROP_OK;
+}
+
+int vardrop_packed_plan(const int32_t* cu_seqlens, const vardrop_packed_cfg* cfg, void* plan, size_t plan_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(packed_validate(*cfg));
+    VD_CHECK(check_ptr(cu_seqlens, "cu_seqlens", true));
+    VD_CHECK(check_plan(plan, plan_bytes, *cfg));
+    return packed_plan_launch(cu_seqlens, *cfg, plan, static_cast<cudaStream_t>(stream));
+}
+
+int vardrop_attn_packed_fwd(const void* q, const void* k, const void* v, const void* plan, size_t plan_bytes, const vardrop_packed_cfg* cfg, void* o, float* lse, void* ws,
+                            size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(packed_validate(*cfg));
+    VD_CHECK(check_ptr(q, "q", true));
+    VD_CHECK(check_ptr(k, "k", true));
+    VD_CHECK(check_ptr(v, "v", true));
+    VD_CHECK(check_plan(plan, plan_bytes, *cfg));
+    VD_CHECK(check_ptr(o, "o", true));
+    VD_CHECK(check_ptr(lse, "lse", true));
+    VD_CHECK(check_ws(ws, ws_bytes, kWsHeaderBytes));
+    return attn_packed_fwd_launch(q, k, v, plan, *cfg, o, lse, ws, static_cast<cudaStream_t>(stream));
+}
+
+int vardrop_attn_packed_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o, const void* plan, size_t plan_bytes,
+                            const vardrop_packed_cfg* cfg, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(packed_validate(*cfg));
+    VD_CHECK(check_ptr(q, "q", true));
+    VD_CHECK(check_ptr(k, "k", true));
+    VD_CHECK(check_ptr(v, "v", true));
+    VD_CHECK(check_ptr(o, "o", true));
+    VD_CHECK(check_ptr(lse, "lse", true));
+    VD_CHECK(check_ptr(d_o, "d_o", true));
+    VD_CHECK(check_plan(plan, plan_bytes, *cfg));
+    VD_CHECK(check_ptr(dq, "dq", true));
+    VD_CHECK(check_ptr(dk, "dk", true));
+    VD_CHECK(check_ptr(dv, "dv", true));
+    VD_CHECK(check_ws(ws, ws_bytes, attn_packed_workspace_bytes(*cfg)));
+    return attn_packed_bwd_launch(q, k, v, o, lse, d_o, plan, *cfg, dq, dk, dv, ws, static_cast<cudaStream_t>(stream));
 }
 
 // parameters and gradients that a configuration has no use for are refused, not ignored

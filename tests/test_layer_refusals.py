@@ -73,6 +73,45 @@ def test_clip_arguments(lib):
     assert call(ok, nb=need - 1) == vd.ERR_WORKSPACE
 
 
+def packed_cfg(**kw):
+    return vd.PackedCfg(*[{**dict(n_seqs=3, T=100, Hq=4, Hkv=2, D=64, sm_scale=0.0, causal=1, sTq=0, sHq=0, sTkv=0, sHkv=0), **kw}[n] for n, _ in vd.PackedCfg._fields_])
+
+
+@pytest.mark.parametrize("kw,status", [(dict(n_seqs=0), 1), (dict(T=0), 1), (dict(Hq=0), 1), (dict(Hkv=0), 1), (dict(Hq=5), 1), (dict(D=128), 2), (dict(D=48), 2), (dict(T=(1 << 24) + 1), 2),
+                                       (dict(n_seqs=(1 << 24) + 1), 2), (dict(Hq=8192), 2), (dict(T=1 << 24, n_seqs=1 << 24), 2), (dict(causal=2), 1), (dict(sm_scale=-1.0), 1),
+                                       (dict(sm_scale=float("nan")), 1), (dict(sm_scale=float("inf")), 1), (dict(sTq=256), 1), (dict(sTq=260, sHq=64), 1), (dict(sTkv=32, sHkv=64), 1),
+                                       (dict(sTq=256, sHq=60), 1), (dict(sTq=-256, sHq=64), 1), (dict(sTkv=1 << 40, sHkv=64), 2)])
+def test_packed_configurations(lib, kw, status):
+    cfg = packed_cfg(**kw)
+    assert lib.vardrop_packed_plan(GOOD, C.byref(cfg), GOOD, 1 << 30, None) == status
+    assert lib.vardrop_attn_packed_fwd(*[GOOD] * 4, 1 << 30, C.byref(cfg), GOOD, GOOD, GOOD, 1 << 30, None) == status
+    assert lib.vardrop_attn_packed_bwd(*[GOOD] * 7, 1 << 30, C.byref(cfg), *[GOOD] * 4, 1 << 40, None) == status
+    assert lib.vardrop_last_error().startswith(b"packed attention")
+    assert vd.vardrop_packed_plan_bytes(cfg) == 0 and vd.vardrop_attn_packed_workspace_bytes(cfg) == 0
+
+
+def test_packed_arguments(lib):
+    cfg = packed_cfg()
+    plan, ws, by = vd.vardrop_packed_plan_bytes(cfg), vd.vardrop_attn_packed_workspace_bytes(cfg), C.byref(cfg)
+    assert plan == 256 + 3 * 16 and ws >= 3 * 128 * 4 * (64 + 1) * 4
+    assert lib.vardrop_packed_plan(None, by, GOOD, plan, None) == lib.vardrop_packed_plan(GOOD, by, None, plan, None) == lib.vardrop_packed_plan(GOOD + 4, by, GOOD, plan, None) == 1
+    assert lib.vardrop_packed_plan(GOOD, by, GOOD, plan - 1, None) == vd.ERR_WORKSPACE and lib.vardrop_packed_plan(GOOD, None, GOOD, plan, None) == 1
+    for at in range(7):                 # q, k, v, plan, o, lse, ws
+        for bad in (None, GOOD + 8):
+            a = [GOOD] * 7
+            a[at] = bad
+            assert lib.vardrop_attn_packed_fwd(*a[:4], plan, by, *a[4:], 256, None) == 1, at
+    assert lib.vardrop_attn_packed_fwd(*[GOOD] * 4, plan - 1, by, *[GOOD] * 3, 256, None) == vd.ERR_WORKSPACE
+    assert lib.vardrop_attn_packed_fwd(*[GOOD] * 4, plan, by, *[GOOD] * 3, 255, None) == vd.ERR_WORKSPACE
+    for at in range(11):                # q, k, v, o, lse, d_o, plan, dq, dk, dv, ws
+        for bad in (None, GOOD + 8):
+            a = [GOOD] * 11
+            a[at] = bad
+            assert lib.vardrop_attn_packed_bwd(*a[:7], plan, by, *a[7:], ws, None) == 1, at
+    assert lib.vardrop_attn_packed_bwd(*[GOOD] * 7, plan, by, *[GOOD] * 4, ws - 1, None) == vd.ERR_WORKSPACE
+
+
 def test_struct_layouts_match_header():
+    assert C.sizeof(vd.PackedCfg) == 64 and vd.PackedCfg.sTq.offset == 32
     assert C.sizeof(vd.NormCfg) == 40 and vd.NormCfg.res_scale.offset == 32
     assert C.sizeof(vd.ClipCfg) == 8 and C.sizeof(Tensor) == 32
