@@ -15,7 +15,7 @@ namespace vardrop {
 
 namespace {
 
-constexpr int kNormPer = 8;              // elements of a row in a thread
+constexpr int kFwdPer = 16, kBwdPer = 8;  // elements of a row in a thread (backward the sums over tokens take as many registers again, or three times)
 constexpr int kNormMaxC = 8192;
 
 struct NormParams {
@@ -33,76 +33,147 @@ struct NormParams {
     float scale, eps, inv_c;
 };
 
-// ---- elements -------------------------------------------------------------------------------------------------------------
-template <class T> __device__ __forceinline__ float to_f(T v);
-template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <> __device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }
-template <class T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+// ---- pairs: two fp32 values in a 64-bit register, for the packed instructions of sm_100 (one issue slot for two results, each rounded as the scalar instruction's) -------
+typedef uint64_t Pair;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ Pair both(float v) { return pair_of(v, v); }
+__device__ __forceinline__ float2 halves(Pair v) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float sum_of(Pair v) { const float2 f = halves(v); return f.x + f.y; }
 
-// A thread's columns: kNormPer / kV vectors of kV, a group's threads side by side.
-template <class T, int kV, int kGroup>
+// ---- elements -------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ Pair widen(uint32_t w, __nv_bfloat16) { return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ Pair widen(uint32_t w, __half) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return pair_of(f.x, f.y);
+}
+__device__ __forceinline__ uint32_t narrow(Pair v, __nv_bfloat16) {
+    const float2 f = halves(v);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t narrow(Pair v, __half) {
+    const float2 f = halves(v);
+    const __half2 r = __floats2half2_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// A thread's columns: kPer / kV vectors of kV, a group's threads side by side; element e of the thread is element e % kV of vector e / kV, and pair p elements 2 p and 2 p + 1.
+template <class T, int kV, int kGroup, int kPer>
 struct Row {
-    static constexpr int kVecs = kNormPer / kV;
-    struct alignas(sizeof(T) * kV) Vec { T v[kV]; };
+    static constexpr int kVecs = kPer / kV, kPairs = kPer / 2, kVecBytes = kV * static_cast<int>(sizeof(T));
+    typedef Pair Values[kPairs];
     static __device__ __forceinline__ int col(int t, int j) { return (j * kGroup + t) * kV; }
-    static __device__ __forceinline__ void load(const T* row, int t, int C, Vec (&to)[kVecs]) {
+    static __device__ __forceinline__ bool whole(int C) { return C == kGroup * kPer; }
+    // words of the vectors (a 16-bit element alone takes a word too) to pairs, and back
+    static constexpr int kWords = kVecBytes < 4 ? 1 : kVecBytes / 4;
+    struct alignas(kVecBytes < 4 ? 4 : kVecBytes) Vec { uint32_t w[kWords]; };
+    static __device__ __forceinline__ Vec load(const T* p) {
+        Vec v;
+        if constexpr (kVecBytes < 4) v.w[0] = *reinterpret_cast<const unsigned short*>(p);
+        else v = *reinterpret_cast<const Vec*>(p);
+        return v;
+    }
+    static __device__ __forceinline__ void unpack(const Vec (&v)[kVecs], Values& to) {
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-            if (col(t, j) < C) to[j] = *reinterpret_cast<const Vec*>(row + col(t, j));
-            else {
-#pragma unroll
-                for (int e = 0; e < kV; ++e) to[j].v[e] = from_f<T>(0.f);
+        for (int p = 0; p < kPairs; ++p) {
+            if constexpr (sizeof(T) == 4) {
+                const int e = 2 * p;
+                to[p] = pair_of(__uint_as_float(v[e / kV].w[e % kV]), __uint_as_float(v[(e + 1) / kV].w[(e + 1) % kV]));
+            } else if constexpr (kV == 1) {
+                to[p] = widen(v[2 * p].w[0] | v[2 * p + 1].w[0] << 16, T{});
+            } else {
+                to[p] = widen(v[2 * p / kV].w[p % (kV / 2)], T{});
             }
         }
     }
-    static __device__ __forceinline__ void floats(const Vec (&from)[kVecs], float (&v)[kNormPer]) {
+    static __device__ __forceinline__ void store(T* row, int t, int C, const Values& v) {
+        Vec x[kVecs];
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j)
-#pragma unroll
-            for (int e = 0; e < kV; ++e) v[j * kV + e] = to_f<T>(from[j].v[e]);
-    }
-    static __device__ __forceinline__ void store(T* row, int t, int C, const float (&v)[kNormPer]) {
+        for (int p = 0; p < kPairs; ++p) {
+            if constexpr (sizeof(T) == 4) {
+                const float2 f = halves(v[p]);
+                const int e = 2 * p;
+                x[e / kV].w[e % kV] = __float_as_uint(f.x);
+                x[(e + 1) / kV].w[(e + 1) % kV] = __float_as_uint(f.y);
+            } else if constexpr (kV == 1) {
+                const uint32_t w = narrow(v[p], T{});
+                x[2 * p].w[0] = w & 0xffffu;
+                x[2 * p + 1].w[0] = w >> 16;
+            } else {
+                x[2 * p / kV].w[p % (kV / 2)] = narrow(v[p], T{});
+            }
+        }
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
             if (col(t, j) >= C) continue;
-            Vec x;
-#pragma unroll
-            for (int e = 0; e < kV; ++e) x.v[e] = from_f<T>(v[j * kV + e]);
-            *reinterpret_cast<Vec*>(row + col(t, j)) = x;
+            if constexpr (kVecBytes < 4) *reinterpret_cast<unsigned short*>(row + col(t, j)) = static_cast<unsigned short>(x[j].w[0]);
+            else *reinterpret_cast<Vec*>(row + col(t, j)) = x[j];
         }
     }
     // of a parameter; `none` where there is none, 0 behind the row's end
-    static __device__ __forceinline__ void param(const float* p, int t, int C, float none, float (&v)[kNormPer]) {
+    static __device__ __forceinline__ void param(const float* p, int t, int C, float none, Values& v) {
+        float f[kPer];
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
             if (p && col(t, j) < C) {
-                if (kV >= 4) {
+                if constexpr (kV % 4 == 0) {
 #pragma unroll
                     for (int e = 0; e < kV; e += 4) {
-                        const float4 f = __ldg(reinterpret_cast<const float4*>(p + col(t, j) + e));
-                        v[j * kV + e] = f.x; v[j * kV + e + 1] = f.y; v[j * kV + e + 2] = f.z; v[j * kV + e + 3] = f.w;
+                        const float4 q = __ldg(reinterpret_cast<const float4*>(p + col(t, j) + e));
+                        f[j * kV + e] = q.x; f[j * kV + e + 1] = q.y; f[j * kV + e + 2] = q.z; f[j * kV + e + 3] = q.w;
                     }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < kV; ++e) v[j * kV + e] = __ldg(p + col(t, j) + e);
+                    for (int e = 0; e < kV; ++e) f[j * kV + e] = __ldg(p + col(t, j) + e);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < kV; ++e) v[j * kV + e] = col(t, j) < C ? none : 0.f;
+                for (int e = 0; e < kV; ++e) f[j * kV + e] = col(t, j) < C ? none : 0.f;
             }
         }
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
     }
-    static __device__ __forceinline__ void param_store(float* p, int t, int C, const float (&v)[kNormPer]) {
+    static __device__ __forceinline__ void param_store(float* to, int t, int C, const Values& v) {
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j)
-            if (col(t, j) < C) {
+        for (int i = 0; i < kPairs; ++i) {
+            const float2 f = halves(v[i]);
+            const int c0 = col(t, 2 * i / kV) + 2 * i % kV, c1 = col(t, (2 * i + 1) / kV) + (2 * i + 1) % kV;
+            if (c0 < C) to[c0] = f.x;
+            if (c1 < C) to[c1] = f.y;
+        }
+    }
+    // zeros again behind the row's end
+    static __device__ __forceinline__ void clear_rest(int t, int C, Values& v) {
+        if (whole(C)) return;
 #pragma unroll
-                for (int e = 0; e < kV; ++e) p[col(t, j) + e] = v[j * kV + e];
-            }
+        for (int i = 0; i < kPairs; ++i) {
+            const float2 f = halves(v[i]);
+            v[i] = pair_of(col(t, 2 * i / kV) < C ? f.x : 0.f, col(t, (2 * i + 1) / kV) < C ? f.y : 0.f);
+        }
     }
 };
 
@@ -112,26 +183,36 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Two sums at once, to every thread of the group.  Groups of several warps go through shared memory, in two places by turns, so that one barrier a sum is enough.
+// Barrier of group `id` (of at most four).  A number that is only known at run time reserves all sixteen barriers, and an SM then holds four CTAs.
+template <int kGroup>
+__device__ __forceinline__ void group_barrier(int id) {
+    if (id == 0) asm volatile("bar.sync 1, %0;" ::"n"(kGroup) : "memory");
+    else if (id == 1) asm volatile("bar.sync 2, %0;" ::"n"(kGroup) : "memory");
+    else if (id == 2) asm volatile("bar.sync 3, %0;" ::"n"(kGroup) : "memory");
+    else asm volatile("bar.sync 4, %0;" ::"n"(kGroup) : "memory");
+}
+// One sum, or two at once, to every thread of the group.  Groups of several warps go through shared memory, in two places by turns, so that one barrier a sum is enough.
 template <int kGroup>
 struct GroupSum {
     float2* place;                       // [2][kGroup / 32] of this group
     int turn = 0, id;
-    __device__ __forceinline__ float2 operator()(float a, float b) {
+    template <bool kTwo>
+    __device__ __forceinline__ float2 of(float a, float b) {
         a = warp_sum(a);
-        b = warp_sum(b);
+        if (kTwo) b = warp_sum(b);
         if (kGroup == 32) return make_float2(a, b);
         constexpr int kWarps = kGroup / 32;
         const int lane = threadIdx.x & 31, warp = (threadIdx.x % kGroup) >> 5;
         float2* at = place + turn * kWarps;
         turn ^= 1;
         if (lane == 0) at[warp] = make_float2(a, b);
-        asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kGroup) : "memory");
+        group_barrier<kGroup>(id);
         float2 s = make_float2(0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            s.x += at[w].x;
-            s.y += at[w].y;
+            const float2 f = at[w];
+            s.x += f.x;
+            if (kTwo) s.y += f.y;
         }
         return s;
     }
@@ -140,85 +221,168 @@ struct GroupSum {
 template <int kGroup>
 constexpr int kNormThreads = kGroup < 256 ? 256 : kGroup;        // of a CTA
 
-// z = (t - mean) r in place; (mean, r)
-template <class R, int kGroup>
-__device__ __forceinline__ float2 normalise(float (&t)[kNormPer], int kind, int thread, const NormParams& P, GroupSum<kGroup>& sum) {
-    float mean = 0.f;
-    if (kind == 2) {
-        float s = 0.f;
+// Rows on their way from memory: a ring in shared memory whose places belong to one thread each, filled by asynchronous copies of the thread's own columns, so
+// that a group has kStages - 1 rows in flight while it works on one, without registers for them and without barriers.  (Loads into registers behind the row before: 65536 x
+// 1024 bf16 forward 188 us, backward 367; like this 118 and 166, bound by the instructions of scalar arithmetic.)  Columns of two bytes, which those copies cannot take, are
+// loaded when they are needed.
+template <class T, int kV, int kGroup, int kPer, int kTensors>
+struct Ring {
+    using R = Row<T, kV, kGroup, kPer>;
+    using Vec = typename R::Vec;
+    static constexpr bool kAsync = R::kVecBytes >= 4;
+    static constexpr int kThreads = kNormThreads<kGroup>;
+    static constexpr int kStageBytes = kThreads * kPer * static_cast<int>(sizeof(T)) * kTensors;
+    static constexpr int kFit = 200 * 1024 / kStageBytes;
+    static constexpr int kStages = kFit < 1 ? 1 : kFit > 3 ? 3 : kFit;
+    static constexpr int kBytes = kAsync ? kStages * kStageBytes : 0;
+    Vec* mine;                           // this thread's first place
+    __device__ __forceinline__ Vec* at(int stage, int k, int j) const { return mine + ((stage * kTensors + k) * R::kVecs + j) * kThreads; }
+    // tensor k of a row (NULL: none) to a stage; commit() behind the last one
+    __device__ __forceinline__ void fetch(int stage, int k, const T* row, int t, int C) {
+        if constexpr (kAsync) {
+            if (!row) return;
 #pragma unroll
-        for (int e = 0; e < kNormPer; ++e) s += t[e];
-        mean = sum(s, 0.f).x * P.inv_c;
-    }
-    float q = 0.f;
-#pragma unroll
-    for (int j = 0; j < R::kVecs; ++j) {
-        if (R::col(thread, j) >= P.C) continue;          // (zeros there, but not once the mean is off)
-#pragma unroll
-        for (int e = j * (kNormPer / R::kVecs); e < (j + 1) * (kNormPer / R::kVecs); ++e) {
-            t[e] -= mean;
-            q += t[e] * t[e];
+            for (int j = 0; j < R::kVecs; ++j) {
+                if (R::col(t, j) >= C) continue;
+                const uint32_t to = smem_u32(at(stage, k, j));
+                if (R::kVecBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + R::col(t, j)) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(row + R::col(t, j)), "n"(R::kVecBytes) : "memory");
+            }
         }
     }
-    const float r = rsqrtf(sum(q, 0.f).x * P.inv_c + P.eps);
+    __device__ __forceinline__ void commit() {
+        if (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ void wait() {             // the oldest stage in flight has landed
+        if (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    }
+    // a row's columns, zeros behind its end
+    __device__ __forceinline__ void read(int stage, int k, const T* row, int t, int C, typename R::Values& to) const {
+        Vec v[R::kVecs];
 #pragma unroll
-    for (int e = 0; e < kNormPer; ++e) t[e] *= r;
-    return make_float2(mean, r);
+        for (int j = 0; j < R::kVecs; ++j) {
+            if (R::col(t, j) < C) {
+                if constexpr (kAsync) v[j] = *at(stage, k, j);
+                else v[j] = R::load(row + R::col(t, j));
+            } else {
+#pragma unroll
+                for (int w = 0; w < R::kWords; ++w) v[j].w[w] = 0u;
+            }
+        }
+        R::unpack(v, to);
+    }
+};
+
+// t without its mean (kind 2), and the (mean, r) of its norm
+template <class R, int kGroup, bool kLayer>
+__device__ __forceinline__ float2 centre(typename R::Values& t, int kind, int thread, const NormParams& P, GroupSum<kGroup>& sum) {
+    float mean = 0.f;
+    if (kLayer && kind == 2) {
+        Pair s = t[0];
+#pragma unroll
+        for (int p = 1; p < R::kPairs; ++p) s = add2(s, t[p]);
+        mean = sum.template of<false>(sum_of(s), 0.f).x * P.inv_c;
+        const Pair minus = both(-mean);
+#pragma unroll
+        for (int p = 0; p < R::kPairs; ++p) t[p] = add2(t[p], minus);
+        R::clear_rest(thread, P.C, t);
+    }
+    Pair q[2] = {both(0.f), both(0.f)};
+#pragma unroll
+    for (int p = 0; p < R::kPairs; ++p) q[p & 1] = fma2(t[p], t[p], q[p & 1]);
+    return make_float2(mean, rsqrtf(sum.template of<false>(sum_of(add2(q[0], q[1])), 0.f).x * P.inv_c + P.eps));
 }
 
+// The rows of a unit that a group works on: first, first + step, ...; the source row of a selection is known one row ahead of its copies.
+struct RowWalk {
+    const int32_t* sel;
+    int n, step;
+    __device__ __forceinline__ int source(int i) const { return sel ? (i < n ? __ldg(sel + i) : 0) : i; }
+};
+
 // ---- forward ----------------------------------------------------------------------------------------------------------------
-template <class T, int kV, int kGroup>
-__global__ void __launch_bounds__(kNormThreads<kGroup>) norm_fwd_kernel(const NormParams P) {
-    using R = Row<T, kV, kGroup>;
-    constexpr int kGroups = kNormThreads<kGroup> / kGroup;
+// kLayer: a mean or a bias somewhere.
+template <class T, int kV, int kGroup, bool kLayer>
+__global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGroup>) norm_fwd_kernel(const NormParams P) {
+    using Rows = Ring<T, kV, kGroup, kFwdPer, 2>;
+    using R = typename Rows::R;
+    constexpr int kGroups = kNormThreads<kGroup> / kGroup, kAhead = Rows::kStages - 1;
+    extern __shared__ __align__(16) unsigned char smem_dyn[];
     __shared__ float2 s_sum[kGroups][2 * (kGroup / 32)];
     const int group = threadIdx.x / kGroup, t = threadIdx.x % kGroup;
-    GroupSum<kGroup> sum{s_sum[group], 0, 1 + group};
+    GroupSum<kGroup> sum{s_sum[group], 0, group};
+    Rows ring{reinterpret_cast<typename Rows::Vec*>(smem_dyn) + threadIdx.x};
     chain_wait();
     chain_release();
+    const T* const X = static_cast<const T*>(P.x);
+    const T* const Y = static_cast<const T*>(P.y);
+    typename R::Values w_pre, b_pre;                     // of this thread's columns, for all rows
+    R::param(P.w_pre, t, P.C, 1.f, w_pre);
+    if (kLayer) R::param(P.b_pre, t, P.C, 0.f, b_pre);
+    const Pair scale = both(P.scale);
 #pragma unroll 1
     for (int unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
         const int b = unit / P.splits, srow = P.S > 1 ? b : 0;
-        const int n = P.n_sel ? P.n_sel[srow] : P.N;
-        const int32_t* sel = P.sel_idx ? P.sel_idx + static_cast<size_t>(srow) * P.N : nullptr;
-        const float* gate = P.gate ? P.gate + static_cast<size_t>(P.gate_rows > 1 ? b : 0) * P.C : nullptr;
+        const RowWalk walk{P.sel_idx ? P.sel_idx + static_cast<size_t>(srow) * P.N : nullptr, P.n_sel ? P.n_sel[srow] : P.N, P.splits * kGroups};
+        const size_t base = static_cast<size_t>(b) * P.N;
+        // N_post's scale and bias with the gate in them: h = a x + w z + c
+        typename R::Values w, c;
+        {
+            typename R::Values g;
+            R::param(P.gate ? P.gate + static_cast<size_t>(P.gate_rows > 1 ? b : 0) * P.C : nullptr, t, P.C, 1.f, g);
+            R::param(P.w_post, t, P.C, 1.f, w);
+            if (kLayer) R::param(P.b_post, t, P.C, 0.f, c);
+#pragma unroll
+            for (int p = 0; p < R::kPairs; ++p) {
+                w[p] = mul2(w[p], g[p]);
+                if (kLayer) c[p] = mul2(c[p], g[p]);
+            }
+        }
+        int i = (unit - b * P.splits) * kGroups + group, stage = 0, ahead = i;
+        int source = walk.source(ahead);
+        auto fetch = [&](int to) {
+            if (ahead < walk.n) {
+                ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
+                ring.fetch(to, 1, Y ? Y + (base + ahead) * P.C : nullptr, t, P.C);
+            }
+            ring.commit();
+            ahead += walk.step;
+            source = walk.source(ahead);
+        };
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) fetch(s);
 #pragma unroll 1
-        for (int i = (unit - b * P.splits) * kGroups + group; i < n; i += P.splits * kGroups) {
-            const size_t row = (static_cast<size_t>(b) * P.N + i) * P.C;
-            const size_t from = sel ? (static_cast<size_t>(b) * P.N + sel[i]) * P.C : row;
-            typename R::Vec vx[R::kVecs], vy[R::kVecs];
-            R::load(static_cast<const T*>(P.x) + from, t, P.C, vx);
+        for (; i < walk.n; i += walk.step) {
+            const int from = Rows::kAsync ? 0 : walk.source(i);
+            fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
+            ring.wait();
+            const size_t row = (base + i) * P.C;
             float2 post = make_float2(0.f, 1.f), pre = post;
-            float h[kNormPer], w[kNormPer];
-            R::floats(vx, h);
+            typename R::Values h;
+            ring.read(stage, 0, X + (base + from) * P.C, t, P.C, h);
 #pragma unroll
-            for (int e = 0; e < kNormPer; ++e) h[e] *= P.scale;
-            if (P.y) {
-                R::load(static_cast<const T*>(P.y) + row, t, P.C, vy);
-                float y[kNormPer], g[kNormPer];
-                R::floats(vy, y);
-                if (P.post) {
-                    post = normalise<R, kGroup>(y, P.post, t, P, sum);
-                    R::param(P.w_post, t, P.C, 1.f, w);
-                    R::param(P.b_post, t, P.C, 0.f, g);
+            for (int p = 0; p < R::kPairs; ++p) h[p] = mul2(h[p], scale);
+            if (Y) {
+                typename R::Values y;
+                ring.read(stage, 1, Y + row, t, P.C, y);
+                if (P.post) post = centre<R, kGroup, kLayer>(y, P.post, t, P, sum);
+                const Pair r = both(post.y);
 #pragma unroll
-                    for (int e = 0; e < kNormPer; ++e) y[e] = fmaf(y[e], w[e], g[e]);
+                for (int p = 0; p < R::kPairs; ++p) {
+                    if (kLayer) h[p] = add2(h[p], c[p]);
+                    h[p] = fma2(mul2(y[p], r), w[p], h[p]);
                 }
-                R::param(gate, t, P.C, 1.f, g);
-#pragma unroll
-                for (int e = 0; e < kNormPer; ++e) h[e] = fmaf(g[e], y[e], h[e]);
             }
             if (P.h) R::store(static_cast<T*>(P.h) + row, t, P.C, h);
             if (P.pre) {
-                pre = normalise<R, kGroup>(h, P.pre, t, P, sum);
-                float bias[kNormPer];
-                R::param(P.w_pre, t, P.C, 1.f, w);
-                R::param(P.b_pre, t, P.C, 0.f, bias);
+                pre = centre<R, kGroup, kLayer>(h, P.pre, t, P, sum);
+                const Pair r = both(pre.y);
 #pragma unroll
-                for (int e = 0; e < kNormPer; ++e) h[e] = fmaf(h[e], w[e], bias[e]);
+                for (int p = 0; p < R::kPairs; ++p) h[p] = kLayer ? fma2(mul2(h[p], r), w_pre[p], b_pre[p]) : mul2(mul2(h[p], r), w_pre[p]);
                 R::store(static_cast<T*>(P.u) + row, t, P.C, h);
             }
-            if (P.stats && t == 0) P.stats[static_cast<size_t>(b) * P.N + i] = make_float4(post.x, post.y, pre.x, pre.y);
+            if (P.stats && t == 0) P.stats[base + i] = make_float4(post.x, post.y, pre.x, pre.y);
+            if (++stage == Rows::kStages) stage = 0;
         }
     }
 }
@@ -227,136 +391,187 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>) norm_fwd_kernel(const No
 // Sums over tokens: with t the gradient of h, zy and zh the normed y and h:
 //   d_gate = w_post o A + b_post o T,  d_w_post = sum_b g_b o A_b,  d_b_post = sum_b g_b o T_b   with A = sum t o zy, T = sum t over the tokens of an instance,
 //   d_w_pre = sum du o zh,  d_b_pre = sum du
-// so a thread keeps four sums a column however many parameters there are.  (A gate that all instances share needs them over all tokens only.)
-template <class T, int kV, int kGroup>
-__global__ void __launch_bounds__(kNormThreads<kGroup>) norm_bwd_kernel(const NormParams P) {
-    using R = Row<T, kV, kGroup>;
-    constexpr int kGroups = kNormThreads<kGroup> / kGroup;
+// so a thread keeps four sums a column however many parameters there are, without a mean or a bias (kLayer) two.  (A gate that all instances share needs them over all
+// tokens only.)
+template <class T, int kV, int kGroup, bool kLayer>
+__global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGroup> > 0 ? 512 / kNormThreads<kGroup> : 1) norm_bwd_kernel(const NormParams P) {
+    using Rows = Ring<T, kV, kGroup, kBwdPer, 4>;
+    using R = typename Rows::R;
+    constexpr int kGroups = kNormThreads<kGroup> / kGroup, kAhead = Rows::kStages - 1, kPairs = R::kPairs;
+    extern __shared__ __align__(16) unsigned char smem_dyn[];
     __shared__ float2 s_sum[kGroups][2 * (kGroup / 32)];
-    __shared__ float s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kGroup * kNormPer : 1];
+    __shared__ Pair s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kGroup * kPairs : 1];
     const int group = threadIdx.x / kGroup, t = threadIdx.x % kGroup;
-    GroupSum<kGroup> sum{s_sum[group], 0, 1 + group};
+    GroupSum<kGroup> sum{s_sum[group], 0, group};
+    Rows ring{reinterpret_cast<typename Rows::Vec*>(smem_dyn) + threadIdx.x};
     chain_wait();
     chain_release();
-    float acc[4][kNormPer];
+    const T* const X = static_cast<const T*>(P.x);
+    const T* const Y = static_cast<const T*>(P.y);
+    const T* const dH = static_cast<const T*>(P.d_h);
+    const T* const dU = static_cast<const T*>(P.d_u);
+    typename R::Values w_pre;                            // of this thread's columns, for all rows
+    R::param(P.w_pre, t, P.C, 1.f, w_pre);
+    typename R::Values acc[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int e = 0; e < kNormPer; ++e) acc[k][e] = 0.f;
+        for (int p = 0; p < kPairs; ++p) acc[k][p] = both(0.f);
+    const Pair scale = both(P.scale);
     // sums k0 and k0 + 1 of all groups to row `at` of their partial sums
     auto flush = [&](int k0, int at) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float (&a)[kNormPer] = acc[k0 + k];
+        for (int k = 0; k < (kLayer ? 2 : 1); ++k) {
+            typename R::Values& a = acc[k0 + k];
             if (kGroups > 1) {
                 __syncthreads();
 #pragma unroll
-                for (int e = 0; e < kNormPer; ++e) s_cols[group][e * kGroup + t] = a[e];
+                for (int p = 0; p < kPairs; ++p) s_cols[group][p * kGroup + t] = a[p];
                 __syncthreads();
                 if (group == 0) {
 #pragma unroll 1
                     for (int g = 1; g < kGroups; ++g)
 #pragma unroll
-                        for (int e = 0; e < kNormPer; ++e) a[e] += s_cols[g][e * kGroup + t];
+                        for (int p = 0; p < kPairs; ++p) a[p] = add2(a[p], s_cols[g][p * kGroup + t]);
                 }
             }
             if (group == 0) R::param_store(P.partial + (static_cast<size_t>(k0 == 0 ? k * P.slots : 2 * P.slots + k * gridDim.x) + at) * P.C, t, P.C, a);
 #pragma unroll
-            for (int e = 0; e < kNormPer; ++e) a[e] = 0.f;
+            for (int p = 0; p < kPairs; ++p) a[p] = both(0.f);
         }
     };
 #pragma unroll 1
     for (int unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
         const int b = unit / P.splits, srow = P.S > 1 ? b : 0;
-        const int n = P.n_sel ? P.n_sel[srow] : P.N;
-        const int32_t* sel = P.sel_idx ? P.sel_idx + static_cast<size_t>(srow) * P.N : nullptr;
-        const float* gate = P.gate ? P.gate + static_cast<size_t>(P.gate_rows > 1 ? b : 0) * P.C : nullptr;
-        const int first = (unit - b * P.splits) * kGroups + group, step = P.splits * kGroups;
-        if (sel) {                                       // rows of dropped tokens
-            const float zero[kNormPer] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const RowWalk walk{P.sel_idx ? P.sel_idx + static_cast<size_t>(srow) * P.N : nullptr, P.n_sel ? P.n_sel[srow] : P.N, P.splits * kGroups};
+        const size_t base = static_cast<size_t>(b) * P.N;
+        const int first = (unit - b * P.splits) * kGroups + group;
+        typename R::Values w, c;                         // N_post's scale and bias with the gate in them
+        {
+            typename R::Values g;
+            R::param(P.gate ? P.gate + static_cast<size_t>(P.gate_rows > 1 ? b : 0) * P.C : nullptr, t, P.C, 1.f, g);
+            R::param(P.w_post, t, P.C, 1.f, w);
+            if (kLayer) R::param(P.b_post, t, P.C, 0.f, c);
+#pragma unroll
+            for (int p = 0; p < kPairs; ++p) {
+                w[p] = mul2(w[p], g[p]);
+                if (kLayer) c[p] = mul2(c[p], g[p]);
+            }
+        }
+        int ahead = first, stage = 0, source = walk.source(first), from = source;
+        float4 st = first < walk.n ? __ldg(P.stats + base + first) : make_float4(0.f, 0.f, 0.f, 0.f);
+        auto fetch = [&](int to) {
+            if (ahead < walk.n) {
+                const size_t row = (base + ahead) * P.C;
+                ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
+                ring.fetch(to, 1, Y ? Y + row : nullptr, t, P.C);
+                ring.fetch(to, 2, dH ? dH + row : nullptr, t, P.C);
+                ring.fetch(to, 3, dU ? dU + row : nullptr, t, P.C);
+            }
+            ring.commit();
+            ahead += walk.step;
+            source = walk.source(ahead);
+        };
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) fetch(s);
+        if (walk.sel) {                                  // rows of dropped tokens, while the first ones come in
+            typename R::Values zero;
+#pragma unroll
+            for (int p = 0; p < kPairs; ++p) zero[p] = both(0.f);
+            // (a look at one token at a time is a chain of loads: a warp looks at 32)
+            const int lane = threadIdx.x & 31;
 #pragma unroll 1
-            for (int i = first; i < P.N; i += step)
-                if (P.inv_idx[static_cast<size_t>(srow) * P.N + i] < 0) R::store(static_cast<T*>(P.dx) + (static_cast<size_t>(b) * P.N + i) * P.C, t, P.C, zero);
+            for (int i0 = first; i0 < P.N; i0 += 32 * walk.step) {
+                const long long mine = i0 + static_cast<long long>(lane) * walk.step;
+                unsigned dropped = __ballot_sync(0xffffffffu, mine < P.N && __ldg(P.inv_idx + static_cast<size_t>(srow) * P.N + (mine < P.N ? mine : 0)) < 0);
+#pragma unroll 1
+                for (; dropped; dropped &= dropped - 1)
+                    R::store(static_cast<T*>(P.dx) + (base + i0 + static_cast<size_t>(__ffs(dropped) - 1) * walk.step) * P.C, t, P.C, zero);
+            }
         }
 #pragma unroll 1
-        for (int i = first; i < n; i += step) {
-            const size_t row = (static_cast<size_t>(b) * P.N + i) * P.C;
-            const size_t from = sel ? (static_cast<size_t>(b) * P.N + sel[i]) * P.C : row;
-            const float4 st = P.stats[static_cast<size_t>(b) * P.N + i];
-            typename R::Vec v[R::kVecs];
-            float h[kNormPer], zy[kNormPer], g[kNormPer], d[kNormPer], w[kNormPer];
-            R::load(static_cast<const T*>(P.x) + from, t, P.C, v);
-            R::floats(v, h);
+        for (int i = first; i < walk.n; i += walk.step) {
+            fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
+            // of the next row, ahead of the wait
+            const int from_next = walk.source(i + walk.step);
+            const float4 st_next = i + walk.step < walk.n ? __ldg(P.stats + base + i + walk.step) : st;
+            ring.wait();
+            const size_t row = (base + i) * P.C;
+            typename R::Values h, zy, d;
+            ring.read(stage, 0, X + (base + from) * P.C, t, P.C, h);
 #pragma unroll
-            for (int e = 0; e < kNormPer; ++e) h[e] *= P.scale;
-            R::param(gate, t, P.C, 1.f, g);
-            if (P.y) {
-                R::load(static_cast<const T*>(P.y) + row, t, P.C, v);
-                R::floats(v, zy);
-                float bias[kNormPer];
-                R::param(P.w_post, t, P.C, 1.f, w);
-                R::param(P.b_post, t, P.C, 0.f, bias);
-                if (P.post) {
+            for (int p = 0; p < kPairs; ++p) h[p] = mul2(h[p], scale);
+            if (Y) {
+                ring.read(stage, 1, Y + row, t, P.C, zy);
+                const Pair r = both(st.y), minus = both(-st.x);
 #pragma unroll
-                    for (int e = 0; e < kNormPer; ++e) zy[e] = (zy[e] - st.x) * st.y;
+                for (int p = 0; p < kPairs; ++p) {
+                    if (kLayer) zy[p] = add2(zy[p], minus);
+                    zy[p] = mul2(zy[p], r);
+                    if (kLayer) h[p] = add2(h[p], c[p]);
+                    h[p] = fma2(zy[p], w[p], h[p]);
                 }
-#pragma unroll
-                for (int e = 0; e < kNormPer; ++e) h[e] = fmaf(g[e], fmaf(zy[e], w[e], bias[e]), h[e]);
             }
-            if (P.d_h) {
-                R::load(static_cast<const T*>(P.d_h) + row, t, P.C, v);
-                R::floats(v, d);
+            if (dH) {
+                ring.read(stage, 2, dH + row, t, P.C, d);
             } else {
 #pragma unroll
-                for (int e = 0; e < kNormPer; ++e) d[e] = 0.f;
+                for (int p = 0; p < kPairs; ++p) d[p] = both(0.f);
             }
             if (P.pre) {
-                float du[kNormPer], wp[kNormPer];
-                R::load(static_cast<const T*>(P.d_u) + row, t, P.C, v);
-                R::floats(v, du);
-                R::param(P.w_pre, t, P.C, 1.f, wp);
-                float s0 = 0.f, s1 = 0.f;
+                typename R::Values du;
+                ring.read(stage, 3, dU + row, t, P.C, du);
+                Pair s0 = both(0.f), s1 = both(0.f);
+                const Pair r = both(st.w), minus = both(-st.z);
 #pragma unroll
-                for (int e = 0; e < kNormPer; ++e) {
-                    h[e] = (h[e] - st.z) * st.w;         // (where no column is, du is 0)
-                    acc[2][e] += du[e] * h[e];
-                    acc[3][e] += du[e];
-                    du[e] *= wp[e];
-                    s0 += du[e] * h[e];
-                    s1 += du[e];
+                for (int p = 0; p < kPairs; ++p) {
+                    if (kLayer) h[p] = add2(h[p], minus);
+                    h[p] = mul2(h[p], r);                // (where no column is, du is 0)
+                    acc[2][p] = fma2(du[p], h[p], acc[2][p]);
+                    if (kLayer) acc[3][p] = add2(acc[3][p], du[p]);
+                    du[p] = mul2(du[p], w_pre[p]);
+                    s0 = fma2(du[p], h[p], s0);
+                    if (kLayer) s1 = add2(s1, du[p]);
                 }
-                const float2 s = sum(s0, s1);
-                const float m0 = s.x * P.inv_c, m1 = P.pre == 2 ? s.y * P.inv_c : 0.f;
+                const float2 s = sum.template of<kLayer>(sum_of(s0), kLayer ? sum_of(s1) : 0.f);
+                const Pair m0 = both(-s.x * P.inv_c), m1 = both(kLayer && P.pre == 2 ? -s.y * P.inv_c : 0.f);
 #pragma unroll
-                for (int e = 0; e < kNormPer; ++e) d[e] = fmaf(st.w, du[e] - m1 - h[e] * m0, d[e]);
+                for (int p = 0; p < kPairs; ++p) {
+                    if (kLayer) du[p] = add2(du[p], m1);
+                    d[p] = fma2(r, fma2(h[p], m0, du[p]), d[p]);
+                }
             }
-            float out[kNormPer];
+            typename R::Values out;
 #pragma unroll
-            for (int e = 0; e < kNormPer; ++e) out[e] = P.scale * d[e];
-            R::store(static_cast<T*>(P.dx) + from, t, P.C, out);
-            if (P.y) {
-                float s0 = 0.f, s1 = 0.f;
+            for (int p = 0; p < kPairs; ++p) out[p] = mul2(scale, d[p]);
+            R::store(static_cast<T*>(P.dx) + (base + from) * P.C, t, P.C, out);
+            if (Y) {
+                Pair s0 = both(0.f), s1 = both(0.f);
 #pragma unroll
-                for (int e = 0; e < kNormPer; ++e) {
-                    acc[0][e] += d[e] * zy[e];
-                    acc[1][e] += d[e];
-                    d[e] *= g[e];
+                for (int p = 0; p < kPairs; ++p) {
+                    acc[0][p] = fma2(d[p], zy[p], acc[0][p]);
+                    if (kLayer) acc[1][p] = add2(acc[1][p], d[p]);
+                    d[p] = mul2(d[p], w[p]);             // (0 where no column is)
                 }
                 if (P.post) {
-                    R::param(P.w_post, t, P.C, 1.f, w);
 #pragma unroll
-                    for (int e = 0; e < kNormPer; ++e) {
-                        d[e] *= w[e];                    // (0 where no column is)
-                        s0 += d[e] * zy[e];
-                        s1 += d[e];
+                    for (int p = 0; p < kPairs; ++p) {
+                        s0 = fma2(d[p], zy[p], s0);
+                        if (kLayer) s1 = add2(s1, d[p]);
                     }
-                    const float2 s = sum(s0, s1);
-                    const float m0 = s.x * P.inv_c, m1 = P.post == 2 ? s.y * P.inv_c : 0.f;
+                    const float2 s = sum.template of<kLayer>(sum_of(s0), kLayer ? sum_of(s1) : 0.f);
+                    const Pair m0 = both(-s.x * P.inv_c), m1 = both(kLayer && P.post == 2 ? -s.y * P.inv_c : 0.f), r = both(st.y);
 #pragma unroll
-                    for (int e = 0; e < kNormPer; ++e) d[e] = st.y * (d[e] - m1 - zy[e] * m0);
+                    for (int p = 0; p < kPairs; ++p) {
+                        if (kLayer) d[p] = add2(d[p], m1);
+                        d[p] = mul2(r, fma2(zy[p], m0, d[p]));
+                    }
                 }
                 R::store(static_cast<T*>(P.dy) + row, t, P.C, d);
             }
+            from = from_next;
+            st = st_next;
+            if (++stage == Rows::kStages) stage = 0;
         }
         if (P.gate_rows > 1) flush(0, unit);
     }
@@ -369,43 +584,50 @@ struct ParamsParams {
     const float* partial;
     const float *gate, *w_post, *b_post;
     float *d_gate, *d_w_post, *d_b_post, *d_w_pre, *d_b_pre;
-    int B, C, gate_rows, splits, slots, ctas;
+    int B, C, gate_rows, splits, slots, ctas, layer;
 };
 constexpr int kColsX = 32, kColsY = 32;
-// Blocks (x, 0): 32 columns of the sums over all tokens; (x, 1 + b): of an instance's gate.  32 rows at a time, then across them, in a fixed order.
+// Blocks (x, 0): 32 columns of the first two sums over all tokens; (x, 1): of the last two; (x, 2 + k): of the gates of instances 32 k to 32 k + 31.  32 rows at a time,
+// then across them, in a fixed order.
 __global__ void __launch_bounds__(kColsX * kColsY) norm_params_kernel(const ParamsParams P) {
-    __shared__ float s[4][kColsY][kColsX + 1];
+    __shared__ float s[2][kColsY][kColsX + 1];
     chain_wait();
     chain_release();
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * kColsX + x;
-    const bool there = c < P.C;
-    const bool one = blockIdx.y == 0, per = P.gate_rows > 1;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    const float* A = P.partial + c;
-    const float* Tt = A + static_cast<size_t>(P.slots) * P.C;
-    const float* U = Tt + static_cast<size_t>(P.slots) * P.C;
-    const float* V = U + static_cast<size_t>(P.ctas) * P.C;
-    if (there && one) {
-        for (int r = y; r < P.slots; r += kColsY) {
-            const float g = per ? __ldg(P.gate + static_cast<size_t>(r / P.splits) * P.C + c) : 1.f;
-            v[0] += g * A[static_cast<size_t>(r) * P.C];
-            v[1] += g * Tt[static_cast<size_t>(r) * P.C];
+    const bool there = c < P.C, per = P.gate_rows > 1;
+    const size_t C = P.C;
+    if (blockIdx.y >= 2) {
+        const int b = (blockIdx.y - 2) * kColsY + y;
+        if (!there || b >= P.gate_rows) return;
+        const float w = P.w_post ? __ldg(P.w_post + c) : 1.f, bias = P.b_post ? __ldg(P.b_post + c) : 0.f;
+        const float* A = P.partial + static_cast<size_t>(b) * P.splits * C + c;
+        const float* T = A + P.slots * C;
+        float a = 0.f, t = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < P.splits; ++r) {
+            a += A[r * C];
+            if (P.layer) t += T[r * C];
         }
-        for (int r = y; r < P.ctas; r += kColsY) {
-            v[2] += U[static_cast<size_t>(r) * P.C];
-            v[3] += V[static_cast<size_t>(r) * P.C];
-        }
-    } else if (there) {
-        const int b = blockIdx.y - 1;
-        for (int r = b * P.splits + y; r < (b + 1) * P.splits; r += kColsY) {
-            v[0] += A[static_cast<size_t>(r) * P.C];
-            v[1] += Tt[static_cast<size_t>(r) * P.C];
+        P.d_gate[b * C + c] = fmaf(w, a, bias * t);
+        return;
+    }
+    const bool last = blockIdx.y == 1;
+    const int rows = last ? P.ctas : P.slots;
+    const float* A = P.partial + (last ? 2 * P.slots * C : 0) + c;
+    const float* T = A + rows * C;
+    float v0 = 0.f, v1 = 0.f;
+    if (there) {
+#pragma unroll 8
+        for (int r = y; r < rows; r += kColsY) {
+            const float g = !last && per ? __ldg(P.gate + static_cast<size_t>(r / P.splits) * C + c) : 1.f;
+            v0 += g * A[r * C];
+            if (P.layer) v1 += g * T[r * C];
         }
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s[k][y][x] = v[k];
+    s[0][y][x] = v0;
+    s[1][y][x] = v1;
     __syncthreads();
-    if (y < 4) {
+    if (y < 2) {
         float sum = 0.f;
 #pragma unroll
         for (int r = 0; r < kColsY; ++r) sum += s[y][r][x];
@@ -414,28 +636,26 @@ __global__ void __launch_bounds__(kColsX * kColsY) norm_params_kernel(const Para
     __syncthreads();
     if (y != 0 || !there) return;
     const float a = s[0][0][x], t = s[1][0][x];
-    const float w = P.w_post ? P.w_post[c] : 1.f, bias = P.b_post ? P.b_post[c] : 0.f;
-    if (!one) {
-        P.d_gate[static_cast<size_t>(blockIdx.y - 1) * P.C + c] = fmaf(w, a, bias * t);
+    if (last) {
+        if (P.d_w_pre) P.d_w_pre[c] = a;
+        if (P.d_b_pre) P.d_b_pre[c] = t;
         return;
     }
     const float g = P.gate && !per ? P.gate[c] : 1.f;
-    if (P.d_gate && !per) P.d_gate[c] = fmaf(w, a, bias * t);
+    if (P.d_gate && !per) P.d_gate[c] = fmaf(P.w_post ? P.w_post[c] : 1.f, a, (P.b_post ? P.b_post[c] : 0.f) * t);
     if (P.d_w_post) P.d_w_post[c] = g * a;
     if (P.d_b_post) P.d_b_post[c] = g * t;
-    if (P.d_w_pre) P.d_w_pre[c] = s[2][0][x];
-    if (P.d_b_pre) P.d_b_pre[c] = s[3][0][x];
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
-int group_of(int C) {
+int group_of(int C, int per) {
     int g = 32;
-    while (g * kNormPer < C) g *= 2;
+    while (g * per < C) g *= 2;
     return g;
 }
 // CTAs that share an instance's tokens, as many as keep every SM's places taken without a second round, but none without a token.
-void shares(const vardrop_norm_cfg& c, int per_sm, int& splits, int& grid) {
-    const int group = group_of(c.C), threads = group < 256 ? 256 : group, groups = threads / group;
+void shares(const vardrop_norm_cfg& c, int per, int per_sm, int& splits, int& grid) {
+    const int group = group_of(c.C, per), threads = group < 256 ? 256 : group, groups = threads / group;
     const int places = sm_count() * per_sm * 256 / threads;
     const int most = (c.N + groups - 1) / groups;
     splits = places / c.B;
@@ -445,30 +665,69 @@ void shares(const vardrop_norm_cfg& c, int per_sm, int& splits, int& grid) {
     grid = static_cast<int>(units < places ? units : places);
     if (grid < 1) grid = 1;
 }
-constexpr int kFwdPerSm = 6, kBwdPerSm = 2;              // CTAs of 256 threads
+constexpr int kFwdPerSm = 2, kBwdPerSm = 2;              // CTAs of 256 threads that an SM holds
 
-template <class T, int kV, int kGroup>
-cudaError_t launch(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
-    constexpr int kThreads = kNormThreads<kGroup>;
-    return bwd ? launch_chained(norm_bwd_kernel<T, kV, kGroup>, dim3(grid), dim3(kThreads), 0, s, P) : launch_chained(norm_fwd_kernel<T, kV, kGroup>, dim3(grid), dim3(kThreads), 0, s, P);
+// Allows a kernel its dynamic shared memory where that is above what every kernel may take.
+template <class K>
+cudaError_t allow_smem(K kernel, int bytes, int& attr_dev) {
+    if (bytes <= 40 * 1024) return cudaSuccess;
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess || attr_dev == dev) return err;
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (err == cudaSuccess) attr_dev = dev;
+    return err;
 }
-template <class T, int kV>
+template <class T, int kV, int kGroup, bool kLayer>
+cudaError_t launch(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
+    if (bwd) {
+        constexpr int kBytes = Ring<T, kV, kGroup, kBwdPer, 4>::kBytes;
+        static thread_local int attr_dev = -1;
+        if (cudaError_t err = allow_smem(norm_bwd_kernel<T, kV, kGroup, kLayer>, kBytes, attr_dev)) return err;
+        return launch_chained(norm_bwd_kernel<T, kV, kGroup, kLayer>, dim3(grid), dim3(kNormThreads<kGroup>), kBytes, s, P);
+    }
+    if constexpr (kGroup * kFwdPer <= kNormMaxC) {
+        constexpr int kBytes = Ring<T, kV, kGroup, kFwdPer, 2>::kBytes;
+        static thread_local int attr_dev = -1;
+        if (cudaError_t err = allow_smem(norm_fwd_kernel<T, kV, kGroup, kLayer>, kBytes, attr_dev)) return err;
+        return launch_chained(norm_fwd_kernel<T, kV, kGroup, kLayer>, dim3(grid), dim3(kNormThreads<kGroup>), kBytes, s, P);
+    }
+    return cudaErrorInvalidValue;
+}
+template <class T, int kV, bool kLayer>
 cudaError_t launch_group(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
-    switch (group_of(P.C)) {
-        case 32: return launch<T, kV, 32>(bwd, grid, P, s);
-        case 64: return launch<T, kV, 64>(bwd, grid, P, s);
-        case 128: return launch<T, kV, 128>(bwd, grid, P, s);
-        case 256: return launch<T, kV, 256>(bwd, grid, P, s);
-        case 512: return launch<T, kV, 512>(bwd, grid, P, s);
-        default: return launch<T, kV, 1024>(bwd, grid, P, s);
+    switch (group_of(P.C, bwd ? kBwdPer : kFwdPer)) {
+        case 32: return launch<T, kV, 32, kLayer>(bwd, grid, P, s);
+        case 64: return launch<T, kV, 64, kLayer>(bwd, grid, P, s);
+        case 128: return launch<T, kV, 128, kLayer>(bwd, grid, P, s);
+        case 256: return launch<T, kV, 256, kLayer>(bwd, grid, P, s);
+        case 512: return launch<T, kV, 512, kLayer>(bwd, grid, P, s);
+        default: return launch<T, kV, 1024, kLayer>(bwd, grid, P, s);
     }
 }
-// Vectors of 16 bytes where every row begins on such a boundary, single elements otherwise.
+template <class T, int kV>
+cudaError_t launch_layer(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
+    return P.pre == 2 || P.post == 2 ? launch_group<T, kV, true>(bwd, grid, P, s) : launch_group<T, kV, false>(bwd, grid, P, s);
+}
+// Vectors as wide as the beginnings of all rows allow: 16 bytes, 4 bytes, a 16-bit element.
+template <class T>
+cudaError_t launch_16bit(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
+    return P.C % 8 == 0 ? launch_layer<T, 8>(bwd, grid, P, s) : P.C % 2 == 0 ? launch_layer<T, 2>(bwd, grid, P, s) : launch_layer<T, 1>(bwd, grid, P, s);
+}
 cudaError_t launch_type(bool bwd, int dtype, int grid, const NormParams& P, cudaStream_t s) {
-    const bool wide = P.C % (dtype == 2 ? 4 : 8) == 0;
-    if (dtype == 0) return wide ? launch_group<__nv_bfloat16, 8>(bwd, grid, P, s) : launch_group<__nv_bfloat16, 1>(bwd, grid, P, s);
-    if (dtype == 1) return wide ? launch_group<__half, 8>(bwd, grid, P, s) : launch_group<__half, 1>(bwd, grid, P, s);
-    return wide ? launch_group<float, 4>(bwd, grid, P, s) : launch_group<float, 1>(bwd, grid, P, s);
+    if (dtype == 0) return launch_16bit<__nv_bfloat16>(bwd, grid, P, s);
+    if (dtype == 1) return launch_16bit<__half>(bwd, grid, P, s);
+    return P.C % 4 == 0 ? launch_layer<float, 4>(bwd, grid, P, s) : launch_layer<float, 1>(bwd, grid, P, s);
+}
+// Where neither a gate nor a selection tells instances apart, all tokens are one's: no CTA is left without a share of an instance.
+vardrop_norm_cfg flat(const vardrop_norm_cfg& c, bool selected) {
+    vardrop_norm_cfg f = c;
+    if (!selected && c.gate_rows <= 1) {
+        f.N = c.B * c.N;
+        f.B = 1;
+        f.S = 0;
+    }
+    return f;
 }
 NormParams params_of(const vardrop_norm_cfg& c, const int32_t* sel_idx, int splits) {
     NormParams P{};
@@ -495,9 +754,10 @@ int norm_validate(const vardrop_norm_cfg& c) {
 }
 
 int norm_fwd_launch(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const float* b_pre, const int32_t* sel_idx,
-                    const int32_t* n_sel, const vardrop_norm_cfg& c, void* h, void* u, float* stats, cudaStream_t stream) {
+                    const int32_t* n_sel, const vardrop_norm_cfg& cfg, void* h, void* u, float* stats, cudaStream_t stream) {
+    const vardrop_norm_cfg c = flat(cfg, sel_idx != nullptr);
     int splits, grid;
-    shares(c, kFwdPerSm, splits, grid);
+    shares(c, kFwdPer, kFwdPerSm, splits, grid);
     NormParams P = params_of(c, sel_idx, splits);
     P.x = x; P.y = y; P.gate = gate; P.w_post = w_post; P.b_post = b_post; P.w_pre = w_pre; P.b_pre = b_pre;
     P.sel_idx = sel_idx; P.n_sel = sel_idx ? n_sel : nullptr;
@@ -506,18 +766,24 @@ int norm_fwd_launch(const void* x, const void* y, const float* gate, const float
     return check_cuda(launch_type(false, c.dtype, grid, P, stream), "norm: forward launch");
 }
 
-size_t norm_workspace_bytes(const vardrop_norm_cfg& c) {
-    int splits, grid;
-    shares(c, kBwdPerSm, splits, grid);
-    const size_t slots = c.gate_rows > 1 ? static_cast<size_t>(c.B) * splits : grid;
-    return kWsHeaderBytes + align_up(sizeof(float) * 2 * (slots + grid) * c.C, 256);
+size_t norm_workspace_bytes(const vardrop_norm_cfg& cfg) {
+    size_t most = 0;
+    for (const bool selected : {false, true}) {          // the query does not say
+        const vardrop_norm_cfg c = flat(cfg, selected);
+        int splits, grid;
+        shares(c, kBwdPer, kBwdPerSm, splits, grid);
+        const size_t slots = c.gate_rows > 1 ? static_cast<size_t>(c.B) * splits : grid, rows = 2 * (slots + grid);
+        most = rows > most ? rows : most;
+    }
+    return kWsHeaderBytes + align_up(sizeof(float) * most * cfg.C, 256);
 }
 
 int norm_bwd_launch(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const int32_t* sel_idx, const int32_t* n_sel,
-                    const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg& c, void* dx, void* dy, float* d_gate, float* d_w_post,
+                    const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg& cfg, void* dx, void* dy, float* d_gate, float* d_w_post,
                     float* d_b_post, float* d_w_pre, float* d_b_pre, void* ws, cudaStream_t stream) {
+    const vardrop_norm_cfg c = flat(cfg, sel_idx != nullptr);
     int splits, grid;
-    shares(c, kBwdPerSm, splits, grid);
+    shares(c, kBwdPer, kBwdPerSm, splits, grid);
     NormParams P = params_of(c, sel_idx, splits);
     P.x = x; P.y = y; P.gate = gate; P.w_post = w_post; P.b_post = b_post; P.w_pre = w_pre;
     P.sel_idx = sel_idx; P.n_sel = sel_idx ? n_sel : nullptr; P.inv_idx = sel_idx ? inv_idx : nullptr;
@@ -530,9 +796,9 @@ int norm_bwd_launch(const void* x, const void* y, const float* gate, const float
         if (int st = check_cuda(launch_type(true, c.dtype, grid, P, stream), "norm: backward launch")) return st;
     }
     if (!d_gate && !d_w_post && !d_b_post && !d_w_pre && !d_b_pre) return VARDROP_OK;
-    ParamsParams Q{P.partial, gate, w_post, b_post, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, c.B, c.C, c.gate_rows, splits, P.slots, grid};
+    ParamsParams Q{P.partial, gate, w_post, b_post, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, c.B, c.C, c.gate_rows, splits, P.slots, grid, c.pre == 2 || c.post == 2};
     LaunchScope ls_(K_NORM_PARAMS, stream);
-    return check_cuda(launch_chained(norm_params_kernel, dim3((c.C + kColsX - 1) / kColsX, 1 + (d_gate && c.gate_rows > 1 ? c.gate_rows : 0)), dim3(kColsX * kColsY), 0, stream, Q),
+    return check_cuda(launch_chained(norm_params_kernel, dim3((c.C + kColsX - 1) / kColsX, 2 + (d_gate && c.gate_rows > 1 ? (c.gate_rows + kColsY - 1) / kColsY : 0)), dim3(kColsX * kColsY), 0, stream, Q),
                       "norm: parameters' gradients launch");
 }
 
