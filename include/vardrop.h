@@ -371,10 +371,11 @@ int vardrop_norm_bwd(const void* x, const void* y, const float* gate, const floa
 /* ------------------------------------------------------------------------------------------------
  * Global gradient norm over many tensors, and clipping (the end of a training step; no counterpart in the paper):
  *   norm = sqrt(sum over all tensors and elements of g^2);   out = g min(1, max_norm / (norm + eps))
- * Squares and sums in fp64, in a fixed order (bit-reproducible); products rounded once to the tensor's type.
+ * Sums in fp64, in a fixed order (bit-reproducible; two neighbouring squares are added in fp32 where that leaves no range); products rounded once to the tensor's type.
  *
  * tensors     (host) [count] of device pointers, element counts (>= 0) and types (0 bf16, 1 fp16, 2 fp32); read before the call returns.  `in` and `out` need the
- *             alignment of their element only; out = in clips in place, otherwise they must not overlap.  count <= 16384.
+ *             alignment of their element only; out = in clips in place, otherwise they must not overlap, nor any two outputs.
+ *             count <= 16384.
  * cfg (host)  max_norm: 0 takes the norm only (no `out` is touched); eps >= 0.
  * norm        [1] fp32 out.
  * ws          scratch of vardrop_grad_clip_workspace_bytes.

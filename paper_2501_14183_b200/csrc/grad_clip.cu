@@ -7,6 +7,10 @@
 // Bound: memory.  The tensors are read twice, as far as they do not fit the L2 cache, and written once.
 #include <cuda_fp16.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "common.cuh"
 #include "kernels.h"
 
@@ -15,7 +19,7 @@ namespace vardrop {
 namespace {
 
 constexpr int kClipThreads = 256;
-constexpr int kClipPerSm = 8;
+constexpr int kClipPerSm = 8, kScalePerSm = 4;       // CTAs that an SM holds (the scaling one keeps a chunk in registers while it waits for the norm)
 constexpr int kClipMaxGrid = 2048;          // partial sums of a launch
 constexpr int kClipFew = 64, kClipMany = 1024;      // table entries of a launch: the small one's parameters are 1.9 KB, the large one's 29 KB of the 32 KB a launch may take
 constexpr int kClipLoads = 4;               // 16-byte vectors a thread has in flight
@@ -109,14 +113,44 @@ __device__ __forceinline__ double block_sum(double v, double* s_warp) {      // 
     return sum;
 }
 
-// Squares in fp64: fp32 ones leave its range at 2^64 and at 2^-63, far inside that of a gradient.
+// The squares of a 16-byte vector.  Conversions to fp64 run at 16 a cycle and SM, one an element would take 240 us of the 335 that the memory needs for 1.08e9 bf16 values (444
+// us together): two squares are added in fp32, at two roundings, wherever both the sums are far inside its range, which squares leave at gradients of 2^64 and 2^-63.
+__device__ __forceinline__ double squares(const uint4& v, int dtype) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (dtype == 2) {
+        const float a = __uint_as_float(w[0]), b = __uint_as_float(w[1]), c = __uint_as_float(w[2]), d = __uint_as_float(w[3]);
+        const float s = fmaf(a, a, b * b), t = fmaf(c, c, d * d);
+        if (fminf(s, t) > 1e-30f && fmaxf(s, t) < 1e30f) return static_cast<double>(s) + static_cast<double>(t);
+        const double A = a, B = b, C = c, D = d;         // (NaN compares false; zeros come here too)
+        return fma(A, A, B * B) + fma(C, C, D * D);
+    }
+    float s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = two_of(w[i], dtype);
+        s[i] = fmaf(x.x, x.x, x.y * x.y);
+    }
+    const float least = fminf(fminf(s[0], s[1]), fminf(s[2], s[3])), most = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    if (least > 1e-30f && most < 1e30f) {
+        return (static_cast<double>(s[0]) + static_cast<double>(s[1])) + (static_cast<double>(s[2]) + static_cast<double>(s[3]));
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = two_of(w[i], dtype);
+        const double a = x.x, b = x.y;
+        sum += fma(a, a, b * b);
+    }
+    return sum;
+}
+
 template <int kMax>
 __global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_norm_kernel(const __grid_constant__ ClipTable<kMax> P) {
     __shared__ double s_warp[kClipThreads / 32];
     chain_wait();
     chain_release();
     const int chunks = P.first[P.count];
-    double sum[2] = {0.0, 0.0};
+    double sum = 0.0;
 #pragma unroll 1
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         const Chunk k = chunk_at(P, c);
@@ -125,29 +159,27 @@ __global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_norm_kernel(con
 #pragma unroll
         for (int j = 0; j < kClipLoads; ++j) v[j] = load_vector(k, k.begin + (static_cast<long long>(j * kClipThreads + threadIdx.x) << (4 - k.elem_log2)));
 #pragma unroll
-        for (int j = 0; j < kClipLoads; ++j) {
-            const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (dtype == 2) {
-                    const double a = __uint_as_float(w[i]);
-                    sum[i & 1] = fma(a, a, sum[i & 1]);
-                } else {
-                    const float2 x = two_of(w[i], dtype);
-                    const double a = x.x, b = x.y;
-                    sum[0] = fma(a, a, sum[0]);
-                    sum[1] = fma(b, b, sum[1]);
-                }
-            }
-        }
+        for (int j = 0; j < kClipLoads; ++j) sum += squares(v[j], dtype);
     }
-    const double total = block_sum(sum[0] + sum[1], s_warp);
+    const double total = block_sum(sum, s_warp);
     if (threadIdx.x == 0) P.partial[P.base + blockIdx.x] = total;
 }
 
 template <int kMax>
-__global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_scale_kernel(const __grid_constant__ ClipTable<kMax> P) {
+__global__ void __launch_bounds__(kClipThreads, kScalePerSm) grad_scale_kernel(const __grid_constant__ ClipTable<kMax> P) {
     __shared__ double s_warp[kClipThreads / 32];
+    // The first chunk is on its way while the norm is still being taken: the launch before this one is always this library's grad_norm_kernel (or a scaling of other tensors), which
+    // writes no gradient and lets dependents in behind its own wait only, so whatever made the gradients has completed.
+    const int chunks = P.max_norm == 0.f ? 0 : P.first[P.count];
+    auto fetch = [&](int c, Chunk& k, uint4 (&v)[kClipLoads]) {
+        k = chunk_at(P, c);
+#pragma unroll
+        for (int j = 0; j < kClipLoads; ++j) v[j] = load_vector(k, k.begin + (static_cast<long long>(j * kClipThreads + threadIdx.x) << (4 - k.elem_log2)));
+    };
+    int c = chunks - 1 - static_cast<int>(blockIdx.x);      // from the end: what the norm's pass read last is in L2
+    Chunk k{};
+    uint4 v[kClipLoads];
+    if (c >= 0) fetch(c, k, v);
     chain_wait();
     chain_release();
     double sum = 0.0;
@@ -158,25 +190,19 @@ __global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_scale_kernel(co
         *P.norm = static_cast<float>(norm);
         if (!finite) set_status(P.status, VARDROP_ERR_NONFINITE);
     }
-    if (P.max_norm == 0.f) return;
     const double ratio = P.max_norm / (norm + P.eps);
     const float factor = finite && ratio < 1.0 ? static_cast<float>(ratio) : 1.f;
-    const int chunks = P.first[P.count];
-    // from the end: what the norm's pass read last is in L2
 #pragma unroll 1
-    for (int c = chunks - 1 - static_cast<int>(blockIdx.x); c >= 0; c -= gridDim.x) {
-        const Chunk k = chunk_at(P, c);
+    while (c >= 0) {
         const int dtype = P.dtype[k.tensor];
         unsigned char* out = static_cast<unsigned char*>(P.out[k.tensor]);
-        if (factor == 1.f && out == P.in[k.tensor]) continue;
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(P.in[k.tensor])) & 15) == 0;
+        const bool skip = factor == 1.f && out == P.in[k.tensor];
         out -= k.from << k.elem_log2;                   // of virtual element 0
         const int per = 16 >> k.elem_log2;
-        uint4 v[kClipLoads];
-#pragma unroll
-        for (int j = 0; j < kClipLoads; ++j) v[j] = load_vector(k, k.begin + static_cast<long long>(j * kClipThreads + threadIdx.x) * per);
 #pragma unroll
         for (int j = 0; j < kClipLoads; ++j) {
+            if (skip) break;
             const long long e = k.begin + static_cast<long long>(j * kClipThreads + threadIdx.x) * per;
             uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
@@ -203,6 +229,8 @@ __global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_scale_kernel(co
                 }
             }
         }
+        c -= gridDim.x;
+        if (c >= 0) fetch(c, k, v);
     }
 }
 
@@ -223,8 +251,34 @@ int fill(ClipTable<kMax>& P, const vardrop_tensor* tensors, int at, int count) {
     P.first[P.count] = static_cast<int>(chunks);
     return VARDROP_OK;
 }
-int grid_of(int chunks) {
-    const int most = kClipPerSm * sm_count() < kClipMaxGrid ? kClipPerSm * sm_count() : kClipMaxGrid;
+// Two outputs that overlap would be scaled by two CTAs at a time.  Tensors mostly come in the order of their addresses, where a look at neighbours is enough.
+int outputs_apart(const vardrop_tensor* tensors, int count) {
+    struct Span { uintptr_t begin, end; };
+    const auto span = [&](int i) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(tensors[i].out);
+        return Span{p, p + (static_cast<uintptr_t>(tensors[i].n) << (tensors[i].dtype == 2 ? 2 : 1))};
+    };
+    uintptr_t last = 0;
+    bool ascending = true;
+    for (int i = 0; i < count && ascending; ++i) {
+        if (tensors[i].n == 0) continue;
+        const Span s = span(i);
+        ascending = s.begin >= last;
+        last = s.end;
+    }
+    if (ascending) return VARDROP_OK;
+    const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[count]);
+    if (!spans) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: no host memory for %d tensors", count);
+    int n = 0;
+    for (int i = 0; i < count; ++i)
+        if (tensors[i].n > 0) spans[n++] = span(i);
+    std::sort(spans.get(), spans.get() + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    for (int i = 1; i < n; ++i)
+        if (spans[i].begin < spans[i - 1].end) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: two outputs overlap");
+    return VARDROP_OK;
+}
+int grid_of(int chunks, int per_sm) {
+    const int most = per_sm * sm_count() < kClipMaxGrid ? per_sm * sm_count() : kClipMaxGrid;
     return chunks < 1 ? 1 : chunks < most ? chunks : most;
 }
 
@@ -239,7 +293,7 @@ int clip_launch(const vardrop_tensor* tensors, int count, const vardrop_clip_cfg
     }
     for (int at = 0; at < count; at += kMax) {
         fill(P, tensors, at, count);
-        const int grid = grid_of(P.first[P.count]);
+        const int grid = grid_of(P.first[P.count], kClipPerSm);
         P.base = P.partials;
         LaunchScope ls_(K_GRAD_NORM, stream);
         if (int st = check_cuda(launch_chained(grad_norm_kernel<kMax>, dim3(grid), dim3(kClipThreads), 0, stream, P), "grad_clip: norm launch")) return st;
@@ -249,7 +303,7 @@ int clip_launch(const vardrop_tensor* tensors, int count, const vardrop_clip_cfg
         fill(P, tensors, at, count);
         P.base = at;
         LaunchScope ls_(K_GRAD_SCALE, stream);
-        if (int st = check_cuda(launch_chained(grad_scale_kernel<kMax>, dim3(cfg.max_norm == 0.f ? 1 : grid_of(P.first[P.count])), dim3(kClipThreads), 0, stream, P), "grad_clip: scale launch")) return st;
+        if (int st = check_cuda(launch_chained(grad_scale_kernel<kMax>, dim3(cfg.max_norm == 0.f ? 1 : grid_of(P.first[P.count], kScalePerSm)), dim3(kClipThreads), 0, stream, P), "grad_clip: scale launch")) return st;
         if (cfg.max_norm == 0.f) break;
     }
     return VARDROP_OK;
@@ -277,7 +331,7 @@ int grad_clip_validate(const vardrop_tensor* tensors, int32_t count, const vardr
         const uintptr_t bytes = static_cast<uintptr_t>(t.n) * (mask + 1);
         if (in != out && in < out + bytes && out < in + bytes) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: output %d overlaps its input", i);
     }
-    return VARDROP_OK;
+    return cfg.max_norm == 0.f ? VARDROP_OK : outputs_apart(tensors, count);
 }
 
 int grad_clip_launch(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg& cfg, float* norm, void* ws, cudaStream_t stream) {

@@ -70,6 +70,8 @@ def test_clip_arguments(lib):
     assert call((GOOD, GOOD + 4, 10, 2)) == call((GOOD + 4, GOOD, 10, 2)) == vd.ERR_INVALID_ARG and b"overlaps" in lib.vardrop_last_error()
     assert call(ok, max_norm=-1.0) == call(ok, max_norm=float("nan")) == call(ok, eps=-1.0) == call(ok, norm=None) == call(ok, count=-1) == vd.ERR_INVALID_ARG
     assert call(*[ok] * 16385) == vd.ERR_UNSUPPORTED
+    apart = [(GOOD + 64 * i, GOOD + 64 * i, 16, 2) for i in range(40)]
+    assert call(*apart, ok) == call(*apart[::-1], (GOOD + 60, GOOD + 60, 2, 0)) == call(ok, ok) == vd.ERR_INVALID_ARG and b"two outputs" in lib.vardrop_last_error()
     assert call(ok, nb=need - 1) == vd.ERR_WORKSPACE
 
 
