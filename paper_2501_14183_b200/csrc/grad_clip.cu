@@ -19,7 +19,7 @@ namespace vardrop {
 namespace {
 
 constexpr int kClipThreads = 256;
-constexpr int kClipPerSm = 8, kScalePerSm = 4;       // CTAs that an SM holds (the scaling one keeps a chunk in registers while it waits for the norm)
+constexpr int kClipPerSm = 4;        // CTAs that an SM holds: 64 registers a thread, for a chunk that is on its way
 constexpr int kClipMaxGrid = 2048;          // partial sums of a launch
 constexpr int kClipFew = 64, kClipMany = 1024;      // table entries of a launch: the small one's parameters are 1.9 KB, the large one's 29 KB of the 32 KB a launch may take
 constexpr int kClipLoads = 4;               // 16-byte vectors a thread has in flight
@@ -89,6 +89,18 @@ __device__ __forceinline__ uint4 load_vector(const Chunk& k, long long e) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// This thread's vectors of a chunk.  Nearly every chunk lies inside its tensor: one look for all of it, and no 64-bit comparison a vector.
+__device__ __forceinline__ bool inside(const Chunk& k) { return k.begin >= k.from && k.begin + (kClipChunkBytes >> k.elem_log2) <= k.to; }
+__device__ __forceinline__ void load_chunk(const Chunk& k, uint4 (&v)[kClipLoads]) {
+    if (inside(k)) {
+        const uint4* p = reinterpret_cast<const uint4*>(k.base + (k.begin << k.elem_log2)) + threadIdx.x;
+#pragma unroll
+        for (int j = 0; j < kClipLoads; ++j) v[j] = p[j * kClipThreads];
+    } else {
+#pragma unroll
+        for (int j = 0; j < kClipLoads; ++j) v[j] = load_vector(k, k.begin + (static_cast<long long>(j * kClipThreads + threadIdx.x) << (4 - k.elem_log2)));
+    }
+}
 __device__ __forceinline__ float2 two_of(uint32_t w, int dtype) {        // of a 16-bit type
     if (dtype == 0) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -115,33 +127,38 @@ __device__ __forceinline__ double block_sum(double v, double* s_warp) {      // 
 
 // The squares of a 16-byte vector.  Conversions to fp64 run at 16 a cycle and SM, one an element would take 240 us of the 335 that the memory needs for 1.08e9 bf16 values (444
 // us together): two squares are added in fp32, at two roundings, wherever both the sums are far inside its range, which squares leave at gradients of 2^64 and 2^-63.
-__device__ __forceinline__ double squares(const uint4& v, int dtype) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if (dtype == 2) {
-        const float a = __uint_as_float(w[0]), b = __uint_as_float(w[1]), c = __uint_as_float(w[2]), d = __uint_as_float(w[3]);
-        const float s = fmaf(a, a, b * b), t = fmaf(c, c, d * d);
-        if (fminf(s, t) > 1e-30f && fmaxf(s, t) < 1e30f) return static_cast<double>(s) + static_cast<double>(t);
-        const double A = a, B = b, C = c, D = d;         // (NaN compares false; zeros come here too)
-        return fma(A, A, B * B) + fma(C, C, D * D);
-    }
-    float s[4];
+template <int kType>
+__device__ __forceinline__ double squares(const uint4 (&v)[kClipLoads]) {
+    constexpr int kSums = kType == 2 ? 2 : 4;
+    double total = 0.0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 x = two_of(w[i], dtype);
-        s[i] = fmaf(x.x, x.x, x.y * x.y);
-    }
-    const float least = fminf(fminf(s[0], s[1]), fminf(s[2], s[3])), most = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    if (least > 1e-30f && most < 1e30f) {
-        return (static_cast<double>(s[0]) + static_cast<double>(s[1])) + (static_cast<double>(s[2]) + static_cast<double>(s[3]));
-    }
-    double sum = 0.0;
+    for (int j = 0; j < kClipLoads; ++j) {
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        float2 x[kSums];
+        float s[kSums];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 x = two_of(w[i], dtype);
-        const double a = x.x, b = x.y;
-        sum += fma(a, a, b * b);
+        for (int i = 0; i < kSums; ++i) {
+            x[i] = kType == 2 ? make_float2(__uint_as_float(w[2 * i % 4]), __uint_as_float(w[2 * i % 4 + 1])) : two_of(w[i], kType);
+            s[i] = fmaf(x[i].x, x[i].x, x[i].y * x[i].y);
+        }
+        float least = s[0], most = s[0];
+#pragma unroll
+        for (int i = 1; i < kSums; ++i) {
+            least = fminf(least, s[i]);
+            most = fmaxf(most, s[i]);
+        }
+        if (least > 1e-30f && most < 1e30f) {
+#pragma unroll
+            for (int i = 0; i < kSums; ++i) total += static_cast<double>(s[i]);
+        } else {                                         // (zeros come here too, and what is not finite: minimum and maximum pass over a NaN, but not its sum)
+#pragma unroll
+            for (int i = 0; i < kSums; ++i) {
+                const double a = x[i].x, b = x[i].y;
+                total += fma(a, a, b * b);
+            }
+        }
     }
-    return sum;
+    return total;
 }
 
 template <int kMax>
@@ -151,30 +168,40 @@ __global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_norm_kernel(con
     chain_release();
     const int chunks = P.first[P.count];
     double sum = 0.0;
-#pragma unroll 1
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+    uint4 v[2][kClipLoads];                 // of this chunk and of the next
+    int dtype[2];
+    auto fetch = [&](int c, int to) {
+        if (c >= chunks) return;
         const Chunk k = chunk_at(P, c);
-        const int dtype = P.dtype[k.tensor];
-        uint4 v[kClipLoads];
+        dtype[to] = P.dtype[k.tensor];
+        load_chunk(k, v[to]);
+    };
+    const int step = gridDim.x;
+    int c = blockIdx.x;
+    fetch(c, 0);
+#pragma unroll 1
+    for (; c < chunks; c += 2 * step) {
 #pragma unroll
-        for (int j = 0; j < kClipLoads; ++j) v[j] = load_vector(k, k.begin + (static_cast<long long>(j * kClipThreads + threadIdx.x) << (4 - k.elem_log2)));
-#pragma unroll
-        for (int j = 0; j < kClipLoads; ++j) sum += squares(v[j], dtype);
+        for (int half = 0; half < 2; ++half) {
+            const int at = c + half * step;
+            fetch(at + step, half ^ 1);
+            if (at >= chunks) break;
+            sum += dtype[half] == 0 ? squares<0>(v[half]) : dtype[half] == 1 ? squares<1>(v[half]) : squares<2>(v[half]);
+        }
     }
     const double total = block_sum(sum, s_warp);
     if (threadIdx.x == 0) P.partial[P.base + blockIdx.x] = total;
 }
 
 template <int kMax>
-__global__ void __launch_bounds__(kClipThreads, kScalePerSm) grad_scale_kernel(const __grid_constant__ ClipTable<kMax> P) {
+__global__ void __launch_bounds__(kClipThreads, kClipPerSm) grad_scale_kernel(const __grid_constant__ ClipTable<kMax> P) {
     __shared__ double s_warp[kClipThreads / 32];
     // The first chunk is on its way while the norm is still being taken: the launch before this one is always this library's grad_norm_kernel (or a scaling of other tensors), which
     // writes no gradient and lets dependents in behind its own wait only, so whatever made the gradients has completed.
     const int chunks = P.max_norm == 0.f ? 0 : P.first[P.count];
     auto fetch = [&](int c, Chunk& k, uint4 (&v)[kClipLoads]) {
         k = chunk_at(P, c);
-#pragma unroll
-        for (int j = 0; j < kClipLoads; ++j) v[j] = load_vector(k, k.begin + (static_cast<long long>(j * kClipThreads + threadIdx.x) << (4 - k.elem_log2)));
+        load_chunk(k, v);
     };
     int c = chunks - 1 - static_cast<int>(blockIdx.x);      // from the end: what the norm's pass read last is in L2
     Chunk k{};
@@ -197,6 +224,7 @@ __global__ void __launch_bounds__(kClipThreads, kScalePerSm) grad_scale_kernel(c
         const int dtype = P.dtype[k.tensor];
         unsigned char* out = static_cast<unsigned char*>(P.out[k.tensor]);
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(P.in[k.tensor])) & 15) == 0;
+        const bool plain = same && inside(k);
         const bool skip = factor == 1.f && out == P.in[k.tensor];
         out -= k.from << k.elem_log2;                   // of virtual element 0
         const int per = 16 >> k.elem_log2;
@@ -214,7 +242,7 @@ __global__ void __launch_bounds__(kClipThreads, kScalePerSm) grad_scale_kernel(c
                     w[i] = word_of(x.x * factor, x.y * factor, dtype);
                 }
             }
-            if (same && e >= k.from && e + per <= k.to) {
+            if (plain || (same && e >= k.from && e + per <= k.to)) {
                 *reinterpret_cast<uint4*>(out + (e << k.elem_log2)) = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
 #pragma unroll
@@ -277,8 +305,8 @@ int outputs_apart(const vardrop_tensor* tensors, int count) {
         if (spans[i].begin < spans[i - 1].end) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: two outputs overlap");
     return VARDROP_OK;
 }
-int grid_of(int chunks, int per_sm) {
-    const int most = per_sm * sm_count() < kClipMaxGrid ? per_sm * sm_count() : kClipMaxGrid;
+int grid_of(int chunks) {
+    const int most = kClipPerSm * sm_count() < kClipMaxGrid ? kClipPerSm * sm_count() : kClipMaxGrid;
     return chunks < 1 ? 1 : chunks < most ? chunks : most;
 }
 
@@ -293,7 +321,7 @@ int clip_launch(const vardrop_tensor* tensors, int count, const vardrop_clip_cfg
     }
     for (int at = 0; at < count; at += kMax) {
         fill(P, tensors, at, count);
-        const int grid = grid_of(P.first[P.count], kClipPerSm);
+        const int grid = grid_of(P.first[P.count]);
         P.base = P.partials;
         LaunchScope ls_(K_GRAD_NORM, stream);
         if (int st = check_cuda(launch_chained(grad_norm_kernel<kMax>, dim3(grid), dim3(kClipThreads), 0, stream, P), "grad_clip: norm launch")) return st;
@@ -303,7 +331,7 @@ int clip_launch(const vardrop_tensor* tensors, int count, const vardrop_clip_cfg
         fill(P, tensors, at, count);
         P.base = at;
         LaunchScope ls_(K_GRAD_SCALE, stream);
-        if (int st = check_cuda(launch_chained(grad_scale_kernel<kMax>, dim3(cfg.max_norm == 0.f ? 1 : grid_of(P.first[P.count], kScalePerSm)), dim3(kClipThreads), 0, stream, P), "grad_clip: scale launch")) return st;
+        if (int st = check_cuda(launch_chained(grad_scale_kernel<kMax>, dim3(cfg.max_norm == 0.f ? 1 : grid_of(P.first[P.count])), dim3(kClipThreads), 0, stream, P), "grad_clip: scale launch")) return st;
         if (cfg.max_norm == 0.f) break;
     }
     return VARDROP_OK;
