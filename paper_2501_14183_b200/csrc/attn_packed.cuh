@@ -6,9 +6,11 @@
 namespace vardrop {
 
 // A plan: a header, then an entry for every 128-token tile of every sequence, those with the most work first.  Entry `level` i of a sequence of n tiles stands for
-// query tile i forward (i + 1 key tiles in causal calls) and key tile n - 1 - i backward (i + 1 query tiles), so that one order serves both.
+// query tile i forward (i + 1 key tiles in causal calls) and key tile n - 1 - i backward (i + 1 query tiles), so that one order serves both.  Sequences of a single tile come
+// last.
 constexpr int kPlanMagic = 0x56445031;
-enum PlanWord { kPlanStatus = 0, kPlanMagicWord, kPlanTiles, kPlanSeqs, kPlanRows, kPlanCausal };
+constexpr int kFewTiles = 2;             // forward: tiles with no more key tiles than this are attn_packed_tile_kernel's
+enum PlanWord { kPlanStatus = 0, kPlanMagicWord, kPlanTiles, kPlanSeqs, kPlanRows, kPlanCausal, kPlanMany /*entries ahead of those with few key tiles*/, kPlanLong /*entries of sequences of several tiles*/ };
 struct alignas(16) PlanEntry {
     int start;              // row of the sequence's first token
     int len;                // its tokens
@@ -70,7 +72,7 @@ struct PlanView {
         return words[kPlanStatus] == VARDROP_OK && words[kPlanMagicWord] == kPlanMagic && words[kPlanSeqs] == n_seqs && words[kPlanRows] == T && words[kPlanCausal] == causal;
     }
     __device__ __forceinline__ const PlanEntry* entries() const { return reinterpret_cast<const PlanEntry*>(words + kWsHeaderBytes / 4); }
-    __device__ __forceinline__ int tiles() const { return fits() ? words[kPlanTiles] : 0; }
+    __device__ __forceinline__ int word(PlanWord w) const { return fits() ? words[w] : 0; }
 };
 
 // Item of a CTA's turn: there and back over the grid, so that what one CTA has more of in one turn it has less of in the next (items come with the most work first).

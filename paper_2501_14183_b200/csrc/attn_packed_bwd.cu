@@ -1,6 +1,6 @@
 // Attention over packed sequences, backward.
 //
-// packed_prep_kernel       Delta_i = sum_d dO_id O_id, and the cleared dQ accumulator.
+// packed_short_kernel      sequences of a single tile, all of it; for the others Delta_i = sum_d dO_id O_id, and the cleared dQ accumulator.
 // attn_packed_bwd_kernel   one persistent CTA per SM over items of one 128-key tile of a key head, with the query tiles of all its query heads; dQ is added into an fp32
 //                          accumulator by bulk reduce-adds.
 // packed_convert_kernel    dQ to bf16 rows.
@@ -27,22 +27,33 @@ struct PackedBwdParams {
 };
 
 // ---------------------------------------------------------------------------------------------------------
-// prep
+// sequences of a single tile, and prep for the others
 // ---------------------------------------------------------------------------------------------------------
-struct PackedPrepParams {
-    const uint4* o;         // [T, Hq, D] bf16
-    const uint4* d_o;       // [T, Hq, D] bf16
-    float* delta;           // [Hq, rows]
-    float4* dq_acc;         // [rows, Hq, 64] fp32
+struct PackedShortParams {
+    const __nv_bfloat16 *q, *k, *v, *d_o, *o;
+    const float* lse;                 // [Hq, T]
+    __nv_bfloat16 *dq, *dk, *dv;
+    float* delta;                     // [Hq, rows]
+    float4* dq_acc;                   // [rows, Hq, 64] fp32
     PlanView plan;
-    int T, Hq, D, rows;
+    int* status;
+    long long sTq, sHq, sTkv, sHkv;
+    int T, Hq, Hkv, group, D, rows, causal;
+    float scale, scale_log2;
 };
-// A CTA takes plan entries (tiles) by turns; a thread per 16-byte chunk of a (token, head) row of 64, the eight threads of a row reduce Delta by shuffles.
-__global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams P) {
-    chain_wait();
-    chain_release();
-    const int n_tiles = P.plan.tiles(), chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
+
+constexpr int kShortThreads = 256;
+constexpr int kShortPerSm = 2;
+constexpr int kShortSmemBytes = 4 * kTileBytes /*Q, dO, K, V*/ + 2 * kTileBytes /*P, then dS: two 64-key panels*/;
+
+// Delta and the cleared accumulator of longer sequences: a CTA takes slices of 1024 16-byte chunks of (token, head) rows of 64 by turns; the eight threads of a row reduce Delta
+// by shuffles.
+__device__ __forceinline__ void prep_slices(const PackedShortParams& P, int n_tiles) {
+    const int chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
     const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;        // four chunks a thread
+    const uint4* const O = reinterpret_cast<const uint4*>(P.o);
+    const uint4* const dO = reinterpret_cast<const uint4*>(P.d_o);
+#pragma unroll 1
     for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
         const int e = static_cast<int>(k / slices), slice = static_cast<int>(k - static_cast<long long>(e) * slices);
         const int4 x = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + e));
@@ -57,8 +68,8 @@ __global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams
             vo[u] = vd[u] = make_uint4(0u, 0u, 0u, 0u);
             if (row[u] < left && row[u] < kTile && (c[u] & 7) < src_chunks_head) {
                 const size_t src = (static_cast<size_t>(x.x + x.z * kTile + row[u]) * P.Hq + (c[u] >> 3)) * src_chunks_head + (c[u] & 7);
-                vo[u] = __ldg(P.o + src);
-                vd[u] = __ldg(P.d_o + src);
+                vo[u] = __ldg(O + src);
+                vd[u] = __ldg(dO + src);
             }
         }
 #pragma unroll
@@ -72,6 +83,225 @@ __global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams
             P.dq_acc[2 * dst + 1] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
+}
+
+// An item is a key head of such a sequence, with its query heads one after another.  Two threads a query row, 64 keys each.  With whole rows of P and dP at hand
+// Delta_i = sum_j P_ij dP_ij comes from them, in fp32: dS then sums to zero over a row as it should, where dO . O with an O of bf16 leaves 2^-9 of a term that for a few keys is as
+// large as dS itself (and neither O nor prep, accumulator and conversion are needed).
+// A chain of latencies like the forward's: two CTAs to an SM, rolled loops over 32 scores; P and dP stay in tensor memory between the two passes over a row.  P^T dO, dS^T Q and
+// dS K take P and dS from shared memory, the first two as transposed views.
+// kGrouped: several query heads a key head; dV and dK add up in columns of their own, which takes all of tensor memory and leaves one CTA to an SM.  Otherwise they come over the
+// scores' columns.
+// Tensor memory: S, P 128 | dP 128, then (dV 64 | dK 64 | dQ 64) over them, or with kGrouped: dQ 64 over S; dV 64 | dK 64 behind.
+template <bool kGrouped>
+__global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kernel(const PackedShortParams P) {
+    extern __shared__ __align__(1024) unsigned char smem_dyn[];
+    __shared__ uint64_t bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ float s_delta[2][kTile];
+    constexpr uint32_t kCols = kGrouped ? 512 : 256;
+    constexpr uint32_t kDv = kGrouped ? 256 : 0, kDk = kGrouped ? 320 : 64, kDq = kGrouped ? 0 : 128;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (smem_u32(smem_dyn) & 1023u) {
+        chain_wait();
+        if (tid == 0) set_status(P.status, VARDROP_ERR_CUDA);
+        return;
+    }
+    if (warp == 0) {
+        tmem_alloc(&tmem_slot, kCols);
+        tmem_relinquish();
+    }
+    if (tid == 0) {
+        mbar_init(&bar, 1);
+        mbar_fence_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    unsigned char* const sQ = smem_dyn;
+    unsigned char* const sdO = sQ + kTileBytes;
+    unsigned char* const sK = sdO + kTileBytes;
+    unsigned char* const sV = sK + kTileBytes;
+    unsigned char* const sP = sV + kTileBytes;
+    const uint32_t tmem = tmem_slot;
+    const int row = (warp & 3) * 32 + lane, half = warp >> 2;
+    const uint32_t tm = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint64_t a_q = umma_desc_sw128(smem_u32(sQ), 16, 1024), b_k = umma_desc_sw128(smem_u32(sK), 16, 1024);           // K-major
+    const uint64_t a_do = umma_desc_sw128(smem_u32(sdO), 16, 1024), b_v = umma_desc_sw128(smem_u32(sV), 16, 1024);
+    const uint64_t t_p = umma_desc_sw128(smem_u32(sP), kTileBytes, 1024), k_p = umma_desc_sw128(smem_u32(sP), 16, 1024);   // transposed; as it is
+    const uint64_t t_q = umma_desc_sw128(smem_u32(sQ), kTileBytes, 1024), t_do = umma_desc_sw128(smem_u32(sdO), kTileBytes, 1024), t_k = umma_desc_sw128(smem_u32(sK), kTileBytes, 1024);
+    chain_wait();
+    chain_release();
+    const bool fits = P.plan.fits();
+    if (!fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
+    const int first = fits ? P.plan.words[kPlanLong] : 0, n_items = fits ? (P.plan.words[kPlanTiles] - first) * P.Hkv : 0;
+    bool ok = true;
+    uint32_t phase = 0;
+    auto wait = [&]() {                                  // for the products behind the last commit
+        ok &= mbar_wait(&bar, phase);
+        phase ^= 1;
+        tc_fence_after();
+    };
+#pragma unroll 1
+    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+        const int e = item / P.Hkv, kvh = item - e * P.Hkv;
+        const int4 entry = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + first + e));
+        const int start = entry.x, len = entry.y, steps = (len + 15) >> 4, groups = (len + 31) >> 5;        // k-steps of 16 tokens, warps' shares of 32
+        const long long kv_off = start * P.sTkv + kvh * P.sHkv;
+#pragma unroll 1
+        for (int g = 0; g < P.group; ++g) {
+            const int h = kvh * P.group + g;
+            // tiles of 32-row shares: Q, dO, and at the item's begin K, V; rows up to the next k-step are zeros, those of shares behind it are not read
+            const int n_load = (g == 0 ? 4 : 2) * groups;
+#pragma unroll 1
+            for (int x = warp; x < n_load; x += kShortThreads / 32) {
+                const int tile = small_div(x, groups), r0 = (x - tile * groups) * 32;
+                const __nv_bfloat16* from = tile == 0 ? P.q + start * P.sTq + h * P.sHq
+                                            : tile == 1 ? P.d_o + (static_cast<long long>(start) * P.Hq + h) * P.D
+                                            : (tile == 2 ? P.k : P.v) + kv_off;
+                copy_32_rows(smem_dyn + tile * kTileBytes + r0 * kRowBytes, from, tile == 0 ? P.sTq : tile == 1 ? static_cast<long long>(P.Hq) * P.D : P.sTkv, nullptr, r0, len, P.D);
+            }
+            const float lse2 = row < len ? __ldg(P.lse + static_cast<size_t>(h) * P.T + start + row) * 1.4426950408889634f : 0.f;
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async_smem();
+            tc_fence_before();
+            __syncthreads();
+            if (warp == 0) {
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t idesc = umma_idesc_bf16(128, steps * 16, 0, 0);
+#pragma unroll 1
+                    for (int ks = 0; ks < P.D / 16; ++ks) tc_mma_bf16(tmem, umma_desc_advance(a_q, ks * 32), umma_desc_advance(b_k, ks * 32), idesc, ks > 0);
+#pragma unroll 1
+                    for (int ks = 0; ks < P.D / 16; ++ks) tc_mma_bf16(tmem + 128, umma_desc_advance(a_do, ks * 32), umma_desc_advance(b_v, ks * 32), idesc, ks > 0);
+                    tc_commit(&bar);
+                }
+                __syncwarp();
+            }
+            wait();
+            // ---- P, rounded to bf16 for P^T dO and as it is over S; Delta ----
+            const int seen = P.causal ? min(len, row + 1) : len, c_end = min(half * 64 + 64, steps * 16);        // keys that this row sees; columns of this thread
+            float delta = 0.f;
+#pragma unroll 1
+            for (int c = half * 64; c < c_end; c += 32) {
+                float s[32], d[32];
+                uint32_t pk[16];
+                tmem_ld32(tm + c, s);
+                tmem_ld32(tm + 128 + c, d);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const float p = fast_exp2(fmaf(s[i], P.scale_log2, -lse2));
+                    s[i] = c + i < seen ? p : 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    d[i] = c + i < seen ? d[i] : 0.f;    // (columns behind the keys hold anything)
+                    delta = fmaf(s[i], d[i], delta);
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) pk[i >> 1] = pack_bf16(s[i], s[i + 1]);
+                tmem_st32(tm + c, reinterpret_cast<const uint32_t*>(s));
+                store_panel(sP + half * kTileBytes, row, (c >> 5) & 1, pk);
+            }
+            s_delta[half][row] = delta;
+            tmem_st_wait();
+            fence_proxy_async_smem();
+            tc_fence_before();
+            ok = __syncthreads_and(ok);
+            if (!ok) { item = n_items; break; }          // a wait gave up somewhere in the CTA: stop
+            tc_fence_after();
+            delta = s_delta[0][row] + s_delta[1][row];
+            // ---- dS ----
+            uint32_t ds[32];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int c = half * 64 + x * 32;
+                if (c < c_end) {
+                    float p[32], d[32];
+                    tmem_ld32(tm + c, p);
+                    tmem_ld32(tm + 128 + c, d);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2)
+                        ds[x * 16 + (i >> 1)] = pack_bf16(c + i < seen ? p[i] * (d[i] - delta) : 0.f, c + i + 1 < seen ? p[i + 1] * (d[i + 1] - delta) : 0.f);
+                }
+            }
+            tc_fence_before();
+            __syncthreads();                             // S and dP have been read
+            if (warp == 0) {
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t idesc = umma_idesc_bf16(128, P.D, 1, 1);
+#pragma unroll 1
+                    for (int ks = 0; ks < steps; ++ks) tc_mma_bf16(tmem + kDv, umma_desc_advance(t_p, ks * 2048), umma_desc_advance(t_do, ks * 2048), idesc, (kGrouped && g > 0) || ks > 0);
+                    tc_commit(&bar);
+                }
+                __syncwarp();
+            }
+            wait();                                      // P has been read
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (half * 64 + x * 32 < c_end) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<uint4*>(sP + half * kTileBytes + row * kRowBytes + (((x * 4 + q) ^ (row & 7)) << 4)) =
+                            make_uint4(ds[x * 16 + 4 * q], ds[x * 16 + 4 * q + 1], ds[x * 16 + 4 * q + 2], ds[x * 16 + 4 * q + 3]);
+                }
+            fence_proxy_async_smem();
+            tc_fence_before();
+            ok = __syncthreads_and(ok);
+            if (!ok) { item = n_items; break; }
+            if (warp == 0) {
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t idesc_k = umma_idesc_bf16(128, P.D, 1, 1), idesc_q = umma_idesc_bf16(128, P.D, 0, 1);
+#pragma unroll 1
+                    for (int ks = 0; ks < steps; ++ks)   // dQ = dS K
+                        tc_mma_bf16(tmem + kDq, umma_desc_advance(k_p, (ks >> 2) * kTileBytes + (ks & 3) * 32), umma_desc_advance(t_k, ks * 2048), idesc_q, ks > 0);
+#pragma unroll 1
+                    for (int ks = 0; ks < steps; ++ks)   // dK = dS^T Q
+                        tc_mma_bf16(tmem + kDk, umma_desc_advance(t_p, ks * 2048), umma_desc_advance(t_q, ks * 2048), idesc_k, (kGrouped && g > 0) || ks > 0);
+                    tc_commit(&bar);
+                }
+                __syncwarp();
+            }
+            wait();
+            // ---- rows out, half of the columns a thread ----
+            auto rows_out = [&](uint32_t col, __nv_bfloat16* to, float mul) {
+                const int c0 = half * (P.D / 2);
+#pragma unroll 1
+                for (int c = c0; c < c0 + P.D / 2; c += 16) {
+                    float v[16];
+                    tmem_ld16(tm + col + c, v);
+                    tmem_ld_wait();
+                    if (row < len) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            *reinterpret_cast<uint4*>(to + c + 8 * q) = make_uint4(pack2(v[8 * q] * mul, v[8 * q + 1] * mul), pack2(v[8 * q + 2] * mul, v[8 * q + 3] * mul),
+                                                                                   pack2(v[8 * q + 4] * mul, v[8 * q + 5] * mul), pack2(v[8 * q + 6] * mul, v[8 * q + 7] * mul));
+                    }
+                }
+            };
+            rows_out(kDq, P.dq + (static_cast<size_t>(start + row) * P.Hq + h) * P.D, P.scale);
+            if (!kGrouped || g + 1 == P.group) {
+                const size_t to = (static_cast<size_t>(start + row) * P.Hkv + kvh) * P.D;
+                rows_out(kDv, P.dv + to, 1.f);
+                rows_out(kDk, P.dk + to, P.scale);
+            }
+            tc_fence_before();
+            ok = __syncthreads_and(ok);                  // tiles and columns are free
+            if (!ok) { item = n_items; break; }
+            tc_fence_after();
+        }
+        if (item == n_items) break;
+    }
+    if (!ok) set_status(P.status, VARDROP_ERR_TIMEOUT);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tmem, kCols);
+    prep_slices(P, first);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -399,8 +629,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
     } else {
         // ------------------------------------------------------------ loads, items --------------------------------------
         const bool fits = P.plan.fits();
-        if (!fits && blockIdx.x == 0 && lane == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
-        const long long n_items = fits ? static_cast<long long>(P.plan.tiles()) * P.Hkv : 0;
+        const long long n_items = fits ? static_cast<long long>(P.plan.word(kPlanLong)) * P.Hkv : 0;
         auto publish = [&](uint32_t i) {
             const long long k = turn_item(static_cast<int>(i));
             Item it{0, -1, 0, 0, 0, 0, 0, 0};
@@ -687,7 +916,7 @@ struct PackedConvertParams {
 __global__ void __launch_bounds__(256) packed_convert_kernel(const PackedConvertParams P) {
     chain_wait();
     chain_release();
-    const int n_tiles = P.plan.tiles(), sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;        // 16-byte results per row
+    const int n_tiles = P.plan.word(kPlanLong), sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;        // 16-byte results per row
     const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;
     for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
         const int e = static_cast<int>(k / slices), slice = static_cast<int>(k - static_cast<long long>(e) * slices);
@@ -722,12 +951,6 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
     const PackedStrides L = packed_strides(c);
     char* base = static_cast<char*>(ws);
     const long long HD = static_cast<long long>(c.Hq) * c.D;
-    CUtensorMap mq, mk, mv, mdo, macc;
-    if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
-    if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
-    if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
-    if (int st = packed_tile_map(&mdo, d_o, c.D, c.Hq, c.T, HD, c.D)) return st;
-    if (int st = packed_acc_map(&macc, base + w.dq_acc, w.rows, c.Hq)) return st;
     PackedBwdParams P{};
     P.q = static_cast<const __nv_bfloat16*>(q); P.k = static_cast<const __nv_bfloat16*>(k); P.v = static_cast<const __nv_bfloat16*>(v);
     P.d_o = static_cast<const __nv_bfloat16*>(d_o);
@@ -743,28 +966,40 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
     P.scale_log2 = least * 1.4426950408889634f;
     P.half_inv_scale = 0.5f / least;
     const long long tiles = packed_tiles(c);
-    const int places = 8 * sm_count();
-    auto grid_of = [&](long long chunks) {
-        const long long blocks = tiles * ((chunks + 1023) / 1024);
-        return static_cast<int>(blocks < places ? blocks : places);
-    };
-    {
-        PackedPrepParams R{};
-        R.o = static_cast<const uint4*>(o); R.d_o = static_cast<const uint4*>(d_o);
-        R.delta = reinterpret_cast<float*>(base + w.delta);
-        R.dq_acc = reinterpret_cast<float4*>(base + w.dq_acc);
-        R.plan = P.plan;
-        R.T = c.T; R.Hq = c.Hq; R.D = c.D; R.rows = w.rows;
-        LaunchScope ls_(K_PACKED_PREP, stream);
-        if (int st = check_cuda(launch_chained(packed_prep_kernel, dim3(grid_of(kTile * c.Hq * 8ll)), dim3(256), 0, stream, R), "packed attention: backward prep launch")) return st;
-    }
+    const bool all_short = c.T <= kTile;
     static thread_local int attr_dev = -1;
     int dev = 0;
     cudaGetDevice(&dev);
     if (attr_dev != dev) {
         if (int st = check_cuda(cudaFuncSetAttribute(attn_packed_bwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kManySmemBytes), "packed attention: smem attribute")) return st;
+        for (auto kernel : {packed_short_kernel<false>, packed_short_kernel<true>})
+            if (int st = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShortSmemBytes), "packed attention: smem attribute")) return st;
         attr_dev = dev;
     }
+    {
+        PackedShortParams R{};
+        R.q = P.q; R.k = P.k; R.v = P.v; R.d_o = P.d_o; R.o = static_cast<const __nv_bfloat16*>(o);
+        R.lse = lse;
+        R.dq = static_cast<__nv_bfloat16*>(dq); R.dk = P.dk; R.dv = P.dv;
+        R.delta = reinterpret_cast<float*>(base + w.delta);
+        R.dq_acc = reinterpret_cast<float4*>(base + w.dq_acc);
+        R.plan = P.plan; R.status = P.status;
+        R.sTq = P.sTq; R.sHq = P.sHq; R.sTkv = P.sTkv; R.sHkv = P.sHkv;
+        R.T = P.T; R.Hq = P.Hq; R.Hkv = P.Hkv; R.group = P.group; R.D = P.D; R.rows = P.rows; R.causal = P.causal;
+        R.scale = P.scale; R.scale_log2 = P.scale * 1.4426950408889634f;
+        const long long items = tiles * c.Hkv, slices = all_short ? 0 : tiles * ((kTile * c.Hq * 8ll + 1023) / 1024), most = items > slices ? items : slices;
+        const long long places = static_cast<long long>(P.group > 1 ? 1 : kShortPerSm) * sm_count();
+        LaunchScope ls_(K_PACKED_SHORT, stream);
+        if (int st = check_cuda(launch_chained(P.group > 1 ? packed_short_kernel<true> : packed_short_kernel<false>, dim3(static_cast<unsigned>(most < places ? most : places)),
+                                               dim3(kShortThreads), kShortSmemBytes, stream, R), "packed attention: backward launch of short sequences")) return st;
+    }
+    if (all_short) return VARDROP_OK;
+    CUtensorMap mq, mk, mv, mdo, macc;
+    if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
+    if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
+    if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
+    if (int st = packed_tile_map(&mdo, d_o, c.D, c.Hq, c.T, HD, c.D)) return st;
+    if (int st = packed_acc_map(&macc, base + w.dq_acc, w.rows, c.Hq)) return st;
     const long long worst = tiles * c.Hkv;
     const int grid = static_cast<int>(worst < sm_count() ? worst : sm_count());          // one CTA per SM (all of tensor memory)
     {
@@ -772,13 +1007,14 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
         if (int st = check_cuda(launch_chained(attn_packed_bwd_kernel, dim3(grid), dim3(kManyThreads), kManySmemBytes, stream, mq, mk, mv, mdo, macc, P),
                                 "packed attention: backward launch")) return st;
     }
+    const long long slices = tiles * ((kTile * c.Hq * (c.D / 8ll) + 1023) / 1024), places = 8ll * sm_count();
     PackedConvertParams F{};
     F.dq_acc = reinterpret_cast<const float4*>(base + w.dq_acc);
     F.dq = static_cast<uint4*>(dq);
     F.plan = P.plan;
     F.Hq = c.Hq; F.D = c.D; F.scale = P.scale;
     LaunchScope ls_(K_PACKED_CONVERT, stream);
-    return check_cuda(launch_chained(packed_convert_kernel, dim3(grid_of(kTile * c.Hq * (c.D / 8ll))), dim3(256), 0, stream, F), "packed attention: backward convert launch");
+    return check_cuda(launch_chained(packed_convert_kernel, dim3(static_cast<unsigned>(slices < places ? slices : places)), dim3(256), 0, stream, F), "packed attention: backward convert launch");
 }
 
 }  // namespace vardrop

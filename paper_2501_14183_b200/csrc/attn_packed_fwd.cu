@@ -2,6 +2,7 @@
 //
 // attn_packed_fwd_kernel   one persistent CTA per SM over items of one 128-query tile of two heads, a warp role for each part of the work: the split of
 //                          attn_fwd_kernel (many tiles), whose roles, tensor memory and softmax it shares; what differs stands below.
+// attn_packed_tile_kernel  tiles with at most two key tiles: 128-thread CTAs, four to an SM, a tile of a head each, as attn_fwd_tile_kernel.
 #include "attn_packed.cuh"
 
 namespace vardrop {
@@ -9,12 +10,12 @@ namespace vardrop {
 namespace {
 
 struct PackedFwdParams {
-    const __nv_bfloat16* v;            // rows of a sequence's last tile (the other loads go through the tensor maps)
+    const __nv_bfloat16 *q, *k, *v;    // read as rows: V of a sequence's last tile, all of the kernel for few key tiles (the other loads go through the tensor maps)
     __nv_bfloat16* o;                  // [T, Hq, D]
     float* lse;                        // [Hq, T]
     PlanView plan;
     int* status;
-    long long sTkv, sHkv;
+    long long sTq, sHq, sTkv, sHkv;
     int T, Hq, group, D;               // group: query heads of a key head
     int causal;
     float scale_log2;                  // sm_scale * log2(e)
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         const bool fits = P.plan.fits();
         if (!fits && blockIdx.x == 0 && lane == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
         const int pairs = (P.Hq + 1) >> 1;
-        const long long n_items = fits ? static_cast<long long>(P.plan.tiles()) * pairs : 0;
+        const long long n_items = fits ? static_cast<long long>(P.plan.word(kPlanMany)) * pairs : 0;
         auto publish = [&](uint32_t i) {
             const long long k = turn_item(static_cast<int>(i));
             Item it{0, 0, 0, 0, 0, -1, 0, 0};
@@ -551,20 +552,265 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
     if (warp == 0) tmem_dealloc(tmem, kFwdTmemCols);
 }
 
+
+// ---------------------------------------------------------------------------------------------------------
+// few key tiles
+// ---------------------------------------------------------------------------------------------------------
+// A chain of latencies in which every path runs once or twice: no roles and no hand-offs but the CTA barrier, rolled loops over 32 scores that stay in tensor memory and are
+// read twice, 48 KB and 128 columns a CTA, so that four CTAs share an SM and fill each other's waits.  All loads are row copies with zeros behind a sequence's end.
+// Tensor memory: S 128; P (bf16) over S's columns 0 .. 63 as they are consumed, P V into columns 64 .. 127.
+constexpr int kTileFwdThreads = 128;
+constexpr uint32_t kTileFwdTmemCols = 128;
+constexpr int kTileFwdSmemBytes = 1024 /*alignment*/ + 3 * kTileBytes /*Q, K, V*/;
+constexpr int kTileFwdPerSm = 4;
+
+// kAll: every tile of the batch is this kernel's, and it is the first launch of the call.  Otherwise it comes behind attn_packed_fwd_kernel, whose CTAs let it in once
+// they have waited for whatever lies before them; it reads nothing that kernel writes and writes other rows, so it waits for it only at its end, to be the later one to complete.
+template <bool kAll>
+__global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_tile_kernel(const PackedFwdParams P) {
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ uint64_t bar_s, bar_o;
+    __shared__ uint32_t tmem_slot;
+    unsigned char* sQ = align_tiles(smem_dyn);
+    unsigned char* sK = sQ + kTileBytes;
+    unsigned char* sV = sK + kTileBytes;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (warp == 0) {
+        tmem_alloc(&tmem_slot, kTileFwdTmemCols);
+        tmem_relinquish();
+    }
+    if (tid == 0) {
+        mbar_init(&bar_s, 1);
+        mbar_init(&bar_o, 1);
+        mbar_fence_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, tm = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    const uint32_t idesc_o = umma_idesc_bf16(128, P.D, 0, 1);
+    const uint64_t d_q = umma_desc_sw128(smem_u32(sQ), 16, 1024), d_k = umma_desc_sw128(smem_u32(sK), 16, 1024);
+    const uint64_t d_v = umma_desc_sw128(smem_u32(sV), kTileBytes, 1024);
+    const uint64_t scale2 = pair_of(P.scale_log2, P.scale_log2);
+    if (kAll) chain_wait();
+    chain_release();
+    const bool fits = P.plan.fits();
+    if (!fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
+    const int first = kAll || !fits ? 0 : P.plan.words[kPlanMany], n_items = fits ? (P.plan.words[kPlanTiles] - first) * P.Hq : 0;
+    bool ok = true;
+    uint32_t t = 0;                                     // key tiles of this CTA so far: parity of bar_s and bar_o
+
+#pragma unroll 1
+    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+        const int e = item / P.Hq, h = item - e * P.Hq, kvh = small_div(h, P.group);
+        const int4 entry = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + first + e));
+        const int start = entry.x, len = entry.y, qt = entry.z, n_kv = P.causal ? qt + 1 : (len + kTile - 1) / kTile;
+        const __nv_bfloat16* const q = P.q + start * P.sTq + h * P.sHq;
+        const __nv_bfloat16* const k = P.k + start * P.sTkv + kvh * P.sHkv;
+        const __nv_bfloat16* const v = P.v + start * P.sTkv + kvh * P.sHkv;
+        // every warp copies its 32 rows of a tile
+        auto load_rows = [&](unsigned char* tile, const __nv_bfloat16* from, long long sT, int t0) {
+            copy_32_rows(tile + warp * 32 * kRowBytes, from, sT, nullptr, t0 * kTile + warp * 32, len, P.D);
+        };
+        load_rows(sQ, q, P.sTq, qt);
+        load_rows(sK, k, P.sTkv, 0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        load_rows(sV, v, P.sTkv, 0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        float o_acc[kDP];                                // more than one key tile: the sum over the tiles before the current one
+        float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < n_kv; ++j, ++t) {
+            const int n_keys = min(kTile, len - j * kTile), n_seen = P.causal && j == qt ? min(n_keys, tid + 1) : n_keys;     // of this row
+            if (j > 0) {
+#pragma unroll 1
+                for (int x = 1; x < 3; ++x) {            // K, V
+                    load_rows(sQ + x * kTileBytes, x == 1 ? k : v, P.sTkv, j);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                }
+            }
+            asm volatile("cp.async.wait_group 1;" ::: "memory");         // Q and K have landed
+            fence_proxy_async_smem();
+            tc_fence_before();
+            __syncthreads();
+            if (warp == 0) {
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t idesc = umma_idesc_bf16(128, (n_keys + 15) & ~15, 0, 0);
+#pragma unroll 1
+                    for (int ks = 0; ks < P.D / 16; ++ks)
+                        tc_mma_bf16(tmem, umma_desc_advance(d_q, ks * 32), umma_desc_advance(d_k, ks * 32), idesc, ks > 0);
+                    tc_commit(&bar_s);
+                }
+                __syncwarp();
+            }
+            ok &= mbar_wait(&bar_s, t & 1);
+            tc_fence_after();
+            // ---- row maximum, 32 scores at a time ----
+            float m_tile = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < n_keys; c += 32) {
+                float s[32];
+                tmem_ld32(tm + c, s);
+                tmem_ld_wait();
+                if (__any_sync(0xffffffffu, n_seen - c < 32)) {       // ragged end, or the diagonal: keys that are not seen never win the maximum
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c + i >= n_seen) s[i] = -INFINITY;
+                }
+                float mx[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) mx[u] = s[u];
+#pragma unroll
+                for (int i = 4; i < 28; i += 8) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) mx[u] = max3(mx[u], s[i + u], s[i + 4 + u]);
+                }
+                m_tile = max3(m_tile, max3(mx[0], s[28], mx[1]), max3(max3(s[29], mx[2], s[30]), mx[3], s[31]));
+            }
+            const float m_new = fmaxf(m_run, m_tile * P.scale_log2), alpha = fast_exp2(m_run - m_new);
+            m_run = m_new;
+            // ---- P = exp2(S scale - maximum), rounded to bf16, over the columns of S that have been read ----
+            const uint64_t shift2 = pair_of(-m_new, -m_new);
+            uint64_t l2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+            auto l_sum = [&]() {
+                float a0, a1, a2, a3;
+                halves_of(l2[0], a0, a1);
+                halves_of(l2[1], a2, a3);
+                return (a0 + a1) + (a2 + a3);
+            };
+#pragma unroll 1
+            for (int c = 0; c < n_keys; c += 32) {
+                float s[32];
+                uint32_t pk[16];
+                tmem_ld32(tm + c, s);
+                tmem_ld_wait();
+                if (__any_sync(0xffffffffu, n_seen - c < 32)) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c + i >= n_seen) s[i] = -INFINITY;
+                }
+#pragma unroll
+                for (int g = 0; g < 6; ++g) {            // batches of eight: exponents of g, exponentials of g - 1, sums and rounding of g - 2
+                    if (g < 4) {
+#pragma unroll
+                        for (int i = 8 * g; i < 8 * g + 8; i += 2) halves_of(fma_pair(pair_of(s[i], s[i + 1]), scale2, shift2), s[i], s[i + 1]);
+                    }
+                    if (g >= 1 && g < 5) {
+#pragma unroll
+                        for (int i = 8 * g - 8; i < 8 * g; ++i) s[i] = fast_exp2(s[i]);       // exp2(-inf) = 0 for the masked keys
+                    }
+                    if (g >= 2) {
+#pragma unroll
+                        for (int i = 8 * g - 16; i < 8 * g - 8; i += 2) {
+                            l2[(i >> 1) & 1] = add_pair(l2[(i >> 1) & 1], pair_of(s[i], s[i + 1]));
+                            pk[i >> 1] = pack_bf16(s[i], s[i + 1]);
+                        }
+                    }
+                }
+                tmem_st16(tm + (c >> 1), pk);            // keys 2 c' and 2 c' + 1 in column c'
+            }
+            l_run = l_run * alpha + l_sum();
+            asm volatile("cp.async.wait_group 0;" ::: "memory");             // V has landed
+            fence_proxy_async_smem();
+            tmem_st_wait();
+            tc_fence_before();
+            ok = __syncthreads_and(ok);
+            if (!ok) { item = n_items; break; }          // a wait gave up somewhere in the CTA: stop
+            if (warp == 0) {
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll 1
+                    for (int ks = 0; ks < (n_keys + 15) >> 4; ++ks)
+                        tc_mma_bf16_ta(tmem + 64, tmem + ks * 8, umma_desc_advance(d_v, ks * 2048), idesc_o, ks > 0);
+                    tc_commit(&bar_o);
+                }
+                __syncwarp();
+            }
+            ok &= mbar_wait(&bar_o, t & 1);              // (agreed on at the next such barrier: no thread leaves by itself)
+            tc_fence_after();
+            if (n_kv > 1) {
+                if (j == 0) {
+                    tmem_ld32(tm + 64, o_acc);
+                    if (P.D > 32) tmem_ld32(tm + 96, o_acc + 32);
+                    tmem_ld_wait();
+                } else {
+                    const uint64_t alpha2 = pair_of(alpha, alpha);
+#pragma unroll
+                    for (int c = 0; c < kDP; c += 32) {
+                        if (c < P.D) {
+                            float ov[32];
+                            tmem_ld32(tm + 64 + c, ov);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int d = 0; d < 32; d += 2)          // rescale and add in one step
+                                halves_of(fma_pair(pair_of(o_acc[c + d], o_acc[c + d + 1]), alpha2, pair_of(ov[d], ov[d + 1])), o_acc[c + d], o_acc[c + d + 1]);
+                        }
+                    }
+                    if (j + 1 == n_kv) {                 // back where a single tile leaves it
+                        tmem_st32(tm + 64, reinterpret_cast<const uint32_t*>(o_acc));
+                        if (P.D > 32) tmem_st32(tm + 96, reinterpret_cast<const uint32_t*>(o_acc + 32));
+                        tmem_st_wait();
+                    }
+                }
+            }
+            tc_fence_before();
+            if (j + 1 < n_kv) __syncthreads();           // the next step's S goes over these columns
+        }
+        if (item == n_items) break;
+        // ---- O / l, rounded to bf16, through Q's tile so that whole rows are written ----
+        {
+            const float inv_l = 1.f / l_run;
+            unsigned char* rowp = sQ + tid * kRowBytes;
+            const int row = qt * kTile + tid;
+            if (row < len) P.lse[static_cast<size_t>(h) * P.T + start + row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+#pragma unroll 1
+            for (int c16 = 0; c16 < P.D / 16; ++c16) {
+                float ov[16];
+                tmem_ld16(tm + 64 + c16 * 16, ov);
+                tmem_ld_wait();
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    *reinterpret_cast<uint4*>(rowp + (((c16 * 2 + q) ^ (tid & 7)) << 4)) =
+                        make_uint4(pack_bf16(ov[8 * q + 0] * inv_l, ov[8 * q + 1] * inv_l), pack_bf16(ov[8 * q + 2] * inv_l, ov[8 * q + 3] * inv_l),
+                                   pack_bf16(ov[8 * q + 4] * inv_l, ov[8 * q + 5] * inv_l), pack_bf16(ov[8 * q + 6] * inv_l, ov[8 * q + 7] * inv_l));
+            }
+            tc_fence_before();
+            __syncwarp();                                // a warp writes the rows it has staged
+            const int c = lane & 7, r0 = warp * 32 + (lane >> 3);
+            if (c * 8 < P.D) {
+                __nv_bfloat16* out = P.o + (static_cast<size_t>(start + qt * kTile + r0) * P.Hq + h) * P.D + c * 8;
+                const unsigned char* from = sQ + r0 * kRowBytes + ((c ^ (r0 & 7)) << 4);
+                const unsigned char* from4 = sQ + (r0 + 4) * kRowBytes + ((c ^ ((r0 + 4) & 7)) << 4);
+                const int left = min(32 - (lane >> 3), len - qt * kTile - r0);
+                const size_t step = static_cast<size_t>(4) * P.Hq * P.D;
+#pragma unroll 1
+                for (int x = 0; x < left; x += 8, out += 2 * step, from += 8 * kRowBytes, from4 += 8 * kRowBytes) {     // rows 4 apart
+                    const uint4 v0 = *reinterpret_cast<const uint4*>(from), v1 = *reinterpret_cast<const uint4*>(from4);
+                    *reinterpret_cast<uint4*>(out) = v0;
+                    if (x + 4 < left) *reinterpret_cast<uint4*>(out + step) = v1;
+                }
+            }
+            __syncthreads();                             // Q's tile is free for the next item
+        }
+    }
+    if (!ok) set_status(P.status, VARDROP_ERR_TIMEOUT);
+    if (!kAll) chain_wait();
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tmem, kTileFwdTmemCols);
+}
 }  // namespace
 
 int attn_packed_fwd_launch(const void* q, const void* k, const void* v, const void* plan, const vardrop_packed_cfg& c, void* o, float* lse, void* ws, cudaStream_t stream) {
     const PackedStrides L = packed_strides(c);
-    CUtensorMap mq, mk, mv;
-    if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
-    if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
-    if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
     PackedFwdParams P{};
-    P.v = static_cast<const __nv_bfloat16*>(v);
+    P.q = static_cast<const __nv_bfloat16*>(q); P.k = static_cast<const __nv_bfloat16*>(k); P.v = static_cast<const __nv_bfloat16*>(v);
     P.o = static_cast<__nv_bfloat16*>(o); P.lse = lse;
     P.plan = PlanView{static_cast<const int32_t*>(plan), c.n_seqs, c.T, c.causal};
     P.status = static_cast<int*>(ws);
-    P.sTkv = L.sTkv; P.sHkv = L.sHkv;
+    P.sTq = L.sTq; P.sHq = L.sHq; P.sTkv = L.sTkv; P.sHkv = L.sHkv;
     P.T = c.T; P.Hq = c.Hq; P.group = c.Hq / c.Hkv; P.D = c.D; P.causal = c.causal;
     const float scale = c.sm_scale > 0.f ? c.sm_scale : 1.f / sqrtf(static_cast<float>(c.D));
     P.scale_log2 = scale * 1.4426950408889634f;
@@ -573,12 +819,28 @@ int attn_packed_fwd_launch(const void* q, const void* k, const void* v, const vo
     cudaGetDevice(&dev);
     if (attr_dev != dev) {
         if (int st = check_cuda(cudaFuncSetAttribute(attn_packed_fwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFwdSmemBytes), "packed attention: smem attribute")) return st;
+        for (auto kernel : {attn_packed_tile_kernel<false>, attn_packed_tile_kernel<true>})
+            if (int st = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileFwdSmemBytes), "packed attention: smem attribute")) return st;
         attr_dev = dev;
     }
-    const long long worst = packed_tiles(c) * ((c.Hq + 1) / 2);
+    const long long tiles = packed_tiles(c), places = static_cast<long long>(kTileFwdPerSm) * sm_count();
+    const dim3 tile_grid(static_cast<unsigned>(tiles * c.Hq < places ? tiles * c.Hq : places));
+    if (c.T <= kFewTiles * kTile) {
+        LaunchScope ls_(K_PACKED_TILE, stream);
+        return check_cuda(launch_chained(attn_packed_tile_kernel<true>, tile_grid, dim3(kTileFwdThreads), kTileFwdSmemBytes, stream, P), "packed attention: forward launch");
+    }
+    CUtensorMap mq, mk, mv;
+    if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
+    if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
+    if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
+    const long long worst = tiles * ((c.Hq + 1) / 2);
     const int grid = static_cast<int>(worst < sm_count() ? worst : sm_count());                 // one CTA per SM
-    LaunchScope ls_(K_PACKED_FWD, stream);
-    return check_cuda(launch_chained(attn_packed_fwd_kernel, dim3(grid), dim3(kFwdThreads), kFwdSmemBytes, stream, mq, mk, mv, P), "packed attention: forward launch");
+    {
+        LaunchScope ls_(K_PACKED_FWD, stream);
+        if (int st = check_cuda(launch_chained(attn_packed_fwd_kernel, dim3(grid), dim3(kFwdThreads), kFwdSmemBytes, stream, mq, mk, mv, P), "packed attention: forward launch")) return st;
+    }
+    LaunchScope ls_(K_PACKED_TILE, stream);
+    return check_cuda(launch_chained(attn_packed_tile_kernel<false>, tile_grid, dim3(kTileFwdThreads), kTileFwdSmemBytes, stream, P), "packed attention: forward launch");
 }
 
 }  // namespace vardrop

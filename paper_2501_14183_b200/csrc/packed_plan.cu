@@ -43,15 +43,16 @@ __device__ __forceinline__ int block_scan(int v, int* s_warp) {      // exclusiv
 // Counting sort: tiles per amount of work, then each tile's place.  Sequences come 1024 at a time, a thread each; their tiles are shared out over all threads again, so a
 // single long sequence takes no longer than many short ones.
 __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanParams P) {
-    __shared__ int s_warp[33], s_bin[kPlanBins], s_bad;
+    __shared__ int s_warp[33], s_bin[kPlanBins + 1], s_bad;
     __shared__ int s_first[kPlanThreads + 1], s_start[kPlanThreads], s_len[kPlanThreads];
     chain_wait();
     chain_release();
     const int tid = threadIdx.x;
-    for (int b = tid; b < P.bins; b += kPlanThreads) s_bin[b] = 0;
+    const int bins = P.bins + 1;             // the last one: sequences of a single tile
+    for (int b = tid; b < bins; b += kPlanThreads) s_bin[b] = 0;
     if (tid == 0) s_bad = 0;
     __syncthreads();
-    int total = 0;
+    int total = 0, many = 0, longer = 0;
     for (int pass = 0; pass < 2; ++pass) {
         int ahead = 0;
         for (int s0 = 0; s0 < P.n_seqs; s0 += kPlanThreads) {
@@ -84,7 +85,7 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
                     else hi = mid - 1;
                 }
                 const int level = t - s_first[lo], n = (s_len[lo] + kTile - 1) / kTile;
-                const int work = P.causal ? level + 1 : n, bin = P.bins - min(work, P.bins);      // bin 0: the most work
+                const int work = P.causal ? level + 1 : n, bin = n == 1 ? P.bins : P.bins - min(work, P.bins);      // bin 0: the most work
                 if (pass == 0) {
                     atomicAdd(&s_bin[bin], 1);
                 } else {
@@ -99,12 +100,15 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
         if (pass == 0) {
             total = ahead;
             int run = 0;
-            for (int b0 = 0; b0 < P.bins; b0 += kPlanThreads) {
-                const int b = b0 + tid, v = b < P.bins ? s_bin[b] : 0;
+            for (int b0 = 0; b0 < bins; b0 += kPlanThreads) {
+                const int b = b0 + tid, v = b < bins ? s_bin[b] : 0;
                 const int at = block_scan(v, s_warp);
-                if (b < P.bins) s_bin[b] = run + at;
+                if (b < bins) s_bin[b] = run + at;
                 run += s_warp[32];
             }
+            __syncthreads();
+            many = P.bins > kFewTiles ? s_bin[P.bins - kFewTiles] : 0;      // where the tiles with that much work begin
+            longer = s_bin[P.bins];
             __syncthreads();
         }
     }
@@ -116,6 +120,8 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
         P.plan[kPlanSeqs] = P.n_seqs;
         P.plan[kPlanRows] = P.T;
         P.plan[kPlanCausal] = P.causal;
+        P.plan[kPlanMany] = bad ? 0 : many;
+        P.plan[kPlanLong] = bad ? 0 : longer;
     }
 }
 
