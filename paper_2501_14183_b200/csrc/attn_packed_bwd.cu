@@ -1,9 +1,10 @@
 // Attention over packed sequences, backward.
 //
-// packed_short_kernel      sequences of a single tile, all of it; for the others Delta_i = sum_d dO_id O_id, and the cleared dQ accumulator.
+// packed_prep_kernel       Delta_i = sum_d dO_id O_id, and the cleared dQ accumulator.
 // attn_packed_bwd_kernel   one persistent CTA per SM over items of one 128-key tile of a key head, with the query tiles of all its query heads; dQ is added into an fp32
 //                          accumulator by bulk reduce-adds.
-// packed_convert_kernel    dQ to bf16 rows.
+// packed_short_kernel      sequences of a single tile, all of it; runs as SMs become free.
+// packed_convert_kernel    dQ of the others to bf16 rows.
 //
 // The roles, tensor memory and arithmetic of a step are those of bwd_many_kernel; what differs: tiles of sequences that end inside, heads that share their keys (their dK
 // and dV add up in tensor memory over the item), the diagonal of a causal call, and the accumulator in which every sequence begins a tile, so that what a last tile adds behind
@@ -27,63 +28,23 @@ struct PackedBwdParams {
 };
 
 // ---------------------------------------------------------------------------------------------------------
-// sequences of a single tile, and prep for the others
+// sequences of a single tile
 // ---------------------------------------------------------------------------------------------------------
 struct PackedShortParams {
-    const __nv_bfloat16 *q, *k, *v, *d_o, *o;
+    const __nv_bfloat16 *q, *k, *v, *d_o;
     const float* lse;                 // [Hq, T]
     __nv_bfloat16 *dq, *dk, *dv;
-    float* delta;                     // [Hq, rows]
-    float4* dq_acc;                   // [rows, Hq, 64] fp32
     PlanView plan;
     int* status;
     long long sTq, sHq, sTkv, sHkv;
-    int T, Hq, Hkv, group, D, rows, causal;
+    int T, Hq, Hkv, group, D, causal;
+    int alone;                        // the only launch of the call; otherwise attn_packed_bwd_kernel's is the one before
     float scale, scale_log2;
 };
 
 constexpr int kShortThreads = 256;
 constexpr int kShortPerSm = 2;
 constexpr int kShortSmemBytes = 4 * kTileBytes /*Q, dO, K, V*/ + 2 * kTileBytes /*P, then dS: two 64-key panels*/;
-
-// Delta and the cleared accumulator of longer sequences: a CTA takes slices of 1024 16-byte chunks of (token, head) rows of 64 by turns; the eight threads of a row reduce Delta
-// by shuffles.
-__device__ __forceinline__ void prep_slices(const PackedShortParams& P, int n_tiles) {
-    const int chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
-    const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;        // four chunks a thread
-    const uint4* const O = reinterpret_cast<const uint4*>(P.o);
-    const uint4* const dO = reinterpret_cast<const uint4*>(P.d_o);
-#pragma unroll 1
-    for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
-        const int e = static_cast<int>(k / slices), slice = static_cast<int>(k - static_cast<long long>(e) * slices);
-        const int4 x = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + e));
-        const int left = x.y - x.z * kTile;
-        uint4 vo[4], vd[4];
-        int row[4], c[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int idx = slice * 1024 + u * 256 + static_cast<int>(threadIdx.x);
-            row[u] = idx < per_tile ? small_div(idx, chunks_row) : kTile;
-            c[u] = idx - row[u] * chunks_row;
-            vo[u] = vd[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (row[u] < left && row[u] < kTile && (c[u] & 7) < src_chunks_head) {
-                const size_t src = (static_cast<size_t>(x.x + x.z * kTile + row[u]) * P.Hq + (c[u] >> 3)) * src_chunks_head + (c[u] & 7);
-                vo[u] = __ldg(O + src);
-                vd[u] = __ldg(dO + src);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float part = sum8(dot8(vo[u], vd[u]));
-            if (row[u] >= kTile) continue;
-            const size_t to = static_cast<size_t>(x.w + x.z) * kTile + row[u];
-            if ((c[u] & 7) == 0) P.delta[static_cast<size_t>(c[u] >> 3) * P.rows + to] = part;
-            const size_t dst = to * chunks_row + c[u];
-            P.dq_acc[2 * dst] = make_float4(0.f, 0.f, 0.f, 0.f);
-            P.dq_acc[2 * dst + 1] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-    }
-}
 
 // An item is a key head of such a sequence, with its query heads one after another.  Two threads a query row, 64 keys each.  With whole rows of P and dP at hand
 // Delta_i = sum_j P_ij dP_ij comes from them, in fp32: dS then sums to zero over a row as it should, where dO . O with an O of bf16 leaves 2^-9 of a term that for a few keys is as
@@ -130,7 +91,9 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
     const uint64_t a_do = umma_desc_sw128(smem_u32(sdO), 16, 1024), b_v = umma_desc_sw128(smem_u32(sV), 16, 1024);
     const uint64_t t_p = umma_desc_sw128(smem_u32(sP), kTileBytes, 1024), k_p = umma_desc_sw128(smem_u32(sP), 16, 1024);   // transposed; as it is
     const uint64_t t_q = umma_desc_sw128(smem_u32(sQ), kTileBytes, 1024), t_do = umma_desc_sw128(smem_u32(sdO), kTileBytes, 1024), t_k = umma_desc_sw128(smem_u32(sK), kTileBytes, 1024);
-    chain_wait();
+    // (The launch before lets this one in once it has waited for its own predecessor, and that for whatever lies before the call; this one reads nothing that they write and
+    // writes other rows.)
+    if (P.alone) chain_wait();
     chain_release();
     const bool fits = P.plan.fits();
     if (!fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
@@ -301,7 +264,58 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
     tc_fence_before();
     __syncthreads();
     if (warp == 0) tmem_dealloc(tmem, kCols);
-    prep_slices(P, first);
+    if (!P.alone && tid == 0) chain_wait();              // this launch is the later one to complete
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// prep
+// ---------------------------------------------------------------------------------------------------------
+struct PackedPrepParams {
+    const uint4* o;         // [T, Hq, D] bf16
+    const uint4* d_o;       // [T, Hq, D] bf16
+    float* delta;           // [Hq, rows]
+    float4* dq_acc;         // [rows, Hq, 64] fp32
+    PlanView plan;
+    int* ticket;
+    int Hq, D, rows;
+};
+// A CTA takes slices of 1024 16-byte chunks of (token, head) rows of 64 by turns; the eight threads of a row reduce Delta by shuffles.
+__global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams P) {
+    chain_wait();
+    chain_release();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.ticket = 0;
+    const int n_tiles = P.plan.word(kPlanLong), chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
+    const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;        // four chunks a thread
+#pragma unroll 1
+    for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
+        const int e = static_cast<int>(k / slices), slice = static_cast<int>(k - static_cast<long long>(e) * slices);
+        const int4 x = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + e));
+        const int left = x.y - x.z * kTile;
+        uint4 vo[4], vd[4];
+        int row[4], c[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int idx = slice * 1024 + u * 256 + static_cast<int>(threadIdx.x);
+            row[u] = idx < per_tile ? small_div(idx, chunks_row) : kTile;
+            c[u] = idx - row[u] * chunks_row;
+            vo[u] = vd[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (row[u] < left && row[u] < kTile && (c[u] & 7) < src_chunks_head) {
+                const size_t src = (static_cast<size_t>(x.x + x.z * kTile + row[u]) * P.Hq + (c[u] >> 3)) * src_chunks_head + (c[u] & 7);
+                vo[u] = __ldg(P.o + src);
+                vd[u] = __ldg(P.d_o + src);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float part = sum8(dot8(vo[u], vd[u]));
+            if (row[u] >= kTile) continue;
+            const size_t to = static_cast<size_t>(x.w + x.z) * kTile + row[u];
+            if ((c[u] & 7) == 0) P.delta[static_cast<size_t>(c[u] >> 3) * P.rows + to] = part;
+            const size_t dst = to * chunks_row + c[u];
+            P.dq_acc[2 * dst] = make_float4(0.f, 0.f, 0.f, 0.f);
+            P.dq_acc[2 * dst + 1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -433,7 +447,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
     }
     if (tid == 0) {
         for (int w = 0; w < 2; ++w) {
-            mbar_init(bar_k_full + w, 32);                   // the loader's lanes: a box's announcing arrival among them, or behind their row copies
+            mbar_init(bar_k_full + w, 1);
             mbar_init(bar_k_free + w, 1);
             mbar_init(bar_s + w, 1);
             mbar_init(bar_dp + w, 1);
@@ -442,10 +456,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             mbar_init(bar_panel + w, kManyTeamWarps);
             mbar_init(bar_kv + w, 1);
         }
-        mbar_init(bar_v_full, 32);
+        mbar_init(bar_v_full, 1);
         mbar_init(bar_v_free, 1);
         for (int s = 0; s < kManyStages; ++s) {
-            mbar_init(bar_q_full + s, 32 + 1);                // the same, and the statistics
+            mbar_init(bar_q_full + s, 2);                     // the boxes' announcing arrival, the statistics
             mbar_init(bar_q_free + s, 2);
         }
         mbar_init(bar_g, 1);
@@ -514,7 +528,6 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         uint32_t t = 0, st = 0, ph = 0, sn = 0, pn = 0;        // query tiles so far, their slot; slot of the tile whose first products come next
         auto wait_slot = [&]() {
             ok &= warp_wait_relaxed(bar_q_full + sn, pn);
-            fence_proxy_async_smem();                          // rows written by asynchronous copies are read by the tensor core
             tc_fence_after();
         };
         auto first = [&](int w) {
@@ -543,10 +556,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
 #pragma unroll 1
         for (uint32_t i = 0; ok && it.len >= 0; ++i) {
             const int n_q = it.steps;
-            it = item_at(i + 1);
 #pragma unroll 1
             for (int x = 0; x < n_q && ok; ++x, ++t) {
-                const bool last = x + 1 == n_q, more = !last || it.len >= 0;
+                const bool last = x + 1 == n_q;
+                bool more = true;
 #pragma unroll 1
                 for (int w = 0; w < 2; ++w) {
                     ok &= warp_wait(bar_handed + w, t & 1);
@@ -564,6 +577,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                         }
                     }
                     __syncwarp();
+                    if (last && w == 0) {                // (an item comes when the loads of the one before have been issued)
+                        it = item_at(i + 1);
+                        more = it.len >= 0;
+                    }
                     if (!more) continue;
                     if (w == 0) {
                         if (last) ok &= warp_wait(bar_kv + warp, (i + 1) & 1);
@@ -581,7 +598,6 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         const uint64_t k_from = umma_desc_sw128(smem_u32(sK), 16, 1024), v_from = umma_desc_sw128(smem_u32(sV), 16, 1024);
         auto copy_kv = [&](uint32_t i, bool v) {               // an item's K or V to tensor memory
             ok &= v ? warp_wait_relaxed(bar_v_full, i & 1) : warp_wait_relaxed(bar_k_full + (i & 1), (i >> 1) & 1);
-            fence_proxy_async_smem();                          // rows written by asynchronous copies are read by the tensor core
             tc_fence_after();
             if (elect_one()) {
                 const uint64_t from = v ? v_from : umma_desc_advance(k_from, (i & 1) * kTileBytes);
@@ -603,9 +619,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         for (uint32_t i = 0; ok && it.len >= 0; ++i) {
             const int n_q = it.steps;
             const uint64_t bk = umma_desc_advance(b_k, (i & 1) * kTileBytes);
-            it = item_at(i + 1);
 #pragma unroll 1
             for (int x = 0; x < n_q && ok; ++x, ++t) {
+                if (x + 1 == n_q) it = item_at(i + 1);
                 if (x + 1 == n_q && it.len >= 0) {           // the last products that read this K (V) are both teams' first ones of this tile
                     ok &= warp_wait(bar_s + 1, t & 1);
                     copy_kv(i + 1, false);
@@ -630,8 +646,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         // ------------------------------------------------------------ loads, items --------------------------------------
         const bool fits = P.plan.fits();
         const long long n_items = fits ? static_cast<long long>(P.plan.word(kPlanLong)) * P.Hkv : 0;
-        auto publish = [&](uint32_t i) {
-            const long long k = turn_item(static_cast<int>(i));
+        auto publish = [&](uint32_t i, long long k) {
             Item it{0, -1, 0, 0, 0, 0, 0, 0};
             if (k < n_items) {
                 const int e = static_cast<int>(k / P.Hkv);
@@ -651,11 +666,16 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             }
             __syncwarp();
         };
-        // A tile of a head, or two of two tensors side by side: as boxes, or, where the sequence ends inside, as rows with zeros behind its end (the next sequence's rows lie
-        // there, and what is zero times something not finite is not zero).  Ends with the arrivals of all lanes.
+        // A tile of a head as rows, where the sequence ends inside: zeros behind its end (the next sequence's rows lie there, and what is zero times something not finite is not
+        // zero).  The copies are waited for and made visible to the tensor core here, so that whoever waits for the tile need not know how it came.
         auto rows_to = [&](unsigned char* to, const __nv_bfloat16* from, long long sT, int tok0, int len) {
 #pragma unroll 1
             for (int g = 0; g < 4; ++g) copy_32_rows(to + g * 32 * kRowBytes, from, sT, nullptr, tok0 + g * 32, len, P.D);
+        };
+        auto rows_done = [&]() {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async_smem();
+            __syncwarp();
         };
         auto load_kv = [&](uint32_t i, const Item& it) {
             ok &= warp_wait_relaxed(bar_k_free + (i & 1), ((i >> 1) & 1) ^ 1);
@@ -668,29 +688,27 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                     tma_load_3d(to, &map_k, bar_k_full + (i & 1), 0, it.kvh, it.start + it.jt * kTile);
                     mbar_expect_tx(bar_v_full, kTileBytes);
                     tma_load_3d(sV, &map_v, bar_v_full, 0, it.kvh, it.start + it.jt * kTile);
-                } else {
-                    mbar_arrive(bar_k_full + (i & 1));
-                    mbar_arrive(bar_v_full);
                 }
             } else {
                 const long long off = it.start * P.sTkv + it.kvh * P.sHkv;
                 rows_to(to, P.k + off, P.sTkv, it.jt * kTile, it.len);
-                cp_async_arrive(bar_k_full + (i & 1));
                 rows_to(sV, P.v + off, P.sTkv, it.jt * kTile, it.len);
-                cp_async_arrive(bar_v_full);
+                rows_done();
+                if (lane == 0) {
+                    mbar_arrive(bar_k_full + (i & 1));
+                    mbar_arrive(bar_v_full);
+                }
             }
             __syncwarp();
         };
         uint32_t st = 0, ph = 0;
-        publish(0);
+        publish(0, blockIdx.x);
         Item next = item_at(0);
         if (next.len >= 0) load_kv(0, next);
 #pragma unroll 1
         for (uint32_t i = 0; ok; ++i) {
             const Item it = next;
             if (it.len < 0) break;
-            publish(i + 1);
-            next = item_at(i + 1);
             const int n_q = it.steps, x0 = (it.len + kTile - 1) / kTile - it.per;
             int h = it.kvh * P.group, x = x0;            // of the step
             // Row statistics of a query tile travel with it, four rows a lane; those of the next tile are asked for ahead of the wait for this one's slot.
@@ -721,6 +739,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                 } else {
                     rows_to(to, P.q + it.start * P.sTq + h * P.sHq, P.sTq, x * kTile, it.len);
                     rows_to(to + kTileBytes, P.d_o + (static_cast<long long>(it.start) * P.Hq + h) * P.D, static_cast<long long>(P.Hq) * P.D, x * kTile, it.len);
+                    rows_done();
+                    if (lane == 0) mbar_arrive(bar_q_full + st);
                 }
                 __syncwarp();
 #pragma unroll
@@ -732,16 +752,16 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                     s_stats[(kManyStages + st) * kTile + e * 32 + lane] = make_uint4(d[0] | d[1] << 16, d[2], 0u, 0u);
                 }
                 fence_proxy_async_smem();
-                __syncwarp();
-                if (!whole) cp_async_arrive(bar_q_full + st);
-                if (!whole ? lane == 0 : true) mbar_arrive(bar_q_full + st);       // (a box's lane 0 has announced it besides)
+                warp_arrive(bar_q_full + st);
                 if (++x == x0 + it.per) { x = x0; ++h; }
                 if (s + 1 < n_q) stats_load(h, x);
                 next_slot(st, ph);
-                if (s == (n_q > 1 ? 1 : 0) && next.len >= 0) load_kv(i + 1, next);
             }
+            if (!ok) break;
+            publish(i + 1, n_items > gridDim.x ? next_item(P.status + kWsTicketBwd, lane) : n_items);
+            next = item_at(i + 1);
+            if (next.len >= 0) load_kv(i + 1, next);
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     }
     } else if (warp < 12) {
         // ------------------------------------------------------------ dQ; dV, dK of an item -----------------------------
@@ -821,7 +841,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                 } else {
                     warp_arrive(bar_gfree);
                 }
-                if (x == 0) item_wait(i + 1);  // (behind the hand-off that the next dQ waits for)
+                if (x + 1 == n_q) item_wait(i + 1);  // (behind the hand-off that the next dQ waits for)
                 ok = group_sync_and(id, ok);             // the panel is complete
                 if (owner && columns) {
                     tma_reduce_add_3d(&map_acc, panel, g * 32, h, (it.base + at) * kTile);
@@ -976,24 +996,33 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
             if (int st = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShortSmemBytes), "packed attention: smem attribute")) return st;
         attr_dev = dev;
     }
-    {
+    auto launch_short = [&]() {
         PackedShortParams R{};
-        R.q = P.q; R.k = P.k; R.v = P.v; R.d_o = P.d_o; R.o = static_cast<const __nv_bfloat16*>(o);
+        R.q = P.q; R.k = P.k; R.v = P.v; R.d_o = P.d_o;
         R.lse = lse;
         R.dq = static_cast<__nv_bfloat16*>(dq); R.dk = P.dk; R.dv = P.dv;
-        R.delta = reinterpret_cast<float*>(base + w.delta);
-        R.dq_acc = reinterpret_cast<float4*>(base + w.dq_acc);
         R.plan = P.plan; R.status = P.status;
         R.sTq = P.sTq; R.sHq = P.sHq; R.sTkv = P.sTkv; R.sHkv = P.sHkv;
-        R.T = P.T; R.Hq = P.Hq; R.Hkv = P.Hkv; R.group = P.group; R.D = P.D; R.rows = P.rows; R.causal = P.causal;
+        R.T = P.T; R.Hq = P.Hq; R.Hkv = P.Hkv; R.group = P.group; R.D = P.D; R.causal = P.causal;
+        R.alone = all_short;
         R.scale = P.scale; R.scale_log2 = P.scale * 1.4426950408889634f;
-        const long long items = tiles * c.Hkv, slices = all_short ? 0 : tiles * ((kTile * c.Hq * 8ll + 1023) / 1024), most = items > slices ? items : slices;
-        const long long places = static_cast<long long>(P.group > 1 ? 1 : kShortPerSm) * sm_count();
+        const long long items = tiles * c.Hkv, places = static_cast<long long>(P.group > 1 ? 1 : kShortPerSm) * sm_count();
         LaunchScope ls_(K_PACKED_SHORT, stream);
-        if (int st = check_cuda(launch_chained(P.group > 1 ? packed_short_kernel<true> : packed_short_kernel<false>, dim3(static_cast<unsigned>(most < places ? most : places)),
-                                               dim3(kShortThreads), kShortSmemBytes, stream, R), "packed attention: backward launch of short sequences")) return st;
+        return check_cuda(launch_chained(P.group > 1 ? packed_short_kernel<true> : packed_short_kernel<false>, dim3(static_cast<unsigned>(items < places ? items : places)),
+                                         dim3(kShortThreads), kShortSmemBytes, stream, R), "packed attention: backward launch of short sequences");
+    };
+    if (all_short) return launch_short();
+    {
+        PackedPrepParams R{};
+        R.o = static_cast<const uint4*>(o); R.d_o = static_cast<const uint4*>(d_o);
+        R.delta = reinterpret_cast<float*>(base + w.delta);
+        R.dq_acc = reinterpret_cast<float4*>(base + w.dq_acc);
+        R.plan = P.plan; R.ticket = P.status + kWsTicketBwd;
+        R.Hq = c.Hq; R.D = c.D; R.rows = w.rows;
+        const long long slices = tiles * ((kTile * c.Hq * 8ll + 1023) / 1024), places = 8ll * sm_count();
+        LaunchScope ls_(K_PACKED_PREP, stream);
+        if (int st = check_cuda(launch_chained(packed_prep_kernel, dim3(static_cast<unsigned>(slices < places ? slices : places)), dim3(256), 0, stream, R), "packed attention: backward prep launch")) return st;
     }
-    if (all_short) return VARDROP_OK;
     CUtensorMap mq, mk, mv, mdo, macc;
     if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
     if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
@@ -1007,6 +1036,7 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
         if (int st = check_cuda(launch_chained(attn_packed_bwd_kernel, dim3(grid), dim3(kManyThreads), kManySmemBytes, stream, mq, mk, mv, mdo, macc, P),
                                 "packed attention: backward launch")) return st;
     }
+    if (int st = launch_short()) return st;
     const long long slices = tiles * ((kTile * c.Hq * (c.D / 8ll) + 1023) / 1024), places = 8ll * sm_count();
     PackedConvertParams F{};
     F.dq_acc = reinterpret_cast<const float4*>(base + w.dq_acc);

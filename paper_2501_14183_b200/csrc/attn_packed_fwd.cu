@@ -149,24 +149,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         it.start = x.x; it.len = x.y; it.qt = x.z; it.h = x.w; it.n_kv = y.x; it.n_act = ok ? y.y : -1; it.split = y.z; it.kvh = y.w;
         return it;
     };
-    // Behind every role's entry code, so that fetching that code overlaps the previous kernel.
-    auto begin = [&]() {
-        chain_wait();
-        chain_release();
-    };
+    // The launch before this one is attn_packed_tile_kernel of the same call, which lets this one in once it has waited for whatever lies before: nothing that is read or
+    // written here is its own but the ticket counter, ahead of which the loader waits for it.
+    chain_release();
 
     if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFwdOtherRegs));
     if (warp == 2) {
         // ---------------------------------------------------------------- loads ----------------------------------
         uint32_t stage_n = 0, n_done = 0;
-        begin();
         const bool fits = P.plan.fits();
         if (!fits && blockIdx.x == 0 && lane == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
         const int pairs = (P.Hq + 1) >> 1;
         const long long n_items = fits ? static_cast<long long>(P.plan.word(kPlanMany)) * pairs : 0;
-        auto publish = [&](uint32_t i) {
-            const long long k = turn_item(static_cast<int>(i));
+        auto publish = [&](uint32_t i, long long k) {
             Item it{0, 0, 0, 0, 0, -1, 0, 0};
             if (k < n_items) {
                 const int e = static_cast<int>(k / pairs), hp = static_cast<int>(k - static_cast<long long>(e) * pairs);
@@ -185,10 +181,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             }
             __syncwarp();
         };
-        publish(0);
+        bool waited = false;
+        publish(0, blockIdx.x);
 #pragma unroll 1
         for (uint32_t i = 0; ok; ++i) {
-            publish(i + 1);
             const Item it = item_at(i);
             if (it.n_act < 0) break;
             const uint32_t qb = n_done & 1;
@@ -218,11 +214,19 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 if (++x == per_step) { x = 0; ++j; }
             }
             ++n_done;
+            if (!ok) break;
+            long long k = n_items;
+            if (n_items > gridDim.x) {
+                if (!waited) chain_wait();               // the counter is zero now
+                waited = true;
+                k = next_item(P.status + kWsTicketFwd, lane);
+            }
+            publish(i + 1, k);
         }
+        if (!waited) chain_wait();                       // this launch is the later one to complete
     } else if (warp == 3) {
         // ---------------------------------------------------------------- V of last tiles -------------------------
         uint32_t stage_n = 0;
-        begin();
 #pragma unroll 1
         for (uint32_t i = 0; ok; ++i) {
             const Item it = item_at(i);
@@ -251,7 +255,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         // Issue warp w serves head w of an item.  Both warps follow every stage of the ring and release it with a commit of their own
         // (a commit with nothing outstanding arrives at once), so the release counts are fixed at two.
         const int w = warp;
-        begin();
         uint32_t stage_n = 0, n_done = 0, n_mine = 0, t = 0;      // ring stages passed, items, items and steps of this head
         const int ks_head = P.D / 16;
         // Operand descriptors are built once and stepped by additions.
@@ -363,7 +366,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
         uint32_t t0 = 0, t1 = 0, n0 = 0, n1 = 0;        // steps and items of the two softmax warpgroups so far
         const int c = r & 7, r0 = (r & ~31) + (lane >> 3);
-        begin();
 #pragma unroll 1
         for (uint32_t i = 0; ok; ++i) {
             const Item it = item_at(i);
@@ -422,7 +424,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t tm_s = tmem + w * 256 + half * 64 + lane_sel, tm_p = tmem + w * 256 + 128 + half * 32 + lane_sel, tm_o = tmem + w * 256 + 192 + lane_sel;
         float* my_max = s_max + w * 4 * kTile + r;
-        begin();
         uint32_t n_mine = 0, t = 0;                     // items and steps of this tile so far
 #pragma unroll 1
         for (uint32_t i = 0; ok; ++i) {
@@ -564,8 +565,7 @@ constexpr uint32_t kTileFwdTmemCols = 128;
 constexpr int kTileFwdSmemBytes = 1024 /*alignment*/ + 3 * kTileBytes /*Q, K, V*/;
 constexpr int kTileFwdPerSm = 4;
 
-// kAll: every tile of the batch is this kernel's, and it is the first launch of the call.  Otherwise it comes behind attn_packed_fwd_kernel, whose CTAs let it in once
-// they have waited for whatever lies before them; it reads nothing that kernel writes and writes other rows, so it waits for it only at its end, to be the later one to complete.
+// kAll: every tile of the batch is this kernel's.  Otherwise attn_packed_fwd_kernel follows, and runs as SMs become free.
 template <bool kAll>
 __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_tile_kernel(const PackedFwdParams P) {
     extern __shared__ unsigned char smem_dyn[];
@@ -592,7 +592,8 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
     const uint64_t d_q = umma_desc_sw128(smem_u32(sQ), 16, 1024), d_k = umma_desc_sw128(smem_u32(sK), 16, 1024);
     const uint64_t d_v = umma_desc_sw128(smem_u32(sV), kTileBytes, 1024);
     const uint64_t scale2 = pair_of(P.scale_log2, P.scale_log2);
-    if (kAll) chain_wait();
+    chain_wait();
+    if (!kAll && blockIdx.x == 0 && tid == 0) P.status[kWsTicketFwd] = 0;
     chain_release();
     const bool fits = P.plan.fits();
     if (!fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
@@ -795,7 +796,6 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
         }
     }
     if (!ok) set_status(P.status, VARDROP_ERR_TIMEOUT);
-    if (!kAll) chain_wait();
     asm volatile("cp.async.wait_all;" ::: "memory");
     tc_fence_before();
     __syncthreads();
@@ -833,14 +833,14 @@ int attn_packed_fwd_launch(const void* q, const void* k, const void* v, const vo
     if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
     if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
     if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
+    {
+        LaunchScope ls_(K_PACKED_TILE, stream);
+        if (int st = check_cuda(launch_chained(attn_packed_tile_kernel<false>, tile_grid, dim3(kTileFwdThreads), kTileFwdSmemBytes, stream, P), "packed attention: forward launch")) return st;
+    }
     const long long worst = tiles * ((c.Hq + 1) / 2);
     const int grid = static_cast<int>(worst < sm_count() ? worst : sm_count());                 // one CTA per SM
-    {
-        LaunchScope ls_(K_PACKED_FWD, stream);
-        if (int st = check_cuda(launch_chained(attn_packed_fwd_kernel, dim3(grid), dim3(kFwdThreads), kFwdSmemBytes, stream, mq, mk, mv, P), "packed attention: forward launch")) return st;
-    }
-    LaunchScope ls_(K_PACKED_TILE, stream);
-    return check_cuda(launch_chained(attn_packed_tile_kernel<false>, tile_grid, dim3(kTileFwdThreads), kTileFwdSmemBytes, stream, P), "packed attention: forward launch");
+    LaunchScope ls_(K_PACKED_FWD, stream);
+    return check_cuda(launch_chained(attn_packed_fwd_kernel, dim3(grid), dim3(kFwdThreads), kFwdSmemBytes, stream, mq, mk, mv, P), "packed attention: forward launch");
 }
 
 }  // namespace vardrop

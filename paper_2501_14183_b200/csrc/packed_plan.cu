@@ -27,36 +27,38 @@ __device__ __forceinline__ int block_scan(int v, int* s_warp) {      // exclusiv
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
     if (warp == 0) {
-        int w = s_warp[lane];
+        int w = lane < static_cast<int>(blockDim.x >> 5) ? s_warp[lane] : 0;
+        const int mine = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, w, o);
             if (lane >= o) w += y;
         }
         if (lane == 31) s_warp[32] = w;
-        s_warp[lane] = w - s_warp[lane];
+        s_warp[lane] = w - mine;
     }
     __syncthreads();
     return x - v + s_warp[warp];
 }
 
-// Counting sort: tiles per amount of work, then each tile's place.  Sequences come 1024 at a time, a thread each; their tiles are shared out over all threads again, so a
+// (128 threads for up to 128 sequences, whose barriers are the cheaper ones; 1024 beyond.)
+// Counting sort: tiles per amount of work, then each tile's place.  Sequences come a thread each, as many at a time as there are threads; their tiles are shared out over all threads again, so a
 // single long sequence takes no longer than many short ones.
 __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanParams P) {
     __shared__ int s_warp[33], s_bin[kPlanBins + 1], s_bad;
     __shared__ int s_first[kPlanThreads + 1], s_start[kPlanThreads], s_len[kPlanThreads];
     chain_wait();
     chain_release();
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, nt = blockDim.x;
     const int bins = P.bins + 1;             // the last one: sequences of a single tile
-    for (int b = tid; b < bins; b += kPlanThreads) s_bin[b] = 0;
+    for (int b = tid; b < bins; b += nt) s_bin[b] = 0;
     if (tid == 0) s_bad = 0;
     __syncthreads();
     int total = 0, many = 0, longer = 0;
     for (int pass = 0; pass < 2; ++pass) {
         int ahead = 0;
-        for (int s0 = 0; s0 < P.n_seqs; s0 += kPlanThreads) {
-            if (pass == 0 || P.n_seqs > kPlanThreads) {
+        for (int s0 = 0; s0 < P.n_seqs; s0 += nt) {
+            if (pass == 0 || P.n_seqs > nt) {
                 const int s = s0 + tid;
                 int start = 0, end = 0;
                 if (s < P.n_seqs) {
@@ -72,13 +74,13 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
                 s_first[tid] = at;
                 s_start[tid] = start;
                 s_len[tid] = end - start;
-                if (tid == 0) s_first[kPlanThreads] = s_warp[32];
+                if (tid == 0) s_first[nt] = s_warp[32];
                 __syncthreads();
             }
             if (s_bad) break;                                // (as long as no offset decreases the tiles cannot be more than the plan has room for)
-            const int count = s_first[kPlanThreads];
-            for (int t = tid; t < count; t += kPlanThreads) {
-                int lo = 0, hi = kPlanThreads - 1;           // last sequence whose first tile is not behind t: empty ones have their successor's
+            const int count = s_first[nt];
+            for (int t = tid; t < count; t += nt) {
+                int lo = 0, hi = nt - 1;           // last sequence whose first tile is not behind t: empty ones have their successor's
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) >> 1;
                     if (s_first[mid] <= t) lo = mid;
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
         if (pass == 0) {
             total = ahead;
             int run = 0;
-            for (int b0 = 0; b0 < bins; b0 += kPlanThreads) {
+            for (int b0 = 0; b0 < bins; b0 += nt) {
                 const int b = b0 + tid, v = b < bins ? s_bin[b] : 0;
                 const int at = block_scan(v, s_warp);
                 if (b < bins) s_bin[b] = run + at;
@@ -188,7 +190,7 @@ int packed_plan_launch(const int32_t* cu_seqlens, const vardrop_packed_cfg& c, v
     P.bins = longest < kPlanBins ? longest : kPlanBins;
     P.cap = packed_tiles(c);
     LaunchScope ls_(K_PACKED_PLAN, stream);
-    return check_cuda(launch_chained(packed_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, P), "packed attention: plan launch");
+    return check_cuda(launch_chained(packed_plan_kernel, dim3(1), dim3(c.n_seqs <= 128 ? 128 : kPlanThreads), 0, stream, P), "packed attention: plan launch");
 }
 
 }  // namespace vardrop
