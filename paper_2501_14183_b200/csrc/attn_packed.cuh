@@ -64,16 +64,34 @@ __device__ __forceinline__ void tma_reduce_add_3d(const void* map, const void* s
                  : "memory");
 }
 
+// One warp's share of a tile of consecutive rows: 32 from tok0 on by 16-byte asynchronous copies, zeros from `len` on and in the upper half of a row of 32.
+__device__ __forceinline__ void copy_32_tokens(unsigned char* rows, const __nv_bfloat16* from, long long sT, int tok0, int len, int D) {
+    const int lane = threadIdx.x & 31, chunk = lane & 7, r = lane >> 3;
+    const uint32_t live = chunk * 8 < D ? 16u : 0u;
+    const __nv_bfloat16* const begin = from + (live ? chunk * 8 : 0);
+    const __nv_bfloat16* src = begin + (tok0 + r) * sT;
+    const uint32_t dst = smem_u32(rows) + r * kRowBytes + (static_cast<uint32_t>(chunk ^ r) << 4);
+    const int left = len - tok0 - r;
+#pragma unroll
+    for (int it = 0; it < 8; ++it, src += 4 * sT) cp_async16((dst ^ ((it & 1) * 64u)) + it * 4 * kRowBytes, 4 * it < left ? src : begin, 4 * it < left ? live : 0u);
+}
+
 // What a kernel needs of the plan's header: the number of tiles, 0 where it is not a plan of this call's kind (which the caller reports).
 struct PlanView {
     const int32_t* words;
     int n_seqs, T, causal;
-    __device__ __forceinline__ bool fits() const {
-        return words[kPlanStatus] == VARDROP_OK && words[kPlanMagicWord] == kPlanMagic && words[kPlanSeqs] == n_seqs && words[kPlanRows] == T && words[kPlanCausal] == causal;
-    }
     __device__ __forceinline__ const PlanEntry* entries() const { return reinterpret_cast<const PlanEntry*>(words + kWsHeaderBytes / 4); }
-    __device__ __forceinline__ int word(PlanWord w) const { return fits() ? words[w] : 0; }
 };
+struct PlanHead {
+    bool fits;                           // a plan of this call's kind
+    int tiles, many, longer;             // 0 where it is not
+};
+__device__ __forceinline__ PlanHead plan_head(const PlanView& v) {
+    const int4 a = *reinterpret_cast<const int4*>(v.words), b = *reinterpret_cast<const int4*>(v.words + 4);       // both at once
+    static_assert(kPlanStatus == 0 && kPlanMagicWord == 1 && kPlanTiles == 2 && kPlanSeqs == 3 && kPlanRows == 4 && kPlanCausal == 5 && kPlanMany == 6 && kPlanLong == 7, "order of the header");
+    const bool fits = a.x == VARDROP_OK && a.y == kPlanMagic && a.w == v.n_seqs && b.x == v.T && b.y == v.causal;
+    return PlanHead{fits, fits ? a.z : 0, fits ? b.z : 0, fits ? b.w : 0};
+}
 
 // Items beyond a CTA's first one are handed out by a counter in the workspace's header, which an earlier launch of the call has set to zero: they come with the most work first, so whoever
 // is free takes the largest that is left.  (Turns there and back over the grid left SMs idle for 12 % of the forward and 14 % of the backward of two sequences of 8192 and 5001

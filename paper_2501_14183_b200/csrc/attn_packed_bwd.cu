@@ -95,9 +95,9 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
     // writes other rows.)
     if (P.alone) chain_wait();
     chain_release();
-    const bool fits = P.plan.fits();
-    if (!fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
-    const int first = fits ? P.plan.words[kPlanLong] : 0, n_items = fits ? (P.plan.words[kPlanTiles] - first) * P.Hkv : 0;
+    const PlanHead head = plan_head(P.plan);
+    if (!head.fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
+    const int first = head.longer, n_items = (head.tiles - first) * P.Hkv;
     bool ok = true;
     uint32_t phase = 0;
     auto wait = [&]() {                                  // for the products behind the last commit
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
                 const __nv_bfloat16* from = tile == 0 ? P.q + start * P.sTq + h * P.sHq
                                             : tile == 1 ? P.d_o + (static_cast<long long>(start) * P.Hq + h) * P.D
                                             : (tile == 2 ? P.k : P.v) + kv_off;
-                copy_32_rows(smem_dyn + tile * kTileBytes + r0 * kRowBytes, from, tile == 0 ? P.sTq : tile == 1 ? static_cast<long long>(P.Hq) * P.D : P.sTkv, nullptr, r0, len, P.D);
+                copy_32_tokens(smem_dyn + tile * kTileBytes + r0 * kRowBytes, from, tile == 0 ? P.sTq : tile == 1 ? static_cast<long long>(P.Hq) * P.D : P.sTkv, r0, len, P.D);
             }
             const float lse2 = row < len ? __ldg(P.lse + static_cast<size_t>(h) * P.T + start + row) * 1.4426950408889634f : 0.f;
             asm volatile("cp.async.wait_all;" ::: "memory");
@@ -230,27 +230,38 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
                 __syncwarp();
             }
             wait();
-            // ---- rows out, half of the columns a thread ----
-            auto rows_out = [&](uint32_t col, __nv_bfloat16* to, float mul) {
-                const int c0 = half * (P.D / 2);
+            // ---- rows out, half of the columns a thread, through tiles that have been read, so that whole rows are written ----
+            const bool last = !kGrouped || g + 1 == P.group;
+            auto stage = [&](unsigned char* tile, uint32_t col, float mul) {
 #pragma unroll 1
-                for (int c = c0; c < c0 + P.D / 2; c += 16) {
+                for (int c = half * (P.D / 2); c < (half + 1) * (P.D / 2); c += 16) {
                     float v[16];
                     tmem_ld16(tm + col + c, v);
                     tmem_ld_wait();
-                    if (row < len) {
 #pragma unroll
-                        for (int q = 0; q < 2; ++q)
-                            *reinterpret_cast<uint4*>(to + c + 8 * q) = make_uint4(pack2(v[8 * q] * mul, v[8 * q + 1] * mul), pack2(v[8 * q + 2] * mul, v[8 * q + 3] * mul),
-                                                                                   pack2(v[8 * q + 4] * mul, v[8 * q + 5] * mul), pack2(v[8 * q + 6] * mul, v[8 * q + 7] * mul));
-                    }
+                    for (int q = 0; q < 2; ++q)
+                        *reinterpret_cast<uint4*>(tile + row * kRowBytes + ((((c >> 3) + q) ^ (row & 7)) << 4)) =
+                            make_uint4(pack2(v[8 * q] * mul, v[8 * q + 1] * mul), pack2(v[8 * q + 2] * mul, v[8 * q + 3] * mul),
+                                       pack2(v[8 * q + 4] * mul, v[8 * q + 5] * mul), pack2(v[8 * q + 6] * mul, v[8 * q + 7] * mul));
                 }
             };
-            rows_out(kDq, P.dq + (static_cast<size_t>(start + row) * P.Hq + h) * P.D, P.scale);
-            if (!kGrouped || g + 1 == P.group) {
-                const size_t to = (static_cast<size_t>(start + row) * P.Hkv + kvh) * P.D;
-                rows_out(kDv, P.dv + to, 1.f);
-                rows_out(kDk, P.dk + to, P.scale);
+            stage(sQ, kDq, P.scale);
+            if (last) {
+                stage(sdO, kDv, 1.f);
+                stage(sP, kDk, P.scale);
+            }
+            __syncthreads();
+            const int chunks_row = P.D >> 3, sh = P.D > 32 ? 3 : 2;
+#pragma unroll 1
+            for (int x = 0; x < (last ? 3 : 1); ++x) {
+                const unsigned char* tile = x == 0 ? sQ : x == 1 ? sdO : sP;
+                const int heads = x == 0 ? P.Hq : P.Hkv;
+                __nv_bfloat16* to = (x == 0 ? P.dq : x == 1 ? P.dv : P.dk) + (static_cast<size_t>(start) * heads + (x == 0 ? h : kvh)) * P.D;
+#pragma unroll 4
+                for (int at = tid; at < len << sh; at += kShortThreads) {
+                    const int r = at >> sh, c = at & (chunks_row - 1);
+                    *reinterpret_cast<uint4*>(to + static_cast<size_t>(r) * heads * P.D + c * 8) = *reinterpret_cast<const uint4*>(tile + r * kRowBytes + ((c ^ (r & 7)) << 4));
+                }
             }
             tc_fence_before();
             ok = __syncthreads_and(ok);                  // tiles and columns are free
@@ -284,7 +295,7 @@ __global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams
     chain_wait();
     chain_release();
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.ticket = 0;
-    const int n_tiles = P.plan.word(kPlanLong), chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
+    const int n_tiles = plan_head(P.plan).longer, chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
     const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;        // four chunks a thread
 #pragma unroll 1
     for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
@@ -644,8 +655,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         }
     } else {
         // ------------------------------------------------------------ loads, items --------------------------------------
-        const bool fits = P.plan.fits();
-        const long long n_items = fits ? static_cast<long long>(P.plan.word(kPlanLong)) * P.Hkv : 0;
+        const long long n_items = static_cast<long long>(plan_head(P.plan).longer) * P.Hkv;
         auto publish = [&](uint32_t i, long long k) {
             Item it{0, -1, 0, 0, 0, 0, 0, 0};
             if (k < n_items) {
@@ -670,7 +680,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         // zero).  The copies are waited for and made visible to the tensor core here, so that whoever waits for the tile need not know how it came.
         auto rows_to = [&](unsigned char* to, const __nv_bfloat16* from, long long sT, int tok0, int len) {
 #pragma unroll 1
-            for (int g = 0; g < 4; ++g) copy_32_rows(to + g * 32 * kRowBytes, from, sT, nullptr, tok0 + g * 32, len, P.D);
+            for (int g = 0; g < 4; ++g) copy_32_tokens(to + g * 32 * kRowBytes, from, sT, tok0 + g * 32, len, P.D);
         };
         auto rows_done = [&]() {
             asm volatile("cp.async.wait_all;" ::: "memory");
@@ -936,7 +946,7 @@ struct PackedConvertParams {
 __global__ void __launch_bounds__(256) packed_convert_kernel(const PackedConvertParams P) {
     chain_wait();
     chain_release();
-    const int n_tiles = P.plan.word(kPlanLong), sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;        // 16-byte results per row
+    const int n_tiles = plan_head(P.plan).longer, sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;        // 16-byte results per row
     const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;
     for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
         const int e = static_cast<int>(k / slices), slice = static_cast<int>(k - static_cast<long long>(e) * slices);
