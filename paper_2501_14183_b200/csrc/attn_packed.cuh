@@ -10,7 +10,8 @@ namespace vardrop {
 // last.
 constexpr int kPlanMagic = 0x56445031;
 constexpr int kFewTiles = 2;             // forward: tiles with no more key tiles than this are attn_packed_tile_kernel's
-enum PlanWord { kPlanStatus = 0, kPlanMagicWord, kPlanTiles, kPlanSeqs, kPlanRows, kPlanCausal, kPlanMany /*entries ahead of those with few key tiles*/, kPlanLong /*entries of sequences of several tiles*/ };
+enum PlanWord { kPlanStatus = 0, kPlanMagicWord, kPlanTiles, kPlanSeqs, kPlanRows, kPlanCausal, kPlanMany /*entries ahead of those with few key tiles*/, kPlanLong /*entries of sequences of several tiles*/,
+                kPlanMostWork /*of one of those, in tiles*/, kPlanWork /*of all of them, fp32*/ };
 struct alignas(16) PlanEntry {
     int start;              // row of the sequence's first token
     int len;                // its tokens
@@ -21,9 +22,16 @@ struct alignas(16) PlanEntry {
 // Tiles that a batch can have at most: a sequence's last one may hold a single token.
 inline long long packed_tiles(const vardrop_packed_cfg& c) { return c.T / kTile + (c.n_seqs < c.T ? c.n_seqs : c.T); }
 
+// Backward, an item (a key tile of a key head) whose query tiles take longer than half of what an SM has to do altogether is split into up to four, whose parts of dK and dV
+// lie in the workspace until the conversion adds them up: largest items bound a call of few, and grouped heads make them large (12 windows of 1 to 1999 tokens, 8 query heads on 2
+// key heads: 148 items, one of 64 steps where an SM's share is 24).  Calls of many tiles do without.
+constexpr int kMostParts = 4, kSplitTiles = 1024, kLeastSteps = 8;
+inline bool packed_may_split(const vardrop_packed_cfg& c) { return packed_tiles(c) * c.Hkv <= kSplitTiles; }
+
 struct PackedWs {
     size_t delta;           // [Hq, tiles 128] fp32
     size_t dq_acc;          // [tiles 128, Hq, 64] fp32
+    size_t parts;           // [tiles 128, (dV, dK), part, Hkv, 64] fp32
     size_t total;
     int rows;               // tiles 128
 };
@@ -33,6 +41,7 @@ inline PackedWs packed_layout(const vardrop_packed_cfg& c) {
     size_t o = align_up(kWsHeaderBytes, 1024);
     w.delta = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * w.rows, 1024);
     w.dq_acc = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * kDP * w.rows, 1024);
+    w.parts = o; o += packed_may_split(c) ? align_up(sizeof(float) * 2 * kMostParts * c.Hkv * kDP * static_cast<size_t>(w.rows), 1024) : 0;
     w.total = o;
     return w;
 }
@@ -76,6 +85,12 @@ __device__ __forceinline__ void copy_32_tokens(unsigned char* rows, const __nv_b
     for (int it = 0; it < 8; ++it, src += 4 * sT) cp_async16((dst ^ ((it & 1) * 64u)) + it * 4 * kRowBytes, 4 * it < left ? src : begin, 4 * it < left ? live : 0u);
 }
 
+__device__ __forceinline__ void tma_store_3d(const void* map, const void* src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+
 // What a kernel needs of the plan's header: the number of tiles, 0 where it is not a plan of this call's kind (which the caller reports).
 struct PlanView {
     const int32_t* words;
@@ -93,14 +108,28 @@ __device__ __forceinline__ PlanHead plan_head(const PlanView& v) {
     return PlanHead{fits, fits ? a.z : 0, fits ? b.z : 0, fits ? b.w : 0};
 }
 
+// How the backward pass splits items: `parts` of an entry at most, one of `steps` query tiles (over all heads of a group) into ceil(steps / chunk).
+struct Split {
+    int parts, chunk;
+};
+__device__ __forceinline__ Split split_of(const PlanView& v, const PlanHead& head, int group, int Hkv, int sms, bool may) {
+    if (head.longer == 0) return Split{1, 1};
+    const int most = v.words[kPlanMostWork] * group;
+    const float share = __int_as_float(v.words[kPlanWork]) * static_cast<float>(group * Hkv) / static_cast<float>(sms);
+    int chunk = most;
+    if (may) chunk = min(most, max(max(kLeastSteps, static_cast<int>(0.5f * share)), (most + kMostParts - 1) / kMostParts));
+    return Split{(most + chunk - 1) / chunk, chunk};
+}
+__device__ __forceinline__ int parts_of(int steps, const Split& s) { return (steps + s.chunk - 1) / s.chunk; }
+
 // Items beyond a CTA's first one are handed out by a counter in the workspace's header, which an earlier launch of the call has set to zero: they come with the most work first, so whoever
 // is free takes the largest that is left.  (Turns there and back over the grid left SMs idle for 12 % of the forward and 14 % of the backward of two sequences of 8192 and 5001
 // tokens, 16 query heads.)  An item is asked for when the loads of the one before have been issued, not earlier: one held ahead is one that somebody else could have begun.
 constexpr int kWsTicketFwd = 8, kWsTicketBwd = 9;        // words of the header
-__device__ __forceinline__ long long next_item(int* ticket, int lane) {
+__device__ __forceinline__ long long next_item(int* ticket, int ctas, int lane) {      // ctas: that have had a first one
     int t = 0;
     if (lane == 0) t = atomicAdd(ticket, 1);
-    return static_cast<long long>(gridDim.x) + __shfl_sync(0xffffffffu, t, 0);
+    return static_cast<long long>(ctas) + __shfl_sync(0xffffffffu, t, 0);
 }
 
 }  // namespace vardrop

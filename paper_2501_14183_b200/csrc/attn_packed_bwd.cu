@@ -24,6 +24,7 @@ struct PackedBwdParams {
     int* status;
     long long sTq, sHq, sTkv, sHkv;
     int T, Hq, Hkv, group, D, rows, causal;
+    int may_split;
     float scale, scale_log2, half_inv_scale;      // of dK; in the exponents, and 0.5 / scale there
 };
 
@@ -410,7 +411,8 @@ constexpr uint32_t kColK = 0, kColV = 32, kColDv = 64, kColDk = 128, kColDq = 19
 
 __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do,
-                                                                           const __grid_constant__ CUtensorMap map_acc, const PackedBwdParams P) {
+                                                                           const __grid_constant__ CUtensorMap map_acc, const __grid_constant__ CUtensorMap map_parts,
+                                                                           const PackedBwdParams P) {
     extern __shared__ __align__(1024) unsigned char smem_dyn[];      // (every address below is a constant then: no registers)
     // Set-up first: it touches nothing another kernel produces, so it runs while the previous kernel of the stream is still finishing.
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem_dyn);
@@ -435,8 +437,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
     uint64_t* bar_item = bars + 30;                 // [8] entry of the item list is written
     uint64_t* bar_left = bars + 39;                 // [3] what an issuing warp whose wait gave up has issued is done
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 38);
-    // Key tile jt of a sequence and key head kvh.  steps: query tiles of all its query heads, `per` of each, which end with the sequence; len < 0 ends the list.
-    struct alignas(16) Item { int start, len, jt, kvh, base, steps, per, pad; };
+    // Key tile jt of a sequence and a key head (kvh: that, and 4096 (1 + part) for one of several parts).  steps: query tiles from the s0-th on of those of all its query heads,
+    // `per` of each, which end with the sequence; len < 0 ends the list.
+    struct alignas(16) Item { int start, len, jt, kvh, base, steps, per, s0; };
     Item* s_item = reinterpret_cast<Item*>(smem_dyn + 512);         // [8]
     uint4* s_ones = reinterpret_cast<uint4*>(smem_dyn + 768);       // [8] bf16 rows of three ones
     uint4* s_stats = s_ones + 8;                                    // [2][kManyStages][128] three bf16 terms of half of -lse / scale, of half of -Delta, of the slot's rows
@@ -487,6 +490,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
         tma_prefetch_desc(&map_acc);
+        if (P.may_split) tma_prefetch_desc(&map_parts);
     }
     if (tid < 8) s_ones[tid] = make_uint4(0x3f803f80u, 0x00003f80u, 0u, 0u);
     fence_proxy_async_smem();
@@ -503,7 +507,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
     auto item_read = [&](uint32_t i) {
         const int4* from = reinterpret_cast<const int4*>(s_item + (i & 7));
         const int4 x = from[0], y = from[1];
-        return Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, 0};
+        return Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
     };
     auto item_at = [&](uint32_t i) {                           // len -1 for an item that did not come
         item_wait(i);
@@ -655,23 +659,38 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         }
     } else {
         // ------------------------------------------------------------ loads, items --------------------------------------
-        const long long n_items = static_cast<long long>(plan_head(P.plan).longer) * P.Hkv;
+        const PlanHead head = plan_head(P.plan);
+        const Split split = split_of(P.plan, head, P.group, P.Hkv, gridDim.x, P.may_split);
+        const int units = P.Hkv * split.parts;                 // of a plan entry
+        const long long n_items = static_cast<long long>(head.longer) * units;
+        // Some SMs are left to packed_short_kernel, which comes next: by the time that either takes, in steps of this kernel: one of the short kernel's heads is three of them (a
+        // CTA, of which an SM holds two without groups), and an item here has the latency of five besides its own.
+        int ctas = gridDim.x;
+        if (head.longer > 0 && head.tiles > head.longer) {
+            const float shorts = static_cast<float>(head.tiles - head.longer) * static_cast<float>(P.Hq) * (P.group > 1 ? 3.f : 1.5f);
+            const float mine = __int_as_float(P.plan.words[kPlanWork]) * static_cast<float>(P.Hq) + 5.f * static_cast<float>(n_items);
+            ctas = max(1, ctas - max(1, __float2int_rn(static_cast<float>(ctas) * (shorts / (shorts + mine)))));
+        }
         auto publish = [&](uint32_t i, long long k) {
             Item it{0, -1, 0, 0, 0, 0, 0, 0};
-            if (k < n_items) {
-                const int e = static_cast<int>(k / P.Hkv);
+#pragma unroll 1
+            for (; k < n_items; k = next_item(P.status + kWsTicketBwd, ctas, lane)) {
+                const int e = static_cast<int>(k / units), unit = static_cast<int>(k - static_cast<long long>(e) * units), kvh = small_div(unit, split.parts), part = unit - kvh * split.parts;
                 const int4 x = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + e));
-                const int n_t = (x.y + kTile - 1) / kTile;
+                const int n_t = (x.y + kTile - 1) / kTile, jt = P.causal ? n_t - 1 - x.z : x.z, per = P.causal ? n_t - jt : n_t, steps = per * P.group;
+                const int parts = parts_of(steps, split), share = (steps + parts - 1) / parts;
+                if (part * share >= steps) continue;           // an entry of fewer parts
                 it.start = x.x; it.len = x.y; it.base = x.w;
-                it.kvh = static_cast<int>(k - static_cast<long long>(e) * P.Hkv);
-                it.jt = P.causal ? n_t - 1 - x.z : x.z;
-                it.per = P.causal ? n_t - it.jt : n_t;
-                it.steps = it.per * P.group;
+                it.jt = jt; it.per = per;
+                it.kvh = kvh + (parts > 1 ? (1 + part) << 12 : 0);
+                it.s0 = part * share;
+                it.steps = min(share, steps - it.s0);
+                break;
             }
             if (lane == 0) {
                 int4* to = reinterpret_cast<int4*>(s_item + (i & 7));
                 to[0] = make_int4(it.start, it.len, it.jt, it.kvh);
-                to[1] = make_int4(it.base, it.steps, it.per, 0);
+                to[1] = make_int4(it.base, it.steps, it.per, it.s0);
                 mbar_arrive(bar_item + (i & 7));
             }
             __syncwarp();
@@ -692,15 +711,16 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             ok &= warp_wait_relaxed(bar_v_free, (i & 1) ^ 1);
             if (!ok) return;
             unsigned char* to = sK + (i & 1) * kTileBytes;
+            const int kvh = it.kvh & 4095;
             if ((it.jt + 1) * kTile <= it.len) {
                 if (lane == 0) {
                     mbar_expect_tx(bar_k_full + (i & 1), kTileBytes);
-                    tma_load_3d(to, &map_k, bar_k_full + (i & 1), 0, it.kvh, it.start + it.jt * kTile);
+                    tma_load_3d(to, &map_k, bar_k_full + (i & 1), 0, kvh, it.start + it.jt * kTile);
                     mbar_expect_tx(bar_v_full, kTileBytes);
-                    tma_load_3d(sV, &map_v, bar_v_full, 0, it.kvh, it.start + it.jt * kTile);
+                    tma_load_3d(sV, &map_v, bar_v_full, 0, kvh, it.start + it.jt * kTile);
                 }
             } else {
-                const long long off = it.start * P.sTkv + it.kvh * P.sHkv;
+                const long long off = it.start * P.sTkv + kvh * P.sHkv;
                 rows_to(to, P.k + off, P.sTkv, it.jt * kTile, it.len);
                 rows_to(sV, P.v + off, P.sTkv, it.jt * kTile, it.len);
                 rows_done();
@@ -712,7 +732,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             __syncwarp();
         };
         uint32_t st = 0, ph = 0;
-        publish(0, blockIdx.x);
+        publish(0, static_cast<int>(blockIdx.x) < ctas ? static_cast<long long>(blockIdx.x) : n_items);
         Item next = item_at(0);
         if (next.len >= 0) load_kv(0, next);
 #pragma unroll 1
@@ -720,7 +740,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             const Item it = next;
             if (it.len < 0) break;
             const int n_q = it.steps, x0 = (it.len + kTile - 1) / kTile - it.per;
-            int h = it.kvh * P.group, x = x0;            // of the step
+            int h = (it.kvh & 4095) * P.group + small_div(it.s0, it.per), x = x0 + it.s0 - small_div(it.s0, it.per) * it.per;            // of the step
             // Row statistics of a query tile travel with it, four rows a lane; those of the next tile are asked for ahead of the wait for this one's slot.
             float st_lse[4], st_delta[4];
             auto stats_load = [&](int h, int x) {
@@ -768,7 +788,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                 next_slot(st, ph);
             }
             if (!ok) break;
-            publish(i + 1, n_items > gridDim.x ? next_item(P.status + kWsTicketBwd, lane) : n_items);
+            publish(i + 1, n_items > ctas ? next_item(P.status + kWsTicketBwd, ctas, lane) : n_items);
             next = item_at(i + 1);
             if (next.len >= 0) load_kv(i + 1, next);
         }
@@ -798,6 +818,33 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             const int n_q = it.steps;
             // dV or dK of the item's keys: a warp's 32 rows through its part of the panel, eight lanes a row
             auto rows_out = [&](uint32_t col, uint64_t* done, uint64_t* freed, float mul, __nv_bfloat16* dst) {
+                if (it.kvh >= 4096) {                    // one of several parts: as fp32, the panel's 32 columns at a time
+#pragma unroll 1
+                    for (int c = 0; c < P.D; c += 32) {
+                        panel_free();
+                        if (c == 0) {
+                            ok &= warp_wait_relaxed(done, i & 1);
+                            tc_fence_after();
+                        }
+                        float v[32];
+                        tmem_ld32(tm + col + c, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            *reinterpret_cast<float4*>(rowp + ((e ^ (row & 7)) << 4)) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                        fence_proxy_async_smem();
+                        if (c + 32 >= P.D) {
+                            tc_fence_before();
+                            warp_arrive(freed);
+                        }
+                        ok = group_sync_and(id, ok);
+                        if (owner) {
+                            tma_store_3d(&map_parts, panel, c, (g * kMostParts + (it.kvh >> 12) - 1) * P.Hkv + (it.kvh & 4095), (it.base + it.jt) * kTile);
+                            bulk_commit_group();
+                        }
+                    }
+                    return;
+                }
                 panel_free();
                 ok &= warp_wait_relaxed(done, i & 1);
                 tc_fence_after();
@@ -817,7 +864,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                 const int c8 = lane & 7;
                 if (c8 * 8 < P.D) {
                     const int row0 = it.jt * kTile + (warp & 3) * 32 + (lane >> 3), left = it.len - row0;         // rows 4 apart, as long as they exist
-                    __nv_bfloat16* out = dst + (static_cast<size_t>(it.start + row0) * P.Hkv + it.kvh) * P.D + c8 * 8;
+                    __nv_bfloat16* out = dst + (static_cast<size_t>(it.start + row0) * P.Hkv + (it.kvh & 4095)) * P.D + c8 * 8;
                     const unsigned char* from = panel + ((warp & 3) * 32 + (lane >> 3)) * kRowBytes;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
@@ -827,7 +874,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                 }
             };
             const int x0 = (it.len + kTile - 1) / kTile - it.per;
-            int h = it.kvh * P.group, at = x0;           // of the step
+            const int g0 = small_div(it.s0, it.per);
+            int h = (it.kvh & 4095) * P.group + g0, at = x0 + it.s0 - g0 * it.per;           // of the step
             int x = 0;
 #pragma unroll 1
             do {
@@ -879,7 +927,12 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             // Rows of keys that do not exist are zeros and their dV, dK go nowhere; P^T = 1 keeps what they add to dQ at zero.
             const float scale = it.jt * kTile + row < it.len ? P.scale_log2 : 0.f;
             const uint64_t scale2 = pair_of(scale, scale);
-            int diagonal = P.causal ? 0 : -1;            // step of the next query tile on the diagonal: the first of every head
+            // step of the next query tile on the diagonal: the first of every head
+            int diagonal = -1;
+            if (P.causal) {
+                const int into = it.s0 - small_div(it.s0, it.per) * it.per;
+                diagonal = into == 0 ? 0 : it.per - into;
+            }
 #pragma unroll 1
             for (int x = 0; x < n_q && ok; ++x, ++t) {
                 if (!__all_sync(0xffffffffu, s_ready)) ok &= warp_wait(bar_s + w, t & 1);
@@ -939,14 +992,17 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
 struct PackedConvertParams {
     const float4* dq_acc;    // [rows, Hq, 64] fp32
     uint4* dq;               // [T, Hq, D] bf16
+    const float4* parts;     // [rows, (dV, dK), part, Hkv, 64] fp32
+    uint4 *dv, *dk;          // [T, Hkv, D] bf16
     PlanView plan;
-    int Hq, D;
+    int Hq, Hkv, group, D, causal, may_split, main_grid;
     float scale;
 };
 __global__ void __launch_bounds__(256) packed_convert_kernel(const PackedConvertParams P) {
     chain_wait();
     chain_release();
-    const int n_tiles = plan_head(P.plan).longer, sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;        // 16-byte results per row
+    const PlanHead head = plan_head(P.plan);
+    const int n_tiles = head.longer, sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;        // 16-byte results per row
     const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;
     for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
         const int e = static_cast<int>(k / slices), slice = static_cast<int>(k - static_cast<long long>(e) * slices);
@@ -971,6 +1027,30 @@ __global__ void __launch_bounds__(256) packed_convert_kernel(const PackedConvert
                                      pack2(a[u][1].x * P.scale, a[u][1].y * P.scale), pack2(a[u][1].z * P.scale, a[u][1].w * P.scale));
         }
     }
+    // dV and dK of key tiles that were worked off in parts, which are added up in their order
+    const Split split = split_of(P.plan, head, P.group, P.Hkv, P.main_grid, P.may_split);
+    if (split.parts == 1) return;
+    const int kv_row = P.Hkv << sh, kv_tile = 2 * kTile * kv_row, kv_slices = (kv_tile + 255) / 256;
+    for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * kv_slices; k += gridDim.x) {
+        const int e = static_cast<int>(k / kv_slices), slice = static_cast<int>(k - static_cast<long long>(e) * kv_slices);
+        const int4 x = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + e));
+        const int n_t = (x.y + kTile - 1) / kTile, jt = P.causal ? n_t - 1 - x.z : x.z, parts = parts_of((P.causal ? n_t - jt : n_t) * P.group, split);
+        if (parts == 1) break;               // entries come with the most work first
+        const int idx = slice * 256 + static_cast<int>(threadIdx.x), which = idx >= kTile * kv_row ? 1 : 0, in = idx - which * kTile * kv_row;
+        const int row = small_div(in, kv_row), c = in - row * kv_row;
+        if (idx >= kv_tile || row >= x.y - jt * kTile) continue;
+        const float4* src = P.parts + (((static_cast<size_t>(x.w + jt) * kTile + row) * 2 + which) * kMostParts * P.Hkv + (c >> sh)) * (kDP / 4) + (c & ((1 << sh) - 1)) * 2;
+        float4 a = __ldcg(src), b = __ldcg(src + 1);
+        for (int p = 1; p < parts; ++p) {
+            src += P.Hkv * (kDP / 4);
+            const float4 f = __ldcg(src), g = __ldcg(src + 1);
+            a.x += f.x; a.y += f.y; a.z += f.z; a.w += f.w;
+            b.x += g.x; b.y += g.y; b.z += g.z; b.w += g.w;
+        }
+        const float mul = which ? P.scale : 1.f;
+        (which ? P.dk : P.dv)[static_cast<size_t>(x.x + jt * kTile + row) * kv_row + c] =
+            make_uint4(pack2(a.x * mul, a.y * mul), pack2(a.z * mul, a.w * mul), pack2(b.x * mul, b.y * mul), pack2(b.z * mul, b.w * mul));
+    }
 }
 
 }  // namespace
@@ -990,6 +1070,7 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
     P.status = reinterpret_cast<int*>(base);
     P.sTq = L.sTq; P.sHq = L.sHq; P.sTkv = L.sTkv; P.sHkv = L.sHkv;
     P.T = c.T; P.Hq = c.Hq; P.Hkv = c.Hkv; P.group = c.Hq / c.Hkv; P.D = c.D; P.rows = w.rows; P.causal = c.causal;
+    P.may_split = packed_may_split(c);
     P.scale = c.sm_scale > 0.f ? c.sm_scale : 1.f / sqrtf(static_cast<float>(c.D));
     // -lse / scale has to be finite: in the exponents a scale counts as 2^-120 at least, against which any score below 2^90 is nothing.  dQ and dK get the scale as it is.
     const float least = fmaxf(P.scale, 7.5231638e-37f);
@@ -1033,17 +1114,20 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
         LaunchScope ls_(K_PACKED_PREP, stream);
         if (int st = check_cuda(launch_chained(packed_prep_kernel, dim3(static_cast<unsigned>(slices < places ? slices : places)), dim3(256), 0, stream, R), "packed attention: backward prep launch")) return st;
     }
-    CUtensorMap mq, mk, mv, mdo, macc;
+    CUtensorMap mq, mk, mv, mdo, macc, mparts{};
+    if (P.may_split) {
+        if (int st = packed_acc_map(&mparts, base + w.parts, w.rows, 2 * kMostParts * c.Hkv)) return st;
+    }
     if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
     if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
     if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
     if (int st = packed_tile_map(&mdo, d_o, c.D, c.Hq, c.T, HD, c.D)) return st;
     if (int st = packed_acc_map(&macc, base + w.dq_acc, w.rows, c.Hq)) return st;
-    const long long worst = tiles * c.Hkv;
+    const long long worst = tiles * c.Hkv * (P.may_split ? kMostParts : 1);
     const int grid = static_cast<int>(worst < sm_count() ? worst : sm_count());          // one CTA per SM (all of tensor memory)
     {
         LaunchScope ls_(K_PACKED_BWD, stream);
-        if (int st = check_cuda(launch_chained(attn_packed_bwd_kernel, dim3(grid), dim3(kManyThreads), kManySmemBytes, stream, mq, mk, mv, mdo, macc, P),
+        if (int st = check_cuda(launch_chained(attn_packed_bwd_kernel, dim3(grid), dim3(kManyThreads), kManySmemBytes, stream, mq, mk, mv, mdo, macc, mparts, P),
                                 "packed attention: backward launch")) return st;
     }
     if (int st = launch_short()) return st;
@@ -1052,7 +1136,9 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
     F.dq_acc = reinterpret_cast<const float4*>(base + w.dq_acc);
     F.dq = static_cast<uint4*>(dq);
     F.plan = P.plan;
-    F.Hq = c.Hq; F.D = c.D; F.scale = P.scale;
+    F.parts = reinterpret_cast<const float4*>(base + w.parts);
+    F.dv = reinterpret_cast<uint4*>(dv); F.dk = reinterpret_cast<uint4*>(dk);
+    F.Hq = c.Hq; F.Hkv = c.Hkv; F.group = P.group; F.D = c.D; F.causal = c.causal; F.may_split = P.may_split; F.main_grid = grid; F.scale = P.scale;
     LaunchScope ls_(K_PACKED_CONVERT, stream);
     return check_cuda(launch_chained(packed_convert_kernel, dim3(static_cast<unsigned>(slices < places ? slices : places)), dim3(256), 0, stream, F), "packed attention: backward convert launch");
 }

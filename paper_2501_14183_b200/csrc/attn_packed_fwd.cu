@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             if (n_items > gridDim.x) {
                 if (!waited) chain_wait();               // the counter is zero now
                 waited = true;
-                k = next_item(P.status + kWsTicketFwd, lane);
+                k = next_item(P.status + kWsTicketFwd, gridDim.x, lane);
             }
             publish(i + 1, k);
         }

@@ -45,16 +45,21 @@ __device__ __forceinline__ int block_scan(int v, int* s_warp) {      // exclusiv
 // Counting sort: tiles per amount of work, then each tile's place.  Sequences come a thread each, as many at a time as there are threads; their tiles are shared out over all threads again, so a
 // single long sequence takes no longer than many short ones.
 __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanParams P) {
-    __shared__ int s_warp[33], s_bin[kPlanBins + 1], s_bad;
+    __shared__ int s_warp[33], s_bin[kPlanBins + 1], s_bad, s_most;
+    __shared__ unsigned long long s_work;
     __shared__ int s_first[kPlanThreads + 1], s_start[kPlanThreads], s_len[kPlanThreads];
     chain_wait();
     chain_release();
     const int tid = threadIdx.x, nt = blockDim.x;
     const int bins = P.bins + 1;             // the last one: sequences of a single tile
     for (int b = tid; b < bins; b += nt) s_bin[b] = 0;
-    if (tid == 0) s_bad = 0;
+    if (tid == 0) {
+        s_bad = s_most = 0;
+        s_work = 0;
+    }
     __syncthreads();
-    int total = 0, many = 0, longer = 0;
+    int total = 0, many = 0, longer = 0, most = 0;
+    long long sum = 0;                       // (whole numbers: the split of the backward pass hangs on it, and has to be the same from run to run)
     for (int pass = 0; pass < 2; ++pass) {
         int ahead = 0;
         for (int s0 = 0; s0 < P.n_seqs; s0 += nt) {
@@ -90,6 +95,10 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
                 const int work = P.causal ? level + 1 : n, bin = n == 1 ? P.bins : P.bins - min(work, P.bins);      // bin 0: the most work
                 if (pass == 0) {
                     atomicAdd(&s_bin[bin], 1);
+                    if (n > 1) {
+                        most = max(most, work);
+                        sum += work;
+                    }
                 } else {
                     const int to = atomicAdd(&s_bin[bin], 1);
                     if (to < P.cap) reinterpret_cast<int4*>(P.plan + kWsHeaderBytes / 4)[to] = make_int4(s_start[lo], s_len[lo], level, ahead + s_first[lo]);
@@ -100,6 +109,12 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
         }
         if (s_bad) break;
         if (pass == 0) {
+            most = __reduce_max_sync(0xffffffffu, most);
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((tid & 31) == 0 && most > 0) {
+                atomicMax(&s_most, most);
+                atomicAdd(&s_work, static_cast<unsigned long long>(sum));
+            }
             total = ahead;
             int run = 0;
             for (int b0 = 0; b0 < bins; b0 += nt) {
@@ -124,6 +139,8 @@ __global__ void __launch_bounds__(kPlanThreads) packed_plan_kernel(const PlanPar
         P.plan[kPlanCausal] = P.causal;
         P.plan[kPlanMany] = bad ? 0 : many;
         P.plan[kPlanLong] = bad ? 0 : longer;
+        P.plan[kPlanMostWork] = bad ? 0 : s_most;
+        P.plan[kPlanWork] = bad ? 0 : __float_as_int(static_cast<float>(s_work));
     }
 }
 
