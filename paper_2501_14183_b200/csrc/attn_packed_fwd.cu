@@ -301,34 +301,50 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             if (rows) fence_proxy_async_smem();          // rows written by asynchronous copies are read by the tensor core
             tc_fence_after();
         };
+        // The scores of the next item's first step go out ahead of the last P V of this one, so that the softmax warps find them when they are done with this one.
+        bool primed = false;
+        Item it = item_at(0);
 #pragma unroll 1
-        for (uint32_t i = 0; ok; ++i) {
-            const Item it = item_at(i);
-            if (it.n_act < 0) break;
+        for (uint32_t i = 0; ok && it.n_act >= 0; ++i) {
             const uint32_t qb = n_done & 1;
             const int per_step = it.split ? 2 : 1;                       // ring stages of a step
+            Item next;
             if (w < it.n_act) {
                 const uint64_t a = umma_desc_advance(d_q, (qb * kFwdTiles + w) * kTileBytes);
                 const uint32_t mine = it.split ? w : 0;
-                wait_full(bar_q_full + qb, (n_done >> 1) & 1, false);
                 uint32_t sn = stage_n + mine;
-                wait_full(bar_kv_full + sn % kFwdStages, (sn / kFwdStages) & 1, it.len < kTile);
-                // The second tile starts a softmax later than the first: in step, both tiles' exponentials queue up and then both tiles'
-                // hand-offs leave the special-function unit idle (3400 cycles a step of 128 keys against 2600).  Not worth its delay for a few steps.
-                // (On a barrier of one phase: bar_p may have gone two phases on by the time this warp's first stage has landed, and its third waits for
-                // a stage of the ring that this warp has yet to release.)
-                if (i == 0 && w == 1 && it.n_kv >= 4) ok &= warp_wait_relaxed(bar_stagger, 0);
-                issue_scores(a, sn % kFwdStages, min(kTile, it.len));
-                if (it.n_kv == 1) tc_commit_w(bar_q_free + qb);
+                if (!primed) {
+                    wait_full(bar_q_full + qb, (n_done >> 1) & 1, false);
+                    wait_full(bar_kv_full + sn % kFwdStages, (sn / kFwdStages) & 1, it.len < kTile);
+                    // The second head starts a softmax later than the first: in step, both heads' exponentials queue up and then both heads'
+                    // hand-offs leave the special-function unit idle.  Not worth its delay for a few steps.  (On a barrier of one phase: bar_p may have gone two phases on
+                    // by the time this warp's first stage has landed, and its third waits for a stage of the ring that this warp has yet to release.)
+                    if (i == 0 && w == 1 && it.n_kv >= 4) ok &= warp_wait_relaxed(bar_stagger, 0);
+                    issue_scores(a, sn % kFwdStages, min(kTile, it.len));
+                    if (it.n_kv == 1) tc_commit_w(bar_q_free + qb);
+                }
+                primed = false;
 #pragma unroll 1
                 for (int j = 0; j < it.n_kv && ok; ++j, ++t) {
-                    if (j + 1 < it.n_kv) {               // the next S, as soon as the warpgroup holds this one
+                    if (j + 1 < it.n_kv) {               // the next S, as soon as the softmax warps hold this one
                         const uint32_t s1 = sn + per_step;
                         wait_full(bar_kv_full + s1 % kFwdStages, (s1 / kFwdStages) & 1, it.len < (j + 2) * kTile);
                         ok &= warp_wait_relaxed(bar_sfree + w, t & 1);
                         tc_fence_after();
                         issue_scores(a, s1 % kFwdStages, min(kTile, it.len - (j + 1) * kTile));
                         if (j + 2 == it.n_kv) tc_commit_w(bar_q_free + qb);
+                    } else {
+                        next = item_at(i + 1);
+                        if (w < next.n_act) {
+                            const uint32_t s1 = stage_n + it.n_kv * per_step + (next.split ? w : 0);
+                            wait_full(bar_q_full + (qb ^ 1), ((n_done + 1) >> 1) & 1, false);
+                            wait_full(bar_kv_full + s1 % kFwdStages, (s1 / kFwdStages) & 1, next.len < kTile);
+                            ok &= warp_wait_relaxed(bar_sfree + w, t & 1);
+                            tc_fence_after();
+                            issue_scores(umma_desc_advance(d_q, ((qb ^ 1) * kFwdTiles + w) * kTileBytes), s1 % kFwdStages, min(kTile, next.len));
+                            if (next.n_kv == 1) tc_commit_w(bar_q_free + (qb ^ 1));
+                            primed = true;
+                        }
                     }
                     ok &= warp_wait_relaxed(bar_p + w, t & 1);
                     if (t == 0 && w == 0 && lane == 0) mbar_arrive(bar_stagger);
@@ -355,9 +371,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     ok &= warp_wait_relaxed(bar_kv_full + so % kFwdStages, (so / kFwdStages) & 1);
                     tc_commit_w(bar_kv_free + so % kFwdStages);
                 }
+                next = item_at(i + 1);
             }
             stage_n += it.n_kv * per_step;
             ++n_done;
+            it = next;
         }
     }
     } else if (warp < 8) {
