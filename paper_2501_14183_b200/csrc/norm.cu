@@ -1,592 +1,33 @@
-// Norms before and after a block with its gate and residual scale: h = a x + g o N_post(y), u = N_pre(h), and their gradients.
+// Norms before and after a block: checks, launches, and the last step of the parameters' gradients (the other kernels: norm_kernels.cuh).
 //
-// norm_fwd_kernel        a group of threads per token, its row in registers.
-// norm_bwd_kernel        the same; sums over tokens stay in registers until a CTA is done with its rows.
-// norm_params_kernel     those sums of all CTAs, in a fixed order.
-//
-// With z = (t - mean) r, e = w o d for the gradient d of N(t):  dt = r (e - mean(e) - z mean(e o z)), without mean(e) for rms.
-// Bound: memory.  Forward x, y in, h, u out; backward x, y, dh, du in, dx, dy out (h again from x and y: read back as h it would come rounded, and the fp32 sums with it).
-#include <cuda_fp16.h>
-
-#include "common.cuh"
-#include "kernels.h"
+// norm_params_kernel     sums over tokens of all CTAs, in a fixed order.
+#include "norm.h"
 
 namespace vardrop {
 
 namespace {
-
-constexpr int kFwdPer = 16, kBwdPer = 8;  // elements of a row in a thread (backward the sums over tokens take as many registers again, or three times)
-constexpr int kFwdPerFew = 10, kBwdPerFew = 6;
-constexpr int kNormMaxC = 8192;
-
-struct NormParams {
-    const void *x, *y;
-    const float *gate, *w_post, *b_post, *w_pre, *b_pre;
-    const int32_t *sel_idx, *n_sel, *inv_idx;
-    void *h, *u;
-    float4* stats;
-    const void *d_h, *d_u;
-    void *dx, *dy;
-    float* partial;                      // [4][units or CTAs, C]: sums over tokens of t o zy, t, du o zh, du
-    int B, N, C, pre, post, gate_rows, S;
-    int splits, units;                   // CTAs that share an instance; B splits
-    int slots;                           // rows of the first two sums
-    float scale, eps, inv_c;
-};
-
-// ---- pairs: two fp32 values in a 64-bit register, for the packed instructions of sm_100 (one issue slot for two results, each rounded as the scalar instruction's) -------
-typedef uint64_t Pair;
-__device__ __forceinline__ Pair pair_of(float lo, float hi) {
-    Pair r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ Pair both(float v) { return pair_of(v, v); }
-__device__ __forceinline__ float2 halves(Pair v) {
-    float2 f;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
-    return f;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-    Pair d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-    Pair d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-    Pair d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ float sum_of(Pair v) { const float2 f = halves(v); return f.x + f.y; }
-
-// ---- elements -------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ Pair widen(uint32_t w, __nv_bfloat16) { return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ Pair widen(uint32_t w, __half) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    return pair_of(f.x, f.y);
-}
-__device__ __forceinline__ uint32_t narrow(Pair v, __nv_bfloat16) {
-    const float2 f = halves(v);
-    const __nv_bfloat162 r = __floats2bfloat162_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ __forceinline__ uint32_t narrow(Pair v, __half) {
-    const float2 f = halves(v);
-    const __half2 r = __floats2half2_rn(f.x, f.y);
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
-
-// A thread's columns: kPer / kV vectors of kV, a group's threads side by side; element e of the thread is element e % kV of vector e / kV, and pair p elements 2 p and 2 p + 1.
-template <class T, int kV, int kGroup, int kPer>
-struct Row {
-    static constexpr int kVecs = kPer / kV, kPairs = kPer / 2, kVecBytes = kV * static_cast<int>(sizeof(T));
-    typedef Pair Values[kPairs];
-    static __device__ __forceinline__ int col(int t, int j) { return (j * kGroup + t) * kV; }
-    static __device__ __forceinline__ bool whole(int C) { return C == kGroup * kPer; }
-    // words of the vectors (a 16-bit element alone takes a word too) to pairs, and back
-    static constexpr int kWords = kVecBytes < 4 ? 1 : kVecBytes / 4;
-    struct alignas(kVecBytes < 4 ? 4 : kVecBytes) Vec { uint32_t w[kWords]; };
-    static __device__ __forceinline__ Vec load(const T* p) {
-        Vec v;
-        if constexpr (kVecBytes < 4) v.w[0] = *reinterpret_cast<const unsigned short*>(p);
-        else v = *reinterpret_cast<const Vec*>(p);
-        return v;
-    }
-    static __device__ __forceinline__ void unpack(const Vec (&v)[kVecs], Values& to) {
-#pragma unroll
-        for (int p = 0; p < kPairs; ++p) {
-            if constexpr (sizeof(T) == 4) {
-                const int e = 2 * p;
-                to[p] = pair_of(__uint_as_float(v[e / kV].w[e % kV]), __uint_as_float(v[(e + 1) / kV].w[(e + 1) % kV]));
-            } else if constexpr (kV == 1) {
-                to[p] = widen(v[2 * p].w[0] | v[2 * p + 1].w[0] << 16, T{});
-            } else {
-                to[p] = widen(v[2 * p / kV].w[p % (kV / 2)], T{});
-            }
-        }
-    }
-    static __device__ __forceinline__ void store(T* row, int t, int C, const Values& v) {
-        Vec x[kVecs];
-#pragma unroll
-        for (int p = 0; p < kPairs; ++p) {
-            if constexpr (sizeof(T) == 4) {
-                const float2 f = halves(v[p]);
-                const int e = 2 * p;
-                x[e / kV].w[e % kV] = __float_as_uint(f.x);
-                x[(e + 1) / kV].w[(e + 1) % kV] = __float_as_uint(f.y);
-            } else if constexpr (kV == 1) {
-                const uint32_t w = narrow(v[p], T{});
-                x[2 * p].w[0] = w & 0xffffu;
-                x[2 * p + 1].w[0] = w >> 16;
-            } else {
-                x[2 * p / kV].w[p % (kV / 2)] = narrow(v[p], T{});
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-            if (col(t, j) >= C) continue;
-            if constexpr (kVecBytes < 4) *reinterpret_cast<unsigned short*>(row + col(t, j)) = static_cast<unsigned short>(x[j].w[0]);
-            else *reinterpret_cast<Vec*>(row + col(t, j)) = x[j];
-        }
-    }
-    // of a parameter; `none` where there is none, 0 behind the row's end
-    static __device__ __forceinline__ void param(const float* p, int t, int C, float none, Values& v) {
-        float f[kPer];
-#pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-            if (p && col(t, j) < C) {
-                if constexpr (kV % 4 == 0) {
-#pragma unroll
-                    for (int e = 0; e < kV; e += 4) {
-                        const float4 q = __ldg(reinterpret_cast<const float4*>(p + col(t, j) + e));
-                        f[j * kV + e] = q.x; f[j * kV + e + 1] = q.y; f[j * kV + e + 2] = q.z; f[j * kV + e + 3] = q.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < kV; ++e) f[j * kV + e] = __ldg(p + col(t, j) + e);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < kV; ++e) f[j * kV + e] = col(t, j) < C ? none : 0.f;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
-    }
-    static __device__ __forceinline__ void param_store(float* to, int t, int C, const Values& v) {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-            const float2 f = halves(v[i]);
-            const int c0 = col(t, 2 * i / kV) + 2 * i % kV, c1 = col(t, (2 * i + 1) / kV) + (2 * i + 1) % kV;
-            if (c0 < C) to[c0] = f.x;
-            if (c1 < C) to[c1] = f.y;
-        }
-    }
-    // zeros again behind the row's end
-    static __device__ __forceinline__ void clear_rest(int t, int C, Values& v) {
-        if (whole(C)) return;
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-            const float2 f = halves(v[i]);
-            v[i] = pair_of(col(t, 2 * i / kV) < C ? f.x : 0.f, col(t, (2 * i + 1) / kV) < C ? f.y : 0.f);
-        }
-    }
-};
-
-// ---- sums over a group ------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-// Barrier of group `id` (of at most four).  A number that is only known at run time reserves all sixteen barriers, and an SM then holds four CTAs.
-template <int kGroup>
-__device__ __forceinline__ void group_barrier(int id) {
-    if (id == 0) asm volatile("bar.sync 1, %0;" ::"n"(kGroup) : "memory");
-    else if (id == 1) asm volatile("bar.sync 2, %0;" ::"n"(kGroup) : "memory");
-    else if (id == 2) asm volatile("bar.sync 3, %0;" ::"n"(kGroup) : "memory");
-    else asm volatile("bar.sync 4, %0;" ::"n"(kGroup) : "memory");
-}
-// One sum, or two at once, to every thread of the group.  Groups of several warps go through shared memory, in two places by turns, so that one barrier a sum is enough.
-template <int kGroup>
-struct GroupSum {
-    float2* place;                       // [2][kGroup / 32] of this group
-    int turn = 0, id;
-    template <bool kTwo>
-    __device__ __forceinline__ float2 of(float a, float b) {
-        a = warp_sum(a);
-        if (kTwo) b = warp_sum(b);
-        if (kGroup == 32) return make_float2(a, b);
-        constexpr int kWarps = kGroup / 32;
-        const int lane = threadIdx.x & 31, warp = (threadIdx.x % kGroup) >> 5;
-        float2* at = place + turn * kWarps;
-        turn ^= 1;
-        if (lane == 0) at[warp] = make_float2(a, b);
-        group_barrier<kGroup>(id);
-        float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float2 f = at[w];
-            s.x += f.x;
-            if (kTwo) s.y += f.y;
-        }
-        return s;
-    }
-};
-
-template <int kGroup>
-constexpr int kNormThreads = kGroup < 256 ? 256 : kGroup;        // of a CTA
-
-// Rows on their way from memory: a ring in shared memory whose places belong to one thread each, filled by asynchronous copies of the thread's own columns, so
-// that a group has kStages - 1 rows in flight while it works on one, without registers for them and without barriers.  (Loads into registers behind the row before: 65536 x
-// 1024 bf16 forward 188 us, backward 367; like this 118 and 166, bound by the instructions of scalar arithmetic.)  Columns of two bytes, which those copies cannot take, are
-// loaded when they are needed.
-template <class T, int kV, int kGroup, int kPer, int kTensors>
-struct Ring {
-    using R = Row<T, kV, kGroup, kPer>;
-    using Vec = typename R::Vec;
-    static constexpr bool kAsync = R::kVecBytes >= 4;
-    static constexpr int kThreads = kNormThreads<kGroup>;
-    static constexpr int kStageBytes = kThreads * kPer * static_cast<int>(sizeof(T)) * kTensors;
-    static constexpr int kFit = 200 * 1024 / kStageBytes;
-    static constexpr int kStages = kFit < 1 ? 1 : kFit > 3 ? 3 : kFit;
-    static constexpr int kBytes = kAsync ? kStages * kStageBytes : 0;
-    Vec* mine;                           // this thread's first place
-    __device__ __forceinline__ Vec* at(int stage, int k, int j) const { return mine + ((stage * kTensors + k) * R::kVecs + j) * kThreads; }
-    // tensor k of a row (NULL: none) to a stage; commit() behind the last one
-    __device__ __forceinline__ void fetch(int stage, int k, const T* row, int t, int C) {
-        if constexpr (kAsync) {
-            if (!row) return;
-#pragma unroll
-            for (int j = 0; j < R::kVecs; ++j) {
-                if (R::col(t, j) >= C) continue;
-                const uint32_t to = smem_u32(at(stage, k, j));
-                if (R::kVecBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + R::col(t, j)) : "memory");
-                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(row + R::col(t, j)), "n"(R::kVecBytes) : "memory");
-            }
-        }
-    }
-    __device__ __forceinline__ void commit() {
-        if (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    __device__ __forceinline__ void wait() {             // the oldest stage in flight has landed
-        if (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-    }
-    // a row's columns, zeros behind its end
-    __device__ __forceinline__ void read(int stage, int k, const T* row, int t, int C, typename R::Values& to) const {
-        Vec v[R::kVecs];
-#pragma unroll
-        for (int j = 0; j < R::kVecs; ++j) {
-            if (R::col(t, j) < C) {
-                if constexpr (kAsync) v[j] = *at(stage, k, j);
-                else v[j] = R::load(row + R::col(t, j));
-            } else {
-#pragma unroll
-                for (int w = 0; w < R::kWords; ++w) v[j].w[w] = 0u;
-            }
-        }
-        R::unpack(v, to);
-    }
-};
-
-// t without its mean (kind 2), and the (mean, r) of its norm
-template <class R, int kGroup, bool kLayer>
-__device__ __forceinline__ float2 centre(typename R::Values& t, int kind, int thread, const NormParams& P, GroupSum<kGroup>& sum) {
-    float mean = 0.f;
-    if (kLayer && kind == 2) {
-        Pair s = t[0];
-#pragma unroll
-        for (int p = 1; p < R::kPairs; ++p) s = add2(s, t[p]);
-        mean = sum.template of<false>(sum_of(s), 0.f).x * P.inv_c;
-        const Pair minus = both(-mean);
-#pragma unroll
-        for (int p = 0; p < R::kPairs; ++p) t[p] = add2(t[p], minus);
-        R::clear_rest(thread, P.C, t);
-    }
-    Pair q[2] = {both(0.f), both(0.f)};
-#pragma unroll
-    for (int p = 0; p < R::kPairs; ++p) q[p & 1] = fma2(t[p], t[p], q[p & 1]);
-    return make_float2(mean, rsqrtf(sum.template of<false>(sum_of(add2(q[0], q[1])), 0.f).x * P.inv_c + P.eps));
-}
-
-// The rows of a unit that a group works on: first, first + step, ...; the source row of a selection is known one row ahead of its copies.
-struct RowWalk {
-    const int32_t* sel;
-    int n, step;
-    __device__ __forceinline__ int source(int i) const { return sel ? (i < n ? __ldg(sel + i) : 0) : i; }
-};
-
-// ---- forward ----------------------------------------------------------------------------------------------------------------
-// kLayer: a mean or a bias somewhere.
-template <class T, int kV, int kGroup, int kPer, bool kLayer>
-__global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGroup>) norm_fwd_kernel(const NormParams P) {
-    using Rows = Ring<T, kV, kGroup, kPer, 2>;
-    using R = typename Rows::R;
-    constexpr int kGroups = kNormThreads<kGroup> / kGroup, kAhead = Rows::kStages - 1;
-    extern __shared__ __align__(16) unsigned char smem_dyn[];
-    __shared__ float2 s_sum[kGroups][2 * (kGroup / 32)];
-    const int group = threadIdx.x / kGroup, t = threadIdx.x % kGroup;
-    GroupSum<kGroup> sum{s_sum[group], 0, group};
-    Rows ring{reinterpret_cast<typename Rows::Vec*>(smem_dyn) + threadIdx.x};
-    chain_wait();
-    chain_release();
-    const T* const X = static_cast<const T*>(P.x);
-    const T* const Y = static_cast<const T*>(P.y);
-    typename R::Values w_pre, b_pre;                     // of this thread's columns, for all rows
-    R::param(P.w_pre, t, P.C, 1.f, w_pre);
-    if (kLayer) R::param(P.b_pre, t, P.C, 0.f, b_pre);
-    const Pair scale = both(P.scale);
-#pragma unroll 1
-    for (int unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
-        const int b = unit / P.splits, srow = P.S > 1 ? b : 0;
-        const RowWalk walk{P.sel_idx ? P.sel_idx + static_cast<size_t>(srow) * P.N : nullptr, P.n_sel ? P.n_sel[srow] : P.N, P.splits * kGroups};
-        const size_t base = static_cast<size_t>(b) * P.N;
-        // N_post's scale and bias with the gate in them: h = a x + w z + c
-        typename R::Values w, c;
-        {
-            typename R::Values g;
-            R::param(P.gate ? P.gate + static_cast<size_t>(P.gate_rows > 1 ? b : 0) * P.C : nullptr, t, P.C, 1.f, g);
-            R::param(P.w_post, t, P.C, 1.f, w);
-            if (kLayer) R::param(P.b_post, t, P.C, 0.f, c);
-#pragma unroll
-            for (int p = 0; p < R::kPairs; ++p) {
-                w[p] = mul2(w[p], g[p]);
-                if (kLayer) c[p] = mul2(c[p], g[p]);
-            }
-        }
-        int i = (unit - b * P.splits) * kGroups + group, stage = 0, ahead = i;
-        int source = walk.source(ahead);
-        auto fetch = [&](int to) {
-            if (ahead < walk.n) {
-                ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
-                ring.fetch(to, 1, Y ? Y + (base + ahead) * P.C : nullptr, t, P.C);
-            }
-            ring.commit();
-            ahead += walk.step;
-            source = walk.source(ahead);
-        };
-#pragma unroll
-        for (int s = 0; s < kAhead; ++s) fetch(s);
-#pragma unroll 1
-        for (; i < walk.n; i += walk.step) {
-            const int from = Rows::kAsync ? 0 : walk.source(i);
-            fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
-            ring.wait();
-            const size_t row = (base + i) * P.C;
-            float2 post = make_float2(0.f, 1.f), pre = post;
-            typename R::Values h;
-            ring.read(stage, 0, X + (base + from) * P.C, t, P.C, h);
-#pragma unroll
-            for (int p = 0; p < R::kPairs; ++p) h[p] = mul2(h[p], scale);
-            if (Y) {
-                typename R::Values y;
-                ring.read(stage, 1, Y + row, t, P.C, y);
-                if (P.post) post = centre<R, kGroup, kLayer>(y, P.post, t, P, sum);
-                const Pair r = both(post.y);
-#pragma unroll
-                for (int p = 0; p < R::kPairs; ++p) {
-                    if (kLayer) h[p] = add2(h[p], c[p]);
-                    h[p] = fma2(mul2(y[p], r), w[p], h[p]);
-                }
-            }
-            if (P.h) R::store(static_cast<T*>(P.h) + row, t, P.C, h);
-            if (P.pre) {
-                pre = centre<R, kGroup, kLayer>(h, P.pre, t, P, sum);
-                const Pair r = both(pre.y);
-#pragma unroll
-                for (int p = 0; p < R::kPairs; ++p) h[p] = kLayer ? fma2(mul2(h[p], r), w_pre[p], b_pre[p]) : mul2(mul2(h[p], r), w_pre[p]);
-                R::store(static_cast<T*>(P.u) + row, t, P.C, h);
-            }
-            if (P.stats && t == 0) P.stats[base + i] = make_float4(post.x, post.y, pre.x, pre.y);
-            if (++stage == Rows::kStages) stage = 0;
-        }
-    }
-}
-
-// ---- backward ---------------------------------------------------------------------------------------------------------------
-// Sums over tokens: with t the gradient of h, zy and zh the normed y and h:
-//   d_gate = w_post o A + b_post o T,  d_w_post = sum_b g_b o A_b,  d_b_post = sum_b g_b o T_b   with A = sum t o zy, T = sum t over the tokens of an instance,
-//   d_w_pre = sum du o zh,  d_b_pre = sum du
-// so a thread keeps four sums a column however many parameters there are, without a mean or a bias (kLayer) two.  (A gate that all instances share needs them over all
-// tokens only.)
-template <class T, int kV, int kGroup, int kPer, bool kLayer>
-__global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGroup> > 0 ? 512 / kNormThreads<kGroup> : 1) norm_bwd_kernel(const NormParams P) {
-    using Rows = Ring<T, kV, kGroup, kPer, 4>;
-    using R = typename Rows::R;
-    constexpr int kGroups = kNormThreads<kGroup> / kGroup, kAhead = Rows::kStages - 1, kPairs = R::kPairs;
-    extern __shared__ __align__(16) unsigned char smem_dyn[];
-    __shared__ float2 s_sum[kGroups][2 * (kGroup / 32)];
-    __shared__ Pair s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kGroup * kPairs : 1];
-    const int group = threadIdx.x / kGroup, t = threadIdx.x % kGroup;
-    GroupSum<kGroup> sum{s_sum[group], 0, group};
-    Rows ring{reinterpret_cast<typename Rows::Vec*>(smem_dyn) + threadIdx.x};
-    chain_wait();
-    chain_release();
-    const T* const X = static_cast<const T*>(P.x);
-    const T* const Y = static_cast<const T*>(P.y);
-    const T* const dH = static_cast<const T*>(P.d_h);
-    const T* const dU = static_cast<const T*>(P.d_u);
-    typename R::Values w_pre;                            // of this thread's columns, for all rows
-    R::param(P.w_pre, t, P.C, 1.f, w_pre);
-    typename R::Values acc[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int p = 0; p < kPairs; ++p) acc[k][p] = both(0.f);
-    const Pair scale = both(P.scale);
-    // sums k0 and k0 + 1 of all groups to row `at` of their partial sums
-    auto flush = [&](int k0, int at) {
-#pragma unroll
-        for (int k = 0; k < (kLayer ? 2 : 1); ++k) {
-            typename R::Values& a = acc[k0 + k];
-            if (kGroups > 1) {
-                __syncthreads();
-#pragma unroll
-                for (int p = 0; p < kPairs; ++p) s_cols[group][p * kGroup + t] = a[p];
-                __syncthreads();
-                if (group == 0) {
-#pragma unroll 1
-                    for (int g = 1; g < kGroups; ++g)
-#pragma unroll
-                        for (int p = 0; p < kPairs; ++p) a[p] = add2(a[p], s_cols[g][p * kGroup + t]);
-                }
-            }
-            if (group == 0) R::param_store(P.partial + (static_cast<size_t>(k0 == 0 ? k * P.slots : 2 * P.slots + k * gridDim.x) + at) * P.C, t, P.C, a);
-#pragma unroll
-            for (int p = 0; p < kPairs; ++p) a[p] = both(0.f);
-        }
-    };
-#pragma unroll 1
-    for (int unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
-        const int b = unit / P.splits, srow = P.S > 1 ? b : 0;
-        const RowWalk walk{P.sel_idx ? P.sel_idx + static_cast<size_t>(srow) * P.N : nullptr, P.n_sel ? P.n_sel[srow] : P.N, P.splits * kGroups};
-        const size_t base = static_cast<size_t>(b) * P.N;
-        const int first = (unit - b * P.splits) * kGroups + group;
-        typename R::Values w, c;                         // N_post's scale and bias with the gate in them
-        {
-            typename R::Values g;
-            R::param(P.gate ? P.gate + static_cast<size_t>(P.gate_rows > 1 ? b : 0) * P.C : nullptr, t, P.C, 1.f, g);
-            R::param(P.w_post, t, P.C, 1.f, w);
-            if (kLayer) R::param(P.b_post, t, P.C, 0.f, c);
-#pragma unroll
-            for (int p = 0; p < kPairs; ++p) {
-                w[p] = mul2(w[p], g[p]);
-                if (kLayer) c[p] = mul2(c[p], g[p]);
-            }
-        }
-        int ahead = first, stage = 0, source = walk.source(first), from = source;
-        float4 st = first < walk.n ? __ldg(P.stats + base + first) : make_float4(0.f, 0.f, 0.f, 0.f);
-        auto fetch = [&](int to) {
-            if (ahead < walk.n) {
-                const size_t row = (base + ahead) * P.C;
-                ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
-                ring.fetch(to, 1, Y ? Y + row : nullptr, t, P.C);
-                ring.fetch(to, 2, dH ? dH + row : nullptr, t, P.C);
-                ring.fetch(to, 3, dU ? dU + row : nullptr, t, P.C);
-            }
-            ring.commit();
-            ahead += walk.step;
-            source = walk.source(ahead);
-        };
-#pragma unroll
-        for (int s = 0; s < kAhead; ++s) fetch(s);
-        if (walk.sel) {                                  // rows of dropped tokens, while the first ones come in
-            typename R::Values zero;
-#pragma unroll
-            for (int p = 0; p < kPairs; ++p) zero[p] = both(0.f);
-            // (a look at one token at a time is a chain of loads: a warp looks at 32)
-            const int lane = threadIdx.x & 31;
-#pragma unroll 1
-            for (int i0 = first; i0 < P.N; i0 += 32 * walk.step) {
-                const long long mine = i0 + static_cast<long long>(lane) * walk.step;
-                unsigned dropped = __ballot_sync(0xffffffffu, mine < P.N && __ldg(P.inv_idx + static_cast<size_t>(srow) * P.N + (mine < P.N ? mine : 0)) < 0);
-#pragma unroll 1
-                for (; dropped; dropped &= dropped - 1)
-                    R::store(static_cast<T*>(P.dx) + (base + i0 + static_cast<size_t>(__ffs(dropped) - 1) * walk.step) * P.C, t, P.C, zero);
-            }
-        }
-#pragma unroll 1
-        for (int i = first; i < walk.n; i += walk.step) {
-            fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
-            // of the next row, ahead of the wait
-            const int from_next = walk.source(i + walk.step);
-            const float4 st_next = i + walk.step < walk.n ? __ldg(P.stats + base + i + walk.step) : st;
-            ring.wait();
-            const size_t row = (base + i) * P.C;
-            typename R::Values h, zy, d;
-            ring.read(stage, 0, X + (base + from) * P.C, t, P.C, h);
-#pragma unroll
-            for (int p = 0; p < kPairs; ++p) h[p] = mul2(h[p], scale);
-            if (Y) {
-                ring.read(stage, 1, Y + row, t, P.C, zy);
-                const Pair r = both(st.y), minus = both(-st.x);
-#pragma unroll
-                for (int p = 0; p < kPairs; ++p) {
-                    if (kLayer) zy[p] = add2(zy[p], minus);
-                    zy[p] = mul2(zy[p], r);
-                    if (kLayer) h[p] = add2(h[p], c[p]);
-                    h[p] = fma2(zy[p], w[p], h[p]);
-                }
-            }
-            if (dH) {
-                ring.read(stage, 2, dH + row, t, P.C, d);
-            } else {
-#pragma unroll
-                for (int p = 0; p < kPairs; ++p) d[p] = both(0.f);
-            }
-            if (P.pre) {
-                typename R::Values du;
-                ring.read(stage, 3, dU + row, t, P.C, du);
-                Pair s0 = both(0.f), s1 = both(0.f);
-                const Pair r = both(st.w), minus = both(-st.z);
-#pragma unroll
-                for (int p = 0; p < kPairs; ++p) {
-                    if (kLayer) h[p] = add2(h[p], minus);
-                    h[p] = mul2(h[p], r);                // (where no column is, du is 0)
-                    acc[2][p] = fma2(du[p], h[p], acc[2][p]);
-                    if (kLayer) acc[3][p] = add2(acc[3][p], du[p]);
-                    du[p] = mul2(du[p], w_pre[p]);
-                    s0 = fma2(du[p], h[p], s0);
-                    if (kLayer) s1 = add2(s1, du[p]);
-                }
-                const float2 s = sum.template of<kLayer>(sum_of(s0), kLayer ? sum_of(s1) : 0.f);
-                const Pair m0 = both(-s.x * P.inv_c), m1 = both(kLayer && P.pre == 2 ? -s.y * P.inv_c : 0.f);
-#pragma unroll
-                for (int p = 0; p < kPairs; ++p) {
-                    if (kLayer) du[p] = add2(du[p], m1);
-                    d[p] = fma2(r, fma2(h[p], m0, du[p]), d[p]);
-                }
-            }
-            typename R::Values out;
-#pragma unroll
-            for (int p = 0; p < kPairs; ++p) out[p] = mul2(scale, d[p]);
-            R::store(static_cast<T*>(P.dx) + (base + from) * P.C, t, P.C, out);
-            if (Y) {
-                Pair s0 = both(0.f), s1 = both(0.f);
-#pragma unroll
-                for (int p = 0; p < kPairs; ++p) {
-                    acc[0][p] = fma2(d[p], zy[p], acc[0][p]);
-                    if (kLayer) acc[1][p] = add2(acc[1][p], d[p]);
-                    d[p] = mul2(d[p], w[p]);             // (0 where no column is)
-                }
-                if (P.post) {
-#pragma unroll
-                    for (int p = 0; p < kPairs; ++p) {
-                        s0 = fma2(d[p], zy[p], s0);
-                        if (kLayer) s1 = add2(s1, d[p]);
-                    }
-                    const float2 s = sum.template of<kLayer>(sum_of(s0), kLayer ? sum_of(s1) : 0.f);
-                    const Pair m0 = both(-s.x * P.inv_c), m1 = both(kLayer && P.post == 2 ? -s.y * P.inv_c : 0.f), r = both(st.y);
-#pragma unroll
-                    for (int p = 0; p < kPairs; ++p) {
-                        if (kLayer) d[p] = add2(d[p], m1);
-                        d[p] = mul2(r, fma2(zy[p], m0, d[p]));
-                    }
-                }
-                R::store(static_cast<T*>(P.dy) + row, t, P.C, d);
-            }
-            from = from_next;
-            st = st_next;
-            if (++stage == Rows::kStages) stage = 0;
-        }
-        if (P.gate_rows > 1) flush(0, unit);
-    }
-    if (P.gate_rows <= 1) flush(0, blockIdx.x);
-    flush(2, blockIdx.x);
-}
 
 // ---- parameters' gradients ----------------------------------------------------------------------------------------------------
 struct ParamsParams {
     const float* partial;
     const float *gate, *w_post, *b_post;
     float *d_gate, *d_w_post, *d_b_post, *d_w_pre, *d_b_pre;
-    int B, C, gate_rows, splits, slots, ctas, layer;
+    const int32_t* begin;
+    int B, C, gate_rows, slots, ctas, layer, splits;       // splits: CTAs of an instance, 0 where runs go over instances
 };
+// CTA that has token r of K, where `ctas` share them
+__device__ __forceinline__ int cta_of(long long r, long long K, int ctas) { return static_cast<int>(((r + 1) * ctas - 1) / K); }
+// Places of an instance's sums: from `first` to `last`, none where the second is smaller.
+struct Places {
+    int first, last;
+};
+__device__ __forceinline__ Places places_of(const ParamsParams& P, int b) {
+    if (P.splits) return Places{b * P.splits, (b + 1) * P.splits - 1};
+    const long long lo = P.begin[b], hi = P.begin[b + 1], K = P.begin[P.B];
+    if (lo >= hi) return Places{0, -1};
+    const int ctas = static_cast<int>(min(K, static_cast<long long>(P.ctas)));
+    return Places{cta_of(lo, K, ctas) + b, cta_of(hi - 1, K, ctas) + b};
+}
 constexpr int kColsX = 32, kColsY = 32;
 // Blocks (x, 0): 32 columns of the first two sums over all tokens; (x, 1): of the last two; (x, 2 + k): of the gates of instances 32 k to 32 k + 31.  32 rows at a time,
 // then across them, in a fixed order.
@@ -601,11 +42,12 @@ __global__ void __launch_bounds__(kColsX * kColsY) norm_params_kernel(const Para
         const int b = (blockIdx.y - 2) * kColsY + y;
         if (!there || b >= P.gate_rows) return;
         const float w = P.w_post ? __ldg(P.w_post + c) : 1.f, bias = P.b_post ? __ldg(P.b_post + c) : 0.f;
-        const float* A = P.partial + static_cast<size_t>(b) * P.splits * C + c;
+        const float* A = P.partial + c;
         const float* T = A + P.slots * C;
+        const Places at = places_of(P, b);
         float a = 0.f, t = 0.f;
 #pragma unroll 4
-        for (int r = 0; r < P.splits; ++r) {
+        for (int r = at.first; r <= at.last; ++r) {
             a += A[r * C];
             if (P.layer) t += T[r * C];
         }
@@ -617,12 +59,22 @@ __global__ void __launch_bounds__(kColsX * kColsY) norm_params_kernel(const Para
     const float* A = P.partial + (last ? 2 * P.slots * C : 0) + c;
     const float* T = A + rows * C;
     float v0 = 0.f, v1 = 0.f;
-    if (there) {
+    if (there && !last && per) {            // by instances, times their gates; a few of them are shared by lanes
+        const int subs = P.B < kColsY ? kColsY / P.B : 1, sub = y % subs;
+        for (int b = y / subs; b < P.B; b += kColsY / subs) {
+            const Places at = places_of(P, b);
+            const float g = __ldg(P.gate + static_cast<size_t>(b) * C + c);
+#pragma unroll 4
+            for (int r = at.first + sub; r <= at.last; r += subs) {
+                v0 += g * A[r * C];
+                if (P.layer) v1 += g * T[r * C];
+            }
+        }
+    } else if (there) {
 #pragma unroll 8
         for (int r = y; r < rows; r += kColsY) {
-            const float g = !last && per ? __ldg(P.gate + static_cast<size_t>(r / P.splits) * C + c) : 1.f;
-            v0 += g * A[r * C];
-            if (P.layer) v1 += g * T[r * C];
+            v0 += A[r * C];
+            if (P.layer) v1 += T[r * C];
         }
     }
     s[0][y][x] = v0;
@@ -649,109 +101,30 @@ __global__ void __launch_bounds__(kColsX * kColsY) norm_params_kernel(const Para
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
-int group_of(int C, int per) {
-    int g = 32;
-    while (g * per < C) g *= 2;
-    return g;
-}
-// CTAs that share an instance's tokens, as many as keep every SM's places taken without a second round, but none without a token.
-void shares(const vardrop_norm_cfg& c, int per, int per_sm, int& splits, int& grid) {
+// CTAs: as many as keep every SM's places taken without a second round, but none without a token.
+struct Shares {
+    NormShare share;
+    int splits, grid;
+};
+Shares shares(const vardrop_norm_cfg& c, bool selected, int per, int per_sm) {
     const int group = group_of(c.C, per), threads = group < 256 ? 256 : group, groups = threads / group;
-    const int places = sm_count() * per_sm * 256 / threads;
-    const int most = (c.N + groups - 1) / groups;
-    splits = places / c.B;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    const long long units = static_cast<long long>(c.B) * splits;
-    grid = static_cast<int>(units < places ? units : places);
-    if (grid < 1) grid = 1;
+    const long long places = static_cast<long long>(sm_count()) * per_sm * 256 / threads, all = static_cast<long long>(c.B) * c.N;
+    auto at_most = [&](long long n) { return static_cast<int>(n < places ? (n > 0 ? n : 1) : places > 0 ? places : 1); };
+    if (!selected && c.gate_rows <= 1) return Shares{kFlat, 0, at_most((all + groups - 1) / groups)};
+    if (selected && c.S > 1) return Shares{kRuns, 0, at_most((all + groups - 1) / groups)};
+    const long long most = (c.N + groups - 1) / groups, even = places / c.B;
+    const int splits = static_cast<int>(even < 1 ? 1 : even < most ? even : most);
+    return Shares{kSplit, splits, at_most(static_cast<long long>(c.B) * splits)};
 }
 constexpr int kFwdPerSm = 2, kBwdPerSm = 2;              // CTAs of 256 threads that an SM holds
 
-// Allows a kernel its dynamic shared memory where that is above what every kernel may take.
-template <class K>
-cudaError_t allow_smem(K kernel, int bytes, int& attr_dev) {
-    if (bytes <= 40 * 1024) return cudaSuccess;
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess || attr_dev == dev) return err;
-    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (err == cudaSuccess) attr_dev = dev;
-    return err;
-}
-template <class T, int kV, int kGroup, int kPer, bool kLayer>
-cudaError_t launch_fwd(int grid, const NormParams& P, cudaStream_t s) {
-    constexpr int kBytes = Ring<T, kV, kGroup, kPer, 2>::kBytes;
-    static thread_local int attr_dev = -1;
-    if (cudaError_t err = allow_smem(norm_fwd_kernel<T, kV, kGroup, kPer, kLayer>, kBytes, attr_dev)) return err;
-    return launch_chained(norm_fwd_kernel<T, kV, kGroup, kPer, kLayer>, dim3(grid), dim3(kNormThreads<kGroup>), kBytes, s, P);
-}
-template <class T, int kV, int kGroup, int kPer, bool kLayer>
-cudaError_t launch_bwd(int grid, const NormParams& P, cudaStream_t s) {
-    constexpr int kBytes = Ring<T, kV, kGroup, kPer, 4>::kBytes;
-    static thread_local int attr_dev = -1;
-    if (cudaError_t err = allow_smem(norm_bwd_kernel<T, kV, kGroup, kPer, kLayer>, kBytes, attr_dev)) return err;
-    return launch_chained(norm_bwd_kernel<T, kV, kGroup, kPer, kLayer>, dim3(grid), dim3(kNormThreads<kGroup>), kBytes, s, P);
-}
-// Rows that are not taken in 16-byte vectors are bound by instructions, and a group of a power of two has up to twice the columns that a row has: where fewer elements a
-// thread do, it gets fewer (5136 rows of 515 fp32, forward and backward: 43.4 us with 16 and 8, 35.0 with 10 and 6).
-template <class T, int kV, int kGroup, bool kLayer>
-cudaError_t launch(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
-    constexpr bool kWide = kV * sizeof(T) == 16;
-    if (bwd) {
-        if constexpr (!kWide) {
-            if (P.C <= kGroup * kBwdPerFew) return launch_bwd<T, kV, kGroup, kBwdPerFew, kLayer>(grid, P, s);
-        }
-        return launch_bwd<T, kV, kGroup, kBwdPer, kLayer>(grid, P, s);
-    }
-    if constexpr (kGroup * kFwdPer <= kNormMaxC) {
-        if constexpr (!kWide) {
-            if (P.C <= kGroup * kFwdPerFew) return launch_fwd<T, kV, kGroup, kFwdPerFew, kLayer>(grid, P, s);
-        }
-        return launch_fwd<T, kV, kGroup, kFwdPer, kLayer>(grid, P, s);
-    }
-    return cudaErrorInvalidValue;
-}
-template <class T, int kV, bool kLayer>
-cudaError_t launch_group(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
-    switch (group_of(P.C, bwd ? kBwdPer : kFwdPer)) {
-        case 32: return launch<T, kV, 32, kLayer>(bwd, grid, P, s);
-        case 64: return launch<T, kV, 64, kLayer>(bwd, grid, P, s);
-        case 128: return launch<T, kV, 128, kLayer>(bwd, grid, P, s);
-        case 256: return launch<T, kV, 256, kLayer>(bwd, grid, P, s);
-        case 512: return launch<T, kV, 512, kLayer>(bwd, grid, P, s);
-        default: return launch<T, kV, 1024, kLayer>(bwd, grid, P, s);
-    }
-}
-template <class T, int kV>
-cudaError_t launch_layer(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
-    return P.pre == 2 || P.post == 2 ? launch_group<T, kV, true>(bwd, grid, P, s) : launch_group<T, kV, false>(bwd, grid, P, s);
-}
-// Vectors as wide as the beginnings of all rows allow: 16 bytes, 4 bytes, a 16-bit element.
-template <class T>
-cudaError_t launch_16bit(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
-    return P.C % 8 == 0 ? launch_layer<T, 8>(bwd, grid, P, s) : P.C % 2 == 0 ? launch_layer<T, 2>(bwd, grid, P, s) : launch_layer<T, 1>(bwd, grid, P, s);
-}
 cudaError_t launch_type(bool bwd, int dtype, int grid, const NormParams& P, cudaStream_t s) {
-    if (dtype == 0) return launch_16bit<__nv_bfloat16>(bwd, grid, P, s);
-    if (dtype == 1) return launch_16bit<__half>(bwd, grid, P, s);
-    return P.C % 4 == 0 ? launch_layer<float, 4>(bwd, grid, P, s) : launch_layer<float, 1>(bwd, grid, P, s);
+    return dtype == 0 ? norm_launch_bf16(bwd, grid, P, s) : dtype == 1 ? norm_launch_fp16(bwd, grid, P, s) : norm_launch_fp32(bwd, grid, P, s);
 }
-// Where neither a gate nor a selection tells instances apart, all tokens are one's: no CTA is left without a share of an instance.
-vardrop_norm_cfg flat(const vardrop_norm_cfg& c, bool selected) {
-    vardrop_norm_cfg f = c;
-    if (!selected && c.gate_rows <= 1) {
-        f.N = c.B * c.N;
-        f.B = 1;
-        f.S = 0;
-    }
-    return f;
-}
-NormParams params_of(const vardrop_norm_cfg& c, const int32_t* sel_idx, int splits) {
+NormParams params_of(const vardrop_norm_cfg& c, const int32_t* sel_idx) {
     NormParams P{};
     P.B = c.B; P.N = c.N; P.C = c.C; P.pre = c.pre; P.post = c.post; P.gate_rows = c.gate_rows;
     P.S = sel_idx && c.S > 1 ? c.S : 1;
-    P.splits = splits; P.units = c.B * splits;
     P.scale = c.res_scale; P.eps = c.eps; P.inv_c = 1.f / static_cast<float>(c.C);
     return P;
 }
@@ -772,11 +145,11 @@ int norm_validate(const vardrop_norm_cfg& c) {
 }
 
 int norm_fwd_launch(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const float* b_pre, const int32_t* sel_idx,
-                    const int32_t* n_sel, const vardrop_norm_cfg& cfg, void* h, void* u, float* stats, cudaStream_t stream) {
-    const vardrop_norm_cfg c = flat(cfg, sel_idx != nullptr);
-    int splits, grid;
-    shares(c, kFwdPer, kFwdPerSm, splits, grid);
-    NormParams P = params_of(c, sel_idx, splits);
+                    const int32_t* n_sel, const vardrop_norm_cfg& c, void* h, void* u, float* stats, cudaStream_t stream) {
+    const Shares w = shares(c, sel_idx != nullptr, kFwdPer, kFwdPerSm);
+    const int grid = w.grid;
+    NormParams P = params_of(c, sel_idx);
+    P.share = w.share; P.splits = w.splits;
     P.x = x; P.y = y; P.gate = gate; P.w_post = w_post; P.b_post = b_post; P.w_pre = w_pre; P.b_pre = b_pre;
     P.sel_idx = sel_idx; P.n_sel = sel_idx ? n_sel : nullptr;
     P.h = h; P.u = u; P.stats = reinterpret_cast<float4*>(stats);
@@ -784,37 +157,49 @@ int norm_fwd_launch(const void* x, const void* y, const float* gate, const float
     return check_cuda(launch_type(false, c.dtype, grid, P, stream), "norm: forward launch");
 }
 
-size_t norm_workspace_bytes(const vardrop_norm_cfg& cfg) {
-    size_t most = 0;
-    for (const bool selected : {false, true}) {          // the query does not say
-        const vardrop_norm_cfg c = flat(cfg, selected);
-        int splits, grid;
-        shares(c, kBwdPer, kBwdPerSm, splits, grid);
-        const size_t slots = c.gate_rows > 1 ? static_cast<size_t>(c.B) * splits : grid, rows = 2 * (slots + grid);
-        most = rows > most ? rows : most;
-    }
-    return kWsHeaderBytes + align_up(sizeof(float) * most * cfg.C, 256);
+namespace {
+// Partial sums and, with a gate an instance, where the instances begin.
+struct NormWs {
+    Shares s;
+    int slots;
+    size_t begin, partial, total;
+};
+NormWs norm_layout(const vardrop_norm_cfg& c, bool selected) {
+    NormWs w;
+    w.s = shares(c, selected, kBwdPer, kBwdPerSm);
+    w.slots = c.gate_rows <= 1 ? w.s.grid : w.s.share == kRuns ? w.s.grid + c.B : c.B * w.s.splits;
+    w.begin = kWsHeaderBytes;
+    w.partial = w.begin + (c.gate_rows > 1 ? align_up(sizeof(int32_t) * (static_cast<size_t>(c.B) + 1), 256) : 0);
+    w.total = w.partial + align_up(sizeof(float) * 2 * (static_cast<size_t>(w.slots) + w.s.grid) * c.C, 256);
+    return w;
+}
+}  // namespace
+
+size_t norm_workspace_bytes(const vardrop_norm_cfg& c) {         // (the query does not say whether tokens are selected)
+    const size_t a = norm_layout(c, false).total, b = norm_layout(c, true).total;
+    return a > b ? a : b;
 }
 
 int norm_bwd_launch(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const int32_t* sel_idx, const int32_t* n_sel,
-                    const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg& cfg, void* dx, void* dy, float* d_gate, float* d_w_post,
+                    const int32_t* inv_idx, const float* stats, const void* d_h, const void* d_u, const vardrop_norm_cfg& c, void* dx, void* dy, float* d_gate, float* d_w_post,
                     float* d_b_post, float* d_w_pre, float* d_b_pre, void* ws, cudaStream_t stream) {
-    const vardrop_norm_cfg c = flat(cfg, sel_idx != nullptr);
-    int splits, grid;
-    shares(c, kBwdPer, kBwdPerSm, splits, grid);
-    NormParams P = params_of(c, sel_idx, splits);
+    const NormWs w = norm_layout(c, sel_idx != nullptr);
+    const int grid = w.s.grid;
+    NormParams P = params_of(c, sel_idx);
+    P.share = w.s.share; P.splits = w.s.splits;
     P.x = x; P.y = y; P.gate = gate; P.w_post = w_post; P.b_post = b_post; P.w_pre = w_pre;
     P.sel_idx = sel_idx; P.n_sel = sel_idx ? n_sel : nullptr; P.inv_idx = sel_idx ? inv_idx : nullptr;
     P.stats = reinterpret_cast<float4*>(const_cast<float*>(stats));
     P.d_h = d_h; P.d_u = d_u; P.dx = dx; P.dy = dy;
-    P.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + kWsHeaderBytes);
-    P.slots = c.gate_rows > 1 ? P.units : grid;
+    P.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + w.partial);
+    P.begin = c.gate_rows > 1 && w.s.share == kRuns ? reinterpret_cast<int32_t*>(static_cast<char*>(ws) + w.begin) : nullptr;
+    P.slots = w.slots;
     {
         LaunchScope ls_(K_NORM_BWD, stream);
         if (int st = check_cuda(launch_type(true, c.dtype, grid, P, stream), "norm: backward launch")) return st;
     }
     if (!d_gate && !d_w_post && !d_b_post && !d_w_pre && !d_b_pre) return VARDROP_OK;
-    ParamsParams Q{P.partial, gate, w_post, b_post, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, c.B, c.C, c.gate_rows, splits, P.slots, grid, c.pre == 2 || c.post == 2};
+    ParamsParams Q{P.partial, gate, w_post, b_post, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, P.begin, c.B, c.C, c.gate_rows, P.slots, grid, c.pre == 2 || c.post == 2, w.s.share == kSplit ? w.s.splits : 0};
     LaunchScope ls_(K_NORM_PARAMS, stream);
     return check_cuda(launch_chained(norm_params_kernel, dim3((c.C + kColsX - 1) / kColsX, 2 + (d_gate && c.gate_rows > 1 ? (c.gate_rows + kColsY - 1) / kColsY : 0)), dim3(kColsX * kColsY), 0, stream, Q),
                       "norm: parameters' gradients launch");
