@@ -204,39 +204,26 @@ struct GroupSum {
 template <int kGroup>
 constexpr int kNormThreads = kGroup < 256 ? 256 : kGroup;        // of a CTA
 
-// Rows on their way from memory: a ring in shared memory, so that a group has kStages - 1 rows in flight while it works on one, without registers for them.  Rows of 16- or 4-byte
-// vectors are copied by the threads that read them, into places of their own, without barriers.  (Loads into registers behind the row before: 65536 x 1024 bf16 forward 188 us, backward
-// 367; like this 118 and 166, bound by the instructions of scalar arithmetic.)  Rows of 16-bit elements in odd numbers begin on any even address: the group copies the 16-byte words
-// that a row lies in as they are, and its threads meet before they read their elements from them (28 x 1225 x 1955 fp16, forward and backward: 703 us with loads of elements when they
-// are needed, LINEARTIME).
+// Rows on their way from memory: a ring in shared memory whose places belong to one thread each, filled by asynchronous copies of the thread's own columns, so
+// that a group has kStages - 1 rows in flight while it works on one, without registers for them and without barriers.  (Loads into registers behind the row before: 65536 x
+// 1024 bf16 forward 188 us, backward 367; like this 118 and 166, bound by the instructions of scalar arithmetic.)  Columns of two bytes, which those copies cannot take, are
+// loaded when they are needed.
 template <class T, int kV, int kGroup, int kPer, int kTensors>
 struct Ring {
     using R = Row<T, kV, kGroup, kPer>;
     using Vec = typename R::Vec;
-    static constexpr bool kWords = R::kVecBytes < 4;
-    static constexpr int kThreads = kNormThreads<kGroup>, kGroups = kThreads / kGroup;
-    static constexpr int kRowBytes = (kGroup * kPer * static_cast<int>(sizeof(T)) + 16 + 127) / 128 * 128;     // kWords: of a row, which may begin anywhere in a word
-    static constexpr int kStageBytes = (kWords ? kGroups * kRowBytes : kThreads * kPer * static_cast<int>(sizeof(T))) * kTensors;
+    static constexpr bool kAsync = R::kVecBytes >= 4;
+    static constexpr int kThreads = kNormThreads<kGroup>;
+    static constexpr int kStageBytes = kThreads * kPer * static_cast<int>(sizeof(T)) * kTensors;
     static constexpr int kFit = 200 * 1024 / kStageBytes;
     static constexpr int kStages = kFit < 1 ? 1 : kFit > 3 ? 3 : kFit;
-    static_assert(!kWords || kStages >= 2, "a row is fetched while the one before is read");
-    static constexpr int kBytes = kStages * kStageBytes;
-    unsigned char* base;                 // kWords: of this group; otherwise this thread's first place
-    __device__ __forceinline__ explicit Ring(unsigned char* smem)
-        : base(smem + (kWords ? static_cast<int>(threadIdx.x) / kGroup * kRowBytes : static_cast<int>(threadIdx.x * sizeof(Vec)))) {}
-    __device__ __forceinline__ Vec* at(int stage, int k, int j) const { return reinterpret_cast<Vec*>(base) + ((stage * kTensors + k) * R::kVecs + j) * kThreads; }
-    __device__ __forceinline__ unsigned char* row_at(int stage, int k) const { return base + (stage * kTensors + k) * kGroups * kRowBytes; }
+    static constexpr int kBytes = kAsync ? kStages * kStageBytes : 0;
+    Vec* mine;                           // this thread's first place
+    __device__ __forceinline__ Vec* at(int stage, int k, int j) const { return mine + ((stage * kTensors + k) * R::kVecs + j) * kThreads; }
     // tensor k of a row (NULL: none) to a stage; commit() behind the last one
     __device__ __forceinline__ void fetch(int stage, int k, const T* row, int t, int C) {
-        if (!row) return;
-        if constexpr (kWords) {
-            const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + C * sizeof(T), from = begin & ~static_cast<uintptr_t>(15);
-            const uint32_t to = smem_u32(row_at(stage, k));
-            for (uintptr_t p = from + 16 * t; p < end; p += 16 * kGroup) {       // (what lies behind the row is not read)
-                const uint32_t bytes = end - p < 16 ? static_cast<uint32_t>(end - p) : 16u;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + static_cast<uint32_t>(p - from)), "l"(p), "r"(bytes) : "memory");
-            }
-        } else {
+        if constexpr (kAsync) {
+            if (!row) return;
 #pragma unroll
             for (int j = 0; j < R::kVecs; ++j) {
                 if (R::col(t, j) >= C) continue;
@@ -246,37 +233,20 @@ struct Ring {
             }
         }
     }
-    __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    // The next stage's row, `fetch_next`, and the wait for the oldest one in flight.  Where threads read what others have copied, they meet: behind that meeting the row before has been read
-    // by all, and its stage is the one to fetch into.
-    template <class F>
-    __device__ __forceinline__ void turn(F fetch_next, int group) {
-        if constexpr (kWords) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-            if (kGroup <= 32) __syncwarp();
-            else group_barrier<kGroup>(group);
-            fetch_next();
-        } else {
-            fetch_next();
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-        }
+    __device__ __forceinline__ void commit() {
+        if (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // ahead of the first fetches of another part: everybody has read the last row of the one before
-    __device__ __forceinline__ void part_begins(int group) {
-        if constexpr (kWords) {
-            if (kGroup <= 32) __syncwarp();
-            else group_barrier<kGroup>(group);
-        }
+    __device__ __forceinline__ void wait() {             // the oldest stage in flight has landed
+        if (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
     }
     // a row's columns, zeros behind its end
     __device__ __forceinline__ void read(int stage, int k, const T* row, int t, int C, typename R::Values& to) const {
         Vec v[R::kVecs];
-        const unsigned char* from = kWords ? row_at(stage, k) + (reinterpret_cast<uintptr_t>(row) & 15) : nullptr;
 #pragma unroll
         for (int j = 0; j < R::kVecs; ++j) {
             if (R::col(t, j) < C) {
-                if constexpr (kWords) v[j].w[0] = *reinterpret_cast<const unsigned short*>(from + R::col(t, j) * sizeof(T));
-                else v[j] = *at(stage, k, j);
+                if constexpr (kAsync) v[j] = *at(stage, k, j);
+                else v[j] = R::load(row + R::col(t, j));
             } else {
 #pragma unroll
                 for (int w = 0; w < R::kWords; ++w) v[j].w[w] = 0u;
@@ -434,7 +404,7 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
     __shared__ long long s_scan[kNormThreads<kGroup> / 32 + 2];
     const int group = threadIdx.x / kGroup, t = threadIdx.x % kGroup;
     GroupSum<kGroup> sum{s_sum[group], 0, group};
-    Rows ring(smem_dyn);
+    Rows ring{reinterpret_cast<typename Rows::Vec*>(smem_dyn) + threadIdx.x};
     chain_wait();
     chain_release();
     const T* const X = static_cast<const T*>(P.x);
@@ -464,7 +434,7 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
             }
         }
         int i = first, stage = 0, ahead = first;
-        int source = walk.source(ahead), from_row = source;
+        int source = walk.source(ahead);
         auto fetch = [&](int to) {
             if (ahead < walk.n) {
                 ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
@@ -474,7 +444,6 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
             ahead += walk.step;
             source = walk.source(ahead);
         };
-        ring.part_begins(group);
 #pragma unroll
         for (int s = 0; s < kAhead; ++s) fetch(s);
         // Groups of less than a warp leave the loop together; one without a token works on a row without columns.
@@ -482,10 +451,9 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
 #pragma unroll 1
         for (; i - behind < walk.n; i += walk.step) {
             const int C = kGroup < 32 && i >= walk.n ? 0 : P.C;
-            const int from = from_row;
-            const int from_next = Rows::kWords ? walk.source(i + walk.step) : 0;       // (its address tells where in a word the row begins)
-            ring.turn([&] { fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages); }, group);
-            from_row = from_next;
+            const int from = Rows::kAsync ? 0 : walk.source(i);
+            fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
+            ring.wait();
             const size_t row = (base + i) * P.C;
             float2 post = make_float2(0.f, 1.f), pre = post;
             typename R::Values h;
@@ -534,7 +502,7 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
     __shared__ Pair s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kGroup * kPairs : 1];
     const int group = threadIdx.x / kGroup, t = threadIdx.x % kGroup;
     GroupSum<kGroup> sum{s_sum[group], 0, group};
-    Rows ring(smem_dyn);
+    Rows ring{reinterpret_cast<typename Rows::Vec*>(smem_dyn) + threadIdx.x};
     chain_wait();
     chain_release();
     const T* const X = static_cast<const T*>(P.x);
@@ -625,16 +593,16 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
             ahead += walk.step;
             source = walk.source(ahead);
         };
-        ring.part_begins(group);
 #pragma unroll
         for (int s = 0; s < kAhead; ++s) fetch(s);
 #pragma unroll 1
         for (int i = first; i - behind < walk.n; i += walk.step) {
             const int C = kGroup < 32 && i >= walk.n ? 0 : P.C;
+            fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
             // of the next row, ahead of the wait
             const int from_next = walk.source(i + walk.step);
             const float4 st_next = i + walk.step < walk.n ? __ldg(P.stats + base + i + walk.step) : make_float4(0.f, 0.f, 0.f, 0.f);
-            ring.turn([&] { fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages); }, group);
+            ring.wait();
             const size_t row = (base + i) * P.C;
             typename R::Values h, zy, d;
             ring.read(stage, 0, X + (base + from) * P.C, t, C, h);
