@@ -85,6 +85,31 @@ __device__ __forceinline__ void copy_32_tokens(unsigned char* rows, const __nv_b
     for (int it = 0; it < 8; ++it, src += 4 * sT) cp_async16((dst ^ ((it & 1) * 64u)) + it * 4 * kRowBytes, 4 * it < left ? src : begin, 4 * it < left ? live : 0u);
 }
 
+// Short sequences under grouped heads: the query rows of several heads of a group share a tile (they see the same keys), head after head.  Row r of such a tile.
+struct PackedRow {
+    int head, token;                     // from the tile's first head on
+};
+__device__ __forceinline__ PackedRow packed_row(int r, int len) {
+    const int g = small_div(r, len);
+    return PackedRow{g, r - g * len};
+}
+// Heads of a group that share a tile.
+__device__ __forceinline__ int heads_a_tile(int len, int left) { return max(1, min(left, small_div(kTile, len))); }
+// One warp's share of such a tile: 32 rows from r0 on, zeros from n_rows on.
+__device__ __forceinline__ void copy_32_packed(unsigned char* rows, const __nv_bfloat16* from, long long sT, long long sH, int r0, int n_rows, int len, int D) {
+    const int lane = threadIdx.x & 31, chunk = lane & 7, r = lane >> 3;
+    const uint32_t live = chunk * 8 < D ? 16u : 0u;
+    const __nv_bfloat16* const begin = from + (live ? chunk * 8 : 0);
+    const uint32_t dst = smem_u32(rows) + r * kRowBytes + (static_cast<uint32_t>(chunk ^ r) << 4);
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {
+        const int at = r0 + r + 4 * it;
+        const bool there = at < n_rows;
+        const PackedRow p = packed_row(there ? at : 0, len);
+        cp_async16((dst ^ ((it & 1) * 64u)) + it * 4 * kRowBytes, begin + p.token * sT + p.head * sH, there ? live : 0u);
+    }
+}
+
 __device__ __forceinline__ void tma_store_3d(const void* map, const void* src, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)

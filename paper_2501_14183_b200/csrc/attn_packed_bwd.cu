@@ -52,6 +52,7 @@ constexpr int kShortSmemBytes = 4 * kTileBytes /*Q, dO, K, V*/ + 2 * kTileBytes 
 // large as dS itself (and neither O nor prep, accumulator and conversion are needed).
 // A chain of latencies like the forward's: two CTAs to an SM, rolled loops over 32 scores; P and dP stay in tensor memory between the two passes over a row.  P^T dO, dS^T Q and
 // dS K take P and dS from shared memory, the first two as transposed views.
+// Grouped heads of a short sequence share tiles, as many as have room (39 sequences of 1 to 13 tokens, 24 query heads on 3, forward and backward: 45 us one after another, 29 like this).
 // kGrouped: several query heads a key head; dV and dK add up in columns of their own, which takes all of tensor memory and leaves one CTA to an SM.  Otherwise they come over the
 // scores' columns.
 // Tensor memory: S, P 128 | dP 128, then (dV 64 | dK 64 | dQ 64) over them, or with kGrouped: dQ 64 over S; dV 64 | dK 64 behind.
@@ -110,22 +111,32 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
     for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
         const int e = item / P.Hkv, kvh = item - e * P.Hkv;
         const int4 entry = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + first + e));
-        const int start = entry.x, len = entry.y, steps = (len + 15) >> 4, groups = (len + 31) >> 5;        // k-steps of 16 tokens, warps' shares of 32
+        const int start = entry.x, len = entry.y, steps = (len + 15) >> 4, groups = (len + 31) >> 5;        // of the keys: k-steps of 16, warps' shares of 32
         const long long kv_off = start * P.sTkv + kvh * P.sHkv;
+        int heads = 1;                                   // that share a tile
 #pragma unroll 1
-        for (int g = 0; g < P.group; ++g) {
+        for (int g = 0; g < P.group; g += heads) {
             const int h = kvh * P.group + g;
+            if (kGrouped) heads = heads_a_tile(len, P.group - g);
+            const int n_rows = heads * len, steps_q = (n_rows + 15) >> 4, groups_q = (n_rows + 31) >> 5;
             // tiles of 32-row shares: Q, dO, and at the item's begin K, V; rows up to the next k-step are zeros, those of shares behind it are not read
-            const int n_load = (g == 0 ? 4 : 2) * groups;
+            const int n_load = 2 * groups_q + (g == 0 ? 2 * groups : 0);
 #pragma unroll 1
             for (int x = warp; x < n_load; x += kShortThreads / 32) {
-                const int tile = small_div(x, groups), r0 = (x - tile * groups) * 32;
-                const __nv_bfloat16* from = tile == 0 ? P.q + start * P.sTq + h * P.sHq
-                                            : tile == 1 ? P.d_o + (static_cast<long long>(start) * P.Hq + h) * P.D
-                                            : (tile == 2 ? P.k : P.v) + kv_off;
-                copy_32_tokens(smem_dyn + tile * kTileBytes + r0 * kRowBytes, from, tile == 0 ? P.sTq : tile == 1 ? static_cast<long long>(P.Hq) * P.D : P.sTkv, r0, len, P.D);
+                if (x < 2 * groups_q) {
+                    const int tile = x >= groups_q, r0 = (x - tile * groups_q) * 32;
+                    const long long sT = tile ? static_cast<long long>(P.Hq) * P.D : P.sTq, sH = tile ? P.D : P.sHq;
+                    const __nv_bfloat16* from = tile ? P.d_o + (static_cast<long long>(start) * P.Hq + h) * P.D : P.q + start * P.sTq + h * P.sHq;
+                    unsigned char* to = smem_dyn + tile * kTileBytes + r0 * kRowBytes;
+                    if (kGrouped && heads > 1) copy_32_packed(to, from, sT, sH, r0, n_rows, len, P.D);
+                    else copy_32_tokens(to, from, sT, r0, len, P.D);
+                } else {
+                    const int y = x - 2 * groups_q, tile = y >= groups, r0 = (y - tile * groups) * 32;
+                    copy_32_tokens((tile ? sV : sK) + r0 * kRowBytes, (tile ? P.v : P.k) + kv_off, P.sTkv, r0, len, P.D);
+                }
             }
-            const float lse2 = row < len ? __ldg(P.lse + static_cast<size_t>(h) * P.T + start + row) * 1.4426950408889634f : 0.f;
+            const PackedRow at = kGrouped && heads > 1 && row < n_rows ? packed_row(row, len) : PackedRow{0, row};
+            const float lse2 = row < n_rows ? __ldg(P.lse + static_cast<size_t>(h + at.head) * P.T + start + at.token) * 1.4426950408889634f : 0.f;
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async_smem();
             tc_fence_before();
@@ -144,7 +155,7 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
             }
             wait();
             // ---- P, rounded to bf16 for P^T dO and as it is over S; Delta ----
-            const int seen = P.causal ? min(len, row + 1) : len, c_end = min(half * 64 + 64, steps * 16);        // keys that this row sees; columns of this thread
+            const int seen = P.causal ? min(len, at.token + 1) : len, c_end = min(half * 64 + 64, steps * 16);        // keys that this row sees; columns of this thread
             float delta = 0.f;
 #pragma unroll 1
             for (int c = half * 64; c < c_end; c += 32) {
@@ -198,7 +209,7 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
                 if (elect_one()) {
                     const uint32_t idesc = umma_idesc_bf16(128, P.D, 1, 1);
 #pragma unroll 1
-                    for (int ks = 0; ks < steps; ++ks) tc_mma_bf16(tmem + kDv, umma_desc_advance(t_p, ks * 2048), umma_desc_advance(t_do, ks * 2048), idesc, (kGrouped && g > 0) || ks > 0);
+                    for (int ks = 0; ks < steps_q; ++ks) tc_mma_bf16(tmem + kDv, umma_desc_advance(t_p, ks * 2048), umma_desc_advance(t_do, ks * 2048), idesc, (kGrouped && g > 0) || ks > 0);
                     tc_commit(&bar);
                 }
                 __syncwarp();
@@ -224,7 +235,7 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
                     for (int ks = 0; ks < steps; ++ks)   // dQ = dS K
                         tc_mma_bf16(tmem + kDq, umma_desc_advance(k_p, (ks >> 2) * kTileBytes + (ks & 3) * 32), umma_desc_advance(t_k, ks * 2048), idesc_q, ks > 0);
 #pragma unroll 1
-                    for (int ks = 0; ks < steps; ++ks)   // dK = dS^T Q
+                    for (int ks = 0; ks < steps_q; ++ks) // dK = dS^T Q
                         tc_mma_bf16(tmem + kDk, umma_desc_advance(t_p, ks * 2048), umma_desc_advance(t_q, ks * 2048), idesc_k, (kGrouped && g > 0) || ks > 0);
                     tc_commit(&bar);
                 }
@@ -232,7 +243,7 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
             }
             wait();
             // ---- rows out, half of the columns a thread, through tiles that have been read, so that whole rows are written ----
-            const bool last = !kGrouped || g + 1 == P.group;
+            const bool last = !kGrouped || g + heads == P.group;
             auto stage = [&](unsigned char* tile, uint32_t col, float mul) {
 #pragma unroll 1
                 for (int c = half * (P.D / 2); c < (half + 1) * (P.D / 2); c += 16) {
@@ -252,16 +263,18 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
                 stage(sP, kDk, P.scale);
             }
             __syncthreads();
-            const int chunks_row = P.D >> 3, sh = P.D > 32 ? 3 : 2;
-#pragma unroll 1
-            for (int x = 0; x < (last ? 3 : 1); ++x) {
-                const unsigned char* tile = x == 0 ? sQ : x == 1 ? sdO : sP;
-                const int heads = x == 0 ? P.Hq : P.Hkv;
-                __nv_bfloat16* to = (x == 0 ? P.dq : x == 1 ? P.dv : P.dk) + (static_cast<size_t>(start) * heads + (x == 0 ? h : kvh)) * P.D;
-#pragma unroll 4
-                for (int at = tid; at < len << sh; at += kShortThreads) {
-                    const int r = at >> sh, c = at & (chunks_row - 1);
-                    *reinterpret_cast<uint4*>(to + static_cast<size_t>(r) * heads * P.D + c * 8) = *reinterpret_cast<const uint4*>(tile + r * kRowBytes + ((c ^ (r & 7)) << 4));
+            const int sh = P.D > 32 ? 3 : 2, c = tid & ((1 << sh) - 1);
+#pragma unroll 2
+            for (int r = tid >> sh; r < n_rows; r += kShortThreads >> sh) {
+                const PackedRow to = kGrouped && heads > 1 ? packed_row(r, len) : PackedRow{0, r};
+                *reinterpret_cast<uint4*>(P.dq + (static_cast<size_t>(start + to.token) * P.Hq + h + to.head) * P.D + c * 8) = *reinterpret_cast<const uint4*>(sQ + r * kRowBytes + ((c ^ (r & 7)) << 4));
+            }
+            if (last) {
+#pragma unroll 2
+                for (int r = tid >> sh; r < len; r += kShortThreads >> sh) {
+                    const size_t to = (static_cast<size_t>(start + r) * P.Hkv + kvh) * P.D + c * 8;
+                    *reinterpret_cast<uint4*>(P.dv + to) = *reinterpret_cast<const uint4*>(sdO + r * kRowBytes + ((c ^ (r & 7)) << 4));
+                    *reinterpret_cast<uint4*>(P.dk + to) = *reinterpret_cast<const uint4*>(sP + r * kRowBytes + ((c ^ (r & 7)) << 4));
                 }
             }
             tc_fence_before();

@@ -626,6 +626,12 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
         const int e = item / P.Hq, h = item - e * P.Hq, kvh = small_div(h, P.group);
         const int4 entry = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + first + e));
         const int start = entry.x, len = entry.y, qt = entry.z, n_kv = P.causal ? qt + 1 : (len + kTile - 1) / kTile;
+        // Grouped heads of a short sequence share a tile: the first of them has the work of all.  (Not where every tile of a head finds a place of its own: what the places of the rows
+        // take is then on the path of a chain of latencies, 7.4 -> 9.0 us for a few short prompts.)
+        const int in_group = h - kvh * P.group, most = len <= kTile / 2 && n_items > static_cast<int>(gridDim.x) ? heads_a_tile(len, P.group) : 1;
+        if (most > 1 && in_group % most != 0) continue;
+        const int heads = most > 1 ? min(most, P.group - in_group) : 1;
+        const PackedRow at = heads > 1 ? packed_row(min(tid, heads * len - 1), len) : PackedRow{0, tid};
         const __nv_bfloat16* const q = P.q + start * P.sTq + h * P.sHq;
         const __nv_bfloat16* const k = P.k + start * P.sTkv + kvh * P.sHkv;
         const __nv_bfloat16* const v = P.v + start * P.sTkv + kvh * P.sHkv;
@@ -633,7 +639,8 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
         auto load_rows = [&](unsigned char* tile, const __nv_bfloat16* from, long long sT, int t0) {
             copy_32_tokens(tile + warp * 32 * kRowBytes, from, sT, t0 * kTile + warp * 32, len, P.D);
         };
-        load_rows(sQ, q, P.sTq, qt);
+        if (heads > 1) copy_32_packed(sQ + warp * 32 * kRowBytes, q, P.sTq, P.sHq, warp * 32, heads * len, len, P.D);
+        else load_rows(sQ, q, P.sTq, qt);
         load_rows(sK, k, P.sTkv, 0);
         asm volatile("cp.async.commit_group;" ::: "memory");
         load_rows(sV, v, P.sTkv, 0);
@@ -642,7 +649,7 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
         float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll 1
         for (int j = 0; j < n_kv; ++j, ++t) {
-            const int n_keys = min(kTile, len - j * kTile), n_seen = P.causal && j == qt ? min(n_keys, tid + 1) : n_keys;     // of this row
+            const int n_keys = min(kTile, len - j * kTile), n_seen = P.causal && j == qt ? min(n_keys, at.token + 1) : n_keys;     // of this row
             if (j > 0) {
 #pragma unroll 1
                 for (int x = 1; x < 3; ++x) {            // K, V
@@ -783,8 +790,8 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
         {
             const float inv_l = 1.f / l_run;
             unsigned char* rowp = sQ + tid * kRowBytes;
-            const int row = qt * kTile + tid;
-            if (row < len) P.lse[static_cast<size_t>(h) * P.T + start + row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+            const int row = qt * kTile + at.token;
+            if (heads > 1 ? tid < heads * len : row < len) P.lse[static_cast<size_t>(h + at.head) * P.T + start + row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
 #pragma unroll 1
             for (int c16 = 0; c16 < P.D / 16; ++c16) {
                 float ov[16];
@@ -799,7 +806,13 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
             tc_fence_before();
             __syncwarp();                                // a warp writes the rows it has staged
             const int c = lane & 7, r0 = warp * 32 + (lane >> 3);
-            if (c * 8 < P.D) {
+            if (heads > 1) {
+#pragma unroll 1
+                for (int r = r0; r < min(warp * 32 + 32, heads * len) && c * 8 < P.D; r += 4) {
+                    const PackedRow to = packed_row(r, len);
+                    *reinterpret_cast<uint4*>(P.o + (static_cast<size_t>(start + to.token) * P.Hq + h + to.head) * P.D + c * 8) = *reinterpret_cast<const uint4*>(sQ + r * kRowBytes + ((c ^ (r & 7)) << 4));
+                }
+            } else if (c * 8 < P.D) {
                 __nv_bfloat16* out = P.o + (static_cast<size_t>(start + qt * kTile + r0) * P.Hq + h) * P.D + c * 8;
                 const unsigned char* from = sQ + r0 * kRowBytes + ((c ^ (r0 & 7)) << 4);
                 const unsigned char* from4 = sQ + (r0 + 4) * kRowBytes + ((c ^ ((r0 + 4) & 7)) << 4);
