@@ -30,8 +30,8 @@ inline bool packed_may_split(const vardrop_packed_cfg& c) { return packed_tiles(
 
 struct PackedWs {
     size_t delta;           // [Hq, tiles 128] fp32
-    size_t dq_acc;          // [tiles 128, Hq, 64] fp32
-    size_t parts;           // [tiles 128, (dV, dK), part, Hkv, 64] fp32
+    size_t dq_acc;          // [tiles 128, Hq, D] fp32
+    size_t parts;           // [tiles 128, (dV, dK), part, Hkv, D] fp32
     size_t total;
     int rows;               // tiles 128
 };
@@ -40,8 +40,8 @@ inline PackedWs packed_layout(const vardrop_packed_cfg& c) {
     w.rows = static_cast<int>(packed_tiles(c) * kTile);
     size_t o = align_up(kWsHeaderBytes, 1024);
     w.delta = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * w.rows, 1024);
-    w.dq_acc = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * kDP * w.rows, 1024);
-    w.parts = o; o += packed_may_split(c) ? align_up(sizeof(float) * 2 * kMostParts * c.Hkv * kDP * static_cast<size_t>(w.rows), 1024) : 0;
+    w.dq_acc = o; o += align_up(sizeof(float) * static_cast<size_t>(c.Hq) * c.D * w.rows, 1024);
+    w.parts = o; o += packed_may_split(c) ? align_up(sizeof(float) * 2 * kMostParts * c.Hkv * c.D * static_cast<size_t>(w.rows), 1024) : 0;
     w.total = o;
     return w;
 }
@@ -59,8 +59,8 @@ inline PackedStrides packed_strides(const vardrop_packed_cfg& c) {
 // Tensor map over [T, H, D] bf16 with the given element strides: box = 128 tokens x 64 elements of a head, 128-byte swizzle; the upper half of a row of a tensor with
 // D = 32, and rows behind the tensor, read as zero.
 int packed_tile_map(CUtensorMap* map, const void* base, int D, int H, int T, long long sT, long long sH);
-// Over the fp32 accumulator [rows, H, 64]: box = 128 rows x 32 floats of a head.
-int packed_acc_map(CUtensorMap* map, const void* base, int rows, int H);
+// Over the fp32 accumulator [rows, H, D]: box = 128 rows x 32 floats of a head.
+int packed_acc_map(CUtensorMap* map, const void* base, int rows, int H, int D);
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const void* map, uint64_t* bar, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"

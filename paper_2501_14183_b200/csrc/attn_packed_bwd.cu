@@ -299,17 +299,17 @@ struct PackedPrepParams {
     const uint4* o;         // [T, Hq, D] bf16
     const uint4* d_o;       // [T, Hq, D] bf16
     float* delta;           // [Hq, rows]
-    float4* dq_acc;         // [rows, Hq, 64] fp32
+    float4* dq_acc;         // [rows, Hq, D] fp32
     PlanView plan;
     int* ticket;
     int Hq, D, rows;
 };
-// A CTA takes slices of 1024 16-byte chunks of (token, head) rows of 64 by turns; the eight threads of a row reduce Delta by shuffles.
+// A CTA takes slices of 1024 16-byte chunks of (token, head) rows by turns; the eight (four) threads of a row reduce Delta by shuffles.
 __global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams P) {
     chain_wait();
     chain_release();
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.ticket = 0;
-    const int n_tiles = plan_head(P.plan).longer, chunks_row = P.Hq * 8, src_chunks_head = P.D / 8;
+    const int n_tiles = plan_head(P.plan).longer, sh = P.D > 32 ? 3 : 2, chunks_row = P.Hq << sh;
     const int per_tile = kTile * chunks_row, slices = (per_tile + 1023) / 1024;        // four chunks a thread
 #pragma unroll 1
     for (long long k = blockIdx.x; k < static_cast<long long>(n_tiles) * slices; k += gridDim.x) {
@@ -324,18 +324,21 @@ __global__ void __launch_bounds__(256) packed_prep_kernel(const PackedPrepParams
             row[u] = idx < per_tile ? small_div(idx, chunks_row) : kTile;
             c[u] = idx - row[u] * chunks_row;
             vo[u] = vd[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (row[u] < left && row[u] < kTile && (c[u] & 7) < src_chunks_head) {
-                const size_t src = (static_cast<size_t>(x.x + x.z * kTile + row[u]) * P.Hq + (c[u] >> 3)) * src_chunks_head + (c[u] & 7);
+            if (row[u] < left && row[u] < kTile) {
+                const size_t src = static_cast<size_t>(x.x + x.z * kTile + row[u]) * chunks_row + c[u];
                 vo[u] = __ldg(P.o + src);
                 vd[u] = __ldg(P.d_o + src);
             }
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const float part = sum8(dot8(vo[u], vd[u]));
+            float part = dot8(vo[u], vd[u]);
+            part += __shfl_xor_sync(0xffffffffu, part, 1);
+            part += __shfl_xor_sync(0xffffffffu, part, 2);
+            if (sh == 3) part += __shfl_xor_sync(0xffffffffu, part, 4);
             if (row[u] >= kTile) continue;
             const size_t to = static_cast<size_t>(x.w + x.z) * kTile + row[u];
-            if ((c[u] & 7) == 0) P.delta[static_cast<size_t>(c[u] >> 3) * P.rows + to] = part;
+            if ((c[u] & ((1 << sh) - 1)) == 0) P.delta[static_cast<size_t>(c[u] >> sh) * P.rows + to] = part;
             const size_t dst = to * chunks_row + c[u];
             P.dq_acc[2 * dst] = make_float4(0.f, 0.f, 0.f, 0.f);
             P.dq_acc[2 * dst + 1] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -676,11 +679,11 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
         const Split split = split_of(P.plan, head, P.group, P.Hkv, gridDim.x, P.may_split);
         const int units = P.Hkv * split.parts;                 // of a plan entry
         const long long n_items = static_cast<long long>(head.longer) * units;
-        // Some SMs are left to packed_short_kernel, which comes next: by the time that either takes, in steps of this kernel: one of the short kernel's heads is three of them (a
-        // CTA, of which an SM holds two without groups), and an item here has the latency of five besides its own.
+        // Some SMs are left to packed_short_kernel, which comes next: by the time that either takes, in steps of this kernel: one of the short kernel's heads counts as one of
+        // them (0.7 without groups, when an SM holds two of its CTAs), and an item here has the latency of five besides its own.
         int ctas = gridDim.x;
         if (head.longer > 0 && head.tiles > head.longer) {
-            const float shorts = static_cast<float>(head.tiles - head.longer) * static_cast<float>(P.Hq) * (P.group > 1 ? 3.f : 1.5f);
+            const float shorts = static_cast<float>(head.tiles - head.longer) * static_cast<float>(P.Hq) * (P.group > 1 ? 1.f : 0.7f);
             const float mine = __int_as_float(P.plan.words[kPlanWork]) * static_cast<float>(P.Hq) + 5.f * static_cast<float>(n_items);
             ctas = max(1, ctas - max(1, __float2int_rn(static_cast<float>(ctas) * (shorts / (shorts + mine)))));
         }
@@ -1003,9 +1006,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
 // dq from the accumulator
 // ---------------------------------------------------------------------------------------------------------
 struct PackedConvertParams {
-    const float4* dq_acc;    // [rows, Hq, 64] fp32
+    const float4* dq_acc;    // [rows, Hq, D] fp32
     uint4* dq;               // [T, Hq, D] bf16
-    const float4* parts;     // [rows, (dV, dK), part, Hkv, 64] fp32
+    const float4* parts;     // [rows, (dV, dK), part, Hkv, D] fp32
     uint4 *dv, *dk;          // [T, Hkv, D] bf16
     PlanView plan;
     int Hq, Hkv, group, D, causal, may_split, main_grid;
@@ -1027,7 +1030,7 @@ __global__ void __launch_bounds__(256) packed_convert_kernel(const PackedConvert
             const int idx = slice * 1024 + u * 256 + static_cast<int>(threadIdx.x);
             if (idx >= there) continue;
             const int row = small_div(idx, chunks_row), c = idx - row * chunks_row;
-            const float4* src = P.dq_acc + ((static_cast<size_t>(x.w + x.z) * kTile + row) * P.Hq + (c >> sh)) * (kDP / 4) + (c & ((1 << sh) - 1)) * 2;
+            const float4* src = P.dq_acc + ((static_cast<size_t>(x.w + x.z) * kTile + row) * chunks_row + c) * 2;
             a[u][0] = __ldcg(src);
             a[u][1] = __ldcg(src + 1);
         }
@@ -1052,10 +1055,10 @@ __global__ void __launch_bounds__(256) packed_convert_kernel(const PackedConvert
         const int idx = slice * 256 + static_cast<int>(threadIdx.x), which = idx >= kTile * kv_row ? 1 : 0, in = idx - which * kTile * kv_row;
         const int row = small_div(in, kv_row), c = in - row * kv_row;
         if (idx >= kv_tile || row >= x.y - jt * kTile) continue;
-        const float4* src = P.parts + (((static_cast<size_t>(x.w + jt) * kTile + row) * 2 + which) * kMostParts * P.Hkv + (c >> sh)) * (kDP / 4) + (c & ((1 << sh) - 1)) * 2;
+        const float4* src = P.parts + (((static_cast<size_t>(x.w + jt) * kTile + row) * 2 + which) * kMostParts * kv_row + c) * 2;
         float4 a = __ldcg(src), b = __ldcg(src + 1);
         for (int p = 1; p < parts; ++p) {
-            src += P.Hkv * (kDP / 4);
+            src += 2 * kv_row;
             const float4 f = __ldcg(src), g = __ldcg(src + 1);
             a.x += f.x; a.y += f.y; a.z += f.z; a.w += f.w;
             b.x += g.x; b.y += g.y; b.z += g.z; b.w += g.w;
@@ -1123,19 +1126,19 @@ int attn_packed_bwd_launch(const void* q, const void* k, const void* v, const vo
         R.dq_acc = reinterpret_cast<float4*>(base + w.dq_acc);
         R.plan = P.plan; R.ticket = P.status + kWsTicketBwd;
         R.Hq = c.Hq; R.D = c.D; R.rows = w.rows;
-        const long long slices = tiles * ((kTile * c.Hq * 8ll + 1023) / 1024), places = 8ll * sm_count();
+        const long long slices = tiles * ((kTile * c.Hq * (c.D / 8ll) + 1023) / 1024), places = 8ll * sm_count();
         LaunchScope ls_(K_PACKED_PREP, stream);
         if (int st = check_cuda(launch_chained(packed_prep_kernel, dim3(static_cast<unsigned>(slices < places ? slices : places)), dim3(256), 0, stream, R), "packed attention: backward prep launch")) return st;
     }
     CUtensorMap mq, mk, mv, mdo, macc, mparts{};
     if (P.may_split) {
-        if (int st = packed_acc_map(&mparts, base + w.parts, w.rows, 2 * kMostParts * c.Hkv)) return st;
+        if (int st = packed_acc_map(&mparts, base + w.parts, w.rows, 2 * kMostParts * c.Hkv, c.D)) return st;
     }
     if (int st = packed_tile_map(&mq, q, c.D, c.Hq, c.T, L.sTq, L.sHq)) return st;
     if (int st = packed_tile_map(&mk, k, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
     if (int st = packed_tile_map(&mv, v, c.D, c.Hkv, c.T, L.sTkv, L.sHkv)) return st;
     if (int st = packed_tile_map(&mdo, d_o, c.D, c.Hq, c.T, HD, c.D)) return st;
-    if (int st = packed_acc_map(&macc, base + w.dq_acc, w.rows, c.Hq)) return st;
+    if (int st = packed_acc_map(&macc, base + w.dq_acc, w.rows, c.Hq, c.D)) return st;
     const long long worst = tiles * c.Hkv * (P.may_split ? kMostParts : 1);
     const int grid = static_cast<int>(worst < sm_count() ? worst : sm_count());          // one CTA per SM (all of tensor memory)
     {

@@ -169,9 +169,9 @@ int packed_tile_map(CUtensorMap* map, const void* base, int D, int H, int T, lon
     const cuuint32_t box[3] = {kDP, 1, kTile};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, dims, strides, box);
 }
-int packed_acc_map(CUtensorMap* map, const void* base, int rows, int H) {
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(kDP), static_cast<cuuint64_t>(H), static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[2] = {kDP * 4ull, static_cast<cuuint64_t>(H) * kDP * 4};
+int packed_acc_map(CUtensorMap* map, const void* base, int rows, int H, int D) {
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(H), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[2] = {D * 4ull, static_cast<cuuint64_t>(H) * D * 4};
     const cuuint32_t box[3] = {32, 1, kTile};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, base, dims, strides, box);
 }
