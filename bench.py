@@ -373,6 +373,64 @@ def pearson_leg(torch, vd, path, w, peaks, barrier, args):
     return res
 
 
+def layer_leg(torch, vd, path, w, peaks, barrier, args):
+    """Times what an encoder layer on kept tokens and the end of its training step have the library do around the projections: the norms of the residual stream with a gate per
+    instance (gathered by the selection), attention over the kept sets packed one behind the other, both with their backward passes, and the clipping of the attention's
+    gradients.  Every instance is hashed and sampled on its own, so that the sets differ in size."""
+    device = path.dev[0]["x"].device
+    B, N, H, D, C = w.B, w.N, w.H, w.D, w.H * w.D
+    bf, f32 = dict(dtype=torch.bfloat16, device=device), dict(dtype=torch.float32, device=device)
+    hcfg, scfg = vd.HashCfg(B, N, w.L, w.k, 0, 0, 1), vd.SelectCfg(B, N, 0, w.rate, SEED, STEP0)
+    keys, freqs, _ = vd.alloc_hash_outputs(hcfg, device=device)
+    sel = vd.alloc_select_outputs(scfg, device=device)
+    vd.vardrop_hash(path.dev[0]["x"], hcfg, keys, freqs, None, vd.alloc_ws(vd.vardrop_hash_workspace_bytes(hcfg), device))
+    vd.vardrop_select(keys, scfg, *(sel[n] for n in ("group_id", "group_offsets", "members", "n_groups", "sel_idx", "n_sel", "inv_idx")),
+                      vd.alloc_ws(vd.vardrop_select_workspace_bytes(scfg), device))
+    cu = torch.zeros(B + 1, dtype=torch.int32, device=device)
+    cu[1:] = torch.cumsum(sel["n_sel"], 0)
+    T = int(cu[-1].item())
+    g = torch.Generator(device=device)
+    g.manual_seed(SEED)
+    rand = lambda *shape, **kw: torch.randn(shape, generator=g, device=device).to(kw.get("dtype", torch.bfloat16))  # noqa: E731
+    x, y, d_h, d_u = (rand(B, N, C) for _ in range(4))
+    h, u, dx, dy = (torch.empty((B, N, C), **bf) for _ in range(4))
+    stats, gate, w_post, w_pre = torch.empty((B, N, 4), **f32), rand(B, C, dtype=torch.float32), rand(C, dtype=torch.float32), rand(C, dtype=torch.float32)
+    d_gate, d_post, d_pre = torch.empty_like(gate), torch.empty_like(w_post), torch.empty_like(w_pre)
+    ncfg = vd.NormCfg(B, N, C, vd.DTYPES[torch.bfloat16], vd.NORM_RMS, vd.NORM_RMS, B, B, 1.0, 1e-5)
+    nws = vd.alloc_ws(vd.vardrop_norm_workspace_bytes(ncfg), device)
+    q, k, v, d_o = (rand(T, H, D) for _ in range(4))
+    o, dq, dk, dv = (torch.empty((T, H, D), **bf) for _ in range(4))
+    lse = torch.empty((H, T), **f32)
+    pcfg = vd.PackedCfg(B, T, H, H, D, 0.0, 0, 0, 0, 0, 0)
+    plan, pws = vd.alloc_packed_plan(pcfg, device), vd.alloc_ws(vd.vardrop_attn_packed_workspace_bytes(pcfg), device)
+    norm, ccfg, cws = torch.empty(1, **f32), vd.ClipCfg(1.0, 1e-6), vd.alloc_ws(vd.vardrop_grad_clip_workspace_bytes(), device)
+
+    def step(_):
+        vd.vardrop_norm_fwd(x, y, gate, w_post, None, w_pre, None, sel["sel_idx"], sel["n_sel"], ncfg, h, u, stats)
+        vd.vardrop_packed_plan(cu, pcfg, plan)
+        vd.vardrop_attn_packed_fwd(q, k, v, plan, pcfg, o, lse, pws)
+        vd.vardrop_attn_packed_bwd(q, k, v, o, lse, d_o, plan, pcfg, dq, dk, dv, pws)
+        vd.vardrop_norm_bwd(x, y, gate, w_post, None, w_pre, sel["sel_idx"], sel["n_sel"], sel["inv_idx"], stats, d_h, d_u, ncfg, dx, dy, d_gate, d_post, None, d_pre, None, nws)
+        vd.vardrop_grad_clip([dq, dk, dv], ccfg, None, norm, cws)
+
+    for i in range(3):
+        step(i)
+    n = max(3, min(args.steps, 20))
+    t = time_region(torch, step, n, barrier)
+    vd.vardrop_profile_enable(True)
+    for i in range(n):
+        step(i)
+    torch.cuda.synchronize()
+    per = {name: ms / cnt * 1e3 for name, (ms, cnt) in vd.vardrop_profile_read().items() if cnt}
+    vd.vardrop_profile_enable(False)
+    for ws in (nws, plan, pws, cws):
+        if vd.vardrop_ws_status(ws) != vd.OK:
+            raise RuntimeError("device status set by an operator of the layer")
+    pairs = int((sel["n_sel"].double() ** 2).sum().item()) * H
+    return {"ms_per_layer": t["median"], "kept_tokens": T, "attention_flops": 14 * D * pairs, "norm_bytes": (8 * T + B * N) * C * 2, "kernel_us": per,
+            "note": "kernel_us from a pass with the per-kernel event timer armed"}
+
+
 def per_launch(per_kernel):
     """{kernel: (total ms, launches)} -> the same with zero-launch kernels dropped."""
     return {k: v for k, v in per_kernel.items() if v[1] > 0}
@@ -500,6 +558,7 @@ def run_gpu(args):
     if not args.no_targets and rank == 0 and world == 1:
         targets = traffic_targets(torch, vd, inputs, dist_util, device, rank, peaks, barrier, w, path, kernels, off)
     pearson = pearson_leg(torch, vd, path, w, peaks, barrier, args) if args.pearson else None
+    layer = layer_leg(torch, vd, path, w, peaks, barrier, args) if args.layer else None
     path.check_status()
 
     ms, ms_mean, ms_e2e = dist_util.max_over_ranks([t_main["median"], t_main["mean"], t_e2e["median"]], dist, device)
@@ -539,6 +598,8 @@ def run_gpu(args):
     }
     if pearson is not None:
         line["pearson"] = pearson
+    if layer is not None:
+        line["layer"] = layer
     print(json.dumps(line))
     if dist is not None:
         dist.destroy_process_group()
@@ -654,6 +715,7 @@ def main():
     ap.add_argument("--single-pass", action="store_true", help="one pass of K steps per timed region, no repetition (for ncu captures)")
     ap.add_argument("--no-targets", action="store_true", help="skip the short Traffic-shaped pass behind the `targets` block")
     ap.add_argument("--pearson", action="store_true", help="also time the variate-redundancy check (Appendix A, Eq. 4) on the workload's windows")
+    ap.add_argument("--layer", action="store_true", help="also time the operators around the attention: packed attention, norms, gradient clipping, on the workload's kept tokens")
     args = ap.parse_args()
     if args.warmup < 3:
         args.warmup = 3
