@@ -295,8 +295,8 @@ int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* m
  * The plan of a batch says where its sequences are and in which order their tiles are worked off.  It is made once from the offsets, on
  * the device, and serves every call on that batch (all layers, forward and backward, any number of them at a time: calls only read it).
  *
- * cfg (host)  n_seqs >= 1; T >= 1 rows of the packed tensors (at most 2^24); Hq a multiple of Hkv; D = 32 or 64; sm_scale (0 selects 1/sqrt(D));
- *             causal 0 or 1; element strides of q (sTq of a token, sHq of a head) and of both k and v (sTkv, sHkv), the head
+ * cfg (host)  n_seqs >= 1; T >= 1 rows of the packed tensors (at most 2^24); Hq a multiple of Hkv; D = 32 or 64; sm_scale up to 1e30 (0 selects
+ *             1/sqrt(D)); causal 0 or 1; element strides of q (sTq of a token, sHq of a head) and of both k and v (sTkv, sHkv), the head
  *             dimension contiguous; the two of a tensor both 0 select the contiguous layout, otherwise each must be a multiple of 8 with sT >= sH >= D (views of
  *             a fused projection [T, Hq + 2 Hkv, D]).  o, lse, d_o, dq, dk, dv are always contiguous.
  * cu_seqlens  [n_seqs + 1] int32: row of each sequence's first token, then the row behind the last one's last; 0 <= cu_seqlens[0], not decreasing (an empty
@@ -374,7 +374,8 @@ int vardrop_norm_bwd(const void* x, const void* y, const float* gate, const floa
  * Sums in fp64, in a fixed order (bit-reproducible; two neighbouring squares are added in fp32 where that leaves no range); products rounded once to the tensor's type.
  *
  * tensors     (host) [count] of device pointers, element counts (>= 0) and types (0 bf16, 1 fp16, 2 fp32); read before the call returns.  `in` and `out` need the
- *             alignment of their element only; out = in clips in place, otherwise they must not overlap, nor any two outputs.
+ *             alignment of their element only; out = in clips in place; otherwise no output may overlap another
+ *             one or any tensor's `in`.
  *             count <= 16384.
  * cfg (host)  max_norm: 0 takes the norm only (no `out` is touched); eps >= 0.
  * norm        [1] fp32 out.

@@ -279,30 +279,38 @@ int fill(ClipTable<kMax>& P, const vardrop_tensor* tensors, int at, int count) {
     P.first[P.count] = static_cast<int>(chunks);
     return VARDROP_OK;
 }
-// Two outputs that overlap would be scaled by two CTAs at a time.  Tensors mostly come in the order of their addresses, where a look at neighbours is enough.
+// An output may overlap neither another one, which two CTAs would scale at a time, nor another tensor's input, which is read ahead of it or behind.  Tensors that are clipped in place
+// mostly come in the order of their addresses, where a look at neighbours is enough.
 int outputs_apart(const vardrop_tensor* tensors, int count) {
-    struct Span { uintptr_t begin, end; };
-    const auto span = [&](int i) {
-        const uintptr_t p = reinterpret_cast<uintptr_t>(tensors[i].out);
-        return Span{p, p + (static_cast<uintptr_t>(tensors[i].n) << (tensors[i].dtype == 2 ? 2 : 1))};
+    struct Span { uintptr_t begin, end; bool written; };
+    const auto span = [&](int i, const void* p, bool written) {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(p);
+        return Span{begin, begin + (static_cast<uintptr_t>(tensors[i].n) << (tensors[i].dtype == 2 ? 2 : 1)), written};
     };
     uintptr_t last = 0;
     bool ascending = true;
     for (int i = 0; i < count && ascending; ++i) {
         if (tensors[i].n == 0) continue;
-        const Span s = span(i);
-        ascending = s.begin >= last;
+        const Span s = span(i, tensors[i].out, true);
+        ascending = tensors[i].in == tensors[i].out && s.begin >= last;
         last = s.end;
     }
     if (ascending) return VARDROP_OK;
-    const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[count]);
+    const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[2 * static_cast<size_t>(count)]);
     if (!spans) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: no host memory for %d tensors", count);
     int n = 0;
-    for (int i = 0; i < count; ++i)
-        if (tensors[i].n > 0) spans[n++] = span(i);
+    for (int i = 0; i < count; ++i) {
+        if (tensors[i].n == 0) continue;
+        spans[n++] = span(i, tensors[i].out, true);
+        if (tensors[i].in != tensors[i].out) spans[n++] = span(i, tensors[i].in, false);
+    }
     std::sort(spans.get(), spans.get() + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
-    for (int i = 1; i < n; ++i)
-        if (spans[i].begin < spans[i - 1].end) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: two outputs overlap");
+    uintptr_t written = 0, read = 0;                     // ends of the spans so far
+    for (int i = 0; i < n; ++i) {
+        const Span& s = spans[i];
+        if (s.begin < written || (s.written && s.begin < read)) return fail(VARDROP_ERR_INVALID_ARG, "grad_clip: an output overlaps another output or another tensor's input");
+        (s.written ? written : read) = std::max(s.written ? written : read, s.end);
+    }
     return VARDROP_OK;
 }
 int grid_of(int chunks) {

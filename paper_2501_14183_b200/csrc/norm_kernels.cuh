@@ -284,7 +284,7 @@ struct Run {
     long long begin;                     // tokens ahead of that instance
 };
 // Tokens of an instance, and the run of a CTA; every thread of the block calls it.  Kept counts of their own are summed up 256 at a time, by every CTA for itself.
-__device__ __forceinline__ int tokens_of(const NormParams& P, int b) { return P.n_sel ? __ldg(P.n_sel + (P.S > 1 ? b : 0)) : P.N; }
+__device__ __forceinline__ int tokens_of(const NormParams& P, int b) { return P.n_sel ? max(0, min(P.N, __ldg(P.n_sel + (P.S > 1 ? b : 0)))) : P.N; }
 __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) {       // s_scan[blockDim / 32 + 2]
     Run r{0, 0, 0, 0, 0};
     const int G = gridDim.x, c = blockIdx.x;

@@ -184,7 +184,7 @@ int packed_validate(const vardrop_packed_cfg& c) {
     if (c.Hq > 4096) return fail(VARDROP_ERR_UNSUPPORTED, "packed attention: Hq=%d above 4096", c.Hq);
     if (packed_tiles(c) * kTile >= (1ll << 31) || packed_tiles(c) * c.Hq >= (1ll << 31)) return fail(VARDROP_ERR_UNSUPPORTED, "packed attention: too many tiles of T=%d n_seqs=%d Hq=%d", c.T, c.n_seqs, c.Hq);
     if (c.causal != 0 && c.causal != 1) return fail(VARDROP_ERR_INVALID_ARG, "packed attention: causal=%d must be 0 or 1", c.causal);
-    if (!(c.sm_scale >= 0.f) || c.sm_scale > 3.0e38f) return fail(VARDROP_ERR_INVALID_ARG, "packed attention: sm_scale must be finite and >= 0 (0 selects 1/sqrt(D))");
+    if (!(c.sm_scale >= 0.f) || c.sm_scale > 1e30f) return fail(VARDROP_ERR_INVALID_ARG, "packed attention: sm_scale must be >= 0 (0 selects 1/sqrt(D)) and at most 1e30");
     const PackedStrides s = packed_strides(c);
     const int64_t pairs[2][2] = {{s.sTq, s.sHq}, {s.sTkv, s.sHkv}};
     for (const auto& p : pairs) {

@@ -1,5 +1,8 @@
 """Argument checks of the operators around the attention: they run ahead of any CUDA call, on a machine without a GPU too."""
 import ctypes as C
+import os
+import re
+import subprocess
 
 import pytest
 
@@ -71,7 +74,10 @@ def test_clip_arguments(lib):
     assert call(ok, max_norm=-1.0) == call(ok, max_norm=float("nan")) == call(ok, eps=-1.0) == call(ok, norm=None) == call(ok, count=-1) == vd.ERR_INVALID_ARG
     assert call(*[ok] * 16385) == vd.ERR_UNSUPPORTED
     apart = [(GOOD + 64 * i, GOOD + 64 * i, 16, 2) for i in range(40)]
-    assert call(*apart, ok) == call(*apart[::-1], (GOOD + 60, GOOD + 60, 2, 0)) == call(ok, ok) == vd.ERR_INVALID_ARG and b"two outputs" in lib.vardrop_last_error()
+    assert call(*apart, ok) == call(*apart[::-1], (GOOD + 60, GOOD + 60, 2, 0)) == call(ok, ok) == vd.ERR_INVALID_ARG and b"overlaps another" in lib.vardrop_last_error()
+    far = 1 << 20                       # one tensor's output on another's input; inputs may be the same
+    assert call((GOOD, far, 16, 2), (far + 64, GOOD + 60, 16, 2)) == vd.ERR_INVALID_ARG and b"another tensor's input" in lib.vardrop_last_error()
+    assert call((GOOD, far, 16, 2), (GOOD, far, 16, 2)) == vd.ERR_INVALID_ARG
     assert call(ok, nb=need - 1) == vd.ERR_WORKSPACE
 
 
@@ -81,7 +87,7 @@ def packed_cfg(**kw):
 
 @pytest.mark.parametrize("kw,status", [(dict(n_seqs=0), 1), (dict(T=0), 1), (dict(Hq=0), 1), (dict(Hkv=0), 1), (dict(Hq=5), 1), (dict(D=128), 2), (dict(D=48), 2), (dict(T=(1 << 24) + 1), 2),
                                        (dict(n_seqs=(1 << 24) + 1), 2), (dict(Hq=8192), 2), (dict(T=1 << 24, n_seqs=1 << 24), 2), (dict(causal=2), 1), (dict(sm_scale=-1.0), 1),
-                                       (dict(sm_scale=float("nan")), 1), (dict(sm_scale=float("inf")), 1), (dict(sTq=256), 1), (dict(sTq=260, sHq=64), 1), (dict(sTkv=32, sHkv=64), 1),
+                                       (dict(sm_scale=float("nan")), 1), (dict(sm_scale=float("inf")), 1), (dict(sm_scale=2e30), 1), (dict(sTq=256), 1), (dict(sTq=260, sHq=64), 1), (dict(sTkv=32, sHkv=64), 1),
                                        (dict(sTq=256, sHq=60), 1), (dict(sTq=-256, sHq=64), 1), (dict(sTkv=1 << 40, sHkv=64), 2)])
 def test_packed_configurations(lib, kw, status):
     cfg = packed_cfg(**kw)
@@ -117,3 +123,112 @@ def test_struct_layouts_match_header():
     assert C.sizeof(vd.PackedCfg) == 64 and vd.PackedCfg.sTq.offset == 32
     assert C.sizeof(vd.NormCfg) == 40 and vd.NormCfg.res_scale.offset == 32
     assert C.sizeof(vd.ClipCfg) == 8 and C.sizeof(Tensor) == 32
+
+
+# What the branch of attn_packed_bwd_kernel that takes results out needs around it to run on the host, a thread a warp: waits that succeed but for one, and a named barrier that says when
+# not all four come.
+HOST_WARPGROUP = r"""
+#include <chrono>
+#include <condition_variable>
+#include <cstdint>
+#include <mutex>
+#include <thread>
+struct uint4 { uint32_t x, y, z, w; };
+struct float4 { float x, y, z, w; };
+typedef uint16_t __nv_bfloat16;
+struct Item { int start, len, jt, kvh, base, steps, per, s0; };
+struct Params { __nv_bfloat16 *dk, *dv; int T, Hq, Hkv, group, D; float scale; } P;
+const int kTile = 128, kRowBytes = 128, kTileBytes = 16384, kMostParts = 4;
+const uint32_t kColDq = 0, kColDv = 0, kColDk = 0;
+alignas(16) unsigned char sOut[2 * 16384];
+int map_acc, map_parts;
+Item items[6];
+std::mutex m;
+std::condition_variable cv;
+int arrived, gone, phase, waits[4], fail_warp, fail_at;
+bool all_ok, result, hung;
+thread_local int me;
+bool group_sync_and(int, bool ok) {
+    std::unique_lock<std::mutex> l(m);
+    if (arrived == 0) all_ok = true;
+    all_ok = all_ok && ok;
+    const int p = phase;
+    if (++arrived == 4) { arrived = 0; result = all_ok; ++phase; cv.notify_all(); return result; }
+    if (!cv.wait_for(l, std::chrono::seconds(5), [&] { return phase != p || gone > 0; }) || phase == p) { hung = true; return false; }
+    return result;
+}
+bool warp_wait_relaxed(uint64_t*, uint32_t) { return !(me == fail_warp && waits[me]++ == fail_at); }
+int small_div(int a, int d) { return a / d; }
+uint32_t pack2(float, float) { return 0; }
+uint4 make_uint4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return {a, b, c, d}; }
+float4 make_float4(float a, float b, float c, float d) { return {a, b, c, d}; }
+template <class... A> void nothing(A&&...) {}
+#define bulk_wait_group_read0 nothing
+#define bulk_wait_group0 nothing
+#define bulk_commit_group nothing
+#define tma_reduce_add_3d nothing
+#define tma_store_3d nothing
+#define tc_fence_after nothing
+#define tc_fence_before nothing
+#define tmem_ld32(at, v) for (float& e : v) e = 0.f
+#define tmem_ld_wait nothing
+#define fence_proxy_async_smem nothing
+void role(int warp, bool& left_ok) {
+    const int lane = 0, tid = warp * 32;
+    uint32_t tmem = 0;
+    bool ok = true;
+    uint64_t bars[64];
+    uint64_t *bar_dv_done = bars, *bar_dv_free = bars, *bar_dk_done = bars, *bar_dk_free = bars, *bar_g = bars, *bar_gfree = bars;
+    auto begin = [] {};
+    auto item_wait = [&](uint32_t) { ok &= warp_wait_relaxed(bars, 0); };
+    auto item_read = [&](uint32_t i) { return items[i]; };
+    auto warp_arrive = [](uint64_t*) {};
+    me = warp & 3;
+BODY
+    left_ok = ok;
+    std::lock_guard<std::mutex> l(m);
+    ++gone;
+    cv.notify_all();
+}
+// number of waits of the warp; -1: a barrier that not all four reach, -2: a warp that leaves without having learnt of the wait that gave up
+extern "C" int run(int group, int failing, int at) {
+    static __nv_bfloat16 data[512 * 2 * 64];
+    P = Params{data, data, 512, 4, 2, 2, 64, 1.f};
+    const Item list[6] = {{0, 300, 0, 0, 0, 6, 3, 0}, {0, 300, 1, 1, 0, 4, 2, 0}, {0, 300, 0, 4096, 0, 3, 3, 0}, {0, 300, 0, 8192, 0, 3, 3, 3}, {0, -1, 0, 0, 0, 0, 0, 0}, {0, -1, 0, 0, 0, 0, 0, 0}};
+    for (int i = 0; i < 6; ++i) items[i] = list[i];
+    arrived = gone = phase = 0; hung = false; fail_warp = failing; fail_at = at;
+    for (int& w : waits) w = 0;
+    bool ok[4];
+    std::thread t[4];
+    for (int w = 0; w < 4; ++w) t[w] = std::thread([=, &ok] { role(4 + 4 * group + w, ok[w]); });
+    for (auto& x : t) x.join();
+    if (hung) return -1;
+    const bool gave_up = waits[failing] > at;
+    for (bool o : ok) if (o == gave_up) return -2;
+    return waits[failing];
+}
+"""
+
+
+def test_warps_that_share_a_named_barrier_leave_together(tmp_path):
+    """Nothing bounds a named barrier.  Whichever wait of whichever warp gives up, whole items and parts of them among what is under way, all four warps learn of it and leave behind the same
+    barrier.  The text of their branch, run on the host with every wait failing in turn."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2501_14183_b200", "csrc", "attn_packed_bwd.cu")
+    text = re.sub(r"//[^\n]*|/\*.*?\*/", "", open(path).read(), flags=re.S)
+    body = text[text.index("attn_packed_bwd_kernel("):]
+    start = body.index("{", body.index("else if (warp < 12)")) + 1
+    depth, end = 1, start
+    while depth:
+        depth += {"{": 1, "}": -1}.get(body[end], 0)
+        end += 1
+    branch = re.sub(r"asm volatile[^\n]*", "", body[start:end - 1])
+    assert "setmaxnreg" not in branch and branch.count("group_sync_and") >= 3
+    (tmp_path / "role.cpp").write_text(HOST_WARPGROUP.replace("BODY", branch))
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-w", "-shared", "-fPIC", "-pthread", "-o", str(tmp_path / "role.so"), str(tmp_path / "role.cpp")])
+    lib = C.CDLL(str(tmp_path / "role.so"))
+    for group in (0, 1):
+        for warp in range(4):
+            waits = lib.run(group, warp, 1 << 30)
+            assert waits >= 5 + 16 + 4, "items, query tiles, finished items"
+            got = [lib.run(group, warp, at) for at in range(waits)]
+            assert min(got) > 0, (group, warp, got)
