@@ -30,7 +30,7 @@ struct NormParams {
 //   kFlat   neither a selection nor a gate tells instances apart: all tokens, by turns
 //   kSplit  as many kept tokens in every instance: the same number of CTAs each, which take its tokens by turns
 //   kRuns   as many as each instance keeps, one behind the other, in equal runs to the CTAs (7 x 4459 x 544 with 529 to 3195 kept took 108 us with CTAs per instance, 84 like this;
-//           where turns can do it, they are the better: runs make 65536 x 1024, forward and backward, 262 us instead of 233)
+//           where turns can do it, they are the better: runs make 65536 x 1024, forward and backward, 245 us instead of 234, a call of one instance 4.3 instead of 3.2)
 enum NormShare { kFlat, kSplit, kRuns };
 
 inline int group_of(int C, int per) {

@@ -206,7 +206,7 @@ constexpr int kNormThreads = kGroup < 256 ? 256 : kGroup;        // of a CTA
 
 // Rows on their way from memory: a ring in shared memory whose places belong to one thread each, filled by asynchronous copies of the thread's own columns, so
 // that a group has kStages - 1 rows in flight while it works on one, without registers for them and without barriers.  (Loads into registers behind the row before: 65536 x
-// 1024 bf16 forward 188 us, backward 367; like this 118 and 166, bound by the instructions of scalar arithmetic.)  Columns of two bytes, which those copies cannot take, are
+// 1024 bf16 forward 188 us, backward 367; like this 118 and 166, bound by the instructions of scalar arithmetic; with pairs 92 and 148.)  Columns of two bytes, which those copies cannot take, are
 // loaded when they are needed.
 template <class T, int kV, int kGroup, int kPer, int kTensors>
 struct Ring {
