@@ -143,6 +143,18 @@ def test_transposed_gradients():
         clip([g[:, :64]], 1.0)
 
 
+def test_offsets_beyond_32_bits():
+    """2.2e9 values of one tensor, zeros but for some behind the 2^31st."""
+    n = 2_200_000_007
+    big = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([5, 2 ** 31 - 1, 2 ** 31, 2 ** 31 + 12345, n - 1], device="cuda")
+    big[at] = 2.0
+    norm, status = clip([big], 1.0)
+    assert status == vd.OK and abs(norm - math.sqrt(20)) < 1e-5
+    want = (2.0 * torch.tensor(1 / (math.sqrt(20) + 1e-6))).bfloat16().cuda()
+    assert bool((big[at] == want).all()) and int(torch.count_nonzero(big)) == 5
+
+
 def test_refusals():
     g = torch.randn(64, device="cuda")
     for grads, outs in (([g.double()], None), ([g.cpu()], None), ([1.0], None), ([g], [g.bfloat16()]), ([g], [g[:63]]), ([g], []), ([g.view(8, 8)], [g.view(8, 8).t()])):

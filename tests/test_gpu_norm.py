@@ -290,6 +290,39 @@ def test_captured_and_replayed_and_on_another_stream():
         assert t is None or torch.equal(t, out[n]), n
 
 
+def test_offsets_beyond_32_bits():
+    """270000 rows of 8192: what the last ones give is what they give alone, bit for bit."""
+    N, C, last = 270000, 8192, 33
+    small = Case(1, last, C, torch.bfloat16, 1, 0, 0, with_y=False, seed=4)
+    want = small.run()
+    big = lambda: torch.empty((1, N, C), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    x, u, d_u, dx = big(), big(), big(), big()
+    x.fill_(1.0)
+    d_u.zero_()
+    x[0, N - last:], d_u[0, N - last:] = small.x[0], small.d_u[0]
+    cfg = vd.NormCfg(1, N, C, 0, 1, 0, 0, 0, 1.0, EPS)
+    stats = torch.empty((1, N, 4), device="cuda")
+    vd.vardrop_norm_fwd(x, None, None, None, None, small.w_pre, None, None, None, cfg, None, u, stats)
+    d_h = torch.zeros_like(x)
+    d_h[0, N - last:] = small.d_h[0]
+    ws = vd.alloc_ws(vd.vardrop_norm_workspace_bytes(cfg))
+    vd.vardrop_norm_bwd(x, None, None, None, None, small.w_pre, None, None, None, stats, d_h, d_u, cfg, dx, None, None, None, None, None, None, ws)
+    assert vd.ws_status(ws) == vd.OK
+    for t, n in ((u, "u"), (dx, "dx")):
+        assert torch.equal(t[0, N - last:], want[n][0]), n
+    assert torch.equal(stats[0, N - last:, 3], want["stats"][0, :, 3])
+
+
+def test_counts_outside_the_rows_are_taken_as_none_or_all():
+    """A count that no selection gives: nothing is written behind the rows that there are."""
+    for n, kept in ((-3, 0), (9, 9), (1 << 30, 9)):
+        c = Case(2, 9, 64, torch.float32, 1, 1, 1, kept=[9], seed=6)
+        c.n_sel.fill_(n)
+        c.kept = [kept] * 2
+        got = c.run()
+        assert bool((got["h"] == 7.0).all()) == (kept == 0) and bool(torch.isfinite(got["d_w_pre"]).all())
+
+
 def test_refusals():
     c = Case(2, 6, 40, torch.float32, 1, 1, 1, seed=14)
     h, u, st = torch.empty_like(c.x), torch.empty_like(c.x), torch.empty(2, 6, 4, device="cuda")

@@ -152,6 +152,32 @@ def test_scales(scale):
     Case([300, 77, 129], 2, 2, 64, 1, scale=scale, seed=2).check()
 
 
+@pytest.mark.parametrize("scale", [1e-40, 1e-30, 1e-6, 2.0])
+@pytest.mark.parametrize("lens", [[40], [300, 131]])
+def test_scales_far_from_one(scale, lens):
+    """Where the scores are next to nothing the exponents' -lse / scale has to stay finite.  A gradient below the least normal bf16 value has half of that value's step (2^-134)."""
+    c = Case(lens, 2, 1, 64, 1, scale=scale, seed=3)
+    if scale > 1e-38:
+        c.check()
+        return
+    out = c.run()
+    val, off, live = reference(c.q, c.k, c.v, c.d_o, c.spans, 1, scale)
+    for n in ("o", "lse", "dv"):
+        got = (out[n].t() if n == "lse" else out[n]).double()[live]
+        assert bool(((got - val[n][live]).abs() <= off[n][live] + 1e-6).all()), n
+    for n in ("dq", "dk"):
+        assert bool(torch.isfinite(out[n].double()[live]).all()) and float(out[n].double()[live].abs().max()) <= 1e-35, n
+
+
+def test_forward_with_a_header_for_a_workspace():
+    c = Case([300, 131, 1], 3, 1, 64, 1, seed=4)
+    want, out = c.run(), c.new()
+    ws = torch.full((512,), 0x7F, dtype=torch.uint8, device="cuda")
+    ws[:4] = 0
+    vd.vardrop_attn_packed_fwd(c.q, c.k, c.v, c.plan, c.cfg, out["o"], out["lse"], ws[:256])
+    assert vd.ws_status(ws) == vd.OK and torch.equal(out["o"], want["o"]) and torch.equal(out["lse"], want["lse"]) and bool((ws[256:] == 0x7F).all())
+
+
 def test_large_scores():
     """Scores in the hundreds: rows in which one key has all the weight, references that move by far more than a step."""
     Case([300, 77, 129, 600], 2, 1, 64, 1, std=5.0, seed=3).check()
