@@ -295,39 +295,48 @@ __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) { 
         r.to = K * (c + 1) / r.ctas;
     };
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    long long K = 0;
-    for (int pass = 0; pass < 2; ++pass) {               // the sum, then the instance in which the run begins
-        long long ahead = 0;
-        for (int b0 = 0; b0 < P.B; b0 += blockDim.x) {
-            const int b = b0 + threadIdx.x;
-            const int n = b < P.B ? tokens_of(P, b) : 0;
-            int x = n;
+    long long K = 0, ahead = 0;
+    int n = 0;                                           // of the instance looked at last, and the tokens ahead of it
+    auto scan = [&](int b, long long& all) {             // one instance a thread
+        n = b < P.B ? tokens_of(P, b) : 0;
+        int x = n;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            __syncthreads();
-            if (lane == 31) s_scan[warp] = x;
-            __syncthreads();
-            long long before = ahead, all = 0;
-            for (int w = 0; w < warps; ++w) {
-                if (w < warp) before += s_scan[w];
-                all += s_scan[w];
-            }
-            if (pass == 0) {
-                if (P.begin && c == 0 && b < P.B) P.begin[b] = static_cast<int>(before + x - n);
-            } else if (n > 0 && before + x - n <= r.from && r.from < before + x) {
-                s_scan[warps] = b;
-                s_scan[warps + 1] = before + x - n;
-            }
-            ahead += all;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
         }
-        if (pass == 0) {
-            K = ahead;
-            if (P.begin && c == 0 && threadIdx.x == 0) P.begin[P.B] = static_cast<int>(K);
-            share(K);
-            if (r.from >= r.to) return r;                // (the same for all threads)
+        __syncthreads();
+        if (lane == 31) s_scan[warp] = x;
+        __syncthreads();
+        ahead = all + x - n;
+        for (int w = 0; w < warps; ++w) {
+            const long long v = s_scan[w];
+            if (w < warp) ahead += v;
+            all += v;
+        }
+    };
+    auto find = [&](int b) {                             // the instance in which the run begins
+        if (n > 0 && ahead <= r.from && r.from < ahead + n) {
+            s_scan[warps] = b;
+            s_scan[warps + 1] = ahead;
+        }
+    };
+#pragma unroll 1
+    for (int b0 = 0; b0 < P.B; b0 += static_cast<int>(blockDim.x)) {
+        scan(b0 + threadIdx.x, K);
+        if (P.begin && c == 0 && b0 + static_cast<int>(threadIdx.x) < P.B) P.begin[b0 + threadIdx.x] = static_cast<int>(ahead);
+    }
+    if (P.begin && c == 0 && threadIdx.x == 0) P.begin[P.B] = static_cast<int>(K);
+    share(K);
+    if (r.from >= r.to) return r;                        // (the same for all threads)
+    if (P.B <= static_cast<int>(blockDim.x)) {
+        find(threadIdx.x);
+    } else {
+        long long all = 0;
+#pragma unroll 1
+        for (int b0 = 0; b0 < P.B; b0 += blockDim.x) {
+            scan(b0 + threadIdx.x, all);
+            find(b0 + threadIdx.x);
         }
     }
     __syncthreads();
