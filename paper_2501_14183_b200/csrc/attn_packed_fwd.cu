@@ -24,9 +24,16 @@ struct PackedFwdParams {
 // front of it (16 prompts of 1 to 1999 tokens, 16 heads: 70.0 us with, 64.9 without).
 __device__ __forceinline__ int few_begin(const PlanHead& head, const PackedFwdParams& P) { return head.many * ((P.Hq + 1) >> 1) >= P.grid ? head.tiles : head.many; }
 
+// Whether items are the key parts of single heads: where items of two heads would leave SMs idle; without a causal mask, whose rows of tiles are alike, where those parts all find an SM.
+// (8192 tokens, 2 heads: 122 -> 70 us; 4 causal sequences of 2048, 4 heads, 112 items: 40 -> 30.  16 of 1100, 2 heads, not causal, 144 items that find an SM each: 31 -> 33 as 288 parts.)
+__device__ __forceinline__ bool in_parts(const PlanHead& head, const PackedFwdParams& P) {
+    return P.causal ? head.many * ((P.Hq + 1) >> 1) < P.grid : head.many * P.Hq <= P.grid;
+}
+
 // An item is the same query tile of two neighbouring heads: under a causal mask both see the same keys, so neither waits for the other, and heads of one group share
-// the loads of K and V (others have K and V of their own, stage by stage in turn).  Roles of a CTA:
-//   warps 0, 1       issue the products of head 0, 1 of an item
+// the loads of K and V (others have K and V of their own, stage by stage in turn).  Where those are fewer than the SMs, an item is the query tile of one head, in the places of two: one
+// takes its key tiles 0, 2, ..., the other 1, 3, ..., and the two parts of O are joined on their way out.  Roles of a CTA:
+//   warps 0, 1       issue the products of head (or part) 0, 1 of an item
 //   warp 2           decodes the items; loads Q (double-buffered across items) and a four-stage ring of K/V tiles as boxes
 //   warp 3           V of a sequence's last tile as rows, zeros behind its end: P is zero there, but what lies there may be not finite, and zero times that is not zero.
 //                    (Rows of Q and K there only reach scores that nothing reads.)
@@ -141,15 +148,23 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
     bool ok = true;
     // Work items, decoded by the loader warp one ahead and passed to the other roles through shared memory.  Eight entries: the loads run at most two items ahead of the
     // products, these one of the rows leaving, so an entry has been read long before its place is taken again.
-    // Tile w of an item: query tile qt of head h + w.  n_act: heads that exist; -1 ends the list.  split: the two heads have key heads kvh and kvh + 1, otherwise both kvh.
-    struct alignas(16) Item { int start, len, qt, h, n_kv, n_act, split, kvh; };
+    // Tile w of an item: query tile qt of head h + w.  n_act: heads that exist; -1 ends the list.  mode: both heads have key head kvh; kTwoKv: kvh and kvh + 1; kParts: the parts of one head.
+    enum { kOneKv = 0, kTwoKv, kParts };
+    struct alignas(16) Item {
+        int start, len, qt, h, n_kv, n_act, mode, kvh;
+        __device__ __forceinline__ int stages() const { return mode == kTwoKv ? 2 * n_kv : n_kv; }         // of the K/V ring
+        __device__ __forceinline__ int per_step() const { return mode == kOneKv ? 1 : 2; }                 // of them, while either tile takes a step
+        __device__ __forceinline__ int first_stage(int w) const { return mode == kOneKv ? 0 : w; }
+        __device__ __forceinline__ int steps(int w) const { return mode == kParts ? (n_kv + 1 - w) >> 1 : n_kv; }
+        __device__ __forceinline__ int key_tile(int w, int j) const { return mode == kParts ? 2 * j + w : j; }
+    };
     Item* s_item = reinterpret_cast<Item*>(smem_dyn + 512);
     auto item_at = [&](uint32_t i) {
         Item it;
         ok &= warp_wait_relaxed(bar_item + (i & 7), (i >> 3) & 1);
         const int4* from = reinterpret_cast<const int4*>(s_item + (i & 7));
         const int4 x = from[0], y = from[1];
-        it.start = x.x; it.len = x.y; it.qt = x.z; it.h = x.w; it.n_kv = y.x; it.n_act = ok ? y.y : -1; it.split = y.z; it.kvh = y.w;
+        it.start = x.x; it.len = x.y; it.qt = x.z; it.h = x.w; it.n_kv = y.x; it.n_act = ok ? y.y : -1; it.mode = y.z; it.kvh = y.w;
         return it;
     };
     // The launch before this one is attn_packed_tile_kernel of the same call, which lets this one in once it has waited for whatever lies before: nothing that is read or
@@ -162,23 +177,24 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         // ---------------------------------------------------------------- loads ----------------------------------
         uint32_t stage_n = 0, n_done = 0;
         const PlanHead head = plan_head(P.plan);
-        const int pairs = (P.Hq + 1) >> 1;
-        const long long n_items = static_cast<long long>(few_begin(head, P)) * pairs;
+        const bool parts = in_parts(head, P);
+        const int per_tile = parts ? P.Hq : (P.Hq + 1) >> 1;
+        const long long n_items = static_cast<long long>(few_begin(head, P)) * per_tile;
         auto publish = [&](uint32_t i, long long k) {
             Item it{0, 0, 0, 0, 0, -1, 0, 0};
             if (k < n_items) {
-                const int e = static_cast<int>(k / pairs), hp = static_cast<int>(k - static_cast<long long>(e) * pairs);
+                const int e = static_cast<int>(k / per_tile), hp = static_cast<int>(k - static_cast<long long>(e) * per_tile);
                 const int4 x = __ldg(reinterpret_cast<const int4*>(P.plan.entries() + e));
-                it.start = x.x; it.len = x.y; it.qt = x.z; it.h = 2 * hp;
+                it.start = x.x; it.len = x.y; it.qt = x.z; it.h = parts ? hp : 2 * hp;
                 it.n_kv = P.causal ? it.qt + 1 : (it.len + kTile - 1) / kTile;
-                it.n_act = min(2, P.Hq - it.h);
+                it.n_act = parts ? 2 : min(2, P.Hq - it.h);
                 it.kvh = small_div(it.h, P.group);
-                it.split = it.n_act == 2 && small_div(it.h + 1, P.group) != it.kvh;
+                it.mode = parts ? kParts : it.n_act == 2 && small_div(it.h + 1, P.group) != it.kvh ? kTwoKv : kOneKv;
             }
             if (lane == 0) {
                 int4* to = reinterpret_cast<int4*>(s_item + (i & 7));
                 to[0] = make_int4(it.start, it.len, it.qt, it.h);
-                to[1] = make_int4(it.n_kv, it.n_act, it.split, it.kvh);
+                to[1] = make_int4(it.n_kv, it.n_act, it.mode, it.kvh);
                 mbar_arrive(bar_item + (i & 7));
             }
             __syncwarp();
@@ -193,16 +209,17 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             ok = warp_wait_relaxed(bar_q_free + qb, ((n_done >> 1) & 1) ^ 1);
             if (!ok) break;
             if (lane == 0) {
-                mbar_expect_tx(bar_q_full + qb, it.n_act * kTileBytes);
+                const int tiles = it.mode == kParts ? 1 : it.n_act;
+                mbar_expect_tx(bar_q_full + qb, tiles * kTileBytes);
 #pragma unroll 1
-                for (int w = 0; w < it.n_act; ++w)
+                for (int w = 0; w < tiles; ++w)
                     tma_load_3d(sQ + (qb * kFwdTiles + w) * kTileBytes, &map_q, bar_q_full + qb, 0, it.h + w, it.start + it.qt * kTile);
             }
             __syncwarp();
-            const int per_step = it.split ? 2 : 1;
+            const int heads = it.mode == kTwoKv ? 2 : 1;             // stages of a key tile
             int x = 0, j = 0;
 #pragma unroll 1
-            for (int l = 0; l < it.n_kv * per_step; ++l, ++stage_n) {
+            for (int l = 0; l < it.stages(); ++l, ++stage_n) {
                 const uint32_t st = stage_n % kFwdStages;
                 ok = warp_wait_relaxed(bar_kv_free + st, ((stage_n / kFwdStages) & 1) ^ 1);
                 if (!ok) break;
@@ -213,7 +230,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     if (whole) tma_load_3d(sK + (2 * st + 1) * kTileBytes, &map_v, bar_kv_full + st, 0, it.kvh + x, it.start + j * kTile);
                 }
                 __syncwarp();
-                if (++x == per_step) { x = 0; ++j; }
+                if (++x == heads) { x = 0; ++j; }
             }
             ++n_done;
             if (!ok) break;
@@ -233,10 +250,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         for (uint32_t i = 0; ok; ++i) {
             const Item it = item_at(i);
             if (it.n_act < 0) break;
-            const int per_step = it.split ? 2 : 1;
+            const int heads = it.mode == kTwoKv ? 2 : 1;             // stages of a key tile
             int x = 0, j = 0;
 #pragma unroll 1
-            for (int l = 0; l < it.n_kv * per_step; ++l, ++stage_n) {
+            for (int l = 0; l < it.stages(); ++l, ++stage_n) {
                 const uint32_t st = stage_n % kFwdStages;
                 ok = warp_wait_relaxed(bar_kv_free + st, ((stage_n / kFwdStages) & 1) ^ 1);
                 if (!ok) break;
@@ -248,7 +265,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     for (int g = 0; g < 4; ++g) copy_32_tokens(sK + (2 * st + 1) * kTileBytes + g * 32 * kRowBytes, from, P.sTkv, j * kTile + g * 32, it.len, P.D);
                     cp_async_arrive(bar_kv_full + st);
                 }
-                if (++x == per_step) { x = 0; ++j; }
+                if (++x == heads) { x = 0; ++j; }
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -307,42 +324,53 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
 #pragma unroll 1
         for (uint32_t i = 0; ok && it.n_act >= 0; ++i) {
             const uint32_t qb = n_done & 1;
-            const int per_step = it.split ? 2 : 1;                       // ring stages of a step
+            const int per_step = it.per_step(), stages = it.stages();
             Item next;
             if (w < it.n_act) {
-                const uint64_t a = umma_desc_advance(d_q, (qb * kFwdTiles + w) * kTileBytes);
-                const uint32_t mine = it.split ? w : 0;
-                uint32_t sn = stage_n + mine;
+                const uint64_t a = umma_desc_advance(d_q, (qb * kFwdTiles + (it.mode == kParts ? 0 : w)) * kTileBytes);
+                const int steps = it.steps(w);
+                uint32_t sn = stage_n + it.first_stage(w);
                 if (!primed) {
                     wait_full(bar_q_full + qb, (n_done >> 1) & 1, false);
                     wait_full(bar_kv_full + sn % kFwdStages, (sn / kFwdStages) & 1, it.len < kTile);
                     // The second head starts a softmax later than the first: in step, both heads' exponentials queue up and then both heads'
                     // hand-offs leave the special-function unit idle.  Not worth its delay for a few steps.  (On a barrier of one phase: bar_p may have gone two phases on
                     // by the time this warp's first stage has landed, and its third waits for a stage of the ring that this warp has yet to release.)
-                    if (i == 0 && w == 1 && it.n_kv >= 4) ok &= warp_wait_relaxed(bar_stagger, 0);
+                    if (i == 0 && w == 1 && steps >= 4) ok &= warp_wait_relaxed(bar_stagger, 0);
                     issue_scores(a, sn % kFwdStages, min(kTile, it.len));
-                    if (it.n_kv == 1) tc_commit_w(bar_q_free + qb);
+                    if (steps == 1) tc_commit_w(bar_q_free + qb);
                 }
                 primed = false;
+                int freed = 0;                                           // stages that this warp has released
+                auto release = [&](int to) {
 #pragma unroll 1
-                for (int j = 0; j < it.n_kv && ok; ++j, ++t) {
-                    if (j + 1 < it.n_kv) {               // the next S, as soon as the softmax warps hold this one
+                    for (; freed < to; ++freed) {
+                        const uint32_t so = stage_n + freed;
+                        ok &= warp_wait_relaxed(bar_kv_full + so % kFwdStages, (so / kFwdStages) & 1);
+                        tc_commit_w(bar_kv_free + so % kFwdStages);
+                    }
+                };
+#pragma unroll 1
+                for (int j = 0; j < steps && ok; ++j, ++t) {
+                    if (j + 1 < steps) {                 // the next S, as soon as the softmax warps hold this one
                         const uint32_t s1 = sn + per_step;
-                        wait_full(bar_kv_full + s1 % kFwdStages, (s1 / kFwdStages) & 1, it.len < (j + 2) * kTile);
+                        const int left = it.len - it.key_tile(w, j + 1) * kTile;
+                        wait_full(bar_kv_full + s1 % kFwdStages, (s1 / kFwdStages) & 1, left < kTile);
                         ok &= warp_wait_relaxed(bar_sfree + w, t & 1);
                         tc_fence_after();
-                        issue_scores(a, s1 % kFwdStages, min(kTile, it.len - (j + 1) * kTile));
-                        if (j + 2 == it.n_kv) tc_commit_w(bar_q_free + qb);
+                        issue_scores(a, s1 % kFwdStages, min(kTile, left));
+                        if (j + 2 == steps) tc_commit_w(bar_q_free + qb);
                     } else {
                         next = item_at(i + 1);
-                        if (w < next.n_act) {
-                            const uint32_t s1 = stage_n + it.n_kv * per_step + (next.split ? w : 0);
+                        const uint32_t s1 = stage_n + stages + next.first_stage(w);
+                        // (not with a stage that comes into the place of one that this warp has yet to release: the second part of an odd number of key tiles)
+                        if (w < next.n_act && s1 < stage_n + freed + kFwdStages) {
                             wait_full(bar_q_full + (qb ^ 1), ((n_done + 1) >> 1) & 1, false);
                             wait_full(bar_kv_full + s1 % kFwdStages, (s1 / kFwdStages) & 1, next.len < kTile);
                             ok &= warp_wait_relaxed(bar_sfree + w, t & 1);
                             tc_fence_after();
-                            issue_scores(umma_desc_advance(d_q, ((qb ^ 1) * kFwdTiles + w) * kTileBytes), s1 % kFwdStages, min(kTile, next.len));
-                            if (next.n_kv == 1) tc_commit_w(bar_q_free + (qb ^ 1));
+                            issue_scores(umma_desc_advance(d_q, ((qb ^ 1) * kFwdTiles + (next.mode == kParts ? 0 : w)) * kTileBytes), s1 % kFwdStages, min(kTile, next.len));
+                            if (next.steps(w) == 1) tc_commit_w(bar_q_free + (qb ^ 1));
                             primed = true;
                         }
                     }
@@ -350,15 +378,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     if (t == 0 && w == 0 && lane == 0) mbar_arrive(bar_stagger);
                     if (j == 0 && n_mine > 0) ok &= warp_wait_relaxed(bar_ofree + w, (n_mine - 1) & 1);     // O of the previous item has been read
                     tc_fence_after();
-                    issue_pv(sn % kFwdStages, min(kTile, it.len - j * kTile), j > 0);
-#pragma unroll 1
-                    for (int x = 0; x < per_step; ++x) {                 // this step's stages: mine is read by the products above
-                        const uint32_t so = stage_n + j * per_step + x;
-                        if (x != static_cast<int>(mine)) ok &= warp_wait_relaxed(bar_kv_full + so % kFwdStages, (so / kFwdStages) & 1);
-                        tc_commit_w(bar_kv_free + so % kFwdStages);
-                    }
+                    issue_pv(sn % kFwdStages, min(kTile, it.len - it.key_tile(w, j) * kTile), j > 0);
+                    release(min(stages, (j + 1) * per_step));            // this step's stages: mine is read by the products above
                     sn += per_step;
                 }
+                if (ok) release(stages);
                 ++n_mine;
             } else {                                     // nothing to compute in this item: keep up with its barriers
                 ok &= warp_wait_relaxed(bar_q_full + qb, (n_done >> 1) & 1);
@@ -366,14 +390,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 if (lane == 0) mbar_arrive(bar_skip + 1);
                 tc_commit_w(bar_q_free + qb);
 #pragma unroll 1
-                for (int l = 0; l < it.n_kv * per_step && ok; ++l) {
+                for (int l = 0; l < stages && ok; ++l) {
                     const uint32_t so = stage_n + l;
                     ok &= warp_wait_relaxed(bar_kv_full + so % kFwdStages, (so / kFwdStages) & 1);
                     tc_commit_w(bar_kv_free + so % kFwdStages);
                 }
                 next = item_at(i + 1);
             }
-            stage_n += it.n_kv * per_step;
+            stage_n += stages;
             ++n_done;
             it = next;
         }
@@ -390,16 +414,28 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         for (uint32_t i = 0; ok; ++i) {
             const Item it = item_at(i);
             if (it.n_act < 0) break;
+            const bool parts = it.mode == kParts;
 #pragma unroll 1
-            for (int w = 0; w < it.n_act; ++w) {
-                const uint32_t t_last = (w ? t1 : t0) + it.n_kv - 1, n_mine = w ? n1 : n0;
+            for (int w = 0; w < (parts ? 1 : it.n_act); ++w) {
                 unsigned char* stage = sOut;
-                ok &= warp_wait_relaxed(bar_l + w, n_mine & 1);
-                ok &= warp_wait(bar_pv + w, t_last & 1);
+#pragma unroll 1
+                for (int p = w; p <= (parts ? 1 : w); ++p) {
+                    ok &= warp_wait_relaxed(bar_l + p, (p ? n1 : n0) & 1);
+                    ok &= warp_wait(bar_pv + p, ((p ? t1 : t0) + it.steps(p) - 1) & 1);
+                }
                 if (!ok) break;
                 tc_fence_after();
-                const float m_ref = s_ref[w * kTile + r], l_sum = s_sum[2 * w * kTile + r] + s_sum[(2 * w + 1) * kTile + r];
-                const float inv_l = 1.f / l_sum;
+                float m_ref = s_ref[w * kTile + r], l_sum = s_sum[2 * w * kTile + r] + s_sum[(2 * w + 1) * kTile + r];
+                float mine = 1.f, other = 0.f;           // factors of the parts
+                if (parts) {                             // both against the larger reference
+                    const float m0 = m_ref, m1 = s_ref[kTile + r];
+                    m_ref = fmaxf(m0, m1);
+                    mine = fast_exp2(m0 - m_ref);
+                    other = fast_exp2(m1 - m_ref);
+                    l_sum = l_sum * mine + (s_sum[2 * kTile + r] + s_sum[3 * kTile + r]) * other;
+                    other *= 1.f / l_sum;
+                }
+                mine *= 1.f / l_sum;
                 const int row = it.qt * kTile + r;
                 unsigned char* rowp = stage + r * kRowBytes;
 #pragma unroll 1
@@ -408,12 +444,22 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     tmem_ld16(tmem + w * 256 + 192 + lane_sel + c16 * 16, ov);
                     tmem_ld_wait();
 #pragma unroll
+                    for (int d = 0; d < 16; ++d) ov[d] *= mine;
+                    if (parts) {
+                        float second[16];
+                        tmem_ld16(tmem + 256 + 192 + lane_sel + c16 * 16, second);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int d = 0; d < 16; ++d) ov[d] = fmaf(second[d], other, ov[d]);
+                    }
+#pragma unroll
                     for (int q = 0; q < 2; ++q)
                         *reinterpret_cast<uint4*>(rowp + (((c16 * 2 + q) ^ (r & 7)) << 4)) =
-                            make_uint4(pack_bf16(ov[8 * q + 0] * inv_l, ov[8 * q + 1] * inv_l), pack_bf16(ov[8 * q + 2] * inv_l, ov[8 * q + 3] * inv_l),
-                                       pack_bf16(ov[8 * q + 4] * inv_l, ov[8 * q + 5] * inv_l), pack_bf16(ov[8 * q + 6] * inv_l, ov[8 * q + 7] * inv_l));
+                            make_uint4(pack_bf16(ov[8 * q + 0], ov[8 * q + 1]), pack_bf16(ov[8 * q + 2], ov[8 * q + 3]),
+                                       pack_bf16(ov[8 * q + 4], ov[8 * q + 5]), pack_bf16(ov[8 * q + 6], ov[8 * q + 7]));
                 }
                 tc_fence_before();
+                if (parts) mbar_arrive(bar_ofree + 1);
                 mbar_arrive(bar_ofree + w);                  // O, maximum and sum are in registers or in the staging tile
                 if (row < it.len) P.lse[static_cast<size_t>(it.h + w) * P.T + it.start + row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
                 __syncwarp();
@@ -433,8 +479,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 }
                 __syncwarp();                                // its rows of the staging tile are free
             }
-            t0 += it.n_kv; ++n0;
-            if (it.n_act > 1) { t1 += it.n_kv; ++n1; }
+            t0 += it.steps(0); ++n0;
+            if (it.n_act > 1) { t1 += it.steps(1); ++n1; }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFwdSoftmaxRegs));
@@ -457,13 +503,15 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             }
             float m_ref = -INFINITY, l_run = 0.f;       // exponentials are taken against m_ref (log2 domain), which trails the running maximum
             bool s_ready = false;                       // a poll's answer takes a hundred cycles: polls go out ahead of where they are needed
+            // keys that this row sees from this half of a step on (may be none; never none of a row's first 64, so a row's reference is finite: parts are of three key tiles or more)
+            int valid = min(it.len, P.causal ? it.qt * kTile + r + 1 : it.len) - it.key_tile(w, 0) * kTile - half * 64;
+            const int stride = it.mode == kParts ? 2 * kTile : kTile;
+            bool first = true;
 #pragma unroll 1
-            for (int j = 0; j < it.n_kv; ++j, ++t) {
+            for (int steps = it.steps(w); steps > 0; --steps, ++t, valid -= stride) {
                 if (!__all_sync(0xffffffffu, s_ready)) ok = warp_wait(bar_s + w, t & 1);
                 if (!ok) break;
                 tc_fence_after();
-                // keys of this half that this row sees (may be none; never none of a row's first 64, so a row's reference is finite)
-                const int valid = min(it.len - j * kTile, P.causal && j == it.qt ? r + 1 : kTile) - half * 64;
                 float s[64];
                 tmem_ld32(tm_s, s);
                 tmem_ld32(tm_s + 32, s + 32);
@@ -492,7 +540,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 const bool pv_done = t == 0 || mbar_test(bar_pv + w, (t - 1) & 1);
                 tile_sync(w);
                 const float m_tile = fmaxf(m_mine, ex[(half ^ 1) * kTile]);
-                if (j == 0) {
+                if (first) {
+                    first = false;
                     m_ref = first_reference(ex[0], m_tile);
                 } else {
                     // O accumulates in tensor memory against m_ref.  It is rescaled only when a row's maximum has outgrown m_ref by
@@ -857,7 +906,7 @@ int attn_packed_fwd_launch(const void* q, const void* k, const void* v, const vo
         attr_dev = dev;
     }
     const long long tiles = packed_tiles(c), places = static_cast<long long>(kTileFwdPerSm) * sm_count();
-    const long long worst = tiles * ((c.Hq + 1) / 2);
+    const long long worst = tiles * c.Hq;
     const int grid = static_cast<int>(worst < sm_count() ? worst : sm_count());                 // one CTA per SM
     P.grid = grid;
     const dim3 tile_grid(static_cast<unsigned>(tiles * c.Hq < places ? tiles * c.Hq : places));

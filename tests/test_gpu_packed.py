@@ -147,6 +147,23 @@ def test_long_sequences(lens, Hq, Hkv, causal):
     Case(lens, Hq, Hkv, 64, causal, seed=1).check()
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv,D", [([1300], 1, 1, 64), ([900, 1500, 400], 1, 1, 32), ([385, 513, 641, 769, 897], 3, 3, 64), ([640, 1281], 4, 2, 32), ([384, 385, 512], 5, 1, 64), ([3333], 2, 2, 64),
+                                           ([300, 20, 1000, 257], 8, 2, 64), ([1100] * 16, 2, 1, 64), ([1100] * 17, 2, 1, 64)])
+@pytest.mark.parametrize("causal", [0, 1])
+def test_few_long_items(lens, Hq, Hkv, D, causal):
+    """Calls in which the query tiles of two heads are fewer than the SMs, with odd and even numbers of key tiles, and those around the line."""
+    Case(lens, Hq, Hkv, D, causal, seed=len(lens)).check()
+
+
+@pytest.mark.parametrize("late", [0, 1])
+def test_parts_of_far_apart_sizes(late):
+    """The keys of one of every two tiles have scores far above the others': one part of a row outweighs the other by more than fp32 holds."""
+    c = Case([900], 1, 1, 64, 0, seed=8)
+    for tile in range(8):
+        c.k[128 * tile:128 * (tile + 1)] *= 4.0 if tile % 2 == late else 0.01
+    c.check()
+
+
 @pytest.mark.parametrize("scale", [0.01, 0.3, 1.0])
 def test_scales(scale):
     Case([300, 77, 129], 2, 2, 64, 1, scale=scale, seed=2).check()
