@@ -290,7 +290,7 @@ int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* m
  * without padding (one selection per instance), windows of different lookbacks, causal along their steps.
  * Query head h reads key head h / (Hq / Hkv).  For token i of a sequence and its tokens j (causal: j <= i):
  *   S_ij = sm_scale q_i . k_j;   lse_i = log sum_j exp(S_ij);   o_i = sum_j exp(S_ij - lse_i) v_j
- * bf16 operands, fp32 accumulation and softmax, P rounded to bf16 before the second product.
+ * bf16 operands, fp32 accumulation and softmax, P rounded to bf16 before the second product; backward P and dS = P o (d_o V^T - d_o . o) before theirs.
  *
  * The plan of a batch says where its sequences are and in which order their tiles are worked off.  It is made once from the offsets, on
  * the device, and serves every call on that batch (all layers, forward and backward, any number of them at a time: calls only read it).

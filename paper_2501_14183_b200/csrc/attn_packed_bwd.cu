@@ -9,6 +9,9 @@
 // The roles, tensor memory and arithmetic of a step are those of bwd_many_kernel; what differs: tiles of sequences that end inside, heads that share their keys (their dK
 // and dV add up in tensor memory over the item), the diagonal of a causal call, and the accumulator in which every sequence begins a tile, so that what a last tile adds behind
 // its end (zeros, but zero times a key that is not finite) lies where nothing reads.
+//
+// P and dS are rounded to bf16, the operand type of the products that take them: half a step, 2^-8 of a value, as the outputs' own.  (dQ is then off by 0.0025 of its norm where rounding it alone
+// gives 0.0017; two bf16 terms a value would take those three of five products twice.)
 #include "attn_packed.cuh"
 
 namespace vardrop {

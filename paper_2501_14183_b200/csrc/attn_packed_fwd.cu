@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 int freed = 0;                                           // stages that this warp has released
                 auto release = [&](int to) {
 #pragma unroll 1
-                    for (; freed < to; ++freed) {
+                    for (; freed < to && ok; ++freed) {
                         const uint32_t so = stage_n + freed;
                         ok &= warp_wait_relaxed(bar_kv_full + so % kFwdStages, (so / kFwdStages) & 1);
                         tc_commit_w(bar_kv_free + so % kFwdStages);
