@@ -341,11 +341,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     if (steps == 1) tc_commit_w(bar_q_free + qb);
                 }
                 primed = false;
-                int freed = 0;                                           // stages that this warp has released
-                auto release = [&](int to) {
+                const uint32_t end = stage_n + stages;
+                auto release = [&](uint32_t so, uint32_t to) {           // ring stages of this item
 #pragma unroll 1
-                    for (; freed < to && ok; ++freed) {
-                        const uint32_t so = stage_n + freed;
+                    for (; so < to && ok; ++so) {
                         ok &= warp_wait_relaxed(bar_kv_full + so % kFwdStages, (so / kFwdStages) & 1);
                         tc_commit_w(bar_kv_free + so % kFwdStages);
                     }
@@ -362,9 +361,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                         if (j + 2 == steps) tc_commit_w(bar_q_free + qb);
                     } else {
                         next = item_at(i + 1);
-                        const uint32_t s1 = stage_n + stages + next.first_stage(w);
+                        const uint32_t s1 = end + next.first_stage(w);
                         // (not with a stage that comes into the place of one that this warp has yet to release: the second part of an odd number of key tiles)
-                        if (w < next.n_act && s1 < stage_n + freed + kFwdStages) {
+                        if (w < next.n_act && s1 < stage_n + kFwdStages) {
                             wait_full(bar_q_full + (qb ^ 1), ((n_done + 1) >> 1) & 1, false);
                             wait_full(bar_kv_full + s1 % kFwdStages, (s1 / kFwdStages) & 1, next.len < kTile);
                             ok &= warp_wait_relaxed(bar_sfree + w, t & 1);
@@ -379,10 +378,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     if (j == 0 && n_mine > 0) ok &= warp_wait_relaxed(bar_ofree + w, (n_mine - 1) & 1);     // O of the previous item has been read
                     tc_fence_after();
                     issue_pv(sn % kFwdStages, min(kTile, it.len - it.key_tile(w, j) * kTile), j > 0);
-                    release(min(stages, (j + 1) * per_step));            // this step's stages: mine is read by the products above
+                    release(stage_n, min(end, stage_n + per_step));      // this step's stages: mine is read by the products above
+                    stage_n += per_step;
                     sn += per_step;
                 }
-                if (ok) release(stages);
+                release(stage_n, end);
+                stage_n = end;
                 ++n_mine;
             } else {                                     // nothing to compute in this item: keep up with its barriers
                 ok &= warp_wait_relaxed(bar_q_full + qb, (n_done >> 1) & 1);
@@ -396,8 +397,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                     tc_commit_w(bar_kv_free + so % kFwdStages);
                 }
                 next = item_at(i + 1);
+                stage_n += stages;
             }
-            stage_n += stages;
             ++n_done;
             it = next;
         }
