@@ -537,8 +537,8 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
                 for (int p = 0; p < kPairs; ++p) s_cols[group][p * kGroup + t] = a[p];
                 __syncthreads();
                 if (group == 0) {
-#pragma unroll 1
-                    for (int g = 1; g < kGroups; ++g)
+#pragma unroll 4
+                    for (int g = 1; g < kGroups; ++g)            // (in this order; loads of several groups at a time)
 #pragma unroll
                         for (int p = 0; p < kPairs; ++p) a[p] = add2(a[p], s_cols[g][p * kGroup + t]);
                 }
