@@ -4,6 +4,7 @@
 //                          attn_fwd_kernel (many tiles), whose roles, tensor memory and softmax it shares; what differs stands below.
 // attn_packed_tile_kernel  tiles with at most two key tiles: 128-thread CTAs, four to an SM, a tile of a head each, as attn_fwd_tile_kernel.
 #include "attn_packed.cuh"
+#include "packed_items.h"
 
 namespace vardrop {
 
@@ -20,15 +21,7 @@ struct PackedFwdParams {
     int causal, grid;                  // CTAs of attn_packed_fwd_kernel
     float scale_log2;                  // sm_scale * log2(e)
 };
-// First of the tiles that attn_packed_tile_kernel takes: those with few key tiles, unless the others fill the SMs: then they are the fine ends of its work, and that kernel would stand in
-// front of it (16 prompts of 1 to 1999 tokens, 16 heads: 70.0 us with, 64.9 without).
-__device__ __forceinline__ int few_begin(const PlanHead& head, const PackedFwdParams& P) { return head.many * ((P.Hq + 1) >> 1) >= P.grid ? head.tiles : head.many; }
-
-// Whether items are the key parts of single heads: where items of two heads would leave SMs idle; without a causal mask, whose rows of tiles are alike, where those parts all find an SM.
-// (8192 tokens, 2 heads: 122 -> 70 us; 4 causal sequences of 2048, 4 heads, 112 items: 40 -> 30.  16 of 1100, 2 heads, not causal, 144 items that find an SM each: 31 -> 33 as 288 parts.)
-__device__ __forceinline__ bool in_parts(const PlanHead& head, const PackedFwdParams& P) {
-    return P.causal ? head.many * ((P.Hq + 1) >> 1) < P.grid : head.many * P.Hq <= P.grid;
-}
+__device__ __forceinline__ FwdTiles tiles_of(const PlanHead& head) { return FwdTiles{head.tiles, head.many}; }
 
 // An item is the same query tile of two neighbouring heads: under a causal mask both see the same keys, so neither waits for the other, and heads of one group share
 // the loads of K and V (others have K and V of their own, stage by stage in turn).  Where those are fewer than the SMs, an item is the query tile of one head, in the places of two: one
@@ -177,9 +170,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
         // ---------------------------------------------------------------- loads ----------------------------------
         uint32_t stage_n = 0, n_done = 0;
         const PlanHead head = plan_head(P.plan);
-        const bool parts = in_parts(head, P);
+        const bool parts = in_parts(tiles_of(head), P.Hq, P.causal, P.grid);
         const int per_tile = parts ? P.Hq : (P.Hq + 1) >> 1;
-        const long long n_items = static_cast<long long>(few_begin(head, P)) * per_tile;
+        const long long n_items = static_cast<long long>(few_begin(tiles_of(head), P.Hq, P.grid)) * per_tile;
         auto publish = [&](uint32_t i, long long k) {
             Item it{0, 0, 0, 0, 0, -1, 0, 0};
             if (k < n_items) {
@@ -504,7 +497,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             }
             float m_ref = -INFINITY, l_run = 0.f;       // exponentials are taken against m_ref (log2 domain), which trails the running maximum
             bool s_ready = false;                       // a poll's answer takes a hundred cycles: polls go out ahead of where they are needed
-            // keys that this row sees from this half of a step on (may be none; never none of a row's first 64, so a row's reference is finite: parts are of three key tiles or more)
+            // keys that this row sees from this half of a step on (may be none; never none of a row's first 64, so a row's reference is finite: tiles in parts have three key tiles or more)
             int valid = min(it.len, P.causal ? it.qt * kTile + r + 1 : it.len) - it.key_tile(w, 0) * kTile - half * 64;
             const int stride = it.mode == kParts ? 2 * kTile : kTile;
             bool first = true;
@@ -667,7 +660,7 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
     chain_release();
     const PlanHead head = plan_head(P.plan);
     if (!head.fits && blockIdx.x == 0 && tid == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
-    const int first = kAll ? 0 : few_begin(head, P), n_items = (head.tiles - first) * P.Hq;
+    const int first = kAll ? 0 : few_begin(tiles_of(head), P.Hq, P.grid), n_items = (head.tiles - first) * P.Hq;
     bool ok = true;
     uint32_t t = 0;                                     // key tiles of this CTA so far: parity of bar_s and bar_o
 

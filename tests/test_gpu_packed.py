@@ -155,6 +155,18 @@ def test_few_long_items(lens, Hq, Hkv, D, causal):
     Case(lens, Hq, Hkv, D, causal, seed=len(lens)).check()
 
 
+@pytest.mark.parametrize("more", [-1, 0, 1])
+@pytest.mark.parametrize("D,causal", [(64, 0), (32, 0), (64, 1)])
+def test_one_head_with_a_long_tile_for_every_sm(more, D, causal):
+    """One head, and as many tiles with more than two key tiles as SMs, one fewer and one more, beside sequences of one and two tiles."""
+    tiles = torch.cuda.get_device_properties(0).multi_processor_count + more
+    if causal:                       # four tiles of a sequence of six have more than two key tiles
+        lens = [768] * (tiles // 4) + ([256 + 128 * (tiles % 4)] if tiles % 4 else [])
+    else:
+        lens = [384] * (tiles // 3 - 1) + [384 + 128 * (tiles % 3)]
+    Case(lens + [100, 1, 0, 130, 256], 1, 1, D, causal, seed=tiles).check()
+
+
 @pytest.mark.parametrize("late", [0, 1])
 def test_parts_of_far_apart_sizes(late):
     """The keys of one of every two tiles have scores far above the others': one part of a row outweighs the other by more than fp32 holds."""
