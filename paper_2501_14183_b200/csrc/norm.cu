@@ -113,7 +113,7 @@ Shares shares(const vardrop_norm_cfg& c, bool selected, int per, int per_sm) {
     if (!selected && c.gate_rows <= 1) return Shares{kFlat, 0, at_most((all + groups - 1) / groups)};
     // a run is worked off instance by instance: CTAs for shorter runs where instances have few tokens (37 x 2 x 157 with one or two kept, forward and backward, 13.5 us instead of 25.6)
     if (selected && c.S > 1) return Shares{kRuns, 0, at_most((all + groups - 1) / groups + c.B)};
-    const long long most = (c.N + groups - 1) / groups, even = places / c.B;
+    const long long most = (static_cast<long long>(c.N) + groups - 1) / groups, even = places / c.B;
     const int splits = static_cast<int>(even < 1 ? 1 : even < most ? even : most);
     return Shares{kSplit, splits, at_most(static_cast<long long>(c.B) * splits)};
 }

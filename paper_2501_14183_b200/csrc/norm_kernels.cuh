@@ -10,6 +10,7 @@
 #include <cuda_fp16.h>
 
 #include "norm.h"
+#include "norm_walk.h"
 
 namespace vardrop {
 
@@ -297,8 +298,8 @@ __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) { 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     long long K = 0, ahead = 0;
     int n = 0;                                           // of the instance looked at last, and the tokens ahead of it
-    auto scan = [&](int b, long long& all) {             // one instance a thread
-        n = b < P.B ? tokens_of(P, b) : 0;
+    auto scan = [&](long long b, long long& all) {       // one instance a thread
+        n = b < P.B ? tokens_of(P, static_cast<int>(b)) : 0;
         int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -315,16 +316,16 @@ __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) { 
             all += v;
         }
     };
-    auto find = [&](int b) {                             // the instance in which the run begins
+    auto find = [&](long long b) {                           // the instance in which the run begins
         if (n > 0 && ahead <= r.from && r.from < ahead + n) {
             s_scan[warps] = b;
             s_scan[warps + 1] = ahead;
         }
     };
 #pragma unroll 1
-    for (int b0 = 0; b0 < P.B; b0 += static_cast<int>(blockDim.x)) {
+    for (long long b0 = 0; b0 < P.B; b0 += blockDim.x) {
         scan(b0 + threadIdx.x, K);
-        if (P.begin && c == 0 && b0 + static_cast<int>(threadIdx.x) < P.B) P.begin[b0 + threadIdx.x] = static_cast<int>(ahead);
+        if (P.begin && c == 0 && b0 + threadIdx.x < P.B) P.begin[b0 + threadIdx.x] = static_cast<int>(ahead);
     }
     if (P.begin && c == 0 && threadIdx.x == 0) P.begin[P.B] = static_cast<int>(K);
     share(K);
@@ -334,7 +335,7 @@ __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) { 
     } else {
         long long all = 0;
 #pragma unroll 1
-        for (int b0 = 0; b0 < P.B; b0 += blockDim.x) {
+        for (long long b0 = 0; b0 < P.B; b0 += blockDim.x) {
             scan(b0 + threadIdx.x, all);
             find(b0 + threadIdx.x);
         }
@@ -346,8 +347,9 @@ __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) { 
 }
 // The parts of a CTA's tokens that lie in one instance, one after another: tokens first, first + step, ... below n, for this group; `slot` is the place of the part's sums.
 struct Parts {
-    int b, first, n, step, slot, base_row;
-    int unit;
+    RowIndex first, n, step;
+    int b, slot, base_row;
+    RowIndex unit;                       // the next one of this CTA, ~0 behind the only one
     long long at, begin;
     Run run;
     __device__ __forceinline__ void start(const NormParams& P, long long* s_scan) {
@@ -361,32 +363,32 @@ struct Parts {
     }
     __device__ __forceinline__ bool next(const NormParams& P, int group, int groups) {
         if (P.share == kFlat) {
-            if (unit < 0) return false;
+            if (unit == ~0u) return false;
             b = base_row = 0;
             first = unit * groups + group;
             n = P.B * P.N;
             step = gridDim.x * groups;
-            slot = unit;
-            unit = -1;
+            slot = static_cast<int>(unit);
+            unit = ~0u;
             return true;
         }
         if (P.share == kSplit) {
-            if (unit >= P.B * P.splits) return false;
-            b = unit / P.splits;
+            if (unit >= static_cast<RowIndex>(P.B * P.splits)) return false;
+            b = static_cast<int>(unit) / P.splits;
             base_row = b * P.N;
-            first = (unit - b * P.splits) * groups + group;
+            first = (static_cast<int>(unit) - b * P.splits) * groups + group;
             n = tokens_of(P, 0);
             step = P.splits * groups;
-            slot = unit;
+            slot = static_cast<int>(unit);
             unit += gridDim.x;
             return true;
         }
         if (at >= run.to) return false;
-        b = unit++;
+        b = static_cast<int>(unit++);
         base_row = b * P.N;
         const int n_b = tokens_of(P, b);
-        first = static_cast<int>(at - begin) + group;
-        n = static_cast<int>(min(static_cast<long long>(n_b), run.to - begin));
+        first = static_cast<RowIndex>(at - begin) + group;
+        n = static_cast<RowIndex>(min(static_cast<long long>(n_b), run.to - begin));
         step = groups;
         slot = blockIdx.x + b;               // (a place of its own: from one such pair to the next the CTA or the instance goes up)
         begin += n_b;
@@ -395,10 +397,10 @@ struct Parts {
     }
 };
 // The source row of a selection is known one row ahead of its copies.
-struct RowWalk {
+struct RowWalk : RowSteps {
     const int32_t* sel;
-    int n, step;
-    __device__ __forceinline__ int source(int i) const { return sel ? (i < n ? __ldg(sel + i) : 0) : i; }
+    __device__ __forceinline__ RowWalk(const int32_t* s, const Parts& part) : RowSteps{part.n, part.step}, sel(s) {}
+    __device__ __forceinline__ RowIndex source(RowIndex i) const { return sel ? (there(i) ? __ldg(sel + i) : 0) : i; }
 };
 
 // ---- forward ----------------------------------------------------------------------------------------------------------------
@@ -426,8 +428,9 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
     part.start(P, s_scan);
 #pragma unroll 1
     while (part.next(P, group, kGroups)) {
-        const int b = part.b, first = part.first;
-        const RowWalk walk{P.sel_idx ? P.sel_idx + static_cast<size_t>(P.S > 1 ? b : 0) * P.N : nullptr, part.n, part.step};
+        const int b = part.b;
+        const RowIndex first = part.first;
+        const RowWalk walk(P.sel_idx ? P.sel_idx + static_cast<size_t>(P.S > 1 ? b : 0) * P.N : nullptr, part);
         const size_t base = part.base_row;
         // N_post's scale and bias with the gate in them: h = a x + w z + c
         typename R::Values w, c;
@@ -442,10 +445,10 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
                 if (kLayer) c[p] = mul2(c[p], g[p]);
             }
         }
-        int i = first, stage = 0, ahead = first;
-        int source = walk.source(ahead);
+        RowIndex i = first, ahead = first, source = walk.source(ahead);
+        int stage = 0;
         auto fetch = [&](int to) {
-            if (ahead < walk.n) {
+            if (walk.there(ahead)) {
                 ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
                 ring.fetch(to, 1, Y ? Y + (base + ahead) * P.C : nullptr, t, P.C);
             }
@@ -456,11 +459,11 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
 #pragma unroll
         for (int s = 0; s < kAhead; ++s) fetch(s);
         // Groups of less than a warp leave the loop together; one without a token works on a row without columns.
-        const int behind = kGroup < 32 ? static_cast<int>(threadIdx.x & 31) / kGroup : 0;
+        const RowIndex behind = kGroup < 32 ? (threadIdx.x & 31) / kGroup : 0;
 #pragma unroll 1
-        for (; i - behind < walk.n; i += walk.step) {
-            const int C = kGroup < 32 && i >= walk.n ? 0 : P.C;
-            const int from = Rows::kAsync ? 0 : walk.source(i);
+        for (; walk.goes_on(i, behind); i += walk.step) {
+            const int C = kGroup < 32 && !walk.there(i) ? 0 : P.C;
+            const RowIndex from = Rows::kAsync ? 0 : walk.source(i);
             fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
             ring.wait();
             const size_t row = (base + i) * P.C;
@@ -572,8 +575,9 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
     part.start(P, s_scan);
 #pragma unroll 1
     while (part.next(P, group, kGroups)) {
-        const int b = part.b, first = part.first;
-        const RowWalk walk{P.sel_idx ? P.sel_idx + static_cast<size_t>(P.S > 1 ? b : 0) * P.N : nullptr, part.n, part.step};
+        const int b = part.b;
+        const RowIndex first = part.first;
+        const RowWalk walk(P.sel_idx ? P.sel_idx + static_cast<size_t>(P.S > 1 ? b : 0) * P.N : nullptr, part);
         const size_t base = part.base_row;
         typename R::Values w, c;                         // N_post's scale and bias with the gate in them
         {
@@ -587,11 +591,12 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
                 if (kLayer) c[p] = mul2(c[p], g[p]);
             }
         }
-        const int behind = kGroup < 32 ? static_cast<int>(threadIdx.x & 31) / kGroup : 0;
-        int ahead = first, stage = 0, source = walk.source(first), from = source;
-        float4 st = first < walk.n ? __ldg(P.stats + base + first) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const RowIndex behind = kGroup < 32 ? (threadIdx.x & 31) / kGroup : 0;
+        RowIndex ahead = first, source = walk.source(first), from = source;
+        int stage = 0;
+        float4 st = walk.there(first) ? __ldg(P.stats + base + first) : make_float4(0.f, 0.f, 0.f, 0.f);
         auto fetch = [&](int to) {
-            if (ahead < walk.n) {
+            if (walk.there(ahead)) {
                 const size_t row = (base + ahead) * P.C;
                 ring.fetch(to, 0, X + (base + source) * P.C, t, P.C);
                 ring.fetch(to, 1, Y ? Y + row : nullptr, t, P.C);
@@ -605,12 +610,12 @@ __global__ void __launch_bounds__(kNormThreads<kGroup>, 512 / kNormThreads<kGrou
 #pragma unroll
         for (int s = 0; s < kAhead; ++s) fetch(s);
 #pragma unroll 1
-        for (int i = first; i - behind < walk.n; i += walk.step) {
-            const int C = kGroup < 32 && i >= walk.n ? 0 : P.C;
+        for (RowIndex i = first; walk.goes_on(i, behind); i += walk.step) {
+            const int C = kGroup < 32 && !walk.there(i) ? 0 : P.C;
             fetch(stage + kAhead < Rows::kStages ? stage + kAhead : stage + kAhead - Rows::kStages);
             // of the next row, ahead of the wait
-            const int from_next = walk.source(i + walk.step);
-            const float4 st_next = i + walk.step < walk.n ? __ldg(P.stats + base + i + walk.step) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const RowIndex from_next = walk.source(i + walk.step);
+            const float4 st_next = walk.there(i + walk.step) ? __ldg(P.stats + base + i + walk.step) : make_float4(0.f, 0.f, 0.f, 0.f);
             ring.wait();
             const size_t row = (base + i) * P.C;
             typename R::Values h, zy, d;

@@ -313,6 +313,23 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(stats[0, N - last:, 3], want["stats"][0, :, 3])
 
 
+@pytest.mark.parametrize("selected", [False, True])
+def test_as_many_rows_as_a_call_may_have(selected):
+    """2^31 - 1 tokens of one channel: the walk over them looks ahead past what 32 bits with a sign hold.  h = x / 2 and dx = d_h / 2 are exact."""
+    N = 2 ** 31 - 1
+    cfg = vd.NormCfg(1, N, 1, vd.DTYPES[torch.bfloat16], 0, 0, 0, 1 if selected else 0, 0.5, EPS)
+    x, d_h = (torch.empty((1, N, 1), dtype=torch.bfloat16, device="cuda").normal_() for _ in range(2))
+    h, dx = (torch.zeros_like(x) for _ in range(2))
+    every = torch.arange(N, dtype=torch.int32, device="cuda")[None] if selected else None
+    n_sel = torch.tensor([N], dtype=torch.int32, device="cuda") if selected else None
+    vd.vardrop_norm_fwd(x, None, None, None, None, None, None, every, n_sel, cfg, h, None, None)
+    stats, ws = torch.empty((1, N, 4), device="cuda"), vd.alloc_ws(vd.vardrop_norm_workspace_bytes(cfg))
+    vd.vardrop_norm_bwd(x, None, None, None, None, None, every, n_sel, every, stats, d_h, None, cfg, dx, None, None, None, None, None, None, ws)
+    for part in range(0, N, 1 << 28):
+        at = slice(part, part + (1 << 28))
+        assert torch.equal(h[:, at], x[:, at] / 2) and torch.equal(dx[:, at], d_h[:, at] / 2), part
+
+
 def test_counts_outside_the_rows_are_taken_as_none_or_all():
     """A count that no selection gives: nothing is written behind the rows that there are."""
     for n, kept in ((-3, 0), (9, 9), (1 << 30, 9)):
