@@ -308,6 +308,9 @@ int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* m
  * o           [T, Hq, D] bf16 out; lse [Hq, T] fp32 out.  Rows that belong to no sequence are left as they are, here and in dq, dk, dv.
  * d_o         [T, Hq, D] bf16, gradient of o.
  * dq          [T, Hq, D], dk and dv [T, Hkv, D] bf16 out (dk, dv summed over the query heads of a key head, in fp32).
+ *             Forward, a row's weights are those of its scores' differences however far from zero the scaled scores are (the scores themselves are fp32 sums).  Backward they come from
+ *             lse, whose 24 bits leave them open by about 2^-20 |lse| of themselves: with a finite |lse| above 2^16 the device status is VARDROP_ERR_UNSUPPORTED, and the gradients of
+ *             its sequence mean nothing.
  * ws          scratch of vardrop_attn_packed_workspace_bytes for the backward call; the forward call only needs its status word (256 bytes).  Nothing is kept
  *             in it from one call to the next.
  * dq is accumulated across key tiles by bulk fp32 reduce-adds that land in no fixed order once a sequence has more than two tiles of 128 tokens, so its low-order bits may

@@ -18,6 +18,10 @@ namespace vardrop {
 
 namespace {
 
+// P is exp(scaled score - lse), and lse comes with the 24 bits of fp32: from |lse| 2^-20 or so on that is what P is known to, 2^-4 of itself here.  Beyond, the call says so.
+constexpr float kMostLse = 65536.f;
+__device__ __forceinline__ bool lse_too_far(float lse) { return fabsf(lse) > kMostLse && fabsf(lse) < INFINITY; }
+
 struct PackedBwdParams {
     const __nv_bfloat16 *q, *k, *v, *d_o;   // rows of a sequence's last tile (the other loads go through the tensor maps)
     const float* lse;                 // [Hq, T]
@@ -139,7 +143,8 @@ __global__ void __launch_bounds__(kShortThreads, kShortPerSm) packed_short_kerne
                 }
             }
             const PackedRow at = kGrouped && heads > 1 && row < n_rows ? packed_row(row, len) : PackedRow{0, row};
-            const float lse2 = row < n_rows ? __ldg(P.lse + static_cast<size_t>(h + at.head) * P.T + start + at.token) * 1.4426950408889634f : 0.f;
+            const float lse = row < n_rows ? __ldg(P.lse + static_cast<size_t>(h + at.head) * P.T + start + at.token) : 0.f, lse2 = lse * 1.4426950408889634f;
+            if (lse_too_far(lse)) set_status(P.status, VARDROP_ERR_UNSUPPORTED);
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async_smem();
             tc_fence_before();
@@ -751,6 +756,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             __syncwarp();
         };
         uint32_t st = 0, ph = 0;
+        bool too_far = false;
         publish(0, static_cast<int>(blockIdx.x) < ctas ? static_cast<long long>(blockIdx.x) : n_items);
         Item next = item_at(0);
         if (next.len >= 0) load_kv(0, next);
@@ -792,6 +798,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
                     if (lane == 0) mbar_arrive(bar_q_full + st);
                 }
                 __syncwarp();
+                if (x == it.jt) {                        // one look at every query tile of a head
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) too_far |= lse_too_far(st_lse[e]);
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t l[3], d[3];
@@ -811,6 +821,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) attn_packed_bwd_kernel(const 
             next = item_at(i + 1);
             if (next.len >= 0) load_kv(i + 1, next);
         }
+        if (too_far) set_status(P.status, VARDROP_ERR_UNSUPPORTED);
     }
     } else if (warp < 12) {
         // ------------------------------------------------------------ dQ; dV, dK of an item -----------------------------

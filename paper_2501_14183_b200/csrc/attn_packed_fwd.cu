@@ -41,10 +41,19 @@ constexpr int kFwdSoftmaxRegs = 96;
 constexpr int kFwdOtherRegs = 48;
 constexpr int kFwdStages = 4;
 constexpr uint32_t kFwdTmemCols = 512;   // of a head: S 128 | P 64 | O 64
-constexpr int kFwdSmemBytes = 8192 /*barriers, row maxima and sums, alignment*/ + 2 * kFwdTiles * kTileBytes /*Q tiles of two items*/ + kFwdStages * 2 * kTileBytes /*K, V ring*/ +
+constexpr int kFwdSmemBytes = 10240 /*barriers, row maxima and sums, alignment*/ + 2 * kFwdTiles * kTileBytes /*Q tiles of two items*/ + kFwdStages * 2 * kTileBytes /*K, V ring*/ +
                               kTileBytes /*O staging*/;
 constexpr float kRescaleStep = 8.f;      // the reference maximum of a row moves only when the running maximum has grown by 2^8
-__device__ __forceinline__ float first_reference(float m_first64, float m_rest) { return m_rest > m_first64 + kRescaleStep ? m_rest : m_first64; }
+__device__ __forceinline__ float first_reference(float m_first64, float m_rest, float scale_log2) { return (m_rest - m_first64) * scale_log2 > kRescaleStep ? m_rest : m_first64; }
+// References and maxima are scores as the products give them, and an exponent is one multiply-add, score scale + shift with shift = -(reference scale).  That product is a rounded one, so the
+// exponents of a row are off by up to half a step of it, all alike: 2^-15 up to kFarScore.  Beyond it could be anything (128 and more once scaled scores are 1e9, and a row's largest
+// exponential is infinite), so there the reference is taken off the scores ahead of the scale.
+constexpr float kFarScore = 1024.f;
+constexpr float kFar = 1.401298464324817e-45f;      // for a shift: the least fp32 value, which adds nothing
+__device__ __forceinline__ float shift_of(float reference, float scale_log2) {
+    const float shift = -reference * scale_log2;
+    return fabsf(shift) > kFarScore ? kFar : shift;
+}
 
 __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
@@ -93,9 +102,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
     uint64_t* bar_skip = bar_stagger + 1;           // [2] tile 1's softmax warps (8), its issue warp are in an item without a second tile
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_skip + 2);
     float* s_max = reinterpret_cast<float*>(smem_dyn + 768);    // [tile][step parity][half][row] maxima of a step
-    float* s_ref = s_max + kFwdTiles * 4 * kTile;               // [tile][row] reference maximum (log2 domain)
+    float* s_ref = s_max + kFwdTiles * 4 * kTile;               // [tile][row] reference maximum
     float* s_sum = s_ref + kFwdTiles * kTile;                   // [tile][half][row] sums
-    unsigned char* sQ = align_tiles(reinterpret_cast<unsigned char*>(s_sum + kFwdTiles * 2 * kTile));
+    float* s_mine = s_sum + kFwdTiles * 2 * kTile;              // [tile][half][row] reference maximum, of its thread alone
+    unsigned char* sQ = align_tiles(reinterpret_cast<unsigned char*>(s_mine + kFwdTiles * 2 * kTile));
     unsigned char* sK = sQ + 2 * kFwdTiles * kTileBytes;       // kFwdStages stages of (K tile, V tile)
     unsigned char* sOut = sK + kFwdStages * 2 * kTileBytes;     // staging tile
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -424,8 +434,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 if (parts) {                             // both against the larger reference
                     const float m0 = m_ref, m1 = s_ref[kTile + r];
                     m_ref = fmaxf(m0, m1);
-                    mine = fast_exp2(m0 - m_ref);
-                    other = fast_exp2(m1 - m_ref);
+                    mine = fast_exp2((m0 - m_ref) * P.scale_log2);
+                    other = fast_exp2((m1 - m_ref) * P.scale_log2);
                     l_sum = l_sum * mine + (s_sum[2 * kTile + r] + s_sum[3 * kTile + r]) * other;
                     other *= 1.f / l_sum;
                 }
@@ -455,7 +465,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 tc_fence_before();
                 if (parts) mbar_arrive(bar_ofree + 1);
                 mbar_arrive(bar_ofree + w);                  // O, maximum and sum are in registers or in the staging tile
-                if (row < it.len) P.lse[static_cast<size_t>(it.h + w) * P.T + it.start + row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+                if (row < it.len) P.lse[static_cast<size_t>(it.h + w) * P.T + it.start + row] = (m_ref * P.scale_log2 + log2f(l_sum)) * 0.6931471805599453f;
                 __syncwarp();
                 if (c * 8 < P.D) {
                     __nv_bfloat16* out = P.o + (static_cast<size_t>(it.start + it.qt * kTile + r0) * P.Hq + it.h + w) * P.D + c * 8;
@@ -495,7 +505,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 ok = warp_wait_relaxed(bar_skip + 1, (i - n_mine) & 1);
                 continue;
             }
-            float m_ref = -INFINITY, l_run = 0.f;       // exponentials are taken against m_ref (log2 domain), which trails the running maximum
+            // Exponentials are taken against a reference that trails the running maximum.  What every step needs of it is its shift; itself it lies in shared memory.
+            float shift = kFar, l_run = 0.f;
+            auto refer_to = [&](float reference) {
+                s_mine[(2 * w + half) * kTile + r] = reference;
+                shift = shift_of(reference, P.scale_log2);
+            };
             bool s_ready = false;                       // a poll's answer takes a hundred cycles: polls go out ahead of where they are needed
             // keys that this row sees from this half of a step on (may be none; never none of a row's first 64, so a row's reference is finite: tiles in parts have three key tiles or more)
             int valid = min(it.len, P.causal ? it.qt * kTile + r + 1 : it.len) - it.key_tile(w, 0) * kTile - half * 64;
@@ -529,24 +544,26 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                 for (int u = 0; u < 4; ++u) mx[u] = fmaxf(mx[u], s[60 + u]);
                 // the other half's maximum of the row, through shared memory (arrays of the two step parities, so one barrier a step is enough)
                 float* ex = my_max + (t & 1) * 2 * kTile;
-                const float m_mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * P.scale_log2;
+                const float m_mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 ex[half * kTile] = m_mine;
                 const bool pv_done = t == 0 || mbar_test(bar_pv + w, (t - 1) & 1);
+                const float above = shift == kFar ? INFINITY : shift;     // a row that is far, or has no reference yet, goes the long way
                 tile_sync(w);
                 const float m_tile = fmaxf(m_mine, ex[(half ^ 1) * kTile]);
-                if (first) {
-                    first = false;
-                    m_ref = first_reference(ex[0], m_tile);
-                } else {
-                    // O accumulates in tensor memory against m_ref.  It is rescaled only when a row's maximum has outgrown m_ref by
-                    // 2^8 (probabilities then stay below 256, exact enough in bf16 and far from overflow); each half takes its
-                    // share of the columns.
-                    const bool grow = m_tile > m_ref + kRescaleStep;
-                    if (__any_sync(0xffffffffu, grow)) {
+                if (__any_sync(0xffffffffu, fmaf(m_tile, P.scale_log2, above) > kRescaleStep)) {
+                    if (first) {
+                        first = false;
+                        refer_to(first_reference(ex[0], m_tile, P.scale_log2));
+                    } else {
+                        // O accumulates in tensor memory against the reference.  It is rescaled only when a row's maximum has outgrown that by
+                        // 2^8 (probabilities then stay below 256, exact enough in bf16 and far from overflow); each half takes its
+                        // share of the columns.
+                        const float m_ref = s_mine[(2 * w + half) * kTile + r];
+                        const bool grow = (m_tile - m_ref) * P.scale_log2 > kRescaleStep;
                         ok = warp_wait(bar_pv + w, (t - 1) & 1);          // O of the previous step is complete
                         tc_fence_after();
-                        const float alpha = grow ? fast_exp2(m_ref - m_tile) : 1.f;
-                        if (grow) m_ref = m_tile;
+                        const float alpha = grow ? fast_exp2((m_ref - m_tile) * P.scale_log2) : 1.f;
+                        if (grow) refer_to(m_tile);
                         l_run *= alpha;
 #pragma unroll 1
                         for (int c = half * (P.D / 2); c < (half + 1) * (P.D / 2); c += 16) {     // sixteen columns at a time: the scores stay in registers
@@ -558,8 +575,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
                             tmem_st16(tm_o + c, reinterpret_cast<const uint32_t*>(ov));
                         }
                     }
+                    if (shift == kFar) {
+                        const float m_ref = s_mine[(2 * w + half) * kTile + r];
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) s[i] -= m_ref;
+                    }
                 }
-                const uint64_t scale2 = pair_of(P.scale_log2, P.scale_log2), shift2 = pair_of(-m_ref, -m_ref);
+                const uint64_t scale2 = pair_of(P.scale_log2, P.scale_log2), shift2 = pair_of(shift, shift);
                 uint64_t l2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};          // four running sums: keys i = 0..3 mod 4
                 uint32_t pk[32];
                 // three batches of eight scores in flight: exponents of batch g, exponentials of batch g - 1, sums and rounding of batch g - 2
@@ -598,7 +620,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_packed_fwd_kernel(const _
             }
             if (!ok) break;
             if (n_mine > 0) ok = warp_wait(bar_ofree + w, (n_mine - 1) & 1);         // the previous item's have been read
-            if (half == 0) s_ref[w * kTile + r] = m_ref;
+            if (half == 0) s_ref[w * kTile + r] = s_mine[2 * w * kTile + r];
             s_sum[(2 * w + half) * kTile + r] = l_run;
             mbar_arrive(bar_l + w);
             ++n_mine;
@@ -739,10 +761,22 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
                 }
                 m_tile = max3(m_tile, max3(mx[0], s[28], mx[1]), max3(max3(s[29], mx[2], s[30]), mx[3], s[31]));
             }
-            const float m_new = fmaxf(m_run, m_tile * P.scale_log2), alpha = fast_exp2(m_run - m_new);
+            const float m_new = fmaxf(m_run, m_tile), alpha = fast_exp2((m_run - m_new) * P.scale_log2), shift = shift_of(m_new, P.scale_log2);
             m_run = m_new;
+            if (__any_sync(0xffffffffu, shift == kFar)) {
+#pragma unroll 1
+                for (int c = 0; c < n_keys; c += 32) {
+                    float s[32];
+                    tmem_ld32(tm + c, s);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) s[i] = shift == kFar ? s[i] - m_new : s[i];
+                    tmem_st32(tm + c, reinterpret_cast<const uint32_t*>(s));
+                }
+                tmem_st_wait();
+            }
             // ---- P = exp2(S scale - maximum), rounded to bf16, over the columns of S that have been read ----
-            const uint64_t shift2 = pair_of(-m_new, -m_new);
+            const uint64_t shift2 = pair_of(shift, shift);
             uint64_t l2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
             auto l_sum = [&]() {
                 float a0, a1, a2, a3;
@@ -834,7 +868,7 @@ __global__ void __launch_bounds__(kTileFwdThreads, kTileFwdPerSm) attn_packed_ti
             const float inv_l = 1.f / l_run;
             unsigned char* rowp = sQ + tid * kRowBytes;
             const int row = qt * kTile + at.token;
-            if (heads > 1 ? tid < heads * len : row < len) P.lse[static_cast<size_t>(h + at.head) * P.T + start + row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+            if (heads > 1 ? tid < heads * len : row < len) P.lse[static_cast<size_t>(h + at.head) * P.T + start + row] = (m_run * P.scale_log2 + log2f(l_run)) * 0.6931471805599453f;
 #pragma unroll 1
             for (int c16 = 0; c16 < P.D / 16; ++c16) {
                 float ov[16];
