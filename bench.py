@@ -373,6 +373,11 @@ def pearson_leg(torch, vd, path, w, peaks, barrier, args):
     return res
 
 
+def layer_norm_bytes(T, B, N, C):
+    """What the norms of the layer leg cannot do without, in bytes of bf16 rows: x, y, d_h, d_u read once and h, u, dy written for T kept tokens, dx written for all."""
+    return (7 * T + B * N) * C * 2
+
+
 def layer_leg(torch, vd, path, w, peaks, barrier, args):
     """Times what an encoder layer on kept tokens and the end of its training step have the library do around the projections: the norms of the residual stream with a gate per
     instance (gathered by the selection), attention over the kept sets packed one behind the other, both with their backward passes, and the clipping of the attention's
@@ -427,7 +432,7 @@ def layer_leg(torch, vd, path, w, peaks, barrier, args):
         if vd.vardrop_ws_status(ws) != vd.OK:
             raise RuntimeError("device status set by an operator of the layer")
     pairs = int((sel["n_sel"].double() ** 2).sum().item()) * H
-    return {"ms_per_layer": t["median"], "kept_tokens": T, "attention_flops": 14 * D * pairs, "norm_bytes": (8 * T + B * N) * C * 2, "kernel_us": per,
+    return {"ms_per_layer": t["median"], "kept_tokens": T, "attention_flops": 14 * D * pairs, "norm_bytes": layer_norm_bytes(T, B, N, C), "kernel_us": per,
             "note": "kernel_us from a pass with the per-kernel event timer armed"}
 
 
