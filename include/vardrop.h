@@ -348,7 +348,8 @@ int vardrop_attn_packed_bwd(const void* q, const void* k, const void* v, const v
  * h           [B, N, C] out; may be NULL (not wanted).
  * u           [B, N, C] out; NULL exactly when pre = 0.
  * stats       [B, N, 4] fp32 out: mean and r of N_post(y), mean and r of N_pre(h); may be NULL where no backward call follows.
- * Rows from n_sel on are left as they are.  x and h, or y and u, may be the same buffer where there is no selection.
+ * Rows from n_sel on are left as they are.  x and h, or y and u, may be the same buffer where there is no selection; outputs that overlap an input whose rows other threads read, or another output,
+ * are refused, here and in the backward call.
  * Sums in fp32, the mean ahead of the squares (two passes over registers), outputs rounded once.
  *
  * Backward: d_h (NULL: 0) and d_u (NULL exactly when pre = 0) are the gradients of h and u, x, y and the parameters as given to the forward call, stats its output.

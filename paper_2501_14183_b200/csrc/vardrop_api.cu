@@ -356,6 +356,29 @@ static int norm_params_check(const vardrop_norm_cfg& c, const void* y, const voi
     return check_ptr(b_pre, "b_pre", false);
 }
 
+// Buffers of a norm call that overlap.  An output that begins where an input of the same rows does is written by the threads that have read them; with a selection x and dx hold other rows than the
+// rest.  Anything else would be read, or written, twice.
+struct NormBuffer {
+    const void* p;
+    size_t bytes;
+    enum Rows { kNone, kOwn, kAll } rows;    // of its own layout; of the kept tokens (all, without a selection); of all tokens
+    const char* name;
+};
+static int norm_overlap_check(const NormBuffer* ins, int n_ins, const NormBuffer* outs, int n_outs) {
+    const auto overlap = [](const NormBuffer& a, const NormBuffer& b) {
+        const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+        return a.p && b.p && a.bytes && b.bytes && pa < pb + b.bytes && pb < pa + a.bytes;
+    };
+    for (int o = 0; o < n_outs; ++o) {
+        for (int i = 0; i < n_ins; ++i)
+            if (overlap(outs[o], ins[i]) && !(outs[o].p == ins[i].p && outs[o].rows == ins[i].rows && outs[o].rows != NormBuffer::kNone))
+                return fail(VARDROP_ERR_INVALID_ARG, "norm: %s and %s overlap", outs[o].name, ins[i].name);
+        for (int i = 0; i < o; ++i)
+            if (overlap(outs[o], outs[i])) return fail(VARDROP_ERR_INVALID_ARG, "norm: %s and %s overlap", outs[o].name, outs[i].name);
+    }
+    return VARDROP_OK;
+}
+
 int vardrop_norm_fwd(const void* x, const void* y, const float* gate, const float* w_post, const float* b_post, const float* w_pre, const float* b_pre,
                      const int32_t* sel_idx, const int32_t* n_sel, const vardrop_norm_cfg* cfg, void* h, void* u, float* stats, void* stream) {
     if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
@@ -369,6 +392,12 @@ int vardrop_norm_fwd(const void* x, const void* y, const float* gate, const floa
     if ((u != nullptr) != (cfg->pre != 0)) return fail(VARDROP_ERR_INVALID_ARG, "norm: pre=%d and u %s", cfg->pre, u ? "given" : "NULL");
     VD_CHECK(check_ptr(u, "u", false));
     VD_CHECK(check_ptr(stats, "stats", false));
+    const size_t tokens = static_cast<size_t>(cfg->B) * cfg->N, rows = tokens * cfg->C * (cfg->dtype == 2 ? 4 : 2), row = sizeof(float) * cfg->C, S = sel_idx && cfg->S > 1 ? cfg->S : 1;
+    const NormBuffer ins[] = {{x, rows, sel_idx ? NormBuffer::kAll : NormBuffer::kOwn, "x"}, {y, rows, NormBuffer::kOwn, "y"}, {gate, row * cfg->gate_rows, NormBuffer::kNone, "gate"},
+                              {w_post, row, NormBuffer::kNone, "w_post"}, {b_post, row, NormBuffer::kNone, "b_post"}, {w_pre, row, NormBuffer::kNone, "w_pre"}, {b_pre, row, NormBuffer::kNone, "b_pre"},
+                              {sel_idx, S * cfg->N * sizeof(int32_t), NormBuffer::kNone, "sel_idx"}, {sel_idx ? n_sel : nullptr, S * sizeof(int32_t), NormBuffer::kNone, "n_sel"}};
+    const NormBuffer outs[] = {{h, rows, NormBuffer::kOwn, "h"}, {u, rows, NormBuffer::kOwn, "u"}, {stats, tokens * 16, NormBuffer::kNone, "stats"}};
+    VD_CHECK(norm_overlap_check(ins, 9, outs, 3));
     return norm_fwd_launch(x, y, gate, w_post, b_post, w_pre, b_pre, sel_idx, n_sel, *cfg, h, u, stats, static_cast<cudaStream_t>(stream));
 }
 
@@ -405,6 +434,16 @@ int vardrop_norm_bwd(const void* x, const void* y, const float* gate, const floa
     VD_CHECK(check_ptr(d_w_pre, "d_w_pre", false));
     VD_CHECK(check_ptr(d_b_pre, "d_b_pre", false));
     VD_CHECK(check_ws(ws, ws_bytes, norm_workspace_bytes(*cfg)));
+    const size_t tokens = static_cast<size_t>(cfg->B) * cfg->N, rows = tokens * cfg->C * (cfg->dtype == 2 ? 4 : 2), row = sizeof(float) * cfg->C, S = sel_idx && cfg->S > 1 ? cfg->S : 1;
+    const size_t index = sel_idx ? S * cfg->N * sizeof(int32_t) : 0;
+    const NormBuffer::Rows of_x = sel_idx ? NormBuffer::kAll : NormBuffer::kOwn;
+    const NormBuffer ins[] = {{x, rows, of_x, "x"}, {y, rows, NormBuffer::kOwn, "y"}, {d_h, rows, NormBuffer::kOwn, "d_h"}, {d_u, rows, NormBuffer::kOwn, "d_u"}, {stats, tokens * 16, NormBuffer::kNone, "stats"},
+                              {gate, row * cfg->gate_rows, NormBuffer::kNone, "gate"}, {w_post, row, NormBuffer::kNone, "w_post"}, {b_post, row, NormBuffer::kNone, "b_post"},
+                              {w_pre, row, NormBuffer::kNone, "w_pre"}, {sel_idx, index, NormBuffer::kNone, "sel_idx"}, {inv_idx, index, NormBuffer::kNone, "inv_idx"},
+                              {n_sel, sel_idx ? S * sizeof(int32_t) : 0, NormBuffer::kNone, "n_sel"}};
+    const NormBuffer outs[] = {{dx, rows, of_x, "dx"}, {dy, rows, NormBuffer::kOwn, "dy"}, {d_gate, row * cfg->gate_rows, NormBuffer::kNone, "d_gate"}, {d_w_post, row, NormBuffer::kNone, "d_w_post"},
+                               {d_b_post, row, NormBuffer::kNone, "d_b_post"}, {d_w_pre, row, NormBuffer::kNone, "d_w_pre"}, {d_b_pre, row, NormBuffer::kNone, "d_b_pre"}};
+    VD_CHECK(norm_overlap_check(ins, 12, outs, 7));
     return norm_bwd_launch(x, y, gate, w_post, b_post, w_pre, sel_idx, n_sel, inv_idx, stats, d_h, d_u, *cfg, dx, dy, d_gate, d_w_post, d_b_post, d_w_pre, d_b_pre, ws,
                            static_cast<cudaStream_t>(stream));
 }
