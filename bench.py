@@ -381,7 +381,7 @@ def layer_norm_bytes(T, B, N, C):
 def layer_leg(torch, vd, path, w, peaks, barrier, args):
     """Times what an encoder layer on kept tokens and the end of its training step have the library do around the projections: the norms of the residual stream with a gate per
     instance (gathered by the selection), attention over the kept sets packed one behind the other, both with their backward passes, and the clipping of the attention's
-    gradients.  Every instance is hashed and sampled on its own, so that the sets differ in size."""
+    gradients.  Rows move between the norms' padded layout and the packed one in the caller's projections or in copies of its own; these are not timed.  Every instance is hashed and sampled on its own, so that the sets differ in size."""
     device = path.dev[0]["x"].device
     B, N, H, D, C = w.B, w.N, w.H, w.D, w.H * w.D
     bf, f32 = dict(dtype=torch.bfloat16, device=device), dict(dtype=torch.float32, device=device)

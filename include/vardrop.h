@@ -295,7 +295,7 @@ int vardrop_pearson_max(const float* x, const vardrop_pearson_cfg* cfg, float* m
  * The plan of a batch says where its sequences are and in which order their tiles are worked off.  It is made once from the offsets, on
  * the device, and serves every call on that batch (all layers, forward and backward, any number of them at a time: calls only read it).
  *
- * cfg (host)  n_seqs >= 1; T >= 1 rows of the packed tensors (at most 2^24); Hq a multiple of Hkv; D = 32 or 64; sm_scale up to 1e30 (0 selects
+ * cfg (host)  n_seqs >= 1; T >= 1 rows of the packed tensors (at most 2^24); Hq a multiple of Hkv, at most 4096 (and T / 128 + n_seqs tiles below 2^24, times Hq below 2^31); D = 32 or 64; sm_scale up to 1e30 (0 selects
  *             1/sqrt(D)); causal 0 or 1; element strides of q (sTq of a token, sHq of a head) and of both k and v (sTkv, sHkv), the head
  *             dimension contiguous; the two of a tensor both 0 select the contiguous layout, otherwise each must be a multiple of 8 with sT >= sH >= D (views of
  *             a fused projection [T, Hq + 2 Hkv, D]).  o, lse, d_o, dq, dk, dv are always contiguous.
@@ -340,7 +340,7 @@ int vardrop_attn_packed_bwd(const void* q, const void* k, const void* v, const v
  * With a selection, y, h, u hold the kept tokens and x every one: row i of instance b has x[b, sel_idx[s(b), i]], the gather that vardrop_attn_fwd makes of q, k, v.
  *
  * cfg (host)  B, N, C (C <= 8192; B N < 2^31); dtype of x, y, h, u and their gradients: 0 bf16, 1 fp16, 2 fp32; pre and post: 0 none, 1 rms, 2 layer;
- *             gate_rows 0 (no gate), 1 or B; S as in vardrop_attn_cfg; res_scale and eps >= 0 finite.
+ *             gate_rows 0 (no gate), 1 or B (at most 65534); S as in vardrop_attn_cfg; res_scale and eps >= 0 finite.
  * x           [B, N, C].
  * y           [B, N, C], rows below n_sel of the instance are read; NULL: h = res_scale x (then post and gate_rows must be 0).
  * gate        [gate_rows, C] fp32.     w_post, b_post, w_pre, b_pre   [C] fp32, NULL: 1 and 0; b only with the kind 2, none with the kind 0.
@@ -375,7 +375,7 @@ int vardrop_norm_bwd(const void* x, const void* y, const float* gate, const floa
 /* ------------------------------------------------------------------------------------------------
  * Global gradient norm over many tensors, and clipping (the end of a training step; no counterpart in the paper):
  *   norm = sqrt(sum over all tensors and elements of g^2);   out = g min(1, max_norm / (norm + eps))
- * Sums in fp64, in a fixed order (bit-reproducible; two neighbouring squares are added in fp32 where that leaves no range); products rounded once to the tensor's type.
+ * Sums in fp64, in a fixed order (bit-reproducible; two neighbouring squares are added in fp32 where that leaves no range); products in fp32, rounded once to the tensor's type.
  *
  * tensors     (host) [count] of device pointers, element counts (>= 0) and types (0 bf16, 1 fp16, 2 fp32); read before the call returns.  `in` and `out` need the
  *             alignment of their element only; out = in clips in place; otherwise no output may overlap another
