@@ -49,7 +49,7 @@ __device__ __forceinline__ float first_reference(float m_first64, float m_rest, 
 // exponents of a row are off by up to half a step of it, all alike: 2^-15 up to kFarScore.  Beyond it could be anything (128 and more once scaled scores are 1e9, and a row's largest
 // exponential is infinite), so there the reference is taken off the scores ahead of the scale.
 constexpr float kFarScore = 1024.f;
-constexpr float kFar = 1.401298464324817e-45f;      // for a shift: the least fp32 value, which adds nothing
+constexpr float kFar = 1.401298464324817e-45f;      // for a shift: the least fp32 value, which adds nothing (and is no zero: the library is built without flushing)
 __device__ __forceinline__ float shift_of(float reference, float scale_log2) {
     const float shift = -reference * scale_log2;
     return fabsf(shift) > kFarScore ? kFar : shift;

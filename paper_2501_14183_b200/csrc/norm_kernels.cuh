@@ -316,7 +316,7 @@ __device__ __forceinline__ Run run_of(const NormParams& P, long long* s_scan) { 
             all += v;
         }
     };
-    auto find = [&](long long b) {                           // the instance in which the run begins
+    auto find = [&](long long b) {                       // the instance in which the run begins
         if (n > 0 && ahead <= r.from && r.from < ahead + n) {
             s_scan[warps] = b;
             s_scan[warps + 1] = ahead;
@@ -727,8 +727,8 @@ cudaError_t launch_bwd(int grid, const NormParams& P, cudaStream_t s) {
     return launch_chained(norm_bwd_kernel<T, kV, kGroup, kPer, kLayer>, dim3(grid), dim3(kNormThreads<kGroup>), kBytes, s, P);
 }
 // Rows that are not taken in 16-byte vectors are bound by instructions, and a group of a power of two has up to twice the columns that a row has: where fewer elements a
-// thread do, it gets fewer (5136 rows of 515 fp32, forward and backward: 43.4 us with 16 and 8, 35.0 with 10 and 6; 17 widths of 131 to 5101 columns, bf16 and fp32: forward 12 to 105 %, both ways 5
-// to 45 % slower without, and none faster).
+// thread do, it gets fewer (5136 rows of 515 fp32, forward and backward: 43.4 us with 16 and 8, 35.0 with 10 and 6; 17 widths of 131 to 5101 columns, bf16 and fp32, are
+// 12 to 105 % slower without it forward and 5 to 45 % both ways, where it applies to them).
 template <class T, int kV, int kGroup, bool kLayer>
 cudaError_t launch(bool bwd, int grid, const NormParams& P, cudaStream_t s) {
     constexpr bool kWide = kV * sizeof(T) == 16;
