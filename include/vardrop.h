@@ -13,6 +13,8 @@
  *   vardrop_attn_packed_fwd, _bwd   attention over packed sequences of different lengths, causal or not, grouped heads
  *   vardrop_norm_fwd, _bwd          norms before and after a block with its gate and residual scale
  *   vardrop_grad_clip               global gradient norm over many tensors, and clipping
+ *   vardrop_embed_fwd, _bwd         token embeddings by index, and the table's gradient
+ *   vardrop_act_fwd, _bwd           the feed-forward's activation, gated or not, with a checkpoint in 8 bits that the backward pass works from
  *
  * Conventions shared by every entry point
  *   - Pointers named in the argument lists are DEVICE pointers unless the comment says "host".
@@ -398,6 +400,58 @@ typedef struct {
 
 size_t vardrop_grad_clip_workspace_bytes(void);
 int vardrop_grad_clip(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg* cfg, float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Token embeddings (no counterpart in the paper): rows of a table by index, for tokens of a vocabulary, or an embedding of its own for each variate (idx = vardrop_select's sel_idx).
+ *   out[t] = scale table[idx[t]], a row of zeros where idx[t] < 0
+ *   d_table[v] = scale (sum of d_out[t] over the tokens with idx[t] = v)        (accumulate = 1: added to what is there)
+ *
+ * cfg (host)  T tokens (at most 2^28), V rows of the table (at most 2^30), C channels (at most 65536); dtype of the table and its gradient, out_dtype of out and d_out: 0 bf16, 1 fp16, 2 fp32;
+ *             scale finite; accumulate 0 or 1 (backward only).
+ * table       [V, C].     idx   [T] int32; negative: no token.  An index from V on is taken as none, and reported: device status VARDROP_ERR_INVALID_ARG.
+ * out         [T, C] out.
+ * d_out       [T, C], gradient of out; rows of tokens without an index are not read.
+ * d_table     [V, C] out; with accumulate = 0 every row is written (zeros where no token has it), with 1 only rows that some token has are read and written.
+ * ws          scratch of vardrop_embed_workspace_bytes for the backward call; the forward call only needs its status word (256 bytes).  Nothing is kept in it.
+ * Sums in fp32 in an order that the tokens' order alone decides (bit-reproducible), rounded once.  No buffer may overlap an output.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t T, V, C, dtype, out_dtype, accumulate;
+    float scale;
+} vardrop_embed_cfg;
+
+size_t vardrop_embed_workspace_bytes(const vardrop_embed_cfg* cfg);
+int vardrop_embed_fwd(const void* table, const int32_t* idx, const vardrop_embed_cfg* cfg, void* out, void* ws, size_t ws_bytes, void* stream);
+int vardrop_embed_bwd(const void* d_out, const int32_t* idx, const vardrop_embed_cfg* cfg, void* d_table, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Activation of a feed-forward block, with a checkpoint in 8 bits (no counterpart in the paper, which takes its encoder's layers as they are):
+ *   y = f(a), or f(a) o b with a gate;   f: relu, gelu (a Phi(a)), silu (a / (1 + exp(-a)))
+ * The forward pass leaves a (and b) in 8 bits, a^ below, from which the backward pass works; a and b themselves need not be kept:
+ *   d_a = d_y o b^ o f'(a^);   d_b = d_y o f(a^);   y^ = f(a^) o b^ (for the weight gradient of the projection that reads y)
+ * 32 neighbouring values of a row share a scale, the smallest power of two 2^e (e >= -127) with max |a| <= 448 2^e over its finite values; a value is the nearest e4m3 number of that scale (ties to even; where that
+ * is past the type's largest, the one below), so a^ is within 2^-4 |a|, or 2^(e-10) where |a| is below 2^(e-6).  Infinities and NaN come back as NaN, each in its own place.
+ *
+ * cfg (host)  B, N, C (C <= 2^20; B N < 2^31; N ceil(C / 32) <= 2^31); dtype of a, b, y and their gradients: 0 bf16, 1 fp16, 2 fp32; kind 0 relu, 1 gelu, 2 silu; gated 0 or 1; S as in vardrop_attn_cfg;
+ *             stride: elements from row to row of a, b, d_a and d_b (0: C; otherwise a multiple of 8 and at least C: both halves of one projection [B, N, 2 C]).
+ * a, b        [B, N, C] with that stride; b is NULL exactly when gated = 0.
+ * n_sel       [S] int32 on the device: rows from n_sel on (of an instance, S = B, or of every one) are not read, and left as they are in all outputs; NULL: every row counts.
+ * y           [B, N, C] out; backward it may be NULL (not wanted).
+ * ckpt        vardrop_act_ckpt_bytes; forward out, NULL: none (inference).  It holds the codes [1 + gated, B, N, C], one byte each, and from the next multiple of 256 on the scales
+ *             [1 + gated, B, N, ceil(C / 32)], e + 127.  The backward call takes it with the configuration that it was made with.
+ * d_y         [B, N, C], gradient of y.
+ * d_a, d_b    [B, N, C] out with the stride; d_b is NULL exactly when gated = 0.
+ * Forward y may be a or b, backward d_a, d_b or y may be d_y, where the rows lie alike; any other overlap with an output is refused.
+ * Arithmetic in fp32, results rounded once; no workspace and no device status.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t B, N, C, dtype, kind, gated, S;
+    int64_t stride;
+} vardrop_act_cfg;
+
+size_t vardrop_act_ckpt_bytes(const vardrop_act_cfg* cfg);
+int vardrop_act_fwd(const void* a, const void* b, const int32_t* n_sel, const vardrop_act_cfg* cfg, void* y, void* ckpt, size_t ckpt_bytes, void* stream);
+int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const int32_t* n_sel, const vardrop_act_cfg* cfg, void* d_a, void* d_b, void* y, void* stream);
 
 #ifdef __cplusplus
 }

@@ -57,8 +57,18 @@ class ClipCfg(C.Structure):
     _fields_ = [("max_norm", C.c_float), ("eps", C.c_float)]
 
 
+class EmbedCfg(C.Structure):
+    _fields_ = [("T", C.c_int32), ("V", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("accumulate", C.c_int32), ("scale", C.c_float)]
+
+
+class ActCfg(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("kind", C.c_int32), ("gated", C.c_int32), ("S", C.c_int32),
+                ("stride", C.c_int64)]         # elements from row to row of a, b, d_a, d_b; 0 = C
+
+
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2
 
 
 class VardropError(RuntimeError):
@@ -72,7 +82,8 @@ EXPORTS = ("vardrop_status_string", "vardrop_last_error", "vardrop_version", "va
            "vardrop_select_workspace_bytes", "vardrop_select", "vardrop_select_static", "vardrop_gather_rows", "vardrop_attn_workspace_bytes", "vardrop_attn_fwd",
            "vardrop_attn_bwd", "vardrop_pearson_workspace_bytes", "vardrop_pearson_max", "vardrop_packed_plan_bytes", "vardrop_packed_plan",
            "vardrop_attn_packed_workspace_bytes", "vardrop_attn_packed_fwd", "vardrop_attn_packed_bwd", "vardrop_norm_fwd", "vardrop_norm_workspace_bytes", "vardrop_norm_bwd",
-           "vardrop_grad_clip_workspace_bytes", "vardrop_grad_clip", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
+           "vardrop_grad_clip_workspace_bytes", "vardrop_grad_clip", "vardrop_embed_workspace_bytes", "vardrop_embed_fwd", "vardrop_embed_bwd", "vardrop_act_ckpt_bytes",
+           "vardrop_act_fwd", "vardrop_act_bwd", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
            "vardrop_profile_kernel_name", "vardrop_profile_read")
 
 
@@ -88,7 +99,7 @@ def load() -> C.CDLL:
         lib.vardrop_status_string.argtypes = [C.c_int]
         for name in ("vardrop_hash_workspace_bytes", "vardrop_select_workspace_bytes", "vardrop_attn_workspace_bytes",
                      "vardrop_pearson_workspace_bytes", "vardrop_norm_workspace_bytes", "vardrop_packed_plan_bytes",
-                     "vardrop_attn_packed_workspace_bytes"):
+                     "vardrop_attn_packed_workspace_bytes", "vardrop_embed_workspace_bytes", "vardrop_act_ckpt_bytes"):
             getattr(lib, name).restype = C.c_size_t
             getattr(lib, name).argtypes = [C.c_void_p]
         lib.vardrop_ws_status.restype = C.c_int
@@ -123,6 +134,11 @@ def load() -> C.CDLL:
         lib.vardrop_grad_clip_workspace_bytes.argtypes = []
         lib.vardrop_grad_clip.restype = C.c_int
         lib.vardrop_grad_clip.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.vardrop_embed_fwd.restype = lib.vardrop_embed_bwd.restype = C.c_int
+        lib.vardrop_embed_fwd.argtypes = lib.vardrop_embed_bwd.argtypes = [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_act_fwd.restype = lib.vardrop_act_bwd.restype = C.c_int
+        lib.vardrop_act_fwd.argtypes = [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_act_bwd.argtypes = [C.c_void_p] * 2 + [C.c_size_t] + [C.c_void_p] * 6
         lib.vardrop_launch_count.restype = C.c_longlong
         lib.vardrop_profile_kernel_name.restype = C.c_char_p
         lib.vardrop_profile_kernel_name.argtypes = [C.c_int]
@@ -250,6 +266,31 @@ def vardrop_grad_clip(grads, cfg: ClipCfg, outs, norm, ws) -> None:
     _check((_marshal or _load_marshal()).grad_clip(grads, cfg, outs, norm, ws), "vardrop_grad_clip")
 
 
+def vardrop_embed_workspace_bytes(cfg: EmbedCfg) -> int:
+    return int(load().vardrop_embed_workspace_bytes(C.byref(cfg)))
+
+
+def vardrop_embed_fwd(table, idx, cfg: EmbedCfg, out, ws) -> None:
+    _check((_marshal or _load_marshal()).embed_fwd(table, idx, cfg, out, ws), "vardrop_embed_fwd")
+
+
+def vardrop_embed_bwd(d_out, idx, cfg: EmbedCfg, d_table, ws) -> None:
+    _check((_marshal or _load_marshal()).embed_bwd(d_out, idx, cfg, d_table, ws), "vardrop_embed_bwd")
+
+
+def vardrop_act_ckpt_bytes(cfg: ActCfg) -> int:
+    return int(load().vardrop_act_ckpt_bytes(C.byref(cfg)))
+
+
+def vardrop_act_fwd(a, b, n_sel, cfg: ActCfg, y, ckpt) -> None:
+    """`ckpt` None: inference, nothing is kept for a backward call."""
+    _check((_marshal or _load_marshal()).act_fwd(a, b, n_sel, cfg, y, ckpt), "vardrop_act_fwd")
+
+
+def vardrop_act_bwd(d_y, ckpt, n_sel, cfg: ActCfg, d_a, d_b, y) -> None:
+    _check((_marshal or _load_marshal()).act_bwd(d_y, ckpt, n_sel, cfg, d_a, d_b, y), "vardrop_act_bwd")
+
+
 def vardrop_launch_count() -> int:
     return int(load().vardrop_launch_count())
 
@@ -289,6 +330,10 @@ def alloc_ws(nbytes: int, device="cuda"):
 
 def alloc_packed_plan(cfg: PackedCfg, device="cuda"):
     return torch.zeros(vardrop_packed_plan_bytes(cfg), dtype=torch.uint8, device=device)
+
+
+def alloc_act_ckpt(cfg: ActCfg, device="cuda"):
+    return torch.empty(vardrop_act_ckpt_bytes(cfg), dtype=torch.uint8, device=device)
 
 
 def alloc_hash_outputs(cfg: HashCfg, device="cuda", want_freqs=True, want_amp=False):

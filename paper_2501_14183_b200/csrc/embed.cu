@@ -1,0 +1,530 @@
+// Token embeddings: out[t] = scale table[idx[t]], and the table's gradient, d_table[v] (+)= scale sum of d_out[t] over the tokens with idx[t] = v.
+//
+// embed_fwd_kernel      rows of the table, several tokens to a thread so that their loads overlap.  Bound: memory.
+// embed_count_kernel, embed_sort_kernel   tokens sorted by index, equal ones in their own order: a radix sort of (index, token) by digits of up to nine bits, so that 512 rows take one pass and 2^18
+//                       two.  Indices that name no row are sorted behind the last one.  embed_sort_small_kernel: all passes in shared memory.
+// embed_sum_kernel      even shares of the sorted tokens: whoever meets all tokens of a row writes it, pieces of a row go to the workspace.  Rows without a token are written as zeros beside it.
+// embed_join_kernel     adds up the pieces, in order.
+//
+// The order of every sum is that of the tokens and does not depend on which CTA runs when: results are bit-reproducible.  Bound: memory, and for few tokens the chain of launches.
+#include <algorithm>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "vec_io.cuh"
+
+namespace vardrop {
+
+namespace {
+
+constexpr int kEmbedThreads = 256;
+constexpr int kSortThreads = 1024, kSortItems = 4, kSortTile = kSortThreads * kSortItems;      // tokens that a CTA ranks at a time
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kMaxDigitBits = 9, kMaxBins = 1 << kMaxDigitBits;
+constexpr int kMaxSortBlocks = 256;             // beyond, a CTA takes several tiles: the offsets of a digit are summed over all CTAs by each of them
+constexpr int kSumBatch = 4;                    // rows that a thread of the sums has on their way
+constexpr int kLeastShare = 8, kMostShare = 128;  // sorted tokens of a share: fewer make more pieces, more leave long chains of loads
+
+struct SortPlan {
+    int bits, passes, tiles_per_block, blocks;
+};
+SortPlan sort_plan(const vardrop_embed_cfg& c) {
+    SortPlan p{};
+    int bits = 1;
+    while ((c.V >> bits) != 0) ++bits;          // of the keys 0 .. V
+    p.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    const int tiles = (c.T + kSortTile - 1) / kSortTile;
+    p.tiles_per_block = (tiles + kMaxSortBlocks - 1) / kMaxSortBlocks;
+    p.blocks = (tiles + p.tiles_per_block - 1) / p.tiles_per_block;
+    return p;
+}
+
+// Threads of a row, and sorted tokens of a share: some 1024 threads for every SM, where there are tokens enough.
+struct SumPlan {
+    int vec, lanes, slabs, share, shares;
+};
+SumPlan sum_plan(const vardrop_embed_cfg& c) {
+    SumPlan p{};
+    p.vec = row_vector(c.C);
+    const int vectors = c.C / p.vec;
+    p.lanes = 1;
+    while (p.lanes < vectors && p.lanes < kEmbedThreads) p.lanes *= 2;
+    p.slabs = (vectors + p.lanes - 1) / p.lanes;
+    const long long wanted = 148ll * 1024 / (static_cast<long long>(p.lanes) * p.slabs);      // (a constant, so that sums do not depend on the device)
+    const long long share = (c.T + std::max(wanted, 1ll) - 1) / std::max(wanted, 1ll);
+    p.share = static_cast<int>(std::min<long long>(std::max<long long>(share, kLeastShare), kMostShare));
+    p.shares = (c.T + p.share - 1) / p.share;
+    return p;
+}
+
+struct EmbedWs {
+    size_t counts, keys[2], tokens[2], pieces, total;
+};
+EmbedWs embed_layout(const vardrop_embed_cfg& c) {
+    const SortPlan s = sort_plan(c);
+    const SumPlan u = sum_plan(c);
+    EmbedWs w;
+    size_t o = align_up(kWsHeaderBytes, 1024);
+    w.counts = o; o += align_up(sizeof(int32_t) * s.passes * s.blocks * kMaxBins, 1024);
+    for (int i = 0; i < 2; ++i) {
+        w.keys[i] = o; o += align_up(sizeof(int32_t) * static_cast<size_t>(c.T), 1024);
+        w.tokens[i] = o; o += align_up(sizeof(int32_t) * static_cast<size_t>(c.T), 1024);
+    }
+    w.pieces = o; o += align_up(sizeof(float) * 2 * u.shares * static_cast<size_t>(c.C), 1024);
+    w.total = o;
+    return w;
+}
+
+// ---- forward ------------------------------------------------------------------------------------------------------------------
+struct EmbedParams {
+    const void* table;
+    const int32_t* idx;
+    void* out;
+    int* status;
+    int T, V, C, lanes;
+    float scale;
+};
+// A row takes `lanes` threads, a CTA kTokens rows for each group of them.
+template <class Tab, class Out, int kVec, int kTokens>
+__global__ void __launch_bounds__(kEmbedThreads) embed_fwd_kernel(const EmbedParams P) {
+    chain_wait();
+    chain_release();
+    const int groups = kEmbedThreads / P.lanes, group = threadIdx.x / P.lanes, lane = threadIdx.x & (P.lanes - 1);
+    const long long t0 = static_cast<long long>(blockIdx.x) * groups * kTokens + group;
+    const Tab* const table = static_cast<const Tab*>(P.table);
+    Out* const out = static_cast<Out*>(P.out);
+    int row[kTokens];
+#pragma unroll
+    for (int u = 0; u < kTokens; ++u) {
+        const long long t = t0 + u * groups;
+        row[u] = t < P.T ? __ldg(P.idx + t) : -1;
+        if (row[u] >= P.V) {
+            if (lane == 0) set_status(P.status, VARDROP_ERR_INVALID_ARG);
+            row[u] = -1;
+        }
+    }
+#pragma unroll 1
+    for (int c = lane * kVec; c < P.C; c += P.lanes * kVec) {
+        Pack<Tab, kVec> in[kTokens];
+#pragma unroll
+        for (int u = 0; u < kTokens; ++u)
+            if (row[u] >= 0) in[u] = load_pack<Tab, kVec>(table + static_cast<size_t>(row[u]) * P.C + c);
+#pragma unroll
+        for (int u = 0; u < kTokens; ++u) {
+            const long long t = t0 + u * groups;
+            if (t >= P.T) break;
+            Pack<Out, kVec> v;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v.e[e] = from_float<Out>(row[u] >= 0 ? to_float(in[u].e[e]) * P.scale : 0.f);
+            store_pack(out + static_cast<size_t>(t) * P.C + c, v);
+        }
+    }
+}
+
+// ---- tokens by index ------------------------------------------------------------------------------------------------------------
+struct SortParams {
+    const int32_t *idx, *keys, *tokens;         // idx: the first pass
+    int32_t *keys_out, *tokens_out, *counts;    // counts [passes, blocks, bins]
+    int* status;
+    int T, V, bits, pass, passes, blocks, tiles_per_block;
+};
+// The key of token t: its index, V where it names no row.
+__device__ __forceinline__ int key_of(const SortParams& P, int t) {
+    const int v = __ldg(P.idx + t);
+    if (v >= P.V) set_status(P.status, VARDROP_ERR_INVALID_ARG);
+    return v < 0 || v >= P.V ? P.V : v;
+}
+
+__global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortParams P) {
+    __shared__ int hist[kMaxBins];
+    const int bins = 1 << P.bits;
+    for (int d = threadIdx.x; d < bins; d += kSortThreads) hist[d] = 0;
+    chain_wait();
+    chain_release();
+    __syncthreads();
+    const long long begin = static_cast<long long>(blockIdx.x) * P.tiles_per_block * kSortTile, end = min(static_cast<long long>(P.T), begin + static_cast<long long>(P.tiles_per_block) * kSortTile);
+    for (long long t = begin + threadIdx.x; t < end; t += kSortThreads) atomicAdd(hist + (key_of(P, static_cast<int>(t)) & (bins - 1)), 1);
+    __syncthreads();
+    for (int d = threadIdx.x; d < bins; d += kSortThreads) {
+        P.counts[static_cast<size_t>(blockIdx.x) * kMaxBins + d] = hist[d];
+        for (int p = 1; p < P.passes; ++p) P.counts[(static_cast<size_t>(p) * P.blocks + blockIdx.x) * kMaxBins + d] = 0;
+    }
+}
+
+struct SortShared {
+    uint16_t count[kSortWarps][kMaxBins];       // of a digit in a warp's tokens, then in those of the warps ahead
+    int base[kMaxBins];                         // place of the digit's next token
+    int part[kSortThreads / 32][2];
+    int sum[2][kSortThreads];
+};
+// Places of a tile's tokens: warp w has the tokens from 128 w on, 32 at a time.  place[i] is added to base[digit].  Moves base on.
+__device__ __forceinline__ void rank_tile(SortShared& S, int bins, const int (&digit)[kSortItems], const bool (&there)[kSortItems], int (&place)[kSortItems]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int d = lane; d < bins; d += 32) S.count[warp][d] = 0;
+    __syncwarp();
+    int rank[kSortItems];
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        const uint32_t active = __ballot_sync(0xffffffffu, there[i]);
+        if (there[i]) {
+            const uint32_t peers = __match_any_sync(active, digit[i]);
+            rank[i] = S.count[warp][digit[i]] + __popc(peers & ((1u << lane) - 1));
+            __syncwarp(active);
+            if ((peers >> lane) == 1u) S.count[warp][digit[i]] += static_cast<uint16_t>(__popc(peers));      // the last of them
+        }
+        __syncwarp();
+    }
+    __syncthreads();
+    int total = 0;
+    if (threadIdx.x < bins) {
+#pragma unroll 8
+        for (int w = 0; w < kSortWarps; ++w) {
+            const int n = S.count[w][threadIdx.x];
+            S.count[w][threadIdx.x] = static_cast<uint16_t>(total);
+            total += n;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) place[i] = there[i] ? S.base[digit[i]] + S.count[warp][digit[i]] + rank[i] : 0;
+    __syncthreads();
+    if (threadIdx.x < bins) S.base[threadIdx.x] += total;
+}
+// base[d] = (tokens of smaller digits) + ahead[d], from the totals of the digits (a value a thread, 0 from bins on).
+__device__ __forceinline__ void digit_bases(SortShared& S, int bins, int total, int ahead) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int up = total;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+        const int n = __shfl_up_sync(0xffffffffu, up, s);
+        if (lane >= s) up += n;
+    }
+    if (lane == 31) S.part[warp][0] = up;
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < warp; ++w) before += S.part[w][0];
+    if (threadIdx.x < bins) S.base[threadIdx.x] = before + up - total + ahead;
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortParams P) {
+    extern __shared__ unsigned char smem_dyn[];
+    SortShared& S = *reinterpret_cast<SortShared*>(smem_dyn);
+    chain_wait();
+    chain_release();
+    const int bins = 1 << P.bits, shift = P.pass * P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // the digit's tokens in all CTAs and in those ahead of this one, summed by several threads a digit
+    const int d = tid & (bins - 1), parts = kSortThreads >> P.bits, part = tid >> P.bits;
+    const int32_t* const counts = P.counts + static_cast<size_t>(P.pass) * P.blocks * kMaxBins;
+    int all = 0, ahead = 0;
+#pragma unroll 4
+    for (int b = part; b < P.blocks; b += parts) {
+        const int n = __ldcg(counts + static_cast<size_t>(b) * kMaxBins + d);
+        all += n;
+        if (b < static_cast<int>(blockIdx.x)) ahead += n;
+    }
+    S.sum[0][tid] = all;
+    S.sum[1][tid] = ahead;
+    __syncthreads();
+    all = ahead = 0;
+    if (tid < bins)
+        for (int p = 0; p < parts; ++p) {
+            all += S.sum[0][p * bins + tid];
+            ahead += S.sum[1][p * bins + tid];
+        }
+    digit_bases(S, bins, all, ahead);
+    const bool last = P.pass + 1 == P.passes;
+    int32_t* const next = P.counts + static_cast<size_t>(P.pass + 1) * P.blocks * kMaxBins;
+#pragma unroll 1
+    for (int tile = 0; tile < P.tiles_per_block; ++tile) {
+        const long long t0 = (static_cast<long long>(blockIdx.x) * P.tiles_per_block + tile) * kSortTile + warp * (32 * kSortItems) + lane;
+        int key[kSortItems], token[kSortItems], digit[kSortItems], place[kSortItems];
+        bool there[kSortItems];
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            const long long t = t0 + 32 * i;
+            there[i] = t < P.T;
+            key[i] = !there[i] ? 0 : P.pass == 0 ? key_of(P, static_cast<int>(t)) : __ldcg(P.keys + t);
+            token[i] = !there[i] ? 0 : P.pass == 0 ? static_cast<int>(t) : __ldcg(P.tokens + t);
+            digit[i] = (key[i] >> shift) & (bins - 1);
+        }
+        rank_tile(S, bins, digit, there, place);
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            if (!there[i]) continue;
+            P.keys_out[place[i]] = key[i];
+            P.tokens_out[place[i]] = token[i];
+            if (!last) atomicAdd(next + static_cast<size_t>(place[i] / (P.tiles_per_block * kSortTile)) * kMaxBins + ((key[i] >> (shift + P.bits)) & (bins - 1)), 1);
+        }
+        __syncthreads();
+    }
+}
+
+// Up to a tile of tokens: every pass by one CTA.
+__global__ void __launch_bounds__(kSortThreads) embed_sort_small_kernel(const SortParams P) {
+    extern __shared__ unsigned char smem_dyn[];
+    SortShared& S = *reinterpret_cast<SortShared*>(smem_dyn);
+    int* const keys = reinterpret_cast<int*>(smem_dyn + sizeof(SortShared));
+    int* const tokens = keys + kSortTile;
+    chain_wait();
+    chain_release();
+    const int bins = 1 << P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int t0 = warp * (32 * kSortItems) + lane;
+    int key[kSortItems], token[kSortItems], digit[kSortItems], place[kSortItems];
+    bool there[kSortItems];
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        token[i] = t0 + 32 * i;
+        there[i] = token[i] < P.T;
+        key[i] = there[i] ? key_of(P, token[i]) : 0;
+    }
+#pragma unroll 1
+    for (int pass = 0; pass < P.passes; ++pass) {
+        const int shift = pass * P.bits;
+        if (tid < bins) S.base[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) digit[i] = (key[i] >> shift) & (bins - 1);
+        rank_tile(S, bins, digit, there, place);            // places among equal digits; base: how many there are
+        __syncthreads();
+        digit_bases(S, bins, tid < bins ? S.base[tid] : 0, 0);
+        const bool last = pass + 1 == P.passes;
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            if (!there[i]) continue;
+            const int to = place[i] + S.base[digit[i]];
+            (last ? P.keys_out : keys)[to] = key[i];
+            (last ? P.tokens_out : tokens)[to] = token[i];
+        }
+        __syncthreads();
+        if (last) break;
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            if (!there[i]) continue;
+            key[i] = keys[t0 + 32 * i];
+            token[i] = tokens[t0 + 32 * i];
+        }
+        __syncthreads();
+    }
+}
+
+// ---- sums -----------------------------------------------------------------------------------------------------------------------
+struct SumParams {
+    const void* d_out;
+    const int32_t *keys, *tokens;
+    void* d_table;
+    float* pieces;                              // [shares, 2, C]: of the row that a share begins in, of the one that it ends in
+    int T, V, C, lanes, share, shares, share_blocks, accumulate;
+    float scale;
+};
+template <class Tab, int kVec>
+__device__ __forceinline__ void finish_row(const SumParams& P, int v, int c, const float (&sum)[kVec]) {
+    Tab* const at = static_cast<Tab*>(P.d_table) + static_cast<size_t>(v) * P.C + c;
+    Pack<Tab, kVec> old, to;
+    if (P.accumulate) old = load_pack<Tab, kVec>(at);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) to.e[e] = from_float<Tab>(P.accumulate ? fmaf(sum[e], P.scale, to_float(old.e[e])) : sum[e] * P.scale);
+    store_pack(at, to);
+}
+// Whether any of the sorted keys is v.
+__device__ __forceinline__ bool has_key(const int32_t* keys, int n, int v) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (__ldcg(keys + mid) < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo < n && __ldcg(keys + lo) == v;
+}
+template <class Tab, class Out, int kVec>
+__global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParams P) {
+    chain_wait();
+    chain_release();
+    if (static_cast<int>(blockIdx.x) >= P.share_blocks) {            // rows without a token: 32 to a warp
+        if (blockIdx.y != 0) return;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const long long v0 = (static_cast<long long>(blockIdx.x - P.share_blocks) * (kEmbedThreads / 32) + warp) * 32;
+        uint32_t empty = __ballot_sync(0xffffffffu, v0 + lane < P.V && !has_key(P.keys, P.T, static_cast<int>(v0 + lane)));
+        Pack<Tab, kVec> zero;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) zero.e[e] = from_float<Tab>(0.f);
+        while (empty) {
+            const int k = __ffs(empty) - 1;
+            empty &= empty - 1;
+            Tab* const row = static_cast<Tab*>(P.d_table) + static_cast<size_t>(v0 + k) * P.C;
+#pragma unroll 4
+            for (int c = lane * kVec; c < P.C; c += 32 * kVec) store_pack(row + c, zero);
+        }
+        return;
+    }
+    const int groups = kEmbedThreads / P.lanes, group = threadIdx.x / P.lanes, lane = threadIdx.x & (P.lanes - 1);
+    const int share = blockIdx.x * groups + group, c = (blockIdx.y * P.lanes + lane) * kVec;
+    if (share >= P.shares || c >= P.C) return;
+    const long long begin = static_cast<long long>(share) * P.share, end = min(static_cast<long long>(P.T), begin + P.share);
+    const Out* const d_out = static_cast<const Out*>(P.d_out) + c;
+    float* const pieces = P.pieces + static_cast<size_t>(share) * 2 * P.C + c;
+    const int ahead = begin > 0 ? __ldcg(P.keys + begin - 1) : -1, behind = end < P.T ? __ldcg(P.keys + end) : -1;
+    float sum[kVec];
+    int row = -1;                               // that `sum` is of
+    bool first = true;                          // it is the share's first one
+    auto leave = [&](bool at_end) {
+        if (row < 0 || row == P.V) return;
+        const bool from_ahead = first && row == ahead, goes_on = at_end && row == behind;
+        if (!from_ahead && !goes_on) {
+            finish_row<Tab, kVec>(P, row, c, sum);
+            return;
+        }
+        float* const to = pieces + (from_ahead ? 0 : P.C);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) to[e] = sum[e];
+    };
+#pragma unroll 1
+    for (long long i = begin; i < end; i += kSumBatch) {
+        int key[kSumBatch];
+        Pack<Out, kVec> in[kSumBatch];
+#pragma unroll
+        for (int u = 0; u < kSumBatch; ++u) {
+            key[u] = i + u < end ? __ldcg(P.keys + i + u) : P.V;
+            if (key[u] < P.V) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(__ldcg(P.tokens + i + u)) * P.C);
+        }
+#pragma unroll
+        for (int u = 0; u < kSumBatch; ++u) {
+            if (i + u >= end) break;
+            if (key[u] != row) {
+                leave(false);
+                first = row < 0;
+                row = key[u];
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+            }
+            if (row == P.V) continue;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[e] += to_float(in[u].e[e]);
+        }
+        if (row == P.V) return;                 // nothing but tokens without a row behind it (the row ahead is done)
+    }
+    leave(true);
+}
+// Rows in pieces: the share that a row begins in adds them up.
+template <class Tab, int kVec>
+__global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumParams P) {
+    chain_wait();
+    chain_release();
+    const int groups = kEmbedThreads / P.lanes, group = threadIdx.x / P.lanes, lane = threadIdx.x & (P.lanes - 1);
+    const int share = blockIdx.x * groups + group, c = (blockIdx.y * P.lanes + lane) * kVec;
+    if (share + 1 >= P.shares || c >= P.C) return;
+    const long long begin = static_cast<long long>(share) * P.share, end = begin + P.share;
+    const int row = __ldcg(P.keys + end - 1);
+    if (row == P.V || __ldcg(P.keys + end) != row) return;
+    if (begin > 0 && __ldcg(P.keys + begin) == row && __ldcg(P.keys + begin - 1) == row) return;        // begins further ahead
+    const float* at = P.pieces + static_cast<size_t>(share) * 2 * P.C + P.C + c;
+    float sum[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) sum[e] = at[e];
+    int last = share + 1;                       // the share that the row ends in
+    while (last + 1 < P.shares && __ldcg(P.keys + static_cast<long long>(last + 1) * P.share) == row) ++last;
+    at += P.C;
+#pragma unroll 8
+    for (int s = share + 1; s <= last; ++s, at += 2 * P.C)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] += __ldcg(at + e);
+    finish_row<Tab, kVec>(P, row, c, sum);
+}
+
+}  // namespace
+
+int embed_validate(const vardrop_embed_cfg& c) {
+    if (c.T < 1 || c.V < 1 || c.C < 1) return fail(VARDROP_ERR_INVALID_ARG, "embed: T, V, C >= 1 required (T=%d V=%d C=%d)", c.T, c.V, c.C);
+    if (!known_dtype(c.dtype) || !known_dtype(c.out_dtype)) return fail(VARDROP_ERR_INVALID_ARG, "embed: dtype=%d or out_dtype=%d is none of 0, 1, 2", c.dtype, c.out_dtype);
+    if (c.accumulate != 0 && c.accumulate != 1) return fail(VARDROP_ERR_INVALID_ARG, "embed: accumulate=%d is neither 0 nor 1", c.accumulate);
+    if (!(c.scale - c.scale == 0.f)) return fail(VARDROP_ERR_INVALID_ARG, "embed: scale is not finite");
+    if (c.T > (1 << 28) || c.V > (1 << 30) || c.C > (1 << 16)) return fail(VARDROP_ERR_UNSUPPORTED, "embed: T=%d above 2^28, V=%d above 2^30 or C=%d above 65536", c.T, c.V, c.C);
+    return VARDROP_OK;
+}
+
+size_t embed_workspace_bytes(const vardrop_embed_cfg& c) { return embed_layout(c).total; }
+
+int embed_fwd_launch(const void* table, const int32_t* idx, const vardrop_embed_cfg& c, void* out, void* ws, cudaStream_t stream) {
+    const SumPlan u = sum_plan(c);
+    const EmbedParams P{table, idx, out, static_cast<int*>(ws), c.T, c.V, c.C, u.lanes, c.scale};
+    const int groups = kEmbedThreads / u.lanes;
+    // several tokens to a thread only where every SM still gets two CTAs
+    const bool many = c.T >= 4ll * groups * 2 * sm_count();
+    const long long per = static_cast<long long>(groups) * (many ? 4 : 1);
+    const dim3 grid(static_cast<unsigned>((c.T + per - 1) / per));
+    LaunchScope ls_(K_EMBED_FWD, stream);
+    const cudaError_t err = with_dtype(c.dtype, [&](auto tab) {
+        return with_dtype(c.out_dtype, [&](auto o) {
+            return with_vector(u.vec, [&](auto vec) {
+                using Tab = decltype(tab);
+                using Out = decltype(o);
+                constexpr int kVec = decltype(vec)::value;
+                return many ? launch_chained(embed_fwd_kernel<Tab, Out, kVec, 4>, grid, dim3(kEmbedThreads), 0, stream, P)
+                            : launch_chained(embed_fwd_kernel<Tab, Out, kVec, 1>, grid, dim3(kEmbedThreads), 0, stream, P);
+            });
+        });
+    });
+    return check_cuda(err, "embed: forward launch");
+}
+
+int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_cfg& c, void* d_table, void* ws, cudaStream_t stream) {
+    const SortPlan s = sort_plan(c);
+    const SumPlan u = sum_plan(c);
+    const EmbedWs w = embed_layout(c);
+    char* const base = static_cast<char*>(ws);
+    int32_t* const keys[2] = {reinterpret_cast<int32_t*>(base + w.keys[0]), reinterpret_cast<int32_t*>(base + w.keys[1])};
+    int32_t* const tokens[2] = {reinterpret_cast<int32_t*>(base + w.tokens[0]), reinterpret_cast<int32_t*>(base + w.tokens[1])};
+    SortParams S{idx, nullptr, nullptr, keys[0], tokens[0], reinterpret_cast<int32_t*>(base + w.counts), static_cast<int*>(ws), c.T, c.V, s.bits, 0, s.passes, s.blocks, s.tiles_per_block};
+    constexpr int kSmall = static_cast<int>(sizeof(SortShared)) + 2 * kSortTile * static_cast<int>(sizeof(int)), kLarge = static_cast<int>(sizeof(SortShared));
+    static thread_local int attr_dev = -1;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (attr_dev != dev) {
+        if (int st = check_cuda(cudaFuncSetAttribute(embed_sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmall), "embed: smem attribute")) return st;
+        if (int st = check_cuda(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLarge), "embed: smem attribute")) return st;
+        attr_dev = dev;
+    }
+    cudaError_t err;
+    int at = 0;                                 // of the sorted arrays
+    if (c.T <= kSortTile) {
+        LaunchScope ls_(K_EMBED_SORT, stream);
+        err = launch_chained(embed_sort_small_kernel, dim3(1), dim3(kSortThreads), kSmall, stream, S);
+        if (int st = check_cuda(err, "embed: sort launch")) return st;
+    } else {
+        { LaunchScope ls_(K_EMBED_COUNT, stream); err = launch_chained(embed_count_kernel, dim3(s.blocks), dim3(kSortThreads), 0, stream, S); }
+        if (int st = check_cuda(err, "embed: count launch")) return st;
+        for (S.pass = 0; S.pass < s.passes; ++S.pass) {
+            at = S.pass & 1;
+            S.keys = keys[at ^ 1]; S.tokens = tokens[at ^ 1];
+            S.keys_out = keys[at]; S.tokens_out = tokens[at];
+            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_chained(embed_sort_kernel, dim3(s.blocks), dim3(kSortThreads), kLarge, stream, S); }
+            if (int st = check_cuda(err, "embed: sort launch")) return st;
+        }
+    }
+    SumParams P{d_out, keys[at], tokens[at], d_table, reinterpret_cast<float*>(base + w.pieces), c.T, c.V, c.C, u.lanes, u.share, u.shares, 0, c.accumulate, c.scale};
+    const int groups = kEmbedThreads / u.lanes;
+    P.share_blocks = (u.shares + groups - 1) / groups;
+    const int zero_blocks = c.accumulate ? 0 : (c.V + kEmbedThreads - 1) / kEmbedThreads;
+    {
+        LaunchScope ls_(K_EMBED_SUM, stream);
+        err = with_dtype(c.dtype, [&](auto tab) {
+            return with_dtype(c.out_dtype, [&](auto o) {
+                return with_vector(u.vec, [&](auto vec) {
+                    return launch_chained(embed_sum_kernel<decltype(tab), decltype(o), decltype(vec)::value>, dim3(P.share_blocks + zero_blocks, u.slabs), dim3(kEmbedThreads), 0, stream, P);
+                });
+            });
+        });
+    }
+    if (int st = check_cuda(err, "embed: sum launch")) return st;
+    if (u.shares == 1) return VARDROP_OK;
+    {
+        LaunchScope ls_(K_EMBED_JOIN, stream);
+        err = with_dtype(c.dtype, [&](auto tab) {
+            return with_vector(u.vec, [&](auto vec) { return launch_chained(embed_join_kernel<decltype(tab), decltype(vec)::value>, dim3(P.share_blocks, u.slabs), dim3(kEmbedThreads), 0, stream, P); });
+        });
+    }
+    return check_cuda(err, "embed: join launch");
+}
+
+}  // namespace vardrop

@@ -13,6 +13,7 @@ namespace vardrop {
 enum KernelId {
     K_HASH = 0, K_SELECT_SMALL, K_SELECT_COUNT, K_SELECT_GROUP, K_SELECT_SAMPLE, K_ATTN_FWD, K_BWD_PREP, K_ATTN_BWD, K_BWD_CONVERT, K_PEARSON_NORM, K_PEARSON_MAX, K_GATHER_ROWS,
     K_SELECT_PLACE, K_SELECT_CLUSTER, K_PACKED_PLAN, K_PACKED_FWD, K_PACKED_TILE, K_PACKED_SHORT, K_PACKED_PREP, K_PACKED_BWD, K_PACKED_CONVERT, K_NORM_FWD, K_NORM_BWD, K_NORM_PARAMS, K_GRAD_NORM, K_GRAD_SCALE,
+    K_EMBED_FWD, K_EMBED_COUNT, K_EMBED_SORT, K_EMBED_SUM, K_EMBED_JOIN, K_ACT_FWD, K_ACT_BWD,
     K_COUNT
 };
 // Wrap a kernel launch: counts it and, when the timer is armed, brackets it with a pair of CUDA events on `stream`.
@@ -99,5 +100,17 @@ int norm_bwd_launch(const void* x, const void* y, const float* gate, const float
 size_t grad_clip_workspace_bytes();
 int grad_clip_validate(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg& cfg);
 int grad_clip_launch(const vardrop_tensor* tensors, int32_t count, const vardrop_clip_cfg& cfg, float* norm, void* ws, cudaStream_t stream);
+
+// embed.cu
+int embed_validate(const vardrop_embed_cfg& cfg);
+size_t embed_workspace_bytes(const vardrop_embed_cfg& cfg);
+int embed_fwd_launch(const void* table, const int32_t* idx, const vardrop_embed_cfg& cfg, void* out, void* ws, cudaStream_t stream);
+int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_cfg& cfg, void* d_table, void* ws, cudaStream_t stream);
+
+// act.cu
+int act_validate(const vardrop_act_cfg& cfg);
+size_t act_ckpt_bytes(const vardrop_act_cfg& cfg);
+int act_fwd_launch(const void* a, const void* b, const int32_t* n_sel, const vardrop_act_cfg& cfg, void* y, void* ckpt, cudaStream_t stream);
+int act_bwd_launch(const void* d_y, const void* ckpt, const int32_t* n_sel, const vardrop_act_cfg& cfg, void* d_a, void* d_b, void* y, cudaStream_t stream);
 
 }  // namespace vardrop

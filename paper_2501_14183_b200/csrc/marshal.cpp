@@ -63,6 +63,16 @@ struct Args {
             return refuse<void>("%s does not have the shape and strides of the configuration", name);
         return p;
     }
+    // a branch of an activation: [B, N, C] with the row stride of the configuration
+    void* branch(int i, const char* name, const vardrop_act_cfg& c, at::ScalarType type) {
+        void* const p = checked(i, name, type, static_cast<int64_t>(c.B) * c.N * c.C, c.stride == 0 ? kContiguous : kStrided);
+        if (!p || c.stride == 0) return p;
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (t.dim() != 3 || t.size(0) != c.B || t.size(1) != c.N || t.size(2) != c.C || (c.N > 1 && t.stride(1) != c.stride) || (c.B > 1 && t.stride(0) != c.N * c.stride) ||
+            (c.C > 1 && t.stride(2) != 1))
+            return refuse<void>("%s does not have the shape and strides of the configuration", name);
+        return p;
+    }
     template <typename T>
     T* refuse(const char* text, const char* name) {
         PyErr_Format(PyExc_ValueError, text, name);
@@ -330,10 +340,66 @@ PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return finish(g, [=](void* s) { return vardrop_grad_clip(tensors, static_cast<int32_t>(count), cfg, norm, ws, nb, s); });
     });
 }
+PyObject* embed_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<5>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_embed_cfg>(2);
+        if (!g.ok) return nullptr;
+        const int64_t T = cfg->T, V = cfg->V, C = cfg->C;
+        const void* const table = g.checked(0, "table", type_of(cfg->dtype), V * C);
+        const auto idx = g.checked<const int32_t>(1, "idx", at::kInt, T);
+        void* const out = g.checked(3, "out", type_of(cfg->out_dtype), T * C);
+        void* const ws = g.checked(4, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(4) : 0;
+        return finish(g, [=](void* s) { return vardrop_embed_fwd(table, idx, cfg, out, ws, nb, s); });
+    });
+}
+PyObject* embed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<5>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_embed_cfg>(2);
+        if (!g.ok) return nullptr;
+        const int64_t T = cfg->T, V = cfg->V, C = cfg->C;
+        const void* const d_out = g.checked(0, "d_out", type_of(cfg->out_dtype), T * C);
+        const auto idx = g.checked<const int32_t>(1, "idx", at::kInt, T);
+        void* const d_table = g.checked(3, "d_table", type_of(cfg->dtype), V * C);
+        void* const ws = g.checked(4, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(4) : 0;
+        return finish(g, [=](void* s) { return vardrop_embed_bwd(d_out, idx, cfg, d_table, ws, nb, s); });
+    });
+}
+PyObject* act_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<6>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_act_cfg>(3);
+        if (!g.ok) return nullptr;
+        const at::ScalarType ty = type_of(cfg->dtype);
+        const void* const in = g.branch(0, "a", *cfg, ty);
+        const void* const gate = g.branch(1, "b", *cfg, ty);
+        const auto n_sel = g.checked<const int32_t>(2, "n_sel", at::kInt, cfg->S > 1 ? cfg->S : 1);
+        void* const y = g.checked(4, "y", ty, static_cast<int64_t>(cfg->B) * cfg->N * cfg->C);
+        void* const ckpt = g.checked(5, "ckpt", at::kByte, 0);
+        const size_t nb = g.ok && ckpt ? g.bytes(5) : 0;
+        return finish(g, [=](void* s) { return vardrop_act_fwd(in, gate, n_sel, cfg, y, ckpt, nb, s); });
+    });
+}
+PyObject* act_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<7>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_act_cfg>(3);
+        if (!g.ok) return nullptr;
+        const at::ScalarType ty = type_of(cfg->dtype);
+        const int64_t all = static_cast<int64_t>(cfg->B) * cfg->N * cfg->C;
+        const void* const d_y = g.checked(0, "d_y", ty, all);
+        const void* const ckpt = g.checked(1, "ckpt", at::kByte, 0);
+        const auto n_sel = g.checked<const int32_t>(2, "n_sel", at::kInt, cfg->S > 1 ? cfg->S : 1);
+        void* const d_a = g.branch(4, "d_a", *cfg, ty);
+        void* const d_b = g.branch(5, "d_b", *cfg, ty);
+        void* const y = g.checked(6, "y", ty, all);
+        const size_t nb = g.ok && ckpt ? g.bytes(1) : 0;
+        return finish(g, [=](void* s) { return vardrop_act_bwd(d_y, ckpt, nb, n_sel, cfg, d_a, d_b, y, s); });
+    });
+}
 
 #define VD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VD_METHOD(hash), VD_METHOD(select), VD_METHOD(select_static), VD_METHOD(gather_rows), VD_METHOD(attn_fwd), VD_METHOD(attn_bwd),
-                           VD_METHOD(pearson_max), VD_METHOD(packed_plan), VD_METHOD(attn_packed_fwd), VD_METHOD(attn_packed_bwd), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), {nullptr, nullptr, 0, nullptr}};
+                           VD_METHOD(pearson_max), VD_METHOD(packed_plan), VD_METHOD(attn_packed_fwd), VD_METHOD(attn_packed_bwd), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), VD_METHOD(embed_fwd), VD_METHOD(embed_bwd), VD_METHOD(act_fwd), VD_METHOD(act_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -50,7 +50,8 @@ std::vector<std::pair<cudaEvent_t, cudaEvent_t>> g_prof_free;              // pa
 const char* const g_kernel_names[K_COUNT] = {"hash_kernel", "select_small_kernel", "select_count_kernel", "select_group_kernel", "select_sample_kernel",
                                              "attn_fwd_kernel", "bwd_prep_kernel", "attn_bwd_kernel", "bwd_convert_kernel", "pearson_normalize_kernel",
                                              "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel", "packed_plan_kernel",
-                                             "attn_packed_fwd_kernel", "attn_packed_tile_kernel", "packed_short_kernel", "packed_prep_kernel", "attn_packed_bwd_kernel", "packed_convert_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel"};
+                                             "attn_packed_fwd_kernel", "attn_packed_tile_kernel", "packed_short_kernel", "packed_prep_kernel", "attn_packed_bwd_kernel", "packed_convert_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel",
+                                             "embed_fwd_kernel", "embed_count_kernel", "embed_sort_kernel", "embed_sum_kernel", "embed_join_kernel", "act_fwd_kernel", "act_bwd_kernel"};
 }  // namespace
 
 LaunchScope::LaunchScope(int id, cudaStream_t stream) : id_(id), stream_(stream), stop_(nullptr) {
@@ -456,6 +457,113 @@ int vardrop_grad_clip(const vardrop_tensor* tensors, int32_t count, const vardro
     VD_CHECK(check_ptr(norm, "norm", true));
     VD_CHECK(check_ws(ws, ws_bytes, grad_clip_workspace_bytes()));
     return grad_clip_launch(tensors, count, *cfg, norm, ws, static_cast<cudaStream_t>(stream));
+}
+
+// Buffers of a call that overlap: rows of `cols` elements, `stride` apart.  Views of one tensor whose rows lie between each other's do not.
+struct Rows {
+    const void* p;
+    size_t rows, cols, stride, size;            // size: of an element
+    const char* name;
+};
+static Rows flat(const void* p, size_t n, size_t size, const char* name) { return Rows{p, 1, n, n, size, name}; }
+static bool rows_overlap(const Rows& x, const Rows& y) {
+    if (!x.p || !y.p || x.rows * x.cols == 0 || y.rows * y.cols == 0) return false;
+    const uintptr_t px = reinterpret_cast<uintptr_t>(x.p), py = reinterpret_cast<uintptr_t>(y.p);
+    const size_t nx = ((x.rows - 1) * x.stride + x.cols) * x.size, ny = ((y.rows - 1) * y.stride + y.cols) * y.size;
+    if (px >= py + ny || py >= px + nx) return false;
+    if (x.stride != y.stride || x.size != y.size) return true;
+    const size_t step = x.stride * x.size, r = (px < py ? py - px : px - py) % step, first = px < py ? x.cols : y.cols, second = px < py ? y.cols : x.cols;
+    return !(r >= first * x.size && r + second * x.size <= step);
+}
+// An output may begin where an input of the same rows does where `same` says so: it is written by the threads that have read it.
+static int overlap_check(const char* call, const Rows* ins, int n_ins, const Rows* outs, int n_outs, bool same) {
+    for (int o = 0; o < n_outs; ++o) {
+        for (int i = 0; i < n_ins; ++i)
+            if (rows_overlap(outs[o], ins[i]) &&
+                !(same && outs[o].p == ins[i].p && outs[o].rows == ins[i].rows && outs[o].cols == ins[i].cols && outs[o].stride == ins[i].stride && outs[o].size == ins[i].size))
+                return fail(VARDROP_ERR_INVALID_ARG, "%s: %s and %s overlap", call, outs[o].name, ins[i].name);
+        for (int i = 0; i < o; ++i)
+            if (rows_overlap(outs[o], outs[i])) return fail(VARDROP_ERR_INVALID_ARG, "%s: %s and %s overlap", call, outs[o].name, outs[i].name);
+    }
+    return VARDROP_OK;
+}
+static size_t elem_bytes(int dtype) { return dtype == 2 ? 4 : 2; }
+
+size_t vardrop_embed_workspace_bytes(const vardrop_embed_cfg* cfg) {
+    if (!cfg || embed_validate(*cfg) != VARDROP_OK) return 0;
+    return embed_workspace_bytes(*cfg);
+}
+
+int vardrop_embed_fwd(const void* table, const int32_t* idx, const vardrop_embed_cfg* cfg, void* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(embed_validate(*cfg));
+    VD_CHECK(check_ptr(table, "table", true));
+    VD_CHECK(check_ptr(idx, "idx", true));
+    VD_CHECK(check_ptr(out, "out", true));
+    VD_CHECK(check_ws(ws, ws_bytes, kWsHeaderBytes));
+    const size_t C = cfg->C;
+    const Rows ins[] = {flat(table, cfg->V * C, elem_bytes(cfg->dtype), "table"), flat(idx, cfg->T, 4, "idx"), flat(ws, kWsHeaderBytes, 1, "ws")};
+    const Rows outs[] = {flat(out, cfg->T * C, elem_bytes(cfg->out_dtype), "out")};
+    VD_CHECK(overlap_check("embed", ins, 3, outs, 1, false));
+    return embed_fwd_launch(table, idx, *cfg, out, ws, static_cast<cudaStream_t>(stream));
+}
+
+int vardrop_embed_bwd(const void* d_out, const int32_t* idx, const vardrop_embed_cfg* cfg, void* d_table, void* ws, size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(embed_validate(*cfg));
+    VD_CHECK(check_ptr(d_out, "d_out", true));
+    VD_CHECK(check_ptr(idx, "idx", true));
+    VD_CHECK(check_ptr(d_table, "d_table", true));
+    VD_CHECK(check_ws(ws, ws_bytes, embed_workspace_bytes(*cfg)));
+    const size_t C = cfg->C;
+    const Rows ins[] = {flat(d_out, cfg->T * C, elem_bytes(cfg->out_dtype), "d_out"), flat(idx, cfg->T, 4, "idx")};
+    const Rows outs[] = {flat(d_table, cfg->V * C, elem_bytes(cfg->dtype), "d_table"), flat(ws, embed_workspace_bytes(*cfg), 1, "ws")};
+    VD_CHECK(overlap_check("embed", ins, 2, outs, 2, false));
+    return embed_bwd_launch(d_out, idx, *cfg, d_table, ws, static_cast<cudaStream_t>(stream));
+}
+
+size_t vardrop_act_ckpt_bytes(const vardrop_act_cfg* cfg) {
+    if (!cfg || act_validate(*cfg) != VARDROP_OK) return 0;
+    return act_ckpt_bytes(*cfg);
+}
+
+static int check_ckpt(const void* ckpt, size_t have, const vardrop_act_cfg& cfg) {
+    if (int st = check_ptr(ckpt, "ckpt", true)) return st;
+    if (have < act_ckpt_bytes(cfg)) return fail(VARDROP_ERR_WORKSPACE, "checkpoint of %zu bytes given, %zu needed", have, act_ckpt_bytes(cfg));
+    return VARDROP_OK;
+}
+
+int vardrop_act_fwd(const void* a, const void* b, const int32_t* n_sel, const vardrop_act_cfg* cfg, void* y, void* ckpt, size_t ckpt_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(act_validate(*cfg));
+    VD_CHECK(check_ptr(a, "a", true));
+    if ((b != nullptr) != (cfg->gated != 0)) return fail(VARDROP_ERR_INVALID_ARG, "act: gated=%d and b %s", cfg->gated, b ? "given" : "NULL");
+    VD_CHECK(check_ptr(b, "b", false));
+    VD_CHECK(check_ptr(n_sel, "n_sel", false));
+    VD_CHECK(check_ptr(y, "y", true));
+    if (ckpt) VD_CHECK(check_ckpt(ckpt, ckpt_bytes, *cfg));
+    const size_t rows = static_cast<size_t>(cfg->B) * cfg->N, C = cfg->C, stride = cfg->stride ? cfg->stride : C, size = elem_bytes(cfg->dtype);
+    const Rows ins[] = {{a, rows, C, stride, size, "a"}, {b, rows, C, stride, size, "b"}, flat(n_sel, cfg->S > 1 ? cfg->S : 1, 4, "n_sel")};
+    const Rows outs[] = {{y, rows, C, C, size, "y"}, flat(ckpt, ckpt ? act_ckpt_bytes(*cfg) : 0, 1, "ckpt")};
+    VD_CHECK(overlap_check("act", ins, 3, outs, 2, true));
+    return act_fwd_launch(a, b, n_sel, *cfg, y, ckpt, static_cast<cudaStream_t>(stream));
+}
+
+int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const int32_t* n_sel, const vardrop_act_cfg* cfg, void* d_a, void* d_b, void* y, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(act_validate(*cfg));
+    VD_CHECK(check_ptr(d_y, "d_y", true));
+    VD_CHECK(check_ckpt(ckpt, ckpt_bytes, *cfg));
+    VD_CHECK(check_ptr(n_sel, "n_sel", false));
+    VD_CHECK(check_ptr(d_a, "d_a", true));
+    if ((d_b != nullptr) != (cfg->gated != 0)) return fail(VARDROP_ERR_INVALID_ARG, "act: gated=%d and d_b %s", cfg->gated, d_b ? "given" : "NULL");
+    VD_CHECK(check_ptr(d_b, "d_b", false));
+    VD_CHECK(check_ptr(y, "y", false));
+    const size_t rows = static_cast<size_t>(cfg->B) * cfg->N, C = cfg->C, stride = cfg->stride ? cfg->stride : C, size = elem_bytes(cfg->dtype);
+    const Rows ins[] = {{d_y, rows, C, C, size, "d_y"}, flat(ckpt, act_ckpt_bytes(*cfg), 1, "ckpt"), flat(n_sel, cfg->S > 1 ? cfg->S : 1, 4, "n_sel")};
+    const Rows outs[] = {{d_a, rows, C, stride, size, "d_a"}, {d_b, rows, C, stride, size, "d_b"}, {y, rows, C, C, size, "y"}};
+    VD_CHECK(overlap_check("act", ins, 3, outs, 3, true));
+    return act_bwd_launch(d_y, ckpt, n_sel, *cfg, d_a, d_b, y, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"
