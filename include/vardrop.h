@@ -15,6 +15,7 @@
  *   vardrop_grad_clip               global gradient norm over many tensors, and clipping
  *   vardrop_embed_fwd, _bwd         token embeddings by index, and the table's gradient
  *   vardrop_act_fwd, _bwd           the feed-forward's activation, gated or not, with a checkpoint in 8 bits that the backward pass works from
+ *   vardrop_loss_fwd, _bwd          softmax cross entropy over a vocabulary, without the logits in memory, and its gradients
  *
  * Conventions shared by every entry point
  *   - Pointers named in the argument lists are DEVICE pointers unless the comment says "host".
@@ -452,6 +453,33 @@ typedef struct {
 size_t vardrop_act_ckpt_bytes(const vardrop_act_cfg* cfg);
 int vardrop_act_fwd(const void* a, const void* b, const int32_t* n_sel, const vardrop_act_cfg* cfg, void* y, void* ckpt, size_t ckpt_bytes, void* stream);
 int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const int32_t* n_sel, const vardrop_act_cfg* cfg, void* d_a, void* d_b, void* y, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Softmax cross entropy over a vocabulary (no counterpart in the paper), without the logits in memory:
+ *   l_tv = scale h[t] . w[v];   lse[t] = log sum_v exp(l_tv);   loss[t] = lse[t] - l_t,label[t];   both 0 where label[t] < 0
+ * Backward, with G_tv = d_loss[t] scale (exp(l_tv - lse[t]) - [v = label[t]]), 0 where label[t] < 0:
+ *   d_h[t] = sum_v G_tv w[v];   d_w[v] = sum_t G_tv h[t]
+ * The logits are worked out again, a piece of the vocabulary at a time; of these G is held, in 16 bits.  Tokens without a label (dropped variates, padding) take no part in any product: what lies in their
+ * rows of h, lse and d_loss does not matter.
+ *
+ * cfg (host)  T tokens and V classes (at most 2^24 each, T V at most 2^46), C channels (a multiple of 8, at most 65536); dtype of h, w and their gradients: 0 bf16, 1 fp16; scale up to 1e30 (0 selects 1).
+ * h           [T, C].     w   [V, C].     labels   [T] int32; negative: none.  A label from V on is taken as none, and reported: device status VARDROP_ERR_INVALID_ARG.
+ * loss, lse   [T] fp32 out.
+ * d_loss      [T] fp32, gradient of loss (1 / labelled tokens for their mean).
+ * d_h         [T, C] out, zeros where there is no label; d_w   [V, C] out, every row written.  Either may be NULL (not wanted).
+ * ws          scratch of vardrop_loss_workspace_bytes, for both calls.  Nothing is kept in it from one to the other.
+ * Products of 16-bit operands with fp32 sums; G is rounded to 16 bits ahead of its products, times a power of two that keeps it in the type's range (a token whose |d_loss| is below 2^-24 of the largest one's
+ * loses precision in fp16).  The weights of a token come from lse, whose 24 bits leave them open by about 2^-24 |lse| of themselves: with a finite |lse| above 2^16 the device status is VARDROP_ERR_UNSUPPORTED.
+ * Values of a labelled token's row that are not finite reach its own loss and d_h, and d_w.  All results are bit-reproducible.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t T, V, C, dtype;
+    float scale;
+} vardrop_loss_cfg;
+
+size_t vardrop_loss_workspace_bytes(const vardrop_loss_cfg* cfg);
+int vardrop_loss_fwd(const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg* cfg, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+int vardrop_loss_bwd(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg* cfg, void* d_h, void* d_w, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -66,6 +66,10 @@ class ActCfg(C.Structure):
                 ("stride", C.c_int64)]         # elements from row to row of a, b, d_a, d_b; 0 = C
 
 
+class LossCfg(C.Structure):
+    _fields_ = [("T", C.c_int32), ("V", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2
@@ -83,7 +87,7 @@ EXPORTS = ("vardrop_status_string", "vardrop_last_error", "vardrop_version", "va
            "vardrop_attn_bwd", "vardrop_pearson_workspace_bytes", "vardrop_pearson_max", "vardrop_packed_plan_bytes", "vardrop_packed_plan",
            "vardrop_attn_packed_workspace_bytes", "vardrop_attn_packed_fwd", "vardrop_attn_packed_bwd", "vardrop_norm_fwd", "vardrop_norm_workspace_bytes", "vardrop_norm_bwd",
            "vardrop_grad_clip_workspace_bytes", "vardrop_grad_clip", "vardrop_embed_workspace_bytes", "vardrop_embed_fwd", "vardrop_embed_bwd", "vardrop_act_ckpt_bytes",
-           "vardrop_act_fwd", "vardrop_act_bwd", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
+           "vardrop_act_fwd", "vardrop_act_bwd", "vardrop_loss_workspace_bytes", "vardrop_loss_fwd", "vardrop_loss_bwd", "vardrop_launch_count", "vardrop_profile_enable", "vardrop_profile_kernels",
            "vardrop_profile_kernel_name", "vardrop_profile_read")
 
 
@@ -99,7 +103,8 @@ def load() -> C.CDLL:
         lib.vardrop_status_string.argtypes = [C.c_int]
         for name in ("vardrop_hash_workspace_bytes", "vardrop_select_workspace_bytes", "vardrop_attn_workspace_bytes",
                      "vardrop_pearson_workspace_bytes", "vardrop_norm_workspace_bytes", "vardrop_packed_plan_bytes",
-                     "vardrop_attn_packed_workspace_bytes", "vardrop_embed_workspace_bytes", "vardrop_act_ckpt_bytes"):
+                     "vardrop_attn_packed_workspace_bytes", "vardrop_embed_workspace_bytes", "vardrop_act_ckpt_bytes",
+                     "vardrop_loss_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
             getattr(lib, name).argtypes = [C.c_void_p]
         lib.vardrop_ws_status.restype = C.c_int
@@ -139,6 +144,9 @@ def load() -> C.CDLL:
         lib.vardrop_act_fwd.restype = lib.vardrop_act_bwd.restype = C.c_int
         lib.vardrop_act_fwd.argtypes = [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
         lib.vardrop_act_bwd.argtypes = [C.c_void_p] * 2 + [C.c_size_t] + [C.c_void_p] * 6
+        lib.vardrop_loss_fwd.restype = lib.vardrop_loss_bwd.restype = C.c_int
+        lib.vardrop_loss_fwd.argtypes = [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
+        lib.vardrop_loss_bwd.argtypes = [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
         lib.vardrop_launch_count.restype = C.c_longlong
         lib.vardrop_profile_kernel_name.restype = C.c_char_p
         lib.vardrop_profile_kernel_name.argtypes = [C.c_int]
@@ -289,6 +297,18 @@ def vardrop_act_fwd(a, b, n_sel, cfg: ActCfg, y, ckpt) -> None:
 
 def vardrop_act_bwd(d_y, ckpt, n_sel, cfg: ActCfg, d_a, d_b, y) -> None:
     _check((_marshal or _load_marshal()).act_bwd(d_y, ckpt, n_sel, cfg, d_a, d_b, y), "vardrop_act_bwd")
+
+
+def vardrop_loss_workspace_bytes(cfg: LossCfg) -> int:
+    return int(load().vardrop_loss_workspace_bytes(C.byref(cfg)))
+
+
+def vardrop_loss_fwd(h, w, labels, cfg: LossCfg, loss, lse, ws) -> None:
+    _check((_marshal or _load_marshal()).loss_fwd(h, w, labels, cfg, loss, lse, ws), "vardrop_loss_fwd")
+
+
+def vardrop_loss_bwd(h, w, labels, lse, d_loss, cfg: LossCfg, d_h, d_w, ws) -> None:
+    _check((_marshal or _load_marshal()).loss_bwd(h, w, labels, lse, d_loss, cfg, d_h, d_w, ws), "vardrop_loss_bwd")
 
 
 def vardrop_launch_count() -> int:

@@ -12,7 +12,7 @@ CSRC = HERE / "csrc"
 LIB = HERE / "libvardrop.so"
 MARSHAL = HERE / "_marshal.so"
 SOURCES = ["vardrop_api.cu", "hash.cu", "hash_rows.cu", "hash_dft.cu", "select.cu", "attn_fwd.cu", "attn_bwd.cu", "attn_bwd_many.cu", "pearson.cu", "gather_rows.cu",
-           "packed_plan.cu", "attn_packed_fwd.cu", "attn_packed_bwd.cu", "norm.cu", "norm_bf16.cu", "norm_fp16.cu", "norm_fp32.cu", "grad_clip.cu", "embed.cu", "act.cu"]
+           "packed_plan.cu", "attn_packed_fwd.cu", "attn_packed_bwd.cu", "norm.cu", "norm_bf16.cu", "norm_fp16.cu", "norm_fp32.cu", "grad_clip.cu", "embed.cu", "act.cu", "loss.cu"]
 
 
 def _nvcc() -> str:

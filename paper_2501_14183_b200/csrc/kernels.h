@@ -14,6 +14,7 @@ enum KernelId {
     K_HASH = 0, K_SELECT_SMALL, K_SELECT_COUNT, K_SELECT_GROUP, K_SELECT_SAMPLE, K_ATTN_FWD, K_BWD_PREP, K_ATTN_BWD, K_BWD_CONVERT, K_PEARSON_NORM, K_PEARSON_MAX, K_GATHER_ROWS,
     K_SELECT_PLACE, K_SELECT_CLUSTER, K_PACKED_PLAN, K_PACKED_FWD, K_PACKED_TILE, K_PACKED_SHORT, K_PACKED_PREP, K_PACKED_BWD, K_PACKED_CONVERT, K_NORM_FWD, K_NORM_BWD, K_NORM_PARAMS, K_GRAD_NORM, K_GRAD_SCALE,
     K_EMBED_FWD, K_EMBED_COUNT, K_EMBED_SORT, K_EMBED_SUM, K_EMBED_JOIN, K_ACT_FWD, K_ACT_BWD,
+    K_LOSS_ROWS, K_LOSS_PACK, K_LOSS_STATS, K_LOSS_JOIN, K_LOSS_GRAD, K_LOSS_DH, K_LOSS_DW, K_LOSS_REST, K_LOSS_SUM,
     K_COUNT
 };
 // Wrap a kernel launch: counts it and, when the timer is armed, brackets it with a pair of CUDA events on `stream`.
@@ -112,5 +113,11 @@ int act_validate(const vardrop_act_cfg& cfg);
 size_t act_ckpt_bytes(const vardrop_act_cfg& cfg);
 int act_fwd_launch(const void* a, const void* b, const int32_t* n_sel, const vardrop_act_cfg& cfg, void* y, void* ckpt, cudaStream_t stream);
 int act_bwd_launch(const void* d_y, const void* ckpt, const int32_t* n_sel, const vardrop_act_cfg& cfg, void* d_a, void* d_b, void* y, cudaStream_t stream);
+
+// loss.cu
+int loss_validate(const vardrop_loss_cfg& cfg);
+size_t loss_workspace_bytes(const vardrop_loss_cfg& cfg);
+int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& cfg, float* loss, float* lse, void* ws, cudaStream_t stream);
+int loss_bwd_launch(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg& cfg, void* d_h, void* d_w, void* ws, cudaStream_t stream);
 
 }  // namespace vardrop

@@ -1,0 +1,679 @@
+// Softmax cross entropy over a vocabulary, logits l = scale h w^T, without the logits in memory:
+//   lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,label;      G = g_t scale (exp(l_tv - lse_t) - [v = label]),  d_h = G w,  d_w = G^T h
+//
+// loss_rows_kernel    tokens that have a label, one behind the other: positions, labels, and backward lse and the factor of their rows.  Only these take part in any product.
+// loss_pack_kernel    their rows of h, where some tokens have none.
+// loss_stats_kernel   products of 256 tokens x 256 rows of w; of each row of a tile the maximum and the sum of exponentials go to memory, and the label's logit.
+// loss_join_kernel    lse and loss from these.
+// loss_grad_kernel    backward, for a piece of the vocabulary at a time: the same products again, G of the piece to memory in 16 bits.
+// loss_dh_kernel      d_h += G w[piece] in fp32;      loss_dw_kernel   d_w[piece] = G^T h.
+// loss_rest_kernel, loss_sum_kernel   d_h, rounded, to the tokens' places (zeros without a label); parts of d_w, where its products were split along the tokens.
+//
+// Bound: the tensor cores, 2 T V C flop forward and 6 T V C backward (2 of them the logits again: to keep them would take 2 T V bytes), and for few tokens reading w.
+#include <type_traits>
+
+#include "attn_common.cuh"
+#include "pair_mma.cuh"
+#include "vec_io.cuh"
+
+namespace vardrop {
+
+namespace {
+
+constexpr int kPairTile = 256, kHalfTile = 128;      // rows and columns of a tile; a CTA's rows
+constexpr int kChunk = 64;                           // of the contracted axis in a stage: 128 bytes
+constexpr int kBoxBytes = 64 * 64 * 2;               // what a copy brings
+constexpr int kStageBytes = 4 * kBoxBytes;           // two boxes of either operand
+constexpr int kStages = 6;
+constexpr int kPairThreads = 384;
+constexpr int kPairSmemBytes = 1024 + 1024 + kStages * kStageBytes;
+constexpr uint32_t kPairTmemCols = 512;              // two accumulators of 256 columns
+constexpr int kGroupRows = 8;                        // row tiles that neighbouring pairs share out among each other
+constexpr size_t kPieceBytes = 256u << 20;           // of G; larger pieces make fewer passes over d_h
+constexpr int kLeastPiece = 1024, kMostSplits = 16, kSplitChunks = 4;
+constexpr float kLog2e = 1.4426950408889634f;
+
+enum LossWord { kLossRows = 16, kLossFactor, kLossInverse };      // words of the workspace's header: labelled tokens; the power of two that G is scaled by, and its inverse
+
+int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+
+// ---- layout ---------------------------------------------------------------------------------------------------------------------
+struct LossPlan {
+    int rows;                   // T up to whole tiles
+    int piece, pieces;          // columns of G
+    int dh_splits, dw_splits;
+    size_t place, pos, label, lse, factor, target, packed, part, g, dh, dw, total;
+};
+LossPlan loss_plan(const vardrop_loss_cfg& c) {
+    LossPlan p{};
+    p.rows = ceil_div(c.T, kPairTile) * kPairTile;
+    const long long all = static_cast<long long>(ceil_div(c.V, kPairTile)) * kPairTile;
+    const long long fit = static_cast<long long>(kPieceBytes / (2ull * p.rows)) / kPairTile * kPairTile;
+    p.piece = static_cast<int>(all < (fit > kLeastPiece ? fit : kLeastPiece) ? all : (fit > kLeastPiece ? fit : kLeastPiece));
+    p.pieces = ceil_div(c.V, p.piece);
+    const int pairs = sm_count() / 2, tn = ceil_div(c.C, kPairTile);
+    // too few tiles for the SMs: parts of the contracted axis, added up in a fixed order afterwards
+    const auto splits = [&](long long tiles, long long chunks) {
+        long long s = tiles < pairs ? pairs / tiles : 1;
+        if (s > chunks / kSplitChunks) s = chunks / kSplitChunks;
+        return static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
+    };
+    p.dh_splits = splits(static_cast<long long>(p.rows / kPairTile) * tn, p.piece / kChunk);
+    p.dw_splits = splits(static_cast<long long>(p.piece / kPairTile) * tn, ceil_div(c.T, kChunk));
+    size_t o = align_up(kWsHeaderBytes, 1024);
+    const auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 1024); return at; };
+    const size_t T = c.T, C = c.C, rows = p.rows;
+    p.place = take(4 * T); p.pos = take(4 * T); p.label = take(4 * T); p.lse = take(4 * T); p.factor = take(4 * T); p.target = take(4 * T);
+    p.packed = take(2 * rows * C);
+    const size_t shared = o;                            // forward and backward each have their own from here on
+    p.part = take(8 * rows * 2 * ceil_div(c.V, kPairTile));
+    const size_t forward = o;
+    o = shared;
+    p.g = take(2 * rows * p.piece);
+    p.dh = take(4 * rows * C * p.dh_splits);
+    p.dw = p.dw_splits > 1 ? take(4ull * p.piece * C * p.dw_splits) : o;
+    p.total = o > forward ? o : forward;
+    return p;
+}
+
+// ---- labelled tokens -----------------------------------------------------------------------------------------------------------
+struct RowsParams {
+    const int32_t* labels;
+    const float *lse, *d_loss;                          // backward
+    float *loss, *lse_out;                              // forward: zeros where there is no label
+    int32_t *place, *pos, *label;                       // token of a row; row of a token, or -1; label of a row
+    float *row_lse, *factor;
+    int* header;
+    int T, V;
+};
+constexpr int kRowsThreads = 1024;
+__global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParams P) {
+    __shared__ int warps[32];
+    __shared__ float most[32];
+    chain_wait();
+    chain_release();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int ahead = 0;
+    float top = 0.f;
+#pragma unroll 1
+    for (long long t0 = 0; t0 < P.T; t0 += kRowsThreads) {
+        const long long t = t0 + threadIdx.x;
+        int label = t < P.T ? __ldg(P.labels + t) : -1;
+        if (label >= P.V) {
+            set_status(P.header, VARDROP_ERR_INVALID_ARG);
+            label = -1;
+        }
+        const bool there = label >= 0;
+        const uint32_t mask = __ballot_sync(0xffffffffu, there);
+        if (lane == 0) warps[warp] = __popc(mask);
+        __syncthreads();
+        int before = 0, all = 0;
+        const int n = warps[lane];
+#pragma unroll
+        for (int w = 0; w < 32; ++w) {
+            const int k = __shfl_sync(0xffffffffu, n, w);
+            if (w < warp) before += k;
+            all += k;
+        }
+        const int row = ahead + before + __popc(mask & ((1u << lane) - 1));
+        if (t < P.T) {
+            if (there) {
+                P.place[row] = static_cast<int>(t);
+                P.label[row] = label;
+                if (P.lse) {
+                    const float lse = P.lse[t], g = P.d_loss[t];
+                    P.row_lse[row] = lse;
+                    P.factor[row] = g;
+                    if (fabsf(lse) > 65536.f && isfinite(lse)) set_status(P.header, VARDROP_ERR_UNSUPPORTED);
+                    if (isfinite(g)) top = fmaxf(top, fabsf(g));
+                }
+            } else if (!P.lse) {
+                P.loss[t] = 0.f;
+                P.lse_out[t] = 0.f;
+            }
+            if (P.lse) P.pos[t] = there ? row : -1;
+        }
+        ahead += all;
+        __syncthreads();
+    }
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+    if (lane == 0) most[warp] = top;
+    __syncthreads();
+    if (warp == 0) {
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most[lane])));
+        if (lane == 0) {
+            // G is stored as factor times (p - 1 or p) times a power of two that takes the largest factor to between 2^13 and 2^14: fp16 has room for it, and 38 powers of two below it
+            const int e = top > 0.f ? min(max(13 - (static_cast<int>(__float_as_uint(top) >> 23) - 127), -126), 126) : 0;
+            P.header[kLossRows] = ahead;
+            P.header[kLossFactor] = (127 + e) << 23;
+            P.header[kLossInverse] = (127 - e) << 23;
+        }
+    }
+}
+
+struct PackParams {
+    const uint4* h;
+    uint4* packed;
+    const int32_t* place;
+    const int* header;
+    int T, vectors;                                     // 16-byte vectors of a row
+};
+constexpr int kPackThreads = 256, kPackRows = 8;        // a warp a row
+__global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const PackParams P) {
+    chain_wait();
+    chain_release();
+    const int n = __ldcg(P.header + kLossRows), row = blockIdx.x * kPackRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (n == P.T || row >= (n + kChunk - 1) / kChunk * kChunk) return;          // (rows of zeros up to a whole chunk: zero times what lies there need not be zero)
+    const uint4* const from = row < n ? P.h + static_cast<size_t>(__ldcg(P.place + row)) * P.vectors : nullptr;
+    uint4* const to = P.packed + static_cast<size_t>(row) * P.vectors;
+#pragma unroll 4
+    for (int i = lane; i < P.vectors; i += 32) to[i] = from ? __ldg(from + i) : make_uint4(0u, 0u, 0u, 0u);
+}
+
+// ---- products -------------------------------------------------------------------------------------------------------------------
+enum LossMode { kStats, kGrad, kDh, kDw };
+struct LossMaps {
+    CUtensorMap h, packed, w, g;
+};
+struct PairParams {
+    int* header;
+    int T, V, C;
+    int v0, v1;                                         // the piece
+    int pitch;                                          // columns of G
+    int splits, add, fp16;
+    float scale;
+    const int32_t* label;
+    const float *row_lse, *factor;
+    float2* part;                                       // [half tiles of the vocabulary, rows]
+    float* target;
+    void* g;
+    float* acc;                                         // [splits, rows, C]
+    void* out;
+    int rows;                                           // of `part` and, times the splits, of `acc`
+};
+struct PairTile {
+    int m, n, k0, k1, split;
+};
+
+template <class T>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 v = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// What a thread does with 128 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
+template <int kMode, class T>
+__device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x, uint32_t tm, int row, int col, int n) {
+    if constexpr (kMode == kStats) {
+        const int left = P.V - col;
+        if (left <= 0) return;
+        const int label = row < n ? __ldg(P.label + row) - col : -1;
+        const float k = P.scale * kLog2e;
+        float m = -INFINITY, s = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < kHalfTile && c < left; c += 32) {
+            __syncwarp();
+            float r[32];
+            tmem_ld32(tm + c, r);
+            tmem_ld_wait();
+            if (label >= c && label < c + 32) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (label == c + e) P.target[row] = r[e] * P.scale;
+            }
+            if (c + 32 > left) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (c + e >= left) r[e] = -INFINITY;
+            }
+            float t[4] = {r[0], r[1], r[2], r[3]};
+#pragma unroll
+            for (int e = 4; e < 32; ++e) t[e & 3] = fmaxf(t[e & 3], r[e]);
+            const float top = fmaxf(m, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+            // differences of the sums ahead of the scale: exact however far from zero the logits are
+            float sum[4] = {s * exp2_fast((m - top) * k), 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[e & 3] += exp2_fast((r[e] - top) * k);
+            s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            m = top;
+        }
+        if (row < n) P.part[static_cast<size_t>(col / kHalfTile) * P.rows + row] = make_float2(m, s);
+    } else if constexpr (kMode == kGrad) {
+        const bool there = row < n;
+        const int left = P.V - P.v0 - col, label = there ? __ldg(P.label + row) - P.v0 - col : -1;
+        const float lse = there ? __ldg(P.row_lse + row) : 0.f, factor = there ? __ldg(P.factor + row) * __int_as_float(__ldcg(P.header + kLossFactor)) : 0.f;
+        uint4* const to = reinterpret_cast<uint4*>(static_cast<T*>(P.g) + static_cast<size_t>(row) * P.pitch + col);
+#pragma unroll 1
+        for (int c = 0; c < kHalfTile; c += 32) {
+            __syncwarp();
+            float r[32];
+            tmem_ld32(tm + c, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                const float p = exp2_fast(fmaf(r[e], P.scale, -lse) * kLog2e);
+                r[e] = factor * (label == c + e ? p - 1.f : p);
+            }
+            if (!there || c + 32 > left) {              // zeros, whatever the products there are
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (!there || c + e >= left) r[e] = 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                to[c / 8 + q] = make_uint4(pack16<T>(r[8 * q], r[8 * q + 1]), pack16<T>(r[8 * q + 2], r[8 * q + 3]), pack16<T>(r[8 * q + 4], r[8 * q + 5]), pack16<T>(r[8 * q + 6], r[8 * q + 7]));
+        }
+    } else {
+        const bool some = x.k1 > x.k0, there = row < (kMode == kDh ? n : P.v1 - P.v0);
+        const bool direct = kMode == kDw && P.splits == 1;
+        const float mul = P.scale * __int_as_float(__ldcg(P.header + kLossInverse));
+        float* const acc = P.acc + (static_cast<size_t>(x.split) * P.rows + row) * P.C + col;
+        T* const out = static_cast<T*>(P.out) + (static_cast<size_t>(P.v0) + row) * P.C + col;
+#pragma unroll 1
+        for (int c = 0; c < kHalfTile && col + c < P.C; c += 32) {
+            __syncwarp();
+            float r[32];
+            tmem_ld32(tm + c, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (!there || col + c + 8 * q >= P.C) continue;       // C is a multiple of 8
+                float* const v = r + 8 * q;
+                if (!some) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+                }
+                if (direct) {
+                    *reinterpret_cast<uint4*>(out + c + 8 * q) =
+                        make_uint4(pack16<T>(v[0] * mul, v[1] * mul), pack16<T>(v[2] * mul, v[3] * mul), pack16<T>(v[4] * mul, v[5] * mul), pack16<T>(v[6] * mul, v[7] * mul));
+                } else {
+                    float4* const at = reinterpret_cast<float4*>(acc + c + 8 * q);
+                    float4 lo = make_float4(v[0], v[1], v[2], v[3]), hi = make_float4(v[4], v[5], v[6], v[7]);
+                    if (P.add) {
+                        const float4 a = at[0], b = at[1];
+                        lo.x += a.x; lo.y += a.y; lo.z += a.z; lo.w += a.w;
+                        hi.x += b.x; hi.y += b.y; hi.z += b.z; hi.w += b.w;
+                    }
+                    at[0] = lo;
+                    at[1] = hi;
+                }
+            }
+        }
+    }
+}
+
+// warp 0          (of either CTA) loads: a ring of stages, 64 of the contracted axis for 128 rows of A and 128 of B
+// warp 1          of the leader: products
+// warps 4 to 11   (of either CTA) take a finished tile out, 128 columns of a row a thread, under the products of the next one
+template <int kMode, class T>
+__global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __grid_constant__ LossMaps maps, const PairParams P) {
+    extern __shared__ unsigned char smem_dyn[];
+    uint64_t* const bar_full = reinterpret_cast<uint64_t*>(smem_dyn);       // [kStages] both CTAs' copies (the leader's)
+    uint64_t* const bar_empty = bar_full + kStages;                         // [kStages] the products that read the stage are done
+    uint64_t* const bar_acc = bar_empty + kStages;                          // [2] the tile is complete
+    uint64_t* const bar_taken = bar_acc + 2;                                // [2] and has been taken out by all sixteen warps (the leader's)
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bar_taken + 2);
+    unsigned char* const stages = align_tiles(smem_dyn + 1024);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    if (warp == 0) pair_tmem_alloc(tmem_slot, kPairTmemCols);
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(bar_full + i, 1);
+            mbar_init(bar_empty + i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_acc + i, 1);
+            mbar_init(bar_taken + i, 16);
+        }
+        mbar_fence_init();
+    }
+    __syncwarp();
+    tc_fence_before();
+    pair_sync();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    chain_wait();
+    chain_release();
+
+    const int n = __ldcg(P.header + kLossRows), columns = P.v1 - P.v0;
+    // rows, columns and contracted axis of the product
+    const int M = kMode == kDw ? columns : n, N = kMode == kStats || kMode == kGrad ? columns : P.C, K = kMode == kDh ? columns : kMode == kDw ? n : P.C;
+    const int tm = (M + kPairTile - 1) / kPairTile, tn = (N + kPairTile - 1) / kPairTile, chunks = (K + kChunk - 1) / kChunk;
+    const long long each = static_cast<long long>(tm) * tn, total = each * P.splits;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    // Neighbouring pairs take tiles of eight rows of tiles, so that what they read at a time is some eight tiles of A and nine of B.
+    const auto tile_at = [&](long long t) {
+        PairTile x;
+        x.split = static_cast<int>(t / each);
+        const int in = static_cast<int>(t - x.split * each), width = kGroupRows * tn, group = in / width, r = in - group * width;
+        const int high = min(kGroupRows, tm - group * kGroupRows);
+        x.n = r / high;
+        x.m = group * kGroupRows + (r - x.n * high);
+        x.k0 = static_cast<int>(static_cast<long long>(chunks) * x.split / P.splits);
+        x.k1 = static_cast<int>(static_cast<long long>(chunks) * (x.split + 1) / P.splits);
+        return x;
+    };
+    constexpr bool a_mn = kMode == kDw, b_mn = kMode == kDh || kMode == kDw;     // the contracted axis is the rows of the tensor
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            const CUtensorMap* const map_h = n == P.T ? &maps.h : &maps.packed;
+            const CUtensorMap* const map_a = kMode == kStats || kMode == kGrad ? map_h : &maps.g;
+            const CUtensorMap* const map_b = kMode == kDw ? map_h : &maps.w;
+            tma_prefetch_desc(map_a);
+            tma_prefetch_desc(map_b);
+            const int row_b = kMode == kDw ? 0 : P.v0;                           // rows of w begin with the piece
+            uint32_t it = 0;
+#pragma unroll 1
+            for (long long t = pair; t < total && ok; t += pairs) {
+                const PairTile x = tile_at(t);
+                const int a0 = x.m * kPairTile + static_cast<int>(rank) * kHalfTile, b0 = x.n * kPairTile + static_cast<int>(rank) * kHalfTile;
+#pragma unroll 1
+                for (int kc = x.k0; kc < x.k1; ++kc, ++it) {
+                    const uint32_t st = it % kStages;
+                    ok = mbar_wait(bar_empty + st, ((it / kStages) & 1) ^ 1);
+                    if (!ok) break;
+                    const uint32_t full = leaders(bar_full + st), to = smem_u32(stages) + st * kStageBytes;
+                    if (rank == 0) mbar_expect_tx(bar_full + st, 2 * kStageBytes);
+                    const int k = kc * kChunk;
+                    if (a_mn) {
+                        pair_load_2d(to, map_a, full, a0, k);
+                        pair_load_2d(to + kBoxBytes, map_a, full, a0 + 64, k);
+                    } else {
+                        pair_load_2d(to, map_a, full, k, a0);
+                        pair_load_2d(to + kBoxBytes, map_a, full, k, a0 + 64);
+                    }
+                    if (b_mn) {
+                        pair_load_2d(to + 2 * kBoxBytes, map_b, full, b0, row_b + k);
+                        pair_load_2d(to + 3 * kBoxBytes, map_b, full, b0 + 64, row_b + k);
+                    } else {
+                        pair_load_2d(to + 2 * kBoxBytes, map_b, full, k, row_b + b0);
+                        pair_load_2d(to + 3 * kBoxBytes, map_b, full, k, row_b + b0 + 64);
+                    }
+                }
+            }
+            // what the leader still sends to this CTA's barriers comes before it leaves
+#pragma unroll 1
+            for (uint32_t j = it > kStages ? it - kStages : 0; j < it && ok; ++j) ok = mbar_wait(bar_empty + j % kStages, (j / kStages) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 1 && rank == 0) {
+        const uint32_t idesc = pair_idesc(P.fp16 != 0, a_mn, b_mn);
+        // rows of 128 bytes: eight of them 1024 apart, panels of 64 rows or columns a box
+        const uint64_t a_desc = umma_desc_sw128(smem_u32(stages), a_mn ? kBoxBytes : 16, 1024), b_desc = umma_desc_sw128(smem_u32(stages) + 2 * kBoxBytes, b_mn ? kBoxBytes : 16, 1024);
+        constexpr uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;      // 16 of the contracted axis
+        uint32_t it = 0, i = 0;
+#pragma unroll 1
+        for (long long t = pair; t < total && ok; t += pairs, ++i) {
+            const PairTile x = tile_at(t);
+            const uint32_t d = tmem + (i & 1) * kPairTile;
+            ok = __all_sync(0xffffffffu, mbar_wait(bar_taken + (i & 1), ((i >> 1) & 1) ^ 1));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int kc = x.k0; kc < x.k1; ++kc, ++it) {
+                const uint32_t st = it % kStages;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_full + st, (it / kStages) & 1));
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t a = umma_desc_advance(a_desc, st * kStageBytes), b = umma_desc_advance(b_desc, st * kStageBytes);
+#pragma unroll
+                    for (int ks = 0; ks < kChunk / 16; ++ks) pair_mma(d, umma_desc_advance(a, ks * a_step), umma_desc_advance(b, ks * b_step), idesc, kc > x.k0 || ks > 0 ? 1u : 0u);
+                    pair_commit(bar_empty + st);
+                }
+                __syncwarp();
+            }
+            if (ok && elect_one()) pair_commit(bar_acc + (i & 1));
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
+        const int in_tile = static_cast<int>(rank) * kHalfTile + (warp & 3) * 32 + lane, half = (warp - 4) >> 2;
+        const uint32_t tm_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * kHalfTile;
+        uint32_t i = 0;
+#pragma unroll 1
+        for (long long t = pair; t < total; t += pairs, ++i) {
+            const PairTile x = tile_at(t);
+            ok = __all_sync(0xffffffffu, mbar_wait(bar_acc + (i & 1), (i >> 1) & 1));
+            if (!ok) break;
+            tc_fence_after();
+            take_out<kMode, T>(P, x, tm_at + (i & 1) * kPairTile, x.m * kPairTile + in_tile, x.n * kPairTile + half * kHalfTile, n);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) leader_arrive(leaders(bar_taken + (i & 1)));
+        }
+    }
+    if (!ok) set_status(P.header, VARDROP_ERR_TIMEOUT);
+    __syncwarp();
+    tc_fence_before();
+    pair_sync();
+    if (warp == 0) pair_tmem_dealloc(tmem, kPairTmemCols);
+}
+
+// ---- lse and loss ---------------------------------------------------------------------------------------------------------------
+struct JoinParams {
+    const float2* part;
+    const float* target;
+    const int32_t* place;
+    const int* header;
+    float *loss, *lse;
+    int halves, rows;                                   // half tiles of the vocabulary; rows of a half tile's sums
+    float scale;
+};
+constexpr int kJoinRows = 32, kJoinParts = 8;
+__global__ void __launch_bounds__(kJoinRows * kJoinParts) loss_join_kernel(const JoinParams P) {
+    __shared__ float2 s[kJoinParts][kJoinRows];
+    chain_wait();
+    chain_release();
+    const int n = __ldcg(P.header + kLossRows), x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * kJoinRows + x;
+    if (blockIdx.x * kJoinRows >= n) return;
+    const float k = P.scale * kLog2e;
+    const auto add = [&](float2 a, float2 b) {
+        const float m = fmaxf(a.x, b.x);
+        return make_float2(m, (a.y == 0.f ? 0.f : a.y * exp2_fast((a.x - m) * k)) + b.y * exp2_fast((b.x - m) * k));
+    };
+    float2 sum = make_float2(-INFINITY, 0.f);
+    if (row < n) {
+#pragma unroll 8
+        for (int j = y; j < P.halves; j += kJoinParts) sum = add(sum, __ldcg(P.part + static_cast<size_t>(j) * P.rows + row));
+    }
+    s[y][x] = sum;
+    __syncthreads();
+    if (y != 0 || row >= n) return;
+#pragma unroll
+    for (int j = 1; j < kJoinParts; ++j)
+        if (j < P.halves) sum = add(sum, s[j][x]);
+    const float lse = fmaf(sum.x, P.scale, logf(sum.y));
+    const int t = P.place[row];
+    P.lse[t] = lse;
+    P.loss[t] = lse - P.target[row];
+}
+
+// ---- gradients' last step -------------------------------------------------------------------------------------------------------
+struct RestParams {
+    const float* acc;
+    const int32_t* pos;                                 // row of a token; NULL: its own
+    const int* header;
+    void* out;
+    size_t part;                                        // elements from one part to the next
+    int count, C, splits;
+    float scale;
+};
+constexpr int kRestThreads = 256;
+// Eight columns a thread.
+template <class T>
+__global__ void __launch_bounds__(kRestThreads) loss_rest_kernel(const RestParams P) {
+    chain_wait();
+    chain_release();
+    const int vectors = P.C / 8;
+    const long long at = static_cast<long long>(blockIdx.x) * kRestThreads + threadIdx.x, t = at / vectors;
+    if (t >= P.count) return;
+    const int c = static_cast<int>(at - t * vectors) * 8;
+    const long long row = P.pos ? __ldcg(P.pos + t) : t;
+    const float mul = P.scale * __int_as_float(__ldcg(P.header + kLossInverse));
+    float v[8] = {};
+    if (row >= 0) {
+#pragma unroll 2
+        for (int s = 0; s < P.splits; ++s) {
+            const Pack<float, 8> a = load_pack<float, 8>(P.acc + s * P.part + row * P.C + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += a.e[e];
+        }
+    }
+    Pack<T, 8> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(row >= 0 ? v[e] * mul : 0.f);
+    store_pack(static_cast<T*>(P.out) + t * P.C + c, o);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// [rows, cols] of 16-bit elements, box = 64 x 64, 128-byte swizzle, zeros outside
+int loss_map(CUtensorMap* map, const void* base, bool fp16, long long rows, long long cols) {
+    static const EncodeTiledFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess;
+        return found ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
+    }();
+    if (!fn) return fail(VARDROP_ERR_CUDA, "loss: cuTensorMapEncodeTiled entry point not available");
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(cols) * 2};
+    const cuuint32_t box[2] = {64, 64}, estr[2] = {1, 1};
+    const CUresult r = fn(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? VARDROP_OK : fail(VARDROP_ERR_CUDA, "loss: cuTensorMapEncodeTiled failed with code %d", static_cast<int>(r));
+}
+
+template <int kMode, class T>
+int launch_products(int id, long long tiles, const LossMaps& maps, const PairParams& P, cudaStream_t stream) {
+    static thread_local int attr_dev = -1;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (attr_dev != dev) {
+        if (int st = check_cuda(cudaFuncSetAttribute(loss_products_kernel<kMode, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmemBytes), "loss: smem attribute")) return st;
+        attr_dev = dev;
+    }
+    const long long pairs = sm_count() / 2;
+    const int grid = 2 * static_cast<int>(tiles < pairs ? tiles : pairs);
+    LaunchScope ls_(id, stream);
+    return check_cuda(launch_chained_clusters(2, loss_products_kernel<kMode, T>, dim3(grid), dim3(kPairThreads), kPairSmemBytes, stream, maps, P), "loss: products launch");
+}
+
+struct LossCall {
+    LossPlan plan;
+    LossMaps maps;
+    PairParams P;
+    char* base;
+};
+// Where things are, and the launches that both passes begin with.
+int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, const float* lse, const float* d_loss, float* loss, float* lse_out, void* ws, bool backward,
+               cudaStream_t stream) {
+    L.plan = loss_plan(c);
+    const LossPlan& p = L.plan;
+    char* const base = L.base = static_cast<char*>(ws);
+    const bool fp16 = c.dtype == 1;
+    if (int st = loss_map(&L.maps.h, h, fp16, c.T, c.C)) return st;
+    if (int st = loss_map(&L.maps.packed, base + p.packed, fp16, p.rows, c.C)) return st;
+    if (int st = loss_map(&L.maps.w, w, fp16, c.V, c.C)) return st;
+    if (backward) {
+        if (int st = loss_map(&L.maps.g, base + p.g, fp16, p.rows, p.piece)) return st;
+    } else {
+        L.maps.g = L.maps.packed;
+    }
+    RowsParams R{labels, lse, d_loss, loss, lse_out, reinterpret_cast<int32_t*>(base + p.place), reinterpret_cast<int32_t*>(base + p.pos), reinterpret_cast<int32_t*>(base + p.label),
+                 reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor), static_cast<int*>(ws), c.T, c.V};
+    { LaunchScope ls_(K_LOSS_ROWS, stream); if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st; }
+    const PackParams K{static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), R.place, R.header, c.T, c.C / 8};
+    { LaunchScope ls_(K_LOSS_PACK, stream); if (int st = check_cuda(launch_chained(loss_pack_kernel, dim3(ceil_div(c.T, kPackRows) + kChunk / kPackRows), dim3(kPackThreads), 0, stream, K), "loss: pack launch")) return st; }
+    PairParams& P = L.P;
+    P = PairParams{};
+    P.header = R.header;
+    P.T = c.T; P.V = c.V; P.C = c.C; P.v0 = 0; P.v1 = c.V; P.pitch = p.piece; P.splits = 1; P.fp16 = fp16; P.scale = c.scale == 0.f ? 1.f : c.scale;
+    P.label = R.label; P.row_lse = R.row_lse; P.factor = R.factor;
+    P.part = reinterpret_cast<float2*>(base + p.part); P.target = reinterpret_cast<float*>(base + p.target);
+    P.g = base + p.g; P.rows = p.rows;
+    return VARDROP_OK;
+}
+
+template <class T>
+int loss_backward(LossCall& L, const vardrop_loss_cfg& c, void* d_h, void* d_w, cudaStream_t stream) {
+    const LossPlan& p = L.plan;
+    const long long tm = p.rows / kPairTile, tn = ceil_div(c.C, kPairTile);
+    const int* const header = L.P.header;
+    const auto rest = [&](int id, const float* acc, const int32_t* pos, void* out, size_t part, int count, int splits) {
+        const RestParams R{acc, pos, header, out, part, count, c.C, splits, L.P.scale};
+        LaunchScope ls_(id, stream);
+        const long long blocks = (static_cast<long long>(count) * (c.C / 8) + kRestThreads - 1) / kRestThreads;
+        return check_cuda(launch_chained(loss_rest_kernel<T>, dim3(static_cast<unsigned>(blocks)), dim3(kRestThreads), 0, stream, R), "loss: rest launch");
+    };
+    for (int i = 0; i < p.pieces; ++i) {
+        PairParams P = L.P;
+        P.v0 = i * p.piece;
+        P.v1 = c.V - P.v0 < p.piece ? c.V : P.v0 + p.piece;
+        const int columns = P.v1 - P.v0, tv = ceil_div(columns, kPairTile);
+        if (int st = launch_products<kGrad, T>(K_LOSS_GRAD, tm * tv, L.maps, P, stream)) return st;
+        if (d_h) {
+            P.splits = p.dh_splits;
+            P.add = i > 0;
+            P.acc = reinterpret_cast<float*>(L.base + p.dh);
+            if (int st = launch_products<kDh, T>(K_LOSS_DH, tm * tn * P.splits, L.maps, P, stream)) return st;
+        }
+        if (d_w) {
+            P.splits = p.dw_splits;
+            P.add = 0;
+            P.acc = reinterpret_cast<float*>(L.base + p.dw);
+            P.rows = p.piece;
+            P.out = d_w;
+            if (int st = launch_products<kDw, T>(K_LOSS_DW, static_cast<long long>(tv) * tn * P.splits, L.maps, P, stream)) return st;
+            if (P.splits > 1) {
+                if (int st = rest(K_LOSS_SUM, P.acc, nullptr, static_cast<T*>(d_w) + static_cast<size_t>(P.v0) * c.C, static_cast<size_t>(p.piece) * c.C, columns, P.splits)) return st;
+            }
+        }
+    }
+    if (!d_h) return VARDROP_OK;
+    return rest(K_LOSS_REST, reinterpret_cast<float*>(L.base + p.dh), reinterpret_cast<const int32_t*>(L.base + p.pos), d_h, static_cast<size_t>(p.rows) * c.C, c.T, p.dh_splits);
+}
+
+}  // namespace
+
+int loss_validate(const vardrop_loss_cfg& c) {
+    if (c.T < 1 || c.V < 1 || c.C < 1) return fail(VARDROP_ERR_INVALID_ARG, "loss: T, V, C >= 1 required (T=%d V=%d C=%d)", c.T, c.V, c.C);
+    if (c.dtype != 0 && c.dtype != 1) return fail(c.dtype == 2 ? VARDROP_ERR_UNSUPPORTED : VARDROP_ERR_INVALID_ARG, "loss: dtype=%d is neither bf16 nor fp16", c.dtype);
+    if (!(c.scale >= 0.f && c.scale <= 1e30f)) return fail(VARDROP_ERR_INVALID_ARG, "loss: scale outside 0..1e30");
+    if (c.C % 8 != 0) return fail(VARDROP_ERR_UNSUPPORTED, "loss: C=%d is no multiple of 8", c.C);
+    if (c.T > (1 << 24) || c.V > (1 << 24) || c.C > (1 << 16)) return fail(VARDROP_ERR_UNSUPPORTED, "loss: T=%d or V=%d above 2^24, or C=%d above 65536", c.T, c.V, c.C);
+    if (static_cast<long long>(ceil_div(c.T, kPairTile)) * ceil_div(c.V, kPairTile) > (1ll << 30)) return fail(VARDROP_ERR_UNSUPPORTED, "loss: T=%d times V=%d above 2^46", c.T, c.V);
+    return VARDROP_OK;
+}
+
+size_t loss_workspace_bytes(const vardrop_loss_cfg& c) { return loss_plan(c).total; }
+
+int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, float* loss, float* lse, void* ws, cudaStream_t stream) {
+    LossCall L;
+    if (int st = loss_begin(L, h, w, labels, c, nullptr, nullptr, loss, lse, ws, false, stream)) return st;
+    const LossPlan& p = L.plan;
+    const int tv = ceil_div(c.V, kPairTile);
+    if (int st = launch_products<kStats, __nv_bfloat16>(K_LOSS_STATS, static_cast<long long>(p.rows / kPairTile) * tv, L.maps, L.P, stream)) return st;
+    const JoinParams J{L.P.part, L.P.target, reinterpret_cast<const int32_t*>(L.base + p.place), L.P.header, loss, lse, ceil_div(c.V, kHalfTile), p.rows, L.P.scale};
+    LaunchScope ls_(K_LOSS_JOIN, stream);
+    return check_cuda(launch_chained(loss_join_kernel, dim3(ceil_div(c.T, kJoinRows)), dim3(kJoinRows * kJoinParts), 0, stream, J), "loss: join launch");
+}
+
+int loss_bwd_launch(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg& c, void* d_h, void* d_w, void* ws, cudaStream_t stream) {
+    LossCall L;
+    if (int st = loss_begin(L, h, w, labels, c, lse, d_loss, nullptr, nullptr, ws, true, stream)) return st;
+    return c.dtype == 1 ? loss_backward<__half>(L, c, d_h, d_w, stream) : loss_backward<__nv_bfloat16>(L, c, d_h, d_w, stream);
+}
+
+}  // namespace vardrop

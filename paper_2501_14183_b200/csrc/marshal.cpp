@@ -396,10 +396,43 @@ PyObject* act_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return finish(g, [=](void* s) { return vardrop_act_bwd(d_y, ckpt, nb, n_sel, cfg, d_a, d_b, y, s); });
     });
 }
+PyObject* loss_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<7>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_loss_cfg>(3);
+        if (!g.ok) return nullptr;
+        const at::ScalarType ty = type_of(cfg->dtype);
+        const int64_t T = cfg->T, V = cfg->V, C = cfg->C;
+        const void* const h = g.checked(0, "h", ty, T * C);
+        const void* const w = g.checked(1, "w", ty, V * C);
+        const auto labels = g.checked<const int32_t>(2, "labels", at::kInt, T);
+        const auto loss = g.checked<float>(4, "loss", at::kFloat, T), lse = g.checked<float>(5, "lse", at::kFloat, T);
+        void* const ws = g.checked(6, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(6) : 0;
+        return finish(g, [=](void* s) { return vardrop_loss_fwd(h, w, labels, cfg, loss, lse, ws, nb, s); });
+    });
+}
+PyObject* loss_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<9>(a, n, [](Args& g) -> PyObject* {
+        const auto cfg = g.cfg<vardrop_loss_cfg>(5);
+        if (!g.ok) return nullptr;
+        const at::ScalarType ty = type_of(cfg->dtype);
+        const int64_t T = cfg->T, V = cfg->V, C = cfg->C;
+        const void* const h = g.checked(0, "h", ty, T * C);
+        const void* const w = g.checked(1, "w", ty, V * C);
+        const auto labels = g.checked<const int32_t>(2, "labels", at::kInt, T);
+        const auto lse = g.checked<const float>(3, "lse", at::kFloat, T), d_loss = g.checked<const float>(4, "d_loss", at::kFloat, T);
+        void* const d_h = g.checked(6, "d_h", ty, T * C);
+        void* const d_w = g.checked(7, "d_w", ty, V * C);
+        void* const ws = g.checked(8, "ws", at::kByte, 0);
+        const size_t nb = g.ok && ws ? g.bytes(8) : 0;
+        return finish(g, [=](void* s) { return vardrop_loss_bwd(h, w, labels, lse, d_loss, cfg, d_h, d_w, ws, nb, s); });
+    });
+}
 
 #define VD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VD_METHOD(hash), VD_METHOD(select), VD_METHOD(select_static), VD_METHOD(gather_rows), VD_METHOD(attn_fwd), VD_METHOD(attn_bwd),
-                           VD_METHOD(pearson_max), VD_METHOD(packed_plan), VD_METHOD(attn_packed_fwd), VD_METHOD(attn_packed_bwd), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), VD_METHOD(embed_fwd), VD_METHOD(embed_bwd), VD_METHOD(act_fwd), VD_METHOD(act_bwd), {nullptr, nullptr, 0, nullptr}};
+                           VD_METHOD(pearson_max), VD_METHOD(packed_plan), VD_METHOD(attn_packed_fwd), VD_METHOD(attn_packed_bwd), VD_METHOD(norm_fwd), VD_METHOD(norm_bwd), VD_METHOD(grad_clip), VD_METHOD(embed_fwd), VD_METHOD(embed_bwd), VD_METHOD(act_fwd), VD_METHOD(act_bwd),
+                           VD_METHOD(loss_fwd), VD_METHOD(loss_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

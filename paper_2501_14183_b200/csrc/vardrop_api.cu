@@ -51,7 +51,8 @@ const char* const g_kernel_names[K_COUNT] = {"hash_kernel", "select_small_kernel
                                              "attn_fwd_kernel", "bwd_prep_kernel", "attn_bwd_kernel", "bwd_convert_kernel", "pearson_normalize_kernel",
                                              "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel", "packed_plan_kernel",
                                              "attn_packed_fwd_kernel", "attn_packed_tile_kernel", "packed_short_kernel", "packed_prep_kernel", "attn_packed_bwd_kernel", "packed_convert_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel",
-                                             "embed_fwd_kernel", "embed_count_kernel", "embed_sort_kernel", "embed_sum_kernel", "embed_join_kernel", "act_fwd_kernel", "act_bwd_kernel"};
+                                             "embed_fwd_kernel", "embed_count_kernel", "embed_sort_kernel", "embed_sum_kernel", "embed_join_kernel", "act_fwd_kernel", "act_bwd_kernel",
+                                             "loss_rows_kernel", "loss_pack_kernel", "loss_stats_kernel", "loss_join_kernel", "loss_grad_kernel", "loss_dh_kernel", "loss_dw_kernel", "loss_rest_kernel", "loss_sum_kernel"};
 }  // namespace
 
 LaunchScope::LaunchScope(int id, cudaStream_t stream) : id_(id), stream_(stream), stop_(nullptr) {
@@ -564,6 +565,47 @@ int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const 
     const Rows outs[] = {{d_a, rows, C, stride, size, "d_a"}, {d_b, rows, C, stride, size, "d_b"}, {y, rows, C, C, size, "y"}};
     VD_CHECK(overlap_check("act", ins, 3, outs, 3, true));
     return act_bwd_launch(d_y, ckpt, n_sel, *cfg, d_a, d_b, y, static_cast<cudaStream_t>(stream));
+}
+
+size_t vardrop_loss_workspace_bytes(const vardrop_loss_cfg* cfg) {
+    if (!cfg || loss_validate(*cfg) != VARDROP_OK) return 0;
+    return loss_workspace_bytes(*cfg);
+}
+
+int vardrop_loss_fwd(const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg* cfg, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(loss_validate(*cfg));
+    VD_CHECK(check_ptr(h, "h", true));
+    VD_CHECK(check_ptr(w, "w", true));
+    VD_CHECK(check_ptr(labels, "labels", true));
+    VD_CHECK(check_ptr(loss, "loss", true));
+    VD_CHECK(check_ptr(lse, "lse", true));
+    VD_CHECK(check_ws(ws, ws_bytes, loss_workspace_bytes(*cfg)));
+    const size_t T = cfg->T, V = cfg->V, C = cfg->C;
+    const Rows ins[] = {flat(h, T * C, 2, "h"), flat(w, V * C, 2, "w"), flat(labels, T, 4, "labels")};
+    const Rows outs[] = {flat(loss, T, 4, "loss"), flat(lse, T, 4, "lse"), flat(ws, loss_workspace_bytes(*cfg), 1, "ws")};
+    VD_CHECK(overlap_check("loss", ins, 3, outs, 3, false));
+    return loss_fwd_launch(h, w, labels, *cfg, loss, lse, ws, static_cast<cudaStream_t>(stream));
+}
+
+int vardrop_loss_bwd(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg* cfg, void* d_h, void* d_w, void* ws, size_t ws_bytes,
+                     void* stream) {
+    if (!cfg) return fail(VARDROP_ERR_INVALID_ARG, "cfg is NULL");
+    VD_CHECK(loss_validate(*cfg));
+    VD_CHECK(check_ptr(h, "h", true));
+    VD_CHECK(check_ptr(w, "w", true));
+    VD_CHECK(check_ptr(labels, "labels", true));
+    VD_CHECK(check_ptr(lse, "lse", true));
+    VD_CHECK(check_ptr(d_loss, "d_loss", true));
+    if (!d_h && !d_w) return fail(VARDROP_ERR_INVALID_ARG, "loss: d_h and d_w are both NULL");
+    VD_CHECK(check_ptr(d_h, "d_h", false));
+    VD_CHECK(check_ptr(d_w, "d_w", false));
+    VD_CHECK(check_ws(ws, ws_bytes, loss_workspace_bytes(*cfg)));
+    const size_t T = cfg->T, V = cfg->V, C = cfg->C;
+    const Rows ins[] = {flat(h, T * C, 2, "h"), flat(w, V * C, 2, "w"), flat(labels, T, 4, "labels"), flat(lse, T, 4, "lse"), flat(d_loss, T, 4, "d_loss")};
+    const Rows outs[] = {flat(d_h, T * C, 2, "d_h"), flat(d_w, V * C, 2, "d_w"), flat(ws, loss_workspace_bytes(*cfg), 1, "ws")};
+    VD_CHECK(overlap_check("loss", ins, 5, outs, 3, false));
+    return loss_bwd_launch(h, w, labels, lse, d_loss, *cfg, d_h, d_w, ws, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-"""Argument checks of the embeddings and the activations: they run ahead of any CUDA call, on a machine without a GPU too."""
+"""Argument checks of the embeddings, the activations and the loss: they run ahead of any CUDA call, on a machine without a GPU too."""
 import ctypes as C
 
 import pytest
@@ -91,6 +91,53 @@ def test_act_arguments(lib):
     assert fwd(by=wide, b=a + 64, y=a) == bwd(by=wide, db=a + 64) == vd.ERR_INVALID_ARG
 
 
+def loss_cfg(**kw):
+    return make(vd.LossCfg, dict(T=100, V=50, C=64, dtype=0, scale=1.0), **kw)
+
+
+@pytest.mark.parametrize("kw,status", [(dict(T=0), 1), (dict(V=0), 1), (dict(C=0), 1), (dict(dtype=3), 1), (dict(dtype=-1), 1), (dict(dtype=2), 2), (dict(scale=-1.0), 1), (dict(scale=float("nan")), 1),
+                                       (dict(scale=2e30), 1), (dict(C=65), 2), (dict(C=4), 2), (dict(C=65544), 2), (dict(T=(1 << 24) + 1), 2), (dict(V=(1 << 24) + 1), 2), (dict(T=1 << 24, V=1 << 24), 2)])
+def test_loss_configurations(lib, kw, status):
+    cfg = loss_cfg(**kw)
+    h, w, labels, loss, lse, ws, d_h, d_w = spots(8, 1 << 44)
+    assert lib.vardrop_loss_fwd(h, w, labels, C.byref(cfg), loss, lse, ws, 1 << 43, None) == status
+    assert lib.vardrop_last_error().startswith(b"loss")
+    assert lib.vardrop_loss_bwd(h, w, labels, lse, loss, C.byref(cfg), d_h, d_w, ws, 1 << 43, None) == status
+    assert vd.vardrop_loss_workspace_bytes(cfg) == 0
+
+
+def test_loss_arguments(lib):
+    cfg = C.byref(loss_cfg())
+    need = vd.vardrop_loss_workspace_bytes(loss_cfg())
+    good = spots(6)                             # h, w, labels, loss, lse, ws
+    fwd = lambda a, nb=need, by=cfg: lib.vardrop_loss_fwd(*a[:3], by, *a[3:], nb, None)  # noqa: E731
+    for at in range(6):
+        for bad in (None, good[at] + 8):
+            assert fwd(good[:at] + [bad] + good[at + 1:]) == vd.ERR_INVALID_ARG, at
+    assert fwd(good, by=None) == vd.ERR_INVALID_ARG and fwd(good, need - 1) == vd.ERR_WORKSPACE
+    for out in (3, 4, 5):
+        for other in range(6):
+            if other != out:
+                a = list(good)
+                a[out] = a[other] + (16 if other < 3 else 0)
+                assert fwd(a) == vd.ERR_INVALID_ARG and b"overlap" in lib.vardrop_last_error(), (out, other)
+    good = spots(8)                             # h, w, labels, lse, d_loss, d_h, d_w, ws
+    bwd = lambda a, nb=need, by=cfg: lib.vardrop_loss_bwd(*a[:5], by, *a[5:], nb, None)  # noqa: E731
+    for at in range(8):
+        for bad in (None, good[at] + 8):
+            if bad is None and at in (5, 6):    # one gradient alone is fine, none at all is not
+                continue
+            assert bwd(good[:at] + [bad] + good[at + 1:]) == vd.ERR_INVALID_ARG, at
+    assert bwd(good[:5] + [None, None] + good[7:]) == bwd(good, by=None) == vd.ERR_INVALID_ARG and bwd(good, need - 1) == vd.ERR_WORKSPACE
+    for out in (5, 6, 7):
+        for other in range(8):
+            if other != out:
+                a = list(good)
+                a[out] = a[other]
+                assert bwd(a) == vd.ERR_INVALID_ARG and b"overlap" in lib.vardrop_last_error(), (out, other)
+
+
 def test_struct_layouts_match_header():
     assert C.sizeof(vd.EmbedCfg) == 28 and vd.EmbedCfg.scale.offset == 24
     assert C.sizeof(vd.ActCfg) == 40 and vd.ActCfg.stride.offset == 32
+    assert C.sizeof(vd.LossCfg) == 20
