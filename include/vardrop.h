@@ -411,7 +411,7 @@ int vardrop_grad_clip(const vardrop_tensor* tensors, int32_t count, const vardro
  *             scale finite; accumulate 0 or 1 (backward only).
  * table       [V, C].     idx   [T] int32; negative: no token.  An index from V on is taken as none, and reported: device status VARDROP_ERR_INVALID_ARG.
  * out         [T, C] out.
- * d_out       [T, C], gradient of out; rows of tokens without an index are not read.
+ * d_out       [T, C], gradient of out; what lies in rows of tokens without an index does not matter.
  * d_table     [V, C] out; with accumulate = 0 every row is written (zeros where no token has it), with 1 only rows that some token has are read and written.
  * ws          scratch of vardrop_embed_workspace_bytes for the backward call; the forward call only needs its status word (256 bytes).  Nothing is kept in it.
  * Sums in fp32 in an order that the tokens' order alone decides (bit-reproducible), rounded once.  No buffer may overlap an output.
@@ -468,7 +468,7 @@ int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const 
  * d_loss      [T] fp32, gradient of loss (1 / labelled tokens for their mean).
  * d_h         [T, C] out, zeros where there is no label; d_w   [V, C] out, every row written.  Either may be NULL (not wanted).
  * ws          scratch of vardrop_loss_workspace_bytes, for both calls.  Nothing is kept in it from one to the other.
- * Products of 16-bit operands with fp32 sums; G is rounded to 16 bits ahead of its products, times a power of two that keeps it in the type's range (a token whose |d_loss| is below 2^-24 of the largest one's
+ * Products of 16-bit operands with fp32 sums; G is rounded to 16 bits ahead of its products, times a number that keeps it in the type's range (a token whose |d_loss| is below 2^-24 of the largest one's
  * loses precision in fp16).  The weights of a token come from lse, whose 24 bits leave them open by about 2^-24 |lse| of themselves: with a finite |lse| above 2^16 the device status is VARDROP_ERR_UNSUPPORTED.
  * Values of a labelled token's row that are not finite reach its own loss and d_h, and d_w.  All results are bit-reproducible.
  * ---------------------------------------------------------------------------------------------- */

@@ -17,8 +17,9 @@ namespace vardrop {
 
 namespace {
 
-constexpr int kActThreads = 256;
+constexpr int kActThreads = 256, kActWarps = kActThreads / 32;
 constexpr int kBlock = 32;                      // values of a row that share a scale
+constexpr int kPer = 8;                         // values of a thread: a warp has eight blocks of a row at a time
 enum { kRelu = 0, kGelu = 1, kSilu = 2 };
 
 struct ActParams {
@@ -30,41 +31,96 @@ struct ActParams {
     int B, N, C, S, blocks, chunks;             // chunks: pieces of a row that a warp takes at a time
 };
 
-__device__ __forceinline__ float upper_tail(float a) { return 0.5f * erfcf(a * -0.70710678f); }      // P(normal <= a)
-// kFull: to fp32's last bits; otherwise the fast forms, good to some 2^-21, which 16-bit results do not feel.
-template <bool kFull>
-__device__ __forceinline__ float exp_of(float a) { return kFull ? expf(a) : __expf(a); }
-template <bool kFull>
-__device__ __forceinline__ float quotient(float a, float b) { return kFull ? a / b : __fdividef(a, b); }
-// 1 / (1 + exp(-a)) with a denominator of at most 2: the fast quotient gives 0 for ones beyond 2^126.
-template <bool kFull>
-__device__ __forceinline__ float logistic(float a) {
-    const float z = exp_of<kFull>(-fabsf(a));
-    return quotient<kFull>(a < 0.f ? z : 1.f, 1.f + z);
+// ---- packed fp32 pairs -------------------------------------------------------------------------------------------------------------
+// These kernels are bound by the instructions that they issue long before the memory (gelu of 8192 x 2048 bf16 forward: 71 a value, 49 us); a pair in one instruction halves those of the arithmetic.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
 }
-template <int kKind, bool kFull>
-__device__ __forceinline__ float act_of(float a) {
-    if (kKind == kRelu) return a < 0.f ? 0.f : a;                   // (a NaN stays one)
-    if (kKind == kGelu) return a * upper_tail(a);
-    return a * logistic<kFull>(a);
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n.reg .b64 x, y, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 w, x, y;\nmov.b64 {%0, %1}, w;\n}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {              // of 1 to some 14 here
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// ---- functions ------------------------------------------------------------------------------------------------------------------------
+// P(normal > z) = exp(-z^2 / 2) R(z), 0 <= z.  R is Mills' ratio over sqrt(2 pi), smooth from 1/2 to 0.4 / z: a polynomial in t = 1 / (1 + 0.32 z) times t, fitted to erfcx for the least
+// largest relative error, 3.2e-8; in fp32 and with the exponential off by 2^-22 and z^2 / 4 steps.
+__device__ __forceinline__ float2 upper_tail(float2 z, float2& e) {
+    const float2 s = mul2(mul2(z, z), both(-0.72134752f));
+    e = make_float2(exp2_of(s.x), exp2_of(s.y));
+    const float2 d = fma2(z, both(0.32f), both(1.f)), t = make_float2(reciprocal(d.x), reciprocal(d.y));
+    float2 r = both(-0.021078268f);
+    r = fma2(r, t, both(0.0954077f));
+    r = fma2(r, t, both(-0.14670828f));
+    r = fma2(r, t, both(0.06532883f));
+    r = fma2(r, t, both(-0.009378026f));
+    r = fma2(r, t, both(0.05865411f));
+    r = fma2(r, t, both(0.08782908f));
+    r = fma2(r, t, both(0.11462236f));
+    r = fma2(r, t, both(0.12766095f));
+    r = fma2(r, t, both(0.12766153f));
+    return mul2(mul2(r, t), e);
+}
+__device__ __forceinline__ float2 far_enough(float2 a) { return make_float2(fminf(fabsf(a.x), 40.f), fminf(fabsf(a.y), 40.f)); }       // tails end long before
+// exp(-|a|) and 1 / (1 + exp(-|a|)): a denominator of at most 2, where 1 + exp(-a) would leave the range
+__device__ __forceinline__ float2 logistic_parts(float2 a, float2& z) {
+    z = make_float2(exp2_of(fabsf(a.x) * -1.44269504f), exp2_of(fabsf(a.y) * -1.44269504f));
+    return make_float2(reciprocal(1.f + z.x), reciprocal(1.f + z.y));
+}
+template <int kKind>
+__device__ __forceinline__ float2 act_of(float2 a) {
+    const float2 up = make_float2(max_or_nan(a.x, 0.f), max_or_nan(a.y, 0.f));
+    if (kKind == kRelu) return up;
+    if (kKind == kGelu) {                       // a (1 - Q(a)) above 0, a Q(-a) below
+        float2 e;
+        const float2 z = far_enough(a), q = upper_tail(z, e);
+        return fma2(make_float2(-z.x, -z.y), q, up);
+    }
+    float2 z;
+    const float2 r = logistic_parts(a, z);
+    return mul2(fma2(make_float2(fminf(a.x, 0.f), fminf(a.y, 0.f)), z, up), r);
 }
 // f(a) and f'(a)
-template <int kKind, bool kFull>
-__device__ __forceinline__ void act_slope(float a, float& f, float& slope) {
+template <int kKind>
+__device__ __forceinline__ void act_slope(float2 a, float2& f, float2& slope) {
+    const float2 up = make_float2(max_or_nan(a.x, 0.f), max_or_nan(a.y, 0.f));
     if (kKind == kRelu) {
-        f = a < 0.f ? 0.f : a;
-        slope = a > 0.f ? 1.f : a == a ? 0.f : a;
+        f = up;
+        slope = make_float2(a.x > 0.f ? 1.f : a.x == a.x ? 0.f : a.x, a.y > 0.f ? 1.f : a.y == a.y ? 0.f : a.y);
     } else if (kKind == kGelu) {
-        const float p = upper_tail(a);
-        f = a * p;
-        slope = fmaf(a * 0.39894228f, exp_of<kFull>(-0.5f * a * a), p);
+        float2 e;
+        const float2 z = far_enough(a), q = upper_tail(z, e);
+        f = fma2(make_float2(-z.x, -z.y), q, up);
+        slope = fma2(mul2(a, both(0.39894228f)), e, make_float2(a.x < 0.f ? q.x : 1.f - q.x, a.y < 0.f ? q.y : 1.f - q.y));
     } else {
-        const float p = logistic<kFull>(a);
-        f = a * p;
-        slope = fmaf(f, 1.f - p, p);
+        float2 z;
+        const float2 r = logistic_parts(a, z), p = mul2(make_float2(a.x < 0.f ? z.x : 1.f, a.y < 0.f ? z.y : 1.f), r);
+        f = mul2(a, p);
+        slope = fma2(f, make_float2(1.f - p.x, 1.f - p.y), p);
     }
 }
 
+// ---- eight bits ---------------------------------------------------------------------------------------------------------------------
 // Biased exponent of the block's scale from the largest magnitude's bits.
 __device__ __forceinline__ int scale_of(uint32_t top) {
     const int e = static_cast<int>(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u);        // 448 = 1.75 2^8
@@ -72,187 +128,244 @@ __device__ __forceinline__ int scale_of(uint32_t top) {
 }
 __device__ __forceinline__ float to_block(int scale) { return __uint_as_float(static_cast<uint32_t>(254 - scale) << 23); }     // 2^-e
 __device__ __forceinline__ float from_block(int scale) { return __uint_as_float(scale ? static_cast<uint32_t>(scale) << 23 : 0x400000u); }
-__device__ __forceinline__ uint32_t magnitude(float v) {            // for the block's maximum: values that are not finite have no part in it
-    const uint32_t m = __float_as_uint(v) & 0x7fffffffu;
-    return m < 0x7f800000u ? m : 0u;
-}
-__device__ __forceinline__ uint32_t code2(float v0, float v1, float mul) {
-    uint32_t c = __nv_cvt_float2_to_fp8x2(make_float2(v0 * mul, v1 * mul), __NV_SATFINITE, __NV_E4M3);
-    if (isinf(v0)) c |= 0x7fu;                                      // no infinities in e4m3: NaN
-    if (isinf(v1)) c |= 0x7f00u;
-    return c;
-}
-__device__ __forceinline__ float2 value2(uint32_t code, float mul) {
+__device__ __forceinline__ uint32_t code2(float2 v) { return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3); }
+__device__ __forceinline__ float2 value2(uint32_t code) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(code), __NV_E4M3);
-    const float2 f = __half22float2(__half2(h));
-    return make_float2(f.x * mul, f.y * mul);
+    return __half22float2(__half2(h));
 }
-
-// Where a warp's piece lies.  kVec 8: 256 columns, eight to a lane, four lanes to a block; kVec 1: a block, a column a lane.
-template <int kVec>
-struct Piece {
-    long long row;                              // of [B, N]
-    int c;                                      // this lane's first column
-    bool live;
-};
-template <int kVec>
-__device__ __forceinline__ Piece<kVec> piece_of(const ActParams& P, int b, int n, uint32_t task) {
-    Piece<kVec> p;
-    const uint32_t i = task / static_cast<uint32_t>(P.chunks), k = task - i * static_cast<uint32_t>(P.chunks);
-    p.row = static_cast<long long>(b) * P.N + i;
-    p.c = static_cast<int>(k * 32 + (threadIdx.x & 31)) * kVec;
-    p.live = i < static_cast<uint32_t>(n) && p.c < P.C;
-    return p;
-}
-// kTasks pieces a warp, those of neighbouring warps next to each other.
-constexpr int kActWarps = kActThreads / 32;
-
+constexpr uint32_t kInfinity = 0x7f800000u;
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 // The largest value of the type that a code stands for: the next one, 2^16 or 2^128, is none of the type's, so what would round to it is held by this one (off by less than 2^-4 of itself all the same).
 template <class T>
 __device__ __forceinline__ float most_held() { return std::is_same<T, __half>::value ? 61440.f : 3.1901471898837980e38f; }
-template <class T, int kVec>
-__device__ __forceinline__ void put_codes(const ActParams& P, int which, const Piece<kVec>& p, float (&v)[kVec]) {
-    uint32_t top = 0;
+// Blocks that hold something beyond that, or not finite: values as their codes are to have them, with a NaN for infinities, which e4m3 does not have.
+template <class T>
+__device__ __forceinline__ float held_as(float v) { return isfinite(v) ? fminf(fmaxf(v, -most_held<T>()), most_held<T>()) : __int_as_float(0x7fffffff); }
+
+// Where a thread's eight values of a piece lie.  kWide: next to each other, four lanes to a block (C a multiple of 8); otherwise 32 apart, a block for each of them (rows begin on any element).
+template <bool kWide>
+struct Piece {
+    long long row;                              // of [B, N]
+    int c;                                      // this lane's first column
+    int left;                                   // columns from there on; 0: nothing to do here
+    __device__ __forceinline__ bool live(int e) const { return kWide ? left > 0 : 32 * e < left; }
+};
+template <class T, bool kWide>
+struct Values {
+    Pack<T, kWide ? kPer : 1> v[kWide ? 1 : kPer];
+    __device__ __forceinline__ float at(int e) const { return to_float(kWide ? v[0].e[e] : v[e].e[0]); }
+    __device__ __forceinline__ void set(int e, float x) { (kWide ? v[0].e[e] : v[e].e[0]) = from_float<T>(x); }
+    // (Without a branch, from the tensor's beginning where there is nothing: a load behind a branch is waited for where the branches join.)
+    __device__ __forceinline__ void load(const T* base, size_t off, const Piece<kWide>& at) {
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) top = max(top, p.live ? magnitude(v[e]) : 0u);
-    if (kVec == 1) {
-        top = __reduce_max_sync(0xffffffffu, top);
-    } else {
+        for (int e = 0; e < (kWide ? 1 : kPer); ++e) v[e] = load_pack<T, kWide ? kPer : 1>(base + (at.live(e) ? off + 32 * e : 0));
+    }
+    __device__ __forceinline__ void store(T* p, const Piece<kWide>& at) const {
+#pragma unroll
+        for (int e = 0; e < (kWide ? 1 : kPer); ++e)
+            if (at.live(e)) store_pack(p + 32 * e, v[e]);
+    }
+};
+// The piece of a warp's task; the next one is the next of the row, or the first one of the next row.
+struct Task {
+    uint32_t row, chunk;
+};
+template <bool kWide>
+__device__ __forceinline__ Piece<kWide> piece_of(const ActParams& P, int b, int n, const Task& t) {
+    Piece<kWide> p;
+    const int lane = threadIdx.x & 31;
+    p.row = static_cast<long long>(b) * P.N + t.row;
+    p.c = static_cast<int>(t.chunk) * (32 * kPer) + (kWide ? lane * kPer : lane);
+    p.left = t.row < static_cast<uint32_t>(n) ? P.C - p.c : 0;
+    return p;
+}
+
+template <class T, bool kWide>
+__device__ __forceinline__ void put_codes(const ActParams& P, int which, const Piece<kWide>& p, float2 (&v)[kPer / 2]) {
+    const size_t row = which * (static_cast<size_t>(P.B) * P.N) + p.row;
+    unsigned char* const at = P.codes + row * P.C + p.c;
+    unsigned char* const scales = P.scales + row * P.blocks + p.c / kBlock;
+    const uint32_t most = magnitude(most_held<T>());
+    if constexpr (kWide) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < kPer / 2; ++k) top = max(top, max(magnitude(v[k].x), magnitude(v[k].y)));
+        if (p.left <= 0) top = 0;
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    }
-    if (!p.live) return;
-    if (top > __float_as_uint(most_held<T>())) {
+        if (__any_sync(0xffffffffu, top > most)) {
+            uint32_t fine = 0;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e)
-            if (isfinite(v[e])) v[e] = fminf(fmaxf(v[e], -most_held<T>()), most_held<T>());
-    }
-    const int scale = scale_of(top);
-    const float mul = to_block(scale);
-    const size_t rows = static_cast<size_t>(P.B) * P.N, row = which * rows + p.row;
-    unsigned char* const at = P.codes + row * P.C + p.c;
-    if constexpr (kVec == 8) {
+            for (int k = 0; k < kPer / 2; ++k) {
+                v[k] = make_float2(held_as<T>(v[k].x), held_as<T>(v[k].y));
+                if (magnitude(v[k].x) < kInfinity) fine = max(fine, magnitude(v[k].x));
+                if (magnitude(v[k].y) < kInfinity) fine = max(fine, magnitude(v[k].y));
+            }
+            if (p.left <= 0) fine = 0;
+            fine = max(fine, __shfl_xor_sync(0xffffffffu, fine, 1));
+            top = max(fine, __shfl_xor_sync(0xffffffffu, fine, 2));
+        }
+        if (p.left <= 0) return;
+        const int scale = scale_of(top);
+        const float2 mul = both(to_block(scale));
         uint2 c;
-        c.x = code2(v[0], v[1], mul) | code2(v[2], v[3], mul) << 16;
-        c.y = code2(v[4], v[5], mul) | code2(v[6], v[7], mul) << 16;
+        c.x = code2(mul2(v[0], mul)) | code2(mul2(v[1], mul)) << 16;
+        c.y = code2(mul2(v[2], mul)) | code2(mul2(v[3], mul)) << 16;
         *reinterpret_cast<uint2*>(at) = c;
+        if ((p.c & (kBlock - 1)) == 0) *scales = static_cast<unsigned char>(scale);
     } else {
-        *at = static_cast<unsigned char>(code2(v[0], 0.f, mul));
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            float x = e & 1 ? v[e / 2].y : v[e / 2].x;
+            uint32_t top = __reduce_max_sync(0xffffffffu, p.live(e) ? magnitude(x) : 0u);
+            if (top > most) {                   // (the whole warp)
+                x = held_as<T>(x);
+                top = __reduce_max_sync(0xffffffffu, p.live(e) && magnitude(x) < kInfinity ? magnitude(x) : 0u);
+            }
+            const int scale = scale_of(top);
+            if (p.live(e)) at[32 * e] = static_cast<unsigned char>(code2(make_float2(x * to_block(scale), 0.f)));
+            if ((threadIdx.x & 31) == 0 && p.live(e)) scales[e] = static_cast<unsigned char>(scale);
+        }
     }
-    if ((p.c & (kBlock - 1)) == 0) P.scales[row * P.blocks + p.c / kBlock] = static_cast<unsigned char>(scale);
 }
 // Codes as they lie in memory, so that the loads of several pieces overlap.
+template <bool kWide>
 struct Held {
-    uint2 codes;
-    int scale;
+    uint2 codes;                                // a byte a value
+    uint2 scales;                               // wide: the one of the block; otherwise a byte a value
+    __device__ __forceinline__ void load(const ActParams& P, int which, const Piece<kWide>& p) {
+        const size_t row = which * (static_cast<size_t>(P.B) * P.N) + p.row;
+        const unsigned char* const at = P.codes + (p.live(0) ? row * P.C + p.c : 0);
+        const unsigned char* const s = P.scales + (p.live(0) ? row * P.blocks + p.c / kBlock : 0);
+        if constexpr (kWide) {
+            codes = *reinterpret_cast<const uint2*>(at);
+            scales.x = *s;
+        } else {
+            uint32_t c[kPer], f[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                c[e] = at[p.live(e) ? 32 * e : 0];
+                f[e] = s[p.live(e) ? e : 0];
+            }
+            codes = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+            scales = make_uint2(f[0] | f[1] << 8 | f[2] << 16 | f[3] << 24, f[4] | f[5] << 8 | f[6] << 16 | f[7] << 24);
+        }
+    }
+    __device__ __forceinline__ float2 pair(int k) const {
+        const float2 v = value2((k < 2 ? codes.x : codes.y) >> (16 * (k & 1)) & 0xffffu);
+        if constexpr (kWide) return mul2(v, both(from_block(static_cast<int>(scales.x))));
+        const uint32_t f = (k < 2 ? scales.x : scales.y) >> (16 * (k & 1));
+        return mul2(v, make_float2(from_block(static_cast<int>(f & 0xffu)), from_block(static_cast<int>(f >> 8 & 0xffu))));
+    }
 };
-template <int kVec>
-__device__ __forceinline__ Held get_codes(const ActParams& P, int which, const Piece<kVec>& p) {
-    const size_t row = which * static_cast<size_t>(P.B) * P.N + p.row;
-    const unsigned char* const at = P.codes + row * P.C + p.c;
-    Held h;
-    if constexpr (kVec == 8) h.codes = *reinterpret_cast<const uint2*>(at);
-    else h.codes = make_uint2(*at, 0u);
-    h.scale = P.scales[row * P.blocks + p.c / kBlock];
-    return h;
-}
-template <int kVec>
-__device__ __forceinline__ void values_of(const Held& h, float (&v)[kVec]) {
-    const float mul = from_block(h.scale);
-    if constexpr (kVec == 8) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 f = value2((k < 2 ? h.codes.x : h.codes.y) >> (16 * (k & 1)) & 0xffffu, mul);
-            v[2 * k] = f.x;
-            v[2 * k + 1] = f.y;
+
+// kTasks neighbouring pieces to a warp.
+template <class F>
+__device__ __forceinline__ void for_instances(const ActParams& P, int tasks, F body) {
+#pragma unroll 1
+    for (int b = blockIdx.y; b < P.B; b += gridDim.y) {
+        const int n = P.n_sel ? min(max(__ldg(P.n_sel + (P.S > 1 ? b : 0)), 0), P.N) : P.N;
+        const uint32_t all = static_cast<uint32_t>(n) * static_cast<uint32_t>(P.chunks), step = gridDim.x * kActWarps * tasks;
+#pragma unroll 1
+        for (uint32_t t0 = (blockIdx.x * kActWarps + (threadIdx.x >> 5)) * tasks; t0 < all; t0 += step) {
+            Task t;
+            t.row = t0 / static_cast<uint32_t>(P.chunks);
+            t.chunk = t0 - t.row * static_cast<uint32_t>(P.chunks);
+            body(b, n, t);
+            if (all - t0 <= step) break;        // (no wrap)
         }
-    } else {
-        v[0] = value2(h.codes.x, mul).x;
     }
 }
 
-template <class T, int kVec, int kKind, bool kGated, int kTasks>
+template <class T, bool kWide, int kKind, bool kGated, int kTasks>
 __global__ void __launch_bounds__(kActThreads) act_fwd_kernel(const ActParams P) {
-    constexpr bool kFull = sizeof(T) == 4;
     chain_wait();
     chain_release();
-#pragma unroll 1
-    for (int b = blockIdx.y; b < P.B; b += gridDim.y) {
-        const int n = P.n_sel ? min(max(__ldg(P.n_sel + (P.S > 1 ? b : 0)), 0), P.N) : P.N;
-        const uint32_t t0 = blockIdx.x * kActWarps * kTasks + (threadIdx.x >> 5);
-        if (t0 >= static_cast<uint32_t>(n) * static_cast<uint32_t>(P.chunks)) continue;
-        Piece<kVec> p[kTasks];
-        Pack<T, kVec> a[kTasks], g[kTasks];
+    for_instances(P, kTasks, [&](int b, int n, Task t) {
+        Piece<kWide> p[kTasks];
+        Values<T, kWide> a[kTasks], g[kTasks];
 #pragma unroll
         for (int u = 0; u < kTasks; ++u) {
-            p[u] = piece_of<kVec>(P, b, n, t0 + u * kActWarps);
-            if (!p[u].live) continue;
+            p[u] = piece_of<kWide>(P, b, n, t);
+            if (++t.chunk == static_cast<uint32_t>(P.chunks)) {
+                t.chunk = 0;
+                ++t.row;
+            }
             const size_t at = static_cast<size_t>(p[u].row) * P.stride + p[u].c;
-            a[u] = load_pack<T, kVec>(static_cast<const T*>(P.a) + at);
-            if (kGated) g[u] = load_pack<T, kVec>(static_cast<const T*>(P.b) + at);
+            a[u].load(static_cast<const T*>(P.a), at, p[u]);
+            if (kGated) g[u].load(static_cast<const T*>(P.b), at, p[u]);
         }
 #pragma unroll
         for (int u = 0; u < kTasks; ++u) {
-            float va[kVec], vb[kVec];
-            Pack<T, kVec> y;
+            float2 va[kPer / 2], vb[kPer / 2];
+            Values<T, kWide> y;
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                va[e] = p[u].live ? to_float(a[u].e[e]) : 0.f;
-                vb[e] = kGated && p[u].live ? to_float(g[u].e[e]) : 1.f;
-                y.e[e] = from_float<T>(kGated ? act_of<kKind, kFull>(va[e]) * vb[e] : act_of<kKind, kFull>(va[e]));
+            for (int k = 0; k < kPer / 2; ++k) {
+                va[k] = make_float2(a[u].at(2 * k), a[u].at(2 * k + 1));
+                float2 f = act_of<kKind>(va[k]);
+                if (kGated) {
+                    vb[k] = make_float2(g[u].at(2 * k), g[u].at(2 * k + 1));
+                    f = mul2(f, vb[k]);
+                }
+                y.set(2 * k, f.x);
+                y.set(2 * k + 1, f.y);
             }
-            if (p[u].live) store_pack(static_cast<T*>(P.y) + static_cast<size_t>(p[u].row) * P.C + p[u].c, y);
+            y.store(static_cast<T*>(P.y) + static_cast<size_t>(p[u].row) * P.C + p[u].c, p[u]);
             if (P.codes) {
-                put_codes<T, kVec>(P, 0, p[u], va);
-                if (kGated) put_codes<T, kVec>(P, 1, p[u], vb);
+                put_codes<T, kWide>(P, 0, p[u], va);
+                if (kGated) put_codes<T, kWide>(P, 1, p[u], vb);
             }
         }
-    }
+    });
 }
 
-template <class T, int kVec, int kKind, bool kGated, int kTasks>
+template <class T, bool kWide, int kKind, bool kGated, int kTasks>
 __global__ void __launch_bounds__(kActThreads) act_bwd_kernel(const ActParams P) {
-    constexpr bool kFull = sizeof(T) == 4;
     chain_wait();
     chain_release();
-#pragma unroll 1
-    for (int b = blockIdx.y; b < P.B; b += gridDim.y) {
-        const int n = P.n_sel ? min(max(__ldg(P.n_sel + (P.S > 1 ? b : 0)), 0), P.N) : P.N;
-        const uint32_t t0 = blockIdx.x * kActWarps * kTasks + (threadIdx.x >> 5);
-        if (t0 >= static_cast<uint32_t>(n) * static_cast<uint32_t>(P.chunks)) continue;
-        Piece<kVec> p[kTasks];
-        Pack<T, kVec> d[kTasks];
-        Held ha[kTasks], hb[kTasks];
+    for_instances(P, kTasks, [&](int b, int n, Task t) {
+        Piece<kWide> p[kTasks];
+        Values<T, kWide> d[kTasks];
+        Held<kWide> ha[kTasks], hb[kTasks];
 #pragma unroll
         for (int u = 0; u < kTasks; ++u) {
-            p[u] = piece_of<kVec>(P, b, n, t0 + u * kActWarps);
-            if (!p[u].live) continue;
-            d[u] = load_pack<T, kVec>(static_cast<const T*>(P.d_y) + static_cast<size_t>(p[u].row) * P.C + p[u].c);
-            ha[u] = get_codes<kVec>(P, 0, p[u]);
-            if (kGated) hb[u] = get_codes<kVec>(P, 1, p[u]);
+            p[u] = piece_of<kWide>(P, b, n, t);
+            if (++t.chunk == static_cast<uint32_t>(P.chunks)) {
+                t.chunk = 0;
+                ++t.row;
+            }
+            d[u].load(static_cast<const T*>(P.d_y), static_cast<size_t>(p[u].row) * P.C + p[u].c, p[u]);
+            ha[u].load(P, 0, p[u]);
+            if (kGated) hb[u].load(P, 1, p[u]);
         }
 #pragma unroll
         for (int u = 0; u < kTasks; ++u) {
-            if (!p[u].live) continue;
-            float va[kVec], vb[kVec];
-            values_of<kVec>(ha[u], va);
-            if (kGated) values_of<kVec>(hb[u], vb);
-            Pack<T, kVec> da, db, y;
+            if (p[u].left <= 0) continue;
+            Values<T, kWide> da, db, y;
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                float f, slope;
-                act_slope<kKind, kFull>(va[e], f, slope);
-                const float dy = to_float(d[u].e[e]);
-                da.e[e] = from_float<T>((kGated ? dy * vb[e] : dy) * slope);
-                if (kGated) db.e[e] = from_float<T>(dy * f);
-                y.e[e] = from_float<T>(kGated ? f * vb[e] : f);
+            for (int k = 0; k < kPer / 2; ++k) {
+                const float2 va = ha[u].pair(k), dy = make_float2(d[u].at(2 * k), d[u].at(2 * k + 1));
+                float2 f, slope, gate = both(1.f);
+                act_slope<kKind>(va, f, slope);
+                if (kGated) gate = hb[u].pair(k);
+                const float2 ra = mul2(kGated ? mul2(dy, gate) : dy, slope);
+                da.set(2 * k, ra.x);
+                da.set(2 * k + 1, ra.y);
+                if (kGated) {
+                    const float2 rb = mul2(dy, f);
+                    db.set(2 * k, rb.x);
+                    db.set(2 * k + 1, rb.y);
+                    f = mul2(f, gate);
+                }
+                y.set(2 * k, f.x);
+                y.set(2 * k + 1, f.y);
             }
             const size_t at = static_cast<size_t>(p[u].row) * P.stride + p[u].c;
-            store_pack(static_cast<T*>(P.d_a) + at, da);
-            if (kGated) store_pack(static_cast<T*>(P.d_b) + at, db);
-            if (P.y) store_pack(static_cast<T*>(P.y) + static_cast<size_t>(p[u].row) * P.C + p[u].c, y);
+            da.store(static_cast<T*>(P.d_a) + at, p[u]);
+            if (kGated) db.store(static_cast<T*>(P.d_b) + at, p[u]);
+            if (P.y) y.store(static_cast<T*>(P.y) + static_cast<size_t>(p[u].row) * P.C + p[u].c, p[u]);
         }
-    }
+    });
 }
 
 template <class F>
@@ -275,7 +388,8 @@ CkptLayout ckpt_layout(const vardrop_act_cfg& c) {
     return l;
 }
 
-constexpr int kActTasks = 4, kMaxGridY = 65535;
+constexpr int kActTasks = 2, kActPerSm = 6, kMaxGridY = 65535;
+long long ceil_div_ll(long long a, long long b) { return (a + b - 1) / b; }
 template <bool kBwd>
 int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cudaStream_t stream) {
     P.n_sel = n_sel;
@@ -283,24 +397,28 @@ int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cuda
     P.stride = c.stride ? c.stride : c.C;
     P.blocks = ckpt_layout(c).blocks;
     const bool wide = c.C % 8 == 0;             // (a stride is a multiple of 8 wherever there is one)
-    P.chunks = wide ? (c.C + 255) / 256 : P.blocks;
+    P.chunks = (c.C + 32 * kPer - 1) / (32 * kPer);
     const long long tasks = static_cast<long long>(c.N) * P.chunks;
     // several pieces to a warp only where every SM still gets four CTAs
     const bool many = tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
     const int per = kActWarps * (many ? kActTasks : 1);
-    const dim3 grid(static_cast<unsigned>((tasks + per - 1) / per), c.B < kMaxGridY ? c.B : kMaxGridY);
+    // Every row counts: a CTA for each few pieces.  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their instance's pieces (a CTA for each few pieces
+    // of all rows, four of five of them without work, made 172 of 862 kept rows of 32 instances 52.7 us instead of 35).
+    const long long full = (tasks + per - 1) / per, held = ceil_div_ll(static_cast<long long>(sm_count()) * kActPerSm, c.B);
+    const dim3 grid(static_cast<unsigned>(n_sel && held < full ? held : full), c.B < kMaxGridY ? c.B : kMaxGridY);
     LaunchScope ls_(kBwd ? K_ACT_BWD : K_ACT_FWD, stream);
     const cudaError_t err = with_dtype(c.dtype, [&](auto t) {
         return with_kind(c.kind, c.gated != 0, [&](auto kind, auto gated) {
             using T = decltype(t);
             constexpr int kKind = decltype(kind)::value;
             constexpr bool kGated = decltype(gated)::value != 0;
-            auto go = [&](auto vec, auto count) {
-                constexpr int kVec = decltype(vec)::value, kTasks = decltype(count)::value;
-                if constexpr (kBwd) return launch_chained(act_bwd_kernel<T, kVec, kKind, kGated, kTasks>, grid, dim3(kActThreads), 0, stream, P);
-                else return launch_chained(act_fwd_kernel<T, kVec, kKind, kGated, kTasks>, grid, dim3(kActThreads), 0, stream, P);
+            auto go = [&](auto by, auto count) {
+                constexpr bool kWide = decltype(by)::value != 0;
+                constexpr int kTasks = decltype(count)::value;
+                if constexpr (kBwd) return launch_chained(act_bwd_kernel<T, kWide, kKind, kGated, kTasks>, grid, dim3(kActThreads), 0, stream, P);
+                else return launch_chained(act_fwd_kernel<T, kWide, kKind, kGated, kTasks>, grid, dim3(kActThreads), 0, stream, P);
             };
-            return wide ? (many ? go(VecSize<8>{}, VecSize<kActTasks>{}) : go(VecSize<8>{}, VecSize<1>{})) : (many ? go(VecSize<1>{}, VecSize<kActTasks>{}) : go(VecSize<1>{}, VecSize<1>{}));
+            return wide ? (many ? go(VecSize<1>{}, VecSize<kActTasks>{}) : go(VecSize<1>{}, VecSize<1>{})) : (many ? go(VecSize<0>{}, VecSize<kActTasks>{}) : go(VecSize<0>{}, VecSize<1>{}));
         });
     });
     return check_cuda(err, kBwd ? "act: backward launch" : "act: forward launch");

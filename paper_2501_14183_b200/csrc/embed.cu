@@ -18,11 +18,13 @@ namespace vardrop {
 namespace {
 
 constexpr int kEmbedThreads = 256;
-constexpr int kSortThreads = 1024, kSortItems = 4, kSortTile = kSortThreads * kSortItems;      // tokens that a CTA ranks at a time
-constexpr int kSortWarps = kSortThreads / 32;
+// Tokens that a CTA ranks at a time.  Many tokens: small tiles, whose ranks are a shorter chain of steps over more CTAs.  Up to 4096 of them: one CTA for every pass.
+constexpr int kSortItems = 4, kSortThreads = 256, kSortTile = kSortThreads * kSortItems, kOneThreads = 1024, kOneTile = kOneThreads * kSortItems;
 constexpr int kMaxDigitBits = 9, kMaxBins = 1 << kMaxDigitBits;
 constexpr int kMaxSortBlocks = 256;             // beyond, a CTA takes several tiles: the offsets of a digit are summed over all CTAs by each of them
-constexpr int kSumBatch = 4;                    // rows that a thread of the sums has on their way
+constexpr int kSumBatch = 8;                    // rows that a thread of the sums has on their way
+constexpr int kJoinBatch = 8;                   // pieces
+constexpr int kSumTokens = 16 * kEmbedThreads;  // that a CTA of the sums holds in shared memory
 constexpr int kLeastShare = 8, kMostShare = 128;  // sorted tokens of a share: fewer make more pieces, more leave long chains of loads
 
 struct SortPlan {
@@ -53,7 +55,7 @@ SumPlan sum_plan(const vardrop_embed_cfg& c) {
     p.slabs = (vectors + p.lanes - 1) / p.lanes;
     const long long wanted = 148ll * 1024 / (static_cast<long long>(p.lanes) * p.slabs);      // (a constant, so that sums do not depend on the device)
     const long long share = (c.T + std::max(wanted, 1ll) - 1) / std::max(wanted, 1ll);
-    p.share = static_cast<int>(std::min<long long>(std::max<long long>(share, kLeastShare), kMostShare));
+    p.share = static_cast<int>(std::min<long long>(std::max<long long>(share, kLeastShare), std::min(kMostShare, kSumTokens / (kEmbedThreads / p.lanes))));
     p.shares = (c.T + p.share - 1) / p.share;
     return p;
 }
@@ -107,9 +109,9 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_fwd_kernel(const EmbedPar
 #pragma unroll 1
     for (int c = lane * kVec; c < P.C; c += P.lanes * kVec) {
         Pack<Tab, kVec> in[kTokens];
+        // (without a condition, here and in the sums: a load behind a branch is waited for where the branches join, which made a batch of them a chain)
 #pragma unroll
-        for (int u = 0; u < kTokens; ++u)
-            if (row[u] >= 0) in[u] = load_pack<Tab, kVec>(table + static_cast<size_t>(row[u]) * P.C + c);
+        for (int u = 0; u < kTokens; ++u) in[u] = load_pack<Tab, kVec>(table + static_cast<size_t>(max(row[u], 0)) * P.C + c);
 #pragma unroll
         for (int u = 0; u < kTokens; ++u) {
             const long long t = t0 + u * groups;
@@ -152,88 +154,100 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortPar
     }
 }
 
+template <int kThreads>
 struct SortShared {
-    uint16_t count[kSortWarps][kMaxBins];       // of a digit in a warp's tokens, then in those of the warps ahead
+    uint16_t count[kThreads / 32][kMaxBins];    // of a digit in a warp's tokens, then in those of the warps ahead
     int base[kMaxBins];                         // place of the digit's next token
-    int part[kSortThreads / 32][2];
-    int sum[2][kSortThreads];
+    int total[kMaxBins];
+    int part[32];
 };
-// Places of a tile's tokens: warp w has the tokens from 128 w on, 32 at a time.  place[i] is added to base[digit].  Moves base on.
-__device__ __forceinline__ void rank_tile(SortShared& S, int bins, const int (&digit)[kSortItems], const bool (&there)[kSortItems], int (&place)[kSortItems]) {
+// Places of a tile's tokens: warp w has the tokens from 128 w on, 32 at a time.  Leaves the tile's tokens of each digit in `total`.
+template <int kThreads>
+__device__ __forceinline__ void rank_tile(SortShared<kThreads>& S, int bins, const int (&digit)[kSortItems], const bool (&there)[kSortItems], int (&place)[kSortItems]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int d = lane; d < bins; d += 32) S.count[warp][d] = 0;
+    for (int d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(S.count[warp])[d] = 0;
     __syncwarp();
     int rank[kSortItems];
+    uint32_t peers[kSortItems];
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
         const uint32_t active = __ballot_sync(0xffffffffu, there[i]);
-        if (there[i]) {
-            const uint32_t peers = __match_any_sync(active, digit[i]);
-            rank[i] = S.count[warp][digit[i]] + __popc(peers & ((1u << lane) - 1));
-            __syncwarp(active);
-            if ((peers >> lane) == 1u) S.count[warp][digit[i]] += static_cast<uint16_t>(__popc(peers));      // the last of them
-        }
+        peers[i] = __match_any_sync(0xffffffffu, digit[i]) & active;
+    }
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        if (there[i]) rank[i] = S.count[warp][digit[i]] + __popc(peers[i] & ((1u << lane) - 1));
+        __syncwarp();
+        if (there[i] && (peers[i] >> lane) == 1u) S.count[warp][digit[i]] += static_cast<uint16_t>(__popc(peers[i]));      // the last of them
         __syncwarp();
     }
     __syncthreads();
-    int total = 0;
-    if (threadIdx.x < bins) {
+#pragma unroll
+    for (int d = threadIdx.x; d < bins; d += kThreads) {
+        int total = 0;
 #pragma unroll 8
-        for (int w = 0; w < kSortWarps; ++w) {
-            const int n = S.count[w][threadIdx.x];
-            S.count[w][threadIdx.x] = static_cast<uint16_t>(total);
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const int n = S.count[w][d];
+            S.count[w][d] = static_cast<uint16_t>(total);
             total += n;
         }
+        S.total[d] = total;
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) place[i] = there[i] ? S.base[digit[i]] + S.count[warp][digit[i]] + rank[i] : 0;
-    __syncthreads();
-    if (threadIdx.x < bins) S.base[threadIdx.x] += total;
+    for (int i = 0; i < kSortItems; ++i) place[i] = there[i] ? S.count[warp][digit[i]] + rank[i] : 0;
 }
-// base[d] = (tokens of smaller digits) + ahead[d], from the totals of the digits (a value a thread, 0 from bins on).
-__device__ __forceinline__ void digit_bases(SortShared& S, int bins, int total, int ahead) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int up = total;
+// base[d] = (tokens of smaller digits) + base[d], from the totals of the digits: a thread has those from kEach of its number on.
+template <int kThreads>
+__device__ __forceinline__ void digit_bases(SortShared<kThreads>& S, int bins, const int* totals) {
+    constexpr int kEach = kMaxBins > kThreads ? kMaxBins / kThreads : 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d0 = threadIdx.x * kEach;
+    int own[kEach], sum = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        own[e] = d0 + e < bins ? totals[d0 + e] : 0;
+        sum += own[e];
+    }
+    int up = sum;
 #pragma unroll
     for (int s = 1; s < 32; s *= 2) {
         const int n = __shfl_up_sync(0xffffffffu, up, s);
         if (lane >= s) up += n;
     }
-    if (lane == 31) S.part[warp][0] = up;
+    if (lane == 31) S.part[warp] = up;
     __syncthreads();
-    int before = 0;
-    for (int w = 0; w < warp; ++w) before += S.part[w][0];
-    if (threadIdx.x < bins) S.base[threadIdx.x] = before + up - total + ahead;
+    int before = up - sum;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w)
+        if (w < warp) before += S.part[w];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        if (d0 + e < bins) S.base[d0 + e] += before;
+        before += own[e];
+    }
     __syncthreads();
 }
 
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortParams P) {
-    extern __shared__ unsigned char smem_dyn[];
-    SortShared& S = *reinterpret_cast<SortShared*>(smem_dyn);
+    __shared__ SortShared<kSortThreads> S;
     chain_wait();
     chain_release();
     const int bins = 1 << P.bits, shift = P.pass * P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    // the digit's tokens in all CTAs and in those ahead of this one, summed by several threads a digit
-    const int d = tid & (bins - 1), parts = kSortThreads >> P.bits, part = tid >> P.bits;
     const int32_t* const counts = P.counts + static_cast<size_t>(P.pass) * P.blocks * kMaxBins;
-    int all = 0, ahead = 0;
-#pragma unroll 4
-    for (int b = part; b < P.blocks; b += parts) {
-        const int n = __ldcg(counts + static_cast<size_t>(b) * kMaxBins + d);
-        all += n;
-        if (b < static_cast<int>(blockIdx.x)) ahead += n;
-    }
-    S.sum[0][tid] = all;
-    S.sum[1][tid] = ahead;
-    __syncthreads();
-    all = ahead = 0;
-    if (tid < bins)
-        for (int p = 0; p < parts; ++p) {
-            all += S.sum[0][p * bins + tid];
-            ahead += S.sum[1][p * bins + tid];
+    // the digit's tokens in all CTAs and in those ahead of this one
+    for (int d = tid; d < bins; d += kSortThreads) {
+        int all = 0, ahead = 0;
+#pragma unroll 16
+        for (int b = 0; b < P.blocks; ++b) {
+            const int n = __ldcg(counts + static_cast<size_t>(b) * kMaxBins + d);
+            all += n;
+            if (b < static_cast<int>(blockIdx.x)) ahead += n;
         }
-    digit_bases(S, bins, all, ahead);
+        S.total[d] = all;
+        S.base[d] = ahead;
+    }
+    __syncthreads();
+    digit_bases(S, bins, S.total);
     const bool last = P.pass + 1 == P.passes;
     int32_t* const next = P.counts + static_cast<size_t>(P.pass + 1) * P.blocks * kMaxBins;
 #pragma unroll 1
@@ -252,21 +266,29 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortPara
         rank_tile(S, bins, digit, there, place);
 #pragma unroll
         for (int i = 0; i < kSortItems; ++i) {
-            if (!there[i]) continue;
-            P.keys_out[place[i]] = key[i];
-            P.tokens_out[place[i]] = token[i];
-            if (!last) atomicAdd(next + static_cast<size_t>(place[i] / (P.tiles_per_block * kSortTile)) * kMaxBins + ((key[i] >> (shift + P.bits)) & (bins - 1)), 1);
+            const int to = place[i] + S.base[digit[i]];
+            if (there[i]) {
+                P.keys_out[to] = key[i];
+                P.tokens_out[to] = token[i];
+            }
+            if (!last) {                        // counts of the next pass, once for lanes that count alike
+                const int at = static_cast<int>(static_cast<uint32_t>(to) / (P.tiles_per_block * kSortTile)) * kMaxBins + ((key[i] >> (shift + P.bits)) & (bins - 1));
+                const uint32_t alike = __match_any_sync(0xffffffffu, there[i] ? at : -1);
+                if (there[i] && (alike >> lane) == 1u) atomicAdd(next + at, __popc(alike));
+            }
         }
+        __syncthreads();
+        for (int d = tid; d < bins; d += kSortThreads) S.base[d] += S.total[d];
         __syncthreads();
     }
 }
 
 // Up to a tile of tokens: every pass by one CTA.
-__global__ void __launch_bounds__(kSortThreads) embed_sort_small_kernel(const SortParams P) {
+__global__ void __launch_bounds__(kOneThreads) embed_sort_small_kernel(const SortParams P) {
     extern __shared__ unsigned char smem_dyn[];
-    SortShared& S = *reinterpret_cast<SortShared*>(smem_dyn);
-    int* const keys = reinterpret_cast<int*>(smem_dyn + sizeof(SortShared));
-    int* const tokens = keys + kSortTile;
+    SortShared<kOneThreads>& S = *reinterpret_cast<SortShared<kOneThreads>*>(smem_dyn);
+    int* const keys = reinterpret_cast<int*>(smem_dyn + sizeof(SortShared<kOneThreads>));
+    int* const tokens = keys + kOneTile;
     chain_wait();
     chain_release();
     const int bins = 1 << P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -283,12 +305,10 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_small_kernel(const So
     for (int pass = 0; pass < P.passes; ++pass) {
         const int shift = pass * P.bits;
         if (tid < bins) S.base[tid] = 0;
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < kSortItems; ++i) digit[i] = (key[i] >> shift) & (bins - 1);
-        rank_tile(S, bins, digit, there, place);            // places among equal digits; base: how many there are
-        __syncthreads();
-        digit_bases(S, bins, tid < bins ? S.base[tid] : 0, 0);
+        rank_tile(S, bins, digit, there, place);
+        digit_bases(S, bins, S.total);
         const bool last = pass + 1 == P.passes;
 #pragma unroll
         for (int i = 0; i < kSortItems; ++i) {
@@ -358,13 +378,24 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParam
         }
         return;
     }
+    // the CTA's shares of the sorted tokens at once, so that no row waits for its token's number
+    __shared__ int keys[kSumTokens + 2], tokens[kSumTokens];
     const int groups = kEmbedThreads / P.lanes, group = threadIdx.x / P.lanes, lane = threadIdx.x & (P.lanes - 1);
+    const long long first_token = static_cast<long long>(blockIdx.x) * groups * P.share;
+    const int held = static_cast<int>(min(static_cast<long long>(groups) * P.share, P.T - first_token));
+    for (int i = threadIdx.x; i < held; i += kEmbedThreads) {
+        keys[i + 1] = __ldcg(P.keys + first_token + i);
+        tokens[i] = __ldcg(P.tokens + first_token + i);
+    }
+    if (threadIdx.x == 0) keys[0] = first_token > 0 ? __ldcg(P.keys + first_token - 1) : -1;
+    if (threadIdx.x == 32) keys[held + 1] = first_token + held < P.T ? __ldcg(P.keys + first_token + held) : -1;
+    __syncthreads();
     const int share = blockIdx.x * groups + group, c = (blockIdx.y * P.lanes + lane) * kVec;
     if (share >= P.shares || c >= P.C) return;
-    const long long begin = static_cast<long long>(share) * P.share, end = min(static_cast<long long>(P.T), begin + P.share);
+    const int begin = group * P.share, end = min(held, begin + P.share);
     const Out* const d_out = static_cast<const Out*>(P.d_out) + c;
     float* const pieces = P.pieces + static_cast<size_t>(share) * 2 * P.C + c;
-    const int ahead = begin > 0 ? __ldcg(P.keys + begin - 1) : -1, behind = end < P.T ? __ldcg(P.keys + end) : -1;
+    const int ahead = keys[begin], behind = keys[end + 1];
     float sum[kVec];
     int row = -1;                               // that `sum` is of
     bool first = true;                          // it is the share's first one
@@ -375,61 +406,109 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParam
             finish_row<Tab, kVec>(P, row, c, sum);
             return;
         }
-        float* const to = pieces + (from_ahead ? 0 : P.C);
+        Pack<float, kVec> to;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) to[e] = sum[e];
+        for (int e = 0; e < kVec; ++e) to.e[e] = sum[e];
+        store_pack(pieces + (from_ahead ? 0 : P.C), to);
     };
 #pragma unroll 1
-    for (long long i = begin; i < end; i += kSumBatch) {
-        int key[kSumBatch];
+    for (int i = begin; i < end; i += kSumBatch) {
         Pack<Out, kVec> in[kSumBatch];
 #pragma unroll
-        for (int u = 0; u < kSumBatch; ++u) {
-            key[u] = i + u < end ? __ldcg(P.keys + i + u) : P.V;
-            if (key[u] < P.V) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(__ldcg(P.tokens + i + u)) * P.C);
-        }
+        for (int u = 0; u < kSumBatch; ++u) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(tokens[min(i + u, end - 1)]) * P.C);
 #pragma unroll
         for (int u = 0; u < kSumBatch; ++u) {
             if (i + u >= end) break;
-            if (key[u] != row) {
+            const int key = keys[i + u + 1];
+            if (key != row) {
                 leave(false);
                 first = row < 0;
-                row = key[u];
+                row = key;
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
             }
-            if (row == P.V) continue;
+            if (row == P.V) return;             // nothing but tokens without a row behind it (the row ahead is done)
 #pragma unroll
             for (int e = 0; e < kVec; ++e) sum[e] += to_float(in[u].e[e]);
         }
-        if (row == P.V) return;                 // nothing but tokens without a row behind it (the row ahead is done)
     }
     leave(true);
 }
-// Rows in pieces: the share that a row begins in adds them up.
+// Rows in pieces: the share that a row begins in adds them up, a warp for 32 accesses of columns; of rows in many pieces (frequent tokens) all warps of the CTA, every eighth piece each.
+constexpr int kJoinWarps = kEmbedThreads / 32, kFewPieces = 8;
+template <int kVec>
+__device__ __forceinline__ void add_pieces(const float* at, size_t step, int count, float (&sum)[kVec]) {
+#pragma unroll 1
+    for (int s = 0; s < count; s += kJoinBatch, at += kJoinBatch * step) {
+        Pack<float, kVec> piece[kJoinBatch];
+#pragma unroll
+        for (int u = 0; u < kJoinBatch; ++u) piece[u] = load_pack<float, kVec>(at + step * min(u, count - 1 - s));
+#pragma unroll
+        for (int u = 0; u < kJoinBatch; ++u)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum[e] += s + u < count ? piece[u].e[e] : 0.f;
+    }
+}
 template <class Tab, int kVec>
 __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumParams P) {
+    __shared__ int many[kJoinWarps][2];                     // row and number of pieces behind its first one, 0: none
+    __shared__ float parts[kJoinWarps][32 * kVec];
     chain_wait();
     chain_release();
-    const int groups = kEmbedThreads / P.lanes, group = threadIdx.x / P.lanes, lane = threadIdx.x & (P.lanes - 1);
-    const int share = blockIdx.x * groups + group, c = (blockIdx.y * P.lanes + lane) * kVec;
-    if (share + 1 >= P.shares || c >= P.C) return;
-    const long long begin = static_cast<long long>(share) * P.share, end = begin + P.share;
-    const int row = __ldcg(P.keys + end - 1);
-    if (row == P.V || __ldcg(P.keys + end) != row) return;
-    if (begin > 0 && __ldcg(P.keys + begin) == row && __ldcg(P.keys + begin - 1) == row) return;        // begins further ahead
-    const float* at = P.pieces + static_cast<size_t>(share) * 2 * P.C + P.C + c;
-    float sum[kVec];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = blockIdx.x * kJoinWarps + warp, c = (blockIdx.y * 32 + lane) * kVec;
+    int row = P.V, count = 0;
+    if (share + 1 < P.shares) {
+        const long long begin = static_cast<long long>(share) * P.share, end = begin + P.share;
+        const int ahead = begin > 0 ? __ldcg(P.keys + begin - 1) : -1, first = __ldcg(P.keys + begin), last = __ldcg(P.keys + end - 1), behind = __ldcg(P.keys + end);
+        if (last != P.V && behind == last && !(first == last && ahead == last)) row = last;       // goes on behind this share, and did not begin ahead of it
+    }
+    if (row != P.V) {                                       // shares behind this one that begin with the row: by 32, then one by one
+        const auto begins = [&](int s) { return s < P.shares && __ldcg(P.keys + static_cast<long long>(s) * P.share) == row; };
+        count = 1;
+        int more;
+        do {
+            more = __popc(__ballot_sync(0xffffffffu, begins(share + count + 32 * (lane + 1))));
+            count += 32 * more;
+        } while (more == 32);
+        count += __popc(__ballot_sync(0xffffffffu, begins(share + count + lane + 1)));
+    }
+    const auto piece = [&](int s, int which) { return P.pieces + (static_cast<size_t>(s) * 2 + which) * P.C + (c < P.C ? c : 0); };
+    const auto own = [&](float (&sum)[kVec], int s) {
+        const Pack<float, kVec> v = load_pack<float, kVec>(piece(s, 1));
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) sum[e] = at[e];
-    int last = share + 1;                       // the share that the row ends in
-    while (last + 1 < P.shares && __ldcg(P.keys + static_cast<long long>(last + 1) * P.share) == row) ++last;
-    at += P.C;
-#pragma unroll 8
-    for (int s = share + 1; s <= last; ++s, at += 2 * P.C)
+        for (int e = 0; e < kVec; ++e) sum[e] = v.e[e];
+    };
+    const size_t step = static_cast<size_t>(2) * P.C;
+    if (row != P.V && count <= kFewPieces) {
+        float sum[kVec];
+        own(sum, share);
+        add_pieces<kVec>(piece(share + 1, 0), step, count, sum);
+        if (c < P.C) finish_row<Tab, kVec>(P, row, c, sum);
+    }
+    if (lane == 0) {
+        many[warp][0] = row;
+        many[warp][1] = count > kFewPieces ? count : 0;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int w = 0; w < kJoinWarps; ++w) {
+        const int pieces = many[w][1], s = blockIdx.x * kJoinWarps + w;
+        if (pieces == 0) continue;                          // (of the whole CTA)
+        float sum[kVec] = {};
+        add_pieces<kVec>(piece(s + 1 + warp, 0), kJoinWarps * step, (pieces - warp + kJoinWarps - 1) / kJoinWarps, sum);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sum[e] += __ldcg(at + e);
-    finish_row<Tab, kVec>(P, row, c, sum);
+        for (int e = 0; e < kVec; ++e) parts[warp][e * 32 + lane] = sum[e];
+        __syncthreads();
+        if (warp == w) {
+            own(sum, s);
+#pragma unroll
+            for (int k = 0; k < kJoinWarps; ++k)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) sum[e] += parts[k][e * 32 + lane];
+            if (c < P.C) finish_row<Tab, kVec>(P, many[w][0], c, sum);
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace
@@ -476,20 +555,19 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     int32_t* const keys[2] = {reinterpret_cast<int32_t*>(base + w.keys[0]), reinterpret_cast<int32_t*>(base + w.keys[1])};
     int32_t* const tokens[2] = {reinterpret_cast<int32_t*>(base + w.tokens[0]), reinterpret_cast<int32_t*>(base + w.tokens[1])};
     SortParams S{idx, nullptr, nullptr, keys[0], tokens[0], reinterpret_cast<int32_t*>(base + w.counts), static_cast<int*>(ws), c.T, c.V, s.bits, 0, s.passes, s.blocks, s.tiles_per_block};
-    constexpr int kSmall = static_cast<int>(sizeof(SortShared)) + 2 * kSortTile * static_cast<int>(sizeof(int)), kLarge = static_cast<int>(sizeof(SortShared));
+    constexpr int kSmall = static_cast<int>(sizeof(SortShared<kOneThreads>)) + 2 * kOneTile * static_cast<int>(sizeof(int));
     static thread_local int attr_dev = -1;
     int dev = 0;
     cudaGetDevice(&dev);
     if (attr_dev != dev) {
         if (int st = check_cuda(cudaFuncSetAttribute(embed_sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmall), "embed: smem attribute")) return st;
-        if (int st = check_cuda(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLarge), "embed: smem attribute")) return st;
         attr_dev = dev;
     }
     cudaError_t err;
     int at = 0;                                 // of the sorted arrays
-    if (c.T <= kSortTile) {
+    if (c.T <= kOneTile) {
         LaunchScope ls_(K_EMBED_SORT, stream);
-        err = launch_chained(embed_sort_small_kernel, dim3(1), dim3(kSortThreads), kSmall, stream, S);
+        err = launch_chained(embed_sort_small_kernel, dim3(1), dim3(kOneThreads), kSmall, stream, S);
         if (int st = check_cuda(err, "embed: sort launch")) return st;
     } else {
         { LaunchScope ls_(K_EMBED_COUNT, stream); err = launch_chained(embed_count_kernel, dim3(s.blocks), dim3(kSortThreads), 0, stream, S); }
@@ -498,7 +576,7 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
             at = S.pass & 1;
             S.keys = keys[at ^ 1]; S.tokens = tokens[at ^ 1];
             S.keys_out = keys[at]; S.tokens_out = tokens[at];
-            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_chained(embed_sort_kernel, dim3(s.blocks), dim3(kSortThreads), kLarge, stream, S); }
+            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_chained(embed_sort_kernel, dim3(s.blocks), dim3(kSortThreads), 0, stream, S); }
             if (int st = check_cuda(err, "embed: sort launch")) return st;
         }
     }
@@ -518,10 +596,11 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     }
     if (int st = check_cuda(err, "embed: sum launch")) return st;
     if (u.shares == 1) return VARDROP_OK;
+    const dim3 join((u.shares + kJoinWarps - 1) / kJoinWarps, (c.C / u.vec + 31) / 32);
     {
         LaunchScope ls_(K_EMBED_JOIN, stream);
         err = with_dtype(c.dtype, [&](auto tab) {
-            return with_vector(u.vec, [&](auto vec) { return launch_chained(embed_join_kernel<decltype(tab), decltype(vec)::value>, dim3(P.share_blocks, u.slabs), dim3(kEmbedThreads), 0, stream, P); });
+            return with_vector(u.vec, [&](auto vec) { return launch_chained(embed_join_kernel<decltype(tab), decltype(vec)::value>, join, dim3(kEmbedThreads), 0, stream, P); });
         });
     }
     return check_cuda(err, "embed: join launch");

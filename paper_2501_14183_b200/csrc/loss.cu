@@ -1,8 +1,8 @@
 // Softmax cross entropy over a vocabulary, logits l = scale h w^T, without the logits in memory:
 //   lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,label;      G = g_t scale (exp(l_tv - lse_t) - [v = label]),  d_h = G w,  d_w = G^T h
 //
-// loss_rows_kernel    tokens that have a label, one behind the other: positions, labels, and backward lse and the factor of their rows.  Only these take part in any product.
-// loss_pack_kernel    their rows of h, where some tokens have none.
+// loss_rows_kernel    tokens that have a label, one behind the other: positions, labels, and backward lse and the factor of their rows; where some have none, also their rows of h.  Only these take
+//                     part in any product.
 // loss_stats_kernel   products of 256 tokens x 256 rows of w; of each row of a tile the maximum and the sum of exponentials go to memory, and the label's logit.
 // loss_join_kernel    lse and loss from these.
 // loss_grad_kernel    backward, for a piece of the vocabulary at a time: the same products again, G of the piece to memory in 16 bits.
@@ -33,7 +33,7 @@ constexpr size_t kPieceBytes = 256u << 20;           // of G; larger pieces make
 constexpr int kLeastPiece = 1024, kMostSplits = 16, kSplitChunks = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
-enum LossWord { kLossRows = 16, kLossFactor, kLossInverse };      // words of the workspace's header: labelled tokens; the power of two that G is scaled by, and its inverse
+enum LossWord { kLossRows = 16, kLossFactor, kLossInverse };      // words of the workspace's header: labelled tokens; what G is scaled by, and its inverse
 
 int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
 
@@ -81,51 +81,111 @@ struct RowsParams {
     const int32_t* labels;
     const float *lse, *d_loss;                          // backward
     float *loss, *lse_out;                              // forward: zeros where there is no label
+    const uint4* h;
+    uint4* packed;
     int32_t *place, *pos, *label;                       // token of a row; row of a token, or -1; label of a row
     float *row_lse, *factor;
     int* header;
-    int T, V;
+    int T, V, share, vectors;                           // tokens of a CTA; 16-byte vectors of a row
 };
-constexpr int kRowsThreads = 1024;
+constexpr int kRowsThreads = 256, kRowsWarps = kRowsThreads / 32, kLeastTokens = 64, kRowsGrid = 296;
+__device__ __forceinline__ float block_max(float v, float* shared) {
+    v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRowsWarps; ++w) v = fmaxf(v, shared[w]);
+    return v;
+}
+// Every CTA counts the labels ahead of its tokens, and all of them, for itself: 64 KB out of L2 for 16384 tokens, and no launch or wait in between (one CTA for all took 27 us for 8192 tokens, this takes 4).
 __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParams P) {
-    __shared__ int warps[32];
-    __shared__ float most[32];
+    __shared__ int sums[2][kRowsWarps], counts[kRowsWarps];
+    __shared__ int rows[kRowsThreads];
+    __shared__ float most[kRowsWarps];
     chain_wait();
     chain_release();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int ahead = 0;
-    float top = 0.f;
-#pragma unroll 1
-    for (long long t0 = 0; t0 < P.T; t0 += kRowsThreads) {
-        const long long t = t0 + threadIdx.x;
-        int label = t < P.T ? __ldg(P.labels + t) : -1;
-        if (label >= P.V) {
-            set_status(P.header, VARDROP_ERR_INVALID_ARG);
-            label = -1;
-        }
-        const bool there = label >= 0;
-        const uint32_t mask = __ballot_sync(0xffffffffu, there);
-        if (lane == 0) warps[warp] = __popc(mask);
-        __syncthreads();
-        int before = 0, all = 0;
-        const int n = warps[lane];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long begin = static_cast<long long>(blockIdx.x) * P.share, end = min(static_cast<long long>(P.T), begin + P.share);
+    const auto live = [&](int label) { return label >= 0 && label < P.V ? 1 : 0; };
+    int ahead = 0, all = 0;
+    const int quads = P.T >> 2;
+#pragma unroll 8
+    for (int i = tid; i < quads; i += kRowsThreads) {
+        const int4 l = __ldg(reinterpret_cast<const int4*>(P.labels) + i);
+        const int k = live(l.x) + live(l.y) + live(l.z) + live(l.w);
+        all += k;
+        if (4ll * i < begin) ahead += k;                // (shares are multiples of four tokens)
+    }
+    for (int t = quads * 4 + tid; t < P.T; t += kRowsThreads) {
+        const int k = live(__ldg(P.labels + t));
+        all += k;
+        if (t < begin) ahead += k;
+    }
+    all = __reduce_add_sync(0xffffffffu, all);
+    ahead = __reduce_add_sync(0xffffffffu, ahead);
+    if (lane == 0) {
+        sums[0][warp] = all;
+        sums[1][warp] = ahead;
+    }
+    __syncthreads();
+    all = ahead = 0;
 #pragma unroll
-        for (int w = 0; w < 32; ++w) {
-            const int k = __shfl_sync(0xffffffffu, n, w);
-            if (w < warp) before += k;
-            all += k;
+    for (int w = 0; w < kRowsWarps; ++w) {
+        all += sums[0][w];
+        ahead += sums[1][w];
+    }
+    const int n = all;
+    if (blockIdx.x == 0) {
+        float top = 0.f;
+        if (P.lse) {
+#pragma unroll 4
+            for (int t = tid; t < P.T; t += kRowsThreads) {
+                const float g = fabsf(__ldg(P.d_loss + t));
+                if (live(__ldg(P.labels + t)) && isfinite(g)) top = fmaxf(top, g);
+            }
+            top = block_max(top, most);
         }
-        const int row = ahead + before + __popc(mask & ((1u << lane) - 1));
-        if (t < P.T) {
+        if (tid == 0) {
+            // G is stored times what takes the largest factor to 16320 = 255 2^6: fp16 has room for it and for 2^-38 of it, and where all factors are alike, as in a mean, the largest entries,
+            // factor (p - 1) at the labels, lose no bits but those of p (a power of two instead left d_w off by 2.5e-3 of its norm where rounding it alone leaves 1.6e-3)
+            const float up = top > 0.f ? fminf(16320.f / top, 8.5e37f) : 1.f;
+            P.header[kLossRows] = n;
+            P.header[kLossFactor] = __float_as_int(up);
+            P.header[kLossInverse] = __float_as_int(1.f / up);
+        }
+    }
+    const bool packs = n != P.T;
+    if (packs && blockIdx.x == gridDim.x - 1) {         // rows of zeros up to a whole chunk: zero times what lies there need not be zero
+        const int fill = (n + kChunk - 1) / kChunk * kChunk;
+        for (long long i = static_cast<long long>(n) * P.vectors + tid; i < static_cast<long long>(fill) * P.vectors; i += kRowsThreads) P.packed[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll 1
+    for (long long t0 = begin; t0 < end; t0 += kRowsThreads) {
+        const long long t = t0 + tid;
+        const int label = t < end ? __ldg(P.labels + t) : -1;
+        if (label >= P.V) set_status(P.header, VARDROP_ERR_INVALID_ARG);
+        const bool there = live(label) != 0;
+        const uint32_t mask = __ballot_sync(0xffffffffu, there);
+        __syncthreads();                                // rows and counts of the tokens before are read
+        if (lane == 0) counts[warp] = __popc(mask);
+        __syncthreads();
+        int row = ahead + __popc(mask & ((1u << lane) - 1));
+#pragma unroll
+        for (int w = 0; w < kRowsWarps; ++w) {
+            if (w < warp) row += counts[w];
+            ahead += counts[w];
+        }
+        rows[tid] = there ? row : -1;
+        if (t < end) {
             if (there) {
                 P.place[row] = static_cast<int>(t);
                 P.label[row] = label;
                 if (P.lse) {
-                    const float lse = P.lse[t], g = P.d_loss[t];
+                    const float lse = __ldg(P.lse + t);
                     P.row_lse[row] = lse;
-                    P.factor[row] = g;
+                    P.factor[row] = __ldg(P.d_loss + t);
                     if (fabsf(lse) > 65536.f && isfinite(lse)) set_status(P.header, VARDROP_ERR_UNSUPPORTED);
-                    if (isfinite(g)) top = fmaxf(top, fabsf(g));
                 }
             } else if (!P.lse) {
                 P.loss[t] = 0.f;
@@ -133,41 +193,16 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
             }
             if (P.lse) P.pos[t] = there ? row : -1;
         }
-        ahead += all;
+        if (!packs) continue;
         __syncthreads();
-    }
-    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-    if (lane == 0) most[warp] = top;
-    __syncthreads();
-    if (warp == 0) {
-        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most[lane])));
-        if (lane == 0) {
-            // G is stored as factor times (p - 1 or p) times a power of two that takes the largest factor to between 2^13 and 2^14: fp16 has room for it, and 38 powers of two below it
-            const int e = top > 0.f ? min(max(13 - (static_cast<int>(__float_as_uint(top) >> 23) - 127), -126), 126) : 0;
-            P.header[kLossRows] = ahead;
-            P.header[kLossFactor] = (127 + e) << 23;
-            P.header[kLossInverse] = (127 - e) << 23;
+        for (int k = warp; k < kRowsThreads && t0 + k < end; k += kRowsWarps) {
+            if (rows[k] < 0) continue;
+            const uint4* const from = P.h + static_cast<size_t>(t0 + k) * P.vectors;
+            uint4* const to = P.packed + static_cast<size_t>(rows[k]) * P.vectors;
+#pragma unroll 4
+            for (int i = lane; i < P.vectors; i += 32) to[i] = __ldg(from + i);
         }
     }
-}
-
-struct PackParams {
-    const uint4* h;
-    uint4* packed;
-    const int32_t* place;
-    const int* header;
-    int T, vectors;                                     // 16-byte vectors of a row
-};
-constexpr int kPackThreads = 256, kPackRows = 8;        // a warp a row
-__global__ void __launch_bounds__(kPackThreads) loss_pack_kernel(const PackParams P) {
-    chain_wait();
-    chain_release();
-    const int n = __ldcg(P.header + kLossRows), row = blockIdx.x * kPackRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (n == P.T || row >= (n + kChunk - 1) / kChunk * kChunk) return;          // (rows of zeros up to a whole chunk: zero times what lies there need not be zero)
-    const uint4* const from = row < n ? P.h + static_cast<size_t>(__ldcg(P.place + row)) * P.vectors : nullptr;
-    uint4* const to = P.packed + static_cast<size_t>(row) * P.vectors;
-#pragma unroll 4
-    for (int i = lane; i < P.vectors; i += 32) to[i] = from ? __ldg(from + i) : make_uint4(0u, 0u, 0u, 0u);
 }
 
 // ---- products -------------------------------------------------------------------------------------------------------------------
@@ -591,11 +626,14 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     } else {
         L.maps.g = L.maps.packed;
     }
-    RowsParams R{labels, lse, d_loss, loss, lse_out, reinterpret_cast<int32_t*>(base + p.place), reinterpret_cast<int32_t*>(base + p.pos), reinterpret_cast<int32_t*>(base + p.label),
-                 reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor), static_cast<int*>(ws), c.T, c.V};
-    { LaunchScope ls_(K_LOSS_ROWS, stream); if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st; }
-    const PackParams K{static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), R.place, R.header, c.T, c.C / 8};
-    { LaunchScope ls_(K_LOSS_PACK, stream); if (int st = check_cuda(launch_chained(loss_pack_kernel, dim3(ceil_div(c.T, kPackRows) + kChunk / kPackRows), dim3(kPackThreads), 0, stream, K), "loss: pack launch")) return st; }
+    RowsParams R{labels, lse, d_loss, loss, lse_out, static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), reinterpret_cast<int32_t*>(base + p.place),
+                 reinterpret_cast<int32_t*>(base + p.pos), reinterpret_cast<int32_t*>(base + p.label), reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor),
+                 static_cast<int*>(ws), c.T, c.V, 0, c.C / 8};
+    R.share = ceil_div(ceil_div(c.T, kRowsGrid), kLeastTokens) * kLeastTokens;
+    {
+        LaunchScope ls_(K_LOSS_ROWS, stream);
+        if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(ceil_div(c.T, R.share)), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st;
+    }
     PairParams& P = L.P;
     P = PairParams{};
     P.header = R.header;

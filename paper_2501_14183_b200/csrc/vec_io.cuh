@@ -11,10 +11,36 @@ template <class T, int N>
 struct alignas(N * sizeof(T) > 16 ? 16 : N * sizeof(T)) Pack {
     T e[N];
 };
+// (As whole words: copied as structs of elements, 16-bit ones took an access each.)
+template <int kBytes>
+struct Word;
+template <> struct Word<2> { using type = uint16_t; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
 template <class T, int N>
-__device__ __forceinline__ Pack<T, N> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, N>*>(p); }
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
+    constexpr int kBytes = N * sizeof(T) > 16 ? 16 : N * sizeof(T);
+    using W = typename Word<kBytes>::type;
+    Pack<T, N> v;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(N * sizeof(T)) / kBytes; ++i) {
+        const W w = reinterpret_cast<const W*>(p)[i];
+        memcpy(reinterpret_cast<char*>(&v) + i * kBytes, &w, kBytes);
+    }
+    return v;
+}
 template <class T, int N>
-__device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) { *reinterpret_cast<Pack<T, N>*>(p) = v; }
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) {
+    constexpr int kBytes = N * sizeof(T) > 16 ? 16 : N * sizeof(T);
+    using W = typename Word<kBytes>::type;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(N * sizeof(T)) / kBytes; ++i) {
+        W w;
+        memcpy(&w, reinterpret_cast<const char*>(&v) + i * kBytes, kBytes);
+        reinterpret_cast<W*>(p)[i] = w;
+    }
+}
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
