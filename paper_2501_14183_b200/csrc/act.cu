@@ -259,20 +259,20 @@ struct Held {
     }
 };
 
-// kTasks neighbouring pieces to a warp.
-template <class F>
-__device__ __forceinline__ void for_instances(const ActParams& P, int tasks, F body) {
+// kTasks neighbouring pieces to a warp; kTasks = 1: and on to further ones, where there are more than the grid takes at a time.
+template <int kTasks, class F>
+__device__ __forceinline__ void for_instances(const ActParams& P, F body) {
 #pragma unroll 1
     for (int b = blockIdx.y; b < P.B; b += gridDim.y) {
         const int n = P.n_sel ? min(max(__ldg(P.n_sel + (P.S > 1 ? b : 0)), 0), P.N) : P.N;
-        const uint32_t all = static_cast<uint32_t>(n) * static_cast<uint32_t>(P.chunks), step = gridDim.x * kActWarps * tasks;
+        const uint32_t all = static_cast<uint32_t>(n) * static_cast<uint32_t>(P.chunks), step = gridDim.x * kActWarps * kTasks;
 #pragma unroll 1
-        for (uint32_t t0 = (blockIdx.x * kActWarps + (threadIdx.x >> 5)) * tasks; t0 < all; t0 += step) {
+        for (uint32_t t0 = (blockIdx.x * kActWarps + (threadIdx.x >> 5)) * kTasks; t0 < all; t0 += step) {
             Task t;
             t.row = t0 / static_cast<uint32_t>(P.chunks);
             t.chunk = t0 - t.row * static_cast<uint32_t>(P.chunks);
             body(b, n, t);
-            if (all - t0 <= step) break;        // (no wrap)
+            if (kTasks > 1 || all - t0 <= step) break;      // (the second: no wrap)
         }
     }
 }
@@ -281,7 +281,7 @@ template <class T, bool kWide, int kKind, bool kGated, int kTasks>
 __global__ void __launch_bounds__(kActThreads) act_fwd_kernel(const ActParams P) {
     chain_wait();
     chain_release();
-    for_instances(P, kTasks, [&](int b, int n, Task t) {
+    for_instances<kTasks>(P, [&](int b, int n, Task t) {
         Piece<kWide> p[kTasks];
         Values<T, kWide> a[kTasks], g[kTasks];
 #pragma unroll
@@ -323,7 +323,7 @@ template <class T, bool kWide, int kKind, bool kGated, int kTasks>
 __global__ void __launch_bounds__(kActThreads) act_bwd_kernel(const ActParams P) {
     chain_wait();
     chain_release();
-    for_instances(P, kTasks, [&](int b, int n, Task t) {
+    for_instances<kTasks>(P, [&](int b, int n, Task t) {
         Piece<kWide> p[kTasks];
         Values<T, kWide> d[kTasks];
         Held<kWide> ha[kTasks], hb[kTasks];
@@ -388,8 +388,7 @@ CkptLayout ckpt_layout(const vardrop_act_cfg& c) {
     return l;
 }
 
-constexpr int kActTasks = 2, kActPerSm = 6, kMaxGridY = 65535;
-long long ceil_div_ll(long long a, long long b) { return (a + b - 1) / b; }
+constexpr int kActTasks = 2, kActPerSm = 8, kMaxGridY = 65535;      // kActPerSm: CTAs that an SM holds, and some more for instances of different sizes
 template <bool kBwd>
 int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cudaStream_t stream) {
     P.n_sel = n_sel;
@@ -399,12 +398,11 @@ int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cuda
     const bool wide = c.C % 8 == 0;             // (a stride is a multiple of 8 wherever there is one)
     P.chunks = (c.C + 32 * kPer - 1) / (32 * kPer);
     const long long tasks = static_cast<long long>(c.N) * P.chunks;
-    // several pieces to a warp only where every SM still gets four CTAs
-    const bool many = tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
+    // Every row counts, and enough of them for four CTAs on every SM: two pieces to a warp.  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their
+    // instance's pieces (a CTA for each few pieces of all rows, four of five of them without work: 172 of 862 kept rows of 32 instances, gelu of 2048, forward and backward, 52.7 us instead of 35).
+    const bool many = !n_sel && tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
     const int per = kActWarps * (many ? kActTasks : 1);
-    // Every row counts: a CTA for each few pieces.  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their instance's pieces (a CTA for each few pieces
-    // of all rows, four of five of them without work, made 172 of 862 kept rows of 32 instances 52.7 us instead of 35).
-    const long long full = (tasks + per - 1) / per, held = ceil_div_ll(static_cast<long long>(sm_count()) * kActPerSm, c.B);
+    const long long full = (tasks + per - 1) / per, held = (static_cast<long long>(sm_count()) * kActPerSm + c.B - 1) / c.B;
     const dim3 grid(static_cast<unsigned>(n_sel && held < full ? held : full), c.B < kMaxGridY ? c.B : kMaxGridY);
     LaunchScope ls_(kBwd ? K_ACT_BWD : K_ACT_FWD, stream);
     const cudaError_t err = with_dtype(c.dtype, [&](auto t) {

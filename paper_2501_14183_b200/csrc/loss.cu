@@ -6,13 +6,14 @@
 // loss_stats_kernel   products of 256 tokens x 256 rows of w; of each row of a tile the maximum and the sum of exponentials go to memory, and the label's logit.
 // loss_join_kernel    lse and loss from these.
 // loss_grad_kernel    backward, for a piece of the vocabulary at a time: the same products again, G of the piece to memory in 16 bits.
-// loss_dh_kernel      d_h += G w[piece] in fp32;      loss_dw_kernel   d_w[piece] = G^T h.
-// loss_rest_kernel, loss_sum_kernel   d_h, rounded, to the tokens' places (zeros without a label); parts of d_w, where its products were split along the tokens.
+// loss_back_kernel    d_h += G w[piece] in fp32 and d_w[piece] = G^T h, the tiles of both in one launch.
+// loss_rest_kernel    d_h, rounded, to the tokens' places (zeros without a label); parts of d_w, where its products were split along the tokens.
 //
 // Bound: the tensor cores, 2 T V C flop forward and 6 T V C backward (2 of them the logits again: to keep them would take 2 T V bytes), and for few tokens reading w.
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "loss_tiles.h"
 #include "pair_mma.cuh"
 #include "vec_io.cuh"
 
@@ -20,20 +21,19 @@ namespace vardrop {
 
 namespace {
 
-constexpr int kPairTile = 256, kHalfTile = 128;      // rows and columns of a tile; a CTA's rows
-constexpr int kChunk = 64;                           // of the contracted axis in a stage: 128 bytes
+constexpr int kHalfTile = 128;                       // a CTA's rows of a tile
 constexpr int kBoxBytes = 64 * 64 * 2;               // what a copy brings
 constexpr int kStageBytes = 4 * kBoxBytes;           // two boxes of either operand
 constexpr int kStages = 6;
 constexpr int kPairThreads = 384;
 constexpr int kPairSmemBytes = 1024 + 1024 + kStages * kStageBytes;
 constexpr uint32_t kPairTmemCols = 512;              // two accumulators of 256 columns
-constexpr int kGroupRows = 8;                        // row tiles that neighbouring pairs share out among each other
 constexpr size_t kPieceBytes = 256u << 20;           // of G; larger pieces make fewer passes over d_h
-constexpr int kLeastPiece = 1024, kMostSplits = 16, kSplitChunks = 4;
+constexpr int kLeastPiece = 1024;
+constexpr size_t kPartBytes = 64u << 20;             // of parts of a gradient's products
 constexpr float kLog2e = 1.4426950408889634f;
 
-enum LossWord { kLossRows = 16, kLossFactor, kLossInverse };      // words of the workspace's header: labelled tokens; what G is scaled by, and its inverse
+enum LossWord { kLossRows = 16, kLossInverse };      // words of the workspace's header: labelled tokens; the inverse of what G is scaled by
 
 int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
 
@@ -41,37 +41,36 @@ int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b
 struct LossPlan {
     int rows;                   // T up to whole tiles
     int piece, pieces;          // columns of G
-    int dh_splits, dw_splits;
-    size_t place, pos, label, lse, factor, target, packed, part, g, dh, dw, total;
+    int dh_rows, dw_parts;      // rows that all parts of d_h's products may take; parts of d_w's
+    int share, shares;          // tokens of a CTA that finds labels
+    size_t place, pos, label, lse, factor, target, most, packed, part, g, dh, dw, total;
 };
+constexpr int kLeastTokens = 16, kRowsGrid = 296;
 LossPlan loss_plan(const vardrop_loss_cfg& c) {
     LossPlan p{};
     p.rows = ceil_div(c.T, kPairTile) * kPairTile;
-    const long long all = static_cast<long long>(ceil_div(c.V, kPairTile)) * kPairTile;
-    const long long fit = static_cast<long long>(kPieceBytes / (2ull * p.rows)) / kPairTile * kPairTile;
-    p.piece = static_cast<int>(all < (fit > kLeastPiece ? fit : kLeastPiece) ? all : (fit > kLeastPiece ? fit : kLeastPiece));
+    p.share = ceil_div(ceil_div(c.T, kRowsGrid), kLeastTokens) * kLeastTokens;
+    p.shares = ceil_div(c.T, p.share);
+    const long long fit = static_cast<long long>(kPieceBytes / (2ull * p.rows)) / kPairTile * kPairTile, most = fit > kLeastPiece ? fit : kLeastPiece;
+    p.pieces = ceil_div(c.V, most);
+    p.piece = ceil_div(ceil_div(c.V, p.pieces), kPairTile) * kPairTile;
     p.pieces = ceil_div(c.V, p.piece);
-    const int pairs = sm_count() / 2, tn = ceil_div(c.C, kPairTile);
-    // too few tiles for the SMs: parts of the contracted axis, added up in a fixed order afterwards
-    const auto splits = [&](long long tiles, long long chunks) {
-        long long s = tiles < pairs ? pairs / tiles : 1;
-        if (s > chunks / kSplitChunks) s = chunks / kSplitChunks;
-        return static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
-    };
-    p.dh_splits = splits(static_cast<long long>(p.rows / kPairTile) * tn, p.piece / kChunk);
-    p.dw_splits = splits(static_cast<long long>(p.piece / kPairTile) * tn, ceil_div(c.T, kChunk));
+    const long long row_bytes = 4ll * c.C, dh = static_cast<long long>(kPartBytes) / row_bytes, dw = static_cast<long long>(kPartBytes) / (row_bytes * p.piece);
+    p.dh_rows = static_cast<int>(dh < p.rows ? p.rows : dh < static_cast<long long>(kMostSplits) * p.rows ? dh : static_cast<long long>(kMostSplits) * p.rows);
+    p.dw_parts = p.pieces > 1 || dw < 2 ? 1 : static_cast<int>(dw < kMostSplits ? dw : kMostSplits);
     size_t o = align_up(kWsHeaderBytes, 1024);
     const auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 1024); return at; };
     const size_t T = c.T, C = c.C, rows = p.rows;
     p.place = take(4 * T); p.pos = take(4 * T); p.label = take(4 * T); p.lse = take(4 * T); p.factor = take(4 * T); p.target = take(4 * T);
+    p.most = take(4ull * p.shares);
     p.packed = take(2 * rows * C);
     const size_t shared = o;                            // forward and backward each have their own from here on
     p.part = take(8 * rows * 2 * ceil_div(c.V, kPairTile));
     const size_t forward = o;
     o = shared;
     p.g = take(2 * rows * p.piece);
-    p.dh = take(4 * rows * C * p.dh_splits);
-    p.dw = p.dw_splits > 1 ? take(4ull * p.piece * C * p.dw_splits) : o;
+    p.dh = take(4ull * p.dh_rows * C);
+    p.dw = take(p.dw_parts > 1 ? 4ull * p.piece * C * p.dw_parts : 0);
     p.total = o > forward ? o : forward;
     return p;
 }
@@ -84,11 +83,11 @@ struct RowsParams {
     const uint4* h;
     uint4* packed;
     int32_t *place, *pos, *label;                       // token of a row; row of a token, or -1; label of a row
-    float *row_lse, *factor;
+    float *row_lse, *factor, *most;                     // most: the largest factor of a share's tokens
     int* header;
     int T, V, share, vectors;                           // tokens of a CTA; 16-byte vectors of a row
 };
-constexpr int kRowsThreads = 256, kRowsWarps = kRowsThreads / 32, kLeastTokens = 64, kRowsGrid = 296;
+constexpr int kRowsThreads = 256, kRowsWarps = kRowsThreads / 32;
 __device__ __forceinline__ float block_max(float v, float* shared) {
     v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
@@ -136,25 +135,8 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
         ahead += sums[1][w];
     }
     const int n = all;
-    if (blockIdx.x == 0) {
-        float top = 0.f;
-        if (P.lse) {
-#pragma unroll 4
-            for (int t = tid; t < P.T; t += kRowsThreads) {
-                const float g = fabsf(__ldg(P.d_loss + t));
-                if (live(__ldg(P.labels + t)) && isfinite(g)) top = fmaxf(top, g);
-            }
-            top = block_max(top, most);
-        }
-        if (tid == 0) {
-            // G is stored times what takes the largest factor to 16320 = 255 2^6: fp16 has room for it and for 2^-38 of it, and where all factors are alike, as in a mean, the largest entries,
-            // factor (p - 1) at the labels, lose no bits but those of p (a power of two instead left d_w off by 2.5e-3 of its norm where rounding it alone leaves 1.6e-3)
-            const float up = top > 0.f ? fminf(16320.f / top, 8.5e37f) : 1.f;
-            P.header[kLossRows] = n;
-            P.header[kLossFactor] = __float_as_int(up);
-            P.header[kLossInverse] = __float_as_int(1.f / up);
-        }
-    }
+    if (blockIdx.x == 0 && tid == 0) P.header[kLossRows] = n;
+    float top = 0.f;                                    // of the factors here
     const bool packs = n != P.T;
     if (packs && blockIdx.x == gridDim.x - 1) {         // rows of zeros up to a whole chunk: zero times what lies there need not be zero
         const int fill = (n + kChunk - 1) / kChunk * kChunk;
@@ -184,7 +166,9 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
                 if (P.lse) {
                     const float lse = __ldg(P.lse + t);
                     P.row_lse[row] = lse;
-                    P.factor[row] = __ldg(P.d_loss + t);
+                    const float g = __ldg(P.d_loss + t);
+                    P.factor[row] = g;
+                    if (isfinite(g)) top = fmaxf(top, fabsf(g));
                     if (fabsf(lse) > 65536.f && isfinite(lse)) set_status(P.header, VARDROP_ERR_UNSUPPORTED);
                 }
             } else if (!P.lse) {
@@ -203,10 +187,21 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
             for (int i = lane; i < P.vectors; i += 32) to[i] = __ldg(from + i);
         }
     }
+    if (!P.lse) return;
+    top = block_max(top, most);
+    if (tid == 0) P.most[blockIdx.x] = top;
+}
+// G is stored times what takes the largest factor to 16320 = 255 2^6: fp16 has room for it and for 2^-38 of it, and where all factors are alike, as in a mean, the largest entries, factor (p - 1) at the labels,
+// lose no bits but those of p (a power of two instead left d_w off by 2.5e-3 of its norm where rounding it alone leaves 1.6e-3).  A warp asks.
+__device__ __forceinline__ float scale_up(const float* most, int shares) {
+    float top = 0.f;
+    for (int i = threadIdx.x & 31; i < shares; i += 32) top = fmaxf(top, __ldcg(most + i));
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+    return top > 0.f ? fminf(16320.f / top, 8.5e37f) : 1.f;
 }
 
 // ---- products -------------------------------------------------------------------------------------------------------------------
-enum LossMode { kStats, kGrad, kDh, kDw };
+enum LossMode { kStats, kGrad, kBack };
 struct LossMaps {
     CUtensorMap h, packed, w, g;
 };
@@ -215,21 +210,18 @@ struct PairParams {
     int T, V, C;
     int v0, v1;                                         // the piece
     int pitch;                                          // columns of G
-    int splits, add, fp16;
+    int add, fp16, shares;
     float scale;
     const int32_t* label;
-    const float *row_lse, *factor;
+    const float *row_lse, *factor, *most;
     float2* part;                                       // [half tiles of the vocabulary, rows]
     float* target;
     void* g;
-    float* acc;                                         // [splits, rows, C]
-    void* out;
-    int rows;                                           // of `part` and, times the splits, of `acc`
+    float *dh, *dw;                                     // [parts, rows of tiles, C], [parts, columns of G, C]
+    void* out;                                          // d_w
+    int rows;                                           // of `part`
+    SplitParams split;
 };
-struct PairTile {
-    int m, n, k0, k1, split;
-};
-
 template <class T>
 __device__ __forceinline__ uint32_t pack16(float a, float b) {
     if constexpr (std::is_same<T, __half>::value) {
@@ -247,8 +239,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // What a thread does with 128 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
-template <int kMode, class T>
-__device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x, uint32_t tm, int row, int col, int n) {
+template <int kMode, class T, class Tiles>
+__device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x, uint32_t tm, int row, int col, int n, float up, const Tiles& tiles) {
     if constexpr (kMode == kStats) {
         const int left = P.V - col;
         if (left <= 0) return;
@@ -286,7 +278,7 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
     } else if constexpr (kMode == kGrad) {
         const bool there = row < n;
         const int left = P.V - P.v0 - col, label = there ? __ldg(P.label + row) - P.v0 - col : -1;
-        const float lse = there ? __ldg(P.row_lse + row) : 0.f, factor = there ? __ldg(P.factor + row) * __int_as_float(__ldcg(P.header + kLossFactor)) : 0.f;
+        const float lse = there ? __ldg(P.row_lse + row) : 0.f, factor = there ? __ldg(P.factor + row) * up : 0.f;
         uint4* const to = reinterpret_cast<uint4*>(static_cast<T*>(P.g) + static_cast<size_t>(row) * P.pitch + col);
 #pragma unroll 1
         for (int c = 0; c < kHalfTile; c += 32) {
@@ -309,10 +301,10 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
                 to[c / 8 + q] = make_uint4(pack16<T>(r[8 * q], r[8 * q + 1]), pack16<T>(r[8 * q + 2], r[8 * q + 3]), pack16<T>(r[8 * q + 4], r[8 * q + 5]), pack16<T>(r[8 * q + 6], r[8 * q + 7]));
         }
     } else {
-        const bool some = x.k1 > x.k0, there = row < (kMode == kDh ? n : P.v1 - P.v0);
-        const bool direct = kMode == kDw && P.splits == 1;
-        const float mul = P.scale * __int_as_float(__ldcg(P.header + kLossInverse));
-        float* const acc = P.acc + (static_cast<size_t>(x.split) * P.rows + row) * P.C + col;
+        const bool some = x.k1 > x.k0, there = row < (x.dw ? P.v1 - P.v0 : n), direct = x.dw && tiles.splits.dw == 1, add = !x.dw && P.add;
+        const float mul = up;
+        const size_t rows = x.dw ? P.split.piece : (n + kPairTile - 1) / kPairTile * kPairTile;
+        float* const acc = (x.dw ? P.dw : P.dh) + (x.part * rows + row) * P.C + col;
         T* const out = static_cast<T*>(P.out) + (static_cast<size_t>(P.v0) + row) * P.C + col;
 #pragma unroll 1
         for (int c = 0; c < kHalfTile && col + c < P.C; c += 32) {
@@ -334,7 +326,7 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
                 } else {
                     float4* const at = reinterpret_cast<float4*>(acc + c + 8 * q);
                     float4 lo = make_float4(v[0], v[1], v[2], v[3]), hi = make_float4(v[4], v[5], v[6], v[7]);
-                    if (P.add) {
+                    if (add) {
                         const float4 a = at[0], b = at[1];
                         lo.x += a.x; lo.y += a.y; lo.z += a.z; lo.w += a.w;
                         hi.x += b.x; hi.y += b.y; hi.z += b.z; hi.w += b.w;
@@ -382,38 +374,28 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
     chain_release();
 
     const int n = __ldcg(P.header + kLossRows), columns = P.v1 - P.v0;
-    // rows, columns and contracted axis of the product
-    const int M = kMode == kDw ? columns : n, N = kMode == kStats || kMode == kGrad ? columns : P.C, K = kMode == kDh ? columns : kMode == kDw ? n : P.C;
-    const int tm = (M + kPairTile - 1) / kPairTile, tn = (N + kPairTile - 1) / kPairTile, chunks = (K + kChunk - 1) / kChunk;
-    const long long each = static_cast<long long>(tm) * tn, total = each * P.splits;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    // Neighbouring pairs take tiles of eight rows of tiles, so that what they read at a time is some eight tiles of A and nine of B.
-    const auto tile_at = [&](long long t) {
-        PairTile x;
-        x.split = static_cast<int>(t / each);
-        const int in = static_cast<int>(t - x.split * each), width = kGroupRows * tn, group = in / width, r = in - group * width;
-        const int high = min(kGroupRows, tm - group * kGroupRows);
-        x.n = r / high;
-        x.m = group * kGroupRows + (r - x.n * high);
-        x.k0 = static_cast<int>(static_cast<long long>(chunks) * x.split / P.splits);
-        x.k1 = static_cast<int>(static_cast<long long>(chunks) * (x.split + 1) / P.splits);
-        return x;
-    };
-    constexpr bool a_mn = kMode == kDw, b_mn = kMode == kDh || kMode == kDw;     // the contracted axis is the rows of the tensor
+    const auto tiles = [&] {
+        if constexpr (kMode == kBack) return GradTiles(P.split, n, columns, pair, pairs);
+        else return LogitTiles{tiles_of(n, kPairTile), tiles_of(columns, kPairTile), tiles_of(P.C, kChunk), pair, pairs};
+    }();
+    // Whether the contracted axis is the rows of the tensor: of G for d_w, of w and h for either gradient.
+    constexpr bool b_mn = kMode == kBack;
+    PairTile x;
     bool ok = true;
     if (warp == 0) {
         if (lane == 0) {
             const CUtensorMap* const map_h = n == P.T ? &maps.h : &maps.packed;
-            const CUtensorMap* const map_a = kMode == kStats || kMode == kGrad ? map_h : &maps.g;
-            const CUtensorMap* const map_b = kMode == kDw ? map_h : &maps.w;
-            tma_prefetch_desc(map_a);
-            tma_prefetch_desc(map_b);
-            const int row_b = kMode == kDw ? 0 : P.v0;                           // rows of w begin with the piece
+            tma_prefetch_desc(map_h);
+            tma_prefetch_desc(&maps.w);
+            if (kMode == kBack) tma_prefetch_desc(&maps.g);
             uint32_t it = 0;
 #pragma unroll 1
-            for (long long t = pair; t < total && ok; t += pairs) {
-                const PairTile x = tile_at(t);
+            for (int i = 0; ok && tiles.at(i, x); ++i) {
                 const int a0 = x.m * kPairTile + static_cast<int>(rank) * kHalfTile, b0 = x.n * kPairTile + static_cast<int>(rank) * kHalfTile;
+                const CUtensorMap* const map_a = kMode == kBack ? &maps.g : map_h;
+                const CUtensorMap* const map_b = x.dw ? map_h : &maps.w;
+                const int row_b = x.dw ? 0 : P.v0;                               // rows of w begin with the piece
 #pragma unroll 1
                 for (int kc = x.k0; kc < x.k1; ++kc, ++it) {
                     const uint32_t st = it % kStages;
@@ -422,20 +404,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
                     const uint32_t full = leaders(bar_full + st), to = smem_u32(stages) + st * kStageBytes;
                     if (rank == 0) mbar_expect_tx(bar_full + st, 2 * kStageBytes);
                     const int k = kc * kChunk;
-                    if (a_mn) {
-                        pair_load_2d(to, map_a, full, a0, k);
-                        pair_load_2d(to + kBoxBytes, map_a, full, a0 + 64, k);
-                    } else {
-                        pair_load_2d(to, map_a, full, k, a0);
-                        pair_load_2d(to + kBoxBytes, map_a, full, k, a0 + 64);
-                    }
-                    if (b_mn) {
-                        pair_load_2d(to + 2 * kBoxBytes, map_b, full, b0, row_b + k);
-                        pair_load_2d(to + 3 * kBoxBytes, map_b, full, b0 + 64, row_b + k);
-                    } else {
-                        pair_load_2d(to + 2 * kBoxBytes, map_b, full, k, row_b + b0);
-                        pair_load_2d(to + 3 * kBoxBytes, map_b, full, k, row_b + b0 + 64);
-                    }
+                    pair_load_2d(to, map_a, full, x.dw ? a0 : k, x.dw ? k : a0);
+                    pair_load_2d(to + kBoxBytes, map_a, full, x.dw ? a0 + 64 : k, x.dw ? k : a0 + 64);
+                    pair_load_2d(to + 2 * kBoxBytes, map_b, full, b_mn ? b0 : k, row_b + (b_mn ? k : b0));
+                    pair_load_2d(to + 3 * kBoxBytes, map_b, full, b_mn ? b0 + 64 : k, row_b + (b_mn ? k : b0 + 64));
                 }
             }
             // what the leader still sends to this CTA's barriers comes before it leaves
@@ -444,14 +416,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
         }
         __syncwarp();
     } else if (warp == 1 && rank == 0) {
-        const uint32_t idesc = pair_idesc(P.fp16 != 0, a_mn, b_mn);
         // rows of 128 bytes: eight of them 1024 apart, panels of 64 rows or columns a box
-        const uint64_t a_desc = umma_desc_sw128(smem_u32(stages), a_mn ? kBoxBytes : 16, 1024), b_desc = umma_desc_sw128(smem_u32(stages) + 2 * kBoxBytes, b_mn ? kBoxBytes : 16, 1024);
-        constexpr uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;      // 16 of the contracted axis
-        uint32_t it = 0, i = 0;
+        const uint64_t a_rows = umma_desc_sw128(smem_u32(stages), 16, 1024), a_cols = umma_desc_sw128(smem_u32(stages), kBoxBytes, 1024);
+        const uint64_t b_desc = umma_desc_sw128(smem_u32(stages) + 2 * kBoxBytes, b_mn ? kBoxBytes : 16, 1024);
+        constexpr uint32_t b_step = b_mn ? 2048 : 32;                            // 16 of the contracted axis
+        uint32_t it = 0;
 #pragma unroll 1
-        for (long long t = pair; t < total && ok; t += pairs, ++i) {
-            const PairTile x = tile_at(t);
+        for (int i = 0; ok && tiles.at(i, x); ++i) {
+            const uint32_t idesc = pair_idesc(P.fp16 != 0, x.dw, b_mn), a_step = x.dw ? 2048 : 32;
+            const uint64_t a_desc = x.dw ? a_cols : a_rows;
             const uint32_t d = tmem + (i & 1) * kPairTile;
             ok = __all_sync(0xffffffffu, mbar_wait(bar_taken + (i & 1), ((i >> 1) & 1) ^ 1));
             if (!ok) break;
@@ -476,14 +449,20 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
     } else if (warp >= 4) {
         const int in_tile = static_cast<int>(rank) * kHalfTile + (warp & 3) * 32 + lane, half = (warp - 4) >> 2;
         const uint32_t tm_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * kHalfTile;
-        uint32_t i = 0;
+        // kGrad: what G is scaled by; kBack: what takes that away from its products
+        float up = 1.f;
+        if (kMode == kGrad) {
+            up = scale_up(P.most, P.shares);
+            if (blockIdx.x == 0 && warp == 4 && lane == 0) P.header[kLossInverse] = __float_as_int(1.f / up);
+        } else if (kMode == kBack) {
+            up = P.scale * __int_as_float(__ldcg(P.header + kLossInverse));
+        }
 #pragma unroll 1
-        for (long long t = pair; t < total; t += pairs, ++i) {
-            const PairTile x = tile_at(t);
+        for (int i = 0; tiles.at(i, x); ++i) {
             ok = __all_sync(0xffffffffu, mbar_wait(bar_acc + (i & 1), (i >> 1) & 1));
             if (!ok) break;
             tc_fence_after();
-            take_out<kMode, T>(P, x, tm_at + (i & 1) * kPairTile, x.m * kPairTile + in_tile, x.n * kPairTile + half * kHalfTile, n);
+            take_out<kMode, T>(P, x, tm_at + (i & 1) * kPairTile, x.m * kPairTile + in_tile, x.n * kPairTile + half * kHalfTile, n, up, tiles);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) leader_arrive(leaders(bar_taken + (i & 1)));
@@ -537,13 +516,14 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) loss_join_kernel(const
 
 // ---- gradients' last step -------------------------------------------------------------------------------------------------------
 struct RestParams {
-    const float* acc;
-    const int32_t* pos;                                 // row of a token; NULL: its own
+    const float *dh, *dw;
+    const int32_t* pos;                                 // row of a token, or -1
     const int* header;
-    void* out;
-    size_t part;                                        // elements from one part to the next
-    int count, C, splits;
+    void *d_h, *d_w;                                    // d_w NULL: written as it is
+    int T, V, C;
+    int h_blocks;                                       // CTAs of d_h
     float scale;
+    SplitParams split;
 };
 constexpr int kRestThreads = 256;
 // Eight columns a thread.
@@ -551,17 +531,22 @@ template <class T>
 __global__ void __launch_bounds__(kRestThreads) loss_rest_kernel(const RestParams P) {
     chain_wait();
     chain_release();
-    const int vectors = P.C / 8;
-    const long long at = static_cast<long long>(blockIdx.x) * kRestThreads + threadIdx.x, t = at / vectors;
-    if (t >= P.count) return;
-    const int c = static_cast<int>(at - t * vectors) * 8;
-    const long long row = P.pos ? __ldcg(P.pos + t) : t;
-    const float mul = P.scale * __int_as_float(__ldcg(P.header + kLossInverse));
+    const bool dw = static_cast<int>(blockIdx.x) >= P.h_blocks;
+    const int n = __ldcg(P.header + kLossRows), vectors = P.C / 8, count = dw ? P.V : P.T;
+    const Splits splits = splits_of(P.split, n);
+    if (dw && splits.dw == 1) return;                   // written as it is
+    const long long at = (static_cast<long long>(blockIdx.x) - (dw ? P.h_blocks : 0)) * kRestThreads + threadIdx.x, t = at / vectors;
+    if (t >= count) return;
+    const int c = static_cast<int>(at - t * vectors) * 8, parts = dw ? splits.dw : splits.dh;
+    const long long row = dw ? t : __ldcg(P.pos + t);
+    const size_t part = static_cast<size_t>(dw ? P.split.piece : (n + kPairTile - 1) / kPairTile * kPairTile) * P.C;
+    const float mul = row >= 0 ? P.scale * __int_as_float(__ldcg(P.header + kLossInverse)) : 0.f;
+    const float* from = (dw ? P.dw : P.dh) + row * P.C + c;
     float v[8] = {};
     if (row >= 0) {
-#pragma unroll 2
-        for (int s = 0; s < P.splits; ++s) {
-            const Pack<float, 8> a = load_pack<float, 8>(P.acc + s * P.part + row * P.C + c);
+#pragma unroll 4
+        for (int s = 0; s < parts; ++s, from += part) {
+            const Pack<float, 8> a = load_pack<float, 8>(from);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += a.e[e];
         }
@@ -569,7 +554,7 @@ __global__ void __launch_bounds__(kRestThreads) loss_rest_kernel(const RestParam
     Pack<T, 8> o;
 #pragma unroll
     for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(row >= 0 ? v[e] * mul : 0.f);
-    store_pack(static_cast<T*>(P.out) + t * P.C + c, o);
+    store_pack(static_cast<T*>(dw ? P.d_w : P.d_h) + t * P.C + c, o);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -628,59 +613,43 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     }
     RowsParams R{labels, lse, d_loss, loss, lse_out, static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), reinterpret_cast<int32_t*>(base + p.place),
                  reinterpret_cast<int32_t*>(base + p.pos), reinterpret_cast<int32_t*>(base + p.label), reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor),
-                 static_cast<int*>(ws), c.T, c.V, 0, c.C / 8};
-    R.share = ceil_div(ceil_div(c.T, kRowsGrid), kLeastTokens) * kLeastTokens;
+                 reinterpret_cast<float*>(base + p.most), static_cast<int*>(ws), c.T, c.V, p.share, c.C / 8};
     {
         LaunchScope ls_(K_LOSS_ROWS, stream);
-        if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(ceil_div(c.T, R.share)), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st;
+        if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(p.shares), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st;
     }
     PairParams& P = L.P;
     P = PairParams{};
     P.header = R.header;
-    P.T = c.T; P.V = c.V; P.C = c.C; P.v0 = 0; P.v1 = c.V; P.pitch = p.piece; P.splits = 1; P.fp16 = fp16; P.scale = c.scale == 0.f ? 1.f : c.scale;
-    P.label = R.label; P.row_lse = R.row_lse; P.factor = R.factor;
+    P.T = c.T; P.V = c.V; P.C = c.C; P.v0 = 0; P.v1 = c.V; P.pitch = p.piece; P.shares = p.shares; P.fp16 = fp16; P.scale = c.scale == 0.f ? 1.f : c.scale;
+    P.label = R.label; P.row_lse = R.row_lse; P.factor = R.factor; P.most = R.most;
     P.part = reinterpret_cast<float2*>(base + p.part); P.target = reinterpret_cast<float*>(base + p.target);
-    P.g = base + p.g; P.rows = p.rows;
+    P.g = base + p.g; P.dh = reinterpret_cast<float*>(base + p.dh); P.dw = reinterpret_cast<float*>(base + p.dw); P.rows = p.rows;
     return VARDROP_OK;
 }
 
 template <class T>
 int loss_backward(LossCall& L, const vardrop_loss_cfg& c, void* d_h, void* d_w, cudaStream_t stream) {
     const LossPlan& p = L.plan;
-    const long long tm = p.rows / kPairTile, tn = ceil_div(c.C, kPairTile);
-    const int* const header = L.P.header;
-    const auto rest = [&](int id, const float* acc, const int32_t* pos, void* out, size_t part, int count, int splits) {
-        const RestParams R{acc, pos, header, out, part, count, c.C, splits, L.P.scale};
-        LaunchScope ls_(id, stream);
-        const long long blocks = (static_cast<long long>(count) * (c.C / 8) + kRestThreads - 1) / kRestThreads;
-        return check_cuda(launch_chained(loss_rest_kernel<T>, dim3(static_cast<unsigned>(blocks)), dim3(kRestThreads), 0, stream, R), "loss: rest launch");
-    };
+    const long long tm = p.rows / kPairTile, tc = ceil_div(c.C, kPairTile);
+    PairParams& P = L.P;
+    P.split = SplitParams{sm_count() / 2, static_cast<int>(tc), p.piece, p.dh_rows, p.dw_parts, d_h != nullptr, d_w != nullptr};
+    P.out = d_w;
     for (int i = 0; i < p.pieces; ++i) {
-        PairParams P = L.P;
         P.v0 = i * p.piece;
         P.v1 = c.V - P.v0 < p.piece ? c.V : P.v0 + p.piece;
-        const int columns = P.v1 - P.v0, tv = ceil_div(columns, kPairTile);
+        P.add = i > 0;
+        const int tv = ceil_div(P.v1 - P.v0, kPairTile);
         if (int st = launch_products<kGrad, T>(K_LOSS_GRAD, tm * tv, L.maps, P, stream)) return st;
-        if (d_h) {
-            P.splits = p.dh_splits;
-            P.add = i > 0;
-            P.acc = reinterpret_cast<float*>(L.base + p.dh);
-            if (int st = launch_products<kDh, T>(K_LOSS_DH, tm * tn * P.splits, L.maps, P, stream)) return st;
-        }
-        if (d_w) {
-            P.splits = p.dw_splits;
-            P.add = 0;
-            P.acc = reinterpret_cast<float*>(L.base + p.dw);
-            P.rows = p.piece;
-            P.out = d_w;
-            if (int st = launch_products<kDw, T>(K_LOSS_DW, static_cast<long long>(tv) * tn * P.splits, L.maps, P, stream)) return st;
-            if (P.splits > 1) {
-                if (int st = rest(K_LOSS_SUM, P.acc, nullptr, static_cast<T*>(d_w) + static_cast<size_t>(P.v0) * c.C, static_cast<size_t>(p.piece) * c.C, columns, P.splits)) return st;
-            }
-        }
+        // (how many parts there are is known on the device)
+        if (int st = launch_products<kBack, T>(K_LOSS_BACK, (d_h ? tm * tc * kMostSplits : 0) + (d_w ? tv * tc * p.dw_parts : 0), L.maps, P, stream)) return st;
     }
-    if (!d_h) return VARDROP_OK;
-    return rest(K_LOSS_REST, reinterpret_cast<float*>(L.base + p.dh), reinterpret_cast<const int32_t*>(L.base + p.pos), d_h, static_cast<size_t>(p.rows) * c.C, c.T, p.dh_splits);
+    const bool parts = d_w && p.dw_parts > 1;
+    if (!d_h && !parts) return VARDROP_OK;
+    const auto blocks = [&](long long count) { return static_cast<int>((count * (c.C / 8) + kRestThreads - 1) / kRestThreads); };
+    const RestParams R{P.dh, P.dw, reinterpret_cast<const int32_t*>(L.base + p.pos), P.header, d_h, d_w, c.T, c.V, c.C, d_h ? blocks(c.T) : 0, P.scale, P.split};
+    LaunchScope ls_(K_LOSS_REST, stream);
+    return check_cuda(launch_chained(loss_rest_kernel<T>, dim3(R.h_blocks + (parts ? blocks(c.V) : 0)), dim3(kRestThreads), 0, stream, R), "loss: rest launch");
 }
 
 }  // namespace
