@@ -3,8 +3,10 @@
 // embed_fwd_kernel      rows of the table, several tokens to a thread so that their loads overlap.  Bound: memory.
 // embed_count_kernel, embed_sort_kernel   tokens sorted by index, equal ones in their own order: a radix sort of (index, token) by digits of up to nine bits, so that 512 rows take one pass and 2^18
 //                       two.  Indices that name no row are sorted behind the last one.  embed_sort_small_kernel: all passes in shared memory.
-// embed_sum_kernel      even shares of the sorted tokens: whoever meets all tokens of a row writes it, pieces of a row go to the workspace.  Rows without a token are written as zeros beside it.
+//                       Beside the sorting, whose CTAs are few and whose steps are a chain of latencies, other CTAs of the same launches write zeros to the whole table.
+// embed_sum_kernel      even shares of the sorted tokens: whoever meets all tokens of a row writes it, pieces of a row go to the workspace.
 // embed_join_kernel     adds up the pieces, in order.
+// embed_scan_kernel     few tokens and rows: a CTA a row looks through all indices for itself, one launch instead of four.
 //
 // The order of every sum is that of the tokens and does not depend on which CTA runs when: results are bit-reproducible.  Bound: memory, and for few tokens the chain of launches.
 #include <algorithm>
@@ -130,7 +132,19 @@ struct SortParams {
     int32_t *keys_out, *tokens_out, *counts;    // counts [passes, blocks, bins]
     int* status;
     int T, V, bits, pass, passes, blocks, tiles_per_block;
+    uint4* zeros;                               // of the table, in 16-byte words: this launch's share, by the CTAs from `workers` on
+    size_t zero_words;
+    int workers;
+    unsigned char* tail;                        // its last bytes, where they are no whole word
+    int tail_bytes;
 };
+// The CTA's part of the launch's zeros.
+__device__ __forceinline__ void write_zeros(const SortParams& P) {
+    if (static_cast<int>(blockIdx.x) == P.workers && static_cast<int>(threadIdx.x) < P.tail_bytes) P.tail[threadIdx.x] = 0;
+    const size_t step = static_cast<size_t>(gridDim.x - P.workers) * blockDim.x;
+#pragma unroll 4
+    for (size_t i = static_cast<size_t>(blockIdx.x - P.workers) * blockDim.x + threadIdx.x; i < P.zero_words; i += step) P.zeros[i] = make_uint4(0u, 0u, 0u, 0u);
+}
 // The key of token t: its index, V where it names no row.
 __device__ __forceinline__ int key_of(const SortParams& P, int t) {
     const int v = __ldg(P.idx + t);
@@ -144,6 +158,10 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortPar
     for (int d = threadIdx.x; d < bins; d += kSortThreads) hist[d] = 0;
     chain_wait();
     chain_release();
+    if (static_cast<int>(blockIdx.x) >= P.workers) {
+        write_zeros(P);
+        return;
+    }
     __syncthreads();
     const long long begin = static_cast<long long>(blockIdx.x) * P.tiles_per_block * kSortTile, end = min(static_cast<long long>(P.T), begin + static_cast<long long>(P.tiles_per_block) * kSortTile);
     for (long long t = begin + threadIdx.x; t < end; t += kSortThreads) atomicAdd(hist + (key_of(P, static_cast<int>(t)) & (bins - 1)), 1);
@@ -232,6 +250,10 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortPara
     __shared__ SortShared<kSortThreads> S;
     chain_wait();
     chain_release();
+    if (static_cast<int>(blockIdx.x) >= P.workers) {
+        write_zeros(P);
+        return;
+    }
     const int bins = 1 << P.bits, shift = P.pass * P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int32_t* const counts = P.counts + static_cast<size_t>(P.pass) * P.blocks * kMaxBins;
     // the digit's tokens in all CTAs and in those ahead of this one
@@ -291,6 +313,10 @@ __global__ void __launch_bounds__(kOneThreads) embed_sort_small_kernel(const Sor
     int* const tokens = keys + kOneTile;
     chain_wait();
     chain_release();
+    if (static_cast<int>(blockIdx.x) >= P.workers) {
+        write_zeros(P);
+        return;
+    }
     const int bins = 1 << P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int t0 = warp * (32 * kSortItems) + lane;
     int key[kSortItems], token[kSortItems], digit[kSortItems], place[kSortItems];
@@ -335,49 +361,31 @@ struct SumParams {
     const int32_t *keys, *tokens;
     void* d_table;
     float* pieces;                              // [shares, 2, C]: of the row that a share begins in, of the one that it ends in
-    int T, V, C, lanes, share, shares, share_blocks, accumulate;
+    int T, V, C, lanes, share, shares, accumulate;
     float scale;
 };
+// `old`: what is there, where that is added to
 template <class Tab, int kVec>
-__device__ __forceinline__ void finish_row(const SumParams& P, int v, int c, const float (&sum)[kVec]) {
-    Tab* const at = static_cast<Tab*>(P.d_table) + static_cast<size_t>(v) * P.C + c;
-    Pack<Tab, kVec> old, to;
-    if (P.accumulate) old = load_pack<Tab, kVec>(at);
+__device__ __forceinline__ void finish_row(const SumParams& P, int v, int c, const float (&sum)[kVec], const Pack<Tab, kVec>& old) {
+    Pack<Tab, kVec> to;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) to.e[e] = from_float<Tab>(P.accumulate ? fmaf(sum[e], P.scale, to_float(old.e[e])) : sum[e] * P.scale);
-    store_pack(at, to);
+    store_pack(static_cast<Tab*>(P.d_table) + static_cast<size_t>(v) * P.C + c, to);
 }
-// Whether any of the sorted keys is v.
-__device__ __forceinline__ bool has_key(const int32_t* keys, int n, int v) {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (__ldcg(keys + mid) < v) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo < n && __ldcg(keys + lo) == v;
+template <class Tab, int kVec>
+__device__ __forceinline__ Pack<Tab, kVec> row_there(const SumParams& P, int v, int c) { return load_pack<Tab, kVec>(static_cast<const Tab*>(P.d_table) + static_cast<size_t>(v) * P.C + c); }
+template <class Tab, int kVec>
+__device__ __forceinline__ void finish_row(const SumParams& P, int v, int c, const float (&sum)[kVec]) {
+    Pack<Tab, kVec> old{};
+    if (P.accumulate) old = row_there<Tab, kVec>(P, v, c);
+    finish_row<Tab, kVec>(P, v, c, sum, old);
 }
-template <class Tab, class Out, int kVec>
+// kAdd: rows are added to, and what is there is on its way with the tokens of the batch (a row is read once for each of its tokens in it, out of L1 but for the first).
+template <class Tab, class Out, int kVec, bool kAdd>
 __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParams P) {
     chain_wait();
     chain_release();
-    if (static_cast<int>(blockIdx.x) >= P.share_blocks) {            // rows without a token: 32 to a warp
-        if (blockIdx.y != 0) return;
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        const long long v0 = (static_cast<long long>(blockIdx.x - P.share_blocks) * (kEmbedThreads / 32) + warp) * 32;
-        uint32_t empty = __ballot_sync(0xffffffffu, v0 + lane < P.V && !has_key(P.keys, P.T, static_cast<int>(v0 + lane)));
-        Pack<Tab, kVec> zero;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) zero.e[e] = from_float<Tab>(0.f);
-        while (empty) {
-            const int k = __ffs(empty) - 1;
-            empty &= empty - 1;
-            Tab* const row = static_cast<Tab*>(P.d_table) + static_cast<size_t>(v0 + k) * P.C;
-#pragma unroll 4
-            for (int c = lane * kVec; c < P.C; c += 32 * kVec) store_pack(row + c, zero);
-        }
-        return;
-    }
+    constexpr int kBatch = kAdd ? kSumBatch / 2 : kSumBatch;
     // the CTA's shares of the sorted tokens at once, so that no row waits for its token's number
     __shared__ int keys[kSumTokens + 2], tokens[kSumTokens];
     const int groups = kEmbedThreads / P.lanes, group = threadIdx.x / P.lanes, lane = threadIdx.x & (P.lanes - 1);
@@ -397,13 +405,14 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParam
     float* const pieces = P.pieces + static_cast<size_t>(share) * 2 * P.C + c;
     const int ahead = keys[begin], behind = keys[end + 1];
     float sum[kVec];
+    Pack<Tab, kVec> old{};
     int row = -1;                               // that `sum` is of
     bool first = true;                          // it is the share's first one
     auto leave = [&](bool at_end) {
         if (row < 0 || row == P.V) return;
         const bool from_ahead = first && row == ahead, goes_on = at_end && row == behind;
         if (!from_ahead && !goes_on) {
-            finish_row<Tab, kVec>(P, row, c, sum);
+            finish_row<Tab, kVec>(P, row, c, sum, old);
             return;
         }
         Pack<float, kVec> to;
@@ -412,18 +421,24 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParam
         store_pack(pieces + (from_ahead ? 0 : P.C), to);
     };
 #pragma unroll 1
-    for (int i = begin; i < end; i += kSumBatch) {
-        Pack<Out, kVec> in[kSumBatch];
+    for (int i = begin; i < end; i += kBatch) {
+        Pack<Out, kVec> in[kBatch];
+        Pack<Tab, kVec> there[kAdd ? kBatch : 1];
+        if (kAdd) {
 #pragma unroll
-        for (int u = 0; u < kSumBatch; ++u) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(tokens[min(i + u, end - 1)]) * P.C);
+            for (int u = 0; u < kBatch; ++u) there[u] = row_there<Tab, kVec>(P, min(keys[min(i + u, end - 1) + 1], P.V - 1), c);
+        }
 #pragma unroll
-        for (int u = 0; u < kSumBatch; ++u) {
+        for (int u = 0; u < kBatch; ++u) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(tokens[min(i + u, end - 1)]) * P.C);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
             if (i + u >= end) break;
             const int key = keys[i + u + 1];
             if (key != row) {
                 leave(false);
                 first = row < 0;
                 row = key;
+                if (kAdd) old = there[u];
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
             }
@@ -511,6 +526,97 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
     }
 }
 
+// ---- few tokens and rows ----------------------------------------------------------------------------------------------------------
+// A CTA has a row (and up to 64 accesses of its columns) to itself: it looks through the indices 4096 at a time, lists the tokens that have the row, in order, and adds theirs up, every group of threads each
+// so-many-th token.
+constexpr int kScanEach = 16, kScanTokens = kEmbedThreads * kScanEach, kScanLanes = 64;
+constexpr long long kScanReads = 16ll << 20;    // indices that all CTAs read, out of L2
+constexpr int kScanMost = 16384, kScanPerRow = 64;      // tokens, and on the average of a row: one that has all of them is one CTA's work
+struct ScanParams {
+    SumParams sum;
+    const int32_t* idx;
+    int* status;
+};
+template <class Tab, class Out, int kVec>
+__global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const ScanParams S) {
+    __shared__ int list[kScanTokens], counts[kEmbedThreads / 32];
+    __shared__ float parts[kEmbedThreads * kVec];
+    chain_wait();
+    chain_release();
+    const SumParams& P = S.sum;
+    const int tid = threadIdx.x, warp = tid >> 5, lane_of_warp = tid & 31, v = blockIdx.x;
+    const int groups = kEmbedThreads / P.lanes, group = tid / P.lanes, lane = tid & (P.lanes - 1), c = (blockIdx.y * P.lanes + lane) * kVec, at = c < P.C ? c : 0;
+    const Out* const d_out = static_cast<const Out*>(P.d_out) + at;
+    Pack<Tab, kVec> old{};
+    if (P.accumulate && group == 0) old = row_there<Tab, kVec>(P, v, at);
+    float sum[kVec] = {};
+    int all = 0;
+#pragma unroll 1
+    for (int t0 = 0; t0 < P.T; t0 += kScanTokens) {
+        const int mine = t0 + tid * kScanEach;
+        int idx[kScanEach];
+        if (mine + kScanEach <= P.T) {
+#pragma unroll
+            for (int q = 0; q < kScanEach / 4; ++q) {
+                const int4 x = __ldg(reinterpret_cast<const int4*>(S.idx + mine) + q);
+                idx[4 * q] = x.x; idx[4 * q + 1] = x.y; idx[4 * q + 2] = x.z; idx[4 * q + 3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kScanEach; ++e) idx[e] = mine + e < P.T ? __ldg(S.idx + mine + e) : -1;
+        }
+        uint32_t hits = 0, bad = 0;
+#pragma unroll
+        for (int e = 0; e < kScanEach; ++e) {
+            hits |= (idx[e] == v ? 1u : 0u) << e;
+            bad |= idx[e] >= P.V ? 1u : 0u;
+        }
+        if (bad && v == 0) set_status(S.status, VARDROP_ERR_INVALID_ARG);
+        const int n = __popc(hits);
+        int up = n;
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+            const int k = __shfl_up_sync(0xffffffffu, up, s);
+            if (lane_of_warp >= s) up += k;
+        }
+        __syncthreads();                        // the list before is read
+        if (lane_of_warp == 31) counts[warp] = up;
+        __syncthreads();
+        int place = up - n, found = 0;
+#pragma unroll
+        for (int w = 0; w < kEmbedThreads / 32; ++w) {
+            if (w < warp) place += counts[w];
+            found += counts[w];
+        }
+        while (hits) {
+            list[place++] = mine + __ffs(hits) - 1;
+            hits &= hits - 1;
+        }
+        __syncthreads();
+        // this group's tokens: those whose place among all of the row is its number, modulo the groups
+        const int begin = (group - all % groups + groups) % groups;
+#pragma unroll 1
+        for (int i = begin; i < found; i += kSumBatch * groups) {
+            Pack<Out, kVec> in[kSumBatch];
+#pragma unroll
+            for (int u = 0; u < kSumBatch; ++u) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(list[min(i + u * groups, found - 1)]) * P.C);
+#pragma unroll
+            for (int u = 0; u < kSumBatch; ++u)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) sum[e] += i + u * groups < found ? to_float(in[u].e[e]) : 0.f;
+        }
+        all += found;
+    }
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) parts[e * kEmbedThreads + tid] = sum[e];
+    __syncthreads();
+    if (group != 0 || c >= P.C || (P.accumulate && all == 0)) return;
+    for (int g = 1; g < groups; ++g)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] += parts[e * kEmbedThreads + g * P.lanes + lane];
+    finish_row<Tab, kVec>(P, v, c, sum, old);
+}
+
 }  // namespace
 
 int embed_validate(const vardrop_embed_cfg& c) {
@@ -554,7 +660,37 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     char* const base = static_cast<char*>(ws);
     int32_t* const keys[2] = {reinterpret_cast<int32_t*>(base + w.keys[0]), reinterpret_cast<int32_t*>(base + w.keys[1])};
     int32_t* const tokens[2] = {reinterpret_cast<int32_t*>(base + w.tokens[0]), reinterpret_cast<int32_t*>(base + w.tokens[1])};
-    SortParams S{idx, nullptr, nullptr, keys[0], tokens[0], reinterpret_cast<int32_t*>(base + w.counts), static_cast<int*>(ws), c.T, c.V, s.bits, 0, s.passes, s.blocks, s.tiles_per_block};
+    SumParams P{d_out, nullptr, nullptr, d_table, reinterpret_cast<float*>(base + w.pieces), c.T, c.V, c.C, u.lanes, u.share, u.shares, c.accumulate, c.scale};
+    const int slabs = (c.C / u.vec + kScanLanes - 1) / kScanLanes;
+    if (c.T <= kScanMost && c.T <= static_cast<long long>(kScanPerRow) * c.V && static_cast<long long>(c.T) * c.V * slabs <= kScanReads && slabs <= 65535) {
+        ScanParams N{P, idx, static_cast<int*>(ws)};
+        if (N.sum.lanes > kScanLanes) N.sum.lanes = kScanLanes;
+        LaunchScope ls_(K_EMBED_SCAN, stream);
+        const cudaError_t err = with_dtype(c.dtype, [&](auto tab) {
+            return with_dtype(c.out_dtype, [&](auto o) {
+                return with_vector(u.vec, [&](auto vec) {
+                    return launch_chained(embed_scan_kernel<decltype(tab), decltype(o), decltype(vec)::value>, dim3(c.V, slabs), dim3(kEmbedThreads), 0, stream, N);
+                });
+            });
+        });
+        return check_cuda(err, "embed: scan launch");
+    }
+    SortParams S{idx, nullptr, nullptr, keys[0], tokens[0], reinterpret_cast<int32_t*>(base + w.counts), static_cast<int*>(ws), c.T, c.V, s.bits, 0, s.passes, s.blocks, s.tiles_per_block, nullptr, 0, 0, nullptr, 0};
+    // The table's zeros, in as many shares as launches sort.
+    const size_t table_bytes = static_cast<size_t>(c.V) * c.C * dtype_bytes(c.dtype), words = c.accumulate ? 0 : table_bytes / 16;
+    const int sorts = c.T <= kOneTile ? 1 : s.passes + 1;
+    if (!c.accumulate && table_bytes % 16 != 0) S.tail = static_cast<unsigned char*>(d_table) + words * 16, S.tail_bytes = static_cast<int>(table_bytes % 16);
+    const auto launch_sort = [&](auto kernel, int workers, int threads, int smem, int which) {
+        const size_t from = words * which / sorts, to = words * (which + 1) / sorts;
+        S.zeros = static_cast<uint4*>(d_table) + from;
+        S.zero_words = to - from;
+        S.workers = workers;
+        const size_t most = static_cast<size_t>(sm_count()) * (2048 / threads), wanted = (S.zero_words + threads * 4 - 1) / (threads * 4) + (S.tail_bytes > 0 ? 1 : 0);
+        const int fill = static_cast<int>(wanted < most ? wanted : most);
+        const cudaError_t e = launch_chained(kernel, dim3(workers + fill), dim3(threads), smem, stream, S);
+        S.tail_bytes = 0;
+        return e;
+    };
     constexpr int kSmall = static_cast<int>(sizeof(SortShared<kOneThreads>)) + 2 * kOneTile * static_cast<int>(sizeof(int));
     static thread_local int attr_dev = -1;
     int dev = 0;
@@ -567,29 +703,33 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     int at = 0;                                 // of the sorted arrays
     if (c.T <= kOneTile) {
         LaunchScope ls_(K_EMBED_SORT, stream);
-        err = launch_chained(embed_sort_small_kernel, dim3(1), dim3(kOneThreads), kSmall, stream, S);
+        err = launch_sort(embed_sort_small_kernel, 1, kOneThreads, kSmall, 0);
         if (int st = check_cuda(err, "embed: sort launch")) return st;
     } else {
-        { LaunchScope ls_(K_EMBED_COUNT, stream); err = launch_chained(embed_count_kernel, dim3(s.blocks), dim3(kSortThreads), 0, stream, S); }
+        { LaunchScope ls_(K_EMBED_COUNT, stream); err = launch_sort(embed_count_kernel, s.blocks, kSortThreads, 0, 0); }
         if (int st = check_cuda(err, "embed: count launch")) return st;
         for (S.pass = 0; S.pass < s.passes; ++S.pass) {
             at = S.pass & 1;
             S.keys = keys[at ^ 1]; S.tokens = tokens[at ^ 1];
             S.keys_out = keys[at]; S.tokens_out = tokens[at];
-            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_chained(embed_sort_kernel, dim3(s.blocks), dim3(kSortThreads), 0, stream, S); }
+            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_sort(embed_sort_kernel, s.blocks, kSortThreads, 0, S.pass + 1); }
             if (int st = check_cuda(err, "embed: sort launch")) return st;
         }
     }
-    SumParams P{d_out, keys[at], tokens[at], d_table, reinterpret_cast<float*>(base + w.pieces), c.T, c.V, c.C, u.lanes, u.share, u.shares, 0, c.accumulate, c.scale};
+    P.keys = keys[at];
+    P.tokens = tokens[at];
     const int groups = kEmbedThreads / u.lanes;
-    P.share_blocks = (u.shares + groups - 1) / groups;
-    const int zero_blocks = c.accumulate ? 0 : (c.V + kEmbedThreads - 1) / kEmbedThreads;
+    const dim3 grid((u.shares + groups - 1) / groups, u.slabs);
     {
         LaunchScope ls_(K_EMBED_SUM, stream);
         err = with_dtype(c.dtype, [&](auto tab) {
             return with_dtype(c.out_dtype, [&](auto o) {
                 return with_vector(u.vec, [&](auto vec) {
-                    return launch_chained(embed_sum_kernel<decltype(tab), decltype(o), decltype(vec)::value>, dim3(P.share_blocks + zero_blocks, u.slabs), dim3(kEmbedThreads), 0, stream, P);
+                    using Tab = decltype(tab);
+                    using Out = decltype(o);
+                    constexpr int kVec = decltype(vec)::value;
+                    return c.accumulate ? launch_chained(embed_sum_kernel<Tab, Out, kVec, true>, grid, dim3(kEmbedThreads), 0, stream, P)
+                                        : launch_chained(embed_sum_kernel<Tab, Out, kVec, false>, grid, dim3(kEmbedThreads), 0, stream, P);
                 });
             });
         });

@@ -2,12 +2,12 @@
 //   lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,label;      G = g_t scale (exp(l_tv - lse_t) - [v = label]),  d_h = G w,  d_w = G^T h
 //
 // loss_rows_kernel    tokens that have a label, one behind the other: positions, labels, and backward lse and the factor of their rows; where some have none, also their rows of h.  Only these take
-//                     part in any product.
+//                     part in any product.  Backward, zeros for the others' d_h.
 // loss_stats_kernel   products of 256 tokens x 256 rows of w; of each row of a tile the maximum and the sum of exponentials go to memory, and the label's logit.
 // loss_join_kernel    lse and loss from these.
 // loss_grad_kernel    backward, for a piece of the vocabulary at a time: the same products again, G of the piece to memory in 16 bits.
 // loss_back_kernel    d_h += G w[piece] in fp32 and d_w[piece] = G^T h, the tiles of both in one launch.
-// loss_rest_kernel    d_h, rounded, to the tokens' places (zeros without a label); parts of d_w, where its products were split along the tokens.
+// loss_rest_kernel    what that left in several pieces or parts, added up and rounded, to its places.
 //
 // Bound: the tensor cores, 2 T V C flop forward and 6 T V C backward (2 of them the logits again: to keep them would take 2 T V bytes), and for few tokens reading w.
 #include <type_traits>
@@ -43,7 +43,7 @@ struct LossPlan {
     int piece, pieces;          // columns of G
     int dh_rows, dw_parts;      // rows that all parts of d_h's products may take; parts of d_w's
     int share, shares;          // tokens of a CTA that finds labels
-    size_t place, pos, label, lse, factor, target, most, packed, part, g, dh, dw, total;
+    size_t place, label, lse, factor, target, most, packed, part, g, dh, dw, total;
 };
 constexpr int kLeastTokens = 16, kRowsGrid = 296;
 LossPlan loss_plan(const vardrop_loss_cfg& c) {
@@ -61,7 +61,7 @@ LossPlan loss_plan(const vardrop_loss_cfg& c) {
     size_t o = align_up(kWsHeaderBytes, 1024);
     const auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes, 1024); return at; };
     const size_t T = c.T, C = c.C, rows = p.rows;
-    p.place = take(4 * T); p.pos = take(4 * T); p.label = take(4 * T); p.lse = take(4 * T); p.factor = take(4 * T); p.target = take(4 * T);
+    p.place = take(4 * T); p.label = take(4 * T); p.lse = take(4 * T); p.factor = take(4 * T); p.target = take(4 * T);
     p.most = take(4ull * p.shares);
     p.packed = take(2 * rows * C);
     const size_t shared = o;                            // forward and backward each have their own from here on
@@ -71,7 +71,7 @@ LossPlan loss_plan(const vardrop_loss_cfg& c) {
     p.g = take(2 * rows * p.piece);
     p.dh = take(4ull * p.dh_rows * C);
     p.dw = take(p.dw_parts > 1 ? 4ull * p.piece * C * p.dw_parts : 0);
-    p.total = o > forward ? o : forward;
+    p.total = (o > forward ? o : forward) + 1024;       // for a beginning that is not aligned
     return p;
 }
 
@@ -81,8 +81,8 @@ struct RowsParams {
     const float *lse, *d_loss;                          // backward
     float *loss, *lse_out;                              // forward: zeros where there is no label
     const uint4* h;
-    uint4* packed;
-    int32_t *place, *pos, *label;                       // token of a row; row of a token, or -1; label of a row
+    uint4 *packed, *d_h;                                // d_h: zeros where there is no label; NULL: not wanted
+    int32_t *place, *label;                             // token and label of a row
     float *row_lse, *factor, *most;                     // most: the largest factor of a share's tokens
     int* header;
     int T, V, share, vectors;                           // tokens of a CTA; 16-byte vectors of a row
@@ -175,12 +175,15 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
                 P.loss[t] = 0.f;
                 P.lse_out[t] = 0.f;
             }
-            if (P.lse) P.pos[t] = there ? row : -1;
         }
         if (!packs) continue;
         __syncthreads();
         for (int k = warp; k < kRowsThreads && t0 + k < end; k += kRowsWarps) {
-            if (rows[k] < 0) continue;
+            if (rows[k] < 0) {
+                if (P.d_h)
+                    for (int i = lane; i < P.vectors; i += 32) P.d_h[static_cast<size_t>(t0 + k) * P.vectors + i] = make_uint4(0u, 0u, 0u, 0u);
+                continue;
+            }
             const uint4* const from = P.h + static_cast<size_t>(t0 + k) * P.vectors;
             uint4* const to = P.packed + static_cast<size_t>(rows[k]) * P.vectors;
 #pragma unroll 4
@@ -210,15 +213,16 @@ struct PairParams {
     int T, V, C;
     int v0, v1;                                         // the piece
     int pitch;                                          // columns of G
-    int add, fp16, shares;
+    int add, whole, fp16, shares;                       // add: not the first piece; whole: the only one
+    int sectors_h, sectors_w;                           // whether sixteen columns of d_h and of d_w are a sector
     float scale;
-    const int32_t* label;
+    const int32_t *label, *place;
     const float *row_lse, *factor, *most;
     float2* part;                                       // [half tiles of the vocabulary, rows]
     float* target;
     void* g;
     float *dh, *dw;                                     // [parts, rows of tiles, C], [parts, columns of G, C]
-    void* out;                                          // d_w
+    void *d_h, *d_w;
     int rows;                                           // of `part`
     SplitParams split;
 };
@@ -236,6 +240,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// A whole 32-byte sector a lane: lanes have different rows, and sixteen bytes of each would be half a sector an instruction.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ void load_sector(float (&v)[8], const void* p) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p) : "memory");
 }
 
 // What a thread does with 128 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
@@ -279,7 +291,7 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
         const bool there = row < n;
         const int left = P.V - P.v0 - col, label = there ? __ldg(P.label + row) - P.v0 - col : -1;
         const float lse = there ? __ldg(P.row_lse + row) : 0.f, factor = there ? __ldg(P.factor + row) * up : 0.f;
-        uint4* const to = reinterpret_cast<uint4*>(static_cast<T*>(P.g) + static_cast<size_t>(row) * P.pitch + col);
+        T* const to = static_cast<T*>(P.g) + static_cast<size_t>(row) * P.pitch + col;
 #pragma unroll 1
         for (int c = 0; c < kHalfTile; c += 32) {
             __syncwarp();
@@ -297,42 +309,56 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
                     if (!there || c + e >= left) r[e] = 0.f;
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                to[c / 8 + q] = make_uint4(pack16<T>(r[8 * q], r[8 * q + 1]), pack16<T>(r[8 * q + 2], r[8 * q + 3]), pack16<T>(r[8 * q + 4], r[8 * q + 5]), pack16<T>(r[8 * q + 6], r[8 * q + 7]));
+            for (int q = 0; q < 2; ++q) {
+                uint32_t v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = pack16<T>(r[16 * q + 2 * e], r[16 * q + 2 * e + 1]);
+                store_sector(to + c + 16 * q, v);
+            }
         }
     } else {
-        const bool some = x.k1 > x.k0, there = row < (x.dw ? P.v1 - P.v0 : n), direct = x.dw && tiles.splits.dw == 1, add = !x.dw && P.add;
+        const bool some = x.k1 > x.k0, there = row < (x.dw ? P.v1 - P.v0 : n), add = !x.dw && P.add;
+        const bool direct = x.dw ? tiles.splits.dw == 1 : P.whole && tiles.splits.dh == 1;        // nothing else comes to it
         const float mul = up;
         const size_t rows = x.dw ? P.split.piece : (n + kPairTile - 1) / kPairTile * kPairTile;
         float* const acc = (x.dw ? P.dw : P.dh) + (x.part * rows + row) * P.C + col;
-        T* const out = static_cast<T*>(P.out) + (static_cast<size_t>(P.v0) + row) * P.C + col;
+        const size_t to = x.dw ? static_cast<size_t>(P.v0) + row : there && direct ? static_cast<size_t>(__ldg(P.place + row)) : 0;
+        T* const out = static_cast<T*>(x.dw ? P.d_w : P.d_h) + to * P.C + col;
 #pragma unroll 1
         for (int c = 0; c < kHalfTile && col + c < P.C; c += 32) {
             __syncwarp();
             float r[32];
             tmem_ld32(tm + c, r);
             tmem_ld_wait();
+            if (!some) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (!there || col + c + 8 * q >= P.C) continue;       // C is a multiple of 8
-                float* const v = r + 8 * q;
-                if (!some) {
+                for (int e = 0; e < 32; ++e) r[e] = 0.f;
+            }
+            if (!there) {
+            } else if (!direct) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+                for (int q = 0; q < 4; ++q) {
+                    if (col + c + 8 * q >= P.C) continue;             // C is a multiple of 8
+                    float v[8] = {};
+                    if (add) load_sector(v, acc + c + 8 * q);
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(r[8 * q + e] + v[e]);
+                    store_sector(acc + c + 8 * q, w);
                 }
-                if (direct) {
-                    *reinterpret_cast<uint4*>(out + c + 8 * q) =
-                        make_uint4(pack16<T>(v[0] * mul, v[1] * mul), pack16<T>(v[2] * mul, v[3] * mul), pack16<T>(v[4] * mul, v[5] * mul), pack16<T>(v[6] * mul, v[7] * mul));
-                } else {
-                    float4* const at = reinterpret_cast<float4*>(acc + c + 8 * q);
-                    float4 lo = make_float4(v[0], v[1], v[2], v[3]), hi = make_float4(v[4], v[5], v[6], v[7]);
-                    if (add) {
-                        const float4 a = at[0], b = at[1];
-                        lo.x += a.x; lo.y += a.y; lo.z += a.z; lo.w += a.w;
-                        hi.x += b.x; hi.y += b.y; hi.z += b.z; hi.w += b.w;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = pack16<T>(r[16 * q + 2 * e] * mul, r[16 * q + 2 * e + 1] * mul);
+                    T* const at = out + c + 16 * q;
+                    if (x.dw ? P.sectors_w : P.sectors_h) {
+                        if (col + c + 16 * q < P.C) store_sector(at, w);
+                    } else {
+                        if (col + c + 16 * q < P.C) *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+                        if (col + c + 16 * q + 8 < P.C) reinterpret_cast<uint4*>(at)[1] = make_uint4(w[4], w[5], w[6], w[7]);
                     }
-                    at[0] = lo;
-                    at[1] = hi;
                 }
             }
         }
@@ -517,44 +543,45 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) loss_join_kernel(const
 // ---- gradients' last step -------------------------------------------------------------------------------------------------------
 struct RestParams {
     const float *dh, *dw;
-    const int32_t* pos;                                 // row of a token, or -1
+    const int32_t* place;                               // token of a row
     const int* header;
-    void *d_h, *d_w;                                    // d_w NULL: written as it is
-    int T, V, C;
+    void *d_h, *d_w;
+    int T, V, C, whole;
     int h_blocks;                                       // CTAs of d_h
     float scale;
     SplitParams split;
 };
-constexpr int kRestThreads = 256;
-// Eight columns a thread.
+constexpr int kRestThreads = 256, kRestRows = 16;       // rows of a CTA
+// Rows that are not in their places yet: of d_h where there were several pieces or parts, of d_w where there were parts.  Eight columns a thread.
 template <class T>
 __global__ void __launch_bounds__(kRestThreads) loss_rest_kernel(const RestParams P) {
     chain_wait();
     chain_release();
     const bool dw = static_cast<int>(blockIdx.x) >= P.h_blocks;
-    const int n = __ldcg(P.header + kLossRows), vectors = P.C / 8, count = dw ? P.V : P.T;
+    const int n = __ldcg(P.header + kLossRows), vectors = P.C / 8, count = dw ? P.V : n;
     const Splits splits = splits_of(P.split, n);
-    if (dw && splits.dw == 1) return;                   // written as it is
-    const long long at = (static_cast<long long>(blockIdx.x) - (dw ? P.h_blocks : 0)) * kRestThreads + threadIdx.x, t = at / vectors;
-    if (t >= count) return;
-    const int c = static_cast<int>(at - t * vectors) * 8, parts = dw ? splits.dw : splits.dh;
-    const long long row = dw ? t : __ldcg(P.pos + t);
+    if (dw ? splits.dw == 1 : P.whole && splits.dh == 1) return;
+    const int first = (static_cast<int>(blockIdx.x) - (dw ? P.h_blocks : 0)) * kRestRows, rows = min(kRestRows, count - first), parts = dw ? splits.dw : splits.dh;
     const size_t part = static_cast<size_t>(dw ? P.split.piece : (n + kPairTile - 1) / kPairTile * kPairTile) * P.C;
-    const float mul = row >= 0 ? P.scale * __int_as_float(__ldcg(P.header + kLossInverse)) : 0.f;
-    const float* from = (dw ? P.dw : P.dh) + row * P.C + c;
-    float v[8] = {};
-    if (row >= 0) {
+    const float mul = P.scale * __int_as_float(__ldcg(P.header + kLossInverse));
+    const float* const base = (dw ? P.dw : P.dh) + static_cast<size_t>(first) * P.C;
+#pragma unroll 1
+    for (int at = threadIdx.x; at < rows * vectors; at += kRestThreads) {
+        const int r = at / vectors, c = (at - r * vectors) * 8;
+        const float* from = base + static_cast<size_t>(r) * P.C + c;
+        float v[8] = {};
 #pragma unroll 4
         for (int s = 0; s < parts; ++s, from += part) {
             const Pack<float, 8> a = load_pack<float, 8>(from);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += a.e[e];
         }
-    }
-    Pack<T, 8> o;
+        Pack<T, 8> o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(row >= 0 ? v[e] * mul : 0.f);
-    store_pack(static_cast<T*>(dw ? P.d_w : P.d_h) + t * P.C + c, o);
+        for (int e = 0; e < 8; ++e) o.e[e] = from_float<T>(v[e] * mul);
+        const size_t to = dw ? static_cast<size_t>(first) + r : static_cast<size_t>(__ldcg(P.place + first + r));
+        store_pack(static_cast<T*>(dw ? P.d_w : P.d_h) + to * P.C + c, o);
+    }
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -597,11 +624,12 @@ struct LossCall {
     char* base;
 };
 // Where things are, and the launches that both passes begin with.
-int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, const float* lse, const float* d_loss, float* loss, float* lse_out, void* ws, bool backward,
-               cudaStream_t stream) {
+int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, const float* lse, const float* d_loss, float* loss, float* lse_out, void* d_h,
+               void* ws, bool backward, cudaStream_t stream) {
     L.plan = loss_plan(c);
     const LossPlan& p = L.plan;
-    char* const base = L.base = static_cast<char*>(ws);
+    // (a workspace begins on any 16 bytes; its header does so there, everything else behind the next multiple of 1024, plus 1024)
+    char* const base = L.base = reinterpret_cast<char*>(align_up(reinterpret_cast<uintptr_t>(ws), 1024));
     const bool fp16 = c.dtype == 1;
     if (int st = loss_map(&L.maps.h, h, fp16, c.T, c.C)) return st;
     if (int st = loss_map(&L.maps.packed, base + p.packed, fp16, p.rows, c.C)) return st;
@@ -611,8 +639,8 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     } else {
         L.maps.g = L.maps.packed;
     }
-    RowsParams R{labels, lse, d_loss, loss, lse_out, static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), reinterpret_cast<int32_t*>(base + p.place),
-                 reinterpret_cast<int32_t*>(base + p.pos), reinterpret_cast<int32_t*>(base + p.label), reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor),
+    RowsParams R{labels, lse, d_loss, loss, lse_out, static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), static_cast<uint4*>(d_h), reinterpret_cast<int32_t*>(base + p.place),
+                 reinterpret_cast<int32_t*>(base + p.label), reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor),
                  reinterpret_cast<float*>(base + p.most), static_cast<int*>(ws), c.T, c.V, p.share, c.C / 8};
     {
         LaunchScope ls_(K_LOSS_ROWS, stream);
@@ -622,7 +650,7 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     P = PairParams{};
     P.header = R.header;
     P.T = c.T; P.V = c.V; P.C = c.C; P.v0 = 0; P.v1 = c.V; P.pitch = p.piece; P.shares = p.shares; P.fp16 = fp16; P.scale = c.scale == 0.f ? 1.f : c.scale;
-    P.label = R.label; P.row_lse = R.row_lse; P.factor = R.factor; P.most = R.most;
+    P.label = R.label; P.place = R.place; P.row_lse = R.row_lse; P.factor = R.factor; P.most = R.most;
     P.part = reinterpret_cast<float2*>(base + p.part); P.target = reinterpret_cast<float*>(base + p.target);
     P.g = base + p.g; P.dh = reinterpret_cast<float*>(base + p.dh); P.dw = reinterpret_cast<float*>(base + p.dw); P.rows = p.rows;
     return VARDROP_OK;
@@ -634,7 +662,9 @@ int loss_backward(LossCall& L, const vardrop_loss_cfg& c, void* d_h, void* d_w, 
     const long long tm = p.rows / kPairTile, tc = ceil_div(c.C, kPairTile);
     PairParams& P = L.P;
     P.split = SplitParams{sm_count() / 2, static_cast<int>(tc), p.piece, p.dh_rows, p.dw_parts, d_h != nullptr, d_w != nullptr};
-    P.out = d_w;
+    P.d_h = d_h; P.d_w = d_w; P.whole = p.pieces == 1;
+    P.sectors_h = c.C % 16 == 0 && reinterpret_cast<uintptr_t>(d_h) % 32 == 0;
+    P.sectors_w = c.C % 16 == 0 && reinterpret_cast<uintptr_t>(d_w) % 32 == 0;
     for (int i = 0; i < p.pieces; ++i) {
         P.v0 = i * p.piece;
         P.v1 = c.V - P.v0 < p.piece ? c.V : P.v0 + p.piece;
@@ -646,10 +676,9 @@ int loss_backward(LossCall& L, const vardrop_loss_cfg& c, void* d_h, void* d_w, 
     }
     const bool parts = d_w && p.dw_parts > 1;
     if (!d_h && !parts) return VARDROP_OK;
-    const auto blocks = [&](long long count) { return static_cast<int>((count * (c.C / 8) + kRestThreads - 1) / kRestThreads); };
-    const RestParams R{P.dh, P.dw, reinterpret_cast<const int32_t*>(L.base + p.pos), P.header, d_h, d_w, c.T, c.V, c.C, d_h ? blocks(c.T) : 0, P.scale, P.split};
+    const RestParams R{P.dh, P.dw, P.place, P.header, d_h, d_w, c.T, c.V, c.C, P.whole, d_h ? ceil_div(c.T, kRestRows) : 0, P.scale, P.split};
     LaunchScope ls_(K_LOSS_REST, stream);
-    return check_cuda(launch_chained(loss_rest_kernel<T>, dim3(R.h_blocks + (parts ? blocks(c.V) : 0)), dim3(kRestThreads), 0, stream, R), "loss: rest launch");
+    return check_cuda(launch_chained(loss_rest_kernel<T>, dim3(R.h_blocks + (parts ? ceil_div(c.V, kRestRows) : 0)), dim3(kRestThreads), 0, stream, R), "loss: rest launch");
 }
 
 }  // namespace
@@ -668,7 +697,7 @@ size_t loss_workspace_bytes(const vardrop_loss_cfg& c) { return loss_plan(c).tot
 
 int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, float* loss, float* lse, void* ws, cudaStream_t stream) {
     LossCall L;
-    if (int st = loss_begin(L, h, w, labels, c, nullptr, nullptr, loss, lse, ws, false, stream)) return st;
+    if (int st = loss_begin(L, h, w, labels, c, nullptr, nullptr, loss, lse, nullptr, ws, false, stream)) return st;
     const LossPlan& p = L.plan;
     const int tv = ceil_div(c.V, kPairTile);
     if (int st = launch_products<kStats, __nv_bfloat16>(K_LOSS_STATS, static_cast<long long>(p.rows / kPairTile) * tv, L.maps, L.P, stream)) return st;
@@ -679,7 +708,7 @@ int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const v
 
 int loss_bwd_launch(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg& c, void* d_h, void* d_w, void* ws, cudaStream_t stream) {
     LossCall L;
-    if (int st = loss_begin(L, h, w, labels, c, lse, d_loss, nullptr, nullptr, ws, true, stream)) return st;
+    if (int st = loss_begin(L, h, w, labels, c, lse, d_loss, nullptr, nullptr, d_h, ws, true, stream)) return st;
     return c.dtype == 1 ? loss_backward<__half>(L, c, d_h, d_w, stream) : loss_backward<__nv_bfloat16>(L, c, d_h, d_w, stream);
 }
 

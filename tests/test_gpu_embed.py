@@ -101,6 +101,26 @@ def test_all_tokens_of_one_row_and_none_at_all(T):
     check_backward(T, 300, 64, FP, BF, 1.0, idx=torch.arange(T, dtype=torch.int32, device="cuda").flip(0) % 300)
 
 
+@pytest.mark.parametrize("T", [200, 6000])
+@pytest.mark.parametrize("V,C", [(1, 1), (1, 3), (2, 3), (3, 7), (5, 9)])
+def test_tables_that_are_no_whole_words(T, V, C):
+    """Tens of tokens a row and more, tables that end inside sixteen bytes, with rows that no token has."""
+    for table in (BF, FP):
+        check_backward(T, V, C, table, BF)
+        check_backward(T, V, C, table, BF, idx=torch.full((T,), -1, dtype=torch.int32, device="cuda"))
+        check_backward(T, V, C, table, BF, idx=torch.full((T,), V - 1, dtype=torch.int32, device="cuda"))
+
+
+def test_neighbours_of_the_table_are_left_alone():
+    T, V, C = 6000, 5, 9
+    idx, d = tokens(T, V, 3), normal((T, C), BF, 4)
+    cfg, ws = config(T, V, C, BF, BF)
+    flat = torch.full((V * C + 64,), 5.0, dtype=BF, device="cuda")
+    vd.vardrop_embed_bwd(d, idx, cfg, flat[:V * C].view(V, C), ws)
+    near(flat[:V * C].view(V, C), *wanted_rows(d, idx, V, 1.0))
+    assert bool((flat[V * C:] == 5.0).all())
+
+
 def test_more_digits_and_tiles_than_one():
     check_backward((1 << 20) + 4097, 7, 3, FP, FP, 1.0, "skewed", 0.1)           # several tiles to a CTA
     check_backward(5000, (1 << 18) + 1, 2, FP, FP, 1.0, "skewed", 0.1)           # three passes

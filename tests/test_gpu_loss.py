@@ -171,6 +171,27 @@ def test_the_same_bits_every_time_and_one_gradient_alone():
         assert all(b is None or torch.equal(a, b) for a, b in zip(first, again))
 
 
+@pytest.mark.parametrize("C", [64, 72])
+def test_buffers_on_any_sixteen_bytes(C):
+    """Tensors and workspace that begin on 16 bytes, not on 32."""
+    case = Case(300, 700, C, gaps=0.2)
+    first = case.run()
+
+    def shifted(t):
+        flat = torch.zeros(t.numel() + 64, dtype=t.dtype, device="cuda")
+        at = 16 // t.element_size() + (-flat.data_ptr() // t.element_size()) % (512 // t.element_size())
+        view = flat[at:at + t.numel()].view(t.shape)
+        assert view.data_ptr() % 32 == 16
+        return view.copy_(t)
+
+    case.h, case.w, case.labels, case.d_loss = (shifted(t) for t in (case.h, case.w, case.labels, case.d_loss))
+    case.ws = shifted(torch.zeros(vd.vardrop_loss_workspace_bytes(case.cfg), dtype=torch.uint8, device="cuda"))
+    loss, lse, d_h, d_w = (shifted(torch.full_like(t, 7.0)) for t in first)
+    vd.vardrop_loss_fwd(case.h, case.w, case.labels, case.cfg, loss, lse, case.ws)
+    vd.vardrop_loss_bwd(case.h, case.w, case.labels, lse, case.d_loss, case.cfg, d_h, d_w, case.ws)
+    assert vd.ws_status(case.ws) == vd.OK and all(torch.equal(a, b) for a, b in zip(first, (loss, lse, d_h, d_w)))
+
+
 def test_labels_behind_the_classes_are_none_and_reported():
     case = Case(50, 30, 16)
     want = case.run()
