@@ -11,6 +11,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "packed_math.cuh"
 #include "vec_io.cuh"
 
 namespace vardrop {
@@ -31,21 +32,7 @@ struct ActParams {
     int B, N, C, S, blocks, chunks;             // chunks: pieces of a row that a warp takes at a time
 };
 
-// ---- packed fp32 pairs -------------------------------------------------------------------------------------------------------------
-// These kernels are bound by the instructions that they issue long before the memory (gelu of 8192 x 2048 bf16 forward: 71 a value, 49 us); a pair in one instruction halves those of the arithmetic.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n.reg .b64 x, y, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 w, x, y;\nmov.b64 {%0, %1}, w;\n}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+// These kernels are bound by the instructions that they issue long before the memory (gelu of 8192 x 2048 bf16 forward: 71 a value, 49 us); arithmetic on pairs halves it.
 __device__ __forceinline__ float exp2_of(float x) {
     float y;
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -121,12 +108,10 @@ __device__ __forceinline__ void act_slope(float2 a, float2& f, float2& slope) {
 }
 
 // ---- eight bits ---------------------------------------------------------------------------------------------------------------------
-// Biased exponent of the block's scale from the largest magnitude's bits.
-__device__ __forceinline__ int scale_of(uint32_t top) {
-    const int e = static_cast<int>(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u);        // 448 = 1.75 2^8
-    return max(e, 0);
-}
-__device__ __forceinline__ float to_block(int scale) { return __uint_as_float(static_cast<uint32_t>(254 - scale) << 23); }     // 2^-e
+// From the largest magnitude's bits of a block: those of the power of two at or above max / 1.75 (the carry of a mantissa beyond 1.75 = 448 / 2^8), its scale's biased exponent and 2^-e.
+__device__ __forceinline__ uint32_t ceiling_of(uint32_t top) { return (top + 0x1fffffu) & 0xff800000u; }
+__device__ __forceinline__ int scale_of(uint32_t top) { return max(static_cast<int>(ceiling_of(top) >> 23) - 8, 0); }
+__device__ __forceinline__ float to_block(uint32_t top) { return __uint_as_float(min((262u << 23) - ceiling_of(top), 254u << 23)); }
 __device__ __forceinline__ float from_block(int scale) { return __uint_as_float(scale ? static_cast<uint32_t>(scale) << 23 : 0x400000u); }
 __device__ __forceinline__ uint32_t code2(float2 v) { return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3); }
 __device__ __forceinline__ float2 value2(uint32_t code) {
@@ -206,14 +191,15 @@ __device__ __forceinline__ void put_codes(const ActParams& P, int which, const P
             top = max(fine, __shfl_xor_sync(0xffffffffu, fine, 2));
         }
         if (p.left <= 0) return;
-        const int scale = scale_of(top);
-        const float2 mul = both(to_block(scale));
+        const float2 mul = both(to_block(top));
         uint2 c;
         c.x = code2(mul2(v[0], mul)) | code2(mul2(v[1], mul)) << 16;
         c.y = code2(mul2(v[2], mul)) | code2(mul2(v[3], mul)) << 16;
         *reinterpret_cast<uint2*>(at) = c;
-        if ((p.c & (kBlock - 1)) == 0) *scales = static_cast<unsigned char>(scale);
+        if ((p.c & (kBlock - 1)) == 0) *scales = static_cast<unsigned char>(scale_of(top));
     } else {
+        const int lane = threadIdx.x & 31;
+        uint32_t mine = 0;                      // lane e keeps block e's, for its scale
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             float x = e & 1 ? v[e / 2].y : v[e / 2].x;
@@ -222,10 +208,10 @@ __device__ __forceinline__ void put_codes(const ActParams& P, int which, const P
                 x = held_as<T>(x);
                 top = __reduce_max_sync(0xffffffffu, p.live(e) && magnitude(x) < kInfinity ? magnitude(x) : 0u);
             }
-            const int scale = scale_of(top);
-            if (p.live(e)) at[32 * e] = static_cast<unsigned char>(code2(make_float2(x * to_block(scale), 0.f)));
-            if ((threadIdx.x & 31) == 0 && p.live(e)) scales[e] = static_cast<unsigned char>(scale);
+            if (p.live(e)) at[32 * e] = static_cast<unsigned char>(code2(make_float2(x * to_block(top), 0.f)));
+            if (lane == e) mine = top;
         }
+        if (lane < kPer && 32 * lane < p.left + lane) scales[lane] = static_cast<unsigned char>(scale_of(mine));       // blocks that begin within the row
     }
 }
 // Codes as they lie in memory, so that the loads of several pieces overlap.
@@ -398,9 +384,9 @@ int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cuda
     const bool wide = c.C % 8 == 0;             // (a stride is a multiple of 8 wherever there is one)
     P.chunks = (c.C + 32 * kPer - 1) / (32 * kPer);
     const long long tasks = static_cast<long long>(c.N) * P.chunks;
-    // Every row counts, and enough of them for four CTAs on every SM: two pieces to a warp.  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their
+    // Every row counts, and enough of them for four CTAs on every SM: two pieces to a warp (where they are vectors).  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their
     // instance's pieces (a CTA for each few pieces of all rows, four of five of them without work: 172 of 862 kept rows of 32 instances, gelu of 2048, forward and backward, 52.7 us instead of 35).
-    const bool many = !n_sel && tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
+    const bool many = !n_sel && wide && tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
     const int per = kActWarps * (many ? kActTasks : 1);
     const long long full = (tasks + per - 1) / per, held = (static_cast<long long>(sm_count()) * kActPerSm + c.B - 1) / c.B;
     const dim3 grid(static_cast<unsigned>(n_sel && held < full ? held : full), c.B < kMaxGridY ? c.B : kMaxGridY);
@@ -416,7 +402,7 @@ int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cuda
                 if constexpr (kBwd) return launch_chained(act_bwd_kernel<T, kWide, kKind, kGated, kTasks>, grid, dim3(kActThreads), 0, stream, P);
                 else return launch_chained(act_fwd_kernel<T, kWide, kKind, kGated, kTasks>, grid, dim3(kActThreads), 0, stream, P);
             };
-            return wide ? (many ? go(VecSize<1>{}, VecSize<kActTasks>{}) : go(VecSize<1>{}, VecSize<1>{})) : (many ? go(VecSize<0>{}, VecSize<kActTasks>{}) : go(VecSize<0>{}, VecSize<1>{}));
+            return !wide ? go(VecSize<0>{}, VecSize<1>{}) : many ? go(VecSize<1>{}, VecSize<kActTasks>{}) : go(VecSize<1>{}, VecSize<1>{});
         });
     });
     return check_cuda(err, kBwd ? "act: backward launch" : "act: forward launch");

@@ -14,6 +14,7 @@
 
 #include "attn_common.cuh"
 #include "loss_tiles.h"
+#include "packed_math.cuh"
 #include "pair_mma.cuh"
 #include "vec_io.cuh"
 
@@ -22,16 +23,19 @@ namespace vardrop {
 namespace {
 
 constexpr int kHalfTile = 128;                       // a CTA's rows of a tile
+constexpr int kTakeCols = 128;                        // columns that a thread takes out of a finished tile
+constexpr int kTakeWarps = 4 * (kPairTile / kTakeCols);
 constexpr int kBoxBytes = 64 * 64 * 2;               // what a copy brings
 constexpr int kStageBytes = 4 * kBoxBytes;           // two boxes of either operand
 constexpr int kStages = 6;
-constexpr int kPairThreads = 384;
+constexpr int kPairThreads = 128 + 32 * kTakeWarps;
 constexpr int kPairSmemBytes = 1024 + 1024 + kStages * kStageBytes;
 constexpr uint32_t kPairTmemCols = 512;              // two accumulators of 256 columns
 constexpr size_t kPieceBytes = 256u << 20;           // of G; larger pieces make fewer passes over d_h
 constexpr int kLeastPiece = 1024;
 constexpr size_t kPartBytes = 64u << 20;             // of parts of a gradient's products
 constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 enum LossWord { kLossRows = 16, kLossInverse };      // words of the workspace's header: labelled tokens; the inverse of what G is scaled by
 
@@ -65,7 +69,7 @@ LossPlan loss_plan(const vardrop_loss_cfg& c) {
     p.most = take(4ull * p.shares);
     p.packed = take(2 * rows * C);
     const size_t shared = o;                            // forward and backward each have their own from here on
-    p.part = take(8 * rows * 2 * ceil_div(c.V, kPairTile));
+    p.part = take(8 * rows * (kPairTile / kTakeCols) * ceil_div(c.V, kPairTile));
     const size_t forward = o;
     o = shared;
     p.g = take(2 * rows * p.piece);
@@ -218,7 +222,7 @@ struct PairParams {
     float scale;
     const int32_t *label, *place;
     const float *row_lse, *factor, *most;
-    float2* part;                                       // [half tiles of the vocabulary, rows]
+    float2* part;                                       // [64 classes each, rows]
     float* target;
     void* g;
     float *dh, *dw;                                     // [parts, rows of tiles, C], [parts, columns of G, C]
@@ -250,7 +254,7 @@ __device__ __forceinline__ void load_sector(float (&v)[8], const void* p) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p) : "memory");
 }
 
-// What a thread does with 128 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
+// What a thread does with 64 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
 template <int kMode, class T, class Tiles>
 __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x, uint32_t tm, int row, int col, int n, float up, const Tiles& tiles) {
     if constexpr (kMode == kStats) {
@@ -260,7 +264,7 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
         const float k = P.scale * kLog2e;
         float m = -INFINITY, s = 0.f;
 #pragma unroll 1
-        for (int c = 0; c < kHalfTile && c < left; c += 32) {
+        for (int c = 0; c < kTakeCols && c < left; c += 32) {
             __syncwarp();
             float r[32];
             tmem_ld32(tm + c, r);
@@ -280,28 +284,43 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
             for (int e = 4; e < 32; ++e) t[e & 3] = fmaxf(t[e & 3], r[e]);
             const float top = fmaxf(m, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
             // differences of the sums ahead of the scale: exact however far from zero the logits are
-            float sum[4] = {s * exp2_fast((m - top) * k), 0.f, 0.f, 0.f};
+            float2 sum[2] = {make_float2(s * exp2_fast((m - top) * k), 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-            for (int e = 0; e < 32; ++e) sum[e & 3] += exp2_fast((r[e] - top) * k);
-            s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            for (int e = 0; e < 32; e += 2) {
+                const float2 d = mul2(add2(make_float2(r[e], r[e + 1]), both(-top)), both(k));
+                sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], make_float2(exp2_fast(d.x), exp2_fast(d.y)));
+            }
+            s = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             m = top;
         }
-        if (row < n) P.part[static_cast<size_t>(col / kHalfTile) * P.rows + row] = make_float2(m, s);
+        if (row < n) P.part[static_cast<size_t>(col / kTakeCols) * P.rows + row] = make_float2(m, s);
     } else if constexpr (kMode == kGrad) {
         const bool there = row < n;
         const int left = P.V - P.v0 - col, label = there ? __ldg(P.label + row) - P.v0 - col : -1;
         const float lse = there ? __ldg(P.row_lse + row) : 0.f, factor = there ? __ldg(P.factor + row) * up : 0.f;
         T* const to = static_cast<T*>(P.g) + static_cast<size_t>(row) * P.pitch + col;
 #pragma unroll 1
-        for (int c = 0; c < kHalfTile; c += 32) {
+        for (int c = 0; c < kTakeCols; c += 32) {
             __syncwarp();
             float r[32];
             tmem_ld32(tm + c, r);
             tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                const float p = exp2_fast(fmaf(r[e], P.scale, -lse) * kLog2e);
-                r[e] = factor * (label == c + e ? p - 1.f : p);
+            for (int e = 0; e < 32; e += 2) {
+                const float2 d = mul2(fma2(make_float2(r[e], r[e + 1]), both(P.scale), both(-lse)), both(kLog2e));
+                r[e] = exp2_fast(d.x);
+                r[e + 1] = exp2_fast(d.y);
+            }
+            if (label >= c && label < c + 32) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (label == c + e) r[e] -= 1.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+                const float2 v = mul2(make_float2(r[e], r[e + 1]), both(factor));
+                r[e] = v.x;
+                r[e + 1] = v.y;
             }
             if (!there || c + 32 > left) {              // zeros, whatever the products there are
 #pragma unroll
@@ -325,7 +344,7 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
         const size_t to = x.dw ? static_cast<size_t>(P.v0) + row : there && direct ? static_cast<size_t>(__ldg(P.place + row)) : 0;
         T* const out = static_cast<T*>(x.dw ? P.d_w : P.d_h) + to * P.C + col;
 #pragma unroll 1
-        for (int c = 0; c < kHalfTile && col + c < P.C; c += 32) {
+        for (int c = 0; c < kTakeCols && col + c < P.C; c += 32) {
             __syncwarp();
             float r[32];
             tmem_ld32(tm + c, r);
@@ -367,14 +386,15 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
 
 // warp 0          (of either CTA) loads: a ring of stages, 64 of the contracted axis for 128 rows of A and 128 of B
 // warp 1          of the leader: products
-// warps 4 to 11   (of either CTA) take a finished tile out, 128 columns of a row a thread, under the products of the next one
+// warps 4 to 19   (of either CTA) take a finished tile out, 64 columns of a row a thread, under the products of the next one (8 warps with 128 columns each took 2.6 us a tile, the products of 512
+//                 channels take 2.2)
 template <int kMode, class T>
 __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __grid_constant__ LossMaps maps, const PairParams P) {
     extern __shared__ unsigned char smem_dyn[];
     uint64_t* const bar_full = reinterpret_cast<uint64_t*>(smem_dyn);       // [kStages] both CTAs' copies (the leader's)
     uint64_t* const bar_empty = bar_full + kStages;                         // [kStages] the products that read the stage are done
     uint64_t* const bar_acc = bar_empty + kStages;                          // [2] the tile is complete
-    uint64_t* const bar_taken = bar_acc + 2;                                // [2] and has been taken out by all sixteen warps (the leader's)
+    uint64_t* const bar_taken = bar_acc + 2;                                // [2] and has been taken out by the warps of both CTAs (the leader's)
     uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bar_taken + 2);
     unsigned char* const stages = align_tiles(smem_dyn + 1024);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -387,7 +407,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_acc + i, 1);
-            mbar_init(bar_taken + i, 16);
+            mbar_init(bar_taken + i, 2 * kTakeWarps);
         }
         mbar_fence_init();
     }
@@ -473,8 +493,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
             __syncwarp();
         }
     } else if (warp >= 4) {
-        const int in_tile = static_cast<int>(rank) * kHalfTile + (warp & 3) * 32 + lane, half = (warp - 4) >> 2;
-        const uint32_t tm_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * kHalfTile;
+        const int in_tile = static_cast<int>(rank) * kHalfTile + (warp & 3) * 32 + lane, part = (warp - 4) >> 2;
+        const uint32_t tm_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + part * kTakeCols;
         // kGrad: what G is scaled by; kBack: what takes that away from its products
         float up = 1.f;
         if (kMode == kGrad) {
@@ -488,7 +508,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
             ok = __all_sync(0xffffffffu, mbar_wait(bar_acc + (i & 1), (i >> 1) & 1));
             if (!ok) break;
             tc_fence_after();
-            take_out<kMode, T>(P, x, tm_at + (i & 1) * kPairTile, x.m * kPairTile + in_tile, x.n * kPairTile + half * kHalfTile, n, up, tiles);
+            take_out<kMode, T>(P, x, tm_at + (i & 1) * kPairTile, x.m * kPairTile + in_tile, x.n * kPairTile + part * kTakeCols, n, up, tiles);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) leader_arrive(leaders(bar_taken + (i & 1)));
@@ -508,7 +528,7 @@ struct JoinParams {
     const int32_t* place;
     const int* header;
     float *loss, *lse;
-    int halves, rows;                                   // half tiles of the vocabulary; rows of a half tile's sums
+    int parts, rows;                                    // of the vocabulary; rows of a part's sums
     float scale;
 };
 constexpr int kJoinRows = 32, kJoinParts = 8;
@@ -526,14 +546,14 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) loss_join_kernel(const
     float2 sum = make_float2(-INFINITY, 0.f);
     if (row < n) {
 #pragma unroll 8
-        for (int j = y; j < P.halves; j += kJoinParts) sum = add(sum, __ldcg(P.part + static_cast<size_t>(j) * P.rows + row));
+        for (int j = y; j < P.parts; j += kJoinParts) sum = add(sum, __ldcg(P.part + static_cast<size_t>(j) * P.rows + row));
     }
     s[y][x] = sum;
     __syncthreads();
     if (y != 0 || row >= n) return;
 #pragma unroll
     for (int j = 1; j < kJoinParts; ++j)
-        if (j < P.halves) sum = add(sum, s[j][x]);
+        if (j < P.parts) sum = add(sum, s[j][x]);
     const float lse = fmaf(sum.x, P.scale, logf(sum.y));
     const int t = P.place[row];
     P.lse[t] = lse;
@@ -701,7 +721,7 @@ int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const v
     const LossPlan& p = L.plan;
     const int tv = ceil_div(c.V, kPairTile);
     if (int st = launch_products<kStats, __nv_bfloat16>(K_LOSS_STATS, static_cast<long long>(p.rows / kPairTile) * tv, L.maps, L.P, stream)) return st;
-    const JoinParams J{L.P.part, L.P.target, reinterpret_cast<const int32_t*>(L.base + p.place), L.P.header, loss, lse, ceil_div(c.V, kHalfTile), p.rows, L.P.scale};
+    const JoinParams J{L.P.part, L.P.target, reinterpret_cast<const int32_t*>(L.base + p.place), L.P.header, loss, lse, ceil_div(c.V, kTakeCols), p.rows, L.P.scale};
     LaunchScope ls_(K_LOSS_JOIN, stream);
     return check_cuda(launch_chained(loss_join_kernel, dim3(ceil_div(c.T, kJoinRows)), dim3(kJoinRows * kJoinParts), 0, stream, J), "loss: join launch");
 }

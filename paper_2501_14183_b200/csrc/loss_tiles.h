@@ -42,19 +42,27 @@ struct PairTile {
     bool dw;                                            // of d_w, not of d_h
 };
 // Tiles of rows x cols in groups of eight rows of tiles: what neighbouring pairs read at a time is some eight tiles of A and nine of B.
-VARDROP_TILES_FN void place_tile(PairTile& x, long long in, int rows, int cols) {
-    const long long width = static_cast<long long>(kGroupRows) * cols;
-    const int group = static_cast<int>(in / width), r = static_cast<int>(in - group * width), left = rows - group * kGroupRows, high = left < kGroupRows ? left : kGroupRows;
-    x.n = r / high;
-    x.m = group * kGroupRows + (r - x.n * high);
+// (32 bits throughout: there are fewer than 2^31 tiles and parts of them, and every role of a CTA divides for every tile.)
+VARDROP_TILES_FN void place_tile(PairTile& x, unsigned in, unsigned rows, unsigned cols) {
+    const unsigned width = kGroupRows * cols, group = in / width, r = in - group * width, left = rows - group * kGroupRows;
+    unsigned n, m;
+    if (left >= kGroupRows) {
+        n = r / kGroupRows;
+        m = r - n * kGroupRows;
+    } else {
+        n = r / left;
+        m = r - n * left;
+    }
+    x.n = static_cast<int>(n);
+    x.m = static_cast<int>(group * kGroupRows + m);
 }
 // Products of n tokens with `columns` rows of w, `deep` chunks each: by turns.
 struct LogitTiles {
     int tm, tv, deep, pair, pairs;
     VARDROP_TILES_FN bool at(int i, PairTile& x) const {
-        const long long t = pair + static_cast<long long>(i) * pairs;
-        if (t >= static_cast<long long>(tm) * tv) return false;
-        place_tile(x, t, tm, tv);
+        const unsigned t = static_cast<unsigned>(pair) + static_cast<unsigned>(i) * static_cast<unsigned>(pairs);
+        if (t >= static_cast<unsigned>(tm) * static_cast<unsigned>(tv)) return false;
+        place_tile(x, t, static_cast<unsigned>(tm), static_cast<unsigned>(tv));
         x.k0 = 0;
         x.k1 = deep;
         x.part = 0;
@@ -66,42 +74,43 @@ struct LogitTiles {
 struct GradTiles {
     int tm, tv, tc, ch, cw, pair, pairs;                // row tiles of d_h and of d_w, tiles of the channels, chunks of d_h's and d_w's contracted axes
     Splits splits;
-    long long all_1, all_2;
+    unsigned all_1, all_2;
     int mine, ahead, late, odd, extra;
     bool w_first;
     VARDROP_TILES_FN GradTiles(const SplitParams& S, int n, int columns, int pair_, int pairs_) {
         tm = tiles_of(n, kPairTile); tv = tiles_of(columns, kPairTile); tc = S.tn; ch = tiles_of(columns, kChunk); cw = tiles_of(n, kChunk);
         pair = pair_; pairs = pairs_;
         splits = splits_of(S, n);
-        const long long all_h = S.dh ? static_cast<long long>(tm) * tc * splits.dh : 0, all_w = S.dw ? static_cast<long long>(tv) * tc * splits.dw : 0;
+        const unsigned all_h = S.dh ? static_cast<unsigned>(tm) * tc * splits.dh : 0u, all_w = S.dw ? static_cast<unsigned>(tv) * tc * splits.dw : 0u;
         const int len_h = ch / splits.dh + kTileCost, len_w = cw / splits.dw + kTileCost;
         w_first = len_w > len_h;
         all_1 = w_first ? all_w : all_h;
         all_2 = w_first ? all_h : all_w;
-        const int longer = w_first ? len_w : len_h, shorter = w_first ? len_h : len_w, turns = static_cast<int>(all_1 / pairs);
-        odd = static_cast<int>(all_1 - static_cast<long long>(turns) * pairs);
+        const int longer = w_first ? len_w : len_h, shorter = w_first ? len_h : len_w, turns = static_cast<int>(all_1 / static_cast<unsigned>(pairs));
+        odd = static_cast<int>(all_1 - static_cast<unsigned>(turns) * static_cast<unsigned>(pairs));
         late = odd == 0 ? 0 : pairs - odd;
         extra = odd == 0 ? 0 : (longer + shorter / 2) / shorter;
         mine = turns + (pair < odd ? 1 : 0);
         ahead = pair < odd ? 0 : extra;
     }
     VARDROP_TILES_FN bool at(int i, PairTile& x) const {
-        long long t;
+        unsigned t;
         if (i < mine) {
-            t = pair + static_cast<long long>(i) * pairs;
+            t = static_cast<unsigned>(pair) + static_cast<unsigned>(i) * static_cast<unsigned>(pairs);
             x.dw = w_first;
         } else {
-            const int j = i - mine;
-            t = j < ahead ? static_cast<long long>(j) * late + (pair - odd) : static_cast<long long>(extra) * late + static_cast<long long>(j - ahead) * pairs + pair;
+            const unsigned j = static_cast<unsigned>(i - mine), first = static_cast<unsigned>(ahead);
+            t = j < first ? j * static_cast<unsigned>(late) + static_cast<unsigned>(pair - odd)
+                          : static_cast<unsigned>(extra) * static_cast<unsigned>(late) + (j - first) * static_cast<unsigned>(pairs) + static_cast<unsigned>(pair);
             if (t >= all_2) return false;
             x.dw = !w_first;
         }
-        const long long each = static_cast<long long>(x.dw ? tv : tm) * tc;
-        const int parts = x.dw ? splits.dw : splits.dh, chunks = x.dw ? cw : ch;
-        x.part = static_cast<int>(t / each);
-        place_tile(x, t - x.part * each, x.dw ? tv : tm, tc);
-        x.k0 = static_cast<int>(static_cast<long long>(chunks) * x.part / parts);
-        x.k1 = static_cast<int>(static_cast<long long>(chunks) * (x.part + 1) / parts);
+        const unsigned rows = static_cast<unsigned>(x.dw ? tv : tm), each = rows * static_cast<unsigned>(tc), parts = static_cast<unsigned>(x.dw ? splits.dw : splits.dh);
+        const unsigned chunks = static_cast<unsigned>(x.dw ? cw : ch), part = parts == 1 ? 0 : t / each;
+        x.part = static_cast<int>(part);
+        place_tile(x, t - part * each, rows, static_cast<unsigned>(tc));
+        x.k0 = parts == 1 ? 0 : static_cast<int>(chunks * part / parts);
+        x.k1 = static_cast<int>(parts == 1 ? chunks : chunks * (part + 1) / parts);
         return true;
     }
 };
