@@ -217,12 +217,12 @@ struct PairParams {
     int T, V, C;
     int v0, v1;                                         // the piece
     int pitch;                                          // columns of G
-    int add, whole, fp16, shares;                       // add: not the first piece; whole: the only one
+    int add, whole, plain, fp16, shares;                // add: not the first piece; whole: the only one; plain: rows are tokens as they are
     int sectors_h, sectors_w;                           // whether sixteen columns of d_h and of d_w are a sector
     float scale;
     const int32_t *label, *place;
     const float *row_lse, *factor, *most;
-    float2* part;                                       // [64 classes each, rows]
+    float2* part;                                       // [128 classes each, rows]
     float* target;
     void* g;
     float *dh, *dw;                                     // [parts, rows of tiles, C], [parts, columns of G, C]
@@ -254,7 +254,7 @@ __device__ __forceinline__ void load_sector(float (&v)[8], const void* p) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p) : "memory");
 }
 
-// What a thread does with 64 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
+// What a thread does with 128 columns of its row of a finished tile: `tm` is where they lie in tensor memory.
 template <int kMode, class T, class Tiles>
 __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x, uint32_t tm, int row, int col, int n, float up, const Tiles& tiles) {
     if constexpr (kMode == kStats) {
@@ -386,8 +386,8 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
 
 // warp 0          (of either CTA) loads: a ring of stages, 64 of the contracted axis for 128 rows of A and 128 of B
 // warp 1          of the leader: products
-// warps 4 to 19   (of either CTA) take a finished tile out, 64 columns of a row a thread, under the products of the next one (8 warps with 128 columns each took 2.6 us a tile, the products of 512
-//                 channels take 2.2)
+// warps 4 to 11   (of either CTA) take a finished tile out, 128 columns of a row a thread, under the products of the next one.  That takes 2.4 us where exponentials are taken (1.1 of them at their
+//                 unit's rate; sixteen warps with half as many columns take as long), the products of 512 channels 2.2: below that, this bounds a tile.
 template <int kMode, class T>
 __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __grid_constant__ LossMaps maps, const PairParams P) {
     extern __shared__ unsigned char smem_dyn[];
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
     chain_wait();
     chain_release();
 
-    const int n = __ldcg(P.header + kLossRows), columns = P.v1 - P.v0;
+    const int n = P.plain ? P.T : __ldcg(P.header + kLossRows), columns = P.v1 - P.v0;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const auto tiles = [&] {
         if constexpr (kMode == kBack) return GradTiles(P.split, n, columns, pair, pairs);
@@ -525,37 +525,64 @@ __global__ void __launch_bounds__(kPairThreads, 1) loss_products_kernel(const __
 struct JoinParams {
     const float2* part;
     const float* target;
-    const int32_t* place;
-    const int* header;
+    const int32_t *place, *labels;                      // labels: where rows are tokens as they are
+    int* header;
     float *loss, *lse;
-    int parts, rows;                                    // of the vocabulary; rows of a part's sums
+    int parts, rows, T, V;                              // parts of the vocabulary; rows of a part's sums
     float scale;
 };
-constexpr int kJoinRows = 32, kJoinParts = 8;
-__global__ void __launch_bounds__(kJoinRows * kJoinParts) loss_join_kernel(const JoinParams P) {
-    __shared__ float2 s[kJoinParts][kJoinRows];
+constexpr int kJoinRows = 32, kJoinWays = 32, kJoinBatch = 8;
+// A maximum and a sum of exponentials relative to it, with further ones added: those of a batch to their largest first.
+template <int kCount>
+__device__ __forceinline__ float2 joined(float2 sum, const float2 (&v)[kCount], float k) {
+    float top = sum.x;
+#pragma unroll
+    for (int e = 0; e < kCount; ++e) top = fmaxf(top, v[e].x);
+    float s = sum.y == 0.f ? 0.f : sum.y * exp2_fast((sum.x - top) * k);
+#pragma unroll
+    for (int e = 0; e < kCount; ++e) s += v[e].y == 0.f ? 0.f : v[e].y * exp2_fast((v[e].x - top) * k);       // (0: none)
+    return make_float2(top, s);
+}
+__global__ void __launch_bounds__(kJoinRows * kJoinWays) loss_join_kernel(const JoinParams P) {
+    __shared__ float2 s[kJoinWays][kJoinRows];
     chain_wait();
     chain_release();
-    const int n = __ldcg(P.header + kLossRows), x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * kJoinRows + x;
+    const int n = P.labels ? P.T : __ldcg(P.header + kLossRows), x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * kJoinRows + x;
     if (blockIdx.x * kJoinRows >= n) return;
     const float k = P.scale * kLog2e;
-    const auto add = [&](float2 a, float2 b) {
-        const float m = fmaxf(a.x, b.x);
-        return make_float2(m, (a.y == 0.f ? 0.f : a.y * exp2_fast((a.x - m) * k)) + b.y * exp2_fast((b.x - m) * k));
-    };
-    float2 sum = make_float2(-INFINITY, 0.f);
-    if (row < n) {
-#pragma unroll 8
-        for (int j = y; j < P.parts; j += kJoinParts) sum = add(sum, __ldcg(P.part + static_cast<size_t>(j) * P.rows + row));
+    const float2 none = make_float2(-INFINITY, 0.f);
+    float2 sum = none;
+    const float2* const from = P.part + min(row, n - 1);
+#pragma unroll 1
+    for (int j = y; j < P.parts; j += kJoinWays * kJoinBatch) {
+        float2 v[kJoinBatch];
+#pragma unroll
+        for (int u = 0; u < kJoinBatch; ++u) v[u] = __ldcg(from + static_cast<size_t>(min(j + u * kJoinWays, P.parts - 1)) * P.rows);
+#pragma unroll
+        for (int u = 0; u < kJoinBatch; ++u)
+            if (j + u * kJoinWays >= P.parts) v[u] = none;
+        sum = joined(sum, v, k);
     }
     s[y][x] = sum;
     __syncthreads();
     if (y != 0 || row >= n) return;
+    float2 v[kJoinWays - 1];
 #pragma unroll
-    for (int j = 1; j < kJoinParts; ++j)
-        if (j < P.parts) sum = add(sum, s[j][x]);
+    for (int j = 1; j < kJoinWays; ++j) v[j - 1] = s[j][x];
+    sum = joined(sum, v, k);
     const float lse = fmaf(sum.x, P.scale, logf(sum.y));
-    const int t = P.place[row];
+    int t = row;
+    if (P.labels) {
+        const int label = __ldg(P.labels + row);
+        if (label >= P.V) set_status(P.header, VARDROP_ERR_INVALID_ARG);
+        if (label < 0 || label >= P.V) {
+            P.lse[t] = 0.f;
+            P.loss[t] = 0.f;
+            return;
+        }
+    } else {
+        t = P.place[row];
+    }
     P.lse[t] = lse;
     P.loss[t] = lse - P.target[row];
 }
@@ -645,7 +672,7 @@ struct LossCall {
 };
 // Where things are, and the launches that both passes begin with.
 int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, const float* lse, const float* d_loss, float* loss, float* lse_out, void* d_h,
-               void* ws, bool backward, cudaStream_t stream) {
+               void* ws, bool backward, bool plain, cudaStream_t stream) {
     L.plan = loss_plan(c);
     const LossPlan& p = L.plan;
     // (a workspace begins on any 16 bytes; its header does so there, everything else behind the next multiple of 1024, plus 1024)
@@ -662,7 +689,7 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     RowsParams R{labels, lse, d_loss, loss, lse_out, static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), static_cast<uint4*>(d_h), reinterpret_cast<int32_t*>(base + p.place),
                  reinterpret_cast<int32_t*>(base + p.label), reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor),
                  reinterpret_cast<float*>(base + p.most), static_cast<int*>(ws), c.T, c.V, p.share, c.C / 8};
-    {
+    if (!plain) {
         LaunchScope ls_(K_LOSS_ROWS, stream);
         if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(p.shares), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st;
     }
@@ -670,7 +697,8 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     P = PairParams{};
     P.header = R.header;
     P.T = c.T; P.V = c.V; P.C = c.C; P.v0 = 0; P.v1 = c.V; P.pitch = p.piece; P.shares = p.shares; P.fp16 = fp16; P.scale = c.scale == 0.f ? 1.f : c.scale;
-    P.label = R.label; P.place = R.place; P.row_lse = R.row_lse; P.factor = R.factor; P.most = R.most;
+    P.plain = plain;
+    P.label = plain ? labels : R.label; P.place = R.place; P.row_lse = R.row_lse; P.factor = R.factor; P.most = R.most;
     P.part = reinterpret_cast<float2*>(base + p.part); P.target = reinterpret_cast<float*>(base + p.target);
     P.g = base + p.g; P.dh = reinterpret_cast<float*>(base + p.dh); P.dw = reinterpret_cast<float*>(base + p.dw); P.rows = p.rows;
     return VARDROP_OK;
@@ -717,18 +745,20 @@ size_t loss_workspace_bytes(const vardrop_loss_cfg& c) { return loss_plan(c).tot
 
 int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const vardrop_loss_cfg& c, float* loss, float* lse, void* ws, cudaStream_t stream) {
     LossCall L;
-    if (int st = loss_begin(L, h, w, labels, c, nullptr, nullptr, loss, lse, nullptr, ws, false, stream)) return st;
+    // One row of tiles, whatever has a label: tokens as they are, and a launch less (32 tokens, 1000 classes, 512 channels: 11.7 -> 9.3 us).  Rows without one come to nothing but themselves here.
+    const bool plain = c.T <= kPairTile;
+    if (int st = loss_begin(L, h, w, labels, c, nullptr, nullptr, loss, lse, nullptr, ws, false, plain, stream)) return st;
     const LossPlan& p = L.plan;
     const int tv = ceil_div(c.V, kPairTile);
     if (int st = launch_products<kStats, __nv_bfloat16>(K_LOSS_STATS, static_cast<long long>(p.rows / kPairTile) * tv, L.maps, L.P, stream)) return st;
-    const JoinParams J{L.P.part, L.P.target, reinterpret_cast<const int32_t*>(L.base + p.place), L.P.header, loss, lse, ceil_div(c.V, kTakeCols), p.rows, L.P.scale};
+    const JoinParams J{L.P.part, L.P.target, L.P.place, plain ? labels : nullptr, L.P.header, loss, lse, ceil_div(c.V, kTakeCols), p.rows, c.T, c.V, L.P.scale};
     LaunchScope ls_(K_LOSS_JOIN, stream);
-    return check_cuda(launch_chained(loss_join_kernel, dim3(ceil_div(c.T, kJoinRows)), dim3(kJoinRows * kJoinParts), 0, stream, J), "loss: join launch");
+    return check_cuda(launch_chained(loss_join_kernel, dim3(ceil_div(c.T, kJoinRows)), dim3(kJoinRows * kJoinWays), 0, stream, J), "loss: join launch");
 }
 
 int loss_bwd_launch(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg& c, void* d_h, void* d_w, void* ws, cudaStream_t stream) {
     LossCall L;
-    if (int st = loss_begin(L, h, w, labels, c, lse, d_loss, nullptr, nullptr, d_h, ws, true, stream)) return st;
+    if (int st = loss_begin(L, h, w, labels, c, lse, d_loss, nullptr, nullptr, d_h, ws, true, false, stream)) return st;
     return c.dtype == 1 ? loss_backward<__half>(L, c, d_h, d_w, stream) : loss_backward<__nv_bfloat16>(L, c, d_h, d_w, stream);
 }
 
