@@ -527,11 +527,13 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
 }
 
 // ---- few tokens and rows ----------------------------------------------------------------------------------------------------------
-// A CTA has a row (and up to 64 accesses of its columns) to itself: it looks through the indices 4096 at a time, lists the tokens that have the row, in order, and adds theirs up, every group of threads each
+// A CTA has a row (and up to 32 accesses of its columns) to itself: it looks through the indices 4096 at a time, lists the tokens that have the row, in order, and adds theirs up, every group of threads each
 // so-many-th token.
-constexpr int kScanEach = 16, kScanTokens = kEmbedThreads * kScanEach, kScanLanes = 64;
-constexpr long long kScanReads = 16ll << 20;    // indices that all CTAs read, out of L2
-constexpr int kScanMost = 16384, kScanPerRow = 64;      // tokens, and on the average of a row: one that has all of them is one CTA's work
+constexpr int kScanEach = 16, kScanTokens = kEmbedThreads * kScanEach, kScanLanes = 32;
+constexpr long long kScanReads = 16ll << 20, kScanCtas = 2368;      // indices that all CTAs read, out of L2; CTAs: two rounds of eight to an SM (29 tokens, 9217 rows of 637: 270 us with 92170 of them)
+// Tokens, and on the average of a row: a frequent one is one CTA's work.  4000 tokens, 300 rows of 512: evenly spread 6.4 us (sorted 19), frequencies like one over the rank 9.7 (19), a third of them in
+// one row 21 (20); 10272 tokens 13.5 (19), 23 (22) and 52 (29); 16384 tokens 18 (18), 34 (22) and 80 (33).  With 64 accesses of columns a CTA 9.5, 32 and 89 for 10272.
+constexpr int kScanMost = 12288, kScanPerRow = 64;
 struct ScanParams {
     SumParams sum;
     const int32_t* idx;
@@ -662,7 +664,7 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     int32_t* const tokens[2] = {reinterpret_cast<int32_t*>(base + w.tokens[0]), reinterpret_cast<int32_t*>(base + w.tokens[1])};
     SumParams P{d_out, nullptr, nullptr, d_table, reinterpret_cast<float*>(base + w.pieces), c.T, c.V, c.C, u.lanes, u.share, u.shares, c.accumulate, c.scale};
     const int slabs = (c.C / u.vec + kScanLanes - 1) / kScanLanes;
-    if (c.T <= kScanMost && c.T <= static_cast<long long>(kScanPerRow) * c.V && static_cast<long long>(c.T) * c.V * slabs <= kScanReads && slabs <= 65535) {
+    if (c.T <= kScanMost && c.T <= static_cast<long long>(kScanPerRow) * c.V && static_cast<long long>(c.T) * c.V * slabs <= kScanReads && static_cast<long long>(c.V) * slabs <= kScanCtas) {
         ScanParams N{P, idx, static_cast<int*>(ws)};
         if (N.sum.lanes > kScanLanes) N.sum.lanes = kScanLanes;
         LaunchScope ls_(K_EMBED_SCAN, stream);
