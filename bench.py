@@ -436,6 +436,66 @@ def layer_leg(torch, vd, path, w, peaks, barrier, args):
             "note": "kernel_us from a pass with the per-kernel event timer armed"}
 
 
+BINS, WIDTH = 4096, 4           # classes of the model leg's loss; width of its feed-forward block in channels of the stream
+
+
+def model_leg(torch, vd, path, w, peaks, barrier, args):
+    """Times what a model on kept tokens has the library do at its two ends and in its feed-forward blocks, with the backward passes: an embedding of its own for each kept variate (one selection for the batch,
+    -1 behind its last variate), a gated activation on the kept rows with its checkpoint in 8 bits, and the loss over binned values of the kept variates."""
+    device = path.dev[0]["x"].device
+    B, N, C = w.B, w.N, w.H * w.D
+    T, F = B * N, WIDTH * w.H * w.D
+    bf = dict(dtype=torch.bfloat16, device=device)
+    hcfg, scfg = vd.HashCfg(B, N, w.L, w.k, 0, 0, 0), vd.SelectCfg(1, N, 0, w.rate, SEED, STEP0)
+    keys, freqs, _ = vd.alloc_hash_outputs(hcfg, device=device)
+    sel = vd.alloc_select_outputs(scfg, device=device)
+    vd.vardrop_hash(path.dev[0]["x"], hcfg, keys, freqs, None, vd.alloc_ws(vd.vardrop_hash_workspace_bytes(hcfg), device))
+    vd.vardrop_select(keys, scfg, *(sel[n] for n in ("group_id", "group_offsets", "members", "n_groups", "sel_idx", "n_sel", "inv_idx")),
+                      vd.alloc_ws(vd.vardrop_select_workspace_bytes(scfg), device))
+    kept = int(sel["n_sel"].item())
+    g = torch.Generator(device=device)
+    g.manual_seed(SEED)
+    rand = lambda *shape, **kw: torch.randn(shape, generator=g, device=device).to(kw.get("dtype", torch.bfloat16))  # noqa: E731
+    idx = sel["sel_idx"].expand(B, N).reshape(-1).contiguous()
+    labels = torch.where(idx >= 0, torch.randint(0, BINS, (T,), generator=g, device=device, dtype=torch.int32), -1)
+    table, d_x = rand(N, C, dtype=torch.float32), rand(T, C)
+    x, d_table = torch.empty((T, C), **bf), torch.empty_like(table)
+    ecfg = vd.EmbedCfg(T, N, C, vd.DTYPES[torch.float32], vd.DTYPES[torch.bfloat16], 0, 1.0)
+    ab, d_y = rand(B, N, 2 * F), rand(B, N, F)
+    d_ab, y, again = torch.empty_like(ab), torch.empty_like(d_y), torch.empty_like(d_y)
+    acfg = vd.ActCfg(B, N, F, vd.DTYPES[torch.bfloat16], vd.ACT_SILU, 1, 1, 2 * F)
+    ckpt = vd.alloc_act_ckpt(acfg, device)
+    u, bins = rand(T, C), rand(BINS, C)
+    loss, lse, d_loss = torch.empty(T, device=device), torch.empty(T, device=device), torch.full((T,), 1.0 / (B * kept), device=device)
+    d_u, d_bins = torch.empty_like(u), torch.empty_like(bins)
+    lcfg = vd.LossCfg(T, BINS, C, vd.DTYPES[torch.bfloat16], C ** -0.5)
+    ews, lws = (vd.alloc_ws(n, device) for n in (vd.vardrop_embed_workspace_bytes(ecfg), vd.vardrop_loss_workspace_bytes(lcfg)))
+
+    def step(_):
+        vd.vardrop_embed_fwd(table, idx, ecfg, x, ews)
+        vd.vardrop_act_fwd(ab[..., :F], ab[..., F:], sel["n_sel"], acfg, y, ckpt)
+        vd.vardrop_loss_fwd(u, bins, labels, lcfg, loss, lse, lws)
+        vd.vardrop_loss_bwd(u, bins, labels, lse, d_loss, lcfg, d_u, d_bins, lws)
+        vd.vardrop_act_bwd(d_y, ckpt, sel["n_sel"], acfg, d_ab[..., :F], d_ab[..., F:], again)
+        vd.vardrop_embed_bwd(d_x, idx, ecfg, d_table, ews)
+
+    for i in range(3):
+        step(i)
+    n = max(3, min(args.steps, 20))
+    t = time_region(torch, step, n, barrier)
+    vd.vardrop_profile_enable(True)
+    for i in range(n):
+        step(i)
+    torch.cuda.synchronize()
+    per = {name: ms / n * 1e3 for name, (ms, cnt) in vd.vardrop_profile_read().items() if cnt}
+    vd.vardrop_profile_enable(False)
+    for ws in (ews, lws):
+        if vd.vardrop_ws_status(ws) != vd.OK:
+            raise RuntimeError("device status set by an operator of the model")
+    return {"ms_per_step": t["median"], "kept_tokens": B * kept, "loss_flops": 6 * B * kept * BINS * C, "kernel_us_per_step": per,
+            "note": "kernel_us_per_step from a pass with the per-kernel event timer armed"}
+
+
 def per_launch(per_kernel):
     """{kernel: (total ms, launches)} -> the same with zero-launch kernels dropped."""
     return {k: v for k, v in per_kernel.items() if v[1] > 0}
@@ -564,6 +624,7 @@ def run_gpu(args):
         targets = traffic_targets(torch, vd, inputs, dist_util, device, rank, peaks, barrier, w, path, kernels, off)
     pearson = pearson_leg(torch, vd, path, w, peaks, barrier, args) if args.pearson else None
     layer = layer_leg(torch, vd, path, w, peaks, barrier, args) if args.layer else None
+    model = model_leg(torch, vd, path, w, peaks, barrier, args) if args.model else None
     path.check_status()
 
     ms, ms_mean, ms_e2e = dist_util.max_over_ranks([t_main["median"], t_main["mean"], t_e2e["median"]], dist, device)
@@ -605,6 +666,8 @@ def run_gpu(args):
         line["pearson"] = pearson
     if layer is not None:
         line["layer"] = layer
+    if model is not None:
+        line["model"] = model
     print(json.dumps(line))
     if dist is not None:
         dist.destroy_process_group()
@@ -721,6 +784,7 @@ def main():
     ap.add_argument("--no-targets", action="store_true", help="skip the short Traffic-shaped pass behind the `targets` block")
     ap.add_argument("--pearson", action="store_true", help="also time the variate-redundancy check (Appendix A, Eq. 4) on the workload's windows")
     ap.add_argument("--layer", action="store_true", help="also time the operators around the attention: packed attention, norms, gradient clipping, on the workload's kept tokens")
+    ap.add_argument("--model", action="store_true", help="also time the operators at a model's ends and in its feed-forward blocks: embeddings, activation, loss, on the workload's kept tokens")
     args = ap.parse_args()
     if args.warmup < 3:
         args.warmup = 3

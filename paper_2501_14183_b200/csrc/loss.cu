@@ -1,6 +1,7 @@
 // Softmax cross entropy over a vocabulary, logits l = scale h w^T, without the logits in memory:
 //   lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,label;      G = g_t scale (exp(l_tv - lse_t) - [v = label]),  d_h = G w,  d_w = G^T h
 //
+// loss_count_kernel   labels of a share of many tokens.
 // loss_rows_kernel    tokens that have a label, one behind the other: positions, labels, and backward lse and the factor of their rows; where some have none, also their rows of h.  Only these take
 //                     part in any product.  Backward, zeros for the others' d_h.
 // loss_stats_kernel   products of 256 tokens x 256 rows of w; of each row of a tile the maximum and the sum of exponentials go to memory, and the label's logit.
@@ -47,7 +48,7 @@ struct LossPlan {
     int piece, pieces;          // columns of G
     int dh_rows, dw_parts;      // rows that all parts of d_h's products may take; parts of d_w's
     int share, shares;          // tokens of a CTA that finds labels
-    size_t place, label, lse, factor, target, most, packed, part, g, dh, dw, total;
+    size_t place, label, lse, factor, target, most, counts, packed, part, g, dh, dw, total;
 };
 constexpr int kLeastTokens = 16, kRowsGrid = 296;
 LossPlan loss_plan(const vardrop_loss_cfg& c) {
@@ -67,6 +68,7 @@ LossPlan loss_plan(const vardrop_loss_cfg& c) {
     const size_t T = c.T, C = c.C, rows = p.rows;
     p.place = take(4 * T); p.label = take(4 * T); p.lse = take(4 * T); p.factor = take(4 * T); p.target = take(4 * T);
     p.most = take(4ull * p.shares);
+    p.counts = take(4ull * p.shares);
     p.packed = take(2 * rows * C);
     const size_t shared = o;                            // forward and backward each have their own from here on
     p.part = take(8 * rows * (kPairTile / kTakeCols) * ceil_div(c.V, kPairTile));
@@ -88,6 +90,7 @@ struct RowsParams {
     uint4 *packed, *d_h;                                // d_h: zeros where there is no label; NULL: not wanted
     int32_t *place, *label;                             // token and label of a row
     float *row_lse, *factor, *most;                     // most: the largest factor of a share's tokens
+    int32_t* counts;                                    // labels of a share, where a launch ahead has counted them
     int* header;
     int T, V, share, vectors;                           // tokens of a CTA; 16-byte vectors of a row
 };
@@ -101,7 +104,27 @@ __device__ __forceinline__ float block_max(float v, float* shared) {
     for (int w = 0; w < kRowsWarps; ++w) v = fmaxf(v, shared[w]);
     return v;
 }
-// Every CTA counts the labels ahead of its tokens, and all of them, for itself: 64 KB out of L2 for 16384 tokens, and no launch or wait in between (one CTA for all took 27 us for 8192 tokens, this takes 4).
+__device__ __forceinline__ int has_label(int label, int V) { return label >= 0 && label < V ? 1 : 0; }
+// Labels of a share, for many tokens.
+__global__ void __launch_bounds__(kRowsThreads) loss_count_kernel(const RowsParams P) {
+    __shared__ int sums[kRowsWarps];
+    chain_wait();
+    chain_release();
+    const long long begin = static_cast<long long>(blockIdx.x) * P.share, end = min(static_cast<long long>(P.T), begin + P.share);
+    int n = 0;
+#pragma unroll 4
+    for (long long t = begin + threadIdx.x; t < end; t += kRowsThreads) n += has_label(__ldg(P.labels + t), P.V);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = n;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    n = 0;
+    for (int w = 0; w < kRowsWarps; ++w) n += sums[w];
+    P.counts[blockIdx.x] = n;
+}
+// Up to kCountHere tokens every CTA counts the labels ahead of its own, and all of them, for itself: 64 KB out of L2 for 16384 tokens, and no launch or wait in between (one CTA for all took 27 us for 8192
+// tokens, this takes 4); beyond, a launch counts each share's first (65536 tokens: 20 -> 12 us).
+constexpr int kCountHere = 16384;
 __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParams P) {
     __shared__ int sums[2][kRowsWarps], counts[kRowsWarps];
     __shared__ int rows[kRowsThreads];
@@ -110,20 +133,28 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
     chain_release();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long begin = static_cast<long long>(blockIdx.x) * P.share, end = min(static_cast<long long>(P.T), begin + P.share);
-    const auto live = [&](int label) { return label >= 0 && label < P.V ? 1 : 0; };
+    const auto live = [&](int label) { return has_label(label, P.V); };
     int ahead = 0, all = 0;
-    const int quads = P.T >> 2;
+    if (P.T > kCountHere) {
+        for (int i = tid; i < static_cast<int>(gridDim.x); i += kRowsThreads) {
+            const int k = __ldcg(P.counts + i);
+            all += k;
+            if (i < static_cast<int>(blockIdx.x)) ahead += k;
+        }
+    } else {
+        const int quads = P.T >> 2;
 #pragma unroll 8
-    for (int i = tid; i < quads; i += kRowsThreads) {
-        const int4 l = __ldg(reinterpret_cast<const int4*>(P.labels) + i);
-        const int k = live(l.x) + live(l.y) + live(l.z) + live(l.w);
-        all += k;
-        if (4ll * i < begin) ahead += k;                // (shares are multiples of four tokens)
-    }
-    for (int t = quads * 4 + tid; t < P.T; t += kRowsThreads) {
-        const int k = live(__ldg(P.labels + t));
-        all += k;
-        if (t < begin) ahead += k;
+        for (int i = tid; i < quads; i += kRowsThreads) {
+            const int4 l = __ldg(reinterpret_cast<const int4*>(P.labels) + i);
+            const int k = live(l.x) + live(l.y) + live(l.z) + live(l.w);
+            all += k;
+            if (4ll * i < begin) ahead += k;            // (shares are multiples of four tokens)
+        }
+        for (int t = quads * 4 + tid; t < P.T; t += kRowsThreads) {
+            const int k = live(__ldg(P.labels + t));
+            all += k;
+            if (t < begin) ahead += k;
+        }
     }
     all = __reduce_add_sync(0xffffffffu, all);
     ahead = __reduce_add_sync(0xffffffffu, ahead);
@@ -182,16 +213,27 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
         }
         if (!packs) continue;
         __syncthreads();
-        for (int k = warp; k < kRowsThreads && t0 + k < end; k += kRowsWarps) {
-            if (rows[k] < 0) {
-                if (P.d_h)
-                    for (int i = lane; i < P.vectors; i += 32) P.d_h[static_cast<size_t>(t0 + k) * P.vectors + i] = make_uint4(0u, 0u, 0u, 0u);
-                continue;
+        // four rows of a warp at a time, their loads without a branch
+        for (int k = warp; k < kRowsThreads && t0 + k < end; k += 4 * kRowsWarps) {
+            int to[4];
+            size_t from[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = k + u * kRowsWarps;
+                to[u] = at < kRowsThreads && t0 + at < end ? rows[at] : -2;
+                from[u] = static_cast<size_t>(t0 + at) * P.vectors;
             }
-            const uint4* const from = P.h + static_cast<size_t>(t0 + k) * P.vectors;
-            uint4* const to = P.packed + static_cast<size_t>(rows[k]) * P.vectors;
-#pragma unroll 4
-            for (int i = lane; i < P.vectors; i += 32) to[i] = __ldg(from + i);
+#pragma unroll 1
+            for (int i = lane; i < P.vectors; i += 32) {
+                uint4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = __ldg(P.h + (to[u] >= 0 ? from[u] + i : static_cast<size_t>(i)));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (to[u] >= 0) P.packed[static_cast<size_t>(to[u]) * P.vectors + i] = v[u];
+                    else if (to[u] == -1 && P.d_h) P.d_h[from[u] + i] = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
         }
     }
     if (!P.lse) return;
@@ -547,44 +589,39 @@ __global__ void __launch_bounds__(kJoinRows * kJoinWays) loss_join_kernel(const 
     __shared__ float2 s[kJoinWays][kJoinRows];
     chain_wait();
     chain_release();
-    const int n = P.labels ? P.T : __ldcg(P.header + kLossRows), x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * kJoinRows + x;
-    if (blockIdx.x * kJoinRows >= n) return;
+    const int n = P.labels ? P.T : __ldcg(P.header + kLossRows), x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const float k = P.scale * kLog2e;
     const float2 none = make_float2(-INFINITY, 0.f);
-    float2 sum = none;
-    const float2* const from = P.part + min(row, n - 1);
 #pragma unroll 1
-    for (int j = y; j < P.parts; j += kJoinWays * kJoinBatch) {
-        float2 v[kJoinBatch];
+    for (int first = blockIdx.x * kJoinRows; first < n; first += gridDim.x * kJoinRows) {
+        const int row = first + x;
+        float2 sum = none;
+        const float2* const from = P.part + min(row, n - 1);
+#pragma unroll 1
+        for (int j = y; j < P.parts; j += kJoinWays * kJoinBatch) {
+            float2 v[kJoinBatch];
 #pragma unroll
-        for (int u = 0; u < kJoinBatch; ++u) v[u] = __ldcg(from + static_cast<size_t>(min(j + u * kJoinWays, P.parts - 1)) * P.rows);
+            for (int u = 0; u < kJoinBatch; ++u) v[u] = __ldcg(from + static_cast<size_t>(min(j + u * kJoinWays, P.parts - 1)) * P.rows);
 #pragma unroll
-        for (int u = 0; u < kJoinBatch; ++u)
-            if (j + u * kJoinWays >= P.parts) v[u] = none;
-        sum = joined(sum, v, k);
-    }
-    s[y][x] = sum;
-    __syncthreads();
-    if (y != 0 || row >= n) return;
-    float2 v[kJoinWays - 1];
-#pragma unroll
-    for (int j = 1; j < kJoinWays; ++j) v[j - 1] = s[j][x];
-    sum = joined(sum, v, k);
-    const float lse = fmaf(sum.x, P.scale, logf(sum.y));
-    int t = row;
-    if (P.labels) {
-        const int label = __ldg(P.labels + row);
-        if (label >= P.V) set_status(P.header, VARDROP_ERR_INVALID_ARG);
-        if (label < 0 || label >= P.V) {
-            P.lse[t] = 0.f;
-            P.loss[t] = 0.f;
-            return;
+            for (int u = 0; u < kJoinBatch; ++u)
+                if (j + u * kJoinWays >= P.parts) v[u] = none;
+            sum = joined(sum, v, k);
         }
-    } else {
-        t = P.place[row];
+        __syncthreads();                                // the rows before are done
+        s[y][x] = sum;
+        __syncthreads();
+        if (y != 0 || row >= n) continue;
+        float2 v[kJoinWays - 1];
+#pragma unroll
+        for (int j = 1; j < kJoinWays; ++j) v[j - 1] = s[j][x];
+        sum = joined(sum, v, k);
+        const float lse = fmaf(sum.x, P.scale, logf(sum.y));
+        const int t = P.labels ? row : P.place[row], label = P.labels ? __ldg(P.labels + row) : 0;
+        if (label >= P.V) set_status(P.header, VARDROP_ERR_INVALID_ARG);
+        const bool there = label >= 0 && label < P.V;
+        P.lse[t] = there ? lse : 0.f;
+        P.loss[t] = there ? lse - P.target[row] : 0.f;
     }
-    P.lse[t] = lse;
-    P.loss[t] = lse - P.target[row];
 }
 
 // ---- gradients' last step -------------------------------------------------------------------------------------------------------
@@ -688,7 +725,11 @@ int loss_begin(LossCall& L, const void* h, const void* w, const int32_t* labels,
     }
     RowsParams R{labels, lse, d_loss, loss, lse_out, static_cast<const uint4*>(h), reinterpret_cast<uint4*>(base + p.packed), static_cast<uint4*>(d_h), reinterpret_cast<int32_t*>(base + p.place),
                  reinterpret_cast<int32_t*>(base + p.label), reinterpret_cast<float*>(base + p.lse), reinterpret_cast<float*>(base + p.factor),
-                 reinterpret_cast<float*>(base + p.most), static_cast<int*>(ws), c.T, c.V, p.share, c.C / 8};
+                 reinterpret_cast<float*>(base + p.most), reinterpret_cast<int32_t*>(base + p.counts), static_cast<int*>(ws), c.T, c.V, p.share, c.C / 8};
+    if (!plain && c.T > kCountHere) {
+        LaunchScope ls_(K_LOSS_COUNT, stream);
+        if (int st = check_cuda(launch_chained(loss_count_kernel, dim3(p.shares), dim3(kRowsThreads), 0, stream, R), "loss: count launch")) return st;
+    }
     if (!plain) {
         LaunchScope ls_(K_LOSS_ROWS, stream);
         if (int st = check_cuda(launch_chained(loss_rows_kernel, dim3(p.shares), dim3(kRowsThreads), 0, stream, R), "loss: rows launch")) return st;
@@ -753,7 +794,7 @@ int loss_fwd_launch(const void* h, const void* w, const int32_t* labels, const v
     if (int st = launch_products<kStats, __nv_bfloat16>(K_LOSS_STATS, static_cast<long long>(p.rows / kPairTile) * tv, L.maps, L.P, stream)) return st;
     const JoinParams J{L.P.part, L.P.target, L.P.place, plain ? labels : nullptr, L.P.header, loss, lse, ceil_div(c.V, kTakeCols), p.rows, c.T, c.V, L.P.scale};
     LaunchScope ls_(K_LOSS_JOIN, stream);
-    return check_cuda(launch_chained(loss_join_kernel, dim3(ceil_div(c.T, kJoinRows)), dim3(kJoinRows * kJoinWays), 0, stream, J), "loss: join launch");
+    return check_cuda(launch_chained(loss_join_kernel, dim3(ceil_div(c.T, kJoinRows) < 2 * sm_count() ? ceil_div(c.T, kJoinRows) : 2 * sm_count()), dim3(kJoinRows * kJoinWays), 0, stream, J), "loss: join launch");
 }
 
 int loss_bwd_launch(const void* h, const void* w, const int32_t* labels, const float* lse, const float* d_loss, const vardrop_loss_cfg& c, void* d_h, void* d_w, void* ws, cudaStream_t stream) {
