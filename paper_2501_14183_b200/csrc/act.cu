@@ -374,7 +374,7 @@ CkptLayout ckpt_layout(const vardrop_act_cfg& c) {
     return l;
 }
 
-constexpr int kActTasks = 2, kActPerSm = 8, kMaxGridY = 65535;      // kActPerSm: CTAs that an SM holds, and some more for instances of different sizes
+constexpr int kActTasks = 2, kActPerSm = 16, kMaxGridY = 65535;      // kActPerSm: twice or thrice what an SM holds, so that instances of different sizes even out (64 instances of 1 to 1000 rows 145 us with 8, 125 with 16)
 template <bool kBwd>
 int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cudaStream_t stream) {
     P.n_sel = n_sel;
@@ -385,7 +385,7 @@ int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cuda
     P.chunks = (c.C + 32 * kPer - 1) / (32 * kPer);
     const long long tasks = static_cast<long long>(c.N) * P.chunks;
     // Every row counts, and enough of them for four CTAs on every SM: two pieces to a warp (where they are vectors).  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their
-    // instance's pieces (a CTA for each few pieces of all rows, four of five of them without work: 172 of 862 kept rows of 32 instances, gelu of 2048, forward and backward, 52.7 us instead of 35).
+    // instance's pieces (a CTA for each few pieces of all rows, four of five of them without work: 172 of 862 kept rows of 32 instances, gelu of 2048, forward and backward, 52.7 us instead of 37).
     const bool many = !n_sel && wide && tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
     const int per = kActWarps * (many ? kActTasks : 1);
     const long long full = (tasks + per - 1) / per, held = (static_cast<long long>(sm_count()) * kActPerSm + c.B - 1) / c.B;

@@ -2,7 +2,7 @@
 //
 // embed_fwd_kernel      rows of the table, several tokens to a thread so that their loads overlap.  Bound: memory.
 // embed_count_kernel, embed_sort_kernel   tokens sorted by index, equal ones in their own order: a radix sort of (index, token) by digits of up to nine bits, so that 512 rows take one pass and 2^18
-//                       two.  Indices that name no row are sorted behind the last one.  embed_sort_small_kernel: all passes in shared memory.
+//                       two.  Indices that name no row are sorted behind the last one.  embed_place_kernel: up to 4096 tokens, by comparing all pairs (8192 take 14 us, two passes 13).
 //                       Beside the sorting, whose CTAs are few and whose steps are a chain of latencies, other CTAs of the same launches write zeros to the whole table.
 // embed_sum_kernel      even shares of the sorted tokens: whoever meets all tokens of a row writes it, pieces of a row go to the workspace.
 // embed_join_kernel     adds up the pieces, in order.
@@ -20,8 +20,8 @@ namespace vardrop {
 namespace {
 
 constexpr int kEmbedThreads = 256;
-// Tokens that a CTA ranks at a time.  Many tokens: small tiles, whose ranks are a shorter chain of steps over more CTAs.  Up to 4096 of them: one CTA for every pass.
-constexpr int kSortItems = 4, kSortThreads = 256, kSortTile = kSortThreads * kSortItems, kOneThreads = 1024, kOneTile = kOneThreads * kSortItems;
+// Tokens that a CTA ranks at a time: small tiles, whose ranks are a shorter chain of steps over more CTAs.
+constexpr int kSortItems = 4, kSortThreads = 256, kSortTile = kSortThreads * kSortItems;
 constexpr int kMaxDigitBits = 9, kMaxBins = 1 << kMaxDigitBits;
 constexpr int kMaxSortBlocks = 256;             // beyond, a CTA takes several tiles: the offsets of a digit are summed over all CTAs by each of them
 constexpr int kSumBatch = 8;                    // rows that a thread of the sums has on their way
@@ -145,11 +145,21 @@ __device__ __forceinline__ void write_zeros(const SortParams& P) {
 #pragma unroll 4
     for (size_t i = static_cast<size_t>(blockIdx.x - P.workers) * blockDim.x + threadIdx.x; i < P.zero_words; i += step) P.zeros[i] = make_uint4(0u, 0u, 0u, 0u);
 }
-// The key of token t: its index, V where it names no row.
-__device__ __forceinline__ int key_of(const SortParams& P, int t) {
-    const int v = __ldg(P.idx + t);
-    if (v >= P.V) set_status(P.status, VARDROP_ERR_INVALID_ARG);
-    return v < 0 || v >= P.V ? P.V : v;
+// The key of an index: V where it names no row.
+__device__ __forceinline__ int key_of(int v, int V) { return v < 0 || v >= V ? V : v; }
+// Keys of four tokens from t on, a multiple of four, kNoToken behind the last one.  `bad`: an index from V on among them.  (Loads without a branch between them, which would make a chain of several.)
+constexpr int kNoToken = 0x7fffffff;
+__device__ __forceinline__ int4 keys_of(const int32_t* idx, long long t, int T, int V, bool& bad) {
+    int4 v;
+    if (t + 4 <= T) {
+        v = __ldg(reinterpret_cast<const int4*>(idx + t));
+    } else {
+        const long long last = T - 1;
+        v = make_int4(__ldg(idx + min(t, last)), __ldg(idx + min(t + 1, last)), __ldg(idx + min(t + 2, last)), __ldg(idx + min(t + 3, last)));
+    }
+    const int n = t >= T ? 0 : T - t < 4 ? static_cast<int>(T - t) : 4;
+    bad |= (n > 0 && v.x >= V) || (n > 1 && v.y >= V) || (n > 2 && v.z >= V) || (n > 3 && v.w >= V);
+    return make_int4(n > 0 ? key_of(v.x, V) : kNoToken, n > 1 ? key_of(v.y, V) : kNoToken, n > 2 ? key_of(v.z, V) : kNoToken, n > 3 ? key_of(v.w, V) : kNoToken);
 }
 
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortParams P) {
@@ -164,7 +174,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortPar
     }
     __syncthreads();
     const long long begin = static_cast<long long>(blockIdx.x) * P.tiles_per_block * kSortTile, end = min(static_cast<long long>(P.T), begin + static_cast<long long>(P.tiles_per_block) * kSortTile);
-    for (long long t = begin + threadIdx.x; t < end; t += kSortThreads) atomicAdd(hist + (key_of(P, static_cast<int>(t)) & (bins - 1)), 1);
+    bool bad = false;
+#pragma unroll 1
+    for (long long t = begin + 4 * threadIdx.x; t < end; t += 4 * kSortThreads) {
+        const int4 k = keys_of(P.idx, t, P.T, P.V, bad);
+        if (k.x != kNoToken) atomicAdd(hist + (k.x & (bins - 1)), 1);
+        if (k.y != kNoToken) atomicAdd(hist + (k.y & (bins - 1)), 1);
+        if (k.z != kNoToken) atomicAdd(hist + (k.z & (bins - 1)), 1);
+        if (k.w != kNoToken) atomicAdd(hist + (k.w & (bins - 1)), 1);
+    }
+    if (bad) set_status(P.status, VARDROP_ERR_INVALID_ARG);
     __syncthreads();
     for (int d = threadIdx.x; d < bins; d += kSortThreads) {
         P.counts[static_cast<size_t>(blockIdx.x) * kMaxBins + d] = hist[d];
@@ -187,10 +206,17 @@ __device__ __forceinline__ void rank_tile(SortShared<kThreads>& S, int bins, con
     __syncwarp();
     int rank[kSortItems];
     uint32_t peers[kSortItems];
+    // Lanes of the same digit, by a vote a bit: __match_any_sync takes 7500 cycles for the 128 of them in a CTA of 32 warps, these 1000.
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-        const uint32_t active = __ballot_sync(0xffffffffu, there[i]);
-        peers[i] = __match_any_sync(0xffffffffu, digit[i]) & active;
+    for (int i = 0; i < kSortItems; ++i) peers[i] = __ballot_sync(0xffffffffu, there[i]);
+#pragma unroll
+    for (int b = 1; b < kMaxBins; b *= 2) {
+        if (b >= bins) break;
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            const uint32_t set = __ballot_sync(0xffffffffu, digit[i] & b);
+            peers[i] &= digit[i] & b ? set : ~set;
+        }
     }
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
@@ -202,12 +228,13 @@ __device__ __forceinline__ void rank_tile(SortShared<kThreads>& S, int bins, con
     __syncthreads();
 #pragma unroll
     for (int d = threadIdx.x; d < bins; d += kThreads) {
-        int total = 0;
-#pragma unroll 8
+        int total = 0, n[kThreads / 32];
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) n[w] = S.count[w][d];
+#pragma unroll
         for (int w = 0; w < kThreads / 32; ++w) {
-            const int n = S.count[w][d];
             S.count[w][d] = static_cast<uint16_t>(total);
-            total += n;
+            total += n[w];
         }
         S.total[d] = total;
     }
@@ -279,10 +306,17 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortPara
         bool there[kSortItems];
 #pragma unroll
         for (int i = 0; i < kSortItems; ++i) {
-            const long long t = t0 + 32 * i;
+            const long long t = t0 + 32 * i, at = min(t, static_cast<long long>(P.T) - 1);
             there[i] = t < P.T;
-            key[i] = !there[i] ? 0 : P.pass == 0 ? key_of(P, static_cast<int>(t)) : __ldcg(P.keys + t);
-            token[i] = !there[i] ? 0 : P.pass == 0 ? static_cast<int>(t) : __ldcg(P.tokens + t);
+            key[i] = __ldcg((P.pass == 0 ? P.idx : P.keys) + at);
+            token[i] = __ldcg((P.pass == 0 ? P.idx : P.tokens) + at);
+        }
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            if (P.pass == 0) {                  // (an index from V on has been reported by the count)
+                key[i] = key_of(key[i], P.V);
+                token[i] = static_cast<int>(t0 + 32 * i);
+            }
             digit[i] = (key[i] >> shift) & (bins - 1);
         }
         rank_tile(S, bins, digit, there, place);
@@ -305,54 +339,57 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const SortPara
     }
 }
 
-// Up to a tile of tokens: every pass by one CTA.
-__global__ void __launch_bounds__(kOneThreads) embed_sort_small_kernel(const SortParams P) {
-    extern __shared__ unsigned char smem_dyn[];
-    SortShared<kOneThreads>& S = *reinterpret_cast<SortShared<kOneThreads>*>(smem_dyn);
-    int* const keys = reinterpret_cast<int*>(smem_dyn + sizeof(SortShared<kOneThreads>));
-    int* const tokens = keys + kOneTile;
+// Few tokens: places by comparing all pairs of them over the whole GPU, with nothing to wait for in between.  A CTA has 32 tokens, one a lane; each of its warps compares them with an eighth of all.
+constexpr int kPlaceThreads = 256, kPlaceWarps = kPlaceThreads / 32, kPlaceMost = 4096;
+__global__ void __launch_bounds__(kPlaceThreads) embed_place_kernel(const SortParams P) {
+    __shared__ __align__(16) int keys[kPlaceMost];
+    __shared__ int counts[kPlaceWarps][32];
     chain_wait();
     chain_release();
     if (static_cast<int>(blockIdx.x) >= P.workers) {
         write_zeros(P);
         return;
     }
-    const int bins = 1 << P.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int t0 = warp * (32 * kSortItems) + lane;
-    int key[kSortItems], token[kSortItems], digit[kSortItems], place[kSortItems];
-    bool there[kSortItems];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * 32, quads = (P.T + 3) / 4;
+    bool bad = false;
+    int4 own_keys[kPlaceMost / 4 / kPlaceThreads];
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-        token[i] = t0 + 32 * i;
-        there[i] = token[i] < P.T;
-        key[i] = there[i] ? key_of(P, token[i]) : 0;
+    for (int i = 0; i < kPlaceMost / 4 / kPlaceThreads; ++i) own_keys[i] = keys_of(P.idx, 4 * min(static_cast<int>(threadIdx.x) + i * kPlaceThreads, quads - 1), P.T, P.V, bad);
+#pragma unroll
+    for (int i = 0; i < kPlaceMost / 4 / kPlaceThreads; ++i) {
+        const int q = threadIdx.x + i * kPlaceThreads;
+        if (q < quads) reinterpret_cast<int4*>(keys)[q] = own_keys[i];
     }
-#pragma unroll 1
-    for (int pass = 0; pass < P.passes; ++pass) {
-        const int shift = pass * P.bits;
-        if (tid < bins) S.base[tid] = 0;
-#pragma unroll
-        for (int i = 0; i < kSortItems; ++i) digit[i] = (key[i] >> shift) & (bins - 1);
-        rank_tile(S, bins, digit, there, place);
-        digit_bases(S, bins, S.total);
-        const bool last = pass + 1 == P.passes;
-#pragma unroll
-        for (int i = 0; i < kSortItems; ++i) {
-            if (!there[i]) continue;
-            const int to = place[i] + S.base[digit[i]];
-            (last ? P.keys_out : keys)[to] = key[i];
-            (last ? P.tokens_out : tokens)[to] = token[i];
-        }
-        __syncthreads();
-        if (last) break;
-#pragma unroll
-        for (int i = 0; i < kSortItems; ++i) {
-            if (!there[i]) continue;
-            key[i] = keys[t0 + 32 * i];
-            token[i] = tokens[t0 + 32 * i];
-        }
-        __syncthreads();
+    if (bad) set_status(P.status, VARDROP_ERR_INVALID_ARG);
+    __syncthreads();
+    const int mine = t0 + lane < P.T ? keys[t0 + lane] : 0;
+    const int begin = quads * warp / kPlaceWarps, end = quads * (warp + 1) / kPlaceWarps, own = t0 / 4;
+    const int4* const all = reinterpret_cast<const int4*>(keys);
+    int n = 0;
+    const int before = min(end, max(begin, own)), inside = min(end, max(begin, own + 8));
+#pragma unroll 4
+    for (int q = begin; q < before; ++q) {      // tokens ahead of these: equal keys come first
+        const int4 k = all[q];
+        n += (k.x <= mine) + (k.y <= mine) + (k.z <= mine) + (k.w <= mine);
     }
+    for (int q = before; q < inside; ++q) {
+        const int4 k = all[q];
+        const int t = 4 * q - t0;
+        n += (k.x < mine || (k.x == mine && t < lane)) + (k.y < mine || (k.y == mine && t + 1 < lane)) + (k.z < mine || (k.z == mine && t + 2 < lane)) + (k.w < mine || (k.w == mine && t + 3 < lane));
+    }
+#pragma unroll 4
+    for (int q = inside; q < end; ++q) {
+        const int4 k = all[q];
+        n += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+    }
+    counts[warp][lane] = n;
+    __syncthreads();
+    if (warp != 0 || t0 + lane >= P.T) return;
+    int place = 0;
+#pragma unroll
+    for (int w = 0; w < kPlaceWarps; ++w) place += counts[w][lane];
+    P.keys_out[place] = mine;
+    P.tokens_out[place] = t0 + lane;
 }
 
 // ---- sums -----------------------------------------------------------------------------------------------------------------------
@@ -680,41 +717,33 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     SortParams S{idx, nullptr, nullptr, keys[0], tokens[0], reinterpret_cast<int32_t*>(base + w.counts), static_cast<int*>(ws), c.T, c.V, s.bits, 0, s.passes, s.blocks, s.tiles_per_block, nullptr, 0, 0, nullptr, 0};
     // The table's zeros, in as many shares as launches sort.
     const size_t table_bytes = static_cast<size_t>(c.V) * c.C * dtype_bytes(c.dtype), words = c.accumulate ? 0 : table_bytes / 16;
-    const int sorts = c.T <= kOneTile ? 1 : s.passes + 1;
+    const int sorts = c.T <= kPlaceMost ? 1 : s.passes + 1;
     if (!c.accumulate && table_bytes % 16 != 0) S.tail = static_cast<unsigned char*>(d_table) + words * 16, S.tail_bytes = static_cast<int>(table_bytes % 16);
-    const auto launch_sort = [&](auto kernel, int workers, int threads, int smem, int which) {
+    const auto launch_sort = [&](auto kernel, int workers, int threads, int which) {
         const size_t from = words * which / sorts, to = words * (which + 1) / sorts;
         S.zeros = static_cast<uint4*>(d_table) + from;
         S.zero_words = to - from;
         S.workers = workers;
         const size_t most = static_cast<size_t>(sm_count()) * (2048 / threads), wanted = (S.zero_words + threads * 4 - 1) / (threads * 4) + (S.tail_bytes > 0 ? 1 : 0);
         const int fill = static_cast<int>(wanted < most ? wanted : most);
-        const cudaError_t e = launch_chained(kernel, dim3(workers + fill), dim3(threads), smem, stream, S);
+        const cudaError_t e = launch_chained(kernel, dim3(workers + fill), dim3(threads), 0, stream, S);
         S.tail_bytes = 0;
         return e;
     };
-    constexpr int kSmall = static_cast<int>(sizeof(SortShared<kOneThreads>)) + 2 * kOneTile * static_cast<int>(sizeof(int));
-    static thread_local int attr_dev = -1;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (attr_dev != dev) {
-        if (int st = check_cuda(cudaFuncSetAttribute(embed_sort_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmall), "embed: smem attribute")) return st;
-        attr_dev = dev;
-    }
     cudaError_t err;
     int at = 0;                                 // of the sorted arrays
-    if (c.T <= kOneTile) {
-        LaunchScope ls_(K_EMBED_SORT, stream);
-        err = launch_sort(embed_sort_small_kernel, 1, kOneThreads, kSmall, 0);
-        if (int st = check_cuda(err, "embed: sort launch")) return st;
+    if (c.T <= kPlaceMost) {
+        LaunchScope ls_(K_EMBED_PLACE, stream);
+        err = launch_sort(embed_place_kernel, (c.T + 31) / 32, kPlaceThreads, 0);
+        if (int st = check_cuda(err, "embed: place launch")) return st;
     } else {
-        { LaunchScope ls_(K_EMBED_COUNT, stream); err = launch_sort(embed_count_kernel, s.blocks, kSortThreads, 0, 0); }
+        { LaunchScope ls_(K_EMBED_COUNT, stream); err = launch_sort(embed_count_kernel, s.blocks, kSortThreads, 0); }
         if (int st = check_cuda(err, "embed: count launch")) return st;
         for (S.pass = 0; S.pass < s.passes; ++S.pass) {
             at = S.pass & 1;
             S.keys = keys[at ^ 1]; S.tokens = tokens[at ^ 1];
             S.keys_out = keys[at]; S.tokens_out = tokens[at];
-            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_sort(embed_sort_kernel, s.blocks, kSortThreads, 0, S.pass + 1); }
+            { LaunchScope ls_(K_EMBED_SORT, stream); err = launch_sort(embed_sort_kernel, s.blocks, kSortThreads, S.pass + 1); }
             if (int st = check_cuda(err, "embed: sort launch")) return st;
         }
     }

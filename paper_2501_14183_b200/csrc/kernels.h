@@ -13,7 +13,7 @@ namespace vardrop {
 enum KernelId {
     K_HASH = 0, K_SELECT_SMALL, K_SELECT_COUNT, K_SELECT_GROUP, K_SELECT_SAMPLE, K_ATTN_FWD, K_BWD_PREP, K_ATTN_BWD, K_BWD_CONVERT, K_PEARSON_NORM, K_PEARSON_MAX, K_GATHER_ROWS,
     K_SELECT_PLACE, K_SELECT_CLUSTER, K_PACKED_PLAN, K_PACKED_FWD, K_PACKED_TILE, K_PACKED_SHORT, K_PACKED_PREP, K_PACKED_BWD, K_PACKED_CONVERT, K_NORM_FWD, K_NORM_BWD, K_NORM_PARAMS, K_GRAD_NORM, K_GRAD_SCALE,
-    K_EMBED_FWD, K_EMBED_COUNT, K_EMBED_SORT, K_EMBED_SUM, K_EMBED_JOIN, K_EMBED_SCAN, K_ACT_FWD, K_ACT_BWD,
+    K_EMBED_FWD, K_EMBED_COUNT, K_EMBED_SORT, K_EMBED_SUM, K_EMBED_JOIN, K_EMBED_SCAN, K_EMBED_PLACE, K_ACT_FWD, K_ACT_BWD,
     K_LOSS_COUNT, K_LOSS_ROWS, K_LOSS_STATS, K_LOSS_JOIN, K_LOSS_GRAD, K_LOSS_BACK, K_LOSS_REST,
     K_COUNT
 };

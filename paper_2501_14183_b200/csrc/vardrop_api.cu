@@ -51,7 +51,7 @@ const char* const g_kernel_names[K_COUNT] = {"hash_kernel", "select_small_kernel
                                              "attn_fwd_kernel", "bwd_prep_kernel", "attn_bwd_kernel", "bwd_convert_kernel", "pearson_normalize_kernel",
                                              "pearson_max_kernel", "gather_rows_kernel", "select_place_kernel", "select_cluster_kernel", "packed_plan_kernel",
                                              "attn_packed_fwd_kernel", "attn_packed_tile_kernel", "packed_short_kernel", "packed_prep_kernel", "attn_packed_bwd_kernel", "packed_convert_kernel", "norm_fwd_kernel", "norm_bwd_kernel", "norm_params_kernel", "grad_norm_kernel", "grad_scale_kernel",
-                                             "embed_fwd_kernel", "embed_count_kernel", "embed_sort_kernel", "embed_sum_kernel", "embed_join_kernel", "embed_scan_kernel", "act_fwd_kernel", "act_bwd_kernel",
+                                             "embed_fwd_kernel", "embed_count_kernel", "embed_sort_kernel", "embed_sum_kernel", "embed_join_kernel", "embed_scan_kernel", "embed_place_kernel", "act_fwd_kernel", "act_bwd_kernel",
                                              "loss_count_kernel", "loss_rows_kernel", "loss_stats_kernel", "loss_join_kernel", "loss_grad_kernel", "loss_back_kernel", "loss_rest_kernel"};
 }  // namespace
 
