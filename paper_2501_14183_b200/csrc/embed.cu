@@ -44,17 +44,59 @@ SortPlan sort_plan(const vardrop_embed_cfg& c) {
     return p;
 }
 
+// Columns of a thread: kReps accesses of kVec.  Eight next to each other where rows are vectors of eight; narrower vectors of long rows in as many accesses as make eight, a row of threads apart, so that as many
+// bytes are on their way (65536 tokens of 1023 bf16 columns, backward: 121 us with one access, 95 with eight); short rows, and the lookup, which has several tokens on their way, one.
+struct Cols {
+    int c0, step, C;                            // first column, distance of the accesses, columns there are
+};
+template <int kVec, int kReps>
+__device__ __forceinline__ Cols cols_of(int slab, int lanes, int lane, int C) { return Cols{slab * lanes * kVec * kReps + lane * kVec, lanes * kVec, C}; }
+template <class T, int kVec, int kReps>
+struct Cells {
+    Pack<T, kVec> v[kReps];
+    __device__ __forceinline__ float at(int e) const { return to_float(v[e / kVec].e[e % kVec]); }
+    __device__ __forceinline__ void set(int e, float x) { v[e / kVec].e[e % kVec] = from_float<T>(x); }
+    // without a branch: column 0 where there is none
+    __device__ __forceinline__ void load(const T* row, const Cols& k) {
+#pragma unroll
+        for (int r = 0; r < kReps; ++r) {
+            const int c = k.c0 + r * k.step;
+            v[r] = load_pack<T, kVec>(row + (c < k.C ? c : 0));
+        }
+    }
+    __device__ __forceinline__ void store(T* row, const Cols& k) const {
+#pragma unroll
+        for (int r = 0; r < kReps; ++r) {
+            const int c = k.c0 + r * k.step;
+            if (c < k.C) store_pack(row + c, v[r]);
+        }
+    }
+};
+constexpr int kLongRow = 256;
+inline int accesses_of(int C) { return C < kLongRow ? 1 : 8 / row_vector(C); }
+inline int lanes_of(int C, int per) {
+    int lanes = 1;
+    while (lanes * per < C && lanes < kEmbedThreads) lanes *= 2;
+    return lanes;
+}
+template <class F>
+cudaError_t with_cells(int vec, int reps, F f) {
+    if (vec == 8) return f(VecSize<8>{}, VecSize<1>{});
+    if (reps == 1) return vec == 4 ? f(VecSize<4>{}, VecSize<1>{}) : vec == 2 ? f(VecSize<2>{}, VecSize<1>{}) : f(VecSize<1>{}, VecSize<1>{});
+    return vec == 4 ? f(VecSize<4>{}, VecSize<2>{}) : vec == 2 ? f(VecSize<2>{}, VecSize<4>{}) : f(VecSize<1>{}, VecSize<8>{});
+}
+
 // Threads of a row, and sorted tokens of a share: some 1024 threads for every SM, where there are tokens enough.
 struct SumPlan {
-    int vec, lanes, slabs, share, shares;
+    int vec, reps, lanes, slabs, share, shares;
 };
 SumPlan sum_plan(const vardrop_embed_cfg& c) {
     SumPlan p{};
     p.vec = row_vector(c.C);
-    const int vectors = c.C / p.vec;
-    p.lanes = 1;
-    while (p.lanes < vectors && p.lanes < kEmbedThreads) p.lanes *= 2;
-    p.slabs = (vectors + p.lanes - 1) / p.lanes;
+    p.reps = accesses_of(c.C);
+    const int per = p.vec * p.reps;
+    p.lanes = lanes_of(c.C, per);
+    p.slabs = (c.C + per * p.lanes - 1) / (per * p.lanes);
     const long long wanted = 148ll * 1024 / (static_cast<long long>(p.lanes) * p.slabs);      // (a constant, so that sums do not depend on the device)
     const long long share = (c.T + std::max(wanted, 1ll) - 1) / std::max(wanted, 1ll);
     p.share = static_cast<int>(std::min<long long>(std::max<long long>(share, kLeastShare), std::min(kMostShare, kSumTokens / (kEmbedThreads / p.lanes))));
@@ -401,24 +443,24 @@ struct SumParams {
     int T, V, C, lanes, share, shares, accumulate;
     float scale;
 };
+template <class Tab, int kVec, int kReps>
+__device__ __forceinline__ void row_there(Cells<Tab, kVec, kReps>& old, const SumParams& P, int v, const Cols& k) { old.load(static_cast<const Tab*>(P.d_table) + static_cast<size_t>(v) * P.C, k); }
 // `old`: what is there, where that is added to
-template <class Tab, int kVec>
-__device__ __forceinline__ void finish_row(const SumParams& P, int v, int c, const float (&sum)[kVec], const Pack<Tab, kVec>& old) {
-    Pack<Tab, kVec> to;
+template <class Tab, int kVec, int kReps>
+__device__ __forceinline__ void finish_row(const SumParams& P, int v, const Cols& k, const float (&sum)[kVec * kReps], const Cells<Tab, kVec, kReps>& old) {
+    Cells<Tab, kVec, kReps> to;
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) to.e[e] = from_float<Tab>(P.accumulate ? fmaf(sum[e], P.scale, to_float(old.e[e])) : sum[e] * P.scale);
-    store_pack(static_cast<Tab*>(P.d_table) + static_cast<size_t>(v) * P.C + c, to);
+    for (int e = 0; e < kVec * kReps; ++e) to.set(e, P.accumulate ? fmaf(sum[e], P.scale, old.at(e)) : sum[e] * P.scale);
+    to.store(static_cast<Tab*>(P.d_table) + static_cast<size_t>(v) * P.C, k);
 }
-template <class Tab, int kVec>
-__device__ __forceinline__ Pack<Tab, kVec> row_there(const SumParams& P, int v, int c) { return load_pack<Tab, kVec>(static_cast<const Tab*>(P.d_table) + static_cast<size_t>(v) * P.C + c); }
-template <class Tab, int kVec>
-__device__ __forceinline__ void finish_row(const SumParams& P, int v, int c, const float (&sum)[kVec]) {
-    Pack<Tab, kVec> old{};
-    if (P.accumulate) old = row_there<Tab, kVec>(P, v, c);
-    finish_row<Tab, kVec>(P, v, c, sum, old);
+template <class Tab, int kVec, int kReps>
+__device__ __forceinline__ void finish_row(const SumParams& P, int v, const Cols& k, const float (&sum)[kVec * kReps]) {
+    Cells<Tab, kVec, kReps> old{};
+    if (P.accumulate) row_there(old, P, v, k);
+    finish_row<Tab, kVec, kReps>(P, v, k, sum, old);
 }
 // kAdd: rows are added to, and what is there is on its way with the tokens of the batch (a row is read once for each of its tokens in it, out of L1 but for the first).
-template <class Tab, class Out, int kVec, bool kAdd>
+template <class Tab, class Out, int kVec, int kReps, bool kAdd>
 __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParams P) {
     chain_wait();
     chain_release();
@@ -435,38 +477,39 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParam
     if (threadIdx.x == 0) keys[0] = first_token > 0 ? __ldcg(P.keys + first_token - 1) : -1;
     if (threadIdx.x == 32) keys[held + 1] = first_token + held < P.T ? __ldcg(P.keys + first_token + held) : -1;
     __syncthreads();
-    const int share = blockIdx.x * groups + group, c = (blockIdx.y * P.lanes + lane) * kVec;
-    if (share >= P.shares || c >= P.C) return;
+    const int share = blockIdx.x * groups + group;
+    const Cols k = cols_of<kVec, kReps>(blockIdx.y, P.lanes, lane, P.C);
+    if (share >= P.shares || k.c0 >= P.C) return;
     const int begin = group * P.share, end = min(held, begin + P.share);
-    const Out* const d_out = static_cast<const Out*>(P.d_out) + c;
-    float* const pieces = P.pieces + static_cast<size_t>(share) * 2 * P.C + c;
+    const Out* const d_out = static_cast<const Out*>(P.d_out);
+    float* const pieces = P.pieces + static_cast<size_t>(share) * 2 * P.C;
     const int ahead = keys[begin], behind = keys[end + 1];
-    float sum[kVec];
-    Pack<Tab, kVec> old{};
+    float sum[kVec * kReps];
+    Cells<Tab, kVec, kReps> old{};
     int row = -1;                               // that `sum` is of
     bool first = true;                          // it is the share's first one
     auto leave = [&](bool at_end) {
         if (row < 0 || row == P.V) return;
         const bool from_ahead = first && row == ahead, goes_on = at_end && row == behind;
         if (!from_ahead && !goes_on) {
-            finish_row<Tab, kVec>(P, row, c, sum, old);
+            finish_row<Tab, kVec, kReps>(P, row, k, sum, old);
             return;
         }
-        Pack<float, kVec> to;
+        Cells<float, kVec, kReps> to;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) to.e[e] = sum[e];
-        store_pack(pieces + (from_ahead ? 0 : P.C), to);
+        for (int e = 0; e < kVec * kReps; ++e) to.set(e, sum[e]);
+        to.store(pieces + (from_ahead ? 0 : P.C), k);
     };
 #pragma unroll 1
     for (int i = begin; i < end; i += kBatch) {
-        Pack<Out, kVec> in[kBatch];
-        Pack<Tab, kVec> there[kAdd ? kBatch : 1];
+        Cells<Out, kVec, kReps> in[kBatch];
+        Cells<Tab, kVec, kReps> there[kAdd ? kBatch : 1];
         if (kAdd) {
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) there[u] = row_there<Tab, kVec>(P, min(keys[min(i + u, end - 1) + 1], P.V - 1), c);
+            for (int u = 0; u < kBatch; ++u) row_there(there[u], P, min(keys[min(i + u, end - 1) + 1], P.V - 1), k);
         }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(tokens[min(i + u, end - 1)]) * P.C);
+        for (int u = 0; u < kBatch; ++u) in[u].load(d_out + static_cast<size_t>(tokens[min(i + u, end - 1)]) * P.C, k);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (i + u >= end) break;
@@ -477,37 +520,38 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sum_kernel(const SumParam
                 row = key;
                 if (kAdd) old = there[u];
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) sum[e] = 0.f;
+                for (int e = 0; e < kVec * kReps; ++e) sum[e] = 0.f;
             }
             if (row == P.V) return;             // nothing but tokens without a row behind it (the row ahead is done)
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) sum[e] += to_float(in[u].e[e]);
+            for (int e = 0; e < kVec * kReps; ++e) sum[e] += in[u].at(e);
         }
     }
     leave(true);
 }
-// Rows in pieces: the share that a row begins in adds them up, a warp for 32 accesses of columns; of rows in many pieces (frequent tokens) all warps of the CTA, every eighth piece each.
+// Rows in pieces: the share that a row begins in adds them up, a warp for 256 columns; of rows in many pieces (frequent tokens) all warps of the CTA, every eighth piece each.
 constexpr int kJoinWarps = kEmbedThreads / 32, kFewPieces = 8;
-template <int kVec>
-__device__ __forceinline__ void add_pieces(const float* at, size_t step, int count, float (&sum)[kVec]) {
+template <int kVec, int kReps>
+__device__ __forceinline__ void add_pieces(const float* at, size_t step, int count, const Cols& k, float (&sum)[kVec * kReps]) {
 #pragma unroll 1
     for (int s = 0; s < count; s += kJoinBatch, at += kJoinBatch * step) {
-        Pack<float, kVec> piece[kJoinBatch];
+        Cells<float, kVec, kReps> piece[kJoinBatch];
 #pragma unroll
-        for (int u = 0; u < kJoinBatch; ++u) piece[u] = load_pack<float, kVec>(at + step * min(u, count - 1 - s));
+        for (int u = 0; u < kJoinBatch; ++u) piece[u].load(at + step * min(u, count - 1 - s), k);
 #pragma unroll
         for (int u = 0; u < kJoinBatch; ++u)
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) sum[e] += s + u < count ? piece[u].e[e] : 0.f;
+            for (int e = 0; e < kVec * kReps; ++e) sum[e] += s + u < count ? piece[u].at(e) : 0.f;
     }
 }
-template <class Tab, int kVec>
+template <class Tab, int kVec, int kReps>
 __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumParams P) {
     __shared__ int many[kJoinWarps][2];                     // row and number of pieces behind its first one, 0: none
-    __shared__ float parts[kJoinWarps][32 * kVec];
+    __shared__ float parts[kJoinWarps][32 * kVec * kReps];
     chain_wait();
     chain_release();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = blockIdx.x * kJoinWarps + warp, c = (blockIdx.y * 32 + lane) * kVec;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = blockIdx.x * kJoinWarps + warp;
+    const Cols k = cols_of<kVec, kReps>(blockIdx.y, 32, lane, P.C);
     int row = P.V, count = 0;
     if (share + 1 < P.shares) {
         const long long begin = static_cast<long long>(share) * P.share, end = begin + P.share;
@@ -524,18 +568,19 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
         } while (more == 32);
         count += __popc(__ballot_sync(0xffffffffu, begins(share + count + lane + 1)));
     }
-    const auto piece = [&](int s, int which) { return P.pieces + (static_cast<size_t>(s) * 2 + which) * P.C + (c < P.C ? c : 0); };
-    const auto own = [&](float (&sum)[kVec], int s) {
-        const Pack<float, kVec> v = load_pack<float, kVec>(piece(s, 1));
+    const auto piece = [&](int s, int which) { return P.pieces + (static_cast<size_t>(s) * 2 + which) * P.C; };
+    const auto own = [&](float (&sum)[kVec * kReps], int s) {
+        Cells<float, kVec, kReps> v;
+        v.load(piece(s, 1), k);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sum[e] = v.e[e];
+        for (int e = 0; e < kVec * kReps; ++e) sum[e] = v.at(e);
     };
     const size_t step = static_cast<size_t>(2) * P.C;
     if (row != P.V && count <= kFewPieces) {
-        float sum[kVec];
+        float sum[kVec * kReps];
         own(sum, share);
-        add_pieces<kVec>(piece(share + 1, 0), step, count, sum);
-        if (c < P.C) finish_row<Tab, kVec>(P, row, c, sum);
+        add_pieces<kVec, kReps>(piece(share + 1, 0), step, count, k, sum);
+        finish_row<Tab, kVec, kReps>(P, row, k, sum);
     }
     if (lane == 0) {
         many[warp][0] = row;
@@ -546,49 +591,50 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
     for (int w = 0; w < kJoinWarps; ++w) {
         const int pieces = many[w][1], s = blockIdx.x * kJoinWarps + w;
         if (pieces == 0) continue;                          // (of the whole CTA)
-        float sum[kVec] = {};
-        add_pieces<kVec>(piece(s + 1 + warp, 0), kJoinWarps * step, (pieces - warp + kJoinWarps - 1) / kJoinWarps, sum);
+        float sum[kVec * kReps] = {};
+        add_pieces<kVec, kReps>(piece(s + 1 + warp, 0), kJoinWarps * step, (pieces - warp + kJoinWarps - 1) / kJoinWarps, k, sum);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) parts[warp][e * 32 + lane] = sum[e];
+        for (int e = 0; e < kVec * kReps; ++e) parts[warp][e * 32 + lane] = sum[e];
         __syncthreads();
         if (warp == w) {
             own(sum, s);
 #pragma unroll
-            for (int k = 0; k < kJoinWarps; ++k)
+            for (int o = 0; o < kJoinWarps; ++o)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) sum[e] += parts[k][e * 32 + lane];
-            if (c < P.C) finish_row<Tab, kVec>(P, many[w][0], c, sum);
+                for (int e = 0; e < kVec * kReps; ++e) sum[e] += parts[o][e * 32 + lane];
+            finish_row<Tab, kVec, kReps>(P, many[w][0], k, sum);
         }
         __syncthreads();
     }
 }
 
 // ---- few tokens and rows ----------------------------------------------------------------------------------------------------------
-// A CTA has a row (and up to 32 accesses of its columns) to itself: it looks through the indices 4096 at a time, lists the tokens that have the row, in order, and adds theirs up, every group of threads each
+// A CTA has a row (and up to 256 of its columns) to itself: it looks through the indices 4096 at a time, lists the tokens that have the row, in order, and adds theirs up, every group of threads each
 // so-many-th token.
 constexpr int kScanEach = 16, kScanTokens = kEmbedThreads * kScanEach, kScanLanes = 32;
 constexpr long long kScanReads = 16ll << 20, kScanCtas = 2368;      // indices that all CTAs read, out of L2; CTAs: two rounds of eight to an SM (29 tokens, 9217 rows of 637: 270 us with 92170 of them)
 // Tokens, and on the average of a row: a frequent one is one CTA's work.  4000 tokens, 300 rows of 512: evenly spread 6.4 us (sorted 19), frequencies like one over the rank 9.7 (19), a third of them in
-// one row 21 (20); 10272 tokens 13.5 (19), 23 (22) and 52 (29); 16384 tokens 18 (18), 34 (22) and 80 (33).  With 64 accesses of columns a CTA 9.5, 32 and 89 for 10272.
+// one row 21 (20); 10272 tokens 13.5 (19), 23 (22) and 52 (29); 16384 tokens 18 (18), 34 (22) and 80 (33).  With 512 columns a CTA 9.5, 32 and 89 for 10272.
 constexpr int kScanMost = 12288, kScanPerRow = 64;
 struct ScanParams {
     SumParams sum;
     const int32_t* idx;
     int* status;
 };
-template <class Tab, class Out, int kVec>
+template <class Tab, class Out, int kVec, int kReps>
 __global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const ScanParams S) {
     __shared__ int list[kScanTokens], counts[kEmbedThreads / 32];
-    __shared__ float parts[kEmbedThreads * kVec];
+    __shared__ float parts[kEmbedThreads * kVec * kReps];
     chain_wait();
     chain_release();
     const SumParams& P = S.sum;
     const int tid = threadIdx.x, warp = tid >> 5, lane_of_warp = tid & 31, v = blockIdx.x;
-    const int groups = kEmbedThreads / P.lanes, group = tid / P.lanes, lane = tid & (P.lanes - 1), c = (blockIdx.y * P.lanes + lane) * kVec, at = c < P.C ? c : 0;
-    const Out* const d_out = static_cast<const Out*>(P.d_out) + at;
-    Pack<Tab, kVec> old{};
-    if (P.accumulate && group == 0) old = row_there<Tab, kVec>(P, v, at);
-    float sum[kVec] = {};
+    const int groups = kEmbedThreads / P.lanes, group = tid / P.lanes, lane = tid & (P.lanes - 1);
+    const Cols k = cols_of<kVec, kReps>(blockIdx.y, P.lanes, lane, P.C);
+    const Out* const d_out = static_cast<const Out*>(P.d_out);
+    Cells<Tab, kVec, kReps> old{};
+    if (P.accumulate && group == 0) row_there(old, P, v, k);
+    float sum[kVec * kReps] = {};
     int all = 0;
 #pragma unroll 1
     for (int t0 = 0; t0 < P.T; t0 += kScanTokens) {
@@ -615,8 +661,8 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const ScanPar
         int up = n;
 #pragma unroll
         for (int s = 1; s < 32; s *= 2) {
-            const int k = __shfl_up_sync(0xffffffffu, up, s);
-            if (lane_of_warp >= s) up += k;
+            const int ahead = __shfl_up_sync(0xffffffffu, up, s);
+            if (lane_of_warp >= s) up += ahead;
         }
         __syncthreads();                        // the list before is read
         if (lane_of_warp == 31) counts[warp] = up;
@@ -636,24 +682,24 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const ScanPar
         const int begin = (group - all % groups + groups) % groups;
 #pragma unroll 1
         for (int i = begin; i < found; i += kSumBatch * groups) {
-            Pack<Out, kVec> in[kSumBatch];
+            Cells<Out, kVec, kReps> in[kSumBatch];
 #pragma unroll
-            for (int u = 0; u < kSumBatch; ++u) in[u] = load_pack<Out, kVec>(d_out + static_cast<size_t>(list[min(i + u * groups, found - 1)]) * P.C);
+            for (int u = 0; u < kSumBatch; ++u) in[u].load(d_out + static_cast<size_t>(list[min(i + u * groups, found - 1)]) * P.C, k);
 #pragma unroll
             for (int u = 0; u < kSumBatch; ++u)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) sum[e] += i + u * groups < found ? to_float(in[u].e[e]) : 0.f;
+                for (int e = 0; e < kVec * kReps; ++e) sum[e] += i + u * groups < found ? in[u].at(e) : 0.f;
         }
         all += found;
     }
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) parts[e * kEmbedThreads + tid] = sum[e];
+    for (int e = 0; e < kVec * kReps; ++e) parts[e * kEmbedThreads + tid] = sum[e];
     __syncthreads();
-    if (group != 0 || c >= P.C || (P.accumulate && all == 0)) return;
+    if (group != 0 || k.c0 >= P.C || (P.accumulate && all == 0)) return;
     for (int g = 1; g < groups; ++g)
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sum[e] += parts[e * kEmbedThreads + g * P.lanes + lane];
-    finish_row<Tab, kVec>(P, v, c, sum, old);
+        for (int e = 0; e < kVec * kReps; ++e) sum[e] += parts[e * kEmbedThreads + g * P.lanes + lane];
+    finish_row<Tab, kVec, kReps>(P, v, k, sum, old);
 }
 
 }  // namespace
@@ -670,9 +716,8 @@ int embed_validate(const vardrop_embed_cfg& c) {
 size_t embed_workspace_bytes(const vardrop_embed_cfg& c) { return embed_layout(c).total; }
 
 int embed_fwd_launch(const void* table, const int32_t* idx, const vardrop_embed_cfg& c, void* out, void* ws, cudaStream_t stream) {
-    const SumPlan u = sum_plan(c);
-    const EmbedParams P{table, idx, out, static_cast<int*>(ws), c.T, c.V, c.C, u.lanes, c.scale};
-    const int groups = kEmbedThreads / u.lanes;
+    const int width = row_vector(c.C), lanes = lanes_of(c.C, width), groups = kEmbedThreads / lanes;
+    const EmbedParams P{table, idx, out, static_cast<int*>(ws), c.T, c.V, c.C, lanes, c.scale};
     // several tokens to a thread only where every SM still gets two CTAs
     const bool many = c.T >= 4ll * groups * 2 * sm_count();
     const long long per = static_cast<long long>(groups) * (many ? 4 : 1);
@@ -680,7 +725,7 @@ int embed_fwd_launch(const void* table, const int32_t* idx, const vardrop_embed_
     LaunchScope ls_(K_EMBED_FWD, stream);
     const cudaError_t err = with_dtype(c.dtype, [&](auto tab) {
         return with_dtype(c.out_dtype, [&](auto o) {
-            return with_vector(u.vec, [&](auto vec) {
+            return with_vector(width, [&](auto vec) {
                 using Tab = decltype(tab);
                 using Out = decltype(o);
                 constexpr int kVec = decltype(vec)::value;
@@ -700,15 +745,15 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
     int32_t* const keys[2] = {reinterpret_cast<int32_t*>(base + w.keys[0]), reinterpret_cast<int32_t*>(base + w.keys[1])};
     int32_t* const tokens[2] = {reinterpret_cast<int32_t*>(base + w.tokens[0]), reinterpret_cast<int32_t*>(base + w.tokens[1])};
     SumParams P{d_out, nullptr, nullptr, d_table, reinterpret_cast<float*>(base + w.pieces), c.T, c.V, c.C, u.lanes, u.share, u.shares, c.accumulate, c.scale};
-    const int slabs = (c.C / u.vec + kScanLanes - 1) / kScanLanes;
+    const int per = u.vec * u.reps, slabs = (c.C + per * kScanLanes - 1) / (per * kScanLanes);
     if (c.T <= kScanMost && c.T <= static_cast<long long>(kScanPerRow) * c.V && static_cast<long long>(c.T) * c.V * slabs <= kScanReads && static_cast<long long>(c.V) * slabs <= kScanCtas) {
         ScanParams N{P, idx, static_cast<int*>(ws)};
         if (N.sum.lanes > kScanLanes) N.sum.lanes = kScanLanes;
         LaunchScope ls_(K_EMBED_SCAN, stream);
         const cudaError_t err = with_dtype(c.dtype, [&](auto tab) {
             return with_dtype(c.out_dtype, [&](auto o) {
-                return with_vector(u.vec, [&](auto vec) {
-                    return launch_chained(embed_scan_kernel<decltype(tab), decltype(o), decltype(vec)::value>, dim3(c.V, slabs), dim3(kEmbedThreads), 0, stream, N);
+                return with_cells(u.vec, u.reps, [&](auto vec, auto reps) {
+                    return launch_chained(embed_scan_kernel<decltype(tab), decltype(o), decltype(vec)::value, decltype(reps)::value>, dim3(c.V, slabs), dim3(kEmbedThreads), 0, stream, N);
                 });
             });
         });
@@ -755,23 +800,23 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
         LaunchScope ls_(K_EMBED_SUM, stream);
         err = with_dtype(c.dtype, [&](auto tab) {
             return with_dtype(c.out_dtype, [&](auto o) {
-                return with_vector(u.vec, [&](auto vec) {
+                return with_cells(u.vec, u.reps, [&](auto vec, auto reps) {
                     using Tab = decltype(tab);
                     using Out = decltype(o);
-                    constexpr int kVec = decltype(vec)::value;
-                    return c.accumulate ? launch_chained(embed_sum_kernel<Tab, Out, kVec, true>, grid, dim3(kEmbedThreads), 0, stream, P)
-                                        : launch_chained(embed_sum_kernel<Tab, Out, kVec, false>, grid, dim3(kEmbedThreads), 0, stream, P);
+                    constexpr int kVec = decltype(vec)::value, kReps = decltype(reps)::value;
+                    return c.accumulate ? launch_chained(embed_sum_kernel<Tab, Out, kVec, kReps, true>, grid, dim3(kEmbedThreads), 0, stream, P)
+                                        : launch_chained(embed_sum_kernel<Tab, Out, kVec, kReps, false>, grid, dim3(kEmbedThreads), 0, stream, P);
                 });
             });
         });
     }
     if (int st = check_cuda(err, "embed: sum launch")) return st;
     if (u.shares == 1) return VARDROP_OK;
-    const dim3 join((u.shares + kJoinWarps - 1) / kJoinWarps, (c.C / u.vec + 31) / 32);
+    const dim3 join((u.shares + kJoinWarps - 1) / kJoinWarps, (c.C + 32 * per - 1) / (32 * per));
     {
         LaunchScope ls_(K_EMBED_JOIN, stream);
         err = with_dtype(c.dtype, [&](auto tab) {
-            return with_vector(u.vec, [&](auto vec) { return launch_chained(embed_join_kernel<decltype(tab), decltype(vec)::value>, join, dim3(kEmbedThreads), 0, stream, P); });
+            return with_cells(u.vec, u.reps, [&](auto vec, auto reps) { return launch_chained(embed_join_kernel<decltype(tab), decltype(vec)::value, decltype(reps)::value>, join, dim3(kEmbedThreads), 0, stream, P); });
         });
     }
     return check_cuda(err, "embed: join launch");
