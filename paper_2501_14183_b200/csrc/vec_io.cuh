@@ -11,7 +11,7 @@ template <class T, int N>
 struct alignas(N * sizeof(T) > 16 ? 16 : N * sizeof(T)) Pack {
     T e[N];
 };
-// (As whole words: copied as structs of elements, 16-bit ones took an access each.)
+// (As whole words: one access whatever the elements' type.)
 template <int kBytes>
 struct Word;
 template <> struct Word<2> { using type = uint16_t; };
