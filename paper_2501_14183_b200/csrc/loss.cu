@@ -763,9 +763,10 @@ int loss_backward(LossCall& L, const vardrop_loss_cfg& c, void* d_h, void* d_w, 
         // (how many parts there are is known on the device)
         if (int st = launch_products<kBack, T>(K_LOSS_BACK, (d_h ? tm * tc * kMostSplits : 0) + (d_w ? tv * tc * p.dw_parts : 0), L.maps, P, stream)) return st;
     }
-    const bool parts = d_w && p.dw_parts > 1;
-    if (!d_h && !parts) return VARDROP_OK;
-    const RestParams R{P.dh, P.dw, P.place, P.header, d_h, d_w, c.T, c.V, c.C, P.whole, d_h ? ceil_div(c.T, kRestRows) : 0, P.scale, P.split};
+    // what may be left in pieces or parts: small problems have neither, and a launch less
+    const bool rows = d_h && (p.pieces > 1 || may_split_dh(P.split)), parts = d_w && may_split_dw(P.split, c.T);
+    if (!rows && !parts) return VARDROP_OK;
+    const RestParams R{P.dh, P.dw, P.place, P.header, d_h, d_w, c.T, c.V, c.C, P.whole, rows ? ceil_div(c.T, kRestRows) : 0, P.scale, P.split};
     LaunchScope ls_(K_LOSS_REST, stream);
     return check_cuda(launch_chained(loss_rest_kernel<T>, dim3(R.h_blocks + (parts ? ceil_div(c.V, kRestRows) : 0)), dim3(kRestThreads), 0, stream, R), "loss: rest launch");
 }

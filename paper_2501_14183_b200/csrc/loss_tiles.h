@@ -12,7 +12,7 @@ namespace vardrop {
 constexpr int kPairTile = 256;                       // rows and columns of a tile
 constexpr int kChunk = 64;                           // of the contracted axis in a stage
 constexpr int kGroupRows = 8;                        // row tiles that neighbouring pairs share out among each other
-constexpr int kMostSplits = 32, kSplitChunks = 4;    // parts of a tile's contracted axis; chunks that one has at least
+constexpr int kMostSplits = 32, kSplitChunks = 8;    // parts of a tile's contracted axis; chunks that one has at least (2 us of products)
 constexpr int kTileCost = 3;                         // what a tile takes beside its chunks, in chunks
 
 VARDROP_TILES_FN int tiles_of(long long n, int each) { return static_cast<int>((n + each - 1) / each); }
@@ -36,6 +36,10 @@ VARDROP_TILES_FN Splits splits_of(const SplitParams& S, int n) {
     s.dw = within(cw / share, S.dw_parts);
     return s;
 }
+
+// Whether there can be more than one part, whatever has a label: of d_h, of d_w.
+VARDROP_TILES_FN bool may_split_dh(const SplitParams& S) { return S.piece / kChunk >= 2 * kSplitChunks; }
+VARDROP_TILES_FN bool may_split_dw(const SplitParams& S, int T) { return S.dw_parts > 1 && tiles_of(T, kChunk) >= 2 * kSplitChunks; }
 
 struct PairTile {
     int m, n, k0, k1, part;                             // tile; chunks of the contracted axis; which part of it that is

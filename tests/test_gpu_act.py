@@ -135,6 +135,38 @@ def test_widths(C, N):
     check(2, N, C, FP, GELU, False)
 
 
+def test_more_instances_than_a_grid_has_rows():
+    B = 70001
+    kept = torch.randint(0, 3, (B,)).tolist()
+    check(B, 2, 8, BF, SILU, True, kept=kept)
+    check(B, 1, 3, FP, RELU, False)
+
+
+@pytest.mark.parametrize("C,stride", [(45, 48), (45, 104), (40, 48), (264, 512)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_rows_with_gaps(C, stride, dtype):
+    """Rows further apart than they are long, in tensors of their own and in one for both branches."""
+    B, N = 3, 20
+    both = torch.full((B, N, 2 * stride), 5.0, dtype=dtype, device="cuda")
+    a, b = make(B, N, C, dtype, True)
+    d_y = make(B, N, C, dtype, False, seed=9)[0]
+    wide = vd.ActCfg(B, N, C, vd.DTYPES[dtype], SILU, 1, 0, 2 * stride)
+    va, vb = both[..., :C], both[..., stride:stride + C]
+    va.copy_(a)
+    vb.copy_(b)
+    grads = torch.full_like(both, 6.0)
+    y, again, ckpt = torch.empty_like(a), torch.empty_like(a), vd.alloc_act_ckpt(wide)
+    vd.vardrop_act_fwd(va, vb, None, wide, y, ckpt)
+    vd.vardrop_act_bwd(d_y, ckpt, None, wide, grads[..., :C], grads[..., stride:stride + C], again)
+    plain = vd.ActCfg(B, N, C, vd.DTYPES[dtype], SILU, 1, 0, 0)
+    want = [torch.empty_like(a) for _ in range(4)]
+    other = vd.alloc_act_ckpt(plain)
+    vd.vardrop_act_fwd(a, b, None, plain, want[0], other)
+    vd.vardrop_act_bwd(d_y, other, None, plain, want[1], want[2], want[3])
+    assert all(torch.equal(x, z) for x, z in zip((y, grads[..., :C], grads[..., stride:stride + C], again), want))
+    assert bool((grads[..., C:stride] == 6.0).all()) and bool((grads[..., stride + C:] == 6.0).all())
+
+
 @pytest.mark.parametrize("kept", [[0], [1], [29], [40], [0, 40, 7, 1, 39], [0, 0, 0, 0, 0]])
 def test_kept_rows(kept):
     check(5, 40, 72, BF, GELU, True, kept=kept)

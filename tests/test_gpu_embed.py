@@ -151,6 +151,25 @@ def test_indices_behind_the_table_are_none_and_reported():
     near(got, *wanted_rows(d, torch.where(idx < 10, idx, -1), 10, 1.0))
 
 
+@pytest.mark.parametrize("T,V", [(300, 20), (3000, 5000), (9000, 5000)])
+def test_indices_behind_the_table_in_every_form_of_the_sums(T, V):
+    idx, d = tokens(T, V, 3), normal((T, 16), BF, 2)
+    idx[::7] += V
+    cfg, ws = config(T, V, 16, FP)
+    got = torch.full((V, 16), float("nan"), device="cuda")
+    vd.vardrop_embed_bwd(d, idx, cfg, got, ws)
+    assert vd.ws_status(ws) == vd.ERR_INVALID_ARG
+    near(got, *wanted_rows(d, torch.where(idx < V, idx, -1), V, 1.0))
+
+
+@pytest.mark.parametrize("C", [255, 256, 257, 258, 260, 2050, 4097])
+def test_rows_of_several_accesses(C):
+    check_forward(200, 60, C, FP, BF, 1.5)
+    check_backward(9000, 700, C, FP, BF, 1.5, "skewed", 0.1)           # sorted
+    check_backward(3000, 4000, C, BF, BF, 1.5, "skewed", 0.1)          # placed
+    check_backward(500, 60, C, HF, HF, 1.0, "skewed", 0.1)             # looked through
+
+
 def test_a_table_behind_32_bit_offsets():
     V, C = (1 << 21) + 3, 1040                  # 2.2e9 elements
     w = torch.zeros((V, C), dtype=BF, device="cuda")

@@ -118,6 +118,13 @@ def test_pieces_and_splits(T, V, C):
     Case(T, V, C, HF, seed=2).check()
 
 
+def test_more_tokens_than_any_row_of_tiles_and_the_widest_channels():
+    Case(300000, 40, 8, gaps=0.9, seed=1).check()
+    Case(3, 5, 65536, seed=2).check()
+    for V, T in ((1000, 1000), (1100, 900), (900, 1100), (1030, 1030)):          # around where the gradients' products are split
+        Case(T, V, 64, gaps=0.1, seed=3).check()
+
+
 @pytest.mark.parametrize("scale,std", [(1.0, 30.0), (100.0, 3.0), (1e-6, 1.0), (1e4, 1.0), (0.0, 1.0)])
 def test_logits_near_and_far(scale, std):
     Case(200, 700, 64, scale=scale, std=std, gaps=0.2).check()

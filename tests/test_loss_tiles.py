@@ -19,6 +19,7 @@ extern "C" int gradients(int n, int columns, int piece, int C, int pairs, int gr
     const int tm = tiles_of(n, 256), tv = tiles_of(columns, 256), tc = S.tn, ch = tiles_of(columns, 64), cw = tiles_of(n, 64);
     if (s.dh < 1 || s.dw < 1 || s.dh > kMostSplits || s.dw > dw_parts) return 1;
     if (tm > 0 && static_cast<long long>(s.dh) * tm * 256 > dh_rows) return 2;
+    if ((s.dh > 1 && !may_split_dh(S)) || (s.dw > 1 && !may_split_dw(S, n))) return 10;      // (n tokens at least)
     std::vector<int> seen_h(static_cast<size_t>(tm) * tc * s.dh), seen_w(static_cast<size_t>(tv) * tc * s.dw), chunks_h(static_cast<size_t>(tm) * tc), chunks_w(static_cast<size_t>(tv) * tc);
     long long longest = 0, sum = 0;
     for (int pair = 0; pair < grid; ++pair) {
