@@ -189,19 +189,30 @@ __device__ __forceinline__ void write_zeros(const SortParams& P) {
 }
 // The key of an index: V where it names no row.
 __device__ __forceinline__ int key_of(int v, int V) { return v < 0 || v >= V ? V : v; }
-// Keys of four tokens from t on, a multiple of four, kNoToken behind the last one.  `bad`: an index from V on among them.  (Loads without a branch between them, which would make a chain of several.)
+// Keys of kCount vectors of four tokens, the numbers first, first + step, ..; kNoToken behind the last token.  `bad`: an index from V on among them.  (No branch stands between the loads, which
+// would make a chain of them: 500 tokens of eight columns took 9.9 us instead of 9.4, 4096 19.1 instead of 18.4.)
 constexpr int kNoToken = 0x7fffffff;
-__device__ __forceinline__ int4 keys_of(const int32_t* idx, long long t, int T, int V, bool& bad) {
-    int4 v;
-    if (t + 4 <= T) {
-        v = __ldg(reinterpret_cast<const int4*>(idx + t));
-    } else {
-        const long long last = T - 1;
-        v = make_int4(__ldg(idx + min(t, last)), __ldg(idx + min(t + 1, last)), __ldg(idx + min(t + 2, last)), __ldg(idx + min(t + 3, last)));
+template <int kCount>
+__device__ __forceinline__ void keys_of(const int32_t* idx, int first, int step, int T, int V, int4 (&k)[kCount], bool& bad) {
+    const int full = T >> 2, rest = T & 3, last = T - 1;
+    const int4 none = make_int4(kNoToken, kNoToken, kNoToken, kNoToken);
+    if (full > 0) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) k[i] = __ldg(reinterpret_cast<const int4*>(idx) + min(first + i * step, full - 1));
     }
-    const int n = t >= T ? 0 : T - t < 4 ? static_cast<int>(T - t) : 4;
-    bad |= (n > 0 && v.x >= V) || (n > 1 && v.y >= V) || (n > 2 && v.z >= V) || (n > 3 && v.w >= V);
-    return make_int4(n > 0 ? key_of(v.x, V) : kNoToken, n > 1 ? key_of(v.y, V) : kNoToken, n > 2 ? key_of(v.z, V) : kNoToken, n > 3 ? key_of(v.w, V) : kNoToken);
+    int4 tail = make_int4(__ldg(idx + min(4 * full, last)), __ldg(idx + min(4 * full + 1, last)), __ldg(idx + min(4 * full + 2, last)), 0);
+    bad |= (rest > 0 && tail.x >= V) || (rest > 1 && tail.y >= V) || (rest > 2 && tail.z >= V);
+    tail = make_int4(rest > 0 ? key_of(tail.x, V) : kNoToken, rest > 1 ? key_of(tail.y, V) : kNoToken, rest > 2 ? key_of(tail.z, V) : kNoToken, kNoToken);
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+        const int q = first + i * step;
+        if (q >= full) {
+            k[i] = q == full ? tail : none;
+        } else {
+            bad |= k[i].x >= V || k[i].y >= V || k[i].z >= V || k[i].w >= V;
+            k[i] = make_int4(key_of(k[i].x, V), key_of(k[i].y, V), key_of(k[i].z, V), key_of(k[i].w, V));
+        }
+    }
 }
 
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortParams P) {
@@ -219,11 +230,12 @@ __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const SortPar
     bool bad = false;
 #pragma unroll 1
     for (long long t = begin + 4 * threadIdx.x; t < end; t += 4 * kSortThreads) {
-        const int4 k = keys_of(P.idx, t, P.T, P.V, bad);
-        if (k.x != kNoToken) atomicAdd(hist + (k.x & (bins - 1)), 1);
-        if (k.y != kNoToken) atomicAdd(hist + (k.y & (bins - 1)), 1);
-        if (k.z != kNoToken) atomicAdd(hist + (k.z & (bins - 1)), 1);
-        if (k.w != kNoToken) atomicAdd(hist + (k.w & (bins - 1)), 1);
+        int4 k[1];
+        keys_of(P.idx, static_cast<int>(t >> 2), 1, P.T, P.V, k, bad);
+        if (k[0].x != kNoToken) atomicAdd(hist + (k[0].x & (bins - 1)), 1);
+        if (k[0].y != kNoToken) atomicAdd(hist + (k[0].y & (bins - 1)), 1);
+        if (k[0].z != kNoToken) atomicAdd(hist + (k[0].z & (bins - 1)), 1);
+        if (k[0].w != kNoToken) atomicAdd(hist + (k[0].w & (bins - 1)), 1);
     }
     if (bad) set_status(P.status, VARDROP_ERR_INVALID_ARG);
     __syncthreads();
@@ -395,8 +407,7 @@ __global__ void __launch_bounds__(kPlaceThreads) embed_place_kernel(const SortPa
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * 32, quads = (P.T + 3) / 4;
     bool bad = false;
     int4 own_keys[kPlaceMost / 4 / kPlaceThreads];
-#pragma unroll
-    for (int i = 0; i < kPlaceMost / 4 / kPlaceThreads; ++i) own_keys[i] = keys_of(P.idx, 4 * min(static_cast<int>(threadIdx.x) + i * kPlaceThreads, quads - 1), P.T, P.V, bad);
+    keys_of(P.idx, threadIdx.x, kPlaceThreads, P.T, P.V, own_keys, bad);
 #pragma unroll
     for (int i = 0; i < kPlaceMost / 4 / kPlaceThreads; ++i) {
         const int q = threadIdx.x + i * kPlaceThreads;
@@ -609,22 +620,24 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
 }
 
 // ---- few tokens and rows ----------------------------------------------------------------------------------------------------------
-// A CTA has a row (and up to 256 of its columns) to itself: it looks through the indices 4096 at a time, lists the tokens that have the row, in order, and adds theirs up, every group of threads each
-// so-many-th token.
-constexpr int kScanEach = 16, kScanTokens = kEmbedThreads * kScanEach, kScanLanes = 32;
+// A CTA has a row (and up to 256 of its columns) to itself: it looks through the indices, all on their way at once, lists the tokens that have the row, by thread and then in order, and adds theirs up, every group of
+// threads each so-many-th token.  (4096 indices a round, each round's sums before the next one's indices, took 13.6 us for the 10272 tokens below instead of 9.4.)
+constexpr int kScanLanes = 32, kScanQuads = 11, kScanFew = 4;      // vectors of four indices that a thread looks at, up to 11264 tokens (the list's 44 KB and the counts go without a request for more) and up to 4096
 constexpr long long kScanReads = 16ll << 20, kScanCtas = 2368;      // indices that all CTAs read, out of L2; CTAs: two rounds of eight to an SM (29 tokens, 9217 rows of 637: 270 us with 92170 of them)
-// Tokens, and on the average of a row: a frequent one is one CTA's work.  4000 tokens, 300 rows of 512: evenly spread 6.4 us (sorted 19), frequencies like one over the rank 9.7 (19), a third of them in
-// one row 21 (20); 10272 tokens 13.5 (19), 23 (22) and 52 (29); 16384 tokens 18 (18), 34 (22) and 80 (33).  With 512 columns a CTA 9.5, 32 and 89 for 10272.
-constexpr int kScanMost = 12288, kScanPerRow = 64;
+// Tokens, and on the average of a row: a frequent one is one CTA's work.  4000 tokens, 300 rows of 512: evenly spread 6.7 us (sorted 19), frequencies like one over the rank 10.3 (19), a third of them in
+// one row 21 (20); 10272 tokens 9.4 (19), 18 (22) and 43 (29).
+constexpr int kScanMost = 4 * kEmbedThreads * kScanQuads, kScanPerRow = 64;
 struct ScanParams {
     SumParams sum;
     const int32_t* idx;
     int* status;
 };
-template <class Tab, class Out, int kVec, int kReps>
+template <class Tab, class Out, int kVec, int kReps, int kQuads>
 __global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const ScanParams S) {
-    __shared__ int list[kScanTokens], counts[kEmbedThreads / 32];
-    __shared__ float parts[kEmbedThreads * kVec * kReps];
+    constexpr int kList = 4 * kEmbedThreads * kQuads, kParts = kEmbedThreads * kVec * kReps;
+    __shared__ int list[kList > kParts ? kList : kParts];
+    __shared__ int counts[kEmbedThreads / 32];
+    float* const parts = reinterpret_cast<float*>(list);           // behind the sums
     chain_wait();
     chain_release();
     const SumParams& P = S.sum;
@@ -632,66 +645,51 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_scan_kernel(const ScanPar
     const int groups = kEmbedThreads / P.lanes, group = tid / P.lanes, lane = tid & (P.lanes - 1);
     const Cols k = cols_of<kVec, kReps>(blockIdx.y, P.lanes, lane, P.C);
     const Out* const d_out = static_cast<const Out*>(P.d_out);
+    int4 idx[kQuads];
+    bool bad = false;
+    keys_of(S.idx, tid, kEmbedThreads, P.T, P.V, idx, bad);
     Cells<Tab, kVec, kReps> old{};
     if (P.accumulate && group == 0) row_there(old, P, v, k);
-    float sum[kVec * kReps] = {};
-    int all = 0;
-#pragma unroll 1
-    for (int t0 = 0; t0 < P.T; t0 += kScanTokens) {
-        const int mine = t0 + tid * kScanEach;
-        int idx[kScanEach];
-        if (mine + kScanEach <= P.T) {
+    uint64_t hits = 0;
 #pragma unroll
-            for (int q = 0; q < kScanEach / 4; ++q) {
-                const int4 x = __ldg(reinterpret_cast<const int4*>(S.idx + mine) + q);
-                idx[4 * q] = x.x; idx[4 * q + 1] = x.y; idx[4 * q + 2] = x.z; idx[4 * q + 3] = x.w;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < kScanEach; ++e) idx[e] = mine + e < P.T ? __ldg(S.idx + mine + e) : -1;
-        }
-        uint32_t hits = 0, bad = 0;
-#pragma unroll
-        for (int e = 0; e < kScanEach; ++e) {
-            hits |= (idx[e] == v ? 1u : 0u) << e;
-            bad |= idx[e] >= P.V ? 1u : 0u;
-        }
-        if (bad && v == 0) set_status(S.status, VARDROP_ERR_INVALID_ARG);
-        const int n = __popc(hits);
-        int up = n;
-#pragma unroll
-        for (int s = 1; s < 32; s *= 2) {
-            const int ahead = __shfl_up_sync(0xffffffffu, up, s);
-            if (lane_of_warp >= s) up += ahead;
-        }
-        __syncthreads();                        // the list before is read
-        if (lane_of_warp == 31) counts[warp] = up;
-        __syncthreads();
-        int place = up - n, found = 0;
-#pragma unroll
-        for (int w = 0; w < kEmbedThreads / 32; ++w) {
-            if (w < warp) place += counts[w];
-            found += counts[w];
-        }
-        while (hits) {
-            list[place++] = mine + __ffs(hits) - 1;
-            hits &= hits - 1;
-        }
-        __syncthreads();
-        // this group's tokens: those whose place among all of the row is its number, modulo the groups
-        const int begin = (group - all % groups + groups) % groups;
-#pragma unroll 1
-        for (int i = begin; i < found; i += kSumBatch * groups) {
-            Cells<Out, kVec, kReps> in[kSumBatch];
-#pragma unroll
-            for (int u = 0; u < kSumBatch; ++u) in[u].load(d_out + static_cast<size_t>(list[min(i + u * groups, found - 1)]) * P.C, k);
-#pragma unroll
-            for (int u = 0; u < kSumBatch; ++u)
-#pragma unroll
-                for (int e = 0; e < kVec * kReps; ++e) sum[e] += i + u * groups < found ? in[u].at(e) : 0.f;
-        }
-        all += found;
+    for (int q = 0; q < kQuads; ++q) {
+        const uint32_t four = (idx[q].x == v ? 1u : 0u) | (idx[q].y == v ? 2u : 0u) | (idx[q].z == v ? 4u : 0u) | (idx[q].w == v ? 8u : 0u);
+        hits |= static_cast<uint64_t>(four) << (4 * q);
     }
+    if (bad && v == 0) set_status(S.status, VARDROP_ERR_INVALID_ARG);
+    const int n = __popcll(hits);
+    int up = n;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+        const int ahead = __shfl_up_sync(0xffffffffu, up, s);
+        if (lane_of_warp >= s) up += ahead;
+    }
+    if (lane_of_warp == 31) counts[warp] = up;
+    __syncthreads();
+    int place = up - n, all = 0;
+#pragma unroll
+    for (int w = 0; w < kEmbedThreads / 32; ++w) {
+        if (w < warp) place += counts[w];
+        all += counts[w];
+    }
+    while (hits) {
+        const int b = __ffsll(static_cast<long long>(hits)) - 1;
+        list[place++] = 4 * (tid + (b >> 2) * kEmbedThreads) + (b & 3);
+        hits &= hits - 1;
+    }
+    __syncthreads();
+    float sum[kVec * kReps] = {};
+#pragma unroll 1
+    for (int i = group; i < all; i += kSumBatch * groups) {
+        Cells<Out, kVec, kReps> in[kSumBatch];
+#pragma unroll
+        for (int u = 0; u < kSumBatch; ++u) in[u].load(d_out + static_cast<size_t>(list[min(i + u * groups, all - 1)]) * P.C, k);
+#pragma unroll
+        for (int u = 0; u < kSumBatch; ++u)
+#pragma unroll
+            for (int e = 0; e < kVec * kReps; ++e) sum[e] += i + u * groups < all ? in[u].at(e) : 0.f;
+    }
+    __syncthreads();
 #pragma unroll
     for (int e = 0; e < kVec * kReps; ++e) parts[e * kEmbedThreads + tid] = sum[e];
     __syncthreads();
@@ -753,7 +751,12 @@ int embed_bwd_launch(const void* d_out, const int32_t* idx, const vardrop_embed_
         const cudaError_t err = with_dtype(c.dtype, [&](auto tab) {
             return with_dtype(c.out_dtype, [&](auto o) {
                 return with_cells(u.vec, u.reps, [&](auto vec, auto reps) {
-                    return launch_chained(embed_scan_kernel<decltype(tab), decltype(o), decltype(vec)::value, decltype(reps)::value>, dim3(c.V, slabs), dim3(kEmbedThreads), 0, stream, N);
+                    using Tab = decltype(tab);
+                    using Out = decltype(o);
+                    constexpr int kVec = decltype(vec)::value, kReps = decltype(reps)::value;
+                    const dim3 grid(c.V, slabs);
+                    return c.T <= 4 * kEmbedThreads * kScanFew ? launch_chained(embed_scan_kernel<Tab, Out, kVec, kReps, kScanFew>, grid, dim3(kEmbedThreads), 0, stream, N)
+                                                               : launch_chained(embed_scan_kernel<Tab, Out, kVec, kReps, kScanQuads>, grid, dim3(kEmbedThreads), 0, stream, N);
                 });
             });
         });

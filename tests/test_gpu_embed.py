@@ -226,6 +226,22 @@ def test_on_a_stream_of_its_own():
     near(got, *wanted_rows(d, idx, V, 1.0))
 
 
+@pytest.mark.parametrize("T", [1, 3, 4, 5, 4094, 4099, 11262, 11264, 11265, 12290])
+@pytest.mark.parametrize("spread", ["even", "skewed"])
+def test_the_last_tokens_of_a_short_call(T, spread):
+    """Numbers of tokens that are and are no multiple of four, up to both ends of the form that looks through all of them; the last one behind the table."""
+    V, C = 300, 48
+    check_backward(T, V, C, FP, BF, 1.5, spread, 0.3)
+    idx, d = tokens(T, V, 3, spread), normal((T, C), BF, 4)
+    idx[-1] = V
+    cfg, ws = config(T, V, C, FP, BF)
+    got = torch.full((V, C), float("nan"), device="cuda")
+    vd.vardrop_embed_bwd(d, idx, cfg, got, ws)
+    assert vd.ws_status(ws) == vd.ERR_INVALID_ARG
+    idx[-1] = -1
+    near(got, *wanted_rows(d, idx, V, 1.0))
+
+
 def test_binding_refuses_other_tensors():
     cfg, ws = config(8, 5, 16)
     w, idx, out = normal((5, 16), BF, 1), tokens(8, 5, 2), torch.empty((8, 16), dtype=BF, device="cuda")
