@@ -471,7 +471,8 @@ int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const 
  * Products of 16-bit operands with the tensor cores' fp32 sums, which lose about half a step for each 16 channels (lse is off by 4e-7 of itself at 512 channels and 1000 classes, 4e-6 at 4096
  * and two); G is rounded to 16 bits ahead of its products, times a number that keeps it in the type's range (a token whose |d_loss| is below 2^-24 of the largest one's
  * loses precision in fp16).  The weights of a token come from lse, whose 24 bits leave them open by about 2^-24 |lse| of themselves: with a finite |lse| above 2^16 the device status is VARDROP_ERR_UNSUPPORTED.
- * Values of a labelled token's row that are not finite reach its own loss and d_h, and d_w.  All results are bit-reproducible.
+ * Values of a labelled token's row that are not finite reach its own loss and d_h, and d_w.  A logit of -inf (a class switched off, by a weight of -inf in a channel that h has above 0) adds nothing to lse, and
+ * its G is 0; the token's d_h is NaN in channels where such a class's w is infinite (0 times infinity, by the formula).  All results are bit-reproducible.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
     int32_t T, V, C, dtype;

@@ -325,11 +325,12 @@ __device__ __forceinline__ void take_out(const PairParams& P, const PairTile& x,
 #pragma unroll
             for (int e = 4; e < 32; ++e) t[e & 3] = fmaxf(t[e & 3], r[e]);
             const float top = fmaxf(m, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
-            // differences of the sums ahead of the scale: exact however far from zero the logits are
-            float2 sum[2] = {make_float2(s * exp2_fast((m - top) * k), 0.f), make_float2(0.f, 0.f)};
+            // differences of the sums ahead of the scale: exact however far from zero the logits are; to zero where all of them so far are -inf (classes that are switched off), which then add nothing
+            const float base = top == -INFINITY ? 0.f : top;
+            float2 sum[2] = {make_float2(s * exp2_fast((m - base) * k), 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-                const float2 d = mul2(add2(make_float2(r[e], r[e + 1]), both(-top)), both(k));
+                const float2 d = mul2(add2(make_float2(r[e], r[e + 1]), both(-base)), both(k));
                 sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], make_float2(exp2_fast(d.x), exp2_fast(d.y)));
             }
             s = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
