@@ -469,8 +469,9 @@ int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const 
  * d_h         [T, C] out, zeros where there is no label; d_w   [V, C] out, every row written.  Either may be NULL (not wanted).
  * ws          scratch of vardrop_loss_workspace_bytes, for both calls.  Nothing is kept in it from one to the other.
  * Products of 16-bit operands with the tensor cores' fp32 sums, which lose about half a step for each 16 channels (lse is off by 4e-7 of itself at 512 channels and 1000 classes, 4e-6 at 4096
- * and two); G is rounded to 16 bits ahead of its products, times a number that keeps it in the type's range (a token whose |d_loss| is below 2^-24 of the largest one's
- * loses precision in fp16).  The weights of a token come from lse, whose 24 bits leave them open by about 2^-24 |lse| of themselves: with a finite |lse| above 2^16 the device status is VARDROP_ERR_UNSUPPORTED.
+ * and two); G is rounded to 16 bits ahead of its products, times a number that takes the largest |d_loss| to 16320.  bf16
+ * has the range for every entry; in fp16 an entry |d_loss| |p - [v = label]| below about 2^-28 of the largest |d_loss| has fewer bits, off by up to 2^-39 of it, and one below 2^-39 is taken as 0: with many
+ * classes, whose p are small, tokens of a much smaller |d_loss| than the largest keep their label's entry and lose of the others.  The weights of a token come from lse, whose 24 bits leave them open by about 2^-24 |lse| of themselves: with a finite |lse| above 2^16 the device status is VARDROP_ERR_UNSUPPORTED.
  * Values of a labelled token's row that are not finite reach its own loss and d_h, and d_w.  A logit of -inf (a class switched off, by a weight of -inf in a channel that h has above 0) adds nothing to lse, and
  * its G is 0; the token's d_h is NaN in channels where such a class's w is infinite (0 times infinity, by the formula).  All results are bit-reproducible.
  * ---------------------------------------------------------------------------------------------- */

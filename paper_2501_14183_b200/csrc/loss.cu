@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(const RowsParam
     top = block_max(top, most);
     if (tid == 0) P.most[blockIdx.x] = top;
 }
-// G is stored times what takes the largest factor to 16320 = 255 2^6: fp16 has room for it and for 2^-38 of it, and where all factors are alike, as in a mean, the largest entries, factor (p - 1) at the labels,
+// G is stored times what takes the largest factor to 16320 = 255 2^6: fp16 has room for it, has all its bits down to 2^-28 of it and its last one at 2^-38, and where all factors are alike, as in a mean, the largest entries, factor (p - 1) at the labels,
 // lose no bits but those of p (a power of two instead left d_w off by 2.5e-3 of its norm where rounding it alone leaves 1.6e-3).  A warp asks.
 __device__ __forceinline__ float scale_up(const float* most, int shares) {
     float top = 0.f;
