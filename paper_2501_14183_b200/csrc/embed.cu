@@ -1,8 +1,8 @@
 // Token embeddings: out[t] = scale table[idx[t]], and the table's gradient, d_table[v] (+)= scale sum of d_out[t] over the tokens with idx[t] = v.
 //
 // embed_fwd_kernel      rows of the table, several tokens to a thread so that their loads overlap.  Bound: memory.
-// embed_count_kernel, embed_sort_kernel   tokens sorted by index, equal ones in their own order: a radix sort of (index, token) by digits of up to nine bits, so that 512 rows take one pass and 2^18
-//                       two.  Indices that name no row are sorted behind the last one.  embed_place_kernel: up to 4096 tokens, by comparing all pairs (8192 take 14 us, two passes 13).
+// embed_count_kernel, embed_sort_kernel   tokens sorted by index, equal ones in their own order: a radix sort of (index, token) by digits of up to nine bits, so that up to 511 rows take one pass and up to
+//                       2^18 - 1 two: indices that name no row are sorted behind the last one, as one row more.  embed_place_kernel: up to 4096 tokens, by comparing all pairs (8192 take 14 us, two passes 13).
 //                       Beside the sorting, whose CTAs are few and whose steps are a chain of latencies, other CTAs of the same launches write zeros to the whole table.
 // embed_sum_kernel      even shares of the sorted tokens: whoever meets all tokens of a row writes it, pieces of a row go to the workspace.
 // embed_join_kernel     adds up the pieces, in order.
@@ -623,9 +623,16 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
 // A CTA has a row (and up to 256 of its columns) to itself: it looks through the indices, all on their way at once, lists the tokens that have the row, by thread and then in order, and adds theirs up, every group of
 // threads each so-many-th token.  (4096 indices a round, each round's sums before the next one's indices, took 13.6 us for the 10272 tokens below instead of 9.4.)
 constexpr int kScanLanes = 32, kScanQuads = 11, kScanFew = 4;      // vectors of four indices that a thread looks at, up to 11264 tokens (the list's 44 KB and the counts go without a request for more) and up to 4096
-constexpr long long kScanReads = 16ll << 20, kScanCtas = 2368;      // indices that all CTAs read, out of L2; CTAs: two rounds of eight to an SM (29 tokens, 9217 rows of 637: 270 us with 92170 of them)
-// Tokens, and on the average of a row: a frequent one is one CTA's work.  4000 tokens, 300 rows of 512: evenly spread 6.7 us (sorted 19), frequencies like one over the rank 10.3 (19), a third of them in
-// one row 21 (20); 10272 tokens 9.4 (19), 18 (22) and 43 (29).
+constexpr long long kScanReads = 16ll << 20, kScanCtas = 2368;      // indices that all CTAs read, out of L2; CTAs: sixteen for every SM (29 tokens, 9217 rows of 637: 270 us with 92170 of them), which
+//                                                                  holds two to six at a time (40 to 128 registers; four where many tokens meet vectors of eight)
+// Tokens, and on the average of a row.  A frequent row is one CTA's work, and how the tokens are spread is known on the device alone: the rule takes them as spread, and loses where most of them have one row.
+// us for bf16 into rows of 512 fp32, looked through (sorted):
+//   tokens, rows       evenly        like one over the rank   a third in one row   all in one row
+//    1000,  300      5.4 ( 9.7)           5.9 ( 9.4)              6.8 ( 9.8)        14.5 (11.7)
+//    4000,  300      6.5 (15.5)           9.9 (16.7)             19.5 (19.4)          46 (26)
+//   10272,  321      9.2 (18.5)          17.7 (21.7)               39 (27)           100 (46)
+//   11264,  176      9.2 (17.1)          21.4 (19.0)               42 (25)           108 (44)
+//   10272,  321, rows of 64:  8.4 (16.7)  9.2 (19.0)             14.3 (24.5)          31 (44)
 constexpr int kScanMost = 4 * kEmbedThreads * kScanQuads, kScanPerRow = 64;
 struct ScanParams {
     SumParams sum;
