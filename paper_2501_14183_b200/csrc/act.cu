@@ -4,7 +4,7 @@
 // act_fwd_kernel, act_bwd_kernel    32 values of a row share a power of two, the smallest 2^e with max |a| <= 448 2^e; a value is an e4m3 of that scale, so it is off by at most 2^-4 of itself (or
 //                                   2^(e-10) where it is below 2^(e-6)).  A power of two costs no rounding of its own, and what 8 bits stand for is exact in the tensor's type.
 //
-// Bound: memory (bf16, gated: 8 bytes and two codes a value forward, 2 and two codes in and 6 out backward); gelu's backward pass is near the instruction rate as well.
+// Bound: memory (bf16, gated: 4 bytes in, 2 and two codes out a value forward, 2 and two codes in and 6 out backward); gelu's backward pass is near the instruction rate as well.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -384,8 +384,8 @@ int act_launch(ActParams P, const vardrop_act_cfg& c, const int32_t* n_sel, cuda
     const bool wide = c.C % 8 == 0;             // (a stride is a multiple of 8 wherever there is one)
     P.chunks = (c.C + 32 * kPer - 1) / (32 * kPer);
     const long long tasks = static_cast<long long>(c.N) * P.chunks;
-    // Every row counts, and enough of them for four CTAs on every SM: two pieces to a warp (where they are vectors).  Kept rows are known on the device only: as many CTAs as the SMs hold at a time, which go through their
-    // instance's pieces (a CTA for each few pieces of all rows, four of five of them without work: 172 of 862 kept rows of 32 instances, gelu of 2048, forward and backward, 52.7 us instead of 37).
+    // Every row counts, and enough of them for four CTAs on every SM: two pieces to a warp (where they are vectors).  Kept rows are known on the device only: two or three times as many CTAs as the SMs hold, which go through their
+    // instance's pieces by strides of the grid (a CTA for each few pieces of all rows, four of five of them without work: 172 of 862 kept rows of 32 instances, gelu of 2048, forward and backward, 52.7 us instead of 37).
     const bool many = !n_sel && wide && tasks * c.B >= 4ll * kActTasks * kActWarps * sm_count();
     const int per = kActWarps * (many ? kActTasks : 1);
     const long long full = (tasks + per - 1) / per, held = (static_cast<long long>(sm_count()) * kActPerSm + c.B - 1) / c.B;

@@ -624,7 +624,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_join_kernel(const SumPara
 // threads each so-many-th token.  (4096 indices a round, each round's sums before the next one's indices, took 13.6 us for the 10272 tokens below instead of 9.4.)
 constexpr int kScanLanes = 32, kScanQuads = 11, kScanFew = 4;      // vectors of four indices that a thread looks at, up to 11264 tokens (the list's 44 KB and the counts go without a request for more) and up to 4096
 constexpr long long kScanReads = 16ll << 20, kScanCtas = 2368;      // indices that all CTAs read, out of L2; CTAs: sixteen for every SM (29 tokens, 9217 rows of 637: 270 us with 92170 of them), which
-//                                                                  holds two to six at a time (40 to 128 registers; four where many tokens meet vectors of eight)
+//                                                                  holds two to six at a time (40 to 128 registers; three or four where many tokens meet vectors of eight)
 // Tokens, and on the average of a row.  A frequent row is one CTA's work, and how the tokens are spread is known on the device alone: the rule takes them as spread, and loses where most of them have one row.
 // us for bf16 into rows of 512 fp32, looked through (sorted):
 //   tokens, rows       evenly        like one over the rank   a third in one row   all in one row
