@@ -36,7 +36,6 @@ constexpr size_t kPieceBytes = 256u << 20;           // of G; larger pieces make
 constexpr int kLeastPiece = 1024;
 constexpr size_t kPartBytes = 64u << 20;             // of parts of a gradient's products
 constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 enum LossWord { kLossRows = 16, kLossInverse };      // words of the workspace's header: labelled tokens; the inverse of what G is scaled by
 

@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "vec_io.cuh"
 
 namespace vardrop {
 
@@ -488,7 +489,6 @@ static int overlap_check(const char* call, const Rows* ins, int n_ins, const Row
     }
     return VARDROP_OK;
 }
-static size_t elem_bytes(int dtype) { return dtype == 2 ? 4 : 2; }
 
 size_t vardrop_embed_workspace_bytes(const vardrop_embed_cfg* cfg) {
     if (!cfg || embed_validate(*cfg) != VARDROP_OK) return 0;
@@ -503,8 +503,8 @@ int vardrop_embed_fwd(const void* table, const int32_t* idx, const vardrop_embed
     VD_CHECK(check_ptr(out, "out", true));
     VD_CHECK(check_ws(ws, ws_bytes, kWsHeaderBytes));
     const size_t C = cfg->C;
-    const Rows ins[] = {flat(table, cfg->V * C, elem_bytes(cfg->dtype), "table"), flat(idx, cfg->T, 4, "idx"), flat(ws, kWsHeaderBytes, 1, "ws")};
-    const Rows outs[] = {flat(out, cfg->T * C, elem_bytes(cfg->out_dtype), "out")};
+    const Rows ins[] = {flat(table, cfg->V * C, dtype_bytes(cfg->dtype), "table"), flat(idx, cfg->T, 4, "idx"), flat(ws, kWsHeaderBytes, 1, "ws")};
+    const Rows outs[] = {flat(out, cfg->T * C, dtype_bytes(cfg->out_dtype), "out")};
     VD_CHECK(overlap_check("embed", ins, 3, outs, 1, false));
     return embed_fwd_launch(table, idx, *cfg, out, ws, static_cast<cudaStream_t>(stream));
 }
@@ -517,8 +517,8 @@ int vardrop_embed_bwd(const void* d_out, const int32_t* idx, const vardrop_embed
     VD_CHECK(check_ptr(d_table, "d_table", true));
     VD_CHECK(check_ws(ws, ws_bytes, embed_workspace_bytes(*cfg)));
     const size_t C = cfg->C;
-    const Rows ins[] = {flat(d_out, cfg->T * C, elem_bytes(cfg->out_dtype), "d_out"), flat(idx, cfg->T, 4, "idx")};
-    const Rows outs[] = {flat(d_table, cfg->V * C, elem_bytes(cfg->dtype), "d_table"), flat(ws, embed_workspace_bytes(*cfg), 1, "ws")};
+    const Rows ins[] = {flat(d_out, cfg->T * C, dtype_bytes(cfg->out_dtype), "d_out"), flat(idx, cfg->T, 4, "idx")};
+    const Rows outs[] = {flat(d_table, cfg->V * C, dtype_bytes(cfg->dtype), "d_table"), flat(ws, embed_workspace_bytes(*cfg), 1, "ws")};
     VD_CHECK(overlap_check("embed", ins, 2, outs, 2, false));
     return embed_bwd_launch(d_out, idx, *cfg, d_table, ws, static_cast<cudaStream_t>(stream));
 }
@@ -543,7 +543,7 @@ int vardrop_act_fwd(const void* a, const void* b, const int32_t* n_sel, const va
     VD_CHECK(check_ptr(n_sel, "n_sel", false));
     VD_CHECK(check_ptr(y, "y", true));
     if (ckpt) VD_CHECK(check_ckpt(ckpt, ckpt_bytes, *cfg));
-    const size_t rows = static_cast<size_t>(cfg->B) * cfg->N, C = cfg->C, stride = cfg->stride ? cfg->stride : C, size = elem_bytes(cfg->dtype);
+    const size_t rows = static_cast<size_t>(cfg->B) * cfg->N, C = cfg->C, stride = cfg->stride ? cfg->stride : C, size = dtype_bytes(cfg->dtype);
     const Rows ins[] = {{a, rows, C, stride, size, "a"}, {b, rows, C, stride, size, "b"}, flat(n_sel, cfg->S > 1 ? cfg->S : 1, 4, "n_sel")};
     const Rows outs[] = {{y, rows, C, C, size, "y"}, flat(ckpt, ckpt ? act_ckpt_bytes(*cfg) : 0, 1, "ckpt")};
     VD_CHECK(overlap_check("act", ins, 3, outs, 2, true));
@@ -560,7 +560,7 @@ int vardrop_act_bwd(const void* d_y, const void* ckpt, size_t ckpt_bytes, const 
     if ((d_b != nullptr) != (cfg->gated != 0)) return fail(VARDROP_ERR_INVALID_ARG, "act: gated=%d and d_b %s", cfg->gated, d_b ? "given" : "NULL");
     VD_CHECK(check_ptr(d_b, "d_b", false));
     VD_CHECK(check_ptr(y, "y", false));
-    const size_t rows = static_cast<size_t>(cfg->B) * cfg->N, C = cfg->C, stride = cfg->stride ? cfg->stride : C, size = elem_bytes(cfg->dtype);
+    const size_t rows = static_cast<size_t>(cfg->B) * cfg->N, C = cfg->C, stride = cfg->stride ? cfg->stride : C, size = dtype_bytes(cfg->dtype);
     const Rows ins[] = {{d_y, rows, C, C, size, "d_y"}, flat(ckpt, act_ckpt_bytes(*cfg), 1, "ckpt"), flat(n_sel, cfg->S > 1 ? cfg->S : 1, 4, "n_sel")};
     const Rows outs[] = {{d_a, rows, C, stride, size, "d_a"}, {d_b, rows, C, stride, size, "d_b"}, {y, rows, C, C, size, "y"}};
     VD_CHECK(overlap_check("act", ins, 3, outs, 3, true));
