@@ -434,7 +434,8 @@ int vardrop_embed_bwd(const void* d_out, const int32_t* idx, const vardrop_embed
  * is past the type's largest, the one below), so a^ is within 2^-4 |a|, or 2^(e-10) where |a| is below 2^(e-6).  Infinities and NaN come back as NaN, each in its own place.
  *
  * cfg (host)  B, N, C (C <= 2^20; B N < 2^31; N ceil(C / 32) <= 2^31); dtype of a, b, y and their gradients: 0 bf16, 1 fp16, 2 fp32; kind 0 relu, 1 gelu, 2 silu; gated 0 or 1; S as in vardrop_attn_cfg;
- *             stride: elements from row to row of a, b, d_a and d_b (0: C; otherwise a multiple of 8 and at least C: both halves of one projection [B, N, 2 C]).
+ *             stride: elements from row to row of a, b, d_a and d_b (0: C; otherwise a multiple of 8 and at least C: both halves of one projection [B, N, 2 C],
+ *             where the second half begins on 16 bytes: C a multiple of 8 in 16 bits, of 4 in fp32).
  * a, b        [B, N, C] with that stride; b is NULL exactly when gated = 0.
  * n_sel       [S] int32 on the device: rows from n_sel on (of an instance, S = B, or of every one) are not read, and left as they are in all outputs; NULL: every row counts.
  * y           [B, N, C] out; backward it may be NULL (not wanted).
